@@ -1,7 +1,6 @@
 // C ABI of the library: argument checks on the host, then kernel launches on
 // the caller's stream.  See include/resq.h for the contract of every entry.
 #include <hip/hip_runtime.h>
-#include <hip/hip_ext.h>
 #include <stdint.h>
 
 #include <atomic>
@@ -16,6 +15,7 @@
 #include "resq_project.hip.h"
 #include "resq_hadamard.hip.h"
 #include "resq_headproj.hip.h"
+#include "resq_launch.h"
 #include "resq_layout.h"
 #include "resq_quantize.hip.h"
 
@@ -26,8 +26,6 @@ namespace {
 constexpr int64_t kMaxK = 1 << 20;
 constexpr int64_t kMaxLoWidth = 1 << 20;  // 1680 * (K - r) < 2^31 (widened low sums)
 constexpr int64_t kMaxHiWidth = 132104;  // 128 * 127 * r < 2^31 (stored asymmetric codes reach -128)
-
-inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 inline int shape_ok(int64_t rows, int64_t K, int64_t r) {
     if (rows < 1 || K < 1 || K > kMaxK || r < 0 || r > K) return 0;
@@ -45,19 +43,6 @@ inline bool blocks_overlap(const void* a, int64_t rows_a, int64_t pitch_a, int64
     if (pitch_a != pitch_b) return true;
     const int64_t shift = (d % pitch_a + pitch_a) % pitch_a;  // b's first column, counted from a's, modulo the row
     return shift < width_a || shift + width_b > pitch_a;
-}
-
-inline int launch_status() { return hipGetLastError() == hipSuccess ? RESQ_OK : RESQ_ERR_HIP; }
-
-// One-shot timing request of resq_time_next_kernel(): the next main kernel this
-// thread launches is bracketed by the two events (exact kernel start and end).
-thread_local hipEvent_t g_time_start = nullptr, g_time_stop = nullptr;
-
-template <typename... KArgs, typename... Args>
-inline void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t lds, hipStream_t st, Args... args) {
-    hipEvent_t e0 = g_time_start, e1 = g_time_stop;
-    g_time_start = g_time_stop = nullptr;
-    hipExtLaunchKernelGGL(kernel, grid, block, lds, st, e0, e1, 0, args...);
 }
 
 // ---- built-in scratch area of resq_sym_eig_static -------------------------------------------
@@ -352,8 +337,7 @@ int resq_quantize_act_asym(const void* x, int64_t ldx, int64_t M, int64_t K, int
 }
 
 static bool kv_cache_shape_ok(int64_t rows, int64_t d_head, int64_t r) {
-    return rows >= 0 && rows <= 0x7FFFFFFF && d_head >= 8 && d_head <= 512 && d_head % 8 == 0 && r >= 0 &&
-           r <= d_head && r % 8 == 0;
+    return rows >= 0 && rows <= 0x7FFFFFFF && kv_head_ok(d_head, r);
 }
 
 size_t resq_kv_cache_row_bytes(int64_t d_head, int64_t r) {

@@ -17,6 +17,8 @@
 
 #include <type_traits>
 
+#include "resq_lanes.hip.h"
+
 namespace resq {
 
 constexpr int kHadThreads = 256;
@@ -31,32 +33,9 @@ struct HadArgs {
     float scale;  // 1 / sqrt(b)
 };
 
-// value of lane (l ^ MASK): data-parallel-primitive moves inside a row of 16
-// lanes where the pattern has one (quad permutes for 1 and 2, a rotation by 8),
-// the swizzle unit inside 32 lanes, a general shuffle across the two halves
-template <int MASK>
-__device__ __forceinline__ float lane_xor(float x) {
-    const int xi = __float_as_int(x);
-    int r;
-    if constexpr (MASK == 1) r = __builtin_amdgcn_update_dpp(xi, xi, 0xB1, 0xF, 0xF, false);       // quad_perm [1,0,3,2]
-    else if constexpr (MASK == 2) r = __builtin_amdgcn_update_dpp(xi, xi, 0x4E, 0xF, 0xF, false);  // quad_perm [2,3,0,1]
-    else if constexpr (MASK == 8) r = __builtin_amdgcn_update_dpp(xi, xi, 0x128, 0xF, 0xF, false); // row_ror:8
-    else if constexpr (MASK == 4) r = __builtin_amdgcn_ds_swizzle(xi, 0x101F);                     // xor 4 within 32
-    else if constexpr (MASK == 16) r = __builtin_amdgcn_ds_swizzle(xi, 0x401F);                    // xor 16 within 32
-    else r = __float_as_int(__shfl_xor(x, MASK));
-    return __int_as_float(r);
-}
-
 // ---- pieces shared with the fused transform + quantize kernel ------------------
 // A lane holds 8 consecutive columns (16 bytes of bf16); column bits 0..2 select
 // the register, bits 3..8 the lane.
-
-__device__ __forceinline__ void unpack8_bf16(const uint4& w, float (&v)[8]) {
-    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        v[j] = __uint_as_float((j & 1) ? (ww[j >> 1] & 0xFFFF0000u) : (ww[j >> 1] << 16));
-}
 
 // butterfly stages of column bits 0..2 (those below log2b)
 __device__ __forceinline__ void wht_in_lane(float (&v)[8], int log2b) {
@@ -95,8 +74,6 @@ __device__ __forceinline__ void wht_across_lanes(float (&v)[8], int log2b, int l
 }
 
 // scale, round to bf16 (nearest even: the hardware conversion), pack
-typedef float v2f_had __attribute__((ext_vector_type(2)));
-typedef __bf16 v2bf_had __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint4 pack8_bf16(const float (&v)[8], float scale) {
     uint32_t o[4];
 #pragma unroll

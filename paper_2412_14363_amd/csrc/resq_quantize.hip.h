@@ -15,6 +15,8 @@
 #include <stdint.h>
 
 #include "resq_hadamard.hip.h"
+#include "resq_kv_row.hip.h"
+#include "resq_lanes.hip.h"
 #include "resq_layout.h"
 
 namespace resq {
@@ -22,36 +24,10 @@ namespace resq {
 constexpr int kQuantThreads = 256;
 constexpr int kQuantWideThreads = 1024;  // per row, where rows are few
 
-__device__ __forceinline__ float bf16_bits_to_f32(uint32_t b) { return __uint_as_float(b << 16); }
-
 __device__ __forceinline__ int quant_code(float x, float scale, int qmax) {
     float q = rintf(x / scale);
     q = fminf(fmaxf(q, -(float)qmax), (float)qmax);
     return (int)q;
-}
-
-// Butterfly reductions over the 64 lanes of a wavefront; the lane exchanges are
-// the cheap ones of the transform kernel (DPP moves, swizzles) where they exist.
-// G = 16, 32 or 64: the reduction runs inside aligned groups of G lanes.
-template <int G = 64>
-__device__ __forceinline__ float wave_max(float a) {
-    a = fmaxf(a, lane_xor<1>(a));
-    a = fmaxf(a, lane_xor<2>(a));
-    a = fmaxf(a, lane_xor<4>(a));
-    a = fmaxf(a, lane_xor<8>(a));
-    if constexpr (G > 16) a = fmaxf(a, lane_xor<16>(a));
-    if constexpr (G > 32) a = fmaxf(a, lane_xor<32>(a));
-    return a;
-}
-template <int G = 64>
-__device__ __forceinline__ int wave_sum(int v) {
-    v += __float_as_int(lane_xor<1>(__int_as_float(v)));
-    v += __float_as_int(lane_xor<2>(__int_as_float(v)));
-    v += __float_as_int(lane_xor<4>(__int_as_float(v)));
-    v += __float_as_int(lane_xor<8>(__int_as_float(v)));
-    if constexpr (G > 16) v += __float_as_int(lane_xor<16>(__int_as_float(v)));
-    if constexpr (G > 32) v += __float_as_int(lane_xor<32>(__int_as_float(v)));
-    return v;
 }
 
 // max over the W wavefronts' partial results in red (16 of them: a lane takes one, the exchanges do the rest)
@@ -244,11 +220,6 @@ __device__ __forceinline__ float quotient(float x, float scale, float inv) {
 constexpr float kQuotientMin = 8.077935669463161e-28f;   // 2^-90
 constexpr float kQuotientMax = 1.2676506002282294e+30f;  // 2^100
 __device__ __forceinline__ bool quotient_range(float scale) { return scale >= kQuotientMin && scale <= kQuotientMax; }
-
-// low bytes of four registers -> one dword
-__device__ __forceinline__ uint32_t pack_low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
-}
 
 // Optional block Walsh-Hadamard transform of the low group in front of the
 // quantizer (the online projection of the down_proj input, Section 4.3): the
@@ -753,15 +724,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_act_short_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// Compact K/V cache rows (Section 5.1 and Appendix C: the cache is quantized per
-// head with the asymmetric quantizer of Eq. 1, an eighth of the channels in 8
-// bits).  One row per head of a token, no padding:
-//   r bytes: the 8-bit codes, 0..255 | (d - r) / 2 bytes: the 4-bit codes, 0..15,
-//   channel r + 2j in bits 0..3, r + 2j + 1 in bits 4..7 | fp32 s_hi, z_hi, s_lo, z_lo
-// with x ~ code * s + z per group: r + (d - r) / 2 + 16 bytes for 2 d bytes of bf16.
-// The quantizer is the short-row kernel above (G lanes per row, no LDS, no
-// barrier); its stored codes (code - 2^(N-1), the GEMM's operand form) become the
-// codes of Eq. 1 with one XOR per four bytes.
+// Compact K/V cache rows (resq_kv_row.hip.h): G lanes per row, no LDS, no barrier.
 // ---------------------------------------------------------------------------
 template <int G>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kv_cache_kernel(
@@ -769,120 +732,23 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kv_cache_kernel(
     int64_t row_bytes) {
     const int gl = threadIdx.x & (G - 1);  // lane inside the group
     const int64_t m_raw = (int64_t)blockIdx.x * (kQuantThreads / G) + threadIdx.x / G;
-    // every lane of a wavefront runs the exchanges and the votes below; groups past
+    // every lane of a wavefront runs the exchanges and the votes; groups past
     // the last row work on the last row and store nothing
     const bool row_live = m_raw < rows;
     const int64_t m = row_live ? m_raw : rows - 1;
-    const int nunits = d >> 3, hi_units = r >> 3;
-    const bool live = gl < nunits, high = gl < hi_units;
-    const uint4 v = live ? reinterpret_cast<const uint4*>(x + m * ldx)[gl] : make_uint4(0u, 0u, 0u, 0u);
-
-    const float inf = __builtin_huge_valf();
-    float mx = -inf, nmn = -inf;
-    if (live) {
-        float f[8];
-        unpack8_bf16(v, f);
-        mx = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
-        nmn = -fminf(fminf(fminf(f[0], f[1]), fminf(f[2], f[3])), fminf(fminf(f[4], f[5]), fminf(f[6], f[7])));
-    }
-    const float mx_h = wave_max<G>(high ? mx : -inf), nmn_h = wave_max<G>(high ? nmn : -inf);
-    const float mx_l = wave_max<G>(live && !high ? mx : -inf);
-    const float nmn_l = wave_max<G>(live && !high ? nmn : -inf);
-    // A lane's columns are all of one group: it needs one scale, one reciprocal and one pass of the
-    // quantizer, with the constants of its own group (run for both groups on all lanes and
-    // selected afterwards, which the votes across the wavefront suggest, it took 6.7 instead of 5.0 us
-    // for 32768 rows of 128 columns at r = 16, and 30.4 instead of 22.4, 4.0 TB/s, for 262144; by events at the
-    // kernel's start and end, a kernel trace says 0.7 us more).
-    const float levels = high ? 255.0f : 15.0f;
-    const float zero = live ? -(high ? nmn_h : nmn_l) : 0.0f;
-    const float range = live ? (high ? mx_h : mx_l) - zero : 0.0f;
-    const float scale = range == 0.0f ? 1.0f : range / levels;  // asym_scale
-    const float inv = 1.0f / scale;
-    constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: quant8_asym, with the codes themselves
-    const float tie = 0.5f - (levels + 1.0f) * 9.5367431640625e-07f;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float ds[8];
-    uint32_t u[8];
-    bool near_tie[8], any_tie = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        ds[j] = __uint_as_float((j & 1) ? (w[j >> 1] & 0xFFFF0000u) : (w[j >> 1] << 16)) - zero;
-        const float t = ds[j] * inv;
-        const float uf = t + kMagic;
-        near_tie[j] = !(fabsf(t - (uf - kMagic)) <= tie);
-        any_tie |= near_tie[j];
-        u[j] = __float_as_uint(uf);
-    }
-    if (__builtin_amdgcn_ballot_w64(any_tie) != 0) {  // wave-uniform, then per element slot
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (__builtin_amdgcn_ballot_w64(near_tie[j]) != 0)
-                u[j] = (uint32_t)(int)fminf(fmaxf(rintf(ds[j] / scale), 0.0f), levels);
-    }
-    if (!row_live || !live) return;
-    uint8_t* row = cache + m * row_bytes;
-    float* par = reinterpret_cast<float*>(row + r + (d - r) / 2);
-    if (high) {
-        uint32_t* dst = reinterpret_cast<uint32_t*>(row + gl * 8);   // rows are 4-byte aligned
-        dst[0] = pack_low_bytes(u[0], u[1], u[2], u[3]);
-        dst[1] = pack_low_bytes(u[4], u[5], u[6], u[7]);
-    } else {
-        uint32_t by[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) by[k] = (u[2 * k + 1] << 4) | (u[2 * k] & 0xFu);
-        *reinterpret_cast<uint32_t*>(row + r + (gl - hi_units) * 4) = pack_low_bytes(by[0], by[1], by[2], by[3]);
-    }
-    // The first lane of a group writes its constants.  A row of one group: all four in one store by the first
-    // lane, scale 1 and zero-point 0 for the absent group (the present one's two and the absent one's apart:
-    // 262144 rows of 128 columns 24.4 / 21.1 us at r = 0, 24.8 / 22.1 at r = 128).
-    if (hi_units == 0 || hi_units == nunits) {
-        if (gl == 0) {
-            par[0] = high ? scale : 1.0f;
-            par[1] = high ? zero : 0.0f;
-            par[2] = high ? 1.0f : scale;
-            par[3] = high ? 0.0f : zero;
-        }
-    } else if (gl == 0 || gl == hi_units) {
-        par[high ? 0 : 2] = scale;
-        par[high ? 1 : 3] = zero;
-    }
+    const uint4 v = gl < (d >> 3) ? reinterpret_cast<const uint4*>(x + m * ldx)[gl] : make_uint4(0u, 0u, 0u, 0u);
+    quantize_kv_row<G>(v, gl, d, r, row_live ? cache + m * row_bytes : nullptr);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16_pair(float lo, float hi) {
-    const v2bf_had r = __builtin_convertvector((v2f_had){lo, hi}, v2bf_had);   // round to nearest even
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
-
-// The reader of such rows: x[m, k] = bf16(code * s + z) (Eq. 1), one lane per eight channels.
+// one lane per eight channels
 template <int G>
 __global__ __launch_bounds__(kQuantThreads) void dequantize_kv_cache_kernel(
     const uint8_t* __restrict__ cache, int64_t row_bytes, int64_t rows, int d, int r, uint16_t* __restrict__ x,
     int64_t ldx) {
     const int gl = threadIdx.x & (G - 1);
     const int64_t m = (int64_t)blockIdx.x * (kQuantThreads / G) + threadIdx.x / G;
-    const int nunits = d >> 3, hi_units = r >> 3;
-    if (m >= rows || gl >= nunits) return;
-    const uint8_t* row = cache + m * row_bytes;
-    const float* par = reinterpret_cast<const float*>(row + r + (d - r) / 2);
-    float f[8];
-    if (gl < hi_units) {
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(row + gl * 8);
-        const uint32_t c0 = src[0], c1 = src[1];
-        const float s = par[0], z = par[1];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = fmaf((float)(((k < 4 ? c0 : c1) >> (8 * (k & 3))) & 0xFFu), s, z);
-    } else {
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(row + r + (gl - hi_units) * 4);
-        const float s = par[2], z = par[3];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = fmaf((float)((c >> (4 * k)) & 0xFu), s, z);
-    }
-    uint4 o;
-    o.x = pack_bf16_pair(f[0], f[1]);
-    o.y = pack_bf16_pair(f[2], f[3]);
-    o.z = pack_bf16_pair(f[4], f[5]);
-    o.w = pack_bf16_pair(f[6], f[7]);
-    reinterpret_cast<uint4*>(x + m * ldx)[gl] = o;
+    if (m >= rows || gl >= (d >> 3)) return;
+    reinterpret_cast<uint4*>(x + m * ldx)[gl] = dequantize_kv_piece(cache + m * row_bytes, gl, d, r);
 }
 
 // ---------------------------------------------------------------------------
