@@ -457,6 +457,125 @@ int resq_dequantize_kv_cache(const void* cache, int64_t row_bytes, int64_t rows,
                              void* x, int64_t ldx, void* stream);
 
 /*
+ * ---- the generation step between the query/key/value projections and the output projection -------------------------------
+ * The K/V cache in PAGES: a page holds page_size rows of compact entries (resq_quantize_kv_cache's rows) for each K/V head, keys
+ * and values in two arrays alike in shape.  The row of head h in row i of page p is at byte
+ *   p * page_stride + h * head_stride + i * row_stride
+ * of its array (strides in bytes, multiples of 4, each at least resq_kv_cache_row_bytes; an axis of one entry has no stride;
+ * rows do not overlap).  A SLOT is p * page_size + i, num_pages * page_size <= 2^31 - 1.  A row of the BLOCK TABLE names the
+ * pages of a sequence in order: its token t is in row t % page_size of page block_table[b][t / page_size].  The attention reads
+ * fastest where a head's rows of a page are contiguous (row_stride = row bytes), page_size is a multiple of 16, and the arrays,
+ * page_stride and head_stride are multiples of 16.
+ * Common to these calls: lengths, positions, slots and table entries are int32 (4-byte aligned); head vectors are bf16 with a
+ * stride from token to token and one from head to head in elements (strides of inputs may be 0).
+ *
+ * The plan of a step, on the GPU: request b has lens[b] tokens in its pages and gets new_tokens[b] more (0 is fine).
+ * Its new tokens follow those of the requests before it in the batch; pages that it lacks are taken off the front of the free
+ * list, in the order of the requests, and entered into its row of the block table.
+ *   lens, new_tokens   int32 [B]; B <= 65536                                             (read)
+ *   free_pages         int32 [n_free] pages to hand out; taken: int32 [1], how many of them are gone already  (read)
+ *   block_table        int32 [B, ld_table], `width` entries used of each row, width * page_size <= 2^31 - 1   (entries of new pages written)
+ *   lens_out           int32 [B]: lens + new_tokens; may be lens                         (written)
+ *   cu_tokens, cu_pages  int32 [B + 1]: new tokens, and new pages, of the requests before b        (written)
+ *   positions, slots   int32 [max_tokens]: of each new token; behind the last one 0 and -1          (written)
+ *   state              int32 [2]: entries of free_pages gone after the call (taken may be this one), and a status:
+ *                      0: done; 1: too few free pages; 2: a table row too narrow; 3: more than max_tokens new tokens;
+ *                      4: a negative length, count or taken (the highest that applies).  Unless it is 0 nothing is handed out:
+ *                      lens_out = lens, the sums are 0, every slot is -1, the block table is as it was  (written)
+ * A token whose page (from the table or the free list) is outside [0, num_pages) gets slot -1.  max_tokens <= 2^31 - 257.
+ * The arrays do not overlap except as said.
+ */
+int resq_kv_slots(const int32_t* lens, const int32_t* new_tokens, int64_t B, int64_t page_size, int64_t num_pages,
+                  const int32_t* free_pages, int64_t n_free, const int32_t* taken, int32_t* block_table, int64_t ld_table,
+                  int64_t width, int64_t max_tokens, int32_t* lens_out, int32_t* cu_tokens, int32_t* cu_pages,
+                  int32_t* positions, int32_t* slots, int32_t* state, void* stream);
+
+/*
+ * The frequencies of a rotary position embedding, on the HOST (no device call): radians per position of each pair of channels,
+ * base^(-2i/rot), as they are or stretched for contexts longer than the original one.
+ *   scaling  RESQ_ROPE_PLAIN   as they are
+ *            RESQ_ROPE_LINEAR  all divided by factor
+ *            RESQ_ROPE_BASE    base * factor^(rot / (rot - 2)) for base: the fastest as it is, the slowest divided by factor
+ *            RESQ_ROPE_BANDS   pairs that make more than `high` turns over original_len as they are, those with fewer than `low`
+ *                              divided by factor, a share of both between
+ *            RESQ_ROPE_RAMP    the same with the share linear in the pair's number (YaRN, arXiv 2309.00071), and
+ *                              *mscale = 0.1 ln(factor) + 1
+ *   rot      even, 2 .. 512; base > 1; factor >= 1 and 0 < low < high, original_len >= 1 where they are used
+ *   freq     HOST, double [rot / 2];  mscale  HOST, one float: what resq_rope_heads multiplies rotated channels by   (written)
+ */
+enum { RESQ_ROPE_PLAIN = 0, RESQ_ROPE_LINEAR = 1, RESQ_ROPE_BASE = 2, RESQ_ROPE_BANDS = 3, RESQ_ROPE_RAMP = 4 };
+int resq_rope_frequencies(int64_t rot, double base, int scaling, double factor, double low, double high, int64_t original_len,
+                          double* freq, float* mscale);
+
+/*
+ * The position embedding of query and key heads, in front of resq_project_heads (Section 4.3 projects them after it), with the
+ * norm of each head in the same pass for models that have one:
+ *   n = x * rsqrt(mean(x^2) + eps) * w   (w: w_q for heads [0, heads_q), w_k for the others; both null: n = x)
+ *   y = n with each pair (a, b) of its first rot channels turned to mscale * (a cos - b sin, b cos + a sin) by the angle
+ *       positions[token] * freq[pair]; pair i is channels (i, i + rot/2), or (2i, 2i + 1) where `interleaved` is not 0
+ * in fp32 with one rounding to bf16 at the end; the angle is taken modulo a turn in fp64, so that it is as exact at position
+ * 2^31 - 1 as at 1.  Channels [rot, d_head) are n alone.
+ *   x, y     bf16 [tokens, heads_q + heads_k, d_head] with strides (ldx, ldxh), (ldy, ldyh); y may be x with the same strides,
+ *            else they do not overlap                                                    (read / written)
+ *   d_head   even, 2 .. 512; rot even, 0 .. d_head (positions and freq may be null for 0); tokens = 0 does nothing
+ *   w_q, w_k bf16 [d_head] or both null; eps >= 0                                        (read)
+ *   positions int32 [tokens]; freq fp64 [rot / 2], 8-byte aligned, in DEVICE memory      (read)
+ * Alignment: 2 bytes; rows of whole 16-byte pieces (x, y 16-byte aligned, strides and d_head multiples of 8, rot a multiple of
+ * 16, or of 8 where interleaved) are moved in such pieces.
+ */
+int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t d_head,
+                    const void* w_q, const void* w_k, float eps, const int32_t* positions, const double* freq, int64_t rot,
+                    int interleaved, float mscale, void* y, int64_t ldy, int64_t ldyh, void* stream);
+
+/*
+ * The paged writer: K and V of new tokens, quantized as by resq_quantize_kv_cache (the same bytes), straight to their slots.
+ *   k, v     bf16 [tokens, heads, d_head] with strides (ldk, ldkh), (ldv, ldvh)           (read)
+ *   slots    int32 [tokens]; tokens whose slot is outside [0, num_pages * page_size) are left out; the others' slots differ
+ *            from one another (a slot named twice is left with bytes of both tokens)      (read)
+ *   k_pages, v_pages   the pages (above)                                                  (rows of the slots written, nothing else)
+ *   d_head, r as resq_quantize_kv_cache; tokens = 0 does nothing
+ * Errors: RESQ_ERR_BUFFER for strides below the row; RESQ_ERR_ALIGN unless k and v are 16-byte aligned, their strides multiples
+ * of 8, the pages 4-byte aligned and their strides multiples of 4.
+ *
+ * resq_gather_kv_cache is the paged reader: the values of the tokens in `slots` (any order, repeats are fine) as
+ * resq_dequantize_kv_cache gives them, zeros for slots outside the pages.  k and v are written, their rows do not overlap.
+ */
+int resq_append_kv_cache(const void* k, int64_t ldk, int64_t ldkh, const void* v, int64_t ldv, int64_t ldvh, int64_t tokens,
+                         int64_t heads, int64_t d_head, int64_t r, const int32_t* slots, void* k_pages, void* v_pages,
+                         int64_t num_pages, int64_t page_size, int64_t page_stride, int64_t head_stride, int64_t row_stride,
+                         void* stream);
+int resq_gather_kv_cache(const void* k_pages, const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride,
+                         int64_t head_stride, int64_t row_stride, const int32_t* slots, int64_t tokens, int64_t heads,
+                         int64_t d_head, int64_t r, void* k, int64_t ldk, int64_t ldkh, void* v, int64_t ldv, int64_t ldvh,
+                         void* stream);
+
+/*
+ * Attention of one new token of each sequence over its pages (the new token's own K and V are there already, as its last row),
+ * queries in 16 bits (Section 5.1), the K/V rows as they stand for: k = code * s + z, not rounded.  For query head h, K/V head
+ * h / (heads_q / heads_k), over the tokens t < len:
+ *   x_t = scale * q . k_t;  softcap > 0: softcap * tanh(x_t / softcap);  window > 0: only the last `window` tokens
+ *   out = sum_t e^(x_t - lse) v_t (rounded to bf16 once),  lse = ln sum_t e^(x_t)
+ * Tokens whose table entry is outside [0, num_pages) take no part.  Where none is left (an empty sequence) out is 0 and lse -inf.
+ *   q, out   bf16 [B, heads_q, d_head] with strides (ldq, ldqh), (ldo, ldoh); rows of out do not overlap, out may be q with the
+ *            same strides                                                                 (read / written)
+ *   lens     int32 [B]; what is above width * page_size (or 2^30) is read as that, what is below 0 as 0     (read)
+ *   block_table  int32 [B, ld_table], `width` entries used of each row                    (read)
+ *   lse      fp32 [B, heads_q] or null                                                    (written)
+ *   d_head   multiple of 8, 8 .. 256; r as resq_quantize_kv_cache; heads_q a multiple of heads_k; B, heads_q <= 65535
+ *   scale    > 0; softcap >= 0 (0: none); window >= 0 (0: none)
+ *   workspace  device memory, 256-byte aligned, resq_attend_kv_cache_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents
+ *            meaningless before and after; calls that overlap (different streams) need one each
+ * The work is cut by the lengths that the GPU finds, so that a captured call serves any lengths.  The cuts, and with them the
+ * order of fp32 sums, depend on all lengths of the call, not on timing: equal calls give equal bits.
+ */
+size_t resq_attend_kv_cache_workspace_bytes(int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head);
+int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head,
+                         int64_t r, const int32_t* lens, const int32_t* block_table, int64_t ld_table, int64_t width,
+                         const void* k_pages, const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride,
+                         int64_t head_stride, int64_t row_stride, float scale, float softcap, int64_t window, void* out,
+                         int64_t ldo, int64_t ldoh, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Online Hadamard projection of the down_proj input (Section 4.3, U_D):
  *   y[m, c0 + g*b + j] = (1/sqrt(b)) * sum_i x[m, c0 + g*b + i] * H_b[i, j]
  * for each block g of b columns in [col_begin, col_end), H_b the Sylvester

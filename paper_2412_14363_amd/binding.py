@@ -48,6 +48,17 @@ SYMBOLS = {
     "resq_kv_cache_row_bytes": (_sz, [_i64, _i64]),
     "resq_quantize_kv_cache": (C.c_int, [_p, _i64, _i64, _i64, _i64, _p, _i64, _p]),
     "resq_dequantize_kv_cache": (C.c_int, [_p, _i64, _i64, _i64, _i64, _p, _i64, _p]),
+    "resq_kv_slots": (C.c_int, [_p, _p, _i64, _i64, _i64, _p, _i64, _p, _p, _i64, _i64, _i64, _p, _p, _p, _p, _p, _p, _p]),
+    "resq_rope_frequencies": (C.c_int, [_i64, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, _i64, _p, _p]),
+    "resq_rope_heads": (C.c_int, [_p, _i64, _i64, _i64, _i64, _i64, _i64, _p, _p, C.c_float, _p, _p, _i64, C.c_int, C.c_float,
+                                  _p, _i64, _i64, _p]),
+    "resq_append_kv_cache": (C.c_int, [_p, _i64, _i64, _p, _i64, _i64, _i64, _i64, _i64, _i64, _p, _p, _p, _i64, _i64, _i64, _i64,
+                                       _i64, _p]),
+    "resq_gather_kv_cache": (C.c_int, [_p, _p, _i64, _i64, _i64, _i64, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64,
+                                       _i64, _p]),
+    "resq_attend_kv_cache_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "resq_attend_kv_cache": (C.c_int, [_p, _i64, _i64, _i64, _i64, _i64, _i64, _i64, _p, _p, _i64, _i64, _p, _p, _i64, _i64, _i64, _i64,
+                                       _i64, C.c_float, C.c_float, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
     "resq_pack_weights": (C.c_int, [_p, _i64, _i64, _i64, _i64, _p, _sz, _p]),
     "resq_unpack_weights": (C.c_int, [_p, _i64, _i64, _i64, _p, _p, _p, _p, _p]),
     "resq_gemm_mixed": (C.c_int, [_p, _p, _p, _p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _p, _p, _p]),
@@ -527,6 +538,232 @@ def resq_dequantize_kv_cache(cache: torch.Tensor, d_head: int, r: int, out: Opti
     st = lib().resq_dequantize_kv_cache(_dev(cache, torch.uint8, "cache"), cache.stride(0), rows, d_head, r,
                                         _dev(out, torch.bfloat16, "out"), out.stride(0), _stream(stream))
     _check(st, "resq_dequantize_kv_cache")
+    return out
+
+
+# ---- the generation step: plan, position embedding, paged K/V cache, attention --------------------------------
+# Sizes are checked here because the kernels rely on them; what the arrays hold (lengths, slots, table entries) is checked by the
+# kernels themselves.
+
+def _same_device(where: str, first: torch.Tensor, *others) -> None:
+    """All tensors on the current device: that is where the call's kernels run."""
+    if not first.is_cuda:
+        raise ValueError(f"{where}: tensors must live in device memory")
+    dev = first.get_device()
+    if dev != _raw_device():
+        raise ValueError(f"{where}: the tensors are on cuda:{dev}, the current device is cuda:{_raw_device()}")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{where}: tensors on {first.device} and {t.device}")
+
+
+def _ints(where: str, name: str, t: torch.Tensor, n: Optional[int] = None) -> int:
+    if t.dtype != torch.int32 or t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1) or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{where}: {name} must be a contiguous int32 vector" + (f" of {n}" if n is not None else ""))
+    return t.data_ptr()
+
+
+def _table(where: str, t: torch.Tensor, batch: int):
+    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != batch or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{where}: block_table must be a row-major int32 [{batch}, pages] tensor")
+    return t.data_ptr(), t.stride(0), t.shape[1]
+
+
+def _head_rows(where: str, name: str, t: torch.Tensor):
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{where}: {name} must be a bf16 [tokens, heads, d_head] tensor whose rows are contiguous")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _kv_pages(where: str, k_pages: torch.Tensor, v_pages: torch.Tensor, heads: int, d_head: int, r: int):
+    """(k, v, num_pages, page_size, page_stride, head_stride, row_stride) of two uint8 [pages, heads, page_size, row bytes] tensors."""
+    n, h, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
+    need = resq_kv_cache_row_bytes(d_head, r)
+    if need == 0:
+        raise ValueError(f"{where}: invalid (d_head, r) = ({d_head}, {r})")
+    if k_pages.dtype != torch.uint8 or v_pages.dtype != torch.uint8 or h != heads or width < need or k_pages.stride(3) != 1:
+        raise ValueError(f"{where}: pages must be uint8 [pages, {heads}, page_size, >= {need}] tensors whose rows are contiguous")
+    if v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride():
+        raise ValueError(f"{where}: k_pages and v_pages must have the same shape and strides")
+    a, b, c, _ = k_pages.stride()
+    return k_pages.data_ptr(), v_pages.data_ptr(), n, size, a, b, c
+
+
+class KvSlots:
+    """Device buffers resq_kv_slots writes: lens [batch], cu_tokens and cu_pages [batch + 1], positions and slots [max_tokens],
+    state [2] (entries of the free list gone, status).  All start at 0, slots at -1."""
+
+    def __init__(self, batch: int, max_tokens: int, device="cuda"):
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.cu_tokens = torch.zeros(batch + 1, dtype=torch.int32, device=device)
+        self.cu_pages = torch.zeros(batch + 1, dtype=torch.int32, device=device)
+        self.positions = torch.zeros(max_tokens, dtype=torch.int32, device=device)
+        self.slots = torch.full((max_tokens,), -1, dtype=torch.int32, device=device)
+        self.state = torch.zeros(2, dtype=torch.int32, device=device)
+
+
+def resq_kv_slots(lens: torch.Tensor, new_tokens: torch.Tensor, free_pages: torch.Tensor, taken: Optional[torch.Tensor],
+                  block_table: torch.Tensor, page_size: int, num_pages: int, out: Optional[KvSlots] = None,
+                  max_tokens: Optional[int] = None, stream=None) -> KvSlots:
+    """The plan of a step: positions and slots of new_tokens[b] tokens of each request behind its lens[b], pages off the free
+    list into block_table.  taken: how many of free_pages are gone (None: out.state's first entry, i.e. go on from the call
+    before).  lens may be out.lens.  out.state[1] is the status, see include/resq.h."""
+    where = "resq_kv_slots"
+    batch = lens.shape[0]
+    if out is None:
+        if max_tokens is None:
+            raise ValueError(f"{where}: give out or max_tokens")
+        out = KvSlots(batch, max_tokens, lens.device)
+    if taken is None:
+        taken = out.state[:1]
+    _same_device(where, lens, new_tokens, free_pages, taken, block_table, out.lens, out.cu_tokens, out.cu_pages, out.positions,
+                 out.slots, out.state)
+    table, ld_table, width = _table(where, block_table, batch)
+    cap = out.slots.shape[0]
+    st = lib().resq_kv_slots(
+        _ints(where, "lens", lens), _ints(where, "new_tokens", new_tokens, batch), batch, page_size, num_pages,
+        _ints(where, "free_pages", free_pages), free_pages.shape[0], _ints(where, "taken", taken, 1), table, ld_table, width, cap,
+        _ints(where, "out.lens", out.lens, batch), _ints(where, "out.cu_tokens", out.cu_tokens, batch + 1),
+        _ints(where, "out.cu_pages", out.cu_pages, batch + 1), _ints(where, "out.positions", out.positions, cap),
+        _ints(where, "out.slots", out.slots), _ints(where, "out.state", out.state, 2), _stream(stream))
+    _check(st, where)
+    return out
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def resq_rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, low: float = 1.0,
+                          high: float = 4.0, original_len: int = 8192, device="cuda"):
+    """(freq fp64 [rot / 2] on `device`, mscale) for resq_rope_heads; scaling: see include/resq.h."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}, got {scaling!r}")
+    freq, mscale = torch.empty(max(rot, 0) // 2, dtype=torch.float64), C.c_float()
+    _check(lib().resq_rope_frequencies(rot, base, ROPE_SCALINGS[scaling], factor, low, high, original_len,
+                                       freq.data_ptr() if freq.numel() else None, C.byref(mscale)), "resq_rope_frequencies")
+    return freq.to(device), mscale.value
+
+
+def resq_rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor], freq: Optional[torch.Tensor], heads_q: Optional[int] = None,
+                    w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    interleaved: bool = False, mscale: float = 1.0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x: bf16 [tokens, heads, d_head], the first heads_q heads (None: all) queries, the others keys; positions int32 [tokens];
+    freq fp64 [rot / 2] (None or empty: no rotation); w_q, w_k: bf16 [d_head] weights of the heads' norm (None: no norm).
+    out may be x."""
+    where = "resq_rope_heads"
+    px, ldx, ldxh = _head_rows(where, "x", x)
+    tokens, heads, d = x.shape
+    if heads_q is None:
+        heads_q = heads
+    if out is None:
+        out = torch.empty((tokens, heads, d), dtype=torch.bfloat16, device=x.device)
+    py, ldy, ldyh = _head_rows(where, "out", out)
+    _same_device(where, x, positions, freq, w_q, w_k, out)
+    rot = 0 if freq is None else 2 * freq.shape[0]
+    if out.shape != x.shape or not 0 <= heads_q <= heads:
+        raise ValueError(f"{where}: out {tuple(out.shape)}, x {tuple(x.shape)} or heads_q = {heads_q} do not match")
+    if rot and (positions is None or freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous()):
+        raise ValueError(f"{where}: freq must be a contiguous fp64 [rot / 2] tensor, with positions")
+    for name, w in (("w_q", w_q), ("w_k", w_k)):
+        if w is not None and (w.dtype != torch.bfloat16 or w.shape != (d,) or not w.is_contiguous()):
+            raise ValueError(f"{where}: {name} must be a contiguous bf16 [{d}] tensor")
+    st = lib().resq_rope_heads(px, ldx, ldxh, tokens, heads_q, heads - heads_q, d,
+                               None if w_q is None else w_q.data_ptr(), None if w_k is None else w_k.data_ptr(), eps,
+                               _ints(where, "positions", positions, tokens) if rot else None, freq.data_ptr() if rot else None,
+                               rot, int(interleaved), mscale, py, ldy, ldyh, _stream(stream))
+    _check(st, where)
+    return out
+
+
+def resq_append_kv_cache(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                         r: int, stream=None) -> None:
+    """k, v: bf16 [tokens, heads, d_head], quantized into rows `slots` (int32 [tokens], below 0: left out) of the uint8
+    [pages, heads, page_size, row bytes] pages."""
+    where = "resq_append_kv_cache"
+    pk, ldk, ldkh = _head_rows(where, "k", k)
+    pv, ldv, ldvh = _head_rows(where, "v", v)
+    tokens, heads, d = k.shape
+    if v.shape != k.shape:
+        raise ValueError(f"{where}: k {tuple(k.shape)} and v {tuple(v.shape)} do not match")
+    _same_device(where, k, v, slots, k_pages, v_pages)
+    pages = _kv_pages(where, k_pages, v_pages, heads, d, r)
+    st = lib().resq_append_kv_cache(pk, ldk, ldkh, pv, ldv, ldvh, tokens, heads, d, r, _ints(where, "slots", slots, tokens), *pages,
+                                    _stream(stream))
+    _check(st, where)
+
+
+def resq_gather_kv_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor, r: int,
+                         k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, d_head: Optional[int] = None,
+                         stream=None):
+    """The values of the rows in `slots` (int32 [tokens]), bf16 [tokens, heads, d_head] each for keys and values; zeros for slots
+    outside the pages.  d_head is that of k where k is given."""
+    where = "resq_gather_kv_cache"
+    if k_pages.dim() != 4:
+        raise ValueError(f"{where}: pages must be [pages, heads, page_size, row bytes] tensors")
+    tokens, heads = slots.shape[0], k_pages.shape[1]
+    if k is None and d_head is None:
+        raise ValueError(f"{where}: give k or d_head")
+    d = d_head if k is None else k.shape[-1]
+    k, v = (torch.empty((tokens, heads, d), dtype=torch.bfloat16, device=k_pages.device) if t is None else t for t in (k, v))
+    pk, ldk, ldkh = _head_rows(where, "k", k)
+    pv, ldv, ldvh = _head_rows(where, "v", v)
+    if k.shape != (tokens, heads, d) or v.shape != k.shape or (d_head is not None and d_head != d):
+        raise ValueError(f"{where}: k {tuple(k.shape)} and v {tuple(v.shape)} must be [{tokens}, {heads}, {d_head or d}]")
+    _same_device(where, k_pages, v_pages, slots, k, v)
+    pages = _kv_pages(where, k_pages, v_pages, heads, d, r)
+    st = lib().resq_gather_kv_cache(*pages, _ints(where, "slots", slots, tokens), tokens, heads, d, r, pk, ldk, ldkh, pv, ldv, ldvh,
+                                    _stream(stream))
+    _check(st, where)
+    return k, v
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def resq_attend_kv_cache_workspace_bytes(batch: int, heads_q: int, heads_k: int, d_head: int) -> int:
+    return int(lib().resq_attend_kv_cache_workspace_bytes(batch, heads_q, heads_k, d_head))
+
+
+def resq_attend_kv_cache_workspace(batch: int, heads_q: int, heads_k: int, d_head: int, device="cuda") -> torch.Tensor:
+    """A workspace for resq_attend_kv_cache calls of these sizes; calls on different streams need one each."""
+    nbytes = resq_attend_kv_cache_workspace_bytes(batch, heads_q, heads_k, d_head)
+    if nbytes == 0:
+        raise ValueError(f"invalid (batch, heads_q, heads_k, d_head) = ({batch}, {heads_q}, {heads_k}, {d_head})")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, lens: torch.Tensor,
+                         block_table: torch.Tensor, r: int, scale: Optional[float] = None, softcap: float = 0.0, window: int = 0,
+                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of one new token of each sequence, q: bf16 [batch, heads, d_head], over the first lens[b] tokens of the pages that
+    block_table [batch, pages] names.  scale: d_head^-0.5 when None.  lse: fp32 [batch, heads], written where given."""
+    where = "resq_attend_kv_cache"
+    pq, ldq, ldqh = _head_rows(where, "q", q)
+    batch, heads, d = q.shape
+    if out is None:
+        out = torch.empty((batch, heads, d), dtype=torch.bfloat16, device=q.device)
+    po, ldo, ldoh = _head_rows(where, "out", out)
+    heads_k = k_pages.shape[1] if k_pages.dim() == 4 else 0
+    if out.shape != q.shape or heads_k == 0 or heads % heads_k:
+        raise ValueError(f"{where}: q {tuple(q.shape)}, out {tuple(out.shape)} or {heads_k} K/V heads do not match")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads) or not lse.is_contiguous()):
+        raise ValueError(f"{where}: lse must be a contiguous fp32 [{batch}, {heads}] tensor")
+    if batch == 0:
+        return out
+    need = resq_attend_kv_cache_workspace_bytes(batch, heads, heads_k, d)
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        if stream is not None:   # made on the current stream, used on another one
+            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError(f"{where}: workspace must be a contiguous uint8 tensor")
+    _same_device(where, q, k_pages, v_pages, lens, block_table, out, lse, workspace)
+    pages = _kv_pages(where, k_pages, v_pages, heads_k, d, r)
+    table, ld_table, width = _table(where, block_table, batch)
+    st = lib().resq_attend_kv_cache(
+        pq, ldq, ldqh, batch, heads, heads_k, d, r, _ints(where, "lens", lens, batch), table, ld_table, width, *pages,
+        d ** -0.5 if scale is None else scale, softcap, window, po, ldo, ldoh, None if lse is None else lse.data_ptr(),
+        workspace.data_ptr(), workspace.numel(), _stream(stream))
+    _check(st, where)
     return out
 
 

@@ -1,0 +1,270 @@
+// C ABI of the generation step's side of the library: position embedding, paged K/V cache, attention over it.
+// Argument checks on the host, then launches on the caller's stream.  See include/resq.h for the contract of every entry.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "resq.h"
+#include "resq_attend.hip.h"
+#include "resq_kv.hip.h"
+#include "resq_launch.h"
+#include "resq_rope.hip.h"
+
+using namespace resq;
+
+namespace {
+
+constexpr int64_t kInt32Max = 0x7FFFFFFF;
+constexpr int64_t kMaxAttendLen = 1 << 30;
+
+// rows of `width` elements, ld from one to the next of n and ldh from one to the next of heads, that do not overlap
+inline bool rows_apart(int64_t n, int64_t ld, int64_t heads, int64_t ldh, int64_t width) {
+    if ((n > 1 && ld < width) || (heads > 1 && ldh < width)) return false;
+    return n <= 1 || heads <= 1 || ld >= (heads - 1) * ldh + width || ldh >= (n - 1) * ld + width;
+}
+
+struct PagesGeometry {
+    int64_t num_pages, page_size, heads, page_stride, head_stride, row_stride;
+};
+
+// checks the pages of a cache; strides of axes with one entry do not matter and become 0
+int check_pages(PagesGeometry& g, const void* k_pages, const void* v_pages, int64_t d_head, int64_t r) {
+    if (!kv_head_ok(d_head, r) || g.num_pages < 1 || g.page_size < 1 || g.num_pages > kInt32Max / g.page_size || g.heads < 1 ||
+        g.heads > 65535)
+        return RESQ_ERR_SHAPE;
+    const int64_t need = r + (d_head - r) / 2 + 16;
+    if (g.num_pages == 1) g.page_stride = 0;
+    if (g.heads == 1) g.head_stride = 0;
+    if (g.page_size == 1) g.row_stride = 0;
+    if ((g.num_pages > 1 && g.page_stride < need) || (g.heads > 1 && g.head_stride < need) ||
+        (g.page_size > 1 && g.row_stride < need))
+        return RESQ_ERR_BUFFER;
+    if (!k_pages || !v_pages) return RESQ_ERR_NULL;
+    if (!aligned(k_pages, 4) || !aligned(v_pages, 4) || g.page_stride % 4 || g.head_stride % 4 || g.row_stride % 4)
+        return RESQ_ERR_ALIGN;
+    return RESQ_OK;
+}
+
+// what the paged writer and the reader check alike; done: nothing to do
+int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int64_t ldkh, const void* v, int64_t ldv, int64_t ldvh,
+                    int64_t tokens, int64_t heads, int64_t d_head, int64_t r, const int32_t* slots, const void* k_pages,
+                    const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride, int64_t head_stride,
+                    int64_t row_stride) {
+    done = true;
+    if (tokens < 0 || tokens > kInt32Max || ldk < 0 || ldkh < 0 || ldv < 0 || ldvh < 0) return RESQ_ERR_SHAPE;
+    PagesGeometry g{num_pages, page_size, heads, page_stride, head_stride, row_stride};
+    const int rc = check_pages(g, k_pages, v_pages, d_head, r);
+    if (rc == RESQ_ERR_SHAPE || rc == RESQ_ERR_BUFFER) return rc;
+    if (tokens == 0) return RESQ_OK;
+    if (!k || !v || !slots) return RESQ_ERR_NULL;
+    if (rc != RESQ_OK) return rc;
+    if (!aligned(k, 16) || !aligned(v, 16) || (tokens > 1 && (ldk % 8 || ldv % 8)) || (heads > 1 && (ldkh % 8 || ldvh % 8)) ||
+        !aligned(slots, 4))
+        return RESQ_ERR_ALIGN;
+    a.x[0] = static_cast<const uint16_t*>(k);
+    a.x[1] = static_cast<const uint16_t*>(v);
+    a.ld[0] = tokens > 1 ? ldk : 0;
+    a.ld[1] = tokens > 1 ? ldv : 0;
+    a.ldh[0] = heads > 1 ? ldkh : 0;
+    a.ldh[1] = heads > 1 ? ldvh : 0;
+    a.tokens = tokens;
+    a.heads = (int)heads;
+    a.d = (int)d_head;
+    a.r = (int)r;
+    a.slots = slots;
+    a.pages[0] = static_cast<uint8_t*>(const_cast<void*>(k_pages));
+    a.pages[1] = static_cast<uint8_t*>(const_cast<void*>(v_pages));
+    a.page_stride = g.page_stride;
+    a.head_stride = g.head_stride;
+    a.row_stride = g.row_stride;
+    a.page_size = (int)page_size;
+    a.num_slots = (uint32_t)(num_pages * page_size);
+    done = false;
+    return RESQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int resq_kv_slots(const int32_t* lens, const int32_t* new_tokens, int64_t B, int64_t page_size, int64_t num_pages,
+                  const int32_t* free_pages, int64_t n_free, const int32_t* taken, int32_t* block_table, int64_t ld_table,
+                  int64_t width, int64_t max_tokens, int32_t* lens_out, int32_t* cu_tokens, int32_t* cu_pages,
+                  int32_t* positions, int32_t* slots, int32_t* state, void* stream) {
+    if (B < 1 || B > 65536 || page_size < 1 || num_pages < 1 || num_pages > kInt32Max / page_size || n_free < 0 ||
+        n_free > kInt32Max || width < 1 || width > kInt32Max / page_size || (B > 1 && ld_table < width) || max_tokens < 1 ||
+        max_tokens > kInt32Max - 256)
+        return RESQ_ERR_SHAPE;
+    if (!lens || !new_tokens || (n_free > 0 && !free_pages) || !taken || !block_table || !lens_out || !cu_tokens || !cu_pages ||
+        !positions || !slots || !state)
+        return RESQ_ERR_NULL;
+    for (const void* p : {(const void*)lens, (const void*)new_tokens, (const void*)free_pages, (const void*)taken,
+                          (const void*)block_table, (const void*)lens_out, (const void*)cu_tokens, (const void*)cu_pages,
+                          (const void*)positions, (const void*)slots, (const void*)state})
+        if (!aligned(p, 4)) return RESQ_ERR_ALIGN;
+    const KvPlanArgs p{lens, new_tokens, (int)B, (int)page_size, (int)num_pages, free_pages, n_free, taken, block_table, ld_table,
+                       (int)width, (int)max_tokens, lens_out, cu_tokens, cu_pages, positions, slots, state};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    launch(kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
+    launch(kv_plan_tokens_kernel, dim3((unsigned)((max_tokens + 255) / 256)), dim3(256), 0, st, p);
+    return launch_status();
+}
+
+int resq_rope_frequencies(int64_t rot, double base, int scaling, double factor, double low, double high, int64_t original_len,
+                          double* freq, float* mscale) {
+    if (rot < 2 || rot > kRopeMaxHead || rot % 2 || !(base > 1.0) || !isfinite(base) || scaling < 0 || scaling > 4) return RESQ_ERR_SHAPE;
+    if (scaling != RESQ_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return RESQ_ERR_SHAPE;
+    if (scaling >= RESQ_ROPE_BANDS && (!(low > 0.0) || !(high > low) || !isfinite(high) || original_len < 1)) return RESQ_ERR_SHAPE;
+    if (!freq || !mscale) return RESQ_ERR_NULL;
+    const double turn = 6.283185307179586477;
+    *mscale = 1.0f;
+    double first = 0.0, last = 0.0;
+    if (scaling == RESQ_ROPE_BASE && rot > 2) base *= pow(factor, (double)rot / (double)(rot - 2));
+    if (scaling == RESQ_ROPE_RAMP) {   // the pairs that make `high` and `low` turns over the original length
+        const double per = rot / (2.0 * log(base));
+        first = fmax(floor(per * log(original_len / (high * turn))), 0.0);
+        last = fmin(ceil(per * log(original_len / (low * turn))), (double)(rot - 1));
+        if (last <= first) last = first + 0.001;
+        *mscale = (float)(0.1 * log(factor) + 1.0);
+    }
+    for (int64_t i = 0; i < rot / 2; ++i) {
+        const double f = pow(base, -2.0 * (double)i / (double)rot);
+        double keep = 1.0;   // share of the frequency that stays as it is; the rest is divided by the factor
+        if (scaling == RESQ_ROPE_LINEAR) keep = 0.0;
+        if (scaling == RESQ_ROPE_BANDS) keep = fmin(fmax((original_len * f / turn - low) / (high - low), 0.0), 1.0);
+        if (scaling == RESQ_ROPE_RAMP) keep = 1.0 - fmin(fmax(((double)i - first) / (last - first), 0.0), 1.0);
+        freq[i] = keep * f + (1.0 - keep) * (f / factor);
+    }
+    return RESQ_OK;
+}
+
+int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t d_head,
+                    const void* w_q, const void* w_k, float eps, const int32_t* positions, const double* freq, int64_t rot,
+                    int interleaved, float mscale, void* y, int64_t ldy, int64_t ldyh, void* stream) {
+    const int64_t heads = heads_q + heads_k;
+    if (tokens < 0 || tokens > kInt32Max || heads_q < 0 || heads_k < 0 || heads_q > 65535 || heads_k > 65535 || heads < 1 || d_head < 2 ||
+        d_head > kRopeMaxHead || d_head % 2 || rot < 0 || rot > d_head || rot % 2 || ldx < 0 || ldxh < 0 || !(eps >= 0.0f) ||
+        !isfinite(eps) || !rows_apart(tokens, ldy, heads, ldyh, d_head))
+        return RESQ_ERR_SHAPE;
+    const bool norm = w_q || w_k;
+    if (tokens == 0) return RESQ_OK;
+    if (!x || !y || (rot > 0 && (!positions || !freq)) || (norm && ((heads_q > 0 && !w_q) || (heads_k > 0 && !w_k)))) return RESQ_ERR_NULL;
+    if (tokens == 1) ldx = ldy = 0;
+    if (heads == 1) ldxh = ldyh = 0;
+    if (x == y && (ldx != ldy || ldxh != ldyh)) return RESQ_ERR_SHAPE;
+    if (!aligned(x, 2) || !aligned(y, 2) || !aligned(w_q, 2) || !aligned(w_k, 2) || !aligned(positions, 4) || !aligned(freq, 8))
+        return RESQ_ERR_ALIGN;
+    const RopeArgs a{static_cast<const uint16_t*>(x), ldx, ldxh, tokens, (int)heads, (int)heads_q, (int)d_head,
+                     static_cast<const uint16_t*>(w_q), static_cast<const uint16_t*>(w_k), eps, positions, freq, (int)rot,
+                     interleaved != 0, mscale, static_cast<uint16_t*>(y), ldy, ldyh};
+    const int64_t blocks = (tokens * heads + 3) / 4;
+    if (blocks > kInt32Max) return RESQ_ERR_SHAPE;
+    launch(rope_heads_kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    return launch_status();
+}
+
+int resq_append_kv_cache(const void* k, int64_t ldk, int64_t ldkh, const void* v, int64_t ldv, int64_t ldvh, int64_t tokens,
+                         int64_t heads, int64_t d_head, int64_t r, const int32_t* slots, void* k_pages, void* v_pages,
+                         int64_t num_pages, int64_t page_size, int64_t page_stride, int64_t head_stride, int64_t row_stride,
+                         void* stream) {
+    KvPagesArgs a;
+    bool done;
+    const int rc = make_pages_args(a, done, k, ldk, ldkh, v, ldv, ldvh, tokens, heads, d_head, r, slots, k_pages, v_pages, num_pages,
+                                   page_size, page_stride, head_stride, row_stride);
+    if (rc != RESQ_OK || done) return rc;
+    const int64_t rows = tokens * heads;
+#define RESQ_LAUNCH_APPEND(G)                                                                                             \
+    do {                                                                                                                  \
+        const int64_t blocks = (rows + kKvThreads / G - 1) / (kKvThreads / G);                                      \
+        if (blocks > kInt32Max) return RESQ_ERR_SHAPE;                                                                    \
+        launch(append_kv_cache_kernel<G>, dim3((unsigned)blocks, 2), dim3(kKvThreads), 0, static_cast<hipStream_t>(stream), a); \
+    } while (0)
+    if (d_head <= 128) RESQ_LAUNCH_APPEND(16);
+    else if (d_head <= 256) RESQ_LAUNCH_APPEND(32);
+    else RESQ_LAUNCH_APPEND(64);
+#undef RESQ_LAUNCH_APPEND
+    return launch_status();
+}
+
+int resq_gather_kv_cache(const void* k_pages, const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride,
+                         int64_t head_stride, int64_t row_stride, const int32_t* slots, int64_t tokens, int64_t heads,
+                         int64_t d_head, int64_t r, void* k, int64_t ldk, int64_t ldkh, void* v, int64_t ldv, int64_t ldvh,
+                         void* stream) {
+    KvPagesArgs a;
+    bool done;
+    if (!rows_apart(tokens, ldk, heads, ldkh, d_head) || !rows_apart(tokens, ldv, heads, ldvh, d_head)) return RESQ_ERR_SHAPE;
+    const int rc = make_pages_args(a, done, k, ldk, ldkh, v, ldv, ldvh, tokens, heads, d_head, r, slots, k_pages, v_pages, num_pages,
+                                   page_size, page_stride, head_stride, row_stride);
+    if (rc != RESQ_OK || done) return rc;
+    const int64_t rows = tokens * heads;
+#define RESQ_LAUNCH_GATHER(G)                                                                                             \
+    do {                                                                                                                  \
+        const int64_t blocks = (rows + kKvThreads / G - 1) / (kKvThreads / G);                                      \
+        if (blocks > kInt32Max) return RESQ_ERR_SHAPE;                                                                    \
+        launch(gather_kv_cache_kernel<G>, dim3((unsigned)blocks, 2), dim3(kKvThreads), 0, static_cast<hipStream_t>(stream), a); \
+    } while (0)
+    if (d_head <= 128) RESQ_LAUNCH_GATHER(16);
+    else if (d_head <= 256) RESQ_LAUNCH_GATHER(32);
+    else RESQ_LAUNCH_GATHER(64);
+#undef RESQ_LAUNCH_GATHER
+    return launch_status();
+}
+
+size_t resq_attend_kv_cache_workspace_bytes(int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head) {
+    if (B < 1 || B > 65535 || heads_q < 1 || heads_q > 65535 || heads_k < 1 || heads_q % heads_k || d_head < 8 ||
+        d_head > kAttendMaxHead || d_head % 8)
+        return 0;
+    return 256;
+}
+
+int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head,
+                         int64_t r, const int32_t* lens, const int32_t* block_table, int64_t ld_table, int64_t width,
+                         const void* k_pages, const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride,
+                         int64_t head_stride, int64_t row_stride, float scale, float softcap, int64_t window, void* out,
+                         int64_t ldo, int64_t ldoh, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    const size_t need = resq_attend_kv_cache_workspace_bytes(B, heads_q, heads_k, d_head);
+    if (need == 0 || ldq < 0 || ldqh < 0 || width < 1 || width > kInt32Max || (B > 1 && ld_table < width) || !(scale > 0.0f) ||
+        !isfinite(scale) || !(softcap >= 0.0f) || !isfinite(softcap) || window < 0 || !rows_apart(B, ldo, heads_q, ldoh, d_head))
+        return RESQ_ERR_SHAPE;
+    PagesGeometry g{num_pages, page_size, heads_k, page_stride, head_stride, row_stride};
+    const int rc = check_pages(g, k_pages, v_pages, d_head, r);
+    if (rc != RESQ_OK && rc != RESQ_ERR_NULL && rc != RESQ_ERR_ALIGN) return rc;
+    if (!q || !lens || !block_table || !out || !workspace) return RESQ_ERR_NULL;
+    if (rc != RESQ_OK) return rc;
+    if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lens, 4) || !aligned(block_table, 4) || !aligned(lse, 4) ||
+        !aligned(workspace, 256))
+        return RESQ_ERR_ALIGN;
+    if (workspace_bytes < need) return RESQ_ERR_BUFFER;
+    const int64_t longest = width > kMaxAttendLen / page_size ? kMaxAttendLen : width * page_size;
+    AttendArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.ldq = ldq;
+    a.ldqh = ldqh;
+    a.B = (int)B;
+    a.heads_k = (int)heads_k;
+    a.share = (int)(heads_q / heads_k);
+    a.d = (int)d_head;
+    a.r = (int)r;
+    a.lens = lens;
+    a.table = block_table;
+    a.ld_table = ld_table;
+    a.pages[0] = static_cast<const uint8_t*>(k_pages);
+    a.pages[1] = static_cast<const uint8_t*>(v_pages);
+    a.num_pages = (int)num_pages;
+    a.page_size = (int)page_size;
+    a.page_stride = g.page_stride;
+    a.head_stride = g.head_stride;
+    a.row_stride = g.row_stride;
+    a.max_len = (int)longest;
+    a.window = window < kMaxAttendLen ? (int)window : 0;
+    a.scale = scale;
+    a.softcap = softcap;
+    a.out = static_cast<uint16_t*>(out);
+    a.ldo = ldo;
+    a.ldoh = ldoh;
+    a.lse = lse;
+    launch(attend_kv_cache_kernel, dim3((unsigned)heads_q, (unsigned)B), dim3(kAttendThreads), 0, static_cast<hipStream_t>(stream), a);
+    return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,519 @@
+"""The operators of a generation step on the GPU (plan, position embedding, paged cache, attention) against plain 64-bit
+implementations (generation_util.py) and, where the library has the same arithmetic already, bit for bit against that."""
+import itertools
+import math
+
+import pytest
+import torch
+
+import generation_util as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def rq():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU; there is no CPU fallback")
+    from paper_2412_14363_amd import binding
+    binding.lib()
+    return binding
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+# ---- the plan ----------------------------------------------------------------------------------
+
+def plan_inputs(seed, batch, new, old, page, width_pad=2, cap_pad=5):
+    g = gen(seed)
+    lens = torch.randint(0, old + 1, (batch,), generator=g).tolist()
+    news = torch.randint(0, new + 1, (batch,), generator=g).tolist()
+    held = [-(-n // page) for n in lens]
+    want = [-(-(n + a) // page) for n, a in zip(lens, news)]
+    total = sum(want) + 7
+    ids = torch.randperm(total, generator=g).tolist()
+    width = max(want) + width_pad
+    table, at = [], 0
+    for h in held:
+        table.append(ids[at:at + h] + [-1] * (width - h))
+        at += h
+    return lens, news, ids[at:], table, total, max(1, sum(news) + cap_pad)
+
+
+def run_plan(rq, lens, news, free, taken, table, page, num_pages, cap, out=None):
+    t = ints(table)
+    p = rq.resq_kv_slots(ints(lens), ints(news), ints(free), ints([taken]), t, page, num_pages, out=out, max_tokens=cap)
+    torch.cuda.synchronize()
+    return [x.tolist() for x in (p.lens, p.cu_tokens, p.cu_pages, p.positions, p.slots, t, p.state)]
+
+
+@pytest.mark.parametrize("batch,new,old,page,cap_pad", [
+    (1, 1, 0, 16, 0), (1, 1, 100, 1, 0), (3, 40, 33, 16, 0), (17, 5, 1000, 24, 300), (64, 1, 4000, 16, 0), (255, 3, 70, 7, 1000),
+    (1024, 1, 50, 16, 0), (1025, 2, 20, 16, 9), (5000, 1, 9, 4, 0), (4, 5000, 3000, 64, 1), (2, 40000, 10, 128, 4096), (9, 0, 30, 16, 3)])
+def test_plan(rq, batch, new, old, page, cap_pad):
+    lens, news, free, table, total, cap = plan_inputs(batch + new, batch, new, old, page, cap_pad=cap_pad)
+    got = run_plan(rq, lens, news, free, 2, table, page, total, cap)
+    assert got == list(map(lambda x: [list(r) for r in x] if x and isinstance(x[0], list) else list(x),
+                           plain.plan(lens, news, free, 2, table, page, total, cap)))
+
+
+@pytest.mark.parametrize("fault,status", [("pages", 1), ("width", 2), ("cap", 3), ("len", 4), ("new", 4), ("taken", 4), ("cap+len", 4)])
+def test_plan_refuses_as_a_whole(rq, fault, status):
+    lens, news, free, table, total, cap = plan_inputs(3, 20, 30, 200, 16)
+    taken = 0
+    if fault == "pages":
+        free = free[:sum(-(-(n + a) // 16) - -(-n // 16) for n, a in zip(lens, news)) - 1]
+    if fault == "width":
+        width = max(-(-(n + a) // 16) for n, a in zip(lens, news)) - 1
+        table = [t[:width] for t in table]
+    if "cap" in fault:
+        cap = sum(news) - 1
+    if "len" in fault:
+        lens[7] = -1
+    if fault == "new":
+        news[19] = -5
+    if fault == "taken":
+        taken = -1
+    got = run_plan(rq, lens, news, free, taken, table, 16, total, cap)
+    assert got == [list(x) for x in plain.plan(lens, news, free, taken, table, 16, total, cap)]
+    assert got[6] == [taken, status] and set(got[4]) == {-1} and got[0] == lens
+
+
+def test_plan_sums_do_not_wrap(rq):
+    # 65536 requests of 2^16 new tokens each: 2^32 in all, more than max_tokens, and 0 modulo 2^32
+    n = 65536
+    t = torch.zeros(n, 8, dtype=torch.int32, device=DEV)
+    p = rq.resq_kv_slots(torch.zeros(n, dtype=torch.int32, device=DEV), torch.full((n,), 1 << 16, dtype=torch.int32, device=DEV),
+                         ints([1, 2, 3]), ints([0]), t, 1 << 20, 100, max_tokens=10)
+    assert p.state.tolist() == [0, 3] and p.slots.tolist() == [-1] * 10 and not t.any()
+
+
+def test_plan_goes_on_from_its_own_state(rq):
+    # in place, step after step, as a captured step does it: lens and taken are the outputs of the step before
+    page, batch = 4, 5
+    free, width, total = list(range(60, 0, -1)), 20, 64
+    table = [[-1] * width for _ in range(batch)]
+    lens, taken = [0] * batch, 0
+    t, p = ints(table), rq.KvSlots(batch, 16)
+    news = ints([0] * batch)
+    for step in range(12):
+        add = [(step + b) % 4 for b in range(batch)]
+        news.copy_(ints(add))
+        rq.resq_kv_slots(p.lens, news, ints(free), None, t, page, total, out=p)
+        lens, cu, cp, pos, slots, table, (taken, status) = plain.plan(lens, add, free, taken, table, page, total, 16)
+        assert status == 0 and p.state.tolist() == [taken, 0]
+        assert (p.lens.tolist(), p.cu_tokens.tolist(), p.cu_pages.tolist()) == (lens, cu, cp)
+        assert (p.positions.tolist(), p.slots.tolist(), t.tolist()) == (pos, slots, table)
+
+
+def test_plan_leaves_out_pages_that_do_not_exist(rq):
+    # a table entry and a free page outside [0, num_pages): their tokens get no slot
+    table = [[99, -1, -1], [1, -1, -1]]
+    got = run_plan(rq, [3, 2], [3, 9], [77, 2, -3], 0, table, 4, 5, 12)
+    want = plain.plan([3, 2], [3, 9], [77, 2, -3], 0, table, 4, 5, 12)
+    assert got == [list(x) for x in want]
+    assert got[4][:12] == [-1, -1, -1, 6, 7, 8, 9, 10, 11, -1, -1, -1]
+
+
+# ---- norm and rotation --------------------------------------------------------------------------
+
+def check_rope(rq, x, positions, freq, heads_q, w_q, w_k, interleaved, mscale, out=None, eps=1e-6):
+    before = x.clone()
+    y = rq.resq_rope_heads(x, positions, freq, heads_q=heads_q, w_q=w_q, w_k=w_k, eps=eps, interleaved=interleaved, mscale=mscale, out=out)
+    torch.cuda.synchronize()
+    want, size = plain.rope(before, positions, freq, heads_q, w_q, w_k, eps, interleaved, mscale)
+    # a rounding to bf16, half of torch.finfo(bfloat16).eps; before it in fp32 a sum of d squares (at most 24 roundings on
+    # the way of each term), a root, a quotient, the products, and angles good to 2^-21: 2^-18 of the operands' size
+    off = (y.cpu().double() - want).abs()
+    bad = off > 2.0 ** -8 * want.abs() + 2.0 ** -18 * size + 1e-38
+    assert not bad.any(), (int(bad.sum()), float((off / (size + 1e-30)).max()))
+    return y
+
+
+@pytest.mark.parametrize("d,rot", [(128, 128), (128, 64), (64, 64), (256, 256), (96, 96), (80, 32), (512, 512), (128, 0), (64, 10), (34, 34),
+                                   (2, 2), (128, 16), (200, 8), (72, 24)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+def test_rope(rq, d, rot, interleaved, norm):
+    for tokens, hq, hk in ((1, 4, 1), (37, 3, 2), (5, 0, 2), (6, 7, 0), (130, 32, 8)):
+        g = gen(tokens * d + rot)
+        x = torch.randn(tokens, hq + hk, d, generator=g).to(torch.bfloat16).to(DEV)
+        w = [(1 + 0.3 * torch.randn(d, generator=g)).to(torch.bfloat16).to(DEV) for _ in range(2)] if norm else [None, None]
+        pos = torch.randint(0, 100000, (tokens,), generator=g, dtype=torch.int32).to(DEV)
+        freq = rq.resq_rope_frequencies(rot, base=500000.0)[0] if rot else None
+        check_rope(rq, x, pos, freq, hq, w[0], w[1], interleaved, 1.25)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rope_at_far_positions(rq, interleaved):
+    # the angle of the fastest pair at 2^31 - 1 is 2^31 radians: in fp32 nothing of it would be left
+    x = torch.randn(9, 3, 64, generator=gen(1)).to(torch.bfloat16).to(DEV)
+    pos = ints([0, 1, -1, 1 << 20, (1 << 24) + 1, 2147483647, -2147483648, 1234567891, 31415926])
+    check_rope(rq, x, pos, rq.resq_rope_frequencies(64)[0], 2, None, None, interleaved, 1.0)
+
+
+@pytest.mark.parametrize("d,rot", [(128, 128), (96, 40), (66, 66)])
+@pytest.mark.parametrize("interleaved,norm", [(False, True), (True, False)])
+def test_rope_layouts(rq, d, rot, interleaved, norm):
+    # heads of a wider projection, head-major memory, broadcast input, unaligned rows, in place: the rest of each buffer stays
+    g = gen(d)
+    freq, mscale = rq.resq_rope_frequencies(rot, scaling="ramp", factor=8.0, low=1.0, high=32.0, original_len=4096)
+    w = [(1 + 0.3 * torch.randn(d, generator=g)).to(torch.bfloat16).to(DEV) for _ in range(2)] if norm else [None, None]
+    tokens, heads = 21, 6
+    pos = torch.randint(0, 30000, (tokens,), generator=g, dtype=torch.int32).to(DEV)
+    for shift, order in itertools.product((0, 1, 8), ("token", "head", "same", "expand")):
+        width = 9 * d + shift
+        flat = torch.randn(tokens, width, generator=g).to(torch.bfloat16).to(DEV)
+        x = flat[:, shift:shift + heads * d].unflatten(1, (heads, d))
+        buf = torch.full((heads, tokens, d + shift), 7.0, dtype=torch.bfloat16, device=DEV)
+        if order == "token":
+            y = check_rope(rq, x, pos, freq, 4, *w, interleaved, mscale)
+            assert y.is_contiguous()
+        elif order == "head":
+            check_rope(rq, x, pos, freq, 4, *w, interleaved, mscale, out=buf.transpose(0, 1)[..., shift:])
+            assert bool((buf[..., :shift] == 7).all())
+        elif order == "same":
+            keep = flat.clone()
+            check_rope(rq, x, pos, freq, 4, *w, interleaved, mscale, out=x)
+            assert torch.equal(flat[:, :shift], keep[:, :shift]) and torch.equal(flat[:, shift + heads * d:], keep[:, shift + heads * d:])
+        else:
+            check_rope(rq, x[:, :1].expand(-1, heads, -1), pos, freq, 4, *w, interleaved, mscale)
+
+
+def test_rope_of_zeros_huge_and_no_tokens(rq):
+    freq = rq.resq_rope_frequencies(64)[0]
+    w = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device=DEV)
+    x[1] = 1e18   # the sum of 64 squares is below the largest fp32
+    x[1, :, 1::2] = -1e17
+    check_rope(rq, x, ints([5, 6, 7]), freq, 1, w, w, False, 1.0)
+    assert rq.resq_rope_heads(x[:0], ints([]), freq).shape == (0, 2, 64)
+
+
+# ---- writer and reader ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,r", [(128, 16), (64, 8), (256, 32), (512, 64), (128, 0), (128, 128), (8, 0), (8, 8), (72, 24), (264, 8)])
+@pytest.mark.parametrize("order", ["head", "token"])
+def test_append_and_gather(rq, d, r, order):
+    nb = plain.row_bytes(d, r)
+    for tokens, heads, page, pad in ((1, 1, 1, 0), (5, 3, 16, 4), (67, 8, 24, 0), (300, 2, 7, 12)):
+        g = gen(tokens + d + r)
+        pages = -(-tokens // page) + 3
+        wide = torch.randn(tokens, 2 * heads, d + 8, generator=g).to(torch.bfloat16).to(DEV)
+        wide[0] = 2.5                                   # a constant head: scale 1
+        k, v = wide[:, :heads, :d], wide[:, heads:, :d]
+        buf = [plain.make_pages(g, pages, heads, page, d, r, order, pad) for _ in range(2)]
+        was = [b.clone() for b in buf]
+        slots = torch.randperm(pages * page, generator=g)[:tokens].to(torch.int32)
+        slots[tokens // 2:tokens // 2 + 3] = torch.tensor([-1, pages * page, -2147483648][:max(0, min(3, tokens - tokens // 2))])
+        sl = slots.to(DEV)
+        rq.resq_append_kv_cache(k, v, sl, *buf, r)
+        back = rq.resq_gather_kv_cache(*buf, sl, r, d_head=d)
+        outs = torch.full((2, heads, tokens, d + 8), 9.0, dtype=torch.bfloat16, device=DEV)
+        rq.resq_gather_kv_cache(*buf, sl, r, k=outs[0, ..., :d].transpose(0, 1), v=outs[1, ..., :d].transpose(0, 1))
+        torch.cuda.synchronize()
+        live = [t for t in range(tokens) if 0 <= int(slots[t]) < pages * page]
+        for x, b, w, y, o in zip((k, v), buf, was, back, outs):
+            rows = rq.resq_quantize_kv_cache(x.reshape(-1, d).contiguous(), r)
+            vals = rq.resq_dequantize_kv_cache(rows, d, r).view(tokens, heads, d)
+            want, val = w.clone(), torch.zeros_like(vals)
+            for t in live:
+                want[slots[t] // page, :, slots[t] % page, :nb] = rows.view(tokens, heads, nb)[t]
+                val[t] = vals[t]
+            assert torch.equal(b, want), "the pages differ from the row quantizer's bytes, or other bytes were written"
+            assert torch.equal(y, val) and torch.equal(o[..., :d].transpose(0, 1), val) and bool((o[..., d:] == 9).all())
+
+
+def test_append_and_gather_without_tokens_and_from_broadcast_heads(rq):
+    pages = plain.make_pages(gen(1), 4, 3, 16, 64, 8)
+    was = pages.clone()
+    none = torch.empty(0, 3, 64, dtype=torch.bfloat16, device=DEV)
+    rq.resq_append_kv_cache(none, none, ints([]), pages, pages, 8)
+    assert rq.resq_gather_kv_cache(pages, pages, ints([]), 8, d_head=64)[0].shape == (0, 3, 64)
+    one = torch.randn(5, 1, 64, generator=gen(2)).to(torch.bfloat16).to(DEV)
+    v_pages = pages.clone()
+    rq.resq_append_kv_cache(one.expand(-1, 3, -1), one.expand(-1, 3, -1), ints([0, 17, 5, 63, 9]), pages, v_pages, 8)
+    assert torch.equal(pages[0, 0, 0], pages[0, 2, 0]) and torch.equal(pages, v_pages) and not torch.equal(pages, was)
+
+
+def test_slots_beyond_2_gib(rq):
+    # pages whose byte offsets pass 32 bits: 5 GB apart
+    d, r, page, n = 128, 16, 16, 6
+    nb, stride = plain.row_bytes(d, r), 1 << 30
+    flat = torch.zeros(2, n * stride, dtype=torch.uint8, device=DEV)
+    k_pages, v_pages = (f.as_strided((n, 2, page, nb), (stride, page * nb, nb, 1), f.storage_offset()) for f in flat)
+    x = torch.randn(n * page, 2, d, generator=gen(1)).to(torch.bfloat16).to(DEV)
+    slots = torch.randperm(n * page, generator=gen(2)).to(torch.int32).to(DEV)
+    rq.resq_append_kv_cache(x, -x, slots, k_pages, v_pages, r)
+    back = rq.resq_gather_kv_cache(k_pages, v_pages, slots, r, d_head=d)
+    rows = rq.resq_quantize_kv_cache(x.view(-1, d), r)
+    assert torch.equal(back[0].view(-1, d), rq.resq_dequantize_kv_cache(rows, d, r))
+    q = torch.randn(1, 4, d, generator=gen(3)).to(torch.bfloat16).to(DEV)
+    table = ints([[5, 0, 4, 1, 3, 2]])
+    lse = torch.empty(1, 4, device=DEV)
+    out = rq.resq_attend_kv_cache(q, k_pages, v_pages, ints([n * page - 3]), table, r, lse=lse)
+    near = [p.contiguous() for p in (k_pages, v_pages)]
+    lse2 = torch.empty(1, 4, device=DEV)
+    assert torch.equal(out, rq.resq_attend_kv_cache(q, *near, ints([n * page - 3]), table, r, lse=lse2)) and torch.equal(lse, lse2)
+
+
+# ---- attention -----------------------------------------------------------------------------------
+
+def attend_case(seed, lens, hq, hk, d, r, page, order="head", pad=0, extra_pages=2, poison=True):
+    """q, pages, lens, table of a batch; what no sequence owns of the pages is poisoned with 0xFF (codes at their ends, scales
+    and zero-points NaN)."""
+    g = gen(seed)
+    held = [-(-max(n, 0) // page) for n in lens]
+    total = sum(held) + extra_pages
+    ids = torch.randperm(total, generator=g)
+    table = torch.full((len(lens), max(held) + 1), -1, dtype=torch.int32)
+    pages = [plain.make_pages(g, total, hk, page, d, r, order, pad, device="cpu") for _ in range(2)]
+    used = torch.zeros(total, page, dtype=torch.bool)
+    at = 0
+    for b, h in enumerate(held):
+        table[b, :h] = ids[at:at + h].to(torch.int32)
+        for i in range(h):
+            used[ids[at + i], :min(page, lens[b] - i * page)] = True
+        at += h
+    if poison:
+        for p in pages:
+            p[~used[:, None, :].expand(-1, hk, -1)] = 255
+    q = torch.randn(len(lens), hq, d, generator=g).to(torch.bfloat16)
+    dev = [p.to(DEV) if order == "head" else p.transpose(1, 2).contiguous().to(DEV).transpose(1, 2) for p in pages]
+    return q.to(DEV), dev[0], dev[1], ints(lens), table.to(DEV)
+
+
+def check_attend(rq, q, k_pages, v_pages, lens, table, r, scale=None, softcap=0.0, window=0, **kw):
+    lse = torch.full(q.shape[:2], 7.0, dtype=torch.float32, device=DEV)
+    want, want_lse, tol, tol_lse = plain.attend(q, k_pages, v_pages, lens.tolist(), table, r, q.shape[-1] ** -0.5 if scale is None else scale,
+                                                softcap, window)
+    out = rq.resq_attend_kv_cache(q, k_pages, v_pages, lens, table, r, scale=scale, softcap=softcap, window=window, lse=lse, **kw)
+    torch.cuda.synchronize()
+    got, got_lse = out.cpu().double(), lse.cpu().double()
+    off = (got - want).abs()
+    bad = ~(off <= tol + 2.0 ** -8 * (want.abs() + tol))
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4].tolist(), float(off[bad].max()))
+    empty = want_lse == -math.inf
+    assert torch.equal(empty, got_lse == -math.inf) and not got[empty].any()
+    off = (got_lse - want_lse)[~empty].abs()
+    assert not (~(off <= tol_lse[~empty])).any(), float((off - tol_lse[~empty]).max())
+    return out, lse
+
+
+LENS = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 511, 513, 700, 1025]
+
+
+@pytest.mark.parametrize("page,order", [(16, "head"), (16, "token"), (1, "head"), (7, "head"), (24, "token"), (32, "head"), (48, "head"),
+                                        (64, "head"), (256, "token"), (2048, "head")])
+def test_attend_lengths_and_pages(rq, page, order):
+    check_attend(rq, *attend_case(page, [0] + LENS + [0], 8, 2, 128, 16, page, order), 16)
+
+
+@pytest.mark.parametrize("hq,hk", [(1, 1), (4, 4), (7, 7), (6, 2), (8, 2), (32, 8), (7, 1), (8, 1), (9, 1), (16, 1), (17, 1), (24, 1), (40, 2), (33, 3)])
+def test_attend_head_layouts(rq, hq, hk):
+    for n, lens in enumerate(([1], [129, 0, 40], [1500])):
+        check_attend(rq, *attend_case(hq + n, lens, hq, hk, 128, 16, 16), 16)
+
+
+@pytest.mark.parametrize("d,r", [(128, 0), (128, 8), (128, 24), (128, 32), (128, 64), (128, 120), (128, 128), (64, 8), (64, 0), (64, 64),
+                                 (64, 32), (256, 32), (256, 0), (256, 256), (256, 128), (256, 200), (8, 0), (8, 8), (16, 8), (40, 16), (72, 8),
+                                 (96, 16), (136, 8), (192, 24), (248, 248)])
+@pytest.mark.parametrize("share", [3, 12])
+def test_attend_widths(rq, d, r, share):
+    check_attend(rq, *attend_case(d + r, [37, 0, 300, 1], 2 * share, 2, d, r, 16), r)
+    check_attend(rq, *attend_case(d + r + 1, [77], share, 1, d, r, 24, "token", pad=8), r)
+
+
+@pytest.mark.parametrize("lens", [[5000], [20000, 3], [131072], [4096] * 20, [1] * 300, [100] * 260 + [9000], [0] * 5])
+@pytest.mark.parametrize("share", [1, 8])
+def test_attend_long_and_many(rq, lens, share):
+    hk = 2 if max(lens) < 50000 else 1
+    check_attend(rq, *attend_case(len(lens), lens, hk * share, hk, 64, 8, 64), 8)
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 31, 100, 128, 1000, 1 << 40])
+@pytest.mark.parametrize("softcap", [0.0, 20.0, 0.5])
+def test_attend_window_and_cap(rq, window, softcap):
+    for page, order in ((16, "head"), (24, "token")):
+        check_attend(rq, *attend_case(window % 97, [0] + LENS, 4, 1, 64, 8, page, order), 8, softcap=softcap, window=window)
+
+
+def test_attend_scales(rq):
+    case = attend_case(5, [300, 1, 40], 8, 2, 128, 16, 16)
+    for scale in (1e-6, 0.02, 3.0, 50.0):   # the last: one token holds all the weight
+        check_attend(rq, *case, 16, scale=scale)
+
+
+def test_attend_pages_that_do_not_exist(rq):
+    # entries outside [0, num_pages) take no part, also where that leaves a sequence nothing
+    for page, order in ((16, "head"), (32, "head"), (24, "token"), (1, "head")):
+        q, k, v, lens, table = attend_case(9, [100, 33, 500, 20], 4, 2, 64, 8, page, order)
+        table[0, 1] = -1
+        table[1, :] = k.shape[0]
+        table[2, ::2] = 2147483647
+        table[3, 0] = -2147483648
+        check_attend(rq, q, k, v, lens, table, 8)
+
+
+def test_attend_lengths_outside_the_table(rq):
+    q, k, v, lens, table = attend_case(11, [64, 64, 64], 4, 2, 64, 8, 16, extra_pages=8)
+    table[:, 4] = torch.arange(3, dtype=torch.int32, device=DEV)   # a row names 80 tokens
+    k.copy_(plain.make_pages(gen(1), *k.shape[:3], 64, 8))
+    v.copy_(plain.make_pages(gen(2), *k.shape[:3], 64, 8))
+    check_attend(rq, q, k, v, ints([2147483647, -2147483648, 81]), table, 8)
+
+
+def test_attend_strides(rq):
+    # queries and outputs inside wider rows, out on q, pages with room between rows, heads and pages, a table inside a wider one
+    q, k, v, lens, table = attend_case(12, [333, 0, 64, 2], 8, 2, 128, 16, 16)
+    want, want_lse = check_attend(rq, q, k, v, lens, table, 16)
+    wide = torch.full((4, 11, 131), 3.0, dtype=torch.bfloat16, device=DEV)
+    qs = wide[:, 2:10, 1:129]
+    qs.copy_(q)
+    big = torch.full((4, 9 + table.shape[1]), -7, dtype=torch.int32, device=DEV)
+    big[:, 5:5 + table.shape[1]] = table
+    spread = []
+    for p in (k, v):
+        s = torch.full((p.shape[0] + 1, 3, 20, p.shape[3] + 4), 255, dtype=torch.uint8, device=DEV)
+        s[:-1, :2, :16, :p.shape[3]] = p
+        spread.append(s[:-1, :2, :16])
+    lse = torch.empty(4, 8, device=DEV)
+    args = (qs, *spread, lens, big[:, 5:5 + table.shape[1]], 16)
+    assert torch.equal(rq.resq_attend_kv_cache(*args, lse=lse), want) and torch.equal(lse, want_lse)
+    outs = torch.full((8, 4, 130), 5.0, dtype=torch.bfloat16, device=DEV)
+    rq.resq_attend_kv_cache(*args, out=outs[..., :128].transpose(0, 1))
+    assert torch.equal(outs[..., :128].transpose(0, 1), want) and bool((outs[..., 128:] == 5).all())
+    rq.resq_attend_kv_cache(*args, out=qs)
+    assert torch.equal(qs, want)
+    wide[:, 2:10, 1:129] = 3.0
+    assert bool((wide == 3).all())
+
+
+def test_attend_values_that_are_not_finite(rq):
+    # a NaN or an infinity in a token that is seen reaches the heads that see it, and no others
+    q, k, v, lens, table = attend_case(13, [50, 50, 50], 4, 2, 64, 8, 16)
+    def poke(pages, b, h, t, at, value):
+        nb = plain.row_bytes(64, 8)
+        row = pages[table[b, t // 16], h, t % 16]
+        row[nb - 16 + 4 * at:nb - 12 + 4 * at] = torch.tensor([value], device=DEV).view(torch.uint8)
+    poke(k, 0, 0, 7, 1, float("nan"))     # zero-point of the 8-bit group of a key
+    poke(v, 1, 1, 49, 3, float("inf"))    # zero-point of the 4-bit group of a value
+    out = rq.resq_attend_kv_cache(q, k, v, lens, table, 8).float()
+    assert out[0, :2].isnan().all() and out[0, 2:].isfinite().all()
+    assert out[1, :2].isfinite().all() and out[1, 2:, :8].isfinite().all() and not out[1, 2:, 8:].isfinite().any()
+    assert out[2].isfinite().all()
+
+
+def test_attend_equal_calls_give_equal_bits(rq):
+    case = attend_case(14, [3000, 10, 7777, 0, 128], 16, 4, 128, 16, 32)
+    first = check_attend(rq, *case, 16)
+    work = rq.resq_attend_kv_cache_workspace(5, 16, 4, 128)
+    for fill in (0, 255, 127):
+        work.fill_(fill)   # whatever is left in the workspace
+        lse = torch.empty(5, 16, device=DEV)
+        assert torch.equal(rq.resq_attend_kv_cache(*case, 16, lse=lse, workspace=work), first[0]) and torch.equal(lse, first[1])
+
+
+def test_attend_on_other_streams(rq):
+    case = attend_case(15, [3000, 10, 777], 16, 4, 128, 16, 32)
+    want = check_attend(rq, *case, 16)[0]
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for n in range(8):   # two calls at once, each with a workspace of its own
+        outs.append(torch.empty_like(want))
+        rq.resq_attend_kv_cache(*case, 16, out=outs[-1], stream=side[n % 2])
+    with torch.cuda.stream(side[0]):
+        outs.append(rq.resq_attend_kv_cache(*case, 16))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+# ---- a step of generation ------------------------------------------------------------------------
+
+def test_steps_of_generation(rq):
+    """Prompts, then tokens one by one: plan, norm and rotation, projection onto the cache basis, paged writer, attention, as a
+    program runs them; the single-token step captured and replayed.  Each attention against the 64-bit one on the pages, and the
+    pages against the row quantizer of what the step before it wrote."""
+    batch, hq, hk, d, r, page, steps = 6, 8, 2, 128, 16, 16, 9
+    heads, width, total = hq + hk, 8, 40
+    g = gen(21)
+    free, table, p = torch.randperm(total, generator=g).to(torch.int32).to(DEV), torch.full((batch, width), -1, dtype=torch.int32, device=DEV), None
+    pages = [torch.full((total, hk, page, plain.row_bytes(d, r)), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    freq, mscale = rq.resq_rope_frequencies(d, base=500000.0, scaling="bands", factor=8.0)
+    w = [(1 + 0.2 * torch.randn(d, generator=g)).to(torch.bfloat16).to(DEV) for _ in range(2)]
+    basis = rq.resq_pack_weights(torch.linalg.qr(torch.randn(d, d, generator=g))[0].contiguous().to(torch.bfloat16).to(DEV), d)
+    keys, values = {}, {}   # slot -> row bytes
+
+    def step(qkv, plan, y):
+        rq.resq_rope_heads(qkv[:, :heads], plan.positions, freq, heads_q=hq, w_q=w[0], w_k=w[1], mscale=mscale, out=y)
+        z = rq.resq_project_heads(y.view(-1, d), basis).view(y.shape)
+        rq.resq_append_kv_cache(z[:, hq:], qkv[:, heads:], plan.slots, *pages, r)
+        return z
+
+    def record(plan, z, qkv):
+        for x, rows in ((z[:, hq:], keys), (qkv[:, heads:], values)):
+            got = rq.resq_quantize_kv_cache(x.reshape(-1, d).contiguous(), r).view(len(x), hk, -1)
+            for t, s in enumerate(plan.slots.tolist()):
+                if s >= 0:
+                    rows[s] = got[t]
+
+    def pages_hold(rows, pages):
+        want = torch.full_like(pages, 255)
+        for s, x in rows.items():
+            want[s // page, :, s % page] = x
+        return torch.equal(pages, want)
+
+    # prompts of ragged lengths, one of them empty so far, in one padded batch
+    news = ints([20, 1, 0, 33, 16, 7])
+    first = rq.KvSlots(batch, 90)
+    rq.resq_kv_slots(first.lens, news, free, None, table, page, total, out=first)
+    assert first.state.tolist()[1] == 0
+    qkv = torch.randn(90, heads + hk, d, generator=g).to(torch.bfloat16).to(DEV)
+    record(first, step(qkv, first, torch.empty(90, heads, d, dtype=torch.bfloat16, device=DEV)), qkv)
+    assert pages_hold(keys, pages[0]) and pages_hold(values, pages[1])
+
+    # then a token each: a captured step that goes on from its own lengths
+    p = rq.KvSlots(batch, batch)
+    p.lens.copy_(first.lens)
+    p.state.copy_(first.state)
+    ones, qkv = ints([1] * batch), torch.empty(batch, heads + hk, d, dtype=torch.bfloat16, device=DEV)
+    y, out, lse = torch.empty(batch, heads, d, dtype=torch.bfloat16, device=DEV), torch.empty(batch, hq, d, dtype=torch.bfloat16, device=DEV), \
+        torch.empty(batch, hq, device=DEV)
+    work = rq.resq_attend_kv_cache_workspace(batch, hq, hk, d)
+
+    def token():
+        rq.resq_kv_slots(p.lens, ones, free, None, table, page, total, out=p)
+        z = step(qkv, p, y)
+        rq.resq_attend_kv_cache(z[:, :hq], *pages, p.lens, table, r, out=out, lse=lse, workspace=work)
+        return z
+
+    kept = {k: v.clone() for k, v in (("lens", p.lens), ("state", p.state), ("table", table))}
+    qkv.copy_(torch.randn(qkv.shape, generator=g))
+    token()                                                   # eager once, and back: a captured step must find everything loaded
+    p.lens.copy_(kept["lens"])
+    p.state.copy_(kept["state"])
+    table.copy_(kept["table"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        z = token()
+    for n in range(steps):
+        qkv.copy_(torch.randn(qkv.shape, generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert p.state.tolist()[1] == 0 and p.lens.tolist() == [a + n + 1 for a in (20, 1, 0, 33, 16, 7)]
+        record(p, z, qkv)
+        assert pages_hold(keys, pages[0]) and pages_hold(values, pages[1])
+        replayed, replayed_lse = out.clone(), lse.clone()
+        eager, eager_lse = check_attend(rq, z[:, :hq], *pages, p.lens, table, r)
+        assert torch.equal(eager, replayed) and torch.equal(eager_lse, replayed_lse)
