@@ -83,6 +83,39 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     return RESQ_OK;
 }
 
+// layout of the attention's workspace: units before each sequence, then maxima and sums, then weighted sums of the partial
+// results, two to a workgroup
+struct AttendWorkspace {
+    size_t ml, acc, bytes;
+    int rows;
+};
+AttendWorkspace attend_workspace(int64_t B, int64_t share, int64_t d_head) {
+    AttendWorkspace w;
+    w.rows = (int)(share < kAttendRows ? share : kAttendRows);
+    w.ml = ((size_t)(B + 1) * sizeof(int64_t) + 255) / 256 * 256;
+    w.acc = w.ml + (size_t)2 * kAttendMaxGrid * kAttendRows * 2 * sizeof(float);
+    w.bytes = w.acc + (size_t)2 * kAttendMaxGrid * w.rows * d_head * sizeof(float);
+    return w;
+}
+
+template <int NL, int HT, int OCC>
+int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
+    int lds = kAttendWaves * 2 * kAttendTile * attend_pitch(NL, HT) + kAttendLdsPad;
+    const int red = kAttendWaves * a.rows * a.d * (int)sizeof(float);
+    if (lds < red) lds = red;
+    AttendArgs args = a;
+    args.lds_red = lds;
+    lds += kAttendWaves * kAttendRows * 2 * (int)sizeof(float);
+    void (*kernel)(const AttendArgs) = a.blocks16 ? attend_kv_cache_kernel<NL, HT, true, OCC> : attend_kv_cache_kernel<NL, HT, false, OCC>;
+    if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               lds) != hipSuccess)
+        return RESQ_ERR_HIP;
+    const int64_t grid = units < 256 * OCC ? units : 256 * OCC;
+    launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
+    launch(attend_join_kernel, dim3((unsigned)(a.B * a.heads_k * a.share)), dim3(kAttendThreads), 0, st, args, grid);
+    return launch_status();
+}
+
 }  // namespace
 
 extern "C" {
@@ -214,7 +247,7 @@ size_t resq_attend_kv_cache_workspace_bytes(int64_t B, int64_t heads_q, int64_t 
     if (B < 1 || B > 65535 || heads_q < 1 || heads_q > 65535 || heads_k < 1 || heads_q % heads_k || d_head < 8 ||
         d_head > kAttendMaxHead || d_head % 8)
         return 0;
-    return 256;
+    return attend_workspace(B, heads_q / heads_k, d_head).bytes;
 }
 
 int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head,
@@ -255,6 +288,16 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.page_stride = g.page_stride;
     a.head_stride = g.head_stride;
     a.row_stride = g.row_stride;
+    a.row_bytes = (int)(r + (d_head - r) / 2 + 16);
+    a.qtiles = (a.share + kAttendRows - 1) / kAttendRows;
+    const AttendWorkspace w = attend_workspace(B, a.share, d_head);
+    a.starts = static_cast<int64_t*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.ml);
+    a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.acc);
+    a.rows = w.rows;
+    a.blocks16 = page_size % 16 == 0 && g.row_stride == a.row_bytes && a.row_bytes % 8 == 0 && g.page_stride % 16 == 0 && g.head_stride % 16 == 0 &&
+                 aligned(k_pages, 16) && aligned(v_pages, 16);
+    a.lds_red = 0;
     a.max_len = (int)longest;
     a.window = window < kMaxAttendLen ? (int)window : 0;
     a.scale = scale;
@@ -263,8 +306,17 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.ldo = ldo;
     a.ldoh = ldoh;
     a.lse = lse;
-    launch(attend_kv_cache_kernel, dim3((unsigned)heads_q, (unsigned)B), dim3(kAttendThreads), 0, static_cast<hipStream_t>(stream), a);
-    return launch_status();
+    const int64_t units = B * heads_k * a.qtiles * ((longest + kAttendUnit - 1) / kAttendUnit);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t low = d_head - r;
+    // the smallest kernel that holds the head's two groups of channels
+    if (low == 0) return r <= 64 ? launch_attend<0, 4, 4>(a, units, st) : r <= 128 ? launch_attend<0, 8, 3>(a, units, st)
+                                                                                   : launch_attend<0, 16, 2>(a, units, st);
+    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 4>(a, units, st) : r <= 64 ? launch_attend<4, 4, 4>(a, units, st)
+                                                                                   : launch_attend<4, 16, 2>(a, units, st);
+    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 4>(a, units, st) : r <= 32 ? launch_attend<8, 2, 3>(a, units, st)
+                           : r <= 64 ? launch_attend<8, 4, 3>(a, units, st) : launch_attend<8, 16, 2>(a, units, st);
+    return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 2>(a, units, st);
 }
 
 }  // extern "C"
