@@ -88,6 +88,27 @@ __device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
+// (x & mask) | bits in one instruction: it takes one constant from a scalar register, the other from a vector register, which
+// the compiler does not arrange by itself
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t y;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "s"(mask), "v"(bits));
+    return y;
+}
+// max and sum over the four lanes l % 16 + 16 k: swaps of halves and of rows of 16 lanes
+__device__ __forceinline__ float rows_max(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // cap * tanh(x / cap): by the exponential, or near 0, where that would cancel, by the series (its sixth term is below 2^-24)
 __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
     const float y = x * inv_cap, y2 = y * y;
@@ -221,10 +242,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             ql[s] = (v4u_att){__builtin_amdgcn_perm(p.z, p.x, 0x05040100u), __builtin_amdgcn_perm(p.z, p.x, 0x07060302u),
                               __builtin_amdgcn_perm(p.w, p.y, 0x05040100u), __builtin_amdgcn_perm(p.w, p.y, 0x07060302u)};
         }
-        sum_h += lane_xor<16>(sum_h);
-        sum_h += lane_xor<32>(sum_h);
-        sum_l += lane_xor<16>(sum_l);
-        sum_l += lane_xor<32>(sum_l);
+        sum_h = rows_sum(sum_h);
+        sum_l = rows_sum(sum_l);
 
         v4f_att acch[HT], accl[NL ? NL : 1];
 #pragma unroll
@@ -340,9 +359,13 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             } else {
                 mask = move_rows(tt);
             }
+            const bool full = mask == 0xFFFFFFFFu;
+            if (!full && lane < kAttendTile && !((mask >> lane) & 1)) {   // weights of 0 times what may be anything
+                float* par = reinterpret_cast<float*>(vt + lane * P + par_off);
+                par[0] = par[1] = par[2] = par[3] = 0.0f;
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            const bool full = mask == 0xFFFFFFFFu;
 
             // ---- scores ----
             float x[8];
@@ -353,7 +376,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 sl = (v4f_att){-16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l};
 #pragma unroll
                 for (int s = 0; s < HS; ++s) {
-                    if (32 * s < a.r) {
+                    if (s == 0 || 32 * s < a.r) {
                         const uint32_t* p = reinterpret_cast<const uint32_t*>(krow + 8 * (4 * s + g));
                         const uint32_t c0 = p[0], c1 = p[1];
                         v4u_att o;
@@ -368,17 +391,16 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 for (int s = 0; s < LS; ++s) {
                     const uint32_t c = *reinterpret_cast<const uint32_t*>(krow + a.r + 4 * (4 * s + g));
                     v4u_att o;
-                    o[0] = ((c << 3) & 0x00780078u) | 0x41804180u;
-                    o[1] = ((c >> 1) & 0x00780078u) | 0x41804180u;
-                    o[2] = ((c >> 5) & 0x00780078u) | 0x41804180u;
-                    o[3] = ((c >> 9) & 0x00780078u) | 0x41804180u;
+                    o[0] = and_or(c << 3, 0x00780078u, 0x41804180u);
+                    o[1] = and_or(c >> 1, 0x00780078u, 0x41804180u);
+                    o[2] = and_or(c >> 5, 0x00780078u, 0x41804180u);
+                    o[3] = and_or(c >> 9, 0x00780078u, 0x41804180u);
                     sl = attend_mfma(o, ql[s], sl);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float* par = reinterpret_cast<const float*>(kt + (16 * h + 4 * g + i) * P + par_off);
-                    float v = 0.0f;
-                    if (a.r > 0) v = fmaf(sh[i], par[0], sum_h * par[1]);
+                    float v = fmaf(sh[i], par[0], sum_h * par[1]);
                     if constexpr (NL > 0) v = fmaf(sl[i], par[2], fmaf(sum_l, par[3], v));
                     x[4 * h + i] = v;
                 }
@@ -390,13 +412,12 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             if (!full) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (!((mask >> (16 * (e >> 2) + 4 * g + (e & 3))) & 1)) x[e] = -inf;
+                    if (!(((mask >> (4 * g)) >> (16 * (e >> 2) + (e & 3))) & 1)) x[e] = -inf;
             }
 
             // ---- the running maximum and sum ----
             float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            top = fmaxf(top, lane_xor<16>(top));
-            top = fmaxf(top, lane_xor<32>(top)) * sc2;
+            top = rows_max(top) * sc2;
             if (__builtin_amdgcn_ballot_w64(top > m2) != 0) {
                 const float m_new = fmaxf(m2, top);
                 const float back = m_new == -inf ? 0.0f : __builtin_amdgcn_exp2f(m2 - m_new);
@@ -417,13 +438,11 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 const float p = __builtin_amdgcn_exp2f(fmaf(x[e], sc2, -base));
                 l += p;
                 const float* par = reinterpret_cast<const float*>(vt + row * P + par_off);
-                float v_sh = par[0], v_zh = par[1], v_sl = par[2], v_zl = par[3];
-                if (!full && !((mask >> row) & 1)) v_sh = v_zh = v_sl = v_zl = 0.0f;
-                ph[e] = p * v_sh;
-                pl[e] = p * v_sl;
-                zero_h = fmaf(p, v_zh, zero_h);
+                ph[e] = p * par[0];
+                pl[e] = p * par[2];
+                zero_h = fmaf(p, par[1], zero_h);
                 if (e & 1) zero_h = fmaf(ph[e], 255.0f, zero_h);
-                zero_l = fmaf(pl[e], e & 1 ? 143.0f : -128.0f, fmaf(p, v_zl, zero_l));
+                zero_l = fmaf(pl[e], e & 1 ? 143.0f : -128.0f, fmaf(p, par[3], zero_l));
             }
 
             // ---- weighted sums of the values' codes ----
@@ -437,12 +456,12 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 }
             };
             auto vrow = [&](int e) { return vt + (16 * (e >> 2) + 4 * g + (e & 3)) * P; };
-            if (a.r > 0) {
+            {
                 v4u_att w, w2;
                 weights(ph, w, w2);
 #pragma unroll
                 for (int j = 0; j < HT; ++j) {
-                    if (16 * j < a.r) {
+                    if (j == 0 || 16 * j < a.r) {
                         v4u_att o;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -476,7 +495,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                     for (int j = 0; j < 4; ++j) {
                         v4u_att o;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] = ((two[i] >> (4 * j)) & 0x000F000Fu) | 0xC3004300u;
+                        for (int i = 0; i < 4; ++i) o[i] = and_or(two[i] >> (4 * j), 0x000F000Fu, 0xC3004300u);
                         accl[4 * k + j] = attend_mfma(o, w, accl[4 * k + j]);
                         accl[4 * k + j] = attend_mfma(o, w2, accl[4 * k + j]);
                     }
@@ -487,12 +506,9 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         }
 
         // ---- the four wavefronts' results together ----
-        l += lane_xor<16>(l);
-        l += lane_xor<32>(l);
-        zero_h += lane_xor<16>(zero_h);
-        zero_h += lane_xor<32>(zero_h);
-        zero_l += lane_xor<16>(zero_l);
-        zero_l += lane_xor<32>(zero_l);
+        l = rows_sum(l);
+        zero_h = rows_sum(zero_h);
+        zero_l = rows_sum(zero_l);
         __syncthreads();   // every wavefront is through with its rows
         const int rows = min(a.share - qt * kAttendRows, kAttendRows);
         float* red = reinterpret_cast<float*>(lds);                           // [wave][rows][d]

@@ -312,9 +312,9 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     // the smallest kernel that holds the head's two groups of channels
     if (low == 0) return r <= 64 ? launch_attend<0, 4, 4>(a, units, st) : r <= 128 ? launch_attend<0, 8, 3>(a, units, st)
                                                                                    : launch_attend<0, 16, 2>(a, units, st);
-    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 4>(a, units, st) : r <= 64 ? launch_attend<4, 4, 4>(a, units, st)
+    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 4>(a, units, st) : r <= 64 ? launch_attend<4, 4, 3>(a, units, st)
                                                                                    : launch_attend<4, 16, 2>(a, units, st);
-    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 4>(a, units, st) : r <= 32 ? launch_attend<8, 2, 3>(a, units, st)
+    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 3>(a, units, st) : r <= 32 ? launch_attend<8, 2, 3>(a, units, st)
                            : r <= 64 ? launch_attend<8, 4, 3>(a, units, st) : launch_attend<8, 16, 2>(a, units, st);
     return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 2>(a, units, st);
 }
