@@ -62,7 +62,7 @@ struct AttendArgs {
     uint16_t* out;
     int64_t ldo, ldoh;
     float* lse;
-    int64_t* starts;   // [B + 1]: units before each sequence (workspace)
+    int32_t* joins;    // [B][heads][2]: a head's first partial result, and the workgroup that has its last one (workspace)
     float* part_ml;    // [2 grid][16][2]: maximum (times log2 e) and sum of a partial result's queries (workspace)
     float* part_acc;   // [2 grid][rows][d]: and its weighted sums (workspace)
     int rows;          // queries of a partial result
@@ -88,13 +88,13 @@ __device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-// (x & mask) | bits in one instruction: it takes one constant from a scalar register, the other from a vector register, which
-// the compiler does not arrange by itself
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
-    uint32_t y;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "s"(mask), "v"(bits));
-    return y;
-}
+// Constants of (x & mask) | bits, which is one instruction if one of the two comes from a scalar register and the other from a
+// vector register: left to itself the compiler writes both into two instructions.
+struct CodeBits {
+    uint32_t mask, bits;
+    __device__ __forceinline__ CodeBits(uint32_t m, uint32_t b) : mask(m), bits(b) { asm volatile("" : "+s"(mask), "+v"(bits)); }
+    __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (x & mask) | bits; }
+};
 // max and sum over the four lanes l % 16 + 16 k: swaps of halves and of rows of 16 lanes
 __device__ __forceinline__ float rows_max(float x) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -117,17 +117,22 @@ __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
     return cap * (y2 < 0.0625f ? small : big);
 }
 
-// bytes from row to row in LDS: what the kernel's groups of channels take, so that every address is a lane's base and a
-// constant
-__host__ __device__ constexpr int attend_pitch(int NL, int HT) { return HT * 16 + NL * 8 + 16 < 272 ? HT * 16 + NL * 8 + 16 : 272; }
-
+// Bytes from row to row in LDS: what the kernel's groups of channels take, so that every address is a lane's base and a
+// constant, and 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks.  A row's scales and
+// zero-points are its last 16 bytes there.
+__host__ __device__ constexpr int attend_row(int NL, int HT) { return HT * 16 + NL * 8 + 16 < 272 ? HT * 16 + NL * 8 + 16 : 272; }
+__host__ __device__ constexpr int attend_pitch(int NL, int HT) { return (attend_row(NL, HT) + 15) / 32 * 32 + 16; }
+// a number that all lanes have, in scalar registers
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
 // NL: 4-bit channels of a lane in the second product (16 NL channels in all), HT: 16-channel tiles of the 8-bit group,
 // BLOCKS: 16 rows of a page from a multiple of 16 on are contiguous pieces of 16 bytes
 template <int NL, int HT, bool BLOCKS, int OCC>
 __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(const AttendArgs a) {
     constexpr int LS = NL / 2, HS = (HT + 1) / 2;   // steps of 32 channels of the first product
     constexpr int P = attend_pitch(NL, HT);
-    constexpr int KU = (2 * P + 63) / 64;           // 16-byte pieces of a tile's keys (values) that a lane moves
+    constexpr int KU = (attend_row(NL, HT) + 63) / 64;   // 16-byte pieces of 16 rows that a lane moves
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int64_t part[kAttendWaves], found_start;
     __shared__ int found_b;
@@ -147,7 +152,6 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         if (lane >= k) upto += u;
     }
     if (lane == 63) part[wave] = upto;
-    if (t == 0) found_b = -1;
     __syncthreads();
     int64_t total = 0, before = 0;
     for (int w = 0; w < kAttendWaves; ++w) {
@@ -155,25 +159,26 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         total += part[w];
     }
     int64_t start = before + upto - mine;   // of this thread's first sequence
+    total = uniform64(total);
     const int64_t W = total < (int64_t)gridDim.x ? total : (int64_t)gridDim.x;
     const int64_t w0 = blockIdx.x;
-    int64_t u = w0 < W ? total * w0 / W : 0, u_end = w0 < W ? total * (w0 + 1) / W : 0;
-    if (blockIdx.x == 0 || (u < u_end && start <= u && u < start + mine)) {
+    if (w0 >= W) return;
+    int64_t u = total * w0 / W;
+    const int64_t u_end = total * (w0 + 1) / W;
+    if (start <= u && u < start + mine) {
         for (int b = b0; b < b1; ++b) {
             const int64_t units = (int64_t)attend_units(a, attend_len(a, b)) * heads;
-            if (blockIdx.x == 0) a.starts[b] = start;
-            if (u < u_end && start <= u && u < start + units) {
+            if (u < start + units) {
                 found_b = b;
                 found_start = start;
+                break;
             }
             start += units;
         }
-        if (blockIdx.x == 0 && t == 0) a.starts[a.B] = total;
     }
     __syncthreads();
-    if (u >= u_end) return;
     int b = __builtin_amdgcn_readfirstlane(found_b);
-    int64_t seq_start = found_start;
+    int64_t seq_start = uniform64(found_start);
     const int64_t u_first = u;
 
     const int RB = a.row_bytes, low = a.d - a.r, par_off = a.r + (low >> 1);
@@ -183,14 +188,16 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     if constexpr (BLOCKS) {
 #pragma unroll
         for (int i = 0; i < 2 * KU; ++i) {
-            const int at = (i >> 1) * 1024 + lane * 16 + (i & 1) * 8, row = at / RB;
-            to[i] = row * P + (at - row * RB);
+            const int at = (i >> 1) * 1024 + lane * 16 + (i & 1) * 8, row = at / RB, col = at - row * RB;
+            to[i] = row * P + col + (col < par_off ? 0 : P - 16 - par_off);
         }
     }
     const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
     const float kLog2e = 1.44269504088896340736f;
     const float sc2 = a.softcap > 0.0f ? kLog2e : a.scale * kLog2e;
     const float inf = __builtin_huge_valf();
+
+    const CodeBits key_bits(0x00780078u, 0x41804180u), value_bits(0x000F000Fu, 0xC3004300u);
 
     while (u < u_end) {
         // ---- the next head in the run ----
@@ -253,7 +260,9 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         float m2 = -inf, l = 0.0f, zero_h = 0.0f, zero_l = 0.0f;   // m2: maximum times log2 e
 
         // ---- rows of a tile to LDS ----
-        uint4 kreg[KU], vreg[KU];
+        uint4 kreg[2 * KU], vreg[2 * KU];   // (where a block is not there they keep what they had: codes of some kind)
+#pragma unroll
+        for (int i = 0; i < 2 * KU; ++i) kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
         int64_t entry = 0;        // BLOCKS: offset of block lane % 2 of the wavefront's tile lane / 2, counted from tile0
         bool entry_ok = false;
         int tile0 = t_begin + wave * kAttendTile;
@@ -275,20 +284,20 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         auto load_blocks = [&](int tt) {
             const int at = 2 * ((tt - tile0) / kAttendUnit);
             const uint64_t ok = __builtin_amdgcn_ballot_w64(entry_ok);
-            const int64_t e0 = ((int64_t)__builtin_amdgcn_readlane((int)(entry >> 32), at) << 32) |
-                               (uint32_t)__builtin_amdgcn_readlane((int)entry, at);
-            const int64_t e1 = ((int64_t)__builtin_amdgcn_readlane((int)(entry >> 32), at + 1) << 32) |
-                               (uint32_t)__builtin_amdgcn_readlane((int)entry, at + 1);
             const bool ok0 = (ok >> at) & 1, ok1 = (ok >> (at + 1)) & 1;
 #pragma unroll
-            for (int i = 0; i < KU; ++i) {
-                const int piece = i * 64 + lane;   // RB of them in a block
-                const bool second = piece >= RB;
-                const int64_t off = (second ? e1 : e0) + (piece - (second ? RB : 0)) * 16;
-                kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (piece < 2 * RB && (second ? ok1 : ok0)) {
-                    kreg[i] = *reinterpret_cast<const uint4*>(a.pages[0] + off);
-                    vreg[i] = *reinterpret_cast<const uint4*>(a.pages[1] + off);
+            for (int h = 0; h < 2; ++h) {
+                if (!(h ? ok1 : ok0)) continue;
+                const int64_t e = ((int64_t)__builtin_amdgcn_readlane((int)(entry >> 32), at + h) << 32) |
+                                  (uint32_t)__builtin_amdgcn_readlane((int)entry, at + h);
+                const uint8_t* kp = a.pages[0] + e;
+                const uint8_t* vp = a.pages[1] + e;
+#pragma unroll
+                for (int i = 0; i < KU; ++i) {   // RB pieces in a block
+                    if (i * 64 + lane < RB) {
+                        kreg[h * KU + i] = *reinterpret_cast<const uint4*>(kp + (uint32_t)(i * 1024 + lane * 16));
+                        vreg[h * KU + i] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(i * 1024 + lane * 16));
+                    }
                 }
             }
             return seen(tt) & ((ok0 ? 0x0000FFFFu : 0u) | (ok1 ? 0xFFFF0000u : 0u));
@@ -296,11 +305,15 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         auto store_blocks = [&]() {
 #pragma unroll
             for (int i = 0; i < KU; ++i) {
-                if (i * 64 + lane < 2 * RB) {
-                    *reinterpret_cast<uint2*>(kt + to[2 * i]) = make_uint2(kreg[i].x, kreg[i].y);
-                    *reinterpret_cast<uint2*>(kt + to[2 * i + 1]) = make_uint2(kreg[i].z, kreg[i].w);
-                    *reinterpret_cast<uint2*>(vt + to[2 * i]) = make_uint2(vreg[i].x, vreg[i].y);
-                    *reinterpret_cast<uint2*>(vt + to[2 * i + 1]) = make_uint2(vreg[i].z, vreg[i].w);
+                if (i * 64 + lane < RB) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 k = kreg[h * KU + i], v = vreg[h * KU + i];
+                        *reinterpret_cast<uint2*>(kt + h * 16 * P + to[2 * i]) = make_uint2(k.x, k.y);
+                        *reinterpret_cast<uint2*>(kt + h * 16 * P + to[2 * i + 1]) = make_uint2(k.z, k.w);
+                        *reinterpret_cast<uint2*>(vt + h * 16 * P + to[2 * i]) = make_uint2(v.x, v.y);
+                        *reinterpret_cast<uint2*>(vt + h * 16 * P + to[2 * i + 1]) = make_uint2(v.z, v.w);
+                    }
                 }
             }
         };
@@ -328,10 +341,11 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int word = i + 64 * j + lane, row = word / words;
+                    const int word = i + 64 * j + lane, row = word / words, col = 4 * (word - row * words);
                     if (row < kAttendTile) {
-                        *reinterpret_cast<uint32_t*>(kt + row * P + 4 * (word - row * words)) = kw[j];
-                        *reinterpret_cast<uint32_t*>(vt + row * P + 4 * (word - row * words)) = vw[j];
+                        const int at = row * P + col + (col < par_off ? 0 : P - 16 - par_off);
+                        *reinterpret_cast<uint32_t*>(kt + at) = kw[j];
+                        *reinterpret_cast<uint32_t*>(vt + at) = vw[j];
                     }
                 }
             }
@@ -360,51 +374,65 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 mask = move_rows(tt);
             }
             const bool full = mask == 0xFFFFFFFFu;
-            if (!full && lane < kAttendTile && !((mask >> lane) & 1)) {   // weights of 0 times what may be anything
-                float* par = reinterpret_cast<float*>(vt + lane * P + par_off);
-                par[0] = par[1] = par[2] = par[3] = 0.0f;
+            // For the values' sums a token's zero-points take in the offsets of its codes there; a token that is not seen gets
+            // zeros, since its weight of 0 would not make 0 of what may be anything.
+            if (lane < kAttendTile) {
+                float4* par = reinterpret_cast<float4*>(vt + lane * P + P - 16);
+                float4 v = *par;
+                v.y = fmaf(v.x, lane & 1 ? 255.0f : 0.0f, v.y);
+                v.w = fmaf(v.z, lane & 1 ? 143.0f : -128.0f, v.w);
+                if (!((mask >> lane) & 1)) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                *par = v;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 
+            __builtin_amdgcn_sched_barrier(0);
             // ---- scores ----
             float x[8];
+            v4f_att sh[2], sl[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint8_t* krow = kt + (16 * h + n) * P;
-                v4f_att sh = {0.0f, 0.0f, 0.0f, 0.0f}, sl;
-                sl = (v4f_att){-16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l};
+                sh[h] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
+                sl[h] = (v4f_att){-16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l};
+            }
 #pragma unroll
-                for (int s = 0; s < HS; ++s) {
-                    if (s == 0 || 32 * s < a.r) {
-                        const uint32_t* p = reinterpret_cast<const uint32_t*>(krow + 8 * (4 * s + g));
-                        const uint32_t c0 = p[0], c1 = p[1];
+            for (int s = 0; s < HS; ++s) {
+                if (s == 0 || 32 * s < a.r) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint2 c = *reinterpret_cast<const uint2*>(kt + (16 * h + n) * P + 8 * (4 * s + g));
                         v4u_att o;
-                        o[0] = upper_halves((float)(c0 & 0xFFu), (float)((c0 >> 8) & 0xFFu));
-                        o[1] = upper_halves((float)((c0 >> 16) & 0xFFu), (float)(c0 >> 24));
-                        o[2] = upper_halves((float)(c1 & 0xFFu), (float)((c1 >> 8) & 0xFFu));
-                        o[3] = upper_halves((float)((c1 >> 16) & 0xFFu), (float)(c1 >> 24));
-                        sh = attend_mfma(o, qh[s], sh);
+                        o[0] = upper_halves((float)(c.x & 0xFFu), (float)((c.x >> 8) & 0xFFu));
+                        o[1] = upper_halves((float)((c.x >> 16) & 0xFFu), (float)(c.x >> 24));
+                        o[2] = upper_halves((float)(c.y & 0xFFu), (float)((c.y >> 8) & 0xFFu));
+                        o[3] = upper_halves((float)((c.y >> 16) & 0xFFu), (float)(c.y >> 24));
+                        sh[h] = attend_mfma(o, qh[s], sh[h]);
                     }
                 }
+            }
 #pragma unroll
-                for (int s = 0; s < LS; ++s) {
-                    const uint32_t c = *reinterpret_cast<const uint32_t*>(krow + a.r + 4 * (4 * s + g));
+            for (int s = 0; s < LS; ++s) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t c = *reinterpret_cast<const uint32_t*>(kt + (16 * h + n) * P + a.r + 4 * (4 * s + g));
                     v4u_att o;
-                    o[0] = and_or(c << 3, 0x00780078u, 0x41804180u);
-                    o[1] = and_or(c >> 1, 0x00780078u, 0x41804180u);
-                    o[2] = and_or(c >> 5, 0x00780078u, 0x41804180u);
-                    o[3] = and_or(c >> 9, 0x00780078u, 0x41804180u);
-                    sl = attend_mfma(o, ql[s], sl);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float* par = reinterpret_cast<const float*>(kt + (16 * h + 4 * g + i) * P + par_off);
-                    float v = fmaf(sh[i], par[0], sum_h * par[1]);
-                    if constexpr (NL > 0) v = fmaf(sl[i], par[2], fmaf(sum_l, par[3], v));
-                    x[4 * h + i] = v;
+                    o[0] = key_bits(c << 3);
+                    o[1] = key_bits(c >> 1);
+                    o[2] = key_bits(c >> 5);
+                    o[3] = key_bits(c >> 9);
+                    sl[h] = attend_mfma(o, ql[s], sl[h]);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);   // (here and below: what a later phase reads does not come earlier, for registers)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float4 par = *reinterpret_cast<const float4*>(kt + (16 * (e >> 2) + 4 * g + (e & 3)) * P + P - 16);
+                float v = fmaf(sh[e >> 2][e & 3], par.x, sum_h * par.y);
+                if constexpr (NL > 0) v = fmaf(sl[e >> 2][e & 3], par.z, fmaf(sum_l, par.w, v));
+                x[e] = v;
+            }
+            __builtin_amdgcn_sched_barrier(0);
             if (a.softcap > 0.0f) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = soft_cap(x[e] * a.scale, a.softcap, inv_cap);
@@ -434,17 +462,16 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             float ph[8], pl[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int row = 16 * (e >> 2) + 4 * g + (e & 3);
+                const float4 par = *reinterpret_cast<const float4*>(vt + (16 * (e >> 2) + 4 * g + (e & 3)) * P + P - 16);
                 const float p = __builtin_amdgcn_exp2f(fmaf(x[e], sc2, -base));
                 l += p;
-                const float* par = reinterpret_cast<const float*>(vt + row * P + par_off);
-                ph[e] = p * par[0];
-                pl[e] = p * par[2];
-                zero_h = fmaf(p, par[1], zero_h);
-                if (e & 1) zero_h = fmaf(ph[e], 255.0f, zero_h);
-                zero_l = fmaf(pl[e], e & 1 ? 143.0f : -128.0f, fmaf(p, par[3], zero_l));
+                ph[e] = p * par.x;
+                pl[e] = p * par.z;
+                zero_h = fmaf(p, par.y, zero_h);
+                zero_l = fmaf(p, par.w, zero_l);
             }
 
+            __builtin_amdgcn_sched_barrier(0);
             // ---- weighted sums of the values' codes ----
             auto weights = [&](const float (&p)[8], v4u_att& first, v4u_att& rest) {   // truncation and remainder
 #pragma unroll
@@ -491,14 +518,15 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         two[i] = __builtin_amdgcn_perm(~c[2 * i + 1][k >> 1], c[2 * i][k >> 1], k & 1 ? 0x07060302u : 0x05040100u);
+                    v4u_att o[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        v4u_att o;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] = and_or(two[i] >> (4 * j), 0x000F000Fu, 0xC3004300u);
-                        accl[4 * k + j] = attend_mfma(o, w, accl[4 * k + j]);
-                        accl[4 * k + j] = attend_mfma(o, w2, accl[4 * k + j]);
+                        for (int i = 0; i < 4; ++i) o[j][i] = value_bits(two[i] >> (4 * j));
+                        accl[4 * k + j] = attend_mfma(o[j], w, accl[4 * k + j]);
                     }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) accl[4 * k + j] = attend_mfma(o[j], w2, accl[4 * k + j]);
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -534,8 +562,14 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                     if ((4 * g + i) * NL + j < low_end) row[a.r + (4 * g + i) * NL + j] = accl[j][i] + zero_l;
         }
         __syncthreads();
+        // a head in one piece is done; a piece of one is partial result 0 of its workgroup, or 1 behind another head
         const bool whole = n_units == units;
         const int64_t slot = 2 * w0 + (u != u_first);
+        if (t == 0) {
+            int32_t* join = a.joins + ((int64_t)b * heads + head) * 2;
+            if (first_unit == 0) join[0] = (int32_t)slot;
+            if (first_unit + n_units == units) join[1] = (int32_t)w0;
+        }
         const int pairs = a.d >> 1;
         for (int e = t; e < rows * pairs; e += kAttendThreads) {
             const int row = e / pairs, ch = 2 * (e - row * pairs);
@@ -572,31 +606,27 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     }
 }
 
-// Joins the partial results of the heads that several workgroups had (grid: the first kernel's), one workgroup to a query; and
-// writes the queries of sequences without tokens.
-__global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a, int64_t grid) {
-    __shared__ float weight[kAttendMaxGrid], red[kAttendThreads], part[2 * kAttendWaves];
+// Joins the partial results of the heads that several workgroups had, one workgroup to a query; and writes the queries of
+// sequences without tokens.
+__global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a) {
+    __shared__ float weight[kAttendMaxGrid], part[2 * kAttendWaves];
+    __shared__ float4 red[kAttendThreads];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int qhead = blockIdx.x % (a.heads_k * a.share), b = blockIdx.x / (a.heads_k * a.share);
+    const int heads_q = a.heads_k * a.share;
+    const int b = blockIdx.x / heads_q, qhead = blockIdx.x - b * heads_q;
     const int hk = qhead / a.share, qi = qhead - hk * a.share, qt = qi / kAttendRows, row = qi - qt * kAttendRows;
-    const int64_t total = a.starts[a.B], start = a.starts[b];
-    const int heads = a.heads_k * a.qtiles;
-    const int64_t units = (a.starts[b + 1] - start) / heads;
+    const int32_t* join = a.joins + ((int64_t)b * a.heads_k * a.qtiles + hk * a.qtiles + qt) * 2;
+    const int slot0 = join[0], w_last = join[1];   // (nobody wrote them for a sequence without tokens)
     uint16_t* dst = a.out + b * a.ldo + qhead * a.ldoh;
     const float inf = __builtin_huge_valf();
-    if (units == 0) {
+    if (attend_len(a, b) == 0) {
         for (int c = t; c < a.d; c += kAttendThreads) dst[c] = 0;
         if (t == 0 && a.lse) a.lse[blockIdx.x] = -inf;
         return;
     }
-    const int64_t W = total < grid ? total : grid;
-    const int64_t u0 = start + (int64_t)(hk * a.qtiles + qt) * units, u1 = u0 + units;
-    // the workgroup that has unit u: the last w with total * w / W <= u
-    const int64_t w_first = ((u0 + 1) * W - 1) / total, w_last = (u1 * W - 1) / total;
-    if (w_first == w_last) return;
-    const int count = (int)(w_last - w_first) + 1;
-    // a workgroup's first head is its partial result 0, its last one (if another) 1
-    auto slot = [&](int i) { return 2 * (w_first + i) + (i == 0 && total * w_first / W != u0 ? 1 : 0); };
+    const int w_first = slot0 >> 1, count = w_last - w_first + 1;
+    if (count == 1) return;
+    auto slot = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (w_first + i)); };
     float top = -inf;
     for (int i = t; i < count; i += kAttendThreads) {
         weight[i] = a.part_ml[(slot(i) * kAttendRows + row) * 2];
@@ -617,19 +647,42 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     if (lane == 0) part[kAttendWaves + wave] = sum;
     __syncthreads();
     sum = (part[kAttendWaves] + part[kAttendWaves + 1]) + (part[kAttendWaves + 2] + part[kAttendWaves + 3]);
-    // channels over the threads, what threads are left over the partial results
-    const int wide = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256, groups = kAttendThreads / wide;
-    const int ch = t & (wide - 1), group = t / wide;
-    float o = 0.0f;
-    if (ch < a.d) {
-        for (int i = group; i < count; i += groups) o = fmaf(weight[i], a.part_acc[(slot(i) * a.rows + row) * a.d + ch], o);
+    // four channels to a thread, what threads are left over the partial results, four of which are on their way at a time
+    const int fours = a.d >> 2, groups = kAttendThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (group < groups) {
+        for (int i = group; i < count; i += 4 * groups) {
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = min(i + k * groups, count - 1);
+                v[k] = *reinterpret_cast<const float4*>(a.part_acc + (slot(j) * a.rows + row) * a.d + ch);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = i + k * groups < count ? weight[i + k * groups] : 0.0f;
+                if (f != 0.0f) {   // (a workgroup that saw nothing)
+                    o.x = fmaf(f, v[k].x, o.x);
+                    o.y = fmaf(f, v[k].y, o.y);
+                    o.z = fmaf(f, v[k].z, o.z);
+                    o.w = fmaf(f, v[k].w, o.w);
+                }
+            }
+        }
     }
     red[t] = o;
     __syncthreads();
-    if (t < a.d) {
-        float v = 0.0f;
-        for (int k = 0; k < groups; ++k) v += red[k * wide + t];
-        dst[t] = (uint16_t)pack_bf16_pair(sum == 0.0f ? 0.0f : v / sum, 0.0f);
+    if (t < fours) {
+        for (int k = 1; k < groups; ++k) {
+            const float4 v = red[k * fours + t];
+            o.x += v.x;
+            o.y += v.y;
+            o.z += v.z;
+            o.w += v.w;
+        }
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        Piece8 p{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
+        *reinterpret_cast<Piece8*>(dst + 4 * t) = p;
         if (t == 0 && a.lse) a.lse[blockIdx.x] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
     }
 }

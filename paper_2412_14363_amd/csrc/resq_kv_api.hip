@@ -83,16 +83,17 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     return RESQ_OK;
 }
 
-// layout of the attention's workspace: units before each sequence, then maxima and sums, then weighted sums of the partial
-// results, two to a workgroup
+// layout of the attention's workspace: where each head's partial results are, then their maxima and sums, then their weighted
+// sums, two results to a workgroup
 struct AttendWorkspace {
     size_t ml, acc, bytes;
     int rows;
 };
-AttendWorkspace attend_workspace(int64_t B, int64_t share, int64_t d_head) {
+AttendWorkspace attend_workspace(int64_t B, int64_t heads_k, int64_t share, int64_t d_head) {
     AttendWorkspace w;
     w.rows = (int)(share < kAttendRows ? share : kAttendRows);
-    w.ml = ((size_t)(B + 1) * sizeof(int64_t) + 255) / 256 * 256;
+    const size_t heads = (size_t)B * heads_k * ((share + kAttendRows - 1) / kAttendRows);
+    w.ml = (heads * 2 * sizeof(int32_t) + 255) / 256 * 256;
     w.acc = w.ml + (size_t)2 * kAttendMaxGrid * kAttendRows * 2 * sizeof(float);
     w.bytes = w.acc + (size_t)2 * kAttendMaxGrid * w.rows * d_head * sizeof(float);
     return w;
@@ -112,7 +113,7 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
         return RESQ_ERR_HIP;
     const int64_t grid = units < 256 * OCC ? units : 256 * OCC;
     launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
-    launch(attend_join_kernel, dim3((unsigned)(a.B * a.heads_k * a.share)), dim3(kAttendThreads), 0, st, args, grid);
+    launch(attend_join_kernel, dim3((unsigned)(a.B * a.heads_k * a.share)), dim3(kAttendThreads), 0, st, args);
     return launch_status();
 }
 
@@ -247,7 +248,7 @@ size_t resq_attend_kv_cache_workspace_bytes(int64_t B, int64_t heads_q, int64_t 
     if (B < 1 || B > 65535 || heads_q < 1 || heads_q > 65535 || heads_k < 1 || heads_q % heads_k || d_head < 8 ||
         d_head > kAttendMaxHead || d_head % 8)
         return 0;
-    return attend_workspace(B, heads_q / heads_k, d_head).bytes;
+    return attend_workspace(B, heads_k, heads_q / heads_k, d_head).bytes;
 }
 
 int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head,
@@ -290,8 +291,8 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.row_stride = g.row_stride;
     a.row_bytes = (int)(r + (d_head - r) / 2 + 16);
     a.qtiles = (a.share + kAttendRows - 1) / kAttendRows;
-    const AttendWorkspace w = attend_workspace(B, a.share, d_head);
-    a.starts = static_cast<int64_t*>(workspace);
+    const AttendWorkspace w = attend_workspace(B, heads_k, a.share, d_head);
+    a.joins = static_cast<int32_t*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.ml);
     a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.acc);
     a.rows = w.rows;
@@ -314,7 +315,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
                                                                                    : launch_attend<0, 16, 2>(a, units, st);
     if (low <= 64) return r <= 16 ? launch_attend<4, 1, 4>(a, units, st) : r <= 64 ? launch_attend<4, 4, 3>(a, units, st)
                                                                                    : launch_attend<4, 16, 2>(a, units, st);
-    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 3>(a, units, st) : r <= 32 ? launch_attend<8, 2, 3>(a, units, st)
+    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 3>(a, units, st)
                            : r <= 64 ? launch_attend<8, 4, 3>(a, units, st) : launch_attend<8, 16, 2>(a, units, st);
     return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 2>(a, units, st);
 }
