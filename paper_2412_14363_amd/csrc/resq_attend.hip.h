@@ -8,15 +8,17 @@
 // out of the sums:
 //   q . k_t = s_h (q_h . c_h) + z_h sum(q_h) + s_l (q_l . c_l) + z_l sum(q_l)
 //   sum_t p_t v_t = sum_t (p_t s_t) c_t + sum_t p_t z_t, for each group of channels
-// Queries of one K/V head are the columns of both products; a wavefront takes 32 tokens at a time.
-//   S (tokens x queries) = K codes x Q: lane l ends with query l % 16 and tokens 4 (l / 16) + i and 16 + those, i < 4
-//   O (channels x queries) += V codes^T x P: its operand P wants of lane l query l % 16 and any eight tokens, which the codes
-//   of V are then taken of too: the eight it has.  Softmax weights never move between lanes.
+// A wavefront takes 32 tokens of one K/V head at a time:
+//   S (queries x tokens) = Q x K codes^T: with up to 8 queries (Q = 8) both halves of the 16 rows hold them, the upper for the
+//   first 16 tokens and the lower for the others, so that a lane ends with one token and four queries, and the softmax works
+//   on no empty lane where queries are 8; with up to 16 (Q = 16) a lane has two tokens
+//   O (channels x queries) += V codes^T x P: the weights P go through LDS to where this product wants them, as two bf16
+//   numbers each, a truncation and its remainder (16 bits in all, so that the output's rounding to bf16 is the one that
+//   counts): with up to 8 queries in the two halves of the columns, else in two products
 // A 4-bit code becomes a bf16 number by being put under the leading bits of 16 (keys) or 128 (values): one shift and one
-// and-or for two codes.  The constants leave again: 16 sum(q) with the accumulator's start; for values every second token has
-// the code's complement and the opposite sign, c + 128 and c - 143, so that the sums stay small, and what remains is a sum of
-// weights.  P goes in as two bf16 numbers, a truncation and its remainder (16 bits in all, so that the output's rounding to
-// bf16 is the one that counts).
+// and-or for two codes.  The constants leave again with the zero-points, once per token; for values every second token has
+// the code's complement and the opposite sign, c + 128 and c - 143, so that the sums stay small.
+// The maximum is looked at again only when a score is 2^8 times what it allows: sums of weights up to 2^8 lose nothing.
 //
 // The work is cut into units of 128 tokens of one head (four wavefronts, 32 tokens each); all units of the call in a row are
 // dealt to the workgroups in runs of equal length, whatever the sequences' lengths are (they are read on the GPU).  A head
@@ -40,6 +42,9 @@ constexpr int kAttendTile = 32;                              // tokens of a wave
 constexpr int kAttendUnit = kAttendTile * kAttendWaves;      // tokens of a unit
 constexpr int kAttendMaxGrid = 1024;
 constexpr int kAttendRows = 16;                              // queries of a workgroup at most
+constexpr int kAttendPRow = 80;                              // bytes of a row of weights in LDS: 32 in bf16, and what keeps rows on other banks
+constexpr float kAttendNone = -3.0e38f;                      // the maximum of no scores: finite, so that differences stay numbers
+constexpr float kAttendSlack = 8.0f;                         // of the running maximum, in powers of two
 constexpr int kAttendLdsPad = 512;                           // reads of whole pieces go this far behind the last row at most
 
 typedef float v4f_att __attribute__((ext_vector_type(4)));
@@ -122,16 +127,21 @@ __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
 // zero-points are its last 16 bytes there.
 __host__ __device__ constexpr int attend_row(int NL, int HT) { return HT * 16 + NL * 8 + 16 < 272 ? HT * 16 + NL * 8 + 16 : 272; }
 __host__ __device__ constexpr int attend_pitch(int NL, int HT) { return (attend_row(NL, HT) + 15) / 32 * 32 + 16; }
+__host__ __device__ constexpr int attend_tiles_bytes(int NL, int HT) {
+    return kAttendWaves * 2 * kAttendTile * attend_pitch(NL, HT) + kAttendLdsPad;
+}
+__host__ __device__ constexpr int attend_weights_bytes(int Q) { return 2 * 2 * Q * kAttendPRow; }   // of a wavefront
 // a number that all lanes have, in scalar registers
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
     return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 // NL: 4-bit channels of a lane in the second product (16 NL channels in all), HT: 16-channel tiles of the 8-bit group,
-// BLOCKS: 16 rows of a page from a multiple of 16 on are contiguous pieces of 16 bytes
-template <int NL, int HT, bool BLOCKS, int OCC>
+// Q: queries that fit, 8 or 16, BLOCKS: 16 rows of a page from a multiple of 16 on are contiguous pieces of 16 bytes
+template <int NL, int HT, int Q, bool BLOCKS, int OCC>
 __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(const AttendArgs a) {
     constexpr int LS = NL / 2, HS = (HT + 1) / 2;   // steps of 32 channels of the first product
     constexpr int P = attend_pitch(NL, HT);
+    constexpr int NT = Q / 8;                       // tokens of a lane in the softmax
     constexpr int KU = (attend_row(NL, HT) + 63) / 64;   // 16-byte pieces of 16 rows that a lane moves
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int64_t part[kAttendWaves], found_start;
@@ -184,6 +194,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     const int RB = a.row_bytes, low = a.d - a.r, par_off = a.r + (low >> 1);
     uint8_t* kt = lds + wave * (2 * kAttendTile * P);
     uint8_t* vt = kt + kAttendTile * P;
+    uint8_t* pt = lds + attend_tiles_bytes(NL, HT) + wave * attend_weights_bytes(Q);   // weights: 8-bit group's, 4-bit group's
     int to[2 * KU];   // where the halves of a lane's pieces go
     if constexpr (BLOCKS) {
 #pragma unroll
@@ -219,18 +230,18 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         const int32_t* table = a.table + b * a.ld_table;
 
         // ---- queries: operands of the first product, and their sums over both groups of channels ----
-        const int qi = qt * kAttendRows + n;   // among the queries of the K/V head
+        const int qi = qt * kAttendRows + (n & (Q - 1));   // among the queries of the K/V head
         const bool q_live = qi < a.share;
         const uint16_t* qrow = a.q + b * a.ldq + (int64_t)(hk * a.share + (q_live ? qi : 0)) * a.ldqh;
         v4u_att qh[HS], ql[LS ? LS : 1];
-        int r_here = a.r, low_here = low;
-        asm volatile("" : "+s"(r_here), "+s"(low_here));
+        int h_here = a.r - 8 * g, l_here = low - 8 * g;
+        asm volatile("" : "+v"(h_here), "+v"(l_here));
         float sum_h = 0.0f, sum_l = 0.0f;
 #pragma unroll
         for (int s = 0; s < HS; ++s) {
             const int ch = 8 * (4 * s + g);
             qh[s] = (v4u_att){0u, 0u, 0u, 0u};
-            if (q_live && ch < r_here) {
+            if (q_live && 32 * s < h_here) {
                 const Piece16 p = *reinterpret_cast<const Piece16*>(qrow + ch);
                 qh[s] = (v4u_att){p.x, p.y, p.z, p.w};
             }
@@ -241,7 +252,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         for (int s = 0; s < LS; ++s) {
             const int ch = 8 * (4 * s + g);
             Piece16 p{0u, 0u, 0u, 0u};
-            if (q_live && ch < low_here) p = *reinterpret_cast<const Piece16*>(qrow + a.r + ch);
+            if (q_live && 32 * s < l_here) p = *reinterpret_cast<const Piece16*>(qrow + a.r + ch);
             const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum_l += __uint_as_float(w[i] << 16) + __uint_as_float(w[i] & 0xFFFF0000u);
@@ -249,15 +260,30 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             ql[s] = (v4u_att){__builtin_amdgcn_perm(p.z, p.x, 0x05040100u), __builtin_amdgcn_perm(p.z, p.x, 0x07060302u),
                               __builtin_amdgcn_perm(p.w, p.y, 0x05040100u), __builtin_amdgcn_perm(p.w, p.y, 0x07060302u)};
         }
+        // the sums of a lane's own four queries: what lane 4 g + i (Q = 8: 4 (g & 1) + i) has summed
         sum_h = rows_sum(sum_h);
         sum_l = rows_sum(sum_l);
+        const int own = Q == 8 ? 4 * (g & 1) : 4 * g;
+        float qsum_h[4], qsum_l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            qsum_h[i] = __shfl(sum_h, own + i);
+            qsum_l[i] = __shfl(sum_l, own + i);
+        }
 
         v4f_att acch[HT], accl[NL ? NL : 1];
 #pragma unroll
         for (int j = 0; j < HT; ++j) acch[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < NL; ++j) accl[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
-        float m2 = -inf, l = 0.0f, zero_h = 0.0f, zero_l = 0.0f;   // m2: maximum times log2 e
+        // of the own four queries: running maximum times log2 e, sum of weights, and weighted sums of zero-points, the last three
+        // over the own tokens
+        float m2[4], l[4], zero_h[4], zero_l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m2[i] = kAttendNone;
+            l[i] = zero_h[i] = zero_l[i] = 0.0f;
+        }
 
         // ---- rows of a tile to LDS ----
         uint4 kreg[2 * KU], vreg[2 * KU];   // (where a block is not there they keep what they had: codes of some kind)
@@ -373,41 +399,63 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             } else {
                 mask = move_rows(tt);
             }
-            const bool full = mask == 0xFFFFFFFFu;
-            // For the values' sums a token's zero-points take in the offsets of its codes there; a token that is not seen gets
-            // zeros, since its weight of 0 would not make 0 of what may be anything.
-            if (lane < kAttendTile) {
-                float4* par = reinterpret_cast<float4*>(vt + lane * P + P - 16);
-                float4 v = *par;
-                v.y = fmaf(v.x, lane & 1 ? 255.0f : 0.0f, v.y);
-                v.w = fmaf(v.z, lane & 1 ? 143.0f : -128.0f, v.w);
-                if (!((mask >> lane) & 1)) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                *par = v;
-            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 
-            __builtin_amdgcn_sched_barrier(0);
-            // ---- scores ----
-            float x[8];
-            v4f_att sh[2], sl[2];
+            // ---- what the tile's work reads of LDS, asked for at once (values' codes only where they leave registers for it) ----
+            constexpr bool kEarly = HT <= 2;
+            uint2 kh[2][HS];
+            uint32_t kl[2][LS ? LS : 1];
+            float4 kpar[NT], vpar[NT];
+            uint32_t vh[8][kEarly ? HT : 1], vl[8][NL < 8 ? 1 : NL / 8];
+            auto vrow = [&](int e) { return vt + (16 * (e >> 2) + 4 * g + (e & 3)) * P; };
+            auto own_token = [&](int h) { return Q == 8 ? 16 * (g >> 1) + n : 16 * h + n; };   // of the softmax
+            auto read_low = [&](uint32_t (&c)[NL < 8 ? 1 : NL / 8], int e) {
+                const uint8_t* p = vrow(e) + a.r + n * (NL / 2);
+                if constexpr (NL == 4) c[0] = *reinterpret_cast<const uint16_t*>(p);
+                else
+#pragma unroll
+                    for (int k = 0; k < NL / 8; ++k) c[k] = reinterpret_cast<const uint32_t*>(p)[k];
+            };
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                sh[h] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
-                sl[h] = (v4f_att){-16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l, -16.0f * sum_l};
+                const uint8_t* row = kt + (16 * h + n) * P;
+#pragma unroll
+                for (int s = 0; s < HS; ++s) kh[h][s] = *reinterpret_cast<const uint2*>(row + 8 * (4 * s + g));
+#pragma unroll
+                for (int s = 0; s < LS; ++s) kl[h][s] = *reinterpret_cast<const uint32_t*>(row + a.r + 4 * (4 * s + g));
             }
+#pragma unroll
+            for (int h = 0; h < NT; ++h) {
+                kpar[h] = *reinterpret_cast<const float4*>(kt + own_token(h) * P + P - 16);
+                vpar[h] = *reinterpret_cast<const float4*>(vt + own_token(h) * P + P - 16);
+            }
+            if constexpr (kEarly) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                    for (int j = 0; j < HT; ++j) vh[e][j] = vrow(e)[16 * j + n];
+                    if constexpr (NL > 0) read_low(vl[e], e);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+
+            // ---- scores ----
+            v4f_att sh[2], sl[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sh[h] = sl[h] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int s = 0; s < HS; ++s) {
                 if (s == 0 || 32 * s < a.r) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint2 c = *reinterpret_cast<const uint2*>(kt + (16 * h + n) * P + 8 * (4 * s + g));
+                        const uint2 c = kh[h][s];
                         v4u_att o;
                         o[0] = upper_halves((float)(c.x & 0xFFu), (float)((c.x >> 8) & 0xFFu));
                         o[1] = upper_halves((float)((c.x >> 16) & 0xFFu), (float)(c.x >> 24));
                         o[2] = upper_halves((float)(c.y & 0xFFu), (float)((c.y >> 8) & 0xFFu));
                         o[3] = upper_halves((float)((c.y >> 16) & 0xFFu), (float)(c.y >> 24));
-                        sh[h] = attend_mfma(o, qh[s], sh[h]);
+                        sh[h] = attend_mfma(qh[s], o, sh[h]);
                     }
                 }
             }
@@ -415,109 +463,155 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             for (int s = 0; s < LS; ++s) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t c = *reinterpret_cast<const uint32_t*>(kt + (16 * h + n) * P + a.r + 4 * (4 * s + g));
+                    const uint32_t c = kl[h][s];
                     v4u_att o;
                     o[0] = key_bits(c << 3);
                     o[1] = key_bits(c >> 1);
                     o[2] = key_bits(c >> 5);
                     o[3] = key_bits(c >> 9);
-                    sl[h] = attend_mfma(o, ql[s], sl[h]);
+                    sl[h] = attend_mfma(ql[s], o, sl[h]);
                 }
             }
-            __builtin_amdgcn_sched_barrier(0);   // (here and below: what a later phase reads does not come earlier, for registers)
+            float x[NT][4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float4 par = *reinterpret_cast<const float4*>(kt + (16 * (e >> 2) + 4 * g + (e & 3)) * P + P - 16);
-                float v = fmaf(sh[e >> 2][e & 3], par.x, sum_h * par.y);
-                if constexpr (NL > 0) v = fmaf(sl[e >> 2][e & 3], par.z, fmaf(sum_l, par.w, v));
-                x[e] = v;
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if (a.softcap > 0.0f) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = soft_cap(x[e] * a.scale, a.softcap, inv_cap);
-            }
-            if (!full) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (!(((mask >> (4 * g)) >> (16 * (e >> 2) + (e & 3))) & 1)) x[e] = -inf;
-            }
-
-            // ---- the running maximum and sum ----
-            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            top = rows_max(top) * sc2;
-            if (__builtin_amdgcn_ballot_w64(top > m2) != 0) {
-                const float m_new = fmaxf(m2, top);
-                const float back = m_new == -inf ? 0.0f : __builtin_amdgcn_exp2f(m2 - m_new);
-                m2 = m_new;
-                l *= back;
-                zero_h *= back;
-                zero_l *= back;
-#pragma unroll
-                for (int j = 0; j < HT; ++j) acch[j] *= back;
-#pragma unroll
-                for (int j = 0; j < NL; ++j) accl[j] *= back;
-            }
-            const float base = m2 == -inf ? 0.0f : m2;
-            float ph[8], pl[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float4 par = *reinterpret_cast<const float4*>(vt + (16 * (e >> 2) + 4 * g + (e & 3)) * P + P - 16);
-                const float p = __builtin_amdgcn_exp2f(fmaf(x[e], sc2, -base));
-                l += p;
-                ph[e] = p * par.x;
-                pl[e] = p * par.z;
-                zero_h = fmaf(p, par.y, zero_h);
-                zero_l = fmaf(p, par.w, zero_l);
-            }
-
-            __builtin_amdgcn_sched_barrier(0);
-            // ---- weighted sums of the values' codes ----
-            auto weights = [&](const float (&p)[8], v4u_att& first, v4u_att& rest) {   // truncation and remainder
+            for (int h = 0; h < NT; ++h) {
+                const float4 par = kpar[h];
+                const float z = fmaf(par.z, -16.0f, par.w);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p0 = p[2 * i], p1 = p[2 * i + 1];
-                    first[i] = upper_halves(p0, p1);
-                    rest[i] = upper_halves(p0 - __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u),
-                                           p1 - __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u));
+                    const float dh = Q == 8 ? (g & 2 ? sh[1][i] : sh[0][i]) : sh[h][i];
+                    float v = fmaf(dh, par.x, qsum_h[i] * par.y);
+                    if constexpr (NL > 0) {
+                        const float dl = Q == 8 ? (g & 2 ? sl[1][i] : sl[0][i]) : sl[h][i];
+                        v = fmaf(dl, par.z, fmaf(qsum_l[i], z, v));
+                    }
+                    x[h][i] = v;
                 }
-            };
-            auto vrow = [&](int e) { return vt + (16 * (e >> 2) + 4 * g + (e & 3)) * P; };
+            }
+            if (a.softcap > 0.0f) {
+#pragma unroll
+                for (int h = 0; h < NT; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[h][i] = soft_cap(x[h][i] * a.scale, a.softcap, inv_cap);
+            }
+            if (mask != 0xFFFFFFFFu) {   // what is not seen has no weight, and its constants may be anything
+#pragma unroll
+                for (int h = 0; h < NT; ++h) {
+                    const bool there = (mask >> own_token(h)) & 1;
+                    vpar[h].x = there ? vpar[h].x : 0.0f;
+                    vpar[h].y = there ? vpar[h].y : 0.0f;
+                    vpar[h].z = there ? vpar[h].z : 0.0f;
+                    vpar[h].w = there ? vpar[h].w : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[h][i] = there ? x[h][i] : -inf;
+                }
+            }
+            float over[NT][4];   // by how many powers of two a score is over the maximum
+            bool rise = false;
+#pragma unroll
+            for (int h = 0; h < NT; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    over[h][i] = fmaf(x[h][i], sc2, -m2[i]);
+                    rise |= over[h][i] > kAttendSlack;
+                }
+
+            // ---- the running maximum, where it has to rise ----
+            if (__builtin_amdgcn_ballot_w64(rise) != 0) {
+                float back[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float top = x[0][i];
+                    if constexpr (NT == 2) top = fmaxf(top, x[1][i]);
+                    top = fmaxf(top, lane_xor<1>(top));
+                    top = fmaxf(top, lane_xor<2>(top));
+                    top = fmaxf(top, lane_xor<4>(top));
+                    top = fmaxf(top, lane_xor<8>(top));
+                    if constexpr (Q == 8) top = fmaxf(top, lane_xor<32>(top));
+                    const float m_new = fmaxf(m2[i], top * sc2);
+                    back[i] = __builtin_amdgcn_exp2f(m2[i] - m_new);
+                    m2[i] = m_new;
+#pragma unroll
+                    for (int h = 0; h < NT; ++h) over[h][i] = fmaf(x[h][i], sc2, -m_new);
+                    l[i] *= back[i];
+                    zero_h[i] *= back[i];
+                    zero_l[i] *= back[i];
+                }
+                // the factor of query n (Q = 8: n % 8), from a lane that has it among its own
+                const int from_lane = Q == 8 ? 16 * ((n >> 2) & 1) : 16 * (n >> 2);
+                const float f0 = __shfl(back[0], from_lane), f1 = __shfl(back[1], from_lane);
+                const float f2 = __shfl(back[2], from_lane), f3 = __shfl(back[3], from_lane);
+                const float f = n & 2 ? (n & 1 ? f3 : f2) : (n & 1 ? f1 : f0);
+#pragma unroll
+                for (int j = 0; j < HT; ++j) acch[j] *= f;
+#pragma unroll
+                for (int j = 0; j < NL; ++j) accl[j] *= f;
+            }
+
+            // ---- weights, times both groups' scales, to LDS; zero-points take in the codes' offsets ----
+#pragma unroll
+            for (int h = 0; h < NT; ++h) {
+                const float4 par = vpar[h];
+                const float zh = fmaf(par.x, n & 1 ? 255.0f : 0.0f, par.y), zl = fmaf(par.z, n & 1 ? 143.0f : -128.0f, par.w);
+                // as the second product counts tokens: 4 g + i, i < 4, then 16 more
+                const int tok = own_token(h), pos = 8 * ((tok >> 2) & 3) + 4 * (tok >> 4) + (tok & 3);
+                uint8_t* dst = pt + own * kAttendPRow + 2 * pos;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(over[h][i]);
+                    l[i] += p;
+                    zero_h[i] = fmaf(p, zh, zero_h[i]);
+                    zero_l[i] = fmaf(p, zl, zero_l[i]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {   // the 8-bit group's rows, then the 4-bit group's: truncations, then remainders
+                        const uint32_t w = __float_as_uint(p * (k ? par.z : par.x));
+                        const uint32_t rest = __float_as_uint(__uint_as_float(w) - __uint_as_float(w & 0xFFFF0000u));
+                        *reinterpret_cast<uint16_t*>(dst + (2 * Q * k + i) * kAttendPRow) = (uint16_t)(w >> 16);
+                        *reinterpret_cast<uint16_t*>(dst + (2 * Q * k + Q + i) * kAttendPRow) = (uint16_t)(rest >> 16);
+                    }
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+
+            // ---- weighted sums of the values' codes ----
+            const v4u_att* pw = reinterpret_cast<const v4u_att*>(pt + n * kAttendPRow + 16 * g);
+            constexpr int kPart = Q * kAttendPRow / 16;   // from truncations to remainders (Q = 8: they are this product's columns 8 to 15)
             {
-                v4u_att w, w2;
-                weights(ph, w, w2);
+                const v4u_att w = pw[0];
 #pragma unroll
                 for (int j = 0; j < HT; ++j) {
                     if (j == 0 || 16 * j < a.r) {
                         v4u_att o;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint32_t c0 = vrow(2 * i)[16 * j + n], c1 = vrow(2 * i + 1)[16 * j + n];
+                            uint32_t c0, c1;
+                            if constexpr (kEarly) {
+                                c0 = vh[2 * i][j];
+                                c1 = vh[2 * i + 1][j];
+                            } else {
+                                c0 = vrow(2 * i)[16 * j + n];
+                                c1 = vrow(2 * i + 1)[16 * j + n];
+                            }
                             o[i] = upper_halves((float)c0, (float)(c1 ^ 255u)) ^ 0x80000000u;
                         }
                         acch[j] = attend_mfma(o, w, acch[j]);
-                        acch[j] = attend_mfma(o, w2, acch[j]);
+                        if constexpr (Q == 16) acch[j] = attend_mfma(o, pw[kPart], acch[j]);
                     }
                 }
             }
             if constexpr (NL > 0) {
-                v4u_att w, w2;
-                weights(pl, w, w2);
-                uint32_t c[8][NL < 8 ? 1 : NL / 8];   // a lane's codes of each token
+                const v4u_att w = pw[2 * kPart];
+                if constexpr (!kEarly) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint8_t* p = vrow(e) + a.r + n * (NL / 2);
-                    if constexpr (NL == 4) c[e][0] = *reinterpret_cast<const uint16_t*>(p);
-                    else
-#pragma unroll
-                        for (int k = 0; k < NL / 8; ++k) c[e][k] = reinterpret_cast<const uint32_t*>(p)[k];
+                    for (int e = 0; e < 8; ++e) read_low(vl[e], e);
                 }
 #pragma unroll
                 for (int k = 0; k < NL / 4; ++k) {   // four channels at a time: half a dword of two tokens in one
                     uint32_t two[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        two[i] = __builtin_amdgcn_perm(~c[2 * i + 1][k >> 1], c[2 * i][k >> 1], k & 1 ? 0x07060302u : 0x05040100u);
+                        two[i] = __builtin_amdgcn_perm(~vl[2 * i + 1][k >> 1], vl[2 * i][k >> 1], k & 1 ? 0x07060302u : 0x05040100u);
                     v4u_att o[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -525,8 +619,10 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                         for (int i = 0; i < 4; ++i) o[j][i] = value_bits(two[i] >> (4 * j));
                         accl[4 * k + j] = attend_mfma(o[j], w, accl[4 * k + j]);
                     }
+                    if constexpr (Q == 16) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) accl[4 * k + j] = attend_mfma(o[j], w2, accl[4 * k + j]);
+                        for (int j = 0; j < 4; ++j) accl[4 * k + j] = attend_mfma(o[j], pw[3 * kPart], accl[4 * k + j]);
+                    }
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -534,32 +630,53 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         }
 
         // ---- the four wavefronts' results together ----
-        l = rows_sum(l);
-        zero_h = rows_sum(zero_h);
-        zero_l = rows_sum(zero_l);
-        __syncthreads();   // every wavefront is through with its rows
-        const int rows = min(a.share - qt * kAttendRows, kAttendRows);
-        float* red = reinterpret_cast<float*>(lds);                           // [wave][rows][d]
-        float* ml = reinterpret_cast<float*>(lds + a.lds_red);                // [wave][16][2]
-        // (limits of their own: comparisons with the ones above would be made once, for all heads, and kept in too many registers)
-        int r_end = a.r, low_end = low;
-        asm volatile("" : "+s"(r_end), "+s"(low_end));
-        if (n < rows) {
-            float* row = red + (wave * rows + n) * a.d;
-            if (g == 0) {
-                ml[(wave * kAttendRows + n) * 2] = m2;
-                ml[(wave * kAttendRows + n) * 2 + 1] = l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                float& v = k == 0 ? l[i] : k == 1 ? zero_h[i] : zero_l[i];
+                v += lane_xor<1>(v);
+                v += lane_xor<2>(v);
+                v += lane_xor<4>(v);
+                v += lane_xor<8>(v);
+                if constexpr (Q == 8) v += lane_xor<32>(v);
             }
+        }
+        if constexpr (Q == 8) {
 #pragma unroll
             for (int j = 0; j < HT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (16 * j + 4 * g + i < r_end) row[16 * j + 4 * g + i] = acch[j][i] + zero_h;
+                for (int i = 0; i < 4; ++i) acch[j][i] += lane_xor<8>(acch[j][i]);
+#pragma unroll
+            for (int j = 0; j < NL; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) accl[j][i] += lane_xor<8>(accl[j][i]);
+        }
+        __syncthreads();   // every wavefront is through with its rows
+        const int rows = min(a.share - qt * kAttendRows, kAttendRows);
+        float* red = reinterpret_cast<float*>(lds);                           // [wave][rows][d]
+        float4* ml = reinterpret_cast<float4*>(lds + a.lds_red);              // [wave][16]: maximum, sum, zero-points' sums
+        if (n == 0 && (Q == 16 || g < 2)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ml[wave * kAttendRows + own + i] = make_float4(m2[i], l[i], zero_h[i], zero_l[i]);
+        }
+        // both groups have a multiple of 8 channels, so that four in a row from a multiple of 4 on are of one group or of none.
+        // (What the limits are is kept from the compiler: it would take the comparisons out of the loop, each in registers.)
+        int h_left = a.r - 4 * g, l_left = low - 4 * g * NL;
+        asm volatile("" : "+v"(h_left), "+v"(l_left));
+        if (n < Q && n < rows) {
+            float* row = red + (wave * rows + n) * a.d;
+#pragma unroll
+            for (int j = 0; j < HT; ++j) {
+                if (16 * j < h_left) *reinterpret_cast<v4f_att*>(row + 16 * j + 4 * g) = acch[j];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < NL; ++j)
-                    if ((4 * g + i) * NL + j < low_end) row[a.r + (4 * g + i) * NL + j] = accl[j][i] + zero_l;
+                for (int j = 0; j < NL; j += 4) {
+                    const v4f_att o = {accl[j][i], accl[j + 1][i], accl[j + 2][i], accl[j + 3][i]};
+                    if (i * NL + j < l_left) *reinterpret_cast<v4f_att*>(row + a.r + (4 * g + i) * NL + j) = o;
+                }
         }
         __syncthreads();
         // a head in one piece is done; a piece of one is partial result 0 of its workgroup, or 1 behind another head
@@ -573,16 +690,16 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         const int pairs = a.d >> 1;
         for (int e = t; e < rows * pairs; e += kAttendThreads) {
             const int row = e / pairs, ch = 2 * (e - row * pairs);
-            float top = -inf, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
+            float top = kAttendNone, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, ml[(w * kAttendRows + row) * 2]);
-            const float base = top == -inf ? 0.0f : top;
+            for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, ml[w * kAttendRows + row].x);
 #pragma unroll
             for (int w = 0; w < kAttendWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(ml[(w * kAttendRows + row) * 2] - base);
-                sum = fmaf(f, ml[(w * kAttendRows + row) * 2 + 1], sum);
-                o0 = fmaf(f, red[(w * rows + row) * a.d + ch], o0);
-                o1 = fmaf(f, red[(w * rows + row) * a.d + ch + 1], o1);
+                const float4 v = ml[w * kAttendRows + row];
+                const float f = __builtin_amdgcn_exp2f(v.x - top), z = ch < a.r ? v.z : v.w;
+                sum = fmaf(f, v.y, sum);
+                o0 = fmaf(f, red[(w * rows + row) * a.d + ch] + z, o0);
+                o1 = fmaf(f, red[(w * rows + row) * a.d + ch + 1] + z, o1);
             }
             const int64_t qhead = hk * a.share + qt * kAttendRows + row;
             if (whole) {
@@ -627,7 +744,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     const int w_first = slot0 >> 1, count = w_last - w_first + 1;
     if (count == 1) return;
     auto slot = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (w_first + i)); };
-    float top = -inf;
+    float top = kAttendNone;
     for (int i = t; i < count; i += kAttendThreads) {
         weight[i] = a.part_ml[(slot(i) * kAttendRows + row) * 2];
         top = fmaxf(top, weight[i]);
@@ -636,10 +753,9 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     if (lane == 0) part[wave] = top;
     __syncthreads();
     top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    const float base = top == -inf ? 0.0f : top;
     float sum = 0.0f;
     for (int i = t; i < count; i += kAttendThreads) {
-        const float f = __builtin_amdgcn_exp2f(weight[i] - base);
+        const float f = __builtin_amdgcn_exp2f(weight[i] - top);
         weight[i] = f;
         sum = fmaf(f, a.part_ml[(slot(i) * kAttendRows + row) * 2 + 1], sum);
     }

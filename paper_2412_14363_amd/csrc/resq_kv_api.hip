@@ -101,13 +101,16 @@ AttendWorkspace attend_workspace(int64_t B, int64_t heads_k, int64_t share, int6
 
 template <int NL, int HT, int OCC>
 int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
-    int lds = kAttendWaves * 2 * kAttendTile * attend_pitch(NL, HT) + kAttendLdsPad;
+    const int Q = a.share <= 8 ? 8 : 16;
+    int lds = attend_tiles_bytes(NL, HT) + kAttendWaves * attend_weights_bytes(Q);
     const int red = kAttendWaves * a.rows * a.d * (int)sizeof(float);
     if (lds < red) lds = red;
     AttendArgs args = a;
     args.lds_red = lds;
-    lds += kAttendWaves * kAttendRows * 2 * (int)sizeof(float);
-    void (*kernel)(const AttendArgs) = a.blocks16 ? attend_kv_cache_kernel<NL, HT, true, OCC> : attend_kv_cache_kernel<NL, HT, false, OCC>;
+    lds += kAttendWaves * kAttendRows * (int)sizeof(float4);
+    void (*kernel)(const AttendArgs);
+    if (Q == 8) kernel = a.blocks16 ? attend_kv_cache_kernel<NL, HT, 8, true, OCC> : attend_kv_cache_kernel<NL, HT, 8, false, OCC>;
+    else kernel = a.blocks16 ? attend_kv_cache_kernel<NL, HT, 16, true, OCC> : attend_kv_cache_kernel<NL, HT, 16, false, OCC>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
@@ -311,12 +314,12 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t low = d_head - r;
     // the smallest kernel that holds the head's two groups of channels
-    if (low == 0) return r <= 64 ? launch_attend<0, 4, 4>(a, units, st) : r <= 128 ? launch_attend<0, 8, 3>(a, units, st)
+    if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
                                                                                    : launch_attend<0, 16, 2>(a, units, st);
-    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 4>(a, units, st) : r <= 64 ? launch_attend<4, 4, 3>(a, units, st)
+    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 2>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
                                                                                    : launch_attend<4, 16, 2>(a, units, st);
-    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 3>(a, units, st)
-                           : r <= 64 ? launch_attend<8, 4, 3>(a, units, st) : launch_attend<8, 16, 2>(a, units, st);
+    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
+                           : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 2>(a, units, st);
     return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 2>(a, units, st);
 }
 
