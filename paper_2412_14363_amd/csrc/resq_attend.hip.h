@@ -100,13 +100,7 @@ struct CodeBits {
     __device__ __forceinline__ CodeBits(uint32_t m, uint32_t b) : mask(m), bits(b) { asm volatile("" : "+s"(mask), "+v"(bits)); }
     __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (x & mask) | bits; }
 };
-// max and sum over the four lanes l % 16 + 16 k: swaps of halves and of rows of 16 lanes
-__device__ __forceinline__ float rows_max(float x) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
+// sum over the four lanes l % 16 + 16 k: swaps of rows of 16 lanes and of halves
 __device__ __forceinline__ float rows_sum(float x) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
@@ -122,86 +116,125 @@ __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
     return cap * (y2 < 0.0625f ? small : big);
 }
 
-// Bytes from row to row in LDS: what the kernel's groups of channels take, so that every address is a lane's base and a
-// constant, and 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks.  A row's scales and
-// zero-points are its last 16 bytes there.
-__host__ __device__ constexpr int attend_row(int NL, int HT) { return HT * 16 + NL * 8 + 16 < 272 ? HT * 16 + NL * 8 + 16 : 272; }
-__host__ __device__ constexpr int attend_pitch(int NL, int HT) { return (attend_row(NL, HT) + 15) / 32 * 32 + 16; }
+// A row comes to LDS in pieces of 16 bytes: its codes (the last of their pieces may hold a part of what follows them, or be
+// there in vain: codes of some kind, which meet zeros or are not written out), and the 16 bytes of its scales and zero-points.
+// The pitch of rows in LDS is a constant, so that every address is a lane's base and a constant, with the constants last, and
+// 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks.
+__host__ __device__ constexpr int attend_pieces(int NL, int HT) { return HT * 16 + NL * 8 < 256 ? (HT * 16 + NL * 8) / 16 + 1 : 17; }
+__host__ __device__ constexpr int attend_pitch(int NL, int HT) { return (attend_pieces(NL, HT) | 1) * 16; }
 __host__ __device__ constexpr int attend_tiles_bytes(int NL, int HT) {
     return kAttendWaves * 2 * kAttendTile * attend_pitch(NL, HT) + kAttendLdsPad;
 }
 __host__ __device__ constexpr int attend_weights_bytes(int Q) { return 2 * 2 * Q * kAttendPRow; }   // of a wavefront
-// a number that all lanes have, in scalar registers
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-    return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+__device__ __forceinline__ int64_t lane_of64(int64_t x, int lane) {
+    return ((int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+// inclusive sums over the lanes of a wavefront
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast:15
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast:31
+    return x;
+}
+// sum and maximum over a row of 16 lanes (quad permutes, then mirrors: what they exchange is alike in the halves by then)
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row_sum16(float x) {
+    x += dpp<0xB1>(x);
+    x += dpp<0x4E>(x);
+    x += dpp<0x141>(x);
+    return x + dpp<0x140>(x);
+}
+__device__ __forceinline__ float row_max16(float x) {
+    x = fmaxf(x, dpp<0xB1>(x));
+    x = fmaxf(x, dpp<0x4E>(x));
+    x = fmaxf(x, dpp<0x141>(x));
+    return fmaxf(x, dpp<0x140>(x));
+}
+// with lane l ^ 32
+__device__ __forceinline__ float halves_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float halves_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 // NL: 4-bit channels of a lane in the second product (16 NL channels in all), HT: 16-channel tiles of the 8-bit group,
-// Q: queries that fit, 8 or 16, BLOCKS: 16 rows of a page from a multiple of 16 on are contiguous pieces of 16 bytes
+// Q: queries that fit, 8 or 16, BLOCKS: pages of a multiple of 16 rows, so that 16 tokens in a row from a multiple of 16 on are one
+// page's
 template <int NL, int HT, int Q, bool BLOCKS, int OCC>
 __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(const AttendArgs a) {
     constexpr int LS = NL / 2, HS = (HT + 1) / 2;   // steps of 32 channels of the first product
     constexpr int P = attend_pitch(NL, HT);
     constexpr int NT = Q / 8;                       // tokens of a lane in the softmax
-    constexpr int KU = (attend_row(NL, HT) + 63) / 64;   // 16-byte pieces of 16 rows that a lane moves
+    constexpr int PL = attend_pieces(NL, HT);
+    constexpr int KU = (kAttendTile * PL + 63) / 64;     // pieces of a tile's keys (values) that a lane moves
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ int64_t part[kAttendWaves], found_start;
-    __shared__ int found_b;
+    __shared__ int part[kAttendWaves], found[3];
 
     const int t = threadIdx.x, lane = t & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int heads = a.heads_k * a.qtiles;   // heads' query tiles of a sequence
 
     // ---- the run of units that is this workgroup's ----
-    const int per = (a.B + kAttendThreads - 1) / kAttendThreads;
+    const int per = (a.B + kAttendThreads - 1) / kAttendThreads;   // sequences of a thread, in a row
     const int b0 = min(t * per, a.B), b1 = min(b0 + per, a.B);
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += (int64_t)attend_units(a, attend_len(a, b)) * heads;
-    int64_t upto = mine;
-    for (int k = 1; k < 64; k <<= 1) {
-        const int64_t u = __shfl_up(upto, k);
-        if (lane >= k) upto += u;
+    int mine = 0, len_b = 0;
+    for (int b = b0; b < b1; ++b) {
+        len_b = attend_len(a, b);
+        mine += attend_units(a, len_b) * heads;
     }
+    int upto = wave_scan(mine);
     if (lane == 63) part[wave] = upto;
     __syncthreads();
-    int64_t total = 0, before = 0;
+    int total = 0, before = 0;
+#pragma unroll
     for (int w = 0; w < kAttendWaves; ++w) {
         if (w == wave) before = total;
         total += part[w];
     }
-    int64_t start = before + upto - mine;   // of this thread's first sequence
-    total = uniform64(total);
-    const int64_t W = total < (int64_t)gridDim.x ? total : (int64_t)gridDim.x;
-    const int64_t w0 = blockIdx.x;
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int W = min(total, (int)gridDim.x), w0 = blockIdx.x;
     if (w0 >= W) return;
-    int64_t u = total * w0 / W;
-    const int64_t u_end = total * (w0 + 1) / W;
+    const int share = total / W, rest = total - share * W;   // the first `rest` runs are a unit longer
+    int u = w0 * share + min(w0, rest);
+    const int u_end = u + share + (w0 < rest), u_first = u;
+    int start = before + upto - mine;   // of this thread's first sequence
     if (start <= u && u < start + mine) {
         for (int b = b0; b < b1; ++b) {
-            const int64_t units = (int64_t)attend_units(a, attend_len(a, b)) * heads;
+            if (per > 1) len_b = attend_len(a, b);
+            const int units = attend_units(a, len_b) * heads;
             if (u < start + units) {
-                found_b = b;
-                found_start = start;
+                found[0] = b;
+                found[1] = start;
+                found[2] = len_b;
                 break;
             }
             start += units;
         }
     }
     __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane(found_b);
-    int64_t seq_start = uniform64(found_start);
-    const int64_t u_first = u;
+    int b = __builtin_amdgcn_readfirstlane(found[0]), seq_start = __builtin_amdgcn_readfirstlane(found[1]);
+    int len = __builtin_amdgcn_readfirstlane(found[2]);
 
-    const int RB = a.row_bytes, low = a.d - a.r, par_off = a.r + (low >> 1);
+    const int RB = a.row_bytes, low = a.d - a.r;
     uint8_t* kt = lds + wave * (2 * kAttendTile * P);
     uint8_t* vt = kt + kAttendTile * P;
     uint8_t* pt = lds + attend_tiles_bytes(NL, HT) + wave * attend_weights_bytes(Q);   // weights: 8-bit group's, 4-bit group's
-    int to[2 * KU];   // where the halves of a lane's pieces go
-    if constexpr (BLOCKS) {
+    // a lane's pieces: the row, what is in front of it in the row, and where it goes
+    int piece_row[KU], piece_off[KU], piece_to[KU];
 #pragma unroll
-        for (int i = 0; i < 2 * KU; ++i) {
-            const int at = (i >> 1) * 1024 + lane * 16 + (i & 1) * 8, row = at / RB, col = at - row * RB;
-            to[i] = row * P + col + (col < par_off ? 0 : P - 16 - par_off);
-        }
+    for (int i = 0; i < KU; ++i) {
+        const int k = i * 64 + lane, row = k / PL, col = k - row * PL;
+        piece_row[i] = min(row, kAttendTile - 1);
+        piece_off[i] = (BLOCKS ? (row & 15) * (int)a.row_stride : 0) + (col < PL - 1 ? min(16 * col, RB - 16) : RB - 16);
+        piece_to[i] = piece_row[i] * P + (col < PL - 1 ? 16 * col : P - 16);
     }
     const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
     const float kLog2e = 1.44269504088896340736f;
@@ -212,16 +245,15 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 
     while (u < u_end) {
         // ---- the next head in the run ----
-        const int len = __builtin_amdgcn_readfirstlane(attend_len(a, b));
-        const int units = attend_units(a, len);
-        const int64_t seq_units = (int64_t)units * heads;
+        const int units = attend_units(a, len), seq_units = units * heads;
         if (u >= seq_start + seq_units) {
             seq_start += seq_units;
             ++b;
+            len = __builtin_amdgcn_readfirstlane(attend_len(a, b));
             continue;
         }
-        const int head = (int)((u - seq_start) / units), first_unit = (int)((u - seq_start) - (int64_t)head * units);
-        const int n_units = (int)(units - first_unit < u_end - u ? units - first_unit : u_end - u);
+        const int head = (u - seq_start) / units, first_unit = (u - seq_start) - head * units;
+        const int n_units = min(units - first_unit, u_end - u);
         const int hk = head / a.qtiles, qt = head - hk * a.qtiles;
         const int t_low = attend_first(a, len), from = t_low & ~(kAttendTile - 1);
         const int t_begin = from + first_unit * kAttendUnit;
@@ -229,30 +261,122 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         const int64_t head_off = hk * a.head_stride;
         const int32_t* table = a.table + b * a.ld_table;
 
+        v4f_att acch[HT], accl[NL ? NL : 1];
+#pragma unroll
+        for (int j = 0; j < HT; ++j) acch[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NL; ++j) accl[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
+        // of the own four queries: running maximum times log2 e, sum of weights, and weighted sums of zero-points, the last three
+        // over the own tokens
+        float m2[4], l[4], zero_h[4], zero_l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m2[i] = kAttendNone;
+            l[i] = zero_h[i] = zero_l[i] = 0.0f;
+        }
+
+        // ---- rows of a tile to LDS, by way of registers, a tile ahead ----
+        uint4 kreg[KU], vreg[KU];   // (where a row is not there they keep what they had: codes of some kind)
+#pragma unroll
+        for (int i = 0; i < KU; ++i) kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
+        int tile0 = t_begin + wave * kAttendTile;
+        // BLOCKS: lane l has the offset of block l % 2 of the wavefront's tile l / 2, counted from tile0.  Else it has the page of
+        // row l % 32 of the tile that is loaded next.
+        int64_t entry = 0;
+        bool entry_ok = false;
+        int page = -1;
+        auto load_entries = [&](int tile) {
+            const int tok = tile + (lane >> 1) * kAttendUnit + (lane & 1) * 16;
+            page = -1;
+            if (tok < t_end) page = table[tok / a.page_size];
+        };
+        auto set_entries = [&](int tile) {
+            const int tok = tile + (lane >> 1) * kAttendUnit + (lane & 1) * 16;
+            entry_ok = (unsigned)page < (unsigned)a.num_pages;
+            entry = entry_ok ? page * a.page_stride + (tok % a.page_size) * a.row_stride + head_off : 0;
+        };
+        auto load_page = [&](int tile) {
+            const int tok = tile + (lane & 31);
+            page = -1;
+            if (tok >= t_low && tok < t_end) page = table[tok / a.page_size];
+        };
+        // the tokens of a tile that are there and seen
+        auto seen = [&](int tile) {
+            const int left = len - tile, skip = t_low - tile;
+            uint32_t mask = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u;
+            if (skip > 0) mask &= 0xFFFFFFFFu << skip;
+            return mask;
+        };
+        // asks for a tile's pieces; returns the mask of its tokens
+        auto load_tile = [&](int tile) {
+            uint32_t mask = seen(tile);
+            if constexpr (BLOCKS) {
+                const int at = 2 * ((tile - tile0) / kAttendUnit);
+                const uint64_t ok = __builtin_amdgcn_ballot_w64(entry_ok);
+                mask &= ((ok >> at) & 1 ? 0x0000FFFFu : 0u) | ((ok >> (at + 1)) & 1 ? 0xFFFF0000u : 0u);
+                const int64_t e0 = lane_of64(entry, at), e1 = lane_of64(entry, at + 1);
+#pragma unroll
+                for (int i = 0; i < KU; ++i) {
+                    const int64_t e = (64 * i + 63) / PL < 16 ? e0 : 64 * i / PL >= 16 ? e1 : piece_row[i] < 16 ? e0 : e1;
+                    if ((64 * (i + 1) <= kAttendTile * PL || 64 * i + lane < kAttendTile * PL) &&
+                        (mask == 0xFFFFFFFFu || ((mask >> piece_row[i]) & 1))) {
+                        kreg[i] = *reinterpret_cast<const uint4*>(a.pages[0] + e + (uint32_t)piece_off[i]);
+                        vreg[i] = *reinterpret_cast<const uint4*>(a.pages[1] + e + (uint32_t)piece_off[i]);
+                    }
+                }
+            } else {
+                const int tok = tile + (lane & 31);
+                const bool ok = (unsigned)page < (unsigned)a.num_pages;
+                const int64_t off = ok ? page * a.page_stride + (tok % a.page_size) * a.row_stride + head_off : 0;
+                mask &= (uint32_t)__builtin_amdgcn_ballot_w64(ok);
+#pragma unroll
+                for (int i = 0; i < KU; ++i) {
+                    const int64_t e = ((int64_t)__shfl((int)(off >> 32), piece_row[i]) << 32) | (uint32_t)__shfl((int)off, piece_row[i]);
+                    if ((64 * (i + 1) <= kAttendTile * PL || 64 * i + lane < kAttendTile * PL) && ((mask >> piece_row[i]) & 1)) {
+                        kreg[i] = *reinterpret_cast<const uint4*>(a.pages[0] + e + piece_off[i]);
+                        vreg[i] = *reinterpret_cast<const uint4*>(a.pages[1] + e + piece_off[i]);
+                    }
+                }
+            }
+            return mask;
+        };
+
+        // the first tile, and behind it in the queue the queries
+        if constexpr (BLOCKS) load_entries(tile0);
+        else load_page(tile0);
         // ---- queries: operands of the first product, and their sums over both groups of channels ----
         const int qi = qt * kAttendRows + (n & (Q - 1));   // among the queries of the K/V head
         const bool q_live = qi < a.share;
         const uint16_t* qrow = a.q + b * a.ldq + (int64_t)(hk * a.share + (q_live ? qi : 0)) * a.ldqh;
-        v4u_att qh[HS], ql[LS ? LS : 1];
-        int h_here = a.r - 8 * g, l_here = low - 8 * g;
+        int h_here = a.r - 8 * g, l_here = low - 8 * g;   // (kept from the compiler, which would hold the comparisons for all heads)
         asm volatile("" : "+v"(h_here), "+v"(l_here));
+        Piece16 raw_h[HS], raw_l[LS ? LS : 1];
+#pragma unroll
+        for (int s = 0; s < HS; ++s) {
+            raw_h[s] = Piece16{0u, 0u, 0u, 0u};
+            if (q_live && 32 * s < h_here) raw_h[s] = *reinterpret_cast<const Piece16*>(qrow + 8 * (4 * s + g));
+        }
+#pragma unroll
+        for (int s = 0; s < LS; ++s) {
+            raw_l[s] = Piece16{0u, 0u, 0u, 0u};
+            if (q_live && 32 * s < l_here) raw_l[s] = *reinterpret_cast<const Piece16*>(qrow + a.r + 8 * (4 * s + g));
+        }
+        uint32_t next_mask = 0;
+        if constexpr (BLOCKS) set_entries(tile0);
+        if (tile0 < t_end) next_mask = load_tile(tile0);
+        if constexpr (!BLOCKS) load_page(tile0 + kAttendUnit);
+
+        v4u_att qh[HS], ql[LS ? LS : 1];
         float sum_h = 0.0f, sum_l = 0.0f;
 #pragma unroll
         for (int s = 0; s < HS; ++s) {
-            const int ch = 8 * (4 * s + g);
-            qh[s] = (v4u_att){0u, 0u, 0u, 0u};
-            if (q_live && 32 * s < h_here) {
-                const Piece16 p = *reinterpret_cast<const Piece16*>(qrow + ch);
-                qh[s] = (v4u_att){p.x, p.y, p.z, p.w};
-            }
+            qh[s] = (v4u_att){raw_h[s].x, raw_h[s].y, raw_h[s].z, raw_h[s].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum_h += __uint_as_float(qh[s][i] << 16) + __uint_as_float(qh[s][i] & 0xFFFF0000u);
         }
 #pragma unroll
         for (int s = 0; s < LS; ++s) {
-            const int ch = 8 * (4 * s + g);
-            Piece16 p{0u, 0u, 0u, 0u};
-            if (q_live && 32 * s < l_here) p = *reinterpret_cast<const Piece16*>(qrow + a.r + ch);
+            const Piece16 p = raw_l[s];
             const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum_l += __uint_as_float(w[i] << 16) + __uint_as_float(w[i] & 0xFFFF0000u);
@@ -271,139 +395,33 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             qsum_l[i] = __shfl(sum_l, own + i);
         }
 
-        v4f_att acch[HT], accl[NL ? NL : 1];
-#pragma unroll
-        for (int j = 0; j < HT; ++j) acch[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < NL; ++j) accl[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
-        // of the own four queries: running maximum times log2 e, sum of weights, and weighted sums of zero-points, the last three
-        // over the own tokens
-        float m2[4], l[4], zero_h[4], zero_l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            m2[i] = kAttendNone;
-            l[i] = zero_h[i] = zero_l[i] = 0.0f;
-        }
 
-        // ---- rows of a tile to LDS ----
-        uint4 kreg[2 * KU], vreg[2 * KU];   // (where a block is not there they keep what they had: codes of some kind)
-#pragma unroll
-        for (int i = 0; i < 2 * KU; ++i) kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
-        int64_t entry = 0;        // BLOCKS: offset of block lane % 2 of the wavefront's tile lane / 2, counted from tile0
-        bool entry_ok = false;
-        int tile0 = t_begin + wave * kAttendTile;
-        auto load_entries = [&](int from_token) {
-            const int tok = from_token + (lane >> 1) * kAttendUnit + (lane & 1) * 16;
-            int page = -1;
-            if (tok < t_end) page = table[tok / a.page_size];
-            entry_ok = (unsigned)page < (unsigned)a.num_pages;
-            entry = entry_ok ? page * a.page_stride + (tok % a.page_size) * a.row_stride + head_off : 0;
-        };
-        // the tokens of the tile at token tt that are there and seen
-        auto seen = [&](int tt) {
-            const int left = len - tt, skip = t_low - tt;
-            uint32_t mask = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u;
-            if (skip > 0) mask &= 0xFFFFFFFFu << skip;
-            return mask;
-        };
-        // whole blocks of 16 rows, 16 bytes per lane and load; returns the tile's mask
-        auto load_blocks = [&](int tt) {
-            const int at = 2 * ((tt - tile0) / kAttendUnit);
-            const uint64_t ok = __builtin_amdgcn_ballot_w64(entry_ok);
-            const bool ok0 = (ok >> at) & 1, ok1 = (ok >> (at + 1)) & 1;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (!(h ? ok1 : ok0)) continue;
-                const int64_t e = ((int64_t)__builtin_amdgcn_readlane((int)(entry >> 32), at + h) << 32) |
-                                  (uint32_t)__builtin_amdgcn_readlane((int)entry, at + h);
-                const uint8_t* kp = a.pages[0] + e;
-                const uint8_t* vp = a.pages[1] + e;
-#pragma unroll
-                for (int i = 0; i < KU; ++i) {   // RB pieces in a block
-                    if (i * 64 + lane < RB) {
-                        kreg[h * KU + i] = *reinterpret_cast<const uint4*>(kp + (uint32_t)(i * 1024 + lane * 16));
-                        vreg[h * KU + i] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(i * 1024 + lane * 16));
-                    }
-                }
-            }
-            return seen(tt) & ((ok0 ? 0x0000FFFFu : 0u) | (ok1 ? 0xFFFF0000u : 0u));
-        };
-        auto store_blocks = [&]() {
+        for (int tt = tile0; tt < t_end; tt += kAttendUnit) {
+            const uint32_t mask = next_mask;
 #pragma unroll
             for (int i = 0; i < KU; ++i) {
-                if (i * 64 + lane < RB) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint4 k = kreg[h * KU + i], v = vreg[h * KU + i];
-                        *reinterpret_cast<uint2*>(kt + h * 16 * P + to[2 * i]) = make_uint2(k.x, k.y);
-                        *reinterpret_cast<uint2*>(kt + h * 16 * P + to[2 * i + 1]) = make_uint2(k.z, k.w);
-                        *reinterpret_cast<uint2*>(vt + h * 16 * P + to[2 * i]) = make_uint2(v.x, v.y);
-                        *reinterpret_cast<uint2*>(vt + h * 16 * P + to[2 * i + 1]) = make_uint2(v.z, v.w);
-                    }
+                if (64 * (i + 1) <= kAttendTile * PL || 64 * i + lane < kAttendTile * PL) {
+                    *reinterpret_cast<uint4*>(kt + piece_to[i]) = kreg[i];
+                    *reinterpret_cast<uint4*>(vt + piece_to[i]) = vreg[i];
                 }
             }
-        };
-        // rows anywhere, 4 bytes per lane and load, row by row through the table; rows that are not there become zeros
-        auto move_rows = [&](int tt) {
-            const int tok = tt + (lane & 31);
-            int page = -1;
-            if (tok < len && tok >= t_low) page = table[tok / a.page_size];
-            const bool ok = (unsigned)page < (unsigned)a.num_pages;
-            const int64_t off = ok ? page * a.page_stride + (tok % a.page_size) * a.row_stride + head_off : 0;
-            const uint32_t mask = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
-            const int words = RB >> 2;
-            for (int i = 0; i < kAttendTile * words; i += 256) {
-                uint32_t kw[4], vw[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int word = i + 64 * j + lane;
-                    const int row = min(word / words, kAttendTile - 1), col = word - row * words;
-                    const int64_t at = ((int64_t)__shfl((int)(off >> 32), row) << 32) | (uint32_t)__shfl((int)off, row);
-                    kw[j] = vw[j] = 0u;
-                    if (word < kAttendTile * words && ((mask >> row) & 1)) {
-                        kw[j] = *reinterpret_cast<const uint32_t*>(a.pages[0] + at + 4 * col);
-                        vw[j] = *reinterpret_cast<const uint32_t*>(a.pages[1] + at + 4 * col);
+            const int next = tt + kAttendUnit;
+            if (next < t_end) {
+                if constexpr (BLOCKS) {
+                    if (next - tile0 >= 32 * kAttendUnit) {
+                        tile0 = next;
+                        load_entries(next);
+                        set_entries(next);
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int word = i + 64 * j + lane, row = word / words, col = 4 * (word - row * words);
-                    if (row < kAttendTile) {
-                        const int at = row * P + col + (col < par_off ? 0 : P - 16 - par_off);
-                        *reinterpret_cast<uint32_t*>(kt + at) = kw[j];
-                        *reinterpret_cast<uint32_t*>(vt + at) = vw[j];
-                    }
-                }
-            }
-            return mask;
-        };
-
-        uint32_t next_mask = 0;
-        if (BLOCKS && tile0 < t_end) {
-            load_entries(tile0);
-            next_mask = load_blocks(tile0);
-        }
-        for (int tt = tile0; tt < t_end; tt += kAttendUnit) {
-            uint32_t mask;
-            if constexpr (BLOCKS) {
-                mask = next_mask;
-                store_blocks();
-                const int nt = tt + kAttendUnit;
-                if (nt < t_end) {
-                    if (nt - tile0 >= 32 * kAttendUnit) {
-                        tile0 = nt;
-                        load_entries(nt);
-                    }
-                    next_mask = load_blocks(nt);
-                }
-            } else {
-                mask = move_rows(tt);
+                next_mask = load_tile(next);
+                if constexpr (!BLOCKS) load_page(next + kAttendUnit);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 
             // ---- what the tile's work reads of LDS, asked for at once (values' codes only where they leave registers for it) ----
-            constexpr bool kEarly = HT <= 2;
+            constexpr bool kEarly = HT <= 2 && NL <= 8;
             uint2 kh[2][HS];
             uint32_t kl[2][LS ? LS : 1];
             float4 kpar[NT], vpar[NT];
@@ -523,11 +541,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 for (int i = 0; i < 4; ++i) {
                     float top = x[0][i];
                     if constexpr (NT == 2) top = fmaxf(top, x[1][i]);
-                    top = fmaxf(top, lane_xor<1>(top));
-                    top = fmaxf(top, lane_xor<2>(top));
-                    top = fmaxf(top, lane_xor<4>(top));
-                    top = fmaxf(top, lane_xor<8>(top));
-                    if constexpr (Q == 8) top = fmaxf(top, lane_xor<32>(top));
+                    top = row_max16(top);
+                    if constexpr (Q == 8) top = halves_max(top);
                     const float m_new = fmaxf(m2[i], top * sc2);
                     back[i] = __builtin_amdgcn_exp2f(m2[i] - m_new);
                     m2[i] = m_new;
@@ -635,11 +650,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
                 float& v = k == 0 ? l[i] : k == 1 ? zero_h[i] : zero_l[i];
-                v += lane_xor<1>(v);
-                v += lane_xor<2>(v);
-                v += lane_xor<4>(v);
-                v += lane_xor<8>(v);
-                if constexpr (Q == 8) v += lane_xor<32>(v);
+                v = row_sum16(v);
+                if constexpr (Q == 8) v = halves_sum(v);
             }
         }
         if constexpr (Q == 8) {
@@ -681,7 +693,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         __syncthreads();
         // a head in one piece is done; a piece of one is partial result 0 of its workgroup, or 1 behind another head
         const bool whole = n_units == units;
-        const int64_t slot = 2 * w0 + (u != u_first);
+        const int64_t slot = 2 * (int64_t)w0 + (u != u_first);
         if (t == 0) {
             int32_t* join = a.joins + ((int64_t)b * heads + head) * 2;
             if (first_unit == 0) join[0] = (int32_t)slot;

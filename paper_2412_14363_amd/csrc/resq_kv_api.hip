@@ -273,6 +273,10 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
         return RESQ_ERR_ALIGN;
     if (workspace_bytes < need) return RESQ_ERR_BUFFER;
     const int64_t longest = width > kMaxAttendLen / page_size ? kMaxAttendLen : width * page_size;
+    // units of the longest sequences that the table can name: counted in 32 bits
+    const int64_t qtiles = (heads_q / heads_k + kAttendRows - 1) / kAttendRows;
+    const int64_t units = B * heads_k * qtiles * ((longest + kAttendUnit - 1) / kAttendUnit);
+    if (units > kInt32Max) return RESQ_ERR_SHAPE;
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(q);
     a.ldq = ldq;
@@ -293,14 +297,13 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.head_stride = g.head_stride;
     a.row_stride = g.row_stride;
     a.row_bytes = (int)(r + (d_head - r) / 2 + 16);
-    a.qtiles = (a.share + kAttendRows - 1) / kAttendRows;
+    a.qtiles = (int)qtiles;
     const AttendWorkspace w = attend_workspace(B, heads_k, a.share, d_head);
     a.joins = static_cast<int32_t*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.ml);
     a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.acc);
     a.rows = w.rows;
-    a.blocks16 = page_size % 16 == 0 && g.row_stride == a.row_bytes && a.row_bytes % 8 == 0 && g.page_stride % 16 == 0 && g.head_stride % 16 == 0 &&
-                 aligned(k_pages, 16) && aligned(v_pages, 16);
+    a.blocks16 = page_size % 16 == 0 && g.row_stride < (1 << 26);
     a.lds_red = 0;
     a.max_len = (int)longest;
     a.window = window < kMaxAttendLen ? (int)window : 0;
@@ -310,17 +313,16 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.ldo = ldo;
     a.ldoh = ldoh;
     a.lse = lse;
-    const int64_t units = B * heads_k * a.qtiles * ((longest + kAttendUnit - 1) / kAttendUnit);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t low = d_head - r;
     // the smallest kernel that holds the head's two groups of channels
     if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
-                                                                                   : launch_attend<0, 16, 2>(a, units, st);
+                                                                                   : launch_attend<0, 16, 1>(a, units, st);
     if (low <= 64) return r <= 16 ? launch_attend<4, 1, 2>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
-                                                                                   : launch_attend<4, 16, 2>(a, units, st);
+                                                                                   : launch_attend<4, 16, 1>(a, units, st);
     if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
-                           : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 2>(a, units, st);
-    return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 2>(a, units, st);
+                           : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 1>(a, units, st);
+    return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 1>(a, units, st);
 }
 
 }  // extern "C"
