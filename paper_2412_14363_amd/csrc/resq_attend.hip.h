@@ -40,6 +40,7 @@ constexpr int kAttendWaves = kAttendThreads / 64;
 constexpr int kAttendMaxHead = 256;
 constexpr int kAttendTile = 32;                              // tokens of a wavefront's step
 constexpr int kAttendUnit = kAttendTile * kAttendWaves;      // tokens of a unit
+constexpr int kAttendHeadCost = 3;
 constexpr int kAttendMaxGrid = 1024;
 constexpr int kAttendRows = 16;                              // queries of a workgroup at most
 constexpr int kAttendPRow = 80;                              // bytes of a row of weights in LDS: 32 in bf16, and what keeps rows on other banks
@@ -84,6 +85,8 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int len) {
     const int from = attend_first(a, len) & ~(kAttendTile - 1);
     return (len - from + kAttendUnit - 1) / kAttendUnit;
 }
+// what a head of so many units costs, counted in units: to begin and to end one takes the time of a few
+__device__ __forceinline__ int attend_cost(int units) { return units == 0 ? 0 : units + kAttendHeadCost; }
 
 __device__ __forceinline__ v4f_att attend_mfma(const v4u_att& x, const v4u_att& y, const v4f_att& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf_att, x), __builtin_bit_cast(v8bf_att, y), c, 0, 0, 0);
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     int mine = 0, len_b = 0;
     for (int b = b0; b < b1; ++b) {
         len_b = attend_len(a, b);
-        mine += attend_units(a, len_b) * heads;
+        mine += attend_cost(attend_units(a, len_b)) * heads;
     }
     int upto = wave_scan(mine);
     if (lane == 63) part[wave] = upto;
@@ -204,19 +207,19 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     if (w0 >= W) return;
     const int share = total / W, rest = total - share * W;   // the first `rest` runs are a unit longer
     int u = w0 * share + min(w0, rest);
-    const int u_end = u + share + (w0 < rest), u_first = u;
+    const int u_end = u + share + (w0 < rest);
     int start = before + upto - mine;   // of this thread's first sequence
     if (start <= u && u < start + mine) {
         for (int b = b0; b < b1; ++b) {
             if (per > 1) len_b = attend_len(a, b);
-            const int units = attend_units(a, len_b) * heads;
-            if (u < start + units) {
+            const int cost = attend_cost(attend_units(a, len_b)) * heads;
+            if (u < start + cost) {
                 found[0] = b;
                 found[1] = start;
                 found[2] = len_b;
                 break;
             }
-            start += units;
+            start += cost;
         }
     }
     __syncthreads();
@@ -243,17 +246,21 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 
     const CodeBits key_bits(0x00780078u, 0x41804180u), value_bits(0x000F000Fu, 0xC3004300u);
 
+    bool first_head = true;
     while (u < u_end) {
         // ---- the next head in the run ----
-        const int units = attend_units(a, len), seq_units = units * heads;
-        if (u >= seq_start + seq_units) {
-            seq_start += seq_units;
+        const int units = attend_units(a, len), cost = attend_cost(units);
+        if (u >= seq_start + cost * heads) {
+            seq_start += cost * heads;
             ++b;
             len = __builtin_amdgcn_readfirstlane(attend_len(a, b));
             continue;
         }
-        const int head = (u - seq_start) / units, first_unit = (u - seq_start) - head * units;
-        const int n_units = min(units - first_unit, u_end - u);
+        const int head = (u - seq_start) / cost, begin = (u - seq_start) - head * cost;
+        const int end = min(cost, begin + (u_end - u));
+        u += end - begin;
+        const int first_unit = max(begin - kAttendHeadCost, 0), n_units = end - kAttendHeadCost - first_unit;
+        if (n_units <= 0) continue;   // this run ends where the head begins
         const int hk = head / a.qtiles, qt = head - hk * a.qtiles;
         const int t_low = attend_first(a, len), from = t_low & ~(kAttendTile - 1);
         const int t_begin = from + first_unit * kAttendUnit;
@@ -693,7 +700,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         __syncthreads();
         // a head in one piece is done; a piece of one is partial result 0 of its workgroup, or 1 behind another head
         const bool whole = n_units == units;
-        const int64_t slot = 2 * (int64_t)w0 + (u != u_first);
+        const int64_t slot = 2 * (int64_t)w0 + !first_head;
+        first_head = false;
         if (t == 0) {
             int32_t* join = a.joins + ((int64_t)b * heads + head) * 2;
             if (first_unit == 0) join[0] = (int32_t)slot;
@@ -731,14 +739,13 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             }
         }
         __syncthreads();   // before the rows of the next head come to LDS
-        u += n_units;
     }
 }
 
 // Joins the partial results of the heads that several workgroups had, one workgroup to a query; and writes the queries of
 // sequences without tokens.
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a) {
-    __shared__ float weight[kAttendMaxGrid], part[2 * kAttendWaves];
+    __shared__ float weight[kAttendMaxGrid], weight_sum[kAttendMaxGrid], part[2 * kAttendWaves];
     __shared__ float4 red[kAttendThreads];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int heads_q = a.heads_k * a.share;
@@ -756,36 +763,41 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     const int w_first = slot0 >> 1, count = w_last - w_first + 1;
     if (count == 1) return;
     auto slot = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (w_first + i)); };
-    float top = kAttendNone;
+    // four channels to a thread, what threads are left over the partial results, four of which are on their way at a time; the
+    // first four are asked for before their weights are known
+    const int fours = a.d >> 2, groups = kAttendThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
+    float4 v[4];
+    auto load_four = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = *reinterpret_cast<const float4*>(a.part_acc + (slot(min(i + k * groups, count - 1)) * a.rows + row) * a.d + ch);
+    };
+    if (group < groups) load_four(group);
+    float top = kAttendNone, sum = 0.0f;
     for (int i = t; i < count; i += kAttendThreads) {
-        weight[i] = a.part_ml[(slot(i) * kAttendRows + row) * 2];
-        top = fmaxf(top, weight[i]);
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (slot(i) * kAttendRows + row) * 2);
+        weight[i] = ml.x;
+        weight_sum[i] = ml.y;
+        top = fmaxf(top, ml.x);
     }
-    top = wave_max(top);
+    top = halves_max(fmaxf(row_max16(top), lane_xor<16>(row_max16(top))));
     if (lane == 0) part[wave] = top;
     __syncthreads();
     top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    float sum = 0.0f;
     for (int i = t; i < count; i += kAttendThreads) {
         const float f = __builtin_amdgcn_exp2f(weight[i] - top);
         weight[i] = f;
-        sum = fmaf(f, a.part_ml[(slot(i) * kAttendRows + row) * 2 + 1], sum);
+        sum = fmaf(f, weight_sum[i], sum);
     }
-    for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
+    sum = row_sum16(sum);
+    sum = rows_sum(sum);
     if (lane == 0) part[kAttendWaves + wave] = sum;
     __syncthreads();
     sum = (part[kAttendWaves] + part[kAttendWaves + 1]) + (part[kAttendWaves + 2] + part[kAttendWaves + 3]);
-    // four channels to a thread, what threads are left over the partial results, four of which are on their way at a time
-    const int fours = a.d >> 2, groups = kAttendThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (group < groups) {
         for (int i = group; i < count; i += 4 * groups) {
-            float4 v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int j = min(i + k * groups, count - 1);
-                v[k] = *reinterpret_cast<const float4*>(a.part_acc + (slot(j) * a.rows + row) * a.d + ch);
-            }
+            if (i != group) load_four(i);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float f = i + k * groups < count ? weight[i + k * groups] : 0.0f;

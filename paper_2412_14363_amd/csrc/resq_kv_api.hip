@@ -275,7 +275,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     const int64_t longest = width > kMaxAttendLen / page_size ? kMaxAttendLen : width * page_size;
     // units of the longest sequences that the table can name: counted in 32 bits
     const int64_t qtiles = (heads_q / heads_k + kAttendRows - 1) / kAttendRows;
-    const int64_t units = B * heads_k * qtiles * ((longest + kAttendUnit - 1) / kAttendUnit);
+    const int64_t units = B * heads_k * qtiles * ((longest + kAttendUnit - 1) / kAttendUnit + kAttendHeadCost);
     if (units > kInt32Max) return RESQ_ERR_SHAPE;
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(q);
@@ -318,7 +318,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     // the smallest kernel that holds the head's two groups of channels
     if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
                                                                                    : launch_attend<0, 16, 1>(a, units, st);
-    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 2>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
+    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
                                                                                    : launch_attend<4, 16, 1>(a, units, st);
     if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
                            : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 1>(a, units, st);
