@@ -73,6 +73,7 @@ struct AttendArgs {
     float* part_acc;   // [2 grid][rows][d]: and its weighted sums (workspace)
     int rows;          // queries of a partial result
     int blocks16;      // 16 rows of a page from a multiple of 16 on are contiguous and 16-byte aligned
+    int fours_magic;   // e * fours_magic >> 16 is e / (d / 4) for e < 1024
     int lds_red;       // bytes in front of the maxima and sums in LDS
 };
 
@@ -230,15 +231,6 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     uint8_t* kt = lds + wave * (2 * kAttendTile * P);
     uint8_t* vt = kt + kAttendTile * P;
     uint8_t* pt = lds + attend_tiles_bytes(NL, HT) + wave * attend_weights_bytes(Q);   // weights: 8-bit group's, 4-bit group's
-    // a lane's pieces: the row, what is in front of it in the row, and where it goes
-    int piece_row[KU], piece_off[KU], piece_to[KU];
-#pragma unroll
-    for (int i = 0; i < KU; ++i) {
-        const int k = i * 64 + lane, row = k / PL, col = k - row * PL;
-        piece_row[i] = min(row, kAttendTile - 1);
-        piece_off[i] = (BLOCKS ? (row & 15) * (int)a.row_stride : 0) + (col < PL - 1 ? min(16 * col, RB - 16) : RB - 16);
-        piece_to[i] = piece_row[i] * P + (col < PL - 1 ? 16 * col : P - 16);
-    }
     const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
     const float kLog2e = 1.44269504088896340736f;
     const float sc2 = a.softcap > 0.0f ? kLog2e : a.scale * kLog2e;
@@ -268,24 +260,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         const int64_t head_off = hk * a.head_stride;
         const int32_t* table = a.table + b * a.ld_table;
 
-        v4f_att acch[HT], accl[NL ? NL : 1];
-#pragma unroll
-        for (int j = 0; j < HT; ++j) acch[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < NL; ++j) accl[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
-        // of the own four queries: running maximum times log2 e, sum of weights, and weighted sums of zero-points, the last three
-        // over the own tokens
-        float m2[4], l[4], zero_h[4], zero_l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            m2[i] = kAttendNone;
-            l[i] = zero_h[i] = zero_l[i] = 0.0f;
-        }
-
         // ---- rows of a tile to LDS, by way of registers, a tile ahead ----
-        uint4 kreg[KU], vreg[KU];   // (where a row is not there they keep what they had: codes of some kind)
-#pragma unroll
-        for (int i = 0; i < KU; ++i) kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
         int tile0 = t_begin + wave * kAttendTile;
         // BLOCKS: lane l has the offset of block l % 2 of the wavefront's tile l / 2, counted from tile0.  Else it has the page of
         // row l % 32 of the tile that is loaded next.
@@ -307,6 +282,36 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             page = -1;
             if (tok >= t_low && tok < t_end) page = table[tok / a.page_size];
         };
+        // the pages of the first tile are asked for before anything else
+        if constexpr (BLOCKS) load_entries(tile0);
+        else load_page(tile0);
+        __builtin_amdgcn_sched_barrier(0);
+        v4f_att acch[HT], accl[NL ? NL : 1];
+#pragma unroll
+        for (int j = 0; j < HT; ++j) acch[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NL; ++j) accl[j] = (v4f_att){0.0f, 0.0f, 0.0f, 0.0f};
+        // of the own four queries: running maximum times log2 e, sum of weights, and weighted sums of zero-points, the last three
+        // over the own tokens
+        float m2[4], l[4], zero_h[4], zero_l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m2[i] = kAttendNone;
+            l[i] = zero_h[i] = zero_l[i] = 0.0f;
+        }
+
+        uint4 kreg[KU], vreg[KU];   // (where a row is not there they keep what they had: codes of some kind)
+#pragma unroll
+        for (int i = 0; i < KU; ++i) kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
+        // a lane's pieces: the row, what is in front of it in the row, and where it goes
+        int piece_row[KU], piece_off[KU], piece_to[KU];
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int k = i * 64 + lane, row = k / PL, col = k - row * PL;
+            piece_row[i] = min(row, kAttendTile - 1);
+            piece_off[i] = (BLOCKS ? (row & 15) * (int)a.row_stride : 0) + (col < PL - 1 ? min(16 * col, RB - 16) : RB - 16);
+            piece_to[i] = piece_row[i] * P + (col < PL - 1 ? 16 * col : P - 16);
+        }
         // the tokens of a tile that are there and seen
         auto seen = [&](int tile) {
             const int left = len - tile, skip = t_low - tile;
@@ -348,9 +353,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             return mask;
         };
 
-        // the first tile, and behind it in the queue the queries
-        if constexpr (BLOCKS) load_entries(tile0);
-        else load_page(tile0);
+        // the queries, behind the pages in the queue, and the first tile
         // ---- queries: operands of the first product, and their sums over both groups of channels ----
         const int qi = qt * kAttendRows + (n & (Q - 1));   // among the queries of the K/V head
         const bool q_live = qi < a.share;
@@ -707,35 +710,35 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             if (first_unit == 0) join[0] = (int32_t)slot;
             if (first_unit + n_units == units) join[1] = (int32_t)w0;
         }
-        const int pairs = a.d >> 1;
-        for (int e = t; e < rows * pairs; e += kAttendThreads) {
-            const int row = e / pairs, ch = 2 * (e - row * pairs);
-            float top = kAttendNone, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, ml[w * kAttendRows + row].x);
+        const int fours = a.d >> 2;   // four channels to a thread, of one group
+        for (int e = t; e < rows * fours; e += kAttendThreads) {
+            const int row = (int)((uint32_t)e * (uint32_t)a.fours_magic >> 16), ch = 4 * (e - row * fours);
+            float4 v[kAttendWaves];
+            v4f_att part_o[kAttendWaves];
 #pragma unroll
             for (int w = 0; w < kAttendWaves; ++w) {
-                const float4 v = ml[w * kAttendRows + row];
-                const float f = __builtin_amdgcn_exp2f(v.x - top), z = ch < a.r ? v.z : v.w;
-                sum = fmaf(f, v.y, sum);
-                o0 = fmaf(f, red[(w * rows + row) * a.d + ch] + z, o0);
-                o1 = fmaf(f, red[(w * rows + row) * a.d + ch + 1] + z, o1);
+                v[w] = ml[w * kAttendRows + row];
+                part_o[w] = *reinterpret_cast<const v4f_att*>(red + (w * rows + row) * a.d + ch);
             }
-            const int64_t qhead = hk * a.share + qt * kAttendRows + row;
+            const float top = fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x));
+            float sum = 0.0f;
+            v4f_att o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kAttendWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(v[w].x - top), z = ch < a.r ? v[w].z : v[w].w;
+                sum = fmaf(f, v[w].y, sum);
+                o += f * (part_o[w] + z);
+            }
+            const int qhead = hk * a.share + qt * kAttendRows + row;
             if (whole) {
                 const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
                 uint16_t* dst = a.out + b * a.ldo + qhead * a.ldoh + ch;
-                reinterpret_cast<Piece4*>(dst)->x = pack_bf16_pair(o0 * inv, o1 * inv);
+                *reinterpret_cast<Piece8*>(dst) = Piece8{pack_bf16_pair(o[0] * inv, o[1] * inv), pack_bf16_pair(o[2] * inv, o[3] * inv)};
                 if (ch == 0 && a.lse)
                     a.lse[(int64_t)b * a.heads_k * a.share + qhead] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
             } else {
-                float* dst = a.part_acc + (slot * a.rows + row) * a.d + ch;
-                dst[0] = o0;
-                dst[1] = o1;
-                if (ch == 0) {
-                    a.part_ml[(slot * kAttendRows + row) * 2] = top;
-                    a.part_ml[(slot * kAttendRows + row) * 2 + 1] = sum;
-                }
+                *reinterpret_cast<v4f_att*>(a.part_acc + (slot * a.rows + row) * a.d + ch) = o;
+                if (ch == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * kAttendRows + row) * 2) = make_float2(top, sum);
             }
         }
         __syncthreads();   // before the rows of the next head come to LDS

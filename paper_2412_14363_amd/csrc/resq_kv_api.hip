@@ -304,6 +304,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.acc);
     a.rows = w.rows;
     a.blocks16 = page_size % 16 == 0 && g.row_stride < (1 << 26);
+    a.fours_magic = 65536 / (a.d / 4) + 1;
     a.lds_red = 0;
     a.max_len = (int)longest;
     a.window = window < kMaxAttendLen ? (int)window : 0;
