@@ -60,7 +60,8 @@ struct AttendArgs {
     const int32_t* table;
     int64_t ld_table;
     const uint8_t* pages[2];
-    int num_pages, page_size;
+    int num_pages;
+    FastDiv page_size;
     int64_t page_stride, head_stride, row_stride;
     int max_len;      // tokens that a table row can name
     int window;       // 0: none
@@ -270,17 +271,17 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         auto load_entries = [&](int tile) {
             const int tok = tile + (lane >> 1) * kAttendUnit + (lane & 1) * 16;
             page = -1;
-            if (tok < t_end) page = table[tok / a.page_size];
+            if (tok < t_end) page = table[a.page_size((uint32_t)tok)];
         };
         auto set_entries = [&](int tile) {
             const int tok = tile + (lane >> 1) * kAttendUnit + (lane & 1) * 16;
             entry_ok = (unsigned)page < (unsigned)a.num_pages;
-            entry = entry_ok ? page * a.page_stride + (tok % a.page_size) * a.row_stride + head_off : 0;
+            entry = entry_ok ? page * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride + head_off : 0;
         };
         auto load_page = [&](int tile) {
             const int tok = tile + (lane & 31);
             page = -1;
-            if (tok >= t_low && tok < t_end) page = table[tok / a.page_size];
+            if (tok >= t_low && tok < t_end) page = table[a.page_size((uint32_t)tok)];
         };
         // the pages of the first tile are asked for before anything else
         if constexpr (BLOCKS) load_entries(tile0);
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             } else {
                 const int tok = tile + (lane & 31);
                 const bool ok = (unsigned)page < (unsigned)a.num_pages;
-                const int64_t off = ok ? page * a.page_stride + (tok % a.page_size) * a.row_stride + head_off : 0;
+                const int64_t off = ok ? page * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride + head_off : 0;
                 mask &= (uint32_t)__builtin_amdgcn_ballot_w64(ok);
 #pragma unroll
                 for (int i = 0; i < KU; ++i) {

@@ -17,17 +17,21 @@ constexpr int kKvThreads = 256;
 // ---------------------------------------------------------------------------
 // The plan.  Request b holds lens[b] tokens in ceil(lens[b] / page_size) pages, named by its row of the block table, and gets
 // news[b] more: its tokens' places in the batch are a prefix sum, the pages it lacks another one, taken off the front of the
-// free list.  One workgroup makes the sums and checks them (nothing changes unless everything fits); then every token finds
-// its request by bisection of the first sum, and the token that opens a page writes the page's entry.
-// Latency: 8 bytes in and 16 out per request, 8 out per token.
+// free list.  Sums first, and checks (nothing changes unless everything fits); then every token finds its request by bisection
+// of the first sum, and the token that opens a page writes the page's entry.
+// Latency: 8 bytes in and 16 out per request, 8 out per token.  Up to kPlanRequests requests take one launch: every workgroup
+// makes the sums for itself, in LDS, and serves some of the tokens; outputs that lie on inputs allow one workgroup only, which
+// reads them all before it writes.  Else the sums go through memory to a second kernel.
 // ---------------------------------------------------------------------------
+constexpr int kPlanRequests = 4096;
+constexpr int kPlanTokens = 1024;     // of a workgroup
 constexpr int kPlanThreads = 1024;
 
 struct KvPlanArgs {
     const int32_t* lens;
     const int32_t* news;
     int B;
-    int page_size;
+    FastDiv page_size;
     int num_pages;
     const int32_t* free_pages;
     int64_t n_free;
@@ -74,127 +78,194 @@ __device__ __forceinline__ void block_scan2(int64_t& a, int64_t& b, int64_t& tot
     b = before_b + sb - b;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvPlanArgs p) {
+__device__ __forceinline__ int64_t plan_pages(const KvPlanArgs& p, int64_t tokens) {   // pages of so many tokens, below 2^32
+    return tokens <= 0x7FFFFFFF ? (tokens == 0 ? 0 : p.page_size((uint32_t)tokens - 1) + 1) : (tokens - 1) / p.page_size.d + 1;
+}
+
+// The sums of a workgroup of kPlanThreads: each thread's requests b0 .. b1 in a row, its first request's sums, the totals and the
+// status.  Sums are in 64 bits; those that are handed out fit 32.
+struct PlanSums {
+    int b0, b1;
+    int64_t tokens, pages, total_tokens, total_pages;
+    int taken, status;
+};
+__device__ __forceinline__ PlanSums plan_sums(const KvPlanArgs& p) {
     __shared__ int64_t part[kPlanThreads / 64][2];
     __shared__ int flags;
     const int t = threadIdx.x;
-    const int per = (p.B + kPlanThreads - 1) / kPlanThreads;   // consecutive requests of a thread
-    const int b0 = min(t * per, p.B), b1 = min(b0 + per, p.B);
+    PlanSums s;
+    const int per = (p.B + kPlanThreads - 1) / kPlanThreads;
+    s.b0 = min(t * per, p.B);
+    s.b1 = min(s.b0 + per, p.B);
     if (t == 0) flags = 0;
-    const int taken = *p.taken;
-    int64_t tokens = 0, pages = 0;
-    int bad = taken < 0 ? 2 : 0;
-    for (int b = b0; b < b1; ++b) {
+    s.taken = *p.taken;
+    s.tokens = s.pages = 0;
+    int bad = s.taken < 0 ? 2 : 0;
+    for (int b = s.b0; b < s.b1; ++b) {
         const int64_t len = p.lens[b], add = p.news[b];
         if (len < 0 || add < 0) {
             bad |= 2;
             continue;
         }
-        const int64_t all = (len + add + p.page_size - 1) / p.page_size;
+        const int64_t all = plan_pages(p, len + add);
         if (all > p.width) bad |= 1;
-        tokens += add;
-        pages += all - (len + p.page_size - 1) / p.page_size;
+        s.tokens += add;
+        s.pages += all - plan_pages(p, len);
     }
-    int64_t total_tokens, total_pages;
-    block_scan2(tokens, pages, total_tokens, total_pages, part);   // (its barrier is behind flags = 0)
+    block_scan2(s.tokens, s.pages, s.total_tokens, s.total_pages, part);   // (its barrier is behind flags = 0)
     if (bad) atomicOr(&flags, bad);
     __syncthreads();
-    const int status = flags & 2 ? 4 : total_tokens > p.max_tokens ? 3 : flags & 1 ? 2 : taken + total_pages > p.n_free ? 1 : 0;
-    for (int b = b0; b < b1; ++b) {
+    s.status = flags & 2 ? 4 : s.total_tokens > p.max_tokens ? 3 : flags & 1 ? 2 : s.taken + s.total_pages > p.n_free ? 1 : 0;
+    return s;
+}
+// what goes out per request; request(b, old length, first token, first page) for the caller's own use
+template <typename F>
+__device__ __forceinline__ void plan_write(const KvPlanArgs& p, const PlanSums& s, bool write, F request) {
+    int64_t tokens = s.tokens, pages = s.pages;
+    for (int b = s.b0; b < s.b1; ++b) {
         const int len = p.lens[b], add = p.news[b];
-        p.cu_tokens[b] = status ? 0 : (int)tokens;
-        p.cu_pages[b] = status ? 0 : (int)pages;
-        p.lens_out[b] = status ? len : len + add;
-        tokens += add;
-        pages += ((int64_t)len + add + p.page_size - 1) / p.page_size - ((int64_t)len + p.page_size - 1) / p.page_size;
+        request(b, len, (int)tokens, (int)pages);
+        if (write) {
+            p.cu_tokens[b] = s.status ? 0 : (int)tokens;
+            p.cu_pages[b] = s.status ? 0 : (int)pages;
+            p.lens_out[b] = s.status ? len : len + add;
+        }
+        if (s.status == 0) {
+            tokens += add;
+            pages += plan_pages(p, (int64_t)len + add) - plan_pages(p, len);
+        }
     }
-    if (t == 0) {
-        p.cu_tokens[p.B] = status ? 0 : (int)total_tokens;
-        p.cu_pages[p.B] = status ? 0 : (int)total_pages;
-        p.state[0] = status ? taken : taken + (int)total_pages;
-        p.state[1] = status;
+    if (write && threadIdx.x == 0) {
+        p.cu_tokens[p.B] = s.status ? 0 : (int)s.total_tokens;
+        p.cu_pages[p.B] = s.status ? 0 : (int)s.total_pages;
+        p.state[0] = s.status ? s.taken : s.taken + (int)s.total_pages;
+        p.state[1] = s.status;
     }
+}
+// position and slot of token t: token `place` of those that request b, which held `old`, gets; pages: the request's first new one
+// in the free list
+__device__ __forceinline__ void plan_token(const KvPlanArgs& p, int t, int b, int old, int place, int64_t pages) {
+    const int pos = old + place;
+    const int at = (int)p.page_size((uint32_t)pos), row = pos - at * (int)p.page_size.d;
+    const int have = (int)plan_pages(p, old);
+    int32_t* entry = p.table + (int64_t)b * p.ld_table + at;
+    int page;
+    if (at >= have) {
+        page = p.free_pages[pages + (at - have)];
+        if (row == 0) *entry = page;   // a new page's first row is new too
+    } else {
+        page = *entry;
+    }
+    p.positions[t] = pos;
+    p.slots[t] = (unsigned)page < (unsigned)p.num_pages ? page * (int)p.page_size.d + row : -1;
+}
+__device__ __forceinline__ void plan_no_token(const KvPlanArgs& p, int t) {
+    p.positions[t] = 0;
+    p.slots[t] = -1;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(const KvPlanArgs p, int tokens_per_block) {
+    extern __shared__ int plan_lds[];   // [B] each: old lengths, first tokens, first pages
+    int *olds = plan_lds, *firsts = plan_lds + p.B, *pages = plan_lds + 2 * p.B;
+    const PlanSums s = plan_sums(p);
+    plan_write(p, s, blockIdx.x == 0, [&](int b, int old, int token, int page) {
+        olds[b] = old;
+        firsts[b] = token;
+        pages[b] = page;
+    });
+    __syncthreads();
+    const int begin = blockIdx.x * tokens_per_block, end = min(begin + tokens_per_block, p.max_tokens);
+    const int total = s.status ? 0 : (int)s.total_tokens;
+    for (int t = begin + threadIdx.x; t < end; t += kPlanThreads) {
+        if (t >= total) {   // behind the last token, and after a refusal
+            plan_no_token(p, t);
+            continue;
+        }
+        int lo = 0, hi = p.B;   // the last request that begins at or before t
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (firsts[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        plan_token(p, t, lo, olds[lo], t - firsts[lo], (int64_t)s.taken + pages[lo]);
+    }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void kv_plan_sums_kernel(const KvPlanArgs p) {
+    const PlanSums s = plan_sums(p);
+    plan_write(p, s, true, [](int, int, int, int) {});
 }
 
 __global__ __launch_bounds__(256) void kv_plan_tokens_kernel(const KvPlanArgs p) {
     const int t = blockIdx.x * 256 + threadIdx.x;
     if (t >= p.max_tokens) return;
-    if (t >= p.cu_tokens[p.B]) {   // behind the last token, and after a refusal: nothing to write
-        p.positions[t] = 0;
-        p.slots[t] = -1;
-        return;
-    }
-    int lo = 0, hi = p.B;   // the last request that begins at or before t
+    if (t >= p.cu_tokens[p.B]) return plan_no_token(p, t);
+    int lo = 0, hi = p.B;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (p.cu_tokens[mid] <= t) lo = mid;
         else hi = mid;
     }
     const int first = p.cu_tokens[lo];
-    const int old = p.lens_out[lo] - (p.cu_tokens[lo + 1] - first);
-    const int pos = old + (t - first);
-    const int at = pos / p.page_size, row = pos - at * p.page_size;
-    const int have = (int)(((int64_t)old + p.page_size - 1) / p.page_size);
-    int32_t* entry = p.table + (int64_t)lo * p.ld_table + at;
-    int page;
-    if (at >= have) {
-        page = p.free_pages[(int64_t)(p.state[0] - p.cu_pages[p.B]) + p.cu_pages[lo] + (at - have)];
-        if (row == 0) *entry = page;   // a new page's first row is new too
-    } else {
-        page = *entry;
-    }
-    p.positions[t] = pos;
-    p.slots[t] = (unsigned)page < (unsigned)p.num_pages ? page * p.page_size + row : -1;
+    plan_token(p, t, lo, p.lens_out[lo] - (p.cu_tokens[lo + 1] - first), t - first,
+               (int64_t)(p.state[0] - p.cu_pages[p.B]) + p.cu_pages[lo]);
 }
 
 // ---------------------------------------------------------------------------
-// The writer and the reader: one row per token, head and kind (blockIdx.y: keys, values), G lanes to a row.
+// The writer and the reader: G lanes to the key and the value of a token and head (both, so that twice the bytes are on their way).
 // Bound by HBM at prefill sizes (2 d_head bytes of bf16 and a row of codes per row), by the launch at a step's.
 // ---------------------------------------------------------------------------
 struct KvPagesArgs {
     const uint16_t* x[2];       // bf16 [tokens, heads, d], keys and values
     int64_t ld[2], ldh[2];      // elements from token to token and from head to head
-    int64_t tokens;
-    int heads, d, r;
+    uint32_t rows;              // tokens * heads
+    FastDiv heads;
+    int d, r;
     const int32_t* slots;
     uint8_t* pages[2];
     int64_t page_stride, head_stride, row_stride;   // bytes
-    int page_size;
+    FastDiv page_size;
     uint32_t num_slots;
 };
 
-__device__ __forceinline__ int64_t kv_row_offset(const KvPagesArgs& a, uint32_t slot, int head) {
-    const uint32_t page = slot / (uint32_t)a.page_size, row = slot - page * (uint32_t)a.page_size;
+__device__ __forceinline__ int64_t kv_row_offset(const KvPagesArgs& a, uint32_t slot, uint32_t head) {
+    const uint32_t page = a.page_size(slot), row = slot - page * a.page_size.d;
     return page * a.page_stride + head * a.head_stride + row * a.row_stride;
 }
 
 template <int G>
 __global__ __launch_bounds__(kKvThreads) void append_kv_cache_kernel(const KvPagesArgs a) {
-    const int gl = threadIdx.x & (G - 1), kind = blockIdx.y;
-    const int64_t rows = a.tokens * a.heads;
-    const int64_t m_raw = (int64_t)blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
-    const int64_t m = m_raw < rows ? m_raw : rows - 1;   // groups past the last row quantize it and store nothing
-    const int64_t token = m / a.heads;
-    const int head = (int)(m - token * a.heads);
+    const int gl = threadIdx.x & (G - 1);
+    const uint32_t m_raw = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
+    const uint32_t m = min(m_raw, a.rows - 1);   // groups past the last row quantize it and store nothing
+    const uint32_t token = a.heads(m), head = m - token * a.heads.d;
     const uint32_t slot = (uint32_t)a.slots[token];
-    const uint16_t* x = a.x[kind] + token * a.ld[kind] + head * a.ldh[kind];
-    const uint4 v = gl < (a.d >> 3) ? reinterpret_cast<const uint4*>(x)[gl] : make_uint4(0u, 0u, 0u, 0u);
-    const bool wanted = m_raw < rows && slot < a.num_slots;
-    quantize_kv_row<G>(v, gl, a.d, a.r, wanted ? a.pages[kind] + kv_row_offset(a, slot, head) : nullptr);
+    uint4 v[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        v[k] = gl < (a.d >> 3) ? reinterpret_cast<const uint4*>(a.x[k] + token * a.ld[k] + head * a.ldh[k])[gl] : make_uint4(0u, 0u, 0u, 0u);
+    const bool wanted = m_raw < a.rows && slot < a.num_slots;
+    const int64_t off = wanted ? kv_row_offset(a, slot, head) : 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) quantize_kv_row<G>(v[k], gl, a.d, a.r, wanted ? a.pages[k] + off : nullptr);
 }
 
 template <int G>
 __global__ __launch_bounds__(kKvThreads) void gather_kv_cache_kernel(const KvPagesArgs a) {
-    const int gl = threadIdx.x & (G - 1), kind = blockIdx.y;
-    const int64_t m = (int64_t)blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
-    if (m >= a.tokens * a.heads || gl >= (a.d >> 3)) return;
-    const int64_t token = m / a.heads;
-    const int head = (int)(m - token * a.heads);
+    const int gl = threadIdx.x & (G - 1);
+    const uint32_t m = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
+    if (m >= a.rows || gl >= (a.d >> 3)) return;
+    const uint32_t token = a.heads(m), head = m - token * a.heads.d;
     const uint32_t slot = (uint32_t)a.slots[token];
-    uint4 o = make_uint4(0u, 0u, 0u, 0u);
-    if (slot < a.num_slots) o = dequantize_kv_piece(a.pages[kind] + kv_row_offset(a, slot, head), gl, a.d, a.r);
-    uint16_t* x = const_cast<uint16_t*>(a.x[kind]) + token * a.ld[kind] + head * a.ldh[kind];
-    reinterpret_cast<uint4*>(x)[gl] = o;
+    uint4 o[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+    if (slot < a.num_slots) {
+        const int64_t off = kv_row_offset(a, slot, head);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) o[k] = dequantize_kv_piece(a.pages[k] + off, gl, a.d, a.r);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        reinterpret_cast<uint4*>(const_cast<uint16_t*>(a.x[k]) + token * a.ld[k] + head * a.ldh[k])[gl] = o[k];
 }
 
 }  // namespace resq

@@ -55,6 +55,7 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     PagesGeometry g{num_pages, page_size, heads, page_stride, head_stride, row_stride};
     const int rc = check_pages(g, k_pages, v_pages, d_head, r);
     if (rc == RESQ_ERR_SHAPE || rc == RESQ_ERR_BUFFER) return rc;
+    if (tokens > kInt32Max / heads) return RESQ_ERR_SHAPE;
     if (tokens == 0) return RESQ_OK;
     if (!k || !v || !slots) return RESQ_ERR_NULL;
     if (rc != RESQ_OK) return rc;
@@ -67,8 +68,8 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     a.ld[1] = tokens > 1 ? ldv : 0;
     a.ldh[0] = heads > 1 ? ldkh : 0;
     a.ldh[1] = heads > 1 ? ldvh : 0;
-    a.tokens = tokens;
-    a.heads = (int)heads;
+    a.rows = (uint32_t)(tokens * heads);
+    a.heads = FastDiv((uint32_t)heads);
     a.d = (int)d_head;
     a.r = (int)r;
     a.slots = slots;
@@ -77,7 +78,7 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     a.page_stride = g.page_stride;
     a.head_stride = g.head_stride;
     a.row_stride = g.row_stride;
-    a.page_size = (int)page_size;
+    a.page_size = FastDiv((uint32_t)page_size);
     a.num_slots = (uint32_t)(num_pages * page_size);
     done = false;
     return RESQ_OK;
@@ -139,10 +140,19 @@ int resq_kv_slots(const int32_t* lens, const int32_t* new_tokens, int64_t B, int
                           (const void*)block_table, (const void*)lens_out, (const void*)cu_tokens, (const void*)cu_pages,
                           (const void*)positions, (const void*)slots, (const void*)state})
         if (!aligned(p, 4)) return RESQ_ERR_ALIGN;
-    const KvPlanArgs p{lens, new_tokens, (int)B, (int)page_size, (int)num_pages, free_pages, n_free, taken, block_table, ld_table,
+    const KvPlanArgs p{lens, new_tokens, (int)B, FastDiv((uint32_t)page_size), (int)num_pages, free_pages, n_free, taken, block_table, ld_table,
                        (int)width, (int)max_tokens, lens_out, cu_tokens, cu_pages, positions, slots, state};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    launch(kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
+    // one launch, see resq_kv.hip.h; in place a single workgroup serves up to four times its tokens that way (two launches take
+    // longer up to there)
+    const bool in_place = lens == lens_out || taken == state;
+    if (B <= kPlanRequests && (!in_place || max_tokens <= 4 * kPlanTokens)) {
+        const int per_block = in_place ? 4 * kPlanTokens : kPlanTokens;
+        launch(kv_plan_kernel, dim3((unsigned)((max_tokens + per_block - 1) / per_block)), dim3(kPlanThreads), 3 * B * sizeof(int), st, p,
+               per_block);
+        return launch_status();
+    }
+    launch(kv_plan_sums_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
     launch(kv_plan_tokens_kernel, dim3((unsigned)((max_tokens + 255) / 256)), dim3(256), 0, st, p);
     return launch_status();
 }
@@ -194,9 +204,28 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
     const RopeArgs a{static_cast<const uint16_t*>(x), ldx, ldxh, tokens, (int)heads, (int)heads_q, (int)d_head,
                      static_cast<const uint16_t*>(w_q), static_cast<const uint16_t*>(w_k), eps, positions, freq, (int)rot,
                      interleaved != 0, mscale, static_cast<uint16_t*>(y), ldy, ldyh};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (aligned(x, 16) && aligned(y, 16) && ldx % 8 == 0 && ldxh % 8 == 0 && ldy % 8 == 0 && ldyh % 8 == 0 && d_head % 8 == 0 &&
+        rot % (interleaved ? 8 : 16) == 0) {
+        // lanes to a head, and tokens to a workgroup: as many as give 256 threads an angle each, while 512 workgroups remain;
+        // with fewer tokens than that a workgroup takes one round of heads
+        const int lg = d_head <= 64 ? 4 : d_head <= 128 ? 8 : d_head <= 256 ? 16 : 32, groups = 256 / lg;
+        int tb_log2 = 0;
+        while ((2 << tb_log2) <= groups && (rot >> 1) * (2 << tb_log2) <= 256 && tokens >= ((int64_t)512 << (tb_log2 + 1))) ++tb_log2;
+        const int per_block = tokens < 512 ? groups >> tb_log2 : (int)heads;
+        const dim3 grid((unsigned)((tokens + (1 << tb_log2) - 1) >> tb_log2), (unsigned)((heads + per_block - 1) / per_block));
+        const size_t lds = (size_t)(rot >> 1) * sizeof(float2) << tb_log2;
+        switch (lg) {
+            case 4: launch(rope_pieces_kernel<4>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
+            case 8: launch(rope_pieces_kernel<8>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
+            case 16: launch(rope_pieces_kernel<16>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
+            default: launch(rope_pieces_kernel<32>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
+        }
+        return launch_status();
+    }
     const int64_t blocks = (tokens * heads + 3) / 4;
     if (blocks > kInt32Max) return RESQ_ERR_SHAPE;
-    launch(rope_heads_kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    launch(rope_heads_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
     return launch_status();
 }
 
@@ -209,13 +238,9 @@ int resq_append_kv_cache(const void* k, int64_t ldk, int64_t ldkh, const void* v
     const int rc = make_pages_args(a, done, k, ldk, ldkh, v, ldv, ldvh, tokens, heads, d_head, r, slots, k_pages, v_pages, num_pages,
                                    page_size, page_stride, head_stride, row_stride);
     if (rc != RESQ_OK || done) return rc;
-    const int64_t rows = tokens * heads;
-#define RESQ_LAUNCH_APPEND(G)                                                                                             \
-    do {                                                                                                                  \
-        const int64_t blocks = (rows + kKvThreads / G - 1) / (kKvThreads / G);                                      \
-        if (blocks > kInt32Max) return RESQ_ERR_SHAPE;                                                                    \
-        launch(append_kv_cache_kernel<G>, dim3((unsigned)blocks, 2), dim3(kKvThreads), 0, static_cast<hipStream_t>(stream), a); \
-    } while (0)
+#define RESQ_LAUNCH_APPEND(G)                                                                                          \
+    launch(append_kv_cache_kernel<G>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G)), dim3(kKvThreads), 0,      \
+           static_cast<hipStream_t>(stream), a)
     if (d_head <= 128) RESQ_LAUNCH_APPEND(16);
     else if (d_head <= 256) RESQ_LAUNCH_APPEND(32);
     else RESQ_LAUNCH_APPEND(64);
@@ -233,13 +258,9 @@ int resq_gather_kv_cache(const void* k_pages, const void* v_pages, int64_t num_p
     const int rc = make_pages_args(a, done, k, ldk, ldkh, v, ldv, ldvh, tokens, heads, d_head, r, slots, k_pages, v_pages, num_pages,
                                    page_size, page_stride, head_stride, row_stride);
     if (rc != RESQ_OK || done) return rc;
-    const int64_t rows = tokens * heads;
-#define RESQ_LAUNCH_GATHER(G)                                                                                             \
-    do {                                                                                                                  \
-        const int64_t blocks = (rows + kKvThreads / G - 1) / (kKvThreads / G);                                      \
-        if (blocks > kInt32Max) return RESQ_ERR_SHAPE;                                                                    \
-        launch(gather_kv_cache_kernel<G>, dim3((unsigned)blocks, 2), dim3(kKvThreads), 0, static_cast<hipStream_t>(stream), a); \
-    } while (0)
+#define RESQ_LAUNCH_GATHER(G)                                                                                          \
+    launch(gather_kv_cache_kernel<G>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G)), dim3(kKvThreads), 0,      \
+           static_cast<hipStream_t>(stream), a)
     if (d_head <= 128) RESQ_LAUNCH_GATHER(16);
     else if (d_head <= 256) RESQ_LAUNCH_GATHER(32);
     else RESQ_LAUNCH_GATHER(64);
@@ -292,7 +313,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.pages[0] = static_cast<const uint8_t*>(k_pages);
     a.pages[1] = static_cast<const uint8_t*>(v_pages);
     a.num_pages = (int)num_pages;
-    a.page_size = (int)page_size;
+    a.page_size = FastDiv((uint32_t)page_size);
     a.page_stride = g.page_stride;
     a.head_stride = g.head_stride;
     a.row_stride = g.row_stride;

@@ -67,4 +67,18 @@ __device__ __forceinline__ uint32_t pack_bf16_pair(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
+// Division of numbers below 2^31 by one that the host knows: by a product with 2^(31 + s) / d, rounded up, s the bits of d - 1
+// (its error, below 2^-31 of the quotient's unit times the dividend, never reaches the next quotient).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    __host__ FastDiv() = default;
+    __host__ explicit FastDiv(uint32_t n) : d(n) {
+        uint32_t s = 0;
+        while ((1u << s) < n && s < 31) ++s;
+        shift = 31 + s;
+        mul = (uint32_t)(((uint64_t)1 << shift) / n + 1);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)((uint64_t)x * mul >> shift); }
+};
+
 }  // namespace resq
