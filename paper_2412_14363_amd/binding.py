@@ -543,50 +543,47 @@ def resq_dequantize_kv_cache(cache: torch.Tensor, d_head: int, r: int, out: Opti
 
 # ---- the generation step: plan, position embedding, paged K/V cache, attention --------------------------------
 # Sizes are checked here because the kernels rely on them; what the arrays hold (lengths, slots, table entries) is checked by the
-# kernels themselves.
+# kernels themselves.  A step's calls are bounded by the host: each is checked in one expression, and only a call that fails it is
+# looked at part by part for what to say.
 
-def _same_device(where: str, first: torch.Tensor, *others) -> None:
+_BF16, _I32, _U8 = torch.bfloat16, torch.int32, torch.uint8
+
+
+def _need(ok: bool, where: str, what: str) -> None:
+    if not ok:
+        raise ValueError(f"{where}: {what}")
+
+
+def _explain_devices(where: str, *tensors) -> None:
     """All tensors on the current device: that is where the call's kernels run."""
-    if not first.is_cuda:
-        raise ValueError(f"{where}: tensors must live in device memory")
-    dev = first.get_device()
-    if dev != _raw_device():
-        raise ValueError(f"{where}: the tensors are on cuda:{dev}, the current device is cuda:{_raw_device()}")
-    for t in others:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"{where}: tensors on {first.device} and {t.device}")
+    for t in tensors:
+        if t is not None:
+            _need(t.is_cuda, where, "tensors must live in device memory")
+            _need(t.get_device() == _raw_device(), where,
+                  f"a tensor is on {t.device}, the current device is cuda:{_raw_device()}")
 
 
-def _ints(where: str, name: str, t: torch.Tensor, n: Optional[int] = None) -> int:
-    if t.dtype != torch.int32 or t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1) or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{where}: {name} must be a contiguous int32 vector" + (f" of {n}" if n is not None else ""))
-    return t.data_ptr()
+def _explain_ints(where: str, name: str, t: torch.Tensor, n: Optional[int] = None) -> None:
+    _need(t.dtype == _I32 and t.dim() == 1 and t.is_contiguous() and (n is None or t.shape[0] == n), where,
+          f"{name} must be a contiguous int32 vector" + (f" of {n}" if n is not None else ""))
 
 
-def _table(where: str, t: torch.Tensor, batch: int):
-    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != batch or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{where}: block_table must be a row-major int32 [{batch}, pages] tensor")
-    return t.data_ptr(), t.stride(0), t.shape[1]
+def _explain_table(where: str, t: torch.Tensor, batch: int) -> None:
+    _need(t.dtype == _I32 and t.dim() == 2 and t.shape[0] == batch and t.shape[1] > 0 and t.stride(1) == 1, where,
+          f"block_table must be a row-major int32 [{batch}, pages] tensor")
 
 
-def _head_rows(where: str, name: str, t: torch.Tensor):
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{where}: {name} must be a bf16 [tokens, heads, d_head] tensor whose rows are contiguous")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+def _explain_heads(where: str, name: str, t: torch.Tensor) -> None:
+    _need(t.dtype == _BF16 and t.dim() == 3 and t.stride(2) == 1, where,
+          f"{name} must be a bf16 [tokens, heads, d_head] tensor whose rows are contiguous")
 
 
-def _kv_pages(where: str, k_pages: torch.Tensor, v_pages: torch.Tensor, heads: int, d_head: int, r: int):
-    """(k, v, num_pages, page_size, page_stride, head_stride, row_stride) of two uint8 [pages, heads, page_size, row bytes] tensors."""
-    n, h, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
-    need = resq_kv_cache_row_bytes(d_head, r)
-    if need == 0:
-        raise ValueError(f"{where}: invalid (d_head, r) = ({d_head}, {r})")
-    if k_pages.dtype != torch.uint8 or v_pages.dtype != torch.uint8 or h != heads or width < need or k_pages.stride(3) != 1:
-        raise ValueError(f"{where}: pages must be uint8 [pages, {heads}, page_size, >= {need}] tensors whose rows are contiguous")
-    if v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride():
-        raise ValueError(f"{where}: k_pages and v_pages must have the same shape and strides")
-    a, b, c, _ = k_pages.stride()
-    return k_pages.data_ptr(), v_pages.data_ptr(), n, size, a, b, c
+def _explain_pages(where: str, k: torch.Tensor, v: torch.Tensor, heads: int, d: int, r: int) -> None:
+    need = resq_kv_cache_row_bytes(d, r)
+    _need(need > 0, where, f"invalid (d_head, r) = ({d}, {r})")
+    _need(k.dim() == 4 and k.dtype == _U8 and v.dtype == _U8 and k.shape[1] == heads and k.shape[3] >= need and k.stride(3) == 1, where,
+          f"pages must be uint8 [pages, {heads}, page_size, >= {need}] tensors whose rows are contiguous")
+    _need(v.shape == k.shape and v.stride() == k.stride(), where, "k_pages and v_pages must have the same shape and strides")
 
 
 class KvSlots:
@@ -594,12 +591,19 @@ class KvSlots:
     state [2] (entries of the free list gone, status).  All start at 0, slots at -1."""
 
     def __init__(self, batch: int, max_tokens: int, device="cuda"):
+        self.batch, self.max_tokens = batch, max_tokens
         self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.cu_tokens = torch.zeros(batch + 1, dtype=torch.int32, device=device)
         self.cu_pages = torch.zeros(batch + 1, dtype=torch.int32, device=device)
         self.positions = torch.zeros(max_tokens, dtype=torch.int32, device=device)
         self.slots = torch.full((max_tokens,), -1, dtype=torch.int32, device=device)
         self.state = torch.zeros(2, dtype=torch.int32, device=device)
+        self.device_index = self.lens.get_device()
+
+    @property
+    def pointers(self):
+        return (self.lens.data_ptr(), self.cu_tokens.data_ptr(), self.cu_pages.data_ptr(), self.positions.data_ptr(),
+                self.slots.data_ptr(), self.state.data_ptr())
 
 
 def resq_kv_slots(lens: torch.Tensor, new_tokens: torch.Tensor, free_pages: torch.Tensor, taken: Optional[torch.Tensor],
@@ -608,25 +612,36 @@ def resq_kv_slots(lens: torch.Tensor, new_tokens: torch.Tensor, free_pages: torc
     """The plan of a step: positions and slots of new_tokens[b] tokens of each request behind its lens[b], pages off the free
     list into block_table.  taken: how many of free_pages are gone (None: out.state's first entry, i.e. go on from the call
     before).  lens may be out.lens.  out.state[1] is the status, see include/resq.h."""
-    where = "resq_kv_slots"
     batch = lens.shape[0]
     if out is None:
-        if max_tokens is None:
-            raise ValueError(f"{where}: give out or max_tokens")
+        _need(max_tokens is not None, "resq_kv_slots", "give out or max_tokens")
         out = KvSlots(batch, max_tokens, lens.device)
+    elif not isinstance(out, KvSlots):
+        raise ValueError("resq_kv_slots: out must be a KvSlots")
     if taken is None:
         taken = out.state[:1]
-    _same_device(where, lens, new_tokens, free_pages, taken, block_table, out.lens, out.cu_tokens, out.cu_pages, out.positions,
-                 out.slots, out.state)
-    table, ld_table, width = _table(where, block_table, batch)
-    cap = out.slots.shape[0]
+    cap = out.max_tokens
+    dev = lens.get_device()
+    ld_table, one = block_table.stride() if block_table.dim() == 2 else (0, 0)
+    if not (lens.dtype == _I32 and new_tokens.dtype == _I32 and free_pages.dtype == _I32 and taken.dtype == _I32
+            and block_table.dtype == _I32 and lens.shape == new_tokens.shape == (batch,) and out.batch == batch
+            and free_pages.dim() == 1 and taken.shape == (1,) and lens.is_contiguous() and new_tokens.is_contiguous()
+            and free_pages.is_contiguous() and one == 1 and block_table.shape[0] == batch and dev >= 0 and dev == _raw_device()
+            and new_tokens.get_device() == dev and free_pages.get_device() == dev and taken.get_device() == dev
+            and block_table.get_device() == dev and out.device_index == dev):
+        where = "resq_kv_slots"
+        _explain_devices(where, lens, new_tokens, free_pages, taken, block_table, out.lens)
+        _explain_ints(where, "lens", lens)
+        _explain_ints(where, "new_tokens", new_tokens, batch)
+        _explain_ints(where, "free_pages", free_pages)
+        _explain_ints(where, "taken", taken, 1)
+        _explain_table(where, block_table, batch)
+        raise ValueError(f"{where}: out holds {out.batch} requests, lens {batch}")
     st = lib().resq_kv_slots(
-        _ints(where, "lens", lens), _ints(where, "new_tokens", new_tokens, batch), batch, page_size, num_pages,
-        _ints(where, "free_pages", free_pages), free_pages.shape[0], _ints(where, "taken", taken, 1), table, ld_table, width, cap,
-        _ints(where, "out.lens", out.lens, batch), _ints(where, "out.cu_tokens", out.cu_tokens, batch + 1),
-        _ints(where, "out.cu_pages", out.cu_pages, batch + 1), _ints(where, "out.positions", out.positions, cap),
-        _ints(where, "out.slots", out.slots), _ints(where, "out.state", out.state, 2), _stream(stream))
-    _check(st, where)
+        lens.data_ptr(), new_tokens.data_ptr(), batch, page_size, num_pages, free_pages.data_ptr(), free_pages.shape[0],
+        taken.data_ptr(), block_table.data_ptr(), ld_table, block_table.shape[1], cap, *out.pointers, _stream(stream))
+    if st:
+        _check(st, "resq_kv_slots")
     return out
 
 
@@ -650,28 +665,46 @@ def resq_rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor], freq: Op
     """x: bf16 [tokens, heads, d_head], the first heads_q heads (None: all) queries, the others keys; positions int32 [tokens];
     freq fp64 [rot / 2] (None or empty: no rotation); w_q, w_k: bf16 [d_head] weights of the heads' norm (None: no norm).
     out may be x."""
-    where = "resq_rope_heads"
-    px, ldx, ldxh = _head_rows(where, "x", x)
-    tokens, heads, d = x.shape
+    tokens, heads, d = shape = x.shape
     if heads_q is None:
         heads_q = heads
     if out is None:
-        out = torch.empty((tokens, heads, d), dtype=torch.bfloat16, device=x.device)
-    py, ldy, ldyh = _head_rows(where, "out", out)
-    _same_device(where, x, positions, freq, w_q, w_k, out)
+        out = torch.empty(shape, dtype=_BF16, device=x.device)
     rot = 0 if freq is None else 2 * freq.shape[0]
-    if out.shape != x.shape or not 0 <= heads_q <= heads:
-        raise ValueError(f"{where}: out {tuple(out.shape)}, x {tuple(x.shape)} or heads_q = {heads_q} do not match")
-    if rot and (positions is None or freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous()):
-        raise ValueError(f"{where}: freq must be a contiguous fp64 [rot / 2] tensor, with positions")
-    for name, w in (("w_q", w_q), ("w_k", w_k)):
-        if w is not None and (w.dtype != torch.bfloat16 or w.shape != (d,) or not w.is_contiguous()):
-            raise ValueError(f"{where}: {name} must be a contiguous bf16 [{d}] tensor")
-    st = lib().resq_rope_heads(px, ldx, ldxh, tokens, heads_q, heads - heads_q, d,
-                               None if w_q is None else w_q.data_ptr(), None if w_k is None else w_k.data_ptr(), eps,
-                               _ints(where, "positions", positions, tokens) if rot else None, freq.data_ptr() if rot else None,
-                               rot, int(interleaved), mscale, py, ldy, ldyh, _stream(stream))
-    _check(st, where)
+    dev = x.get_device()
+    ldx, ldxh, one = x.stride()
+    ldy, ldyh, one_y = out.stride()
+    pos = freqs = wq = wk = None
+    ok = (x.dtype == _BF16 and out.dtype == _BF16 and one == 1 and one_y == 1 and out.shape == shape and 0 <= heads_q <= heads
+          and dev >= 0 and dev == _raw_device() and out.get_device() == dev)
+    if rot and ok:
+        ok = (positions is not None and positions.dtype == _I32 and positions.shape == (tokens,) and positions.is_contiguous()
+              and freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous() and positions.get_device() == dev
+              and freq.get_device() == dev)
+        if ok:
+            pos, freqs = positions.data_ptr(), freq.data_ptr()
+    if w_q is not None and ok:
+        ok = w_q.dtype == _BF16 and w_q.shape == (d,) and w_q.is_contiguous() and w_q.get_device() == dev
+        wq = w_q.data_ptr()
+    if w_k is not None and ok:
+        ok = w_k.dtype == _BF16 and w_k.shape == (d,) and w_k.is_contiguous() and w_k.get_device() == dev
+        wk = w_k.data_ptr()
+    if not ok:
+        where = "resq_rope_heads"
+        _explain_heads(where, "x", x)
+        _explain_heads(where, "out", out)
+        _explain_devices(where, x, positions, freq, w_q, w_k, out)
+        _need(out.shape == shape and 0 <= heads_q <= heads, where,
+              f"out {tuple(out.shape)}, x {tuple(shape)} or heads_q = {heads_q} do not match")
+        _need(not rot or (positions is not None and freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous()), where,
+              "freq must be a contiguous fp64 [rot / 2] tensor, with positions")
+        if rot:
+            _explain_ints(where, "positions", positions, tokens)
+        raise ValueError(f"{where}: w_q and w_k must be contiguous bf16 [{d}] tensors")
+    st = lib().resq_rope_heads(x.data_ptr(), ldx, ldxh, tokens, heads_q, heads - heads_q, d, wq, wk, eps, pos, freqs, rot,
+                               1 if interleaved else 0, mscale, out.data_ptr(), ldy, ldyh, _stream(stream))
+    if st:
+        _check(st, "resq_rope_heads")
     return out
 
 
@@ -679,17 +712,31 @@ def resq_append_kv_cache(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
                          r: int, stream=None) -> None:
     """k, v: bf16 [tokens, heads, d_head], quantized into rows `slots` (int32 [tokens], below 0: left out) of the uint8
     [pages, heads, page_size, row bytes] pages."""
-    where = "resq_append_kv_cache"
-    pk, ldk, ldkh = _head_rows(where, "k", k)
-    pv, ldv, ldvh = _head_rows(where, "v", v)
-    tokens, heads, d = k.shape
-    if v.shape != k.shape:
-        raise ValueError(f"{where}: k {tuple(k.shape)} and v {tuple(v.shape)} do not match")
-    _same_device(where, k, v, slots, k_pages, v_pages)
-    pages = _kv_pages(where, k_pages, v_pages, heads, d, r)
-    st = lib().resq_append_kv_cache(pk, ldk, ldkh, pv, ldv, ldvh, tokens, heads, d, r, _ints(where, "slots", slots, tokens), *pages,
+    tokens, heads, d = shape = k.shape
+    dev = k.get_device()
+    ldk, ldkh, one = k.stride()
+    ldv, ldvh, one_v = v.stride() if v.dim() == 3 else (0, 0, 0)
+    need = resq_kv_cache_row_bytes(d, r)
+    n, h, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
+    strides = k_pages.stride()
+    if not (k.dtype == _BF16 and v.dtype == _BF16 and slots.dtype == _I32 and k_pages.dtype == _U8 and v_pages.dtype == _U8
+            and one == 1 and one_v == 1 and v.shape == shape and slots.shape == (tokens,) and slots.is_contiguous()
+            and h == heads and 0 < need <= width and strides[3] == 1 and v_pages.shape == k_pages.shape and v_pages.stride() == strides
+            and dev >= 0 and dev == _raw_device() and v.get_device() == dev and slots.get_device() == dev
+            and k_pages.get_device() == dev and v_pages.get_device() == dev):
+        where = "resq_append_kv_cache"
+        _explain_heads(where, "k", k)
+        _explain_heads(where, "v", v)
+        _need(v.shape == shape, where, f"k {tuple(shape)} and v {tuple(v.shape)} do not match")
+        _explain_devices(where, k, v, slots, k_pages, v_pages)
+        _explain_pages(where, k_pages, v_pages, heads, d, r)
+        _explain_ints(where, "slots", slots, tokens)
+        raise ValueError(f"{where}: invalid arguments")
+    st = lib().resq_append_kv_cache(k.data_ptr(), ldk, ldkh, v.data_ptr(), ldv, ldvh, tokens, heads, d, r, slots.data_ptr(),
+                                    k_pages.data_ptr(), v_pages.data_ptr(), n, size, strides[0], strides[1], strides[2],
                                     _stream(stream))
-    _check(st, where)
+    if st:
+        _check(st, "resq_append_kv_cache")
 
 
 def resq_gather_kv_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor, r: int,
@@ -697,23 +744,39 @@ def resq_gather_kv_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: to
                          stream=None):
     """The values of the rows in `slots` (int32 [tokens]), bf16 [tokens, heads, d_head] each for keys and values; zeros for slots
     outside the pages.  d_head is that of k where k is given."""
-    where = "resq_gather_kv_cache"
-    if k_pages.dim() != 4:
-        raise ValueError(f"{where}: pages must be [pages, heads, page_size, row bytes] tensors")
-    tokens, heads = slots.shape[0], k_pages.shape[1]
-    if k is None and d_head is None:
-        raise ValueError(f"{where}: give k or d_head")
-    d = d_head if k is None else k.shape[-1]
-    k, v = (torch.empty((tokens, heads, d), dtype=torch.bfloat16, device=k_pages.device) if t is None else t for t in (k, v))
-    pk, ldk, ldkh = _head_rows(where, "k", k)
-    pv, ldv, ldvh = _head_rows(where, "v", v)
-    if k.shape != (tokens, heads, d) or v.shape != k.shape or (d_head is not None and d_head != d):
-        raise ValueError(f"{where}: k {tuple(k.shape)} and v {tuple(v.shape)} must be [{tokens}, {heads}, {d_head or d}]")
-    _same_device(where, k_pages, v_pages, slots, k, v)
-    pages = _kv_pages(where, k_pages, v_pages, heads, d, r)
-    st = lib().resq_gather_kv_cache(*pages, _ints(where, "slots", slots, tokens), tokens, heads, d, r, pk, ldk, ldkh, pv, ldv, ldvh,
+    _need(k_pages.dim() == 4, "resq_gather_kv_cache", "pages must be [pages, heads, page_size, row bytes] tensors")
+    n, heads, size, width = k_pages.shape
+    tokens = slots.shape[0]
+    if k is None or v is None:
+        _need(k is not None or d_head is not None, "resq_gather_kv_cache", "give k or d_head")
+        shape = (tokens, heads, d_head if k is None else k.shape[-1])
+        k, v = (torch.empty(shape, dtype=_BF16, device=k_pages.device) if t is None else t for t in (k, v))
+    shape = k.shape
+    d = shape[-1]
+    dev = k_pages.get_device()
+    ldk, ldkh, one = k.stride() if k.dim() == 3 else (0, 0, 0)
+    ldv, ldvh, one_v = v.stride() if v.dim() == 3 else (0, 0, 0)
+    need = resq_kv_cache_row_bytes(d, r)
+    strides = k_pages.stride()
+    if not (k.dtype == _BF16 and v.dtype == _BF16 and slots.dtype == _I32 and k_pages.dtype == _U8 and v_pages.dtype == _U8
+            and one == 1 and one_v == 1 and shape == (tokens, heads, d) and v.shape == shape and (d_head is None or d_head == d)
+            and slots.dim() == 1 and slots.is_contiguous() and 0 < need <= width and strides[3] == 1 and v_pages.shape == k_pages.shape
+            and v_pages.stride() == strides and dev >= 0 and dev == _raw_device() and k.get_device() == dev and v.get_device() == dev
+            and slots.get_device() == dev and v_pages.get_device() == dev):
+        where = "resq_gather_kv_cache"
+        _explain_heads(where, "k", k)
+        _explain_heads(where, "v", v)
+        _need(shape == (tokens, heads, d) and v.shape == shape and (d_head is None or d_head == d), where,
+              f"k {tuple(shape)} and v {tuple(v.shape)} must be [{tokens}, {heads}, {d_head or d}]")
+        _explain_devices(where, k_pages, v_pages, slots, k, v)
+        _explain_pages(where, k_pages, v_pages, heads, d, r)
+        _explain_ints(where, "slots", slots, tokens)
+        raise ValueError(f"{where}: invalid arguments")
+    st = lib().resq_gather_kv_cache(k_pages.data_ptr(), v_pages.data_ptr(), n, size, strides[0], strides[1], strides[2],
+                                    slots.data_ptr(), tokens, heads, d, r, k.data_ptr(), ldk, ldkh, v.data_ptr(), ldv, ldvh,
                                     _stream(stream))
-    _check(st, where)
+    if st:
+        _check(st, "resq_gather_kv_cache")
     return k, v
 
 
@@ -736,34 +799,54 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
                          workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of one new token of each sequence, q: bf16 [batch, heads, d_head], over the first lens[b] tokens of the pages that
     block_table [batch, pages] names.  scale: d_head^-0.5 when None.  lse: fp32 [batch, heads], written where given."""
-    where = "resq_attend_kv_cache"
-    pq, ldq, ldqh = _head_rows(where, "q", q)
-    batch, heads, d = q.shape
+    batch, heads, d = shape = q.shape
     if out is None:
-        out = torch.empty((batch, heads, d), dtype=torch.bfloat16, device=q.device)
-    po, ldo, ldoh = _head_rows(where, "out", out)
-    heads_k = k_pages.shape[1] if k_pages.dim() == 4 else 0
-    if out.shape != q.shape or heads_k == 0 or heads % heads_k:
-        raise ValueError(f"{where}: q {tuple(q.shape)}, out {tuple(out.shape)} or {heads_k} K/V heads do not match")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads) or not lse.is_contiguous()):
-        raise ValueError(f"{where}: lse must be a contiguous fp32 [{batch}, {heads}] tensor")
+        out = torch.empty(shape, dtype=_BF16, device=q.device)
     if batch == 0:
         return out
-    need = resq_attend_kv_cache_workspace_bytes(batch, heads, heads_k, d)
+    n, heads_k, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
-        if stream is not None:   # made on the current stream, used on another one
+        nbytes = resq_attend_kv_cache_workspace_bytes(batch, heads, heads_k, d)
+        workspace = torch.empty(max(nbytes, 1), dtype=_U8, device=q.device)
+        if stream is not None and q.is_cuda:   # made on the current stream, used on another one
             workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
-    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError(f"{where}: workspace must be a contiguous uint8 tensor")
-    _same_device(where, q, k_pages, v_pages, lens, block_table, out, lse, workspace)
-    pages = _kv_pages(where, k_pages, v_pages, heads_k, d, r)
-    table, ld_table, width = _table(where, block_table, batch)
+    dev = q.get_device()
+    ldq, ldqh, one = q.stride()
+    ldo, ldoh, one_o = out.stride() if out.dim() == 3 else (0, 0, 0)
+    need = resq_kv_cache_row_bytes(d, r)
+    strides = k_pages.stride()
+    ld_table, one_t = block_table.stride() if block_table.dim() == 2 else (0, 0)
+    sums = None
+    ok = (q.dtype == _BF16 and out.dtype == _BF16 and lens.dtype == _I32 and block_table.dtype == _I32 and k_pages.dtype == _U8
+          and v_pages.dtype == _U8 and workspace.dtype == _U8 and one == 1 and one_o == 1 and one_t == 1 and out.shape == shape
+          and heads_k > 0 and heads % heads_k == 0 and 0 < need <= width and strides[3] == 1 and v_pages.shape == k_pages.shape
+          and v_pages.stride() == strides and lens.shape == (batch,) and lens.is_contiguous() and block_table.shape[0] == batch
+          and workspace.is_contiguous() and dev >= 0 and dev == _raw_device() and out.get_device() == dev and lens.get_device() == dev
+          and block_table.get_device() == dev and k_pages.get_device() == dev and v_pages.get_device() == dev
+          and workspace.get_device() == dev)
+    if lse is not None and ok:
+        ok = lse.dtype == torch.float32 and lse.shape == (batch, heads) and lse.is_contiguous() and lse.get_device() == dev
+        sums = lse.data_ptr()
+    if not ok:
+        where = "resq_attend_kv_cache"
+        _explain_heads(where, "q", q)
+        _explain_heads(where, "out", out)
+        _need(out.shape == shape and heads_k > 0 and heads % heads_k == 0, where,
+              f"q {tuple(shape)}, out {tuple(out.shape)} or {heads_k} K/V heads do not match")
+        _need(lse is None or (lse.dtype == torch.float32 and lse.shape == (batch, heads) and lse.is_contiguous()), where,
+              f"lse must be a contiguous fp32 [{batch}, {heads}] tensor")
+        _need(workspace.dtype == _U8 and workspace.is_contiguous(), where, "workspace must be a contiguous uint8 tensor")
+        _explain_devices(where, q, k_pages, v_pages, lens, block_table, out, lse, workspace)
+        _explain_pages(where, k_pages, v_pages, heads_k, d, r)
+        _explain_table(where, block_table, batch)
+        _explain_ints(where, "lens", lens, batch)
+        raise ValueError(f"{where}: invalid arguments")
     st = lib().resq_attend_kv_cache(
-        pq, ldq, ldqh, batch, heads, heads_k, d, r, _ints(where, "lens", lens, batch), table, ld_table, width, *pages,
-        d ** -0.5 if scale is None else scale, softcap, window, po, ldo, ldoh, None if lse is None else lse.data_ptr(),
-        workspace.data_ptr(), workspace.numel(), _stream(stream))
-    _check(st, where)
+        q.data_ptr(), ldq, ldqh, batch, heads, heads_k, d, r, lens.data_ptr(), block_table.data_ptr(), ld_table, block_table.shape[1],
+        k_pages.data_ptr(), v_pages.data_ptr(), n, size, strides[0], strides[1], strides[2], d ** -0.5 if scale is None else scale,
+        softcap, window, out.data_ptr(), ldo, ldoh, sums, workspace.data_ptr(), workspace.shape[0], _stream(stream))
+    if st:
+        _check(st, "resq_attend_kv_cache")
     return out
 
 

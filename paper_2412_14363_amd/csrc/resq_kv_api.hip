@@ -143,11 +143,10 @@ int resq_kv_slots(const int32_t* lens, const int32_t* new_tokens, int64_t B, int
     const KvPlanArgs p{lens, new_tokens, (int)B, FastDiv((uint32_t)page_size), (int)num_pages, free_pages, n_free, taken, block_table, ld_table,
                        (int)width, (int)max_tokens, lens_out, cu_tokens, cu_pages, positions, slots, state};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    // one launch, see resq_kv.hip.h; in place a single workgroup serves up to four times its tokens that way (two launches take
-    // longer up to there)
+    // one launch where it can be, see resq_kv.hip.h
     const bool in_place = lens == lens_out || taken == state;
-    if (B <= kPlanRequests && (!in_place || max_tokens <= 4 * kPlanTokens)) {
-        const int per_block = in_place ? 4 * kPlanTokens : kPlanTokens;
+    if (B <= kPlanRequests && (!in_place || max_tokens <= kPlanTokensInPlace)) {
+        const int per_block = in_place ? kPlanTokensInPlace : kPlanTokens;
         launch(kv_plan_kernel, dim3((unsigned)((max_tokens + per_block - 1) / per_block)), dim3(kPlanThreads), 3 * B * sizeof(int), st, p,
                per_block);
         return launch_status();
@@ -239,7 +238,7 @@ int resq_append_kv_cache(const void* k, int64_t ldk, int64_t ldkh, const void* v
                                    page_size, page_stride, head_stride, row_stride);
     if (rc != RESQ_OK || done) return rc;
 #define RESQ_LAUNCH_APPEND(G)                                                                                          \
-    launch(append_kv_cache_kernel<G>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G)), dim3(kKvThreads), 0,      \
+    launch(append_kv_cache_kernel<G>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G), 2), dim3(kKvThreads), 0,   \
            static_cast<hipStream_t>(stream), a)
     if (d_head <= 128) RESQ_LAUNCH_APPEND(16);
     else if (d_head <= 256) RESQ_LAUNCH_APPEND(32);
