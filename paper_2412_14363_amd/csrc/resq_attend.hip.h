@@ -205,8 +205,11 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
         total += part[w];
     }
     total = __builtin_amdgcn_readfirstlane(total);
-    const int W = min(total, (int)gridDim.x), w0 = blockIdx.x;
-    if (w0 >= W) return;
+    // Workgroups go to the eight dies in turn; runs that follow one another, whose heads lie side by side in token-major pages (and
+    // whose queries share a K/V head's rows where they are more than 16), stay on one die and meet in its L2.
+    const int W = min(total, (int)gridDim.x), per_die = (W + 7) >> 3;
+    const int w0 = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per_die || w0 >= W) return;
     const int share = total / W, rest = total - share * W;   // the first `rest` runs are a unit longer
     int u = w0 * share + min(w0, rest);
     const int u_end = u + share + (w0 < rest);

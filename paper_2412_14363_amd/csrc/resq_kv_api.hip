@@ -115,7 +115,7 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
-    const int64_t grid = units < 256 * OCC ? units : 256 * OCC;
+    const int64_t grid = units < 256 * OCC ? (units + 7) / 8 * 8 : 256 * OCC;   // a multiple of the dies
     launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
     launch(attend_join_kernel, dim3((unsigned)(a.B * a.heads_k * a.share)), dim3(kAttendThreads), 0, st, args);
     return launch_status();
@@ -343,7 +343,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
                                                                                    : launch_attend<4, 16, 1>(a, units, st);
     if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
                            : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 1>(a, units, st);
-    return r <= 32 ? launch_attend<16, 2, 2>(a, units, st) : launch_attend<16, 8, 1>(a, units, st);
+    return r <= 32 ? launch_attend<16, 2, 1>(a, units, st) : launch_attend<16, 8, 1>(a, units, st);
 }
 
 }  // extern "C"
