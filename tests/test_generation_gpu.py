@@ -423,6 +423,19 @@ def test_attend_equal_calls_give_equal_bits(rq):
         assert torch.equal(rq.resq_attend_kv_cache(*case, 16, lse=lse, workspace=work), first[0]) and torch.equal(lse, first[1])
 
 
+def test_attend_calls_of_many_sizes_share_a_workspace(rq):
+    # one after another without a wait between them, each with other heads, lengths and cuts than the one before, and again
+    cases = [(attend_case(31, [3000, 10, 7777, 0, 128], 16, 4, 128, 16, 32), 16), (attend_case(32, [40000], 8, 1, 64, 8, 16), 8),
+             (attend_case(33, [700] * 40, 6, 6, 64, 8, 24, "token"), 8), (attend_case(34, [900, 5, 2000], 34, 2, 96, 0, 16), 0),
+             (attend_case(35, [0, 0], 2, 1, 64, 8, 16), 8), (attend_case(36, [1500, 1400], 4, 2, 256, 32, 16), 32)]
+    work = max((rq.resq_attend_kv_cache_workspace(*case[0].shape[:2], case[1].shape[1], case[0].shape[2]) for case, _ in cases), key=len)
+    want = [check_attend(rq, *case, r)[0] for case, r in cases]
+    torch.cuda.synchronize()
+    got = [[rq.resq_attend_kv_cache(*case, r, workspace=work) for case, r in cases] for _ in range(30)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for round_ in got for a, b in zip(round_, want))
+
+
 def test_attend_on_other_streams(rq):
     case = attend_case(15, [3000, 10, 777], 16, 4, 128, 16, 32)
     want = check_attend(rq, *case, 16)[0]
