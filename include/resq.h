@@ -463,11 +463,12 @@ int resq_dequantize_kv_cache(const void* cache, int64_t row_bytes, int64_t rows,
  *   p * page_stride + h * head_stride + i * row_stride
  * of its array (strides in bytes, multiples of 4, each at least resq_kv_cache_row_bytes; an axis of one entry has no stride;
  * rows do not overlap).  A SLOT is p * page_size + i, num_pages * page_size <= 2^31 - 1.  A row of the BLOCK TABLE names the
- * pages of a sequence in order: its token t is in row t % page_size of page block_table[b][t / page_size].  The attention reads
- * fastest where a head's rows of a page are contiguous (row_stride = row bytes), page_size is a multiple of 16, and the arrays,
- * page_stride and head_stride are multiples of 16.
+ * pages of a sequence in order: its token t is in row t % page_size of page block_table[b][t / page_size].  Any strides do for the
+ * attention; it reads fastest where page_size is a multiple of 16 and row_stride below 2^26.
  * Common to these calls: lengths, positions, slots and table entries are int32 (4-byte aligned); head vectors are bf16 with a
- * stride from token to token and one from head to head in elements (strides of inputs may be 0).
+ * stride from token to token and one from head to head in elements (strides of inputs may be 0).  Calls of more rows than a launch
+ * can count (about 2^26 of 512 channels, 2^28 of 128) are refused with RESQ_ERR_SHAPE.  resq_time_next_kernel times a call's first
+ * kernel.
  *
  * The plan of a step, on the GPU: request b has lens[b] tokens in its pages and gets new_tokens[b] more (0 is fine).
  * Its new tokens follow those of the requests before it in the batch; pages that it lacks are taken off the front of the free
@@ -562,7 +563,8 @@ int resq_gather_kv_cache(const void* k_pages, const void* v_pages, int64_t num_p
  *   block_table  int32 [B, ld_table], `width` entries used of each row                    (read)
  *   lse      fp32 [B, heads_q] or null                                                    (written)
  *   d_head   multiple of 8, 8 .. 256; r as resq_quantize_kv_cache; heads_q a multiple of heads_k; B, heads_q <= 65535
- *   scale    > 0; softcap >= 0 (0: none); window >= 0 (0: none)
+ *   scale    > 0; softcap 0 (none) or a normal number above; window >= 0 (0: none)
+ *   B * heads_q < 2^24, and B * heads_k * ceil(heads_q / heads_k / 16) * (ceil(width * page_size / 128) + 3) < 2^31
  *   workspace  device memory, 256-byte aligned, resq_attend_kv_cache_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents
  *            meaningless before and after; calls that overlap (different streams) need one each
  * The work is cut by the lengths that the GPU finds, so that a captured call serves any lengths.  The cuts, and with them the

@@ -615,7 +615,11 @@ def resq_kv_slots(lens: torch.Tensor, new_tokens: torch.Tensor, free_pages: torc
     batch = lens.shape[0]
     if out is None:
         _need(max_tokens is not None, "resq_kv_slots", "give out or max_tokens")
-        out = KvSlots(batch, max_tokens, lens.device)
+        if stream is not None and lens.is_cuda:   # its buffers are cleared where the plan runs
+            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+                out = KvSlots(batch, max_tokens, lens.device)
+        else:
+            out = KvSlots(batch, max_tokens, lens.device)
     elif not isinstance(out, KvSlots):
         raise ValueError("resq_kv_slots: out must be a KvSlots")
     if taken is None:
@@ -844,7 +848,7 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     st = lib().resq_attend_kv_cache(
         q.data_ptr(), ldq, ldqh, batch, heads, heads_k, d, r, lens.data_ptr(), block_table.data_ptr(), ld_table, block_table.shape[1],
         k_pages.data_ptr(), v_pages.data_ptr(), n, size, strides[0], strides[1], strides[2], d ** -0.5 if scale is None else scale,
-        softcap, window, out.data_ptr(), ldo, ldoh, sums, workspace.data_ptr(), workspace.shape[0], _stream(stream))
+        softcap, window, out.data_ptr(), ldo, ldoh, sums, workspace.data_ptr(), workspace.numel(), _stream(stream))
     if st:
         _check(st, "resq_attend_kv_cache")
     return out

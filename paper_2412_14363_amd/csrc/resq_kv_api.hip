@@ -1,5 +1,6 @@
 // C ABI of the generation step's side of the library: position embedding, paged K/V cache, attention over it.
 // Argument checks on the host, then launches on the caller's stream.  See include/resq.h for the contract of every entry.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -55,7 +56,8 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     PagesGeometry g{num_pages, page_size, heads, page_stride, head_stride, row_stride};
     const int rc = check_pages(g, k_pages, v_pages, d_head, r);
     if (rc == RESQ_ERR_SHAPE || rc == RESQ_ERR_BUFFER) return rc;
-    if (tokens > kInt32Max / heads) return RESQ_ERR_SHAPE;
+    const int64_t lanes = d_head <= 128 ? 16 : d_head <= 256 ? 32 : 64;   // of a row (below)
+    if (tokens > kInt32Max / heads || !launch_fits(tokens * heads + 63, lanes)) return RESQ_ERR_SHAPE;
     if (tokens == 0) return RESQ_OK;
     if (!k || !v || !slots) return RESQ_ERR_NULL;
     if (rc != RESQ_OK) return rc;
@@ -214,6 +216,7 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
         const int per_block = tokens < 512 ? groups >> tb_log2 : (int)heads;
         const dim3 grid((unsigned)((tokens + (1 << tb_log2) - 1) >> tb_log2), (unsigned)((heads + per_block - 1) / per_block));
         const size_t lds = (size_t)(rot >> 1) * sizeof(float2) << tb_log2;
+        if (!launch_fits(grid.x, 256)) return RESQ_ERR_SHAPE;
         switch (lg) {
             case 4: launch(rope_pieces_kernel<4>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
             case 8: launch(rope_pieces_kernel<8>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
@@ -223,7 +226,7 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
         return launch_status();
     }
     const int64_t blocks = (tokens * heads + 3) / 4;
-    if (blocks > kInt32Max) return RESQ_ERR_SHAPE;
+    if (!launch_fits(blocks, 256)) return RESQ_ERR_SHAPE;
     launch(rope_heads_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
     return launch_status();
 }
@@ -281,7 +284,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
                          int64_t ldo, int64_t ldoh, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     const size_t need = resq_attend_kv_cache_workspace_bytes(B, heads_q, heads_k, d_head);
     if (need == 0 || ldq < 0 || ldqh < 0 || width < 1 || width > kInt32Max || (B > 1 && ld_table < width) || !(scale > 0.0f) ||
-        !isfinite(scale) || !(softcap >= 0.0f) || !isfinite(softcap) || window < 0 || !rows_apart(B, ldo, heads_q, ldoh, d_head))
+        !isfinite(scale) || !(softcap == 0.0f || softcap >= FLT_MIN) || !isfinite(softcap) || window < 0 || !rows_apart(B, ldo, heads_q, ldoh, d_head))
         return RESQ_ERR_SHAPE;
     PagesGeometry g{num_pages, page_size, heads_k, page_stride, head_stride, row_stride};
     const int rc = check_pages(g, k_pages, v_pages, d_head, r);
@@ -296,7 +299,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     // units of the longest sequences that the table can name: counted in 32 bits
     const int64_t qtiles = (heads_q / heads_k + kAttendRows - 1) / kAttendRows;
     const int64_t units = B * heads_k * qtiles * ((longest + kAttendUnit - 1) / kAttendUnit + kAttendHeadCost);
-    if (units > kInt32Max) return RESQ_ERR_SHAPE;
+    if (units > kInt32Max || !launch_fits(B * heads_q, kAttendThreads)) return RESQ_ERR_SHAPE;
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(q);
     a.ldq = ldq;

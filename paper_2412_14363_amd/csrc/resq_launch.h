@@ -24,6 +24,9 @@ inline void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t lds, 
     hipExtLaunchKernelGGL(kernel, grid, block, lds, st, e0, e1, 0, args...);
 }
 
+// a launch counts the threads along an axis in 32 bits
+inline bool launch_fits(int64_t blocks, int64_t threads) { return blocks <= 0xFFFFFFFFll / threads; }
+
 // a head's row of the compact K/V cache: d_head and the width r of its 8-bit group
 inline bool kv_head_ok(int64_t d_head, int64_t r) {
     return d_head >= 8 && d_head <= 512 && d_head % 8 == 0 && r >= 0 && r <= d_head && r % 8 == 0;

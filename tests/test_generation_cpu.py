@@ -42,7 +42,8 @@ ROPE = dict(x=P, ldx=1280, ldxh=128, tokens=8, heads_q=8, heads_k=2, d=128, w_q=
     (dict(eps=-1.0), SHAPE), (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE), (dict(ldx=-1), SHAPE), (dict(ldyh=120), SHAPE),
     (dict(ldy=1279), SHAPE), (dict(ldy=128, ldyh=1000, y=2 * P), SHAPE), (dict(ldx=1288), SHAPE), (dict(x=None), NULL),
     (dict(y=None), NULL), (dict(positions=None), NULL), (dict(freq=None), NULL), (dict(w_q=None), NULL), (dict(w_k=None), NULL),
-    (dict(x=P + 1), ALIGN), (dict(freq=P + 4), ALIGN), (dict(w_q=P + 1), ALIGN), (dict(positions=P + 2), ALIGN), (dict(tokens=0, x=None), OK)])
+    (dict(x=P + 1), ALIGN), (dict(freq=P + 4), ALIGN), (dict(w_q=P + 1), ALIGN), (dict(positions=P + 2), ALIGN), (dict(tokens=0, x=None), OK),
+    (dict(tokens=1 << 29, heads_q=1, heads_k=0), SHAPE), (dict(tokens=1 << 24, x=P + 2), SHAPE)])   # more threads than a launch counts
 def test_rope_refuses(change, status):
     assert call("resq_rope_heads", ROPE, **change) == status
 
@@ -60,7 +61,8 @@ PAGE_FAULTS = [
 @pytest.mark.parametrize("change,status", PAGE_FAULTS + [
     (dict(tokens=-1), SHAPE), (dict(heads=0), SHAPE), (dict(ldk=-8), SHAPE), (dict(k=None), NULL), (dict(v=None), NULL), (dict(slots=None), NULL),
     (dict(k=P + 8), ALIGN), (dict(v=P + 2), ALIGN), (dict(ldk=1028), ALIGN), (dict(ldv=2048, ldvh=132), ALIGN), (dict(slots=P + 2), ALIGN),
-    (dict(tokens=0, k=None, slots=None), OK)])
+    (dict(tokens=0, k=None, slots=None), OK), (dict(tokens=1 << 28), SHAPE), (dict(tokens=1 << 25), SHAPE),
+    (dict(tokens=1 << 24, d=256, ldk=2048, ldkh=256, ldv=2048, ldvh=256, row_stride=256, head_stride=4096, page_stride=32768), SHAPE)])
 def test_append_and_gather_refuse(change, status):
     assert call("resq_append_kv_cache", APPEND, **change) == status
     order = ["k_pages", "v_pages", "num_pages", "page_size", "page_stride", "head_stride", "row_stride", "slots", "tokens", "heads", "d", "r",
@@ -87,7 +89,8 @@ ATTEND = dict(q=P, ldq=4096, ldqh=128, B=4, heads_q=32, heads_k=8, d=128, r=16, 
     (dict(scale=0.0), SHAPE), (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE),
     (dict(softcap=-1.0), SHAPE), (dict(softcap=float("nan")), SHAPE), (dict(window=-1), SHAPE), (dict(q=None), NULL), (dict(lens=None), NULL),
     (dict(table=None), NULL), (dict(out=None), NULL), (dict(workspace=None), NULL), (dict(q=P + 1), ALIGN), (dict(out=P + 1), ALIGN),
-    (dict(lens=P + 2), ALIGN), (dict(table=P + 2), ALIGN), (dict(lse=P + 2), ALIGN), (dict(workspace=P + 16), ALIGN), (dict(nbytes=64), BUFFER)])
+    (dict(lens=P + 2), ALIGN), (dict(table=P + 2), ALIGN), (dict(lse=P + 2), ALIGN), (dict(workspace=P + 16), ALIGN), (dict(nbytes=64), BUFFER),
+    (dict(B=65535, heads_q=512, heads_k=512, ldo=65536), SHAPE), (dict(softcap=1e-39), SHAPE)])
 def test_attend_refuses(change, status):
     assert call("resq_attend_kv_cache", ATTEND, **change) == status
 

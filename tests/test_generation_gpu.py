@@ -115,6 +115,20 @@ def test_plan_goes_on_from_its_own_state(rq):
         assert (p.positions.tolist(), p.slots.tolist(), t.tolist()) == (pos, slots, table)
 
 
+def test_plan_on_another_stream(rq):
+    # buffers that the call makes for itself are cleared before the plan is in them, whatever the current stream still does
+    side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device=DEV)
+    args = [ints([5, 0, 16]), ints([1, 3, 2]), ints([7, 4, 2, 9])]
+    table, taken = ints([[3, -1], [-1, -1], [1, -1]]), ints([0])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        busy = busy @ busy * 1e-2
+    p = rq.resq_kv_slots(*args, taken, table, 16, 10, max_tokens=8, stream=side)
+    torch.cuda.synchronize()
+    assert p.slots.tolist() == [3 * 16 + 5, 7 * 16, 7 * 16 + 1, 7 * 16 + 2, 4 * 16, 4 * 16 + 1, -1, -1]
+    assert p.positions.tolist() == [5, 0, 1, 2, 16, 17, 0, 0] and p.state.tolist() == [2, 0] and p.lens.tolist() == [6, 3, 18]
+
+
 def test_plan_leaves_out_pages_that_do_not_exist(rq):
     # a table entry and a free page outside [0, num_pages): their tokens get no slot
     table = [[99, -1, -1], [1, -1, -1]]
@@ -243,6 +257,17 @@ def test_append_and_gather_without_tokens_and_from_broadcast_heads(rq):
     v_pages = pages.clone()
     rq.resq_append_kv_cache(one.expand(-1, 3, -1), one.expand(-1, 3, -1), ints([0, 17, 5, 63, 9]), pages, v_pages, 8)
     assert torch.equal(pages[0, 0, 0], pages[0, 2, 0]) and torch.equal(pages, v_pages) and not torch.equal(pages, was)
+
+
+def test_gather_of_repeated_slots(rq):
+    pages = [plain.make_pages(gen(n), 4, 3, 16, 64, 8) for n in (3, 4)]
+    slots = ints([5, 5, 63, -1, 5, 0, 63])
+    every = rq.resq_gather_kv_cache(*pages, ints(list(range(64))), 8, d_head=64)
+    k = torch.empty(7, 3, 64, dtype=torch.bfloat16, device=DEV)
+    for got, of in zip(rq.resq_gather_kv_cache(*pages, slots, 8, k=k), every):
+        want = of[slots.clamp(min=0).long()]
+        want[3] = 0
+        assert torch.equal(got, want)
 
 
 def test_slots_beyond_2_gib(rq):
@@ -449,6 +474,26 @@ def test_attend_on_other_streams(rq):
         outs.append(rq.resq_attend_kv_cache(*case, 16))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+def test_attend_graphs_share_a_workspace(rq):
+    # two captured calls, one with rows of 16 KB in LDS per wavefront, replayed in turn with eager calls between them
+    cases = [(attend_case(41, [900, 0, 33], 4, 2, 256, 256, 16), 256), (attend_case(42, [5000, 77], 16, 2, 128, 16, 24, "token"), 16)]
+    work = max((rq.resq_attend_kv_cache_workspace(*case[0].shape[:2], case[1].shape[1], case[0].shape[2]) for case, _ in cases), key=len)
+    outs = [torch.empty_like(case[0]) for case, _ in cases]
+    graphs = []
+    for (case, r), out in zip(cases, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            rq.resq_attend_kv_cache(*case, r, out=out, workspace=work)
+    want = [check_attend(rq, *case, r)[0] for case, r in cases]
+    for _ in range(4):
+        for k in (0, 1, 1, 0):
+            outs[k].fill_(7)
+            graphs[k].replay()
+            rq.resq_attend_kv_cache(*cases[1 - k][0], cases[1 - k][1], workspace=work)
+            torch.cuda.synchronize()
+            assert torch.equal(outs[k], want[k])
 
 
 # ---- a step of generation ------------------------------------------------------------------------
