@@ -43,6 +43,8 @@ constexpr int kAttendUnit = kAttendTile * kAttendWaves;      // tokens of a unit
 constexpr int kAttendHeadCost = 3;
 constexpr int kAttendMaxGrid = 1024;
 constexpr int kAttendRows = 16;                              // queries of a workgroup at most
+constexpr int kAttendJoinFew = 8;                            // partial results that a thread reads at once
+constexpr int kAttendJoinSplit = 1024;                       // heads from which a workgroup joins all of a head's queries, see there
 constexpr int kAttendPRow = 80;                              // bytes of a row of weights in LDS: 32 in bf16, and what keeps rows on other banks
 constexpr float kAttendNone = -3.0e38f;                      // the maximum of no scores: finite, so that differences stay numbers
 constexpr float kAttendSlack = 8.0f;                         // of the running maximum, in powers of two
@@ -434,8 +436,10 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 
-            // ---- what the tile's work reads of LDS, asked for at once (values' codes only where they leave registers for it) ----
-            constexpr bool kEarly = HT <= 2 && NL <= 8;
+            // ---- what the tile's work reads of LDS, asked for at once; values' codes only where they leave registers for it (32 x
+            // 4096 tokens of 8 heads: 256 channels in 8 bits 128 us against 162, 32 of 256 78 against 84; where both groups are
+            // wide they do not fit: 64 of 256 323 against 112) and it changes something (64 of 128: 56.2 and 56.8) ----
+            constexpr bool kEarly = HT <= 2 || (NL == 0 && HT == 16);
             uint2 kh[2][HS];
             uint32_t kl[2][LS ? LS : 1];
             float4 kpar[NT], vpar[NT];
@@ -749,88 +753,131 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     }
 }
 
-// Joins the partial results of the heads that several workgroups had, one workgroup to a query; and writes the queries of
-// sequences without tokens.
+// Joins the partial results of the heads that several workgroups had, and writes the queries of sequences without tokens; a
+// workgroup to a head's queries, or to one of them (grid.y) where there are few.
+//   m = max m_i, f_i = 2^(m_i - m), out = sum f_i acc_i / sum f_i l_i, lse = m ln 2 + ln sum f_i l_i
+// Few partial results, the usual case: four channels of a query to a thread, all its reads at once.  More: all threads to one
+// query after the other, in three barriers each.
+// Bound by the launch and two dependent reads: 2.6 us for 8 heads of 4 queries in 7 parts, 5.4 in 64 parts.  A workgroup to every
+// query always: 256 sequences of 512 tokens 58.5 us with the main kernel instead of 56; to every head always: one of 8192 tokens
+// 20.4 instead of 14.2 (64 parts).  512 threads instead of 256: 63 us for those 256 sequences.
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a) {
     __shared__ float weight[kAttendMaxGrid], weight_sum[kAttendMaxGrid], part[2 * kAttendWaves];
     __shared__ float4 red[kAttendThreads];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int heads_q = a.heads_k * a.share;
-    const int b = blockIdx.x / heads_q, qhead = blockIdx.x - b * heads_q;
-    const int hk = qhead / a.share, qi = qhead - hk * a.share, qt = qi / kAttendRows, row = qi - qt * kAttendRows;
-    const int32_t* join = a.joins + ((int64_t)b * a.heads_k * a.qtiles + hk * a.qtiles + qt) * 2;
+    const int heads = a.heads_k * a.qtiles;
+    const int b = blockIdx.x / heads, head = blockIdx.x - b * heads;
+    const int hk = head / a.qtiles, qt = head - hk * a.qtiles;
+    const int32_t* join = a.joins + (int64_t)blockIdx.x * 2;
     const int slot0 = join[0], w_last = join[1];   // (nobody wrote them for a sequence without tokens)
-    uint16_t* dst = a.out + b * a.ldo + qhead * a.ldoh;
+    const int rows = min(a.share - qt * kAttendRows, kAttendRows);
+    const int row0 = gridDim.y > 1 ? blockIdx.y : 0, row1 = gridDim.y > 1 ? min(row0 + 1, rows) : rows;
+    const int q0 = hk * a.share + qt * kAttendRows;   // the query head of row 0
+    uint16_t* out = a.out + b * a.ldo + q0 * a.ldoh;
+    float* lse = a.lse ? a.lse + (int64_t)b * a.heads_k * a.share + q0 : nullptr;
     const float inf = __builtin_huge_valf();
-    if (attend_len(a, b) == 0) {
-        for (int c = t; c < a.d; c += kAttendThreads) dst[c] = 0;
-        if (t == 0 && a.lse) a.lse[blockIdx.x] = -inf;
+    const int fours = a.d >> 2;
+    auto write = [&](int row, int ch, const float4& o, float top, float sum) {
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<Piece8*>(out + row * a.ldoh + ch) = Piece8{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
+        if (ch == 0 && lse) lse[row] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
+    };
+    const bool empty = attend_len(a, b) == 0;
+    const int w_first = slot0 >> 1, count = w_last - w_first + 1;
+    if (!empty && count == 1) return;
+    auto slot = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (w_first + i)); };
+    if (empty || count <= kAttendJoinFew) {
+        for (int e = row0 * fours + t; e < row1 * fours; e += kAttendThreads) {
+            const int row = (int)((uint32_t)e * (uint32_t)a.fours_magic >> 16), ch = 4 * (e - row * fours);
+            float4 v[kAttendJoinFew], o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float2 ml[kAttendJoinFew];
+            float top = kAttendNone, sum = 0.0f;
+            if (!empty) {
+#pragma unroll
+                for (int i = 0; i < kAttendJoinFew; ++i)
+                    if (i < count) {
+                        ml[i] = *reinterpret_cast<const float2*>(a.part_ml + (slot(i) * kAttendRows + row) * 2);
+                        v[i] = *reinterpret_cast<const float4*>(a.part_acc + (slot(i) * a.rows + row) * a.d + ch);
+                    }
+#pragma unroll
+                for (int i = 0; i < kAttendJoinFew; ++i)
+                    if (i < count) top = fmaxf(top, ml[i].x);
+#pragma unroll
+                for (int i = 0; i < kAttendJoinFew; ++i)
+                    if (i < count) {
+                        const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+                        sum = fmaf(f, ml[i].y, sum);
+                        o.x = fmaf(f, v[i].x, o.x);
+                        o.y = fmaf(f, v[i].y, o.y);
+                        o.z = fmaf(f, v[i].z, o.z);
+                        o.w = fmaf(f, v[i].w, o.w);
+                    }
+            }
+            write(row, ch, o, top, sum);
+        }
         return;
     }
-    const int w_first = slot0 >> 1, count = w_last - w_first + 1;
-    if (count == 1) return;
-    auto slot = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (w_first + i)); };
     // four channels to a thread, what threads are left over the partial results, four of which are on their way at a time; the
     // first four are asked for before their weights are known
-    const int fours = a.d >> 2, groups = kAttendThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
-    float4 v[4];
-    auto load_four = [&](int i) {
+    const int groups = kAttendThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
+    for (int row = row0; row < row1; ++row) {
+        float4 v[4];
+        auto load_four = [&](int i) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = *reinterpret_cast<const float4*>(a.part_acc + (slot(min(i + k * groups, count - 1)) * a.rows + row) * a.d + ch);
-    };
-    if (group < groups) load_four(group);
-    float top = kAttendNone, sum = 0.0f;
-    for (int i = t; i < count; i += kAttendThreads) {
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (slot(i) * kAttendRows + row) * 2);
-        weight[i] = ml.x;
-        weight_sum[i] = ml.y;
-        top = fmaxf(top, ml.x);
-    }
-    top = halves_max(fmaxf(row_max16(top), lane_xor<16>(row_max16(top))));
-    if (lane == 0) part[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    for (int i = t; i < count; i += kAttendThreads) {
-        const float f = __builtin_amdgcn_exp2f(weight[i] - top);
-        weight[i] = f;
-        sum = fmaf(f, weight_sum[i], sum);
-    }
-    sum = row_sum16(sum);
-    sum = rows_sum(sum);
-    if (lane == 0) part[kAttendWaves + wave] = sum;
-    __syncthreads();
-    sum = (part[kAttendWaves] + part[kAttendWaves + 1]) + (part[kAttendWaves + 2] + part[kAttendWaves + 3]);
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (group < groups) {
-        for (int i = group; i < count; i += 4 * groups) {
-            if (i != group) load_four(i);
+            for (int k = 0; k < 4; ++k)
+                v[k] = *reinterpret_cast<const float4*>(a.part_acc + (slot(min(i + k * groups, count - 1)) * a.rows + row) * a.d + ch);
+        };
+        if (group < groups) load_four(group);
+        float top = kAttendNone, sum = 0.0f;
+        for (int i = t; i < count; i += kAttendThreads) {
+            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (slot(i) * kAttendRows + row) * 2);
+            weight[i] = ml.x;
+            weight_sum[i] = ml.y;
+            top = fmaxf(top, ml.x);
+        }
+        top = halves_max(fmaxf(row_max16(top), lane_xor<16>(row_max16(top))));
+        if (lane == 0) part[wave] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        for (int i = t; i < count; i += kAttendThreads) {
+            const float f = __builtin_amdgcn_exp2f(weight[i] - top);
+            weight[i] = f;
+            sum = fmaf(f, weight_sum[i], sum);
+        }
+        sum = row_sum16(sum);
+        sum = rows_sum(sum);
+        if (lane == 0) part[kAttendWaves + wave] = sum;
+        __syncthreads();
+        sum = (part[kAttendWaves] + part[kAttendWaves + 1]) + (part[kAttendWaves + 2] + part[kAttendWaves + 3]);
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (group < groups) {
+            for (int i = group; i < count; i += 4 * groups) {
+                if (i != group) load_four(i);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float f = i + k * groups < count ? weight[i + k * groups] : 0.0f;
-                if (f != 0.0f) {   // (a workgroup that saw nothing)
-                    o.x = fmaf(f, v[k].x, o.x);
-                    o.y = fmaf(f, v[k].y, o.y);
-                    o.z = fmaf(f, v[k].z, o.z);
-                    o.w = fmaf(f, v[k].w, o.w);
+                for (int k = 0; k < 4; ++k) {
+                    const float f = i + k * groups < count ? weight[i + k * groups] : 0.0f;
+                    if (f != 0.0f) {   // (a workgroup that saw nothing)
+                        o.x = fmaf(f, v[k].x, o.x);
+                        o.y = fmaf(f, v[k].y, o.y);
+                        o.z = fmaf(f, v[k].z, o.z);
+                        o.w = fmaf(f, v[k].w, o.w);
+                    }
                 }
             }
         }
-    }
-    red[t] = o;
-    __syncthreads();
-    if (t < fours) {
-        for (int k = 1; k < groups; ++k) {
-            const float4 v = red[k * fours + t];
-            o.x += v.x;
-            o.y += v.y;
-            o.z += v.z;
-            o.w += v.w;
+        red[t] = o;
+        __syncthreads();
+        if (t < fours) {
+            for (int k = 1; k < groups; ++k) {
+                const float4 v = red[k * fours + t];
+                o.x += v.x;
+                o.y += v.y;
+                o.z += v.z;
+                o.w += v.w;
+            }
+            write(row, 4 * t, o, top, sum);
         }
-        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-        Piece8 p{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
-        *reinterpret_cast<Piece8*>(dst + 4 * t) = p;
-        if (t == 0 && a.lse) a.lse[blockIdx.x] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
+        __syncthreads();   // before the next query's weights
     }
 }
 

@@ -119,7 +119,8 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
         return RESQ_ERR_HIP;
     const int64_t grid = units < 256 * OCC ? (units + 7) / 8 * 8 : 256 * OCC;   // a multiple of the dies
     launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
-    launch(attend_join_kernel, dim3((unsigned)(a.B * a.heads_k * a.share)), dim3(kAttendThreads), 0, st, args);
+    const int64_t heads = (int64_t)a.B * a.heads_k * a.qtiles;
+    launch(attend_join_kernel, dim3((unsigned)heads, heads < kAttendJoinSplit ? (unsigned)a.rows : 1), dim3(kAttendThreads), 0, st, args);
     return launch_status();
 }
 
