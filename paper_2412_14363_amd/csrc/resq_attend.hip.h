@@ -21,10 +21,14 @@
 // The maximum is looked at again only when a score is 2^8 times what it allows: sums of weights up to 2^8 lose nothing.
 //
 // The work is cut into units of 128 tokens of one head (four wavefronts, 32 tokens each); all units of the call in a row are
-// dealt to the workgroups in runs of equal length, whatever the sequences' lengths are (they are read on the GPU).  A head
-// that ends up with several workgroups is joined by a second kernel from their maxima, sums and partial outputs.
+// dealt to the workgroups in runs of equal cost, whatever the sequences' lengths are (they are read on the GPU).  A head
+// that ends up with several workgroups is joined by a second kernel from their maxima, sums and partial outputs.  (Joined by the
+// workgroup that is done last, a sequence of 131072 tokens took 68 us instead of 46: 64 parts read by one workgroup.)
 //
-// Bound: HBM, 2 row bytes per token and K/V head.
+// Bound: HBM, 2 row bytes per token and K/V head, where the runs are long: heads of 128 (r = 16), 8 for 32 queries, one sequence of
+// 131072 tokens 38.2 us, 4.8 TB/s, 48 ragged ones up to 8192 53 us, 5.0 TB/s (a plain read of 256 MiB reaches 5.4).  Short runs: the
+// way to the first tile (lengths, then pages, then rows, each a read of its own) and out again, about 5 us; one sequence of 777
+// tokens 7.8 us, 24 of 64-channel heads behind a window of 1500 18.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -40,8 +44,9 @@ constexpr int kAttendWaves = kAttendThreads / 64;
 constexpr int kAttendMaxHead = 256;
 constexpr int kAttendTile = 32;                              // tokens of a wavefront's step
 constexpr int kAttendUnit = kAttendTile * kAttendWaves;      // tokens of a unit
+// what it costs to begin and to end a head, in units: 48 ragged sequences 73.7 us at 0, 54.6 at 2, 52.6 at 3, 52.7 at 4
 constexpr int kAttendHeadCost = 3;
-constexpr int kAttendMaxGrid = 1024;
+constexpr int kAttendMaxGrid = 3 * 256;                      // workgroups: three to a compute unit at most
 constexpr int kAttendRows = 16;                              // queries of a workgroup at most
 constexpr int kAttendJoinFew = 8;                            // partial results that a thread reads at once
 constexpr int kAttendJoinSplit = 1024;                       // heads from which a workgroup joins all of a head's queries, see there
@@ -75,7 +80,7 @@ struct AttendArgs {
     float* part_ml;    // [2 grid][16][2]: maximum (times log2 e) and sum of a partial result's queries (workspace)
     float* part_acc;   // [2 grid][rows][d]: and its weighted sums (workspace)
     int rows;          // queries of a partial result
-    int blocks16;      // 16 rows of a page from a multiple of 16 on are contiguous and 16-byte aligned
+    int blocks16;      // page_size is a multiple of 16, and 16 rows' offsets fit 32 bits
     int fours_magic;   // e * fours_magic >> 16 is e / (d / 4) for e < 1024
     int lds_red;       // bytes in front of the maxima and sums in LDS
 };
@@ -89,7 +94,7 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int len) {
     const int from = attend_first(a, len) & ~(kAttendTile - 1);
     return (len - from + kAttendUnit - 1) / kAttendUnit;
 }
-// what a head of so many units costs, counted in units: to begin and to end one takes the time of a few
+// what a head of so many units costs, counted in units
 __device__ __forceinline__ int attend_cost(int units) { return units == 0 ? 0 : units + kAttendHeadCost; }
 
 __device__ __forceinline__ v4f_att attend_mfma(const v4u_att& x, const v4u_att& y, const v4f_att& c) {
@@ -126,7 +131,8 @@ __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
 // A row comes to LDS in pieces of 16 bytes: its codes (the last of their pieces may hold a part of what follows them, or be
 // there in vain: codes of some kind, which meet zeros or are not written out), and the 16 bytes of its scales and zero-points.
 // The pitch of rows in LDS is a constant, so that every address is a lane's base and a constant, with the constants last, and
-// 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks.
+// 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks (32 x 4096 tokens of 8 heads of 128: 53 us,
+// at a multiple of 32 68).
 __host__ __device__ constexpr int attend_pieces(int NL, int HT) { return HT * 16 + NL * 8 < 256 ? (HT * 16 + NL * 8) / 16 + 1 : 17; }
 __host__ __device__ constexpr int attend_pitch(int NL, int HT) { return (attend_pieces(NL, HT) | 1) * 16; }
 __host__ __device__ constexpr int attend_tiles_bytes(int NL, int HT) {
@@ -174,7 +180,8 @@ __device__ __forceinline__ float halves_max(float x) {
 }
 // NL: 4-bit channels of a lane in the second product (16 NL channels in all), HT: 16-channel tiles of the 8-bit group,
 // Q: queries that fit, 8 or 16, BLOCKS: pages of a multiple of 16 rows, so that 16 tokens in a row from a multiple of 16 on are one
-// page's
+// page's and two scalar offsets serve a tile instead of one per row (32 x 4096 tokens of 8 heads of 128 without an 8-bit group 42.9
+// us against 45.4, 256 in 8 bits 161 against 171, 256 x 512 tokens 57.8 against 60.7), OCC: workgroups to a compute unit
 template <int NL, int HT, int Q, bool BLOCKS, int OCC>
 __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(const AttendArgs a) {
     constexpr int LS = NL / 2, HS = (HT + 1) / 2;   // steps of 32 channels of the first product
@@ -208,7 +215,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     }
     total = __builtin_amdgcn_readfirstlane(total);
     // Workgroups go to the eight dies in turn; runs that follow one another, whose heads lie side by side in token-major pages (and
-    // whose queries share a K/V head's rows where they are more than 16), stay on one die and meet in its L2.
+    // whose queries share a K/V head's rows where they are more than 16), stay on one die and meet in its L2 (32 x 4096 tokens of
+    // token-major pages 54 us, dealt in turn 72).
     const int W = min(total, (int)gridDim.x), per_die = (W + 7) >> 3;
     const int w0 = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per_die || w0 >= W) return;

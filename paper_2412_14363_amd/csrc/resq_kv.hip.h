@@ -19,9 +19,10 @@ constexpr int kKvThreads = 256;
 // news[b] more: its tokens' places in the batch are a prefix sum, the pages it lacks another one, taken off the front of the
 // free list.  Sums first, and checks (nothing changes unless everything fits); then every token finds its request by bisection
 // of the first sum, and the token that opens a page writes the page's entry.
-// Latency: 8 bytes in and 16 out per request, 8 out per token.  Up to kPlanRequests requests take one launch: every workgroup
-// makes the sums for itself, in LDS, and serves some of the tokens; outputs that lie on inputs allow one workgroup only, which
-// reads them all before it writes.  Else the sums go through memory to a second kernel.
+// Latency: 8 bytes in and 16 out per request, 8 out per token.  Up to kPlanRequests requests (whose sums fit LDS) take one launch:
+// every workgroup makes the sums for itself and serves some of the tokens; outputs that lie on inputs allow one workgroup only,
+// which reads them all before it writes.  Else the sums go through memory to a second kernel.  3.3 us for 32 requests of a token or
+// 4096 tokens, 5.9 for 1024 requests, 19 for 4096 (16 to a thread).
 // ---------------------------------------------------------------------------
 constexpr int kPlanRequests = 4096;
 constexpr int kPlanThreads = 256;
@@ -223,9 +224,10 @@ __global__ __launch_bounds__(256) void kv_plan_tokens_kernel(const KvPlanArgs p)
 
 // ---------------------------------------------------------------------------
 // The writer, G lanes to a row of keys or values (blockIdx.y), and the reader, G lanes to both of a token and head (so that twice
-// the bytes are on their way; the writer has the quantizer's arithmetic, and takes longer so: 8.8 instead of 7.9 us for 2911
-// tokens of 8 heads).
-// Bound by HBM at prefill sizes (2 d_head bytes of bf16 and a row of codes per row), by the launch at a step's.
+// the bytes are on their way: 21.5 instead of 25.3 us for 16384 tokens of 8 heads of 128; the writer has the quantizer's arithmetic,
+// and takes longer so: 8.8 instead of 7.9 for 2911 tokens).
+// The reader is bound by HBM (16384 tokens: 20.5 us, 4.4 TB/s read and written), the writer by the quantizer's instructions, some 270
+// per wavefront of four rows (16384 tokens: 27.4 us, 3.3 TB/s), both by the launch at a step's sizes (16 tokens: 2.8 and 2.5 us).
 // ---------------------------------------------------------------------------
 struct KvPagesArgs {
     const uint16_t* x[2];       // bf16 [tokens, heads, d], keys and values

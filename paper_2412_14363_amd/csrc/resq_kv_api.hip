@@ -117,6 +117,8 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
+    // as many workgroups as run at once, one run each: no head begins more often than that asks for (four times as many at OCC = 2: 47
+    // instead of 37 us for one sequence of 131072 tokens)
     const int64_t grid = units < 256 * OCC ? (units + 7) / 8 * 8 : 256 * OCC;   // a multiple of the dies
     launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
     const int64_t heads = (int64_t)a.B * a.heads_k * a.qtiles;
@@ -146,7 +148,9 @@ int resq_kv_slots(const int32_t* lens, const int32_t* new_tokens, int64_t B, int
     const KvPlanArgs p{lens, new_tokens, (int)B, FastDiv((uint32_t)page_size), (int)num_pages, free_pages, n_free, taken, block_table, ld_table,
                        (int)width, (int)max_tokens, lens_out, cu_tokens, cu_pages, positions, slots, state};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    // one launch where it can be, see resq_kv.hip.h
+    // One launch where it can be, see resq_kv.hip.h: 3.3 us for 32 requests of a token, two take 4.4; 32 and 1024 tokens in place 4.0 and
+    // 5.0.  In place one workgroup has to serve all tokens: 16384 of them 8.2 us, two launches 5.2, from 1024 or so on they are even.  1024
+    // tokens to a workgroup where there can be several, instead of 256: 5.4 for 3.5 (1024 tokens).
     const bool in_place = lens == lens_out || taken == state;
     if (B <= kPlanRequests && (!in_place || max_tokens <= kPlanTokensInPlace)) {
         const int per_block = in_place ? kPlanTokensInPlace : kPlanTokens;
@@ -209,8 +213,10 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (aligned(x, 16) && aligned(y, 16) && ldx % 8 == 0 && ldxh % 8 == 0 && ldy % 8 == 0 && ldyh % 8 == 0 && d_head % 8 == 0 &&
         rot % (interleaved ? 8 : 16) == 0) {
-        // lanes to a head, and tokens to a workgroup: as many as give 256 threads an angle each, while 512 workgroups remain;
-        // with fewer tokens than that a workgroup takes one round of heads
+        // Lanes to a head, and tokens to a workgroup: as many as give 256 threads an angle each, while 512 workgroups remain; with fewer
+        // tokens than that a workgroup takes one round of heads.  Us at heads of 64, 24 of them, 8192 tokens: 9.0, one token to a
+        // workgroup 16.1; 2048 tokens of 40 heads of 128 8.0 and 8.7; 1024 with 512 / 128 workgroups as the least 5.3 / 5.9.  All heads of
+        // one token in one workgroup 3.0, in rounds of 32 2.7; 2048 tokens in such rounds 8.9, whole 8.0.
         const int lg = d_head <= 64 ? 4 : d_head <= 128 ? 8 : d_head <= 256 ? 16 : 32, groups = 256 / lg;
         int tb_log2 = 0;
         while ((2 << tb_log2) <= groups && (rot >> 1) * (2 << tb_log2) <= 256 && tokens >= ((int64_t)512 << (tb_log2 + 1))) ++tb_log2;
@@ -340,7 +346,10 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.lse = lse;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t low = d_head - r;
-    // the smallest kernel that holds the head's two groups of channels
+    // The smallest kernel that holds the head's two groups of channels, in as many workgroups to a compute unit as its registers allow
+    // without spilling in the loop.  32 x 4096 tokens of 8 heads, in us: the next larger kernel for 128 (r = 16) 56.3 instead of 53.2, 64 (8)
+    // 39.8 instead of 31.6, 256 (32) 99.7 instead of 83; a workgroup less 58.7 for 53.2, 34 for 31.6 (128, r = 32: 58 for 49); one more, with
+    // spills, 183 for 83 (256, r = 32), 330 for 161 (r = 256), 103 for 55 (128, r = 64).
     if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
                                                                                    : launch_attend<0, 16, 1>(a, units, st);
     if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)

@@ -40,7 +40,8 @@ __device__ __forceinline__ void rope_angle(int position, double freq, float& c, 
 // Rows of whole 16-byte pieces, two of them to a lane, LG lanes to a head: the two pieces that a pair's halves are in, or two in
 // a row.  The lanes of a workgroup are dealt to TB tokens (a power of two), each head group of which takes every so many heads
 // of its token; the tokens' cosines and sines are taken once per workgroup, into LDS and from there into registers.
-// Bound by HBM from a few thousand rows on (4 bytes per channel), by the launch at a step's sizes.
+// Bound by HBM from a few thousand rows on (4 bytes per channel: 8192 tokens of 40 heads of 128 26.7 us, 6.3 TB/s, part of it from
+// the caches), by the launch at a step's sizes (one token 2.7 us).
 template <int LG>
 __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int tb_log2, int heads_per_block) {
     constexpr int kGroups = 256 / LG;
