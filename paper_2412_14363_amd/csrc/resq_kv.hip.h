@@ -226,14 +226,16 @@ __global__ __launch_bounds__(256) void kv_plan_tokens_kernel(const KvPlanArgs p)
 // The writer, G lanes to a row of keys or values (blockIdx.y), and the reader, G lanes to both of a token and head (so that twice
 // the bytes are on their way: 21.5 instead of 25.3 us for 16384 tokens of 8 heads of 128; the writer has the quantizer's arithmetic,
 // and takes longer so: 8.8 instead of 7.9 for 2911 tokens).
-// The reader is bound by HBM (16384 tokens: 20.5 us, 4.4 TB/s read and written), the writer by the quantizer's instructions, some 270
-// per wavefront of four rows (16384 tokens: 27.4 us, 3.3 TB/s), both by the launch at a step's sizes (16 tokens: 2.8 and 2.5 us).
+// The reader is bound by HBM (16384 tokens: 17.7 us, 5.1 TB/s read and written; 20.5 where slots are in no order, of whose 88-byte
+// rows it fetches whole lines, 53 MB for 23), the writer by the quantizer's instructions, some 270 per wavefront of four rows (27.4
+// us, 3.3 TB/s), both by the launch at a step's sizes (16 tokens: 2.8 and 3.0 us).
 // ---------------------------------------------------------------------------
 struct KvPagesArgs {
     const uint16_t* x[2];       // bf16 [tokens, heads, d], keys and values
     int64_t ld[2], ldh[2];      // elements from token to token and from head to head
     uint32_t rows;              // tokens * heads
-    FastDiv heads;
+    FastDiv inner;              // tokens where they follow one another in `rows`, heads where those do
+    bool tokens_inner;
     int d, r;
     const int32_t* slots;
     uint8_t* pages[2];
@@ -247,12 +249,22 @@ __device__ __forceinline__ int64_t kv_row_offset(const KvPagesArgs& a, uint32_t 
     return page * a.page_stride + head * a.head_stride + row * a.row_stride;
 }
 
+// Rows that lie side by side in a page, a head's tokens or a token's heads, follow one another, so that a workgroup has their lines
+// whole and no two dies fetch the same one (the reader on 16384 tokens in runs of 16, 8 heads of 128, head by head in the pages: 17.7
+// us, with a token's heads in a row 19.4; 256 channels 29.5 and 31.9).
+__device__ __forceinline__ void kv_row_of(const KvPagesArgs& a, uint32_t m, uint32_t& token, uint32_t& head) {
+    const uint32_t outer = a.inner(m), inner = m - outer * a.inner.d;
+    token = a.tokens_inner ? inner : outer;
+    head = a.tokens_inner ? outer : inner;
+}
+
 template <int G>
 __global__ __launch_bounds__(kKvThreads) void append_kv_cache_kernel(const KvPagesArgs a) {
     const int gl = threadIdx.x & (G - 1), kind = blockIdx.y;
     const uint32_t m_raw = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
     const uint32_t m = min(m_raw, a.rows - 1);   // groups past the last row quantize it and store nothing
-    const uint32_t token = a.heads(m), head = m - token * a.heads.d;
+    uint32_t token, head;
+    kv_row_of(a, m, token, head);
     const uint32_t slot = (uint32_t)a.slots[token];
     const uint16_t* x = a.x[kind] + token * a.ld[kind] + head * a.ldh[kind];
     const uint4 v = gl < (a.d >> 3) ? reinterpret_cast<const uint4*>(x)[gl] : make_uint4(0u, 0u, 0u, 0u);
@@ -265,7 +277,8 @@ __global__ __launch_bounds__(kKvThreads) void gather_kv_cache_kernel(const KvPag
     const int gl = threadIdx.x & (G - 1);
     const uint32_t m = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
     if (m >= a.rows || gl >= (a.d >> 3)) return;
-    const uint32_t token = a.heads(m), head = m - token * a.heads.d;
+    uint32_t token, head;
+    kv_row_of(a, m, token, head);
     const uint32_t slot = (uint32_t)a.slots[token];
     uint4 o[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
     if (slot < a.num_slots) {
