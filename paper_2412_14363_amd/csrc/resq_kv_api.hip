@@ -233,9 +233,9 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
         }
         return launch_status();
     }
-    const int64_t blocks = (tokens * heads + 3) / 4;
-    if (!launch_fits(blocks, 256)) return RESQ_ERR_SHAPE;
-    launch(rope_heads_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    if (!launch_fits(tokens, 256)) return RESQ_ERR_SHAPE;
+    const int per_block = tokens < 512 ? 4 : (int)heads;   // as above
+    launch(rope_heads_kernel, dim3((unsigned)tokens, (unsigned)((heads + per_block - 1) / per_block)), dim3(256), 0, st, a, per_block);
     return launch_status();
 }
 

@@ -173,44 +173,68 @@ __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int 
     }
 }
 
-// Any other rows: one wavefront to a head of a token, element by element.
-__global__ __launch_bounds__(256) void rope_heads_kernel(const RopeArgs a) {
+// Any other rows, element by element: a workgroup to a token, whose cosines and sines it takes once, a wavefront to every fourth
+// head; the next head's elements are asked for before this one's are turned.
+__global__ __launch_bounds__(256) void rope_heads_kernel(const RopeArgs a, int heads_per_block) {
+    constexpr int kEach = kRopeMaxHead / 64;   // elements of a lane at most
     __shared__ float rows[4][kRopeMaxHead];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t m = (int64_t)blockIdx.x * 4 + wave;
-    const bool live = m < a.tokens * a.heads;
-    const int64_t token = live ? m / a.heads : 0;
-    const int head = live ? (int)(m - token * a.heads) : 0;
-    const uint16_t* x = a.x + token * a.ldx + head * a.ldxh;
-    const uint16_t* w = head < a.heads_q ? a.w_q : a.w_k;
-    float* row = rows[wave];
-    float sum = 0.0f;
-    for (int c = lane; c < a.d; c += 64) {
-        const float v = bf16_bits_to_f32(x[c]);
-        row[c] = v;
-        sum += v * v;
-    }
-    if (w) {
-        for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
-        const float inv = 1.0f / sqrtf(sum / (float)a.d + a.eps);
-        for (int c = lane; c < a.d; c += 64) row[c] = row[c] * inv * bf16_bits_to_f32(w[c]);
-    }
-    __syncthreads();
-    if (!live) return;
-    uint16_t* y = a.y + token * a.ldy + head * a.ldyh;
-    const int half = a.rot >> 1;
-    for (int i = lane; i < half; i += 64) {
-        const int ca = a.interleaved ? 2 * i : i, cb = a.interleaved ? 2 * i + 1 : i + half;
+    __shared__ float2 turns[kRopeMaxHead / 2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = a.rot >> 1;
+    const int64_t token = blockIdx.x;
+    const int h_begin = blockIdx.y * heads_per_block, h_end = min(a.heads, h_begin + heads_per_block);
+    const uint16_t* x = a.x + token * a.ldx;
+    uint32_t v[kEach] = {};
+    auto load = [&](int head) {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (64 * k < a.d && 64 * k + lane < a.d) v[k] = x[head * a.ldxh + 64 * k + lane];
+    };
+    int head = h_begin + wave;
+    if (head < h_end) load(head);
+    for (int i = threadIdx.x; i < half; i += 256) {
         float c, s;
         rope_angle(a.positions[token], a.freq[i], c, s);
-        c *= a.mscale;
-        s *= a.mscale;
-        const float va = row[ca], vb = row[cb];
-        const uint32_t o = pack_bf16_pair(va * c - vb * s, vb * c + va * s);
-        y[ca] = (uint16_t)o;
-        y[cb] = (uint16_t)(o >> 16);
+        turns[i] = make_float2(c * a.mscale, s * a.mscale);
     }
-    for (int c = a.rot + lane; c < a.d; c += 64) y[c] = (uint16_t)pack_bf16_pair(row[c], 0.0f);
+    __syncthreads();
+    float* row = rows[wave];
+    for (; head < h_end; head += 4) {
+        float f[kEach], sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            f[k] = 64 * k + lane < a.d ? bf16_bits_to_f32(v[k]) : 0.0f;
+            sum = fmaf(f[k], f[k], sum);
+        }
+        if (head + 4 < h_end) load(head + 4);
+        const uint16_t* w = head < a.heads_q ? a.w_q : a.w_k;
+        float inv = 1.0f;
+        if (w) {
+            for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
+            inv = 1.0f / sqrtf(sum / (float)a.d + a.eps);
+        }
+        uint16_t* y = a.y + token * a.ldy + head * a.ldyh;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int c = 64 * k + lane;
+            if (64 * k < a.d && c < a.d) {
+                const float g = w ? f[k] * inv * bf16_bits_to_f32(w[c]) : f[k];
+                if (c < a.rot) row[c] = g;
+                else y[c] = (uint16_t)pack_bf16_pair(g, 0.0f);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        for (int i = lane; i < half; i += 64) {
+            const int ca = a.interleaved ? 2 * i : i, cb = a.interleaved ? 2 * i + 1 : i + half;
+            const float2 cs = turns[i];
+            const float va = row[ca], vb = row[cb];
+            const uint32_t o = pack_bf16_pair(va * cs.x - vb * cs.y, vb * cs.x + va * cs.y);
+            y[ca] = (uint16_t)o;
+            y[cb] = (uint16_t)(o >> 16);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 }  // namespace resq
