@@ -522,7 +522,7 @@ int resq_rope_frequencies(int64_t rot, double base, int scaling, double factor, 
  *   w_q, w_k bf16 [d_head] or both null; eps >= 0                                        (read)
  *   positions int32 [tokens]; freq fp64 [rot / 2], 8-byte aligned, in DEVICE memory      (read)
  * Alignment: 2 bytes; rows of whole 16-byte pieces (x, y 16-byte aligned, strides and d_head multiples of 8, rot a multiple of
- * 16, or of 8 where interleaved) are moved in such pieces.
+ * 16 unless interleaved) are the fastest.
  */
 int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t d_head,
                     const void* w_q, const void* w_k, float eps, const int32_t* positions, const double* freq, int64_t rot,

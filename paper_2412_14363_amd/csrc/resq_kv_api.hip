@@ -212,30 +212,30 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
                      static_cast<const uint16_t*>(w_q), static_cast<const uint16_t*>(w_k), eps, positions, freq, (int)rot,
                      interleaved != 0, mscale, static_cast<uint16_t*>(y), ldy, ldyh};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (aligned(x, 16) && aligned(y, 16) && ldx % 8 == 0 && ldxh % 8 == 0 && ldy % 8 == 0 && ldyh % 8 == 0 && d_head % 8 == 0 &&
-        rot % (interleaved ? 8 : 16) == 0) {
-        // Lanes to a head, and tokens to a workgroup: as many as give 256 threads an angle each, while 512 workgroups remain; with fewer
-        // tokens than that a workgroup takes one round of heads.  Us at heads of 64, 24 of them, 8192 tokens: 9.0, one token to a
-        // workgroup 16.1; 2048 tokens of 40 heads of 128 8.0 and 8.7; 1024 with 512 / 128 workgroups as the least 5.3 / 5.9.  All heads of
-        // one token in one workgroup 3.0, in rounds of 32 2.7; 2048 tokens in such rounds 8.9, whole 8.0.
-        const int lg = d_head <= 64 ? 4 : d_head <= 128 ? 8 : d_head <= 256 ? 16 : 32, groups = 256 / lg;
-        int tb_log2 = 0;
-        while ((2 << tb_log2) <= groups && (rot >> 1) * (2 << tb_log2) <= 256 && tokens >= ((int64_t)512 << (tb_log2 + 1))) ++tb_log2;
-        const int per_block = tokens < 512 ? groups >> tb_log2 : (int)heads;
-        const dim3 grid((unsigned)((tokens + (1 << tb_log2) - 1) >> tb_log2), (unsigned)((heads + per_block - 1) / per_block));
-        const size_t lds = (size_t)(rot >> 1) * sizeof(float2) << tb_log2;
-        if (!launch_fits(grid.x, 256)) return RESQ_ERR_SHAPE;
-        switch (lg) {
-            case 4: launch(rope_pieces_kernel<4>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
-            case 8: launch(rope_pieces_kernel<8>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
-            case 16: launch(rope_pieces_kernel<16>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
-            default: launch(rope_pieces_kernel<32>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
-        }
-        return launch_status();
+    const bool any = !(aligned(x, 16) && aligned(y, 16) && ldx % 8 == 0 && ldxh % 8 == 0 && ldy % 8 == 0 && ldyh % 8 == 0 && d_head % 8 == 0 &&
+                       rot % (interleaved ? 2 : 16) == 0);
+    // Lanes to a head, and tokens to a workgroup: as many as give 256 threads an angle each, while 512 workgroups remain; with fewer
+    // tokens than that a workgroup takes one round of heads.  Us at heads of 64, 24 of them, 8192 tokens: 9.0, one token to a
+    // workgroup 16.1; 2048 tokens of 40 heads of 128 8.0 and 8.7; 1024 with 512 / 128 workgroups as the least 5.3 / 5.9.  All heads of
+    // one token in one workgroup 3.0, in rounds of 32 2.7; 2048 tokens in such rounds 8.9, whole 8.0.
+    const int64_t lanes = interleaved ? (d_head + 15) / 16 : (rot / 2 + 7) / 8 + (d_head - rot + 15) / 16;
+    const int lg = lanes <= 4 ? 4 : lanes <= 8 ? 8 : lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64, groups = 256 / lg;
+    int tb_log2 = 0;
+    while ((2 << tb_log2) <= groups && (rot >> 1) * (2 << tb_log2) <= 256 && tokens >= ((int64_t)512 << (tb_log2 + 1))) ++tb_log2;
+    const int per_block = tokens < 512 ? groups >> tb_log2 : (int)heads;
+    const dim3 grid((unsigned)((tokens + (1 << tb_log2) - 1) >> tb_log2), (unsigned)((heads + per_block - 1) / per_block));
+    const size_t lds = (size_t)(rot ? rot >> 1 : 1) * sizeof(float2) << tb_log2;
+    if (!launch_fits(grid.x, 256)) return RESQ_ERR_SHAPE;
+#define RESQ_LAUNCH_ROPE(LG)                                                                                                \
+    launch(any ? rope_pieces_kernel<LG, true> : rope_pieces_kernel<LG, false>, grid, dim3(256), lds, st, a, tb_log2, per_block)
+    switch (lg) {
+        case 4: RESQ_LAUNCH_ROPE(4); break;
+        case 8: RESQ_LAUNCH_ROPE(8); break;
+        case 16: RESQ_LAUNCH_ROPE(16); break;
+        case 32: RESQ_LAUNCH_ROPE(32); break;
+        default: launch(rope_pieces_kernel<64, true>, grid, dim3(256), lds, st, a, tb_log2, per_block); break;
     }
-    if (!launch_fits(tokens, 256)) return RESQ_ERR_SHAPE;
-    const int per_block = tokens < 512 ? 4 : (int)heads;   // as above
-    launch(rope_heads_kernel, dim3((unsigned)tokens, (unsigned)((heads + per_block - 1) / per_block)), dim3(256), 0, st, a, per_block);
+#undef RESQ_LAUNCH_ROPE
     return launch_status();
 }
 

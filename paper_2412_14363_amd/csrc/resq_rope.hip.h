@@ -37,15 +37,51 @@ __device__ __forceinline__ void rope_angle(int position, double freq, float& c, 
     sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
 }
 
-// Rows of whole 16-byte pieces, two of them to a lane, LG lanes to a head: the two pieces that a pair's halves are in, or two in
-// a row.  The lanes of a workgroup are dealt to TB tokens (a power of two), each head group of which takes every so many heads
-// of its token; the tokens' cosines and sines are taken once per workgroup, into LDS and from there into registers.
-// Bound by HBM from a few thousand rows on (4 bytes per channel: 8192 tokens of 40 heads of 128 26.7 us, 6.3 TB/s, part of it from
-// the caches), by the launch at a step's sizes (one token 2.7 us).
-template <int LG>
+// n of a row's elements in a piece of eight, from any address on (ANY), or eight or none at a multiple of 16 bytes
+template <bool ANY>
+__device__ __forceinline__ void load_piece(const uint16_t* p, int n, uint4& v) {
+    if constexpr (ANY) {
+        if (n >= 8) {
+            const Piece16 o = *reinterpret_cast<const Piece16*>(p);
+            v = make_uint4(o.x, o.y, o.z, o.w);
+        } else if (n > 0) {
+            uint32_t w[8] = {};
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < n) w[j] = p[j];
+            v = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6]);
+        }
+    } else if (n > 0) {
+        v = *reinterpret_cast<const uint4*>(p);
+    }
+}
+template <bool ANY>
+__device__ __forceinline__ void store_piece(uint16_t* p, int n, const uint4& v) {
+    if constexpr (ANY) {
+        if (n >= 8) {
+            *reinterpret_cast<Piece16*>(p) = Piece16{v.x, v.y, v.z, v.w};
+        } else if (n > 0) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < n) p[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+    } else if (n > 0) {
+        *reinterpret_cast<uint4*>(p) = v;
+    }
+}
+
+// Two 16-byte pieces to a lane, LG lanes to a head: the two pieces that a pair's halves are in, or two in a row.  The lanes of a
+// workgroup are dealt to TB tokens (a power of two), each head group of which takes every so many heads of its token; the tokens'
+// cosines and sines are taken once per workgroup, into LDS and from there into registers.
+// ANY: rows whose pieces begin anywhere.  2048 tokens of 40 heads of 128, 54 channels turned, 14.0 us (a wavefront to a head, element by
+// element, 24.7), with all turned, the norm, and rows 130 apart 12.5 (32); whole pieces of the same size 8.0.
+// Bound by HBM from a few thousand rows on (4 bytes per channel: 8192 tokens of 40 heads of 128 26.5 us, 6.3 TB/s, part of it from
+// the caches), by the launch at a step's sizes (one token 2.6 us).
+template <int LG, bool ANY>
 __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int tb_log2, int heads_per_block) {
     constexpr int kGroups = 256 / LG;
-    extern __shared__ float2 turns[];   // [TB][rot / 2]
+    extern __shared__ float2 turns[];   // [TB][rot / 2], one at least
     const int gl = threadIdx.x & (LG - 1), group = threadIdx.x / LG;
     const int gt = kGroups >> tb_log2;   // groups of a token
     const int64_t token0 = (int64_t)blockIdx.x << tb_log2;
@@ -54,25 +90,36 @@ __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int 
     const int h_end = min(a.heads, (int)(blockIdx.y + 1) * heads_per_block);
     int head = blockIdx.y * heads_per_block + (group - mine * gt);
     const bool live = token < a.tokens;
-    const int half = a.rot >> 1, pieces = a.d >> 3;
+    const int half = a.rot >> 1;
 
-    // the lane's pieces: halves of eight pairs, or neighbours
-    int pa, pb;
-    if (!a.interleaved && gl < a.rot >> 4) {
-        pa = gl;
-        pb = gl + (a.rot >> 4);
-    } else {
-        pa = 2 * gl;   // (half layout: in front of them rot / 16 lanes with two pieces each)
-        pb = pa + 1;
+    // the lane's pieces, first channels and widths: halves of eight pairs, or neighbours.  The last piece of a stretch of channels is
+    // its last eight, what it has in common with the one before done twice (and counted once).
+    int ca, cb, na, nb, skip_a = 0, skip_b = 0;
+    const int pair_lanes = a.interleaved ? 0 : ANY ? (half + 7) >> 3 : a.rot >> 4;   // half layout: in front of the others
+    const bool pair_halves = gl < pair_lanes;
+    const int begin = pair_halves ? 0 : a.interleaved ? 0 : a.rot, end = pair_halves ? half : a.d;
+    ca = begin + (pair_halves ? 8 : 16) * (gl - (pair_halves ? 0 : pair_lanes));
+    cb = pair_halves ? ca : ca + 8;
+    na = min(8, end - ca);
+    nb = min(8, end - cb);
+    if (ANY && end - begin >= 8) {
+        if (na > 0 && na < 8) {
+            skip_a = 8 - na;
+            ca = end - (na = 8);
+        }
+        if (nb > 0 && nb < 8) {
+            skip_b = 8 - nb;
+            cb = end - (nb = 8);
+        }
     }
-    const bool has_a = pa < pieces, has_b = pb < pieces;
+    if (pair_halves) cb += half;
     const uint16_t* xrow = a.x + (live ? token : 0) * a.ldx;
     auto load = [&](int h, uint4 (&v)[2]) {
         v[0] = v[1] = make_uint4(0u, 0u, 0u, 0u);
         if (live && h < h_end) {
-            const uint4* p = reinterpret_cast<const uint4*>(xrow + h * a.ldxh);
-            if (has_a) v[0] = p[pa];
-            if (has_b) v[1] = p[pb];
+            const uint16_t* p = xrow + h * a.ldxh;
+            load_piece<ANY>(p + ca, na, v[0]);
+            load_piece<ANY>(p + cb, nb, v[1]);
         }
     };
     uint4 v[2], next[2];
@@ -94,27 +141,21 @@ __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int 
             const uint16_t* wp = k ? a.w_k : a.w_q;
             w[k][0] = w[k][1] = make_uint4(0u, 0u, 0u, 0u);
             if (!wp) continue;
-            if (has_a) {
-                const Piece16 p = reinterpret_cast<const Piece16*>(wp)[pa];
-                w[k][0] = make_uint4(p.x, p.y, p.z, p.w);
-            }
-            if (has_b) {
-                const Piece16 p = reinterpret_cast<const Piece16*>(wp)[pb];
-                w[k][1] = make_uint4(p.x, p.y, p.z, p.w);
-            }
+            load_piece<true>(wp + ca, na, w[k][0]);
+            load_piece<true>(wp + cb, nb, w[k][1]);
         }
     }
     __syncthreads();
-    // pair j of the lane: half layout, channels j of both pieces; interleaved, four pairs of each piece
+    // pair j of the lane: half layout, channels j of both pieces; interleaved, four pairs of each piece; those there are to turn
     float2 cs[8];
-    const bool turn_a = 8 * pa < a.rot, turn_b = 8 * pb < a.rot;
+    uint32_t turn = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int i = a.interleaved ? 4 * (j < 4 ? pa : pb) + (j & 3) : 8 * pa + j;
-        const bool turn = a.interleaved && j >= 4 ? turn_b : turn_a;
-        cs[j] = turn ? turns[mine * half + i] : make_float2(1.0f, 0.0f);
+        const int i = a.interleaved ? ((j < 4 ? ca : cb) >> 1) + (j & 3) : ca + j;
+        const bool there = (a.interleaved || pair_halves) && i < half;
+        cs[j] = turns[mine * half + (there ? i : 0)];
+        turn |= (uint32_t)there << j;
     }
-    const bool pair_halves = !a.interleaved && turn_a;
     uint16_t* yrow = a.y + (live ? token : 0) * a.ldy;
 
     while (head - (group - mine * gt) < h_end) {   // (all lanes together: the norm's exchanges)
@@ -125,12 +166,16 @@ __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int 
         if (a.w_q || a.w_k) {
             float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(f[0][j], f[0][j], fmaf(f[1][j], f[1][j], sum));
+            for (int j = 0; j < 8; ++j) {
+                const float p = !ANY || j >= skip_a ? f[0][j] : 0.0f, q = !ANY || j >= skip_b ? f[1][j] : 0.0f;
+                sum = fmaf(p, p, fmaf(q, q, sum));
+            }
             if constexpr (LG > 1) sum += lane_xor<1>(sum);
             if constexpr (LG > 2) sum += lane_xor<2>(sum);
             if constexpr (LG > 4) sum += lane_xor<4>(sum);
             if constexpr (LG > 8) sum += lane_xor<8>(sum);
             if constexpr (LG > 16) sum += lane_xor<16>(sum);
+            if constexpr (LG > 32) sum += lane_xor<32>(sum);
             const float inv = 1.0f / sqrtf(sum / (float)a.d + a.eps);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -155,85 +200,22 @@ __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int 
                     for (int j = 0; j < 4; ++j) {
                         const float p = f[k][2 * j], q = f[k][2 * j + 1];
                         const float2 t = cs[4 * k + j];
-                        f[k][2 * j] = p * t.x - q * t.y;
-                        f[k][2 * j + 1] = q * t.x + p * t.y;
+                        const bool turned = turn >> (4 * k + j) & 1;   // (not by a factor of 0: the other may be infinite)
+                        f[k][2 * j] = turned ? p * t.x - q * t.y : p;
+                        f[k][2 * j + 1] = turned ? q * t.x + p * t.y : q;
                     }
             }
-            uint4* dst = reinterpret_cast<uint4*>(yrow + head * a.ldyh);
+            uint16_t* dst = yrow + head * a.ldyh;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint4 o = make_uint4(pack_bf16_pair(f[k][0], f[k][1]), pack_bf16_pair(f[k][2], f[k][3]),
                                            pack_bf16_pair(f[k][4], f[k][5]), pack_bf16_pair(f[k][6], f[k][7]));
-                if (k == 0 ? has_a : has_b) dst[k == 0 ? pa : pb] = o;
+                store_piece<ANY>(dst + (k == 0 ? ca : cb), k == 0 ? na : nb, o);
             }
         }
         v[0] = next[0];
         v[1] = next[1];
         head += gt;
-    }
-}
-
-// Any other rows, element by element: a workgroup to a token, whose cosines and sines it takes once, a wavefront to every fourth
-// head; the next head's elements are asked for before this one's are turned.
-__global__ __launch_bounds__(256) void rope_heads_kernel(const RopeArgs a, int heads_per_block) {
-    constexpr int kEach = kRopeMaxHead / 64;   // elements of a lane at most
-    __shared__ float rows[4][kRopeMaxHead];
-    __shared__ float2 turns[kRopeMaxHead / 2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = a.rot >> 1;
-    const int64_t token = blockIdx.x;
-    const int h_begin = blockIdx.y * heads_per_block, h_end = min(a.heads, h_begin + heads_per_block);
-    const uint16_t* x = a.x + token * a.ldx;
-    uint32_t v[kEach] = {};
-    auto load = [&](int head) {
-#pragma unroll
-        for (int k = 0; k < kEach; ++k)
-            if (64 * k < a.d && 64 * k + lane < a.d) v[k] = x[head * a.ldxh + 64 * k + lane];
-    };
-    int head = h_begin + wave;
-    if (head < h_end) load(head);
-    for (int i = threadIdx.x; i < half; i += 256) {
-        float c, s;
-        rope_angle(a.positions[token], a.freq[i], c, s);
-        turns[i] = make_float2(c * a.mscale, s * a.mscale);
-    }
-    __syncthreads();
-    float* row = rows[wave];
-    for (; head < h_end; head += 4) {
-        float f[kEach], sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            f[k] = 64 * k + lane < a.d ? bf16_bits_to_f32(v[k]) : 0.0f;
-            sum = fmaf(f[k], f[k], sum);
-        }
-        if (head + 4 < h_end) load(head + 4);
-        const uint16_t* w = head < a.heads_q ? a.w_q : a.w_k;
-        float inv = 1.0f;
-        if (w) {
-            for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
-            inv = 1.0f / sqrtf(sum / (float)a.d + a.eps);
-        }
-        uint16_t* y = a.y + token * a.ldy + head * a.ldyh;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const int c = 64 * k + lane;
-            if (64 * k < a.d && c < a.d) {
-                const float g = w ? f[k] * inv * bf16_bits_to_f32(w[c]) : f[k];
-                if (c < a.rot) row[c] = g;
-                else y[c] = (uint16_t)pack_bf16_pair(g, 0.0f);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        for (int i = lane; i < half; i += 64) {
-            const int ca = a.interleaved ? 2 * i : i, cb = a.interleaved ? 2 * i + 1 : i + half;
-            const float2 cs = turns[i];
-            const float va = row[ca], vb = row[cb];
-            const uint32_t o = pack_bf16_pair(va * cs.x - vb * cs.y, vb * cs.x + va * cs.y);
-            y[ca] = (uint16_t)o;
-            y[cb] = (uint16_t)(o >> 16);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
 }
 

@@ -43,7 +43,7 @@ ROPE = dict(x=P, ldx=1280, ldxh=128, tokens=8, heads_q=8, heads_k=2, d=128, w_q=
     (dict(ldy=1279), SHAPE), (dict(ldy=128, ldyh=1000, y=2 * P), SHAPE), (dict(ldx=1288), SHAPE), (dict(x=None), NULL),
     (dict(y=None), NULL), (dict(positions=None), NULL), (dict(freq=None), NULL), (dict(w_q=None), NULL), (dict(w_k=None), NULL),
     (dict(x=P + 1), ALIGN), (dict(freq=P + 4), ALIGN), (dict(w_q=P + 1), ALIGN), (dict(positions=P + 2), ALIGN), (dict(tokens=0, x=None), OK),
-    (dict(tokens=1 << 29, heads_q=1, heads_k=0), SHAPE), (dict(tokens=1 << 24, x=P + 2), SHAPE)])   # more threads than a launch counts
+    (dict(tokens=1 << 29, heads_q=1, heads_k=0), SHAPE), (dict(tokens=1 << 30, x=P + 2), SHAPE)])   # more threads than a launch counts
 def test_rope_refuses(change, status):
     assert call("resq_rope_heads", ROPE, **change) == status
 

@@ -175,6 +175,27 @@ def test_rope_at_far_positions(rq, interleaved):
     check_rope(rq, x, pos, rq.resq_rope_frequencies(64)[0], 2, None, None, interleaved, 1.0)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(128, 54), (128, 102), (96, 24), (64, 22), (64, 6), (256, 250), (512, 500), (512, 510), (10, 4), (2, 2), (90, 90)])
+def test_rope_of_any_width(rq, d, rot, interleaved):
+    # widths that cut pieces of eight channels anywhere, many tokens to a workgroup and one, with values beside the turned channels that
+    # must reach no other channel
+    g = gen(d + rot)
+    freq, _ = rq.resq_rope_frequencies(rot)
+    w = (1 + 0.2 * torch.randn(d, generator=g)).to(torch.bfloat16).to(DEV)
+    for tokens, heads in ((1, 3), (37, 5), (2100, 3)):
+        x = torch.randn(tokens, heads, d, generator=g).to(torch.bfloat16).to(DEV)
+        pos = torch.randint(0, 5000, (tokens,), generator=g).to(torch.int32).to(DEV)
+        check_rope(rq, x, pos, freq, 2, w, w, interleaved, 1.25)
+        inplace = x.clone()
+        assert torch.equal(rq.resq_rope_heads(inplace, pos, freq, interleaved=interleaved, out=inplace),
+                           check_rope(rq, x, pos, freq, heads, None, None, interleaved, 1.0))
+        if rot < d:
+            x[..., rot] = float("inf")
+            out = rq.resq_rope_heads(x, pos, freq, interleaved=interleaved)
+            assert bool((out[..., rot] == float("inf")).all()) and int(out.isfinite().sum()) == tokens * heads * (d - 1)
+
+
 @pytest.mark.parametrize("d,rot", [(128, 128), (96, 40), (66, 66)])
 @pytest.mark.parametrize("interleaved,norm", [(False, True), (True, False)])
 def test_rope_layouts(rq, d, rot, interleaved, norm):
