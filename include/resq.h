@@ -462,7 +462,8 @@ int resq_dequantize_kv_cache(const void* cache, int64_t row_bytes, int64_t rows,
  * and values in two arrays alike in shape.  The row of head h in row i of page p is at byte
  *   p * page_stride + h * head_stride + i * row_stride
  * of its array (strides in bytes, multiples of 4, each at least resq_kv_cache_row_bytes; an axis of one entry has no stride;
- * rows do not overlap).  A SLOT is p * page_size + i, num_pages * page_size <= 2^31 - 1.  A row of the BLOCK TABLE names the
+ * rows do not overlap).  In pages r may also be an odd multiple of 4 below d_head <= 256: rows of r + (d_head - r) / 2 + 16 bytes
+ * in the same order, addresses and strides multiples of 2.  A SLOT is p * page_size + i, num_pages * page_size <= 2^31 - 1.  A row of the BLOCK TABLE names the
  * pages of a sequence in order: its token t is in row t % page_size of page block_table[b][t / page_size].  Any strides do for the
  * attention; it reads fastest where page_size is a multiple of 16 and row_stride below 2^26.
  * Common to these calls: lengths, positions, slots and table entries are int32 (4-byte aligned); head vectors are bf16 with a
@@ -534,9 +535,9 @@ int resq_rope_heads(const void* x, int64_t ldx, int64_t ldxh, int64_t tokens, in
  *   slots    int32 [tokens]; tokens whose slot is outside [0, num_pages * page_size) are left out; the others' slots differ
  *            from one another (a slot named twice is left with bytes of both tokens)      (read)
  *   k_pages, v_pages   the pages (above)                                                  (rows of the slots written, nothing else)
- *   d_head, r as resq_quantize_kv_cache; tokens = 0 does nothing
+ *   d_head, r as resq_quantize_kv_cache, or r as said above; tokens = 0 does nothing
  * Errors: RESQ_ERR_BUFFER for strides below the row; RESQ_ERR_ALIGN unless k and v are 16-byte aligned, their strides multiples
- * of 8, the pages 4-byte aligned and their strides multiples of 4.
+ * of 8, the pages 4-byte aligned and their strides multiples of 4 (2 and 2 where r is no multiple of 8).
  *
  * resq_gather_kv_cache is the paged reader: the values of the tokens in `slots` (any order, repeats are fine) as
  * resq_dequantize_kv_cache gives them, zeros for slots outside the pages.  k and v are written, their rows do not overlap.
@@ -562,7 +563,7 @@ int resq_gather_kv_cache(const void* k_pages, const void* v_pages, int64_t num_p
  *   lens     int32 [B]; what is above width * page_size (or 2^30) is read as that, what is below 0 as 0     (read)
  *   block_table  int32 [B, ld_table], `width` entries used of each row                    (read)
  *   lse      fp32 [B, heads_q] or null                                                    (written)
- *   d_head   multiple of 8, 8 .. 256; r as resq_quantize_kv_cache; heads_q a multiple of heads_k; B, heads_q <= 65535
+ *   d_head   multiple of 8, 8 .. 256; r as for the writer; heads_q a multiple of heads_k; B, heads_q <= 65535
  *   scale    > 0; softcap 0 (none) or a normal number above; window >= 0 (0: none)
  *   B * heads_q < 2^24, and B * heads_k * ceil(heads_q / heads_k / 16) * (ceil(width * page_size / 128) + 3) < 2^31
  *   workspace  device memory, 256-byte aligned, resq_attend_kv_cache_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents

@@ -578,8 +578,16 @@ def _explain_heads(where: str, name: str, t: torch.Tensor) -> None:
           f"{name} must be a bf16 [tokens, heads, d_head] tensor whose rows are contiguous")
 
 
+@functools.lru_cache(maxsize=1024, typed=True)
+def _page_row_bytes(d: int, r: int) -> int:
+    """Bytes of a head's row in pages, 0 where there are none; r may also be an odd multiple of four there, see include/resq.h."""
+    if r % 8 == 4 and 0 < r < d <= 256 and d % 8 == 0:
+        return r + (d - r) // 2 + 16
+    return resq_kv_cache_row_bytes(d, r)
+
+
 def _explain_pages(where: str, k: torch.Tensor, v: torch.Tensor, heads: int, d: int, r: int) -> None:
-    need = resq_kv_cache_row_bytes(d, r)
+    need = _page_row_bytes(d, r)
     _need(need > 0, where, f"invalid (d_head, r) = ({d}, {r})")
     _need(k.dim() == 4 and k.dtype == _U8 and v.dtype == _U8 and k.shape[1] == heads and k.shape[3] >= need and k.stride(3) == 1, where,
           f"pages must be uint8 [pages, {heads}, page_size, >= {need}] tensors whose rows are contiguous")
@@ -720,7 +728,7 @@ def resq_append_kv_cache(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
     dev = k.get_device()
     ldk, ldkh, one = k.stride()
     ldv, ldvh, one_v = v.stride() if v.dim() == 3 else (0, 0, 0)
-    need = resq_kv_cache_row_bytes(d, r)
+    need = _page_row_bytes(d, r)
     n, h, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
     strides = k_pages.stride()
     if not (k.dtype == _BF16 and v.dtype == _BF16 and slots.dtype == _I32 and k_pages.dtype == _U8 and v_pages.dtype == _U8
@@ -760,7 +768,7 @@ def resq_gather_kv_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: to
     dev = k_pages.get_device()
     ldk, ldkh, one = k.stride() if k.dim() == 3 else (0, 0, 0)
     ldv, ldvh, one_v = v.stride() if v.dim() == 3 else (0, 0, 0)
-    need = resq_kv_cache_row_bytes(d, r)
+    need = _page_row_bytes(d, r)
     strides = k_pages.stride()
     if not (k.dtype == _BF16 and v.dtype == _BF16 and slots.dtype == _I32 and k_pages.dtype == _U8 and v_pages.dtype == _U8
             and one == 1 and one_v == 1 and shape == (tokens, heads, d) and v.shape == shape and (d_head is None or d_head == d)
@@ -817,7 +825,7 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     dev = q.get_device()
     ldq, ldqh, one = q.stride()
     ldo, ldoh, one_o = out.stride() if out.dim() == 3 else (0, 0, 0)
-    need = resq_kv_cache_row_bytes(d, r)
+    need = _page_row_bytes(d, r)
     strides = k_pages.stride()
     ld_table, one_t = block_table.stride() if block_table.dim() == 2 else (0, 0)
     sums = None

@@ -383,13 +383,23 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 #pragma unroll
         for (int s = 0; s < LS; ++s) {
             raw_l[s] = Piece16{0u, 0u, 0u, 0u};
-            if (q_live && 32 * s < l_here) raw_l[s] = *reinterpret_cast<const Piece16*>(qrow + a.r + 8 * (4 * s + g));
+            // (the last four alone: with the four in front of them)
+            if (q_live && 32 * s < l_here)
+                raw_l[s] = *reinterpret_cast<const Piece16*>(qrow + a.r + 8 * (4 * s + g) - (l_here - 32 * s == 4 ? 4 : 0));
         }
         uint32_t next_mask = 0;
         if constexpr (BLOCKS) set_entries(tile0);
         if (tile0 < t_end) next_mask = load_tile(tile0);
         if constexpr (!BLOCKS) load_page(tile0 + kAttendUnit);
 
+        if (a.r & 4) {   // pieces of which four channels are the group's
+#pragma unroll
+            for (int s = 0; s < HS; ++s)
+                if (h_here - 32 * s == 4) raw_h[s].z = raw_h[s].w = 0u;
+#pragma unroll
+            for (int s = 0; s < LS; ++s)
+                if (l_here - 32 * s == 4) raw_l[s] = Piece16{raw_l[s].z, raw_l[s].w, 0u, 0u};
+        }
         v4u_att qh[HS], ql[LS ? LS : 1];
         float sum_h = 0.0f, sum_l = 0.0f;
 #pragma unroll
@@ -698,7 +708,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 #pragma unroll
             for (int i = 0; i < 4; ++i) ml[wave * kAttendRows + own + i] = make_float4(m2[i], l[i], zero_h[i], zero_l[i]);
         }
-        // both groups have a multiple of 8 channels, so that four in a row from a multiple of 4 on are of one group or of none.
+        // both groups have a multiple of 4 channels, so that four in a row from a multiple of 4 on are of one group or of none.
         // (What the limits are is kept from the compiler: it would take the comparisons out of the loop, each in registers.)
         int h_left = a.r - 4 * g, l_left = low - 4 * g * NL;
         asm volatile("" : "+v"(h_left), "+v"(l_left));

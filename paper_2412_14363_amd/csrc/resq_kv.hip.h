@@ -260,7 +260,7 @@ __device__ __forceinline__ void kv_row_of(const KvPagesArgs& a, uint32_t m, uint
     head = a.tokens_inner ? outer : inner;
 }
 
-template <int G>
+template <int G, int C>
 __global__ __launch_bounds__(kKvThreads) void append_kv_cache_kernel(const KvPagesArgs a) {
     const int gl = threadIdx.x & (G - 1), kind = blockIdx.y;
     const uint32_t m_raw = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
@@ -269,19 +269,37 @@ __global__ __launch_bounds__(kKvThreads) void append_kv_cache_kernel(const KvPag
     kv_row_of(a, m, token, head);
     const uint32_t slot = (uint32_t)a.slots[token];
     const uint16_t* x = a.x[kind] + token * a.ld[kind] + head * a.ldh[kind];
-    const uint4 v = gl < (a.d >> 3) ? reinterpret_cast<const uint4*>(x)[gl] : make_uint4(0u, 0u, 0u, 0u);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (gl < a.d / C) {
+        if constexpr (C == 8) {
+            v = reinterpret_cast<const uint4*>(x)[gl];
+        } else {
+            const uint2 half = reinterpret_cast<const uint2*>(x)[gl];
+            v.x = half.x;
+            v.y = half.y;
+        }
+    }
     const bool wanted = m_raw < a.rows && slot < a.num_slots;
-    quantize_kv_row<G>(v, gl, a.d, a.r, wanted ? a.pages[kind] + kv_row_offset(a, slot, head) : nullptr);
+    quantize_kv_row<G, C>(v, gl, a.d, a.r, wanted ? a.pages[kind] + kv_row_offset(a, slot, head) : nullptr);
 }
 
-template <int G>
+template <int G, int C>
 __global__ __launch_bounds__(kKvThreads) void gather_kv_cache_kernel(const KvPagesArgs a) {
     const int gl = threadIdx.x & (G - 1);
     const uint32_t m = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
-    if (m >= a.rows || gl >= (a.d >> 3)) return;
+    if (m >= a.rows || gl >= a.d / C) return;
     uint32_t token, head;
     kv_row_of(a, m, token, head);
     const uint32_t slot = (uint32_t)a.slots[token];
+    if constexpr (C == 4) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint2 o = make_uint2(0u, 0u);
+            if (slot < a.num_slots) o = dequantize_kv_half_piece(a.pages[k] + kv_row_offset(a, slot, head), gl, a.d, a.r);
+            reinterpret_cast<uint2*>(const_cast<uint16_t*>(a.x[k]) + token * a.ld[k] + head * a.ldh[k])[gl] = o;
+        }
+        return;
+    }
     uint4 o[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
     if (slot < a.num_slots) {
         const int64_t off = kv_row_offset(a, slot, head);

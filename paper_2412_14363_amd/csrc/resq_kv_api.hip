@@ -24,13 +24,18 @@ inline bool rows_apart(int64_t n, int64_t ld, int64_t heads, int64_t ldh, int64_
     return n <= 1 || heads <= 1 || ld >= (heads - 1) * ldh + width || ldh >= (n - 1) * ld + width;
 }
 
+// a head's row in pages: as everywhere, or with an 8-bit group of an odd multiple of four channels, at even addresses then
+inline bool page_head_ok(int64_t d_head, int64_t r) {
+    return kv_head_ok(d_head, r) || (kv_head_ok(d_head, r - 4) && r < d_head && d_head <= 256);
+}
+
 struct PagesGeometry {
     int64_t num_pages, page_size, heads, page_stride, head_stride, row_stride;
 };
 
 // checks the pages of a cache; strides of axes with one entry do not matter and become 0
 int check_pages(PagesGeometry& g, const void* k_pages, const void* v_pages, int64_t d_head, int64_t r) {
-    if (!kv_head_ok(d_head, r) || g.num_pages < 1 || g.page_size < 1 || g.num_pages > kInt32Max / g.page_size || g.heads < 1 ||
+    if (!page_head_ok(d_head, r) || g.num_pages < 1 || g.page_size < 1 || g.num_pages > kInt32Max / g.page_size || g.heads < 1 ||
         g.heads > 65535)
         return RESQ_ERR_SHAPE;
     const int64_t need = r + (d_head - r) / 2 + 16;
@@ -41,7 +46,8 @@ int check_pages(PagesGeometry& g, const void* k_pages, const void* v_pages, int6
         (g.page_size > 1 && g.row_stride < need))
         return RESQ_ERR_BUFFER;
     if (!k_pages || !v_pages) return RESQ_ERR_NULL;
-    if (!aligned(k_pages, 4) || !aligned(v_pages, 4) || g.page_stride % 4 || g.head_stride % 4 || g.row_stride % 4)
+    const int align = r % 8 ? 2 : 4;
+    if (!aligned(k_pages, align) || !aligned(v_pages, align) || g.page_stride % align || g.head_stride % align || g.row_stride % align)
         return RESQ_ERR_ALIGN;
     return RESQ_OK;
 }
@@ -56,7 +62,7 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     PagesGeometry g{num_pages, page_size, heads, page_stride, head_stride, row_stride};
     const int rc = check_pages(g, k_pages, v_pages, d_head, r);
     if (rc == RESQ_ERR_SHAPE || rc == RESQ_ERR_BUFFER) return rc;
-    const int64_t lanes = d_head <= 128 ? 16 : d_head <= 256 ? 32 : 64;   // of a row (below)
+    const int64_t lanes = (d_head <= 128 ? 16 : d_head <= 256 ? 32 : 64) * (r % 8 ? 2 : 1);   // of a row (below)
     if (tokens > kInt32Max / heads || !launch_fits(tokens * heads + 63, lanes)) return RESQ_ERR_SHAPE;
     if (tokens == 0) return RESQ_OK;
     if (!k || !v || !slots) return RESQ_ERR_NULL;
@@ -248,12 +254,15 @@ int resq_append_kv_cache(const void* k, int64_t ldk, int64_t ldkh, const void* v
     const int rc = make_pages_args(a, done, k, ldk, ldkh, v, ldv, ldvh, tokens, heads, d_head, r, slots, k_pages, v_pages, num_pages,
                                    page_size, page_stride, head_stride, row_stride);
     if (rc != RESQ_OK || done) return rc;
-#define RESQ_LAUNCH_APPEND(G)                                                                                          \
-    launch(append_kv_cache_kernel<G>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G), 2), dim3(kKvThreads), 0,   \
+#define RESQ_LAUNCH_APPEND(G, C)                                                                                       \
+    launch(append_kv_cache_kernel<G, C>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G), 2), dim3(kKvThreads), 0,   \
            static_cast<hipStream_t>(stream), a)
-    if (d_head <= 128) RESQ_LAUNCH_APPEND(16);
-    else if (d_head <= 256) RESQ_LAUNCH_APPEND(32);
-    else RESQ_LAUNCH_APPEND(64);
+    if (r % 8) {
+        if (d_head <= 128) RESQ_LAUNCH_APPEND(32, 4);
+        else RESQ_LAUNCH_APPEND(64, 4);
+    } else if (d_head <= 128) RESQ_LAUNCH_APPEND(16, 8);
+    else if (d_head <= 256) RESQ_LAUNCH_APPEND(32, 8);
+    else RESQ_LAUNCH_APPEND(64, 8);
 #undef RESQ_LAUNCH_APPEND
     return launch_status();
 }
@@ -268,12 +277,15 @@ int resq_gather_kv_cache(const void* k_pages, const void* v_pages, int64_t num_p
     const int rc = make_pages_args(a, done, k, ldk, ldkh, v, ldv, ldvh, tokens, heads, d_head, r, slots, k_pages, v_pages, num_pages,
                                    page_size, page_stride, head_stride, row_stride);
     if (rc != RESQ_OK || done) return rc;
-#define RESQ_LAUNCH_GATHER(G)                                                                                          \
-    launch(gather_kv_cache_kernel<G>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G)), dim3(kKvThreads), 0,      \
+#define RESQ_LAUNCH_GATHER(G, C)                                                                                       \
+    launch(gather_kv_cache_kernel<G, C>, dim3((a.rows + kKvThreads / G - 1) / (kKvThreads / G)), dim3(kKvThreads), 0,      \
            static_cast<hipStream_t>(stream), a)
-    if (d_head <= 128) RESQ_LAUNCH_GATHER(16);
-    else if (d_head <= 256) RESQ_LAUNCH_GATHER(32);
-    else RESQ_LAUNCH_GATHER(64);
+    if (r % 8) {
+        if (d_head <= 128) RESQ_LAUNCH_GATHER(32, 4);
+        else RESQ_LAUNCH_GATHER(64, 4);
+    } else if (d_head <= 128) RESQ_LAUNCH_GATHER(16, 8);
+    else if (d_head <= 256) RESQ_LAUNCH_GATHER(32, 8);
+    else RESQ_LAUNCH_GATHER(64, 8);
 #undef RESQ_LAUNCH_GATHER
     return launch_status();
 }

@@ -13,19 +13,28 @@
 
 namespace resq {
 
-// One row: v holds channels [8 gl, 8 gl + 8) of it in lane gl of the G lanes (all lanes of a wavefront call this: exchanges
-// and votes), row is where its bytes go, null for none.
-template <int G>
+// a row's numbers at any even address (a row of paged K/V whose r is an odd multiple of four has 4 k + 2 bytes)
+struct __attribute__((packed, aligned(2))) EvenDword { uint32_t v; };
+struct __attribute__((packed, aligned(2))) EvenFloat { float v; };
+
+// One row: v holds channels [C gl, C gl + C) of it in lane gl of the G lanes (all lanes of a wavefront call this: exchanges
+// and votes), row is where its bytes go, null for none.  C = 8, or 4 where r is not a multiple of eight: a lane's are of one group.
+template <int G, int C = 8>
 __device__ __forceinline__ void quantize_kv_row(const uint4 v, int gl, int d, int r, uint8_t* __restrict__ row) {
-    const int nunits = d >> 3, hi_units = r >> 3;
+    const int nunits = d / C, hi_units = r / C;
     const bool live = gl < nunits, high = gl < hi_units;
     const float inf = __builtin_huge_valf();
     float mx = -inf, nmn = -inf;
     if (live) {
         float f[8];
         unpack8_bf16(v, f);
-        mx = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
-        nmn = -fminf(fminf(fminf(f[0], f[1]), fminf(f[2], f[3])), fminf(fminf(f[4], f[5]), fminf(f[6], f[7])));
+        if constexpr (C == 8) {
+            mx = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+            nmn = -fminf(fminf(fminf(f[0], f[1]), fminf(f[2], f[3])), fminf(fminf(f[4], f[5]), fminf(f[6], f[7])));
+        } else {
+            mx = fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
+            nmn = -fminf(fminf(f[0], f[1]), fminf(f[2], f[3]));
+        }
     }
     const float mx_h = wave_max<G>(high ? mx : -inf), nmn_h = wave_max<G>(high ? nmn : -inf);
     const float mx_l = wave_max<G>(live && !high ? mx : -inf);
@@ -43,11 +52,11 @@ __device__ __forceinline__ void quantize_kv_row(const uint4 v, int gl, int d, in
     constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: quant8_asym, with the codes themselves
     const float tie = 0.5f - (levels + 1.0f) * 9.5367431640625e-07f;
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float ds[8];
-    uint32_t u[8];
-    bool near_tie[8], any_tie = false;
+    float ds[C];
+    uint32_t u[C];
+    bool near_tie[C], any_tie = false;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < C; ++j) {
         ds[j] = __uint_as_float((j & 1) ? (w[j >> 1] & 0xFFFF0000u) : (w[j >> 1] << 16)) - zero;
         const float t = ds[j] * inv;
         const float uf = t + kMagic;
@@ -57,11 +66,23 @@ __device__ __forceinline__ void quantize_kv_row(const uint4 v, int gl, int d, in
     }
     if (__builtin_amdgcn_ballot_w64(any_tie) != 0) {  // wave-uniform, then per element slot
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < C; ++j)
             if (__builtin_amdgcn_ballot_w64(near_tie[j]) != 0)
                 u[j] = (uint32_t)(int)fminf(fmaxf(rintf(ds[j] / scale), 0.0f), levels);
     }
     if (!row || !live) return;
+    if constexpr (C == 4) {
+        if (high) reinterpret_cast<EvenDword*>(row + gl * 4)->v = pack_low_bytes(u[0], u[1], u[2], u[3]);
+        else
+            *reinterpret_cast<uint16_t*>(row + r + (gl - hi_units) * 2) =
+                (uint16_t)((u[0] & 0xFu) | (u[1] & 0xFu) << 4 | (u[2] & 0xFu) << 8 | (u[3] & 0xFu) << 12);
+        if (gl == 0 || gl == hi_units) {   // (both groups are there: r is no multiple of eight, d is)
+            EvenFloat* p = reinterpret_cast<EvenFloat*>(row + r + (d - r) / 2) + (high ? 0 : 2);
+            p[0].v = scale;
+            p[1].v = zero;
+        }
+        return;
+    }
     float* par = reinterpret_cast<float*>(row + r + (d - r) / 2);
     if (high) {
         uint32_t* dst = reinterpret_cast<uint32_t*>(row + gl * 8);   // rows are 4-byte aligned
@@ -87,6 +108,19 @@ __device__ __forceinline__ void quantize_kv_row(const uint4 v, int gl, int d, in
         par[high ? 0 : 2] = scale;
         par[high ? 1 : 3] = zero;
     }
+}
+
+// The reader of rows with C = 4: channels [4 gl, 4 gl + 4).
+__device__ __forceinline__ uint2 dequantize_kv_half_piece(const uint8_t* __restrict__ row, int gl, int d, int r) {
+    const bool high = 4 * gl < r;
+    const EvenFloat* par = reinterpret_cast<const EvenFloat*>(row + r + (d - r) / 2) + (high ? 0 : 2);
+    const uint32_t c = high ? reinterpret_cast<const EvenDword*>(row + gl * 4)->v
+                            : *reinterpret_cast<const uint16_t*>(row + r + (gl - (r >> 2)) * 2);
+    const float s = par[0].v, z = par[1].v;
+    float f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = fmaf((float)(high ? (c >> (8 * k)) & 0xFFu : (c >> (4 * k)) & 0xFu), s, z);
+    return make_uint2(pack_bf16_pair(f[0], f[1]), pack_bf16_pair(f[2], f[3]));
 }
 
 // The reader of such rows: channels [8 gl, 8 gl + 8) of x[m, k] = bf16(code * s + z) (Eq. 1).

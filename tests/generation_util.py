@@ -14,7 +14,7 @@ def decode_rows(rows, d, r):
     """float64 [..., d] values of uint8 [..., row bytes] compact rows."""
     rows = rows.cpu()
     low = r + (d - r) // 2
-    par = rows[..., low:low + 16].contiguous().view(torch.float32).double()
+    par = rows[..., low:low + 16].clone(memory_format=torch.contiguous_format).view(torch.float32).double()
     out = torch.empty(*rows.shape[:-1], d, dtype=torch.float64)
     out[..., :r] = rows[..., :r].double() * par[..., 0:1] + par[..., 1:2]
     packed = rows[..., r:low].long()
@@ -103,7 +103,7 @@ def attend(q, k_pages, v_pages, lens, table, r, scale, softcap=0.0, window=0):
             kr, vr = k_pages[ids, h, t % page], v_pages[ids, h, t % page]
             k, v = decode_rows(kr, d, r), decode_rows(vr, d, r)
             low = r + (d - r) // 2
-            steps = [x[..., low:low + 16].contiguous().view(torch.float32).double() for x in (kr, vr)]
+            steps = [x[..., low:low + 16].clone(memory_format=torch.contiguous_format).view(torch.float32).double() for x in (kr, vr)]
             up = lambda p, hi, lo: torch.cat((hi * p[:, 0:1].expand(-1, r), lo * p[:, 2:3].expand(-1, d - r)), 1).abs()
             kbig, vbig = k.abs() + up(steps[0], 256, 32), v.abs() + up(steps[1], 255, 143)
             for i in range(h * share, (h + 1) * share):

@@ -51,7 +51,10 @@ def test_rope_refuses(change, status):
 APPEND = dict(k=P, ldk=1024, ldkh=128, v=P, ldv=1024, ldvh=128, tokens=4, heads=8, d=128, r=16, slots=P, k_pages=P, v_pages=P, num_pages=10,
               page_size=16, page_stride=8 * 16 * 88, head_stride=16 * 88, row_stride=88, stream=None)
 PAGE_FAULTS = [
-    (dict(d=124), SHAPE), (dict(d=520), SHAPE), (dict(r=136), SHAPE), (dict(r=12), SHAPE), (dict(r=-8), SHAPE), (dict(num_pages=0), SHAPE),
+    (dict(d=124), SHAPE), (dict(d=520), SHAPE), (dict(r=136), SHAPE), (dict(r=10), SHAPE), (dict(r=-8), SHAPE),
+    (dict(r=-4), SHAPE),
+    (dict(r=12, row_stride=91, head_stride=1456, page_stride=11648), ALIGN), (dict(r=12, row_stride=84), BUFFER),
+    (dict(r=12, k_pages=P + 1), ALIGN), (dict(num_pages=0), SHAPE),
     (dict(page_size=0), SHAPE), (dict(num_pages=1 << 27), SHAPE), (dict(row_stride=84), BUFFER),
     (dict(head_stride=80), BUFFER), (dict(page_stride=0), BUFFER), (dict(k_pages=None), NULL), (dict(v_pages=None), NULL),
     (dict(k_pages=P + 2), ALIGN), (dict(v_pages=P + 1), ALIGN), (dict(row_stride=90), ALIGN), (dict(head_stride=1410), ALIGN),
@@ -61,7 +64,8 @@ PAGE_FAULTS = [
 @pytest.mark.parametrize("change,status", PAGE_FAULTS + [
     (dict(tokens=-1), SHAPE), (dict(heads=0), SHAPE), (dict(ldk=-8), SHAPE), (dict(k=None), NULL), (dict(v=None), NULL), (dict(slots=None), NULL),
     (dict(k=P + 8), ALIGN), (dict(v=P + 2), ALIGN), (dict(ldk=1028), ALIGN), (dict(ldv=2048, ldvh=132), ALIGN), (dict(slots=P + 2), ALIGN),
-    (dict(tokens=0, k=None, slots=None), OK), (dict(tokens=1 << 28), SHAPE), (dict(tokens=1 << 25), SHAPE),
+    (dict(tokens=0, k=None, slots=None), OK), (dict(tokens=1 << 28), SHAPE),
+    (dict(d=264, r=12, ldk=2112, ldkh=264, ldv=2112, ldvh=264, row_stride=512, head_stride=8192, page_stride=1 << 17), SHAPE), (dict(tokens=1 << 25), SHAPE),
     (dict(tokens=1 << 24, d=256, ldk=2048, ldkh=256, ldv=2048, ldvh=256, row_stride=256, head_stride=4096, page_stride=32768), SHAPE)])
 def test_append_and_gather_refuse(change, status):
     assert call("resq_append_kv_cache", APPEND, **change) == status

@@ -280,6 +280,51 @@ def test_append_and_gather_without_tokens_and_from_broadcast_heads(rq):
     assert torch.equal(pages[0, 0, 0], pages[0, 2, 0]) and torch.equal(pages, v_pages) and not torch.equal(pages, was)
 
 
+def quantized_rows(rq, x, r):
+    """Rows of x [n, d] by the row quantizer, each group by itself in a row of its own, filled up with a channel that it has."""
+    def group(x, high):
+        n = x.shape[1]
+        full = torch.cat((x, x[:, :1].expand(-1, -n % 8)), 1).contiguous()
+        rows = rq.resq_quantize_kv_cache(full, full.shape[1] if high else 0)
+        at = rows.shape[1] - 16 + (0 if high else 8)
+        return rows[:, :n if high else n // 2], rows[:, at:at + 8]
+    (hi, hi_par), (lo, lo_par) = group(x[:, :r], True), group(x[:, r:], False)
+    return torch.cat((hi, lo, hi_par, lo_par), 1)
+
+
+@pytest.mark.parametrize("d,r", [(96, 12), (64, 20), (8, 4), (128, 124), (256, 4), (200, 100)])
+@pytest.mark.parametrize("order", ["head", "token"])
+def test_append_and_gather_of_halved_pieces(rq, d, r, order):
+    # 8-bit groups of an odd multiple of four channels: rows at even addresses
+    for tokens, heads, page, pad in ((1, 1, 1, 0), (67, 5, 24, 0), (300, 3, 16, 4)):
+        g = gen(tokens + d + r)
+        pages = -(-tokens // page) + 2
+        k, v = (torch.randn(tokens, heads, d, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+        k[0] = 2.5
+        buf = [plain.make_pages(g, pages, heads, page, d, r, order, pad) for _ in range(2)]
+        want = [b.clone() for b in buf]
+        slots = torch.randperm(pages * page, generator=g)[:tokens]
+        slots[tokens // 2] = -1
+        rq.resq_append_kv_cache(k, v, slots.to(torch.int32).to(DEV), *buf, r)
+        back = rq.resq_gather_kv_cache(*buf, slots.to(torch.int32).to(DEV), r, d_head=d)
+        live = slots >= 0
+        for x, b, w, y in zip((k, v), buf, want, back):
+            rows = quantized_rows(rq, x.reshape(-1, d), r).view(tokens, heads, -1)
+            for t in range(tokens):
+                if live[t]:
+                    w[slots[t] // page, :, slots[t] % page, :rows.shape[2]] = rows[t]
+            assert torch.equal(b, w), "the pages differ from the groups' bytes, or other bytes were written"
+            exact = plain.decode_rows(rows, d, r) * live[:, None, None]
+            # one rounding to fp32, one to bf16
+            assert bool(((y.cpu().double() - exact).abs() <= (2.0 ** -8 + 2.0 ** -20) * exact.abs()).all())
+
+
+@pytest.mark.parametrize("d,r", [(96, 12), (64, 20), (8, 4), (128, 124), (256, 4), (200, 100), (256, 140), (64, 4), (96, 92), (256, 252)])
+@pytest.mark.parametrize("page,order,share", [(16, "head", 4), (24, "token", 1), (16, "token", 12), (1, "head", 8)])
+def test_attend_of_halved_pieces(rq, d, r, page, order, share):
+    check_attend(rq, *attend_case(51, [300, 0, 1, 129], 2 * share, 2, d, r, page, order), r)
+
+
 def test_gather_of_repeated_slots(rq):
     pages = [plain.make_pages(gen(n), 4, 3, 16, 64, 8) for n in (3, 4)]
     slots = ints([5, 5, 63, -1, 5, 0, 63])
