@@ -229,15 +229,14 @@ __global__ __launch_bounds__(256) void kv_plan_tokens_kernel(const KvPlanArgs p)
 // The reader is bound by HBM (16384 tokens, 90 MB at least: 19.4 us from the last-level cache where slots come in runs of a page, 20.7 in
 // no order, when it fetches whole lines for 88-byte rows, 50 MB for 23; 28.5 on memory that no cache has), the writer by the
 // quantizer's instructions, some 270 per wavefront of four rows (27.4 us, 3.3 TB/s), both by the launch at a step's sizes (16 tokens: 2.8
-// and 3.0 us).  With a head's tokens in a row, or workgroups in a row on one die, runs take 17.7 and 18.1 us, but 256 channels on
-// memory that no cache has 58 instead of 53.8, and slots in no order 22.2 and 22.9 instead of 21.5.
+// and 3.0 us).  With a head's tokens in a row where they lie so in the pages, and such workgroups in a row on one die, runs take 17.7
+// and 18.1 us, but 256 channels on memory that no cache has 58 instead of 53.8, and slots in no order 22.2 and 22.9 instead of 21.5.
 // ---------------------------------------------------------------------------
 struct KvPagesArgs {
     const uint16_t* x[2];       // bf16 [tokens, heads, d], keys and values
     int64_t ld[2], ldh[2];      // elements from token to token and from head to head
     uint32_t rows;              // tokens * heads
-    FastDiv inner;              // tokens where they follow one another in `rows`, heads where those do
-    bool tokens_inner;
+    FastDiv heads;
     int d, r;
     const int32_t* slots;
     uint8_t* pages[2];
@@ -251,22 +250,12 @@ __device__ __forceinline__ int64_t kv_row_offset(const KvPagesArgs& a, uint32_t 
     return page * a.page_stride + head * a.head_stride + row * a.row_stride;
 }
 
-// Rows that lie side by side in a page, a head's tokens or a token's heads, follow one another, so that a workgroup has their lines
-// whole and no two dies fetch the same one (the reader on 16384 tokens in runs of 16, 8 heads of 128, head by head in the pages: 17.7
-// us, with a token's heads in a row 19.4; 256 channels 29.5 and 31.9).
-__device__ __forceinline__ void kv_row_of(const KvPagesArgs& a, uint32_t m, uint32_t& token, uint32_t& head) {
-    const uint32_t outer = a.inner(m), inner = m - outer * a.inner.d;
-    token = a.tokens_inner ? inner : outer;
-    head = a.tokens_inner ? outer : inner;
-}
-
 template <int G, int C>
 __global__ __launch_bounds__(kKvThreads) void append_kv_cache_kernel(const KvPagesArgs a) {
     const int gl = threadIdx.x & (G - 1), kind = blockIdx.y;
     const uint32_t m_raw = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
     const uint32_t m = min(m_raw, a.rows - 1);   // groups past the last row quantize it and store nothing
-    uint32_t token, head;
-    kv_row_of(a, m, token, head);
+    const uint32_t token = a.heads(m), head = m - token * a.heads.d;
     const uint32_t slot = (uint32_t)a.slots[token];
     const uint16_t* x = a.x[kind] + token * a.ld[kind] + head * a.ldh[kind];
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -288,8 +277,7 @@ __global__ __launch_bounds__(kKvThreads) void gather_kv_cache_kernel(const KvPag
     const int gl = threadIdx.x & (G - 1);
     const uint32_t m = blockIdx.x * (kKvThreads / G) + threadIdx.x / G;
     if (m >= a.rows || gl >= a.d / C) return;
-    uint32_t token, head;
-    kv_row_of(a, m, token, head);
+    const uint32_t token = a.heads(m), head = m - token * a.heads.d;
     const uint32_t slot = (uint32_t)a.slots[token];
     if constexpr (C == 4) {
 #pragma unroll

@@ -77,8 +77,7 @@ int make_pages_args(KvPagesArgs& a, bool& done, const void* k, int64_t ldk, int6
     a.ldh[0] = heads > 1 ? ldkh : 0;
     a.ldh[1] = heads > 1 ? ldvh : 0;
     a.rows = (uint32_t)(tokens * heads);
-    a.tokens_inner = g.row_stride < g.head_stride;
-    a.inner = FastDiv((uint32_t)(a.tokens_inner ? tokens : heads));
+    a.heads = FastDiv((uint32_t)heads);
     a.d = (int)d_head;
     a.r = (int)r;
     a.slots = slots;
