@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256) void kv_plan_tokens_kernel(const KvPlanArgs p)
 // the bytes are on their way: 21.5 instead of 25.3 us for 16384 tokens of 8 heads of 128; the writer has the quantizer's arithmetic,
 // and takes longer so: 8.8 instead of 7.9 for 2911 tokens).
 // The reader is bound by HBM (16384 tokens, 90 MB at least: 19.4 us from the last-level cache where slots come in runs of a page, 20.7 in
-// no order, when it fetches whole lines for 88-byte rows, 50 MB for 23; 28.5 on memory that no cache has), the writer by the
+// no order, when it fetches whole lines for 88-byte rows, 53 MB for 23; 28.5 on memory that no cache has), the writer by the
 // quantizer's instructions, some 270 per wavefront of four rows (27.4 us, 3.3 TB/s), both by the launch at a step's sizes (16 tokens: 2.8
 // and 3.0 us).  With a head's tokens in a row where they lie so in the pages, and such workgroups in a row on one die, runs take 17.7
 // and 18.1 us, but 256 channels on memory that no cache has 58 instead of 53.8, and slots in no order 22.2 and 22.9 instead of 21.5.
