@@ -143,6 +143,34 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+# Buffers that a call makes for itself.  The allocator orders a block's uses on the stream that it was allocated on alone: one from the
+# current stream's share may still be written by that stream's unfinished work when a kernel on another stream begins on it.  So
+# they are allocated on the call's own stream, and what is handed out is recorded on the current one, where the caller goes on with
+# it: freed, it is not handed out again before what that stream has by then is done.
+
+def _made(make, stream, device: torch.device, handed_out: bool = True):
+    """What make() allocates (a tensor, a tuple of them or an object that holds them) for a call on `stream`."""
+    if stream is None or device.type != "cuda":
+        return make()
+    if not hasattr(stream, "cuda_stream"):   # a handle; 0 is the default stream's
+        stream = torch.cuda.ExternalStream(int(stream), device) if int(stream) else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        new = make()
+    if handed_out:
+        current = torch.cuda.current_stream(device)
+        for t in (new,) if isinstance(new, torch.Tensor) else new if isinstance(new, tuple) else vars(new).values():
+            if isinstance(t, torch.Tensor):
+                t.record_stream(current)
+    return new
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """An output that a call makes for itself."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return _made(lambda: torch.empty(shape, dtype=dtype, device=device), stream, device)
+
+
 # ---- layout queries ---------------------------------------------------------
 # Functions of their arguments alone, asked for by every GEMM call's buffer checks: the last answers
 # are kept (0.1 us instead of 0.9).
@@ -623,11 +651,7 @@ def resq_kv_slots(lens: torch.Tensor, new_tokens: torch.Tensor, free_pages: torc
     batch = lens.shape[0]
     if out is None:
         _need(max_tokens is not None, "resq_kv_slots", "give out or max_tokens")
-        if stream is not None and lens.is_cuda:   # its buffers are cleared where the plan runs
-            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
-                out = KvSlots(batch, max_tokens, lens.device)
-        else:
-            out = KvSlots(batch, max_tokens, lens.device)
+        out = _made(lambda: KvSlots(batch, max_tokens, lens.device), stream, lens.device)   # (cleared where the plan runs)
     elif not isinstance(out, KvSlots):
         raise ValueError("resq_kv_slots: out must be a KvSlots")
     if taken is None:
@@ -681,7 +705,7 @@ def resq_rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor], freq: Op
     if heads_q is None:
         heads_q = heads
     if out is None:
-        out = torch.empty(shape, dtype=_BF16, device=x.device)
+        out = _empty(shape, _BF16, x.device, stream)
     rot = 0 if freq is None else 2 * freq.shape[0]
     dev = x.get_device()
     ldx, ldxh, one = x.stride()
@@ -762,7 +786,7 @@ def resq_gather_kv_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: to
     if k is None or v is None:
         _need(k is not None or d_head is not None, "resq_gather_kv_cache", "give k or d_head")
         shape = (tokens, heads, d_head if k is None else k.shape[-1])
-        k, v = (torch.empty(shape, dtype=_BF16, device=k_pages.device) if t is None else t for t in (k, v))
+        k, v = (_empty(shape, _BF16, k_pages.device, stream) if t is None else t for t in (k, v))
     shape = k.shape
     d = shape[-1]
     dev = k_pages.get_device()
@@ -813,15 +837,13 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     block_table [batch, pages] names.  scale: d_head^-0.5 when None.  lse: fp32 [batch, heads], written where given."""
     batch, heads, d = shape = q.shape
     if out is None:
-        out = torch.empty(shape, dtype=_BF16, device=q.device)
+        out = _empty(shape, _BF16, q.device, stream)
     if batch == 0:
         return out
     n, heads_k, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
     if workspace is None:
         nbytes = resq_attend_kv_cache_workspace_bytes(batch, heads, heads_k, d)
-        workspace = torch.empty(max(nbytes, 1), dtype=_U8, device=q.device)
-        if stream is not None and q.is_cuda:   # made on the current stream, used on another one
-            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+        workspace = _made(lambda: torch.empty(max(nbytes, 1), dtype=_U8, device=q.device), stream, q.device, handed_out=False)
     dev = q.get_device()
     ldq, ldqh, one = q.stride()
     ldo, ldoh, one_o = out.stride() if out.dim() == 3 else (0, 0, 0)

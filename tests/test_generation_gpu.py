@@ -542,6 +542,33 @@ def test_attend_on_other_streams(rq):
     assert all(torch.equal(o, want) for o in outs)
 
 
+def test_buffers_that_a_call_makes_on_another_stream(rq):
+    """Outputs and workspace that a call on `stream` makes for itself are not blocks that the current stream has work on: that work
+    would land in them behind the call.  The stream as an object, as a handle, and as the default stream's handle, 0."""
+    case = attend_case(17, [3000, 10, 777], 16, 4, 128, 16, 32)
+    x, freq = torch.randn(300, 6, 128, generator=gen(18)).to(torch.bfloat16).to(DEV), rq.resq_rope_frequencies(128)[0]
+    positions, slots = ints(list(range(300))), ints(list(range(0, 96, 2)))
+    calls = [lambda s: (rq.resq_attend_kv_cache(*case, 16, stream=s),), lambda s: (rq.resq_rope_heads(x, positions, freq, stream=s),),
+             lambda s: rq.resq_gather_kv_cache(case[1], case[2], slots, 16, d_head=128, stream=s)]
+    want = [f(None) for f in calls]
+    sizes = {t.nbytes for ts in want for t in ts} | {rq.resq_attend_kv_cache_workspace_bytes(3, 16, 4, 128)}
+    side, own = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream, current in ((side, own), (side.cuda_stream, own), (0, own), (side, torch.cuda.default_stream())):
+        with torch.cuda.stream(current):
+            for f, expected in zip(calls, want):
+                busy = torch.randn(2048, 2048, device=DEV)
+                for _ in range(40):
+                    busy = busy @ busy * 1e-2
+                junk = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(4)]
+                for j in junk:
+                    j.fill_(255)   # behind what is running
+                del junk, j
+                got = f(stream)
+                torch.cuda.synchronize()
+                assert len(got) == len(expected) and all(torch.equal(a, b) for a, b in zip(got, expected))
+
+
 def test_attend_graphs_share_a_workspace(rq):
     # two captured calls, one with rows of 16 KB in LDS per wavefront, replayed in turn with eager calls between them
     cases = [(attend_case(41, [900, 0, 33], 4, 2, 256, 256, 16), 256), (attend_case(42, [5000, 77], 16, 2, 128, 16, 24, "token"), 16)]
