@@ -230,7 +230,7 @@ def resq_quantize_act(x: torch.Tensor, r: int, out: Optional[ActCodes] = None,
     if x.stride(1) != 1:
         raise ValueError("x must be row-major")
     if out is None:
-        out = ActCodes(M, K, r, x.device)
+        out = _made(lambda: ActCodes(M, K, r, x.device), stream, x.device)
     st = lib().resq_quantize_act(_dev(x, torch.bfloat16, "x"), x.stride(0), M, K, r,
                                  out.q_hi.data_ptr() if r > 0 else None,
                                  out.q_lo.data_ptr() if K - r > 0 else None,
@@ -250,7 +250,7 @@ def resq_hadamard_quantize_act(x: torch.Tensor, r: int, block: int = 0,
     if x_rot is not None and x_rot.stride(1) != 1:
         raise ValueError("x_rot must be row-major")
     if out is None:
-        out = ActCodes(M, K, r, x.device)
+        out = _made(lambda: ActCodes(M, K, r, x.device), stream, x.device)
     st = lib().resq_hadamard_quantize_act(
         _dev(x, torch.bfloat16, "x"), x.stride(0), M, K, r, block,
         out.q_hi.data_ptr() if r > 0 else None, out.q_lo.data_ptr(),
@@ -267,7 +267,7 @@ def resq_quantize_act_asym(x: torch.Tensor, r: int, hadamard_block: int = 0,
     if x.stride(1) != 1:
         raise ValueError("x must be row-major")
     if out is None:
-        out = ActCodes(M, K, r, x.device)
+        out = _made(lambda: ActCodes(M, K, r, x.device), stream, x.device)
     hi, lo = r > 0, K - r > 0
     st = lib().resq_quantize_act_asym(
         _dev(x, torch.bfloat16, "x"), x.stride(0), M, K, r, hadamard_block,
@@ -298,7 +298,7 @@ def resq_quantize_gemm_mixed(x: torch.Tensor, packed: torch.Tensor, N: int, r: i
     if x.stride(1) != 1:
         raise ValueError("x must be row-major")
     if y is None:
-        y = torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
+        y = _empty((M, N), torch.bfloat16, x.device, stream)
     if y.stride(1) != 1:
         raise ValueError("y must be row-major")
     need = resq_packed_weight_bytes(N, K, r)
@@ -321,7 +321,7 @@ def resq_hadamard_quantize_act_asym(x: torch.Tensor, r: int, block: int = 0,
     if x_rot is not None and x_rot.stride(1) != 1:
         raise ValueError("x_rot must be row-major")
     if out is None:
-        out = ActCodes(M, K, r, x.device)
+        out = _made(lambda: ActCodes(M, K, r, x.device), stream, x.device)
     hi = r > 0
     st = lib().resq_hadamard_quantize_act_asym(
         _dev(x, torch.bfloat16, "x"), x.stride(0), M, K, r, block,
@@ -341,7 +341,7 @@ def resq_gemm_mixed_asym(act: ActCodes, packed: torch.Tensor, N: int,
                          dbg_acc_lo: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M, K, r = act.M, act.K, act.r
     if y is None:
-        y = torch.empty((M, N), dtype=torch.bfloat16, device=packed.device)
+        y = _empty((M, N), torch.bfloat16, packed.device, stream)
     if y.stride(1) != 1:
         raise ValueError("y must be row-major")
     _check_layer_buffers("resq_gemm_mixed_asym", act, packed, N, N, y,
@@ -364,7 +364,7 @@ def resq_pack_weights(w: torch.Tensor, r: int, packed: Optional[torch.Tensor] = 
     if w.stride(1) != 1:
         raise ValueError("w must be row-major [N, K]")
     if packed is None:
-        packed = alloc_packed(N, K, r, w.device)
+        packed = _made(lambda: alloc_packed(N, K, r, w.device), stream, w.device)
     st = lib().resq_pack_weights(_dev(w, torch.bfloat16, "w"), w.stride(0), N, K, r,
                                  _dev(packed, torch.uint8, "packed"), packed.numel(),
                                  _stream(stream))
@@ -377,10 +377,10 @@ def resq_unpack_weights(packed: torch.Tensor, N: int, K: int, r: int, stream=Non
     need = resq_packed_weight_bytes(N, K, r)
     if need == 0 or packed.numel() < need:
         raise ValueError(f"resq_unpack_weights: packed holds {packed.numel()} bytes, (N, K, r) = ({N}, {K}, {r}) needs {need}")
-    w_hi = torch.empty((N, r), dtype=torch.int8, device=dev)
-    w_lo = torch.empty((N, K - r), dtype=torch.int8, device=dev)
-    sw_hi = torch.empty(N, dtype=torch.int16, device=dev)
-    sw_lo = torch.empty(N, dtype=torch.int16, device=dev)
+    w_hi = _empty((N, r), torch.int8, dev, stream)
+    w_lo = _empty((N, K - r), torch.int8, dev, stream)
+    sw_hi = _empty(N, torch.int16, dev, stream)
+    sw_lo = _empty(N, torch.int16, dev, stream)
     st = lib().resq_unpack_weights(_dev(packed, torch.uint8, "packed"), N, K, r,
                                    w_hi.data_ptr() if r > 0 else None,
                                    w_lo.data_ptr() if K - r > 0 else None,
@@ -395,7 +395,7 @@ def resq_gemm_mixed(act: ActCodes, packed: torch.Tensor, N: int, y: Optional[tor
                     dbg_acc_lo: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M, K, r = act.M, act.K, act.r
     if y is None:
-        y = torch.empty((M, N), dtype=torch.bfloat16, device=packed.device)
+        y = _empty((M, N), torch.bfloat16, packed.device, stream)
     if y.stride(1) != 1:
         raise ValueError("y must be row-major")
     _check_layer_buffers("resq_gemm_mixed", act, packed, N, N, y,
@@ -418,7 +418,7 @@ def resq_gemm_mixed_swiglu(act: ActCodes, packed: torch.Tensor, N2: int,
     """packed: 2F interleaved (gate, up) channels; returns y [M, F] = silu(gate) * up."""
     M, K, r = act.M, act.K, act.r
     if y is None:
-        y = torch.empty((M, N2 // 2), dtype=torch.bfloat16, device=packed.device)
+        y = _empty((M, N2 // 2), torch.bfloat16, packed.device, stream)
     if y.stride(1) != 1:
         raise ValueError("y must be row-major")
     if N2 % 2:
@@ -440,7 +440,7 @@ def resq_gram_accumulate(x: torch.Tensor, c: Optional[torch.Tensor] = None, stre
     if x.stride(1) != 1:
         raise ValueError("x must be row-major")
     if c is None:
-        c = torch.zeros((K, K), dtype=torch.float32, device=x.device)
+        c = _made(lambda: torch.zeros((K, K), dtype=torch.float32, device=x.device), stream, x.device)   # (cleared where it is added to)
     st = lib().resq_gram_accumulate(_dev(x, torch.bfloat16, "x"), x.stride(0), T, K,
                                     _dev(c, torch.float32, "c"), c.stride(0), _stream(stream))
     _check(st, "resq_gram_accumulate")
@@ -451,9 +451,9 @@ def resq_sym_eig(c: torch.Tensor, sweeps: int = 12, stream=None):
     """Eigenvalues (decreasing, fp32 [K]) and eigenvectors (columns of fp32 [K, K]) of the symmetric c."""
     K = c.shape[0]
     nbytes = lib().resq_sym_eig_workspace_bytes(K)
-    work = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=c.device)
-    lam = torch.empty(K, dtype=torch.float32, device=c.device)
-    p = torch.empty((K, K), dtype=torch.float32, device=c.device)
+    work = _made(lambda: torch.empty(max(nbytes, 1), dtype=torch.uint8, device=c.device), stream, c.device, handed_out=False)
+    lam = _empty(K, torch.float32, c.device, stream)
+    p = _empty((K, K), torch.float32, c.device, stream)
     st = lib().resq_sym_eig(_dev(c, torch.float32, "c"), c.stride(0), K, sweeps, lam.data_ptr(), p.data_ptr(),
                             p.stride(0), work.data_ptr(), nbytes, _stream(stream))
     _check(st, "resq_sym_eig")
@@ -483,7 +483,7 @@ def resq_project_rows(a: torch.Tensor, u: torch.Tensor, out: Optional[torch.Tens
     if a.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("a must be bf16 or fp32")
     if out is None:
-        out = torch.empty((rows, J), dtype=out_dtype or a.dtype, device=a.device)
+        out = _empty((rows, J), out_dtype or a.dtype, a.device, stream)
     if out.stride(1) != 1 or out.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("out must be row-major bf16 or fp32")
     st = lib().resq_project_rows(_dev(a, a.dtype, "a"), int(a.dtype == torch.bfloat16), a.stride(0), rows, K,
@@ -512,7 +512,7 @@ def resq_project_heads(x: torch.Tensor, packed: torch.Tensor, y: Optional[torch.
     if x.stride(1) != 1:
         raise ValueError("x must be row-major")
     if y is None:
-        y = torch.empty((rows, d), dtype=torch.bfloat16, device=x.device)
+        y = _empty((rows, d), torch.bfloat16, x.device, stream)
     if y.stride(1) != 1:
         raise ValueError("y must be row-major")
     need = resq_packed_weight_bytes(d, d, d)
@@ -541,7 +541,7 @@ def resq_quantize_kv_cache(x: torch.Tensor, r: int, cache: Optional[torch.Tensor
     if need == 0:
         raise ValueError(f"invalid (d_head, r) = ({d}, {r})")
     if cache is None:
-        cache = torch.empty((rows, need), dtype=torch.uint8, device=x.device)
+        cache = _empty((rows, need), torch.uint8, x.device, stream)
     have = cache.shape   # (a new object every time it is asked for)
     if len(have) != 2 or have[0] != rows or cache.stride(1) != 1 or have[1] < need:
         raise ValueError(f"cache must be a row-major [{rows}, >= {need}] byte tensor")
@@ -560,7 +560,7 @@ def resq_dequantize_kv_cache(cache: torch.Tensor, d_head: int, r: int, out: Opti
     if need == 0 or len(have) != 2 or cache.stride(1) != 1 or have[1] < need:
         raise ValueError(f"cache must be a row-major [rows, >= {need}] byte tensor for (d_head, r) = ({d_head}, {r})")
     if out is None:
-        out = torch.empty((rows, d_head), dtype=torch.bfloat16, device=cache.device)
+        out = _empty((rows, d_head), torch.bfloat16, cache.device, stream)
     if out.shape != (rows, d_head) or out.stride(1) != 1:
         raise ValueError(f"out must be a row-major [{rows}, {d_head}] tensor")
     st = lib().resq_dequantize_kv_cache(_dev(cache, torch.uint8, "cache"), cache.stride(0), rows, d_head, r,
@@ -890,7 +890,7 @@ def resq_online_hadamard(x: torch.Tensor, col_begin: int, col_end: int, block: i
     if x.stride(1) != 1:
         raise ValueError("x must be row-major")
     if out is None:
-        out = torch.empty_like(x)
+        out = _made(lambda: torch.empty_like(x), stream, x.device)
     if out.stride() != x.stride():
         raise ValueError("out must have x's layout")
     st = lib().resq_online_hadamard(_dev(x, torch.bfloat16, "x"), _dev(out, torch.bfloat16, "out"),

@@ -128,6 +128,12 @@ __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
     return cap * (y2 < 0.0625f ? small : big);
 }
 
+// 16 bytes of a row in pages, at any even address
+__device__ __forceinline__ uint4 piece_at(const uint8_t* p) {
+    const Piece16 o = *reinterpret_cast<const Piece16*>(p);
+    return make_uint4(o.x, o.y, o.z, o.w);
+}
+
 // A row comes to LDS in pieces of 16 bytes: its codes (the last of their pieces may hold a part of what follows them, or be
 // there in vain: codes of some kind, which meet zeros or are not written out), and the 16 bytes of its scales and zero-points.
 // The pitch of rows in LDS is a constant, so that every address is a lane's base and a constant, with the constants last, and
@@ -346,8 +352,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                     const int64_t e = (64 * i + 63) / PL < 16 ? e0 : 64 * i / PL >= 16 ? e1 : piece_row[i] < 16 ? e0 : e1;
                     if ((64 * (i + 1) <= kAttendTile * PL || 64 * i + lane < kAttendTile * PL) &&
                         (mask == 0xFFFFFFFFu || ((mask >> piece_row[i]) & 1))) {
-                        kreg[i] = *reinterpret_cast<const uint4*>(a.pages[0] + e + (uint32_t)piece_off[i]);
-                        vreg[i] = *reinterpret_cast<const uint4*>(a.pages[1] + e + (uint32_t)piece_off[i]);
+                        kreg[i] = piece_at(a.pages[0] + e + (uint32_t)piece_off[i]);
+                        vreg[i] = piece_at(a.pages[1] + e + (uint32_t)piece_off[i]);
                     }
                 }
             } else {
@@ -359,8 +365,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
                 for (int i = 0; i < KU; ++i) {
                     const int64_t e = ((int64_t)__shfl((int)(off >> 32), piece_row[i]) << 32) | (uint32_t)__shfl((int)off, piece_row[i]);
                     if ((64 * (i + 1) <= kAttendTile * PL || 64 * i + lane < kAttendTile * PL) && ((mask >> piece_row[i]) & 1)) {
-                        kreg[i] = *reinterpret_cast<const uint4*>(a.pages[0] + e + piece_off[i]);
-                        vreg[i] = *reinterpret_cast<const uint4*>(a.pages[1] + e + piece_off[i]);
+                        kreg[i] = piece_at(a.pages[0] + e + piece_off[i]);
+                        vreg[i] = piece_at(a.pages[1] + e + piece_off[i]);
                     }
                 }
             }
