@@ -504,6 +504,28 @@ def test_attend_values_that_are_not_finite(rq):
     assert out[2].isfinite().all()
 
 
+def test_attend_weights_keep_their_bits(rq):
+    """Few tokens of equal scores (queries of zero): the mean of the values, to the roundings of 32-bit arithmetic and 2^-17 of half the
+    values' range.  Sums are of codes with their offsets, at most 143 steps of a 4-bit group and 255 of the 8-bit one, and of zero-points:
+    some eight roundings of 2^-24 of the largest partial sum, below 2^-20 of the mean of those magnitudes; weights go in as two bf16
+    numbers, each the nearest (2^-8), which leave 2^-17 at most, and that meets the middle of the codes, 7.5 (127.5) steps from their ends."""
+    for d, r, hq, hk in ((128, 16, 8, 2), (64, 8, 3, 3), (128, 0, 12, 1), (256, 32, 4, 2), (128, 128, 2, 2), (96, 12, 20, 1)):
+        lens = [1, 2, 3, 4, 5, 7] * 6
+        q, k, v, lens, table = attend_case(d + r, lens, hq, hk, d, r, 16)
+        q.zero_()
+        got = rq.resq_attend_kv_cache(q, k, v, lens, table, r).cpu().double()
+        low = r + (d - r) // 2
+        for b, n in enumerate(lens.tolist()):
+            rows = v[table[b, 0].item(), :, :n].cpu()
+            par = rows[..., low:low + 16].clone(memory_format=torch.contiguous_format).view(torch.float32).double().abs()
+            size = torch.cat(((255 * par[..., 0:1] + par[..., 1:2]).expand(-1, -1, r), (271 * par[..., 2:3] + par[..., 3:4]).expand(-1, -1, d - r)), -1)
+            want = plain.decode_rows(rows, d, r).mean(1).repeat_interleave(hq // hk, 0)
+            half = torch.cat(((127.5 * par[..., 0:1]).expand(-1, -1, r), (7.5 * par[..., 2:3]).expand(-1, -1, d - r)), -1)
+            tol = (2.0 ** -20 * size + 2.0 ** -17 * half).mean(1).repeat_interleave(hq // hk, 0)
+            off = (got[b] - want).abs()
+            assert not (off > tol + 2.0 ** -8 * (want.abs() + tol)).any(), (d, r, n, float(((off - 2.0 ** -8 * want.abs()) / tol).max()))
+
+
 def test_attend_equal_calls_give_equal_bits(rq):
     case = attend_case(14, [3000, 10, 7777, 0, 128], 16, 4, 128, 16, 32)
     first = check_attend(rq, *case, 16)

@@ -76,3 +76,13 @@ def test_attend_cuts(attend):
     # a head in more parts than the join reads at once, several heads in a run, more sequences than a workgroup has threads
     check(attend, [case([1300], 1, 1, 8, 0, 64), case([500, 3, 0, 90], 6, 3, 16, 8, 16), case([1] * 150 + [0] * 120 + [140], 1, 1, 8, 0, 16),
                    case([0] * 5, 2, 2, 32, 8, 16)])
+
+
+def test_attend_weights_keep_their_bits(attend):
+    # scores are below 8 here, and off by less than 2^-20 for their sums of at most 128 products; weights are off by 2^-17 of half the
+    # codes' range (which is no more than a value's size here, zero-point and code apart); fp32 sums are of up to 16 times a value's
+    # size, 2^-24 of that for each of a few roundings
+    cases = [case([1, 2, 3, 4, 5, 40], 4, 2, d, r, 16) for d, r in ((128, 16), (64, 8), (64, 0), (128, 128), (96, 12))]
+    cases.append(case([1, 2, 3, 33], 12, 1, 64, 8, 16))
+    for c, (off_out, off_lse) in zip(cases, attend(cases), strict=True):
+        assert off_out <= 2.0 ** -16 and off_lse <= 2.0 ** -20, (c, off_out, off_lse)
