@@ -515,8 +515,8 @@ int resq_rope_frequencies(int64_t rot, double base, int scaling, double factor, 
  *   n = x * rsqrt(mean(x^2) + eps) * w   (w: w_q for heads [0, heads_q), w_k for the others; both null: n = x)
  *   y = n with each pair (a, b) of its first rot channels turned to mscale * (a cos - b sin, b cos + a sin) by the angle
  *       positions[token] * freq[pair]; pair i is channels (i, i + rot/2), or (2i, 2i + 1) where `interleaved` is not 0
- * in fp32 with one rounding to bf16 at the end; the angle is taken modulo a turn in fp64, so that it is as exact at position
- * 2^31 - 1 as at 1.  Channels [rot, d_head) are n alone.
+ * in fp32 with one rounding to bf16 at the end; the angle is taken modulo a turn in pairs of fp64 numbers, before it is rounded to fp32,
+ * so that it is as exact at position 2^31 - 1 as at 1.  Channels [rot, d_head) are n alone.
  *   x, y     bf16 [tokens, heads_q + heads_k, d_head] with strides (ldx, ldxh), (ldy, ldyh); y may be x with the same strides,
  *            else they do not overlap                                                    (read / written)
  *   d_head   even, 2 .. 512; rot even, 0 .. d_head (positions and freq may be null for 0); tokens = 0 does nothing

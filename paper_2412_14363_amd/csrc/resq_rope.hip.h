@@ -2,7 +2,7 @@
 // each head in the same pass where a model has one:
 //   n = x * rsqrt(mean(x^2) + eps) * w                                (fp32, not rounded in between; or n = x)
 //   (a, b) -> m * (a cos - b sin, b cos + a sin),  angle = position * freq[i] for pair i
-// and one rounding to bf16 at the end.  The angle is reduced modulo a turn in fp64, so that far positions lose nothing.
+// and one rounding to bf16 at the end.  The angle is reduced modulo a turn in pairs of fp64 numbers, so that far positions lose nothing.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -30,11 +30,14 @@ struct RopeArgs {
     int64_t ldy, ldyh;
 };
 
-// cos and sin of position * freq radians
+// cos and sin of position * freq radians.  Both products are held as a double and its error, so that what is left of whole turns is
+// right to the last of its fp32 bits (a double alone is 3e-7 radians off at position 2^31, more than fp32 is).
 __device__ __forceinline__ void rope_angle(int position, double freq, float& c, float& s) {
-    constexpr double kTurn = 0.15915494309189533577;   // 1 / (2 pi)
-    const double turns = (double)position * (freq * kTurn);
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+#pragma clang fp contract(off)   // (turns - rint(turns) as a product and a difference in one would hold `rest` already)
+    constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;   // 1 / (2 pi)
+    const double p = position, f = freq * kTurn, f_rest = fma(freq, kTurnRest, fma(freq, kTurn, -f));
+    const double turns = p * f, rest = fma(p, f_rest, fma(p, f, -turns));
+    sincospif(2.0f * (float)((turns - rint(turns)) + rest), &s, &c);
 }
 
 // n of a row's elements in a piece of eight, from any address on (ANY), or eight or none at a multiple of 16 bytes

@@ -2,6 +2,7 @@
 implementations (generation_util.py) and, where the library has the same arithmetic already, bit for bit against that."""
 import itertools
 import math
+from decimal import Decimal, getcontext
 
 import pytest
 import torch
@@ -222,6 +223,28 @@ def test_rope_layouts(rq, d, rot, interleaved, norm):
             assert torch.equal(flat[:, :shift], keep[:, :shift]) and torch.equal(flat[:, shift + heads * d:], keep[:, shift + heads * d:])
         else:
             check_rope(rq, x[:, :1].expand(-1, heads, -1), pos, freq, 4, *w, interleaved, mscale)
+
+
+def test_rope_angles_near_whole_turns(rq):
+    """(1, 0) turned by an angle that is a tiny rest of many turns: its sine is that rest, in fp32 (2^-22 for the rounding, the sine and the
+    products) and rounded to bf16, however far the position."""
+    getcontext().prec = 90
+    turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899")
+    freq = torch.tensor([1.0, 500000.0 ** (-2 / 128), 0.7071, 0.0123456789], dtype=torch.float64)
+    g = torch.Generator().manual_seed(8)
+    near = torch.randint(1 << 29, (1 << 31) - 1, (1 << 20,), generator=g).double()
+    positions = [0, 1, 710, 312689, 4272943, 411557987, 2147483647, -411557987]
+    for f in freq:   # the nearest of a million far positions
+        rest = near * (f / (2 * math.pi))
+        positions.append(int(near[(rest - rest.round()).abs().argmin()]))
+    x = torch.zeros(len(positions), 1, 8)
+    x[..., :4] = 1
+    y = rq.resq_rope_heads(x.to(torch.bfloat16).to(DEV), ints(positions), freq.to(DEV)).cpu().double()
+    for t, p in enumerate(positions):
+        for i, f in enumerate(freq.tolist()):
+            angle = p * Decimal(f)
+            want = math.sin(float(angle - turn * (angle / turn).to_integral_value()))
+            assert abs(float(y[t, 0, 4 + i]) - want) <= (2.0 ** -8 + 2.0 ** -21) * abs(want), (p, f, want, float(y[t, 0, 4 + i]))
 
 
 def test_rope_of_zeros_huge_and_no_tokens(rq):
