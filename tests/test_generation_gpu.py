@@ -461,6 +461,25 @@ def test_attend_window_and_cap(rq, window, softcap):
         check_attend(rq, *attend_case(window % 97, [0] + LENS, 4, 1, 64, 8, page, order), 8, softcap=softcap, window=window)
 
 
+@pytest.mark.parametrize("batch", [66, 600, 5001, 65535])
+def test_attend_many_sequences_without_tokens(rq, batch):
+    """Live sequences at both ends and in the middle of a padded batch; the last time they have more units than there are workgroups, so
+    that one's run holds the first one's end (its fifth unit), steps over all the others and holds the last one's beginning."""
+    for live in ([(0, 1), (batch - 1, 33)], [(0, 40), (1, 3), (batch // 2, 100), (batch // 2 + 1, 1), (batch - 2, 16), (batch - 1, 700)], [(0, 200), (batch - 1, 120000)]):
+        lens = torch.zeros(batch, dtype=torch.int32)
+        lens[[b for b, _ in live]] = torch.tensor([n for _, n in live], dtype=torch.int32)
+        q, k, v, few, table = attend_case(batch, [n for _, n in live], 2, 1, 16, 8, 256)
+        at = lens.nonzero().flatten().to(DEV)
+        wide, queries = torch.full((batch, table.shape[1]), -1, dtype=torch.int32, device=DEV), torch.ones(batch, 2, 16, dtype=torch.bfloat16, device=DEV)
+        wide[at], queries[at] = table, q
+        want, want_lse = check_attend(rq, q, k, v, few, table, 8)
+        lse = torch.full((batch, 2), 7.0, device=DEV)
+        out = rq.resq_attend_kv_cache(queries, k, v, lens.to(DEV), wide, 8, lse=lse)
+        assert torch.equal(out[at], want) and torch.equal(lse[at], want_lse)
+        out[at], lse[at] = 0, -math.inf
+        assert not out.any() and bool((lse == -math.inf).all())
+
+
 def test_attend_scales(rq):
     case = attend_case(5, [300, 1, 40], 8, 2, 128, 16, 16)
     for scale in (1e-6, 0.02, 3.0, 50.0):   # the last: one token holds all the weight

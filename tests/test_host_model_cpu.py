@@ -75,6 +75,7 @@ def test_attend_windows_caps_and_missing_pages(attend):
 def test_attend_cuts(attend):
     # a head in more parts than the join reads at once, several heads in a run, more sequences than a workgroup has threads
     check(attend, [case([1300], 1, 1, 8, 0, 64), case([500, 3, 0, 90], 6, 3, 16, 8, 16), case([1] * 150 + [0] * 120 + [140], 1, 1, 8, 0, 16),
+                   case([30] + [0] * 200 + [40] + [0] * 64 + [3], 1, 1, 8, 0, 16),
                    case([0] * 5, 2, 2, 32, 8, 16)])
 
 
