@@ -116,6 +116,33 @@ def test_plan_goes_on_from_its_own_state(rq):
         assert (p.positions.tolist(), p.slots.tolist(), t.tolist()) == (pos, slots, table)
 
 
+@pytest.mark.parametrize("batch,cap,new", [(1, 1025, 600), (7, 3000, 300), (700, 1400, 2), (4096, 1024, 0), (4097, 900, 0), (5000, 6000, 1)])
+@pytest.mark.parametrize("own", ["lens and taken", "lens", "taken"])
+def test_plan_in_place_by_one_launch_and_by_two(rq, batch, cap, new, own):
+    """More than 1024 tokens, or 4096 requests, in place: two steps, a refusal in between that changes nothing."""
+    g = gen(batch + cap)
+    page, width = 16, 80
+    total = batch * 4 + 200
+    free, table = torch.randperm(total, generator=g).tolist(), [[-1] * width for _ in range(batch)]
+    t, p, lens, taken = ints(table), rq.KvSlots(batch, cap), [0] * batch, 0
+    free_pages = ints(free)
+    for step in range(3):
+        add = torch.randint(0, new + 1, (batch,), generator=g).tolist()
+        if new == 0:
+            for b in torch.randint(0, batch, (40,), generator=g).tolist():
+                add[b] = 20
+        if step == 1:
+            add[batch // 2] = cap + 1
+        a = p.lens if "lens" in own else ints(lens)
+        b = None if "taken" in own else ints([taken])
+        rq.resq_kv_slots(a, ints(add), free_pages, b, t, page, total, out=p)
+        lens, cu, cp, positions, slots, table, state = plain.plan(lens, add, free, taken, table, page, total, cap)
+        assert state[1] == (3 if step == 1 else 0)
+        assert (p.state.tolist(), p.lens.tolist(), p.cu_tokens.tolist(), p.cu_pages.tolist()) == (state, lens, list(cu), list(cp))
+        assert (p.positions.tolist(), p.slots.tolist(), t.tolist()) == (list(positions), list(slots), [list(x) for x in table])
+        taken = state[0]
+
+
 def test_plan_on_another_stream(rq):
     # buffers that the call makes for itself are cleared before the plan is in them, whatever the current stream still does
     side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device=DEV)
@@ -478,6 +505,27 @@ def test_attend_many_sequences_without_tokens(rq, batch):
         assert torch.equal(out[at], want) and torch.equal(lse[at], want_lse)
         out[at], lse[at] = 0, -math.inf
         assert not out.any() and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("hq,hk,d,r", [(9, 1, 64, 8), (16, 1, 128, 16), (34, 2, 128, 16), (4, 1, 128, 16), (8, 2, 256, 32), (24, 2, 256, 256), (3, 3, 96, 12),
+                                       (12, 1, 128, 20), (6, 3, 128, 64)])
+@pytest.mark.parametrize("window,softcap", [(1, 20.0), (100, 0.0), (129, 5.0), (0, 30.0)])
+def test_attend_window_and_cap_of_other_heads(rq, hq, hk, d, r, window, softcap):
+    for page, order in ((16, "head"), (24, "token")):
+        check_attend(rq, *attend_case(window + d + hq, [0, 1, 33, 130, 700], hq, hk, d, r, page, order), r, softcap=softcap, window=window)
+
+
+@pytest.mark.parametrize("share", [1, 3, 8, 17])
+def test_attend_many_heads_and_many_parts(rq, share):
+    # 1024 heads and more, whose queries one workgroup each puts together, some from more parts than a thread reads at once
+    lens = torch.randint(0, 90, (300,), generator=gen(share)).tolist() + [20000]
+    check_attend(rq, *attend_case(share, lens, 4 * share, 4, 64, 8, 16), 8)
+
+
+@pytest.mark.parametrize("window", [0, 400000])
+def test_attend_runs_of_more_tiles_than_page_entries(rq, window):
+    # a workgroup's run of more than 4096 tokens of one head: its wavefronts look up pages a second time
+    check_attend(rq, *attend_case(3, [410000] * 8, 2, 1, 8, 0, 16), 0, window=window)
 
 
 def test_attend_scales(rq):
