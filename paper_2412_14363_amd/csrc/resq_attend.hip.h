@@ -15,8 +15,8 @@
 //   O (channels x queries) += V codes^T x P: the weights P go through LDS to where this product wants them, as two bf16
 //   numbers each, the nearest one and the one nearest to what it leaves: with up to 8 queries in the two halves of the columns,
 //   else in two products.  What both leave, at most 2^-17 of the weight, meets the middle of its operands (135.5, 127.5) in fp32 beside the
-//   zero-points, so that an output is off by at most 2^-17 of half its values' range: 256 x 512 tokens 55.5 us, with two truncations
-//   and nothing made of the rest 54.0 (a hundred times the error), with a third bf16 number, and a product more, 56.6 (no error)
+//   zero-points, so that an output is off by at most 2^-17 of half its values' range: 256 x 512 tokens 55.9 us, with two truncations
+//   and nothing made of the rest 54.9 (a hundred times the error), with a third bf16 number, and a product more, 56.8 (no error)
 // A 4-bit code becomes a bf16 number by being put under the leading bits of 16 (keys) or 128 (values): one shift and one
 // and-or for two codes.  The constants leave again with the zero-points, once per token; for values every second token has
 // the code's complement and the opposite sign, c + 128 and c - 143, so that the sums stay small.
@@ -25,12 +25,17 @@
 // The work is cut into units of 128 tokens of one head (four wavefronts, 32 tokens each); all units of the call in a row are
 // dealt to the workgroups in runs of equal cost, whatever the sequences' lengths are (they are read on the GPU).  A head
 // that ends up with several workgroups is joined by a second kernel from their maxima, sums and partial outputs.  (Joined by the
-// workgroup that is done last, a sequence of 131072 tokens took 68 us instead of 46: 64 parts read by one workgroup.)
+// workgroup that is done last, a sequence of 131072 tokens took half as long again: 64 parts read by one workgroup.)
 //
-// Bound: HBM, 2 row bytes per token and K/V head, where the runs are long: heads of 128 (r = 16), 8 for 32 queries, one sequence of
-// 131072 tokens 38.2 us, 4.8 TB/s, 48 ragged ones up to 8192 53 us, 5.0 TB/s (a plain read of 256 MiB reaches 5.4).  Short runs: the
-// way to the first tile (lengths, then pages, then rows, each a read of its own) and out again, about 5 us; one sequence of 777
-// tokens 7.8 us, 24 of 64-channel heads behind a window of 1500 18.
+// Times here and at the dispatch are of whole calls, both kernels, in a captured graph over three sets of inputs in turn (those of
+// more than some 90 MB come from HBM), medians; "N x T" is N sequences of T tokens, 8 K/V heads of 128 with 32 queries, r = 16 and pages
+// of 16 rows unless it says otherwise.
+// Bound where runs are long: HBM, 2 row bytes per token and K/V head, with the vector ALU (400 instructions a tile) close behind.  This
+// kernel alone, by a trace: 48 ragged sequences up to 8192 tokens 57 us, 4.6 TB/s, one of 131072 with 64 queries 41 us, 4.5 TB/s (a plain read
+// of as much 6.3).  Short runs: the way to the first tile (lengths, then pages, then rows, each a read of its own) and out again, about
+// 5 us of the 8.1 that one sequence of 777 tokens takes.  Few queries to a K/V head: the vector ALU, because a lane does the softmax
+// of four queries whether they are there or not (24 sequences, heads of 64 with one query each, window 1500: 566 instructions a
+// tile, some 10 us of 19.4).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -46,7 +51,8 @@ constexpr int kAttendWaves = kAttendThreads / 64;
 constexpr int kAttendMaxHead = 256;
 constexpr int kAttendTile = 32;                              // tokens of a wavefront's step
 constexpr int kAttendUnit = kAttendTile * kAttendWaves;      // tokens of a unit
-// what it costs to begin and to end a head, in units: 48 ragged sequences 73.7 us at 0, 54.6 at 2, 52.6 at 3, 52.7 at 4
+// what it costs to begin and to end a head, in units: 48 ragged sequences 80.1 us at 0, 63.8 at 2, 62.3 at 3, 62.1 at 4; behind a
+// window of 1500 24.1, 25.2, 22.8, 25.6; equal lengths lose by it: 32 x 4096 45.0 at 0, 46.9 at 3, 256 x 512 55.8 and 56.5
 constexpr int kAttendHeadCost = 3;
 constexpr int kAttendMaxGrid = 3 * 256;                      // workgroups: three to a compute unit at most
 constexpr int kAttendRows = 16;                              // queries of a workgroup at most
@@ -139,8 +145,8 @@ __device__ __forceinline__ uint4 piece_at(const uint8_t* p) {
 // A row comes to LDS in pieces of 16 bytes: its codes (the last of their pieces may hold a part of what follows them, or be
 // there in vain: codes of some kind, which meet zeros or are not written out), and the 16 bytes of its scales and zero-points.
 // The pitch of rows in LDS is a constant, so that every address is a lane's base and a constant, with the constants last, and
-// 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks (32 x 4096 tokens of 8 heads of 128: 53 us,
-// at a multiple of 32 68).
+// 16 more than a multiple of 32, so that 16 rows, and rows 4 apart, spread over all banks (32 x 4096: 47 us,
+// the same at 96 bytes in place of 112, 64.5 at 128).
 __host__ __device__ constexpr int attend_pieces(int NL, int HT) { return HT * 16 + NL * 8 < 256 ? (HT * 16 + NL * 8) / 16 + 1 : 17; }
 __host__ __device__ constexpr int attend_pitch(int NL, int HT) { return (attend_pieces(NL, HT) | 1) * 16; }
 __host__ __device__ constexpr int attend_tiles_bytes(int NL, int HT) {
@@ -188,8 +194,8 @@ __device__ __forceinline__ float halves_max(float x) {
 }
 // NL: 4-bit channels of a lane in the second product (16 NL channels in all), HT: 16-channel tiles of the 8-bit group,
 // Q: queries that fit, 8 or 16, BLOCKS: pages of a multiple of 16 rows, so that 16 tokens in a row from a multiple of 16 on are one
-// page's and two scalar offsets serve a tile instead of one per row (32 x 4096 tokens of 8 heads of 128 without an 8-bit group 42.9
-// us against 45.4, 256 in 8 bits 161 against 171, 256 x 512 tokens 57.8 against 60.7), OCC: workgroups to a compute unit
+// page's and two scalar offsets serve a tile instead of one per row (32 x 4096 without an 8-bit group 44.9
+// us against 46.9, 256 channels in 8 bits 132 against 175, 256 x 512 56.5 against 58.9), OCC: workgroups to a compute unit
 template <int NL, int HT, int Q, bool BLOCKS, int OCC>
 __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(const AttendArgs a) {
     constexpr int LS = NL / 2, HS = (HT + 1) / 2;   // steps of 32 channels of the first product
@@ -223,8 +229,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
     }
     total = __builtin_amdgcn_readfirstlane(total);
     // Workgroups go to the eight dies in turn; runs that follow one another, whose heads lie side by side in token-major pages (and
-    // whose queries share a K/V head's rows where they are more than 16), stay on one die and meet in its L2 (32 x 4096 tokens of
-    // token-major pages 54 us, dealt in turn 72).
+    // whose queries share a K/V head's rows where they are more than 16), stay on one die and meet in its L2 (32 x 4096 in
+    // token-major pages 57.0 us, dealt in turn 75.6).
     const int W = min(total, (int)gridDim.x), per_die = (W + 7) >> 3;
     const int w0 = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per_die || w0 >= W) return;
@@ -473,8 +479,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             __builtin_amdgcn_wave_barrier();
 
             // ---- what the tile's work reads of LDS, asked for at once; values' codes only where they leave registers for it (32 x
-            // 4096 tokens of 8 heads: 256 channels in 8 bits 128 us against 162, 32 of 256 78 against 84; where both groups are
-            // wide they do not fit: 64 of 256 323 against 112) and it changes something (64 of 128: 56.2 and 56.8) ----
+            // 4096: 256 channels in 8 bits 132 us against 162, 32 of 256 82.5 against 92.1, heads of 64 36.3 against 37.6, of 128 46.9
+            // and 47.1; where both groups are wide they do not fit: 64 of 256 351 against 119; 64 of 128 56.3 against 57.3, left) ----
             constexpr bool kEarly = HT <= 2 || (NL == 0 && HT == 16);
             uint2 kh[2][HS];
             uint32_t kl[2][LS ? LS : 1];
@@ -806,9 +812,9 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 //   m = max m_i, f_i = 2^(m_i - m), out = sum f_i acc_i / sum f_i l_i, lse = m ln 2 + ln sum f_i l_i
 // Few partial results, the usual case: four channels of a query to a thread, all its reads at once.  More: all threads to one
 // query after the other, in three barriers each.
-// Bound by the launch and two dependent reads: 2.6 us for 8 heads of 4 queries in 7 parts, 5.4 in 64 parts.  A workgroup to every
-// query always: 256 sequences of 512 tokens 58.5 us with the main kernel instead of 56; to every head always: one of 8192 tokens
-// 20.4 instead of 14.2 (64 parts).  512 threads instead of 256: 63 us for those 256 sequences.
+// Bound by the launch and two dependent reads: by a trace 3.8 us for 8 heads of 4 queries in 7 parts, 5.6 for 8 of 8 in 64.  A workgroup
+// to every query always: 256 x 512 59.5 us with the main kernel instead of 56.5; to every head always: 1 x 8192 22.1 instead of 15.1,
+// 1 x 131072 with 64 queries 68.5 instead of 49.0.  512 threads instead of 256: 256 x 512 an eighth more.
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a) {
     __shared__ float weight[kAttendMaxGrid], weight_sum[kAttendMaxGrid], part[2 * kAttendWaves];
     __shared__ float4 red[kAttendThreads];

@@ -123,8 +123,8 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
-    // as many workgroups as run at once, one run each: no head begins more often than that asks for (four times as many at OCC = 2: 47
-    // instead of 37 us for one sequence of 131072 tokens)
+    // as many workgroups as run at once, one run each: no head begins more often than that asks for (four times as many: 1 x 131072
+    // 67.1 us instead of 49.0, 256 x 512 58.6 instead of 56.5)
     const int64_t grid = units < 256 * OCC ? (units + 7) / 8 * 8 : 256 * OCC;   // a multiple of the dies
     launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
     const int64_t heads = (int64_t)a.B * a.heads_k * a.qtiles;
@@ -359,9 +359,10 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t low = d_head - r;
     // The smallest kernel that holds the head's two groups of channels, in as many workgroups to a compute unit as its registers allow
-    // without spilling in the loop.  32 x 4096 tokens of 8 heads, in us: the next larger kernel for 128 (r = 16) 56.3 instead of 53.2, 64 (8)
-    // 39.8 instead of 31.6, 256 (32) 99.7 instead of 83; a workgroup less 58.7 for 53.2, 34 for 31.6 (128, r = 32: 58 for 49); one more, with
-    // spills, 183 for 83 (256, r = 32), 330 for 161 (r = 256), 103 for 55 (128, r = 64).
+    // without spilling vector registers in the loop over tiles (<0, 16> in pages that are no multiple of 16 rows has one to four there; some
+    // others have up to 28 around it, once a head).  32 x 4096, in us: the next larger kernel for 128 (r = 16) 48.3 instead of 46.9, 64 (8)
+    // 43.7 instead of 36.3, 256 (32) 103.5 instead of 82.5; a workgroup less 54.7 for 46.9, 37.7 for 36.3 (128, r = 32: 62.4 for 51.1); one more,
+    // with spills, 310 for 82.5 (256, r = 32), 781 for 132.5 (r = 256), 57.2 for 57.3 (128, r = 64).
     if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
                                                                                    : launch_attend<0, 16, 1>(a, units, st);
     if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)

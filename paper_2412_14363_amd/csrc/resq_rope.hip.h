@@ -78,8 +78,9 @@ __device__ __forceinline__ void store_piece(uint16_t* p, int n, const uint4& v) 
 // workgroup are dealt to TB tokens (a power of two), each head group of which takes every so many heads of its token; the tokens'
 // cosines and sines are taken once per workgroup, into LDS and from there into registers.
 // ANY: rows whose pieces begin anywhere.  2048 tokens of 40 heads of 128, 54 channels turned, 14.0 us (a wavefront to a head, element by
-// element, 24.7), with all turned, the norm, and rows 130 apart 12.5 (32); whole pieces of the same size 8.0.
-// Bound by HBM from a few thousand rows on (4 bytes per channel: 8192 tokens of 40 heads of 128 26.5 us, 6.3 TB/s, part of it from
+// element, 24.7), with all turned, the norm, and rows 130 apart 12.5 (32); whole pieces of the same size 8.1 (in a captured graph,
+// on one set of inputs; on three sets in turn 9.0).
+// Bound by HBM from a few thousand rows on (4 bytes per channel: 8192 tokens of 40 heads of 128 26.3 us, 6.4 TB/s, part of it from
 // the caches), by the launch at a step's sizes (one token 2.6 us).
 template <int LG, bool ANY>
 __global__ __launch_bounds__(256) void rope_pieces_kernel(const RopeArgs a, int tb_log2, int heads_per_block) {

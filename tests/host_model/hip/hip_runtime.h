@@ -177,8 +177,10 @@ inline void launch(F f, dim3 grid, dim3 block, size_t lds_bytes) {
     for (uint32_t y = 0; y < grid.y; ++y)
         for (uint32_t x = 0; x < grid.x; ++x) {
             block_idx = dim3(x, y);
-            lds = lds_bytes ? static_cast<uint8_t*>(aligned_alloc(16, lds_bytes)) : nullptr;
-            if (lds) memset(lds, 0xFF, lds_bytes);
+            void* p = nullptr;
+            if (lds_bytes && posix_memalign(&p, 16, lds_bytes)) fail("no memory for LDS");
+            if (p) memset(p, 0xFF, lds_bytes);
+            lds = static_cast<uint8_t*>(p);
             run_block((int)block.x);
             free(lds);
         }

@@ -1,4 +1,4 @@
-"""The generation step's kernels in their own source on the CPU (host_model/): every lane of every wavefront, built with the sanitizers for
+"""The attention's entry point and kernels in their own source on the CPU (host_model/): every lane of every wavefront, built with the sanitizers for
 addresses, alignment and undefined behaviour, on arrays of exactly the size that a call needs.  An access outside of the pages,
 the block table, the lengths, the queries, the outputs, the workspace or LDS ends the run."""
 import os
