@@ -681,6 +681,37 @@ def test_buffers_that_a_call_makes_on_another_stream(rq):
                 assert len(got) == len(expected) and all(torch.equal(a, b) for a, b in zip(got, expected))
 
 
+def test_calls_without_tokens_on_another_stream(rq):
+    side, freq = torch.cuda.Stream(), rq.resq_rope_frequencies(64)[0]
+    none = torch.empty(0, 2, 64, dtype=torch.bfloat16, device=DEV)
+    pages = [torch.zeros(3, 2, 16, 52, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    assert rq.resq_rope_heads(none, ints([]), freq, stream=side).shape == (0, 2, 64)
+    assert rq.resq_gather_kv_cache(*pages, ints([]), 8, d_head=64, stream=side)[1].shape == (0, 2, 64)
+    assert rq.resq_attend_kv_cache(none, *pages, ints([]), torch.empty(0, 3, dtype=torch.int32, device=DEV), 8, stream=side).shape == (0, 2, 64)
+
+
+def test_buffers_that_a_captured_call_makes_on_another_stream(rq):
+    # a side stream that forks off the capture and comes back to it; replays with the program's own work and allocations between them
+    case = attend_case(19, [300, 10, 777], 16, 4, 128, 16, 32)
+    x, freq, positions = torch.randn(300, 6, 128, generator=gen(18)).to(torch.bfloat16).to(DEV), rq.resq_rope_frequencies(128)[0], ints(list(range(300)))
+    want = rq.resq_attend_kv_cache(*case, 16), rq.resq_rope_heads(x, positions, freq)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = rq.resq_attend_kv_cache(*case, 16, stream=side), rq.resq_rope_heads(x, positions, freq, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(4):
+        junk = [torch.full_like(t, 5) for t in got for _ in range(4)]
+        for t in got:
+            t.fill_(7)
+        graph.replay()
+        again = rq.resq_attend_kv_cache(*case, 16, stream=side), rq.resq_rope_heads(x, positions, freq, stream=side)
+        del junk
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got + again, want + want))
+
+
 def test_attend_graphs_share_a_workspace(rq):
     # two captured calls, one with rows of 16 KB in LDS per wavefront, replayed in turn with eager calls between them
     cases = [(attend_case(41, [900, 0, 33], 4, 2, 256, 256, 16), 256), (attend_case(42, [5000, 77], 16, 2, 128, 16, 24, "token"), 16)]
