@@ -579,6 +579,35 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
                          int64_t ldo, int64_t ldoh, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention over whole prompts: causal, sequences packed one after the other, on top of cached tokens or not.  Sequence b has
+ * the queries cu_q[b] .. cu_q[b + 1] - 1 and the keys cu_k[b] .. cu_k[b + 1] - 1; its queries are the last ones of its keys' tokens (nk keys, nq
+ * queries: query i stands at own = i + nk - nq).  For query head h, K/V head h / (heads_q / heads_k), over the keys j <= own:
+ *   x_j = scale * q . k_j;  softcap > 0: softcap * tanh(x_j / softcap);  window > 0: only the last `window` keys, j > own - window
+ *   out = sum_j e^(x_j - lse) v_j (rounded to bf16 once),  lse = ln sum_j e^(x_j)
+ * Weights go into the products rounded to bf16 (off by 2^-8 of each at most), sums are fp32.  Where a query sees no key (more queries than keys) out is 0
+ * and lse -inf.  What a query does not see has no part in its result, infinities and NaN neither.
+ *   q, out   bf16 [tokens_q, heads_q, d_head] with strides (ldq, ldqh), (ldo, ldoh); rows of out do not overlap; rows outside of the
+ *            sequences are left as they were                                             (read / written)
+ *   k, v     bf16 [tokens_k, heads_k, d_head] with strides (ldk, ldkh), (ldv, ldvh): views of a projection's output, or what
+ *            resq_gather_kv_cache wrote                                                  (read)
+ *   cu_q, cu_k  int32 [B + 1], not decreasing, from resq_kv_slots' cu_tokens; may be one array.  What is below 0 or above tokens_q
+ *            (tokens_k) is read as that; results of arrays that decrease are unspecified (no access leaves the tensors)  (read)
+ *   lse      fp32 [tokens_q, heads_q] or null                                            (written)
+ *   d_head   multiple of 8, 8 .. 256; heads_q a multiple of heads_k; 1 <= B <= 65535; tokens_q = 0 does nothing
+ *   scale, softcap, window   as resq_attend_kv_cache
+ *   tokens_q, tokens_k <= 2^30, tokens_q * heads_q < 2^31 - 65536
+ *   workspace  device memory, 256-byte aligned, resq_attend_prompts_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents
+ *            meaningless before and after; calls that overlap (different streams) need one each
+ * Alignment: k and v 16 bytes, their strides multiples of 8 (else RESQ_ERR_ALIGN); the others their elements'.
+ * How the keys of few queries are cut into parts depends on the sizes alone: equal calls give equal bits.
+ */
+size_t resq_attend_prompts_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head);
+int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens_q, const void* k, int64_t ldk, int64_t ldkh, const void* v,
+                        int64_t ldv, int64_t ldvh, int64_t tokens_k, const int32_t* cu_q, const int32_t* cu_k, int64_t B, int64_t heads_q,
+                        int64_t heads_k, int64_t d_head, float scale, float softcap, int64_t window, void* out, int64_t ldo, int64_t ldoh,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Online Hadamard projection of the down_proj input (Section 4.3, U_D):
  *   y[m, c0 + g*b + j] = (1/sqrt(b)) * sum_i x[m, c0 + g*b + i] * H_b[i, j]
  * for each block g of b columns in [col_begin, col_end), H_b the Sylvester

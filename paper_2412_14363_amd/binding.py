@@ -59,6 +59,9 @@ SYMBOLS = {
     "resq_attend_kv_cache_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
     "resq_attend_kv_cache": (C.c_int, [_p, _i64, _i64, _i64, _i64, _i64, _i64, _i64, _p, _p, _i64, _i64, _p, _p, _i64, _i64, _i64, _i64,
                                        _i64, C.c_float, C.c_float, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
+    "resq_attend_prompts_workspace_bytes": (_sz, [_i64] * 6),
+    "resq_attend_prompts": (C.c_int, [_p, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _i64, _i64, _i64, C.c_float,
+                                      C.c_float, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
     "resq_pack_weights": (C.c_int, [_p, _i64, _i64, _i64, _i64, _p, _sz, _p]),
     "resq_unpack_weights": (C.c_int, [_p, _i64, _i64, _i64, _p, _p, _p, _p, _p]),
     "resq_gemm_mixed": (C.c_int, [_p, _p, _p, _p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _p, _p, _p]),
@@ -881,6 +884,77 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
         softcap, window, out.data_ptr(), ldo, ldoh, sums, workspace.data_ptr(), workspace.numel(), _stream(stream))
     if st:
         _check(st, "resq_attend_kv_cache")
+    return out
+
+
+# ---- what stands around a layer's products: attention over whole prompts ---------------------------------------
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def resq_attend_prompts_workspace_bytes(tokens_q: int, tokens_k: int, batch: int, heads_q: int, heads_k: int, d_head: int) -> int:
+    return int(lib().resq_attend_prompts_workspace_bytes(tokens_q, tokens_k, batch, heads_q, heads_k, d_head))
+
+
+def resq_attend_prompts_workspace(tokens_q: int, tokens_k: int, batch: int, heads_q: int, heads_k: int, d_head: int,
+                                  device="cuda") -> torch.Tensor:
+    """A workspace for resq_attend_prompts calls of these sizes; calls on different streams need one each."""
+    nbytes = resq_attend_prompts_workspace_bytes(tokens_q, tokens_k, batch, heads_q, heads_k, d_head)
+    if nbytes == 0:
+        raise ValueError(f"invalid (tokens_q, tokens_k, batch, heads_q, heads_k, d_head) = "
+                         f"({tokens_q}, {tokens_k}, {batch}, {heads_q}, {heads_k}, {d_head})")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def resq_attend_prompts(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
+                        scale: Optional[float] = None, softcap: float = 0.0, window: int = 0, out: Optional[torch.Tensor] = None,
+                        lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Causal attention of packed sequences, q: bf16 [tokens, heads, d_head], k, v: bf16 [keys, K/V heads, d_head]; cu_q, cu_k (None: cu_q):
+    int32 [batch + 1], where each sequence's queries and keys begin; its queries are its last tokens.  scale: d_head^-0.5 when None.
+    lse: fp32 [tokens, heads], written where given.  Rows of out outside of the sequences stay as they are."""
+    tokens, heads, d = shape = q.shape
+    if out is None:
+        out = _empty(shape, _BF16, q.device, stream)
+    if cu_k is None:
+        cu_k = cu_q
+    keys, heads_k, _ = k.shape if k.dim() == 3 else (0, 0, 0)
+    batch = cu_q.shape[0] - 1 if cu_q.dim() == 1 else 0
+    if workspace is None:
+        nbytes = resq_attend_prompts_workspace_bytes(tokens, keys, batch, heads, heads_k, d)
+        workspace = _made(lambda: torch.empty(max(nbytes, 1), dtype=_U8, device=q.device), stream, q.device, handed_out=False)
+    dev = q.get_device()
+    ldq, ldqh, one = q.stride()
+    ldk, ldkh, one_k = k.stride() if k.dim() == 3 else (0, 0, 0)
+    ldv, ldvh, one_v = v.stride() if v.dim() == 3 else (0, 0, 0)
+    ldo, ldoh, one_o = out.stride() if out.dim() == 3 else (0, 0, 0)
+    sums = None
+    ok = (q.dtype == _BF16 and k.dtype == _BF16 and v.dtype == _BF16 and out.dtype == _BF16 and cu_q.dtype == _I32 and cu_k.dtype == _I32
+          and workspace.dtype == _U8 and one == 1 and one_k == 1 and one_v == 1 and one_o == 1 and out.shape == shape and v.shape == k.shape
+          and k.shape[2] == d and heads_k > 0 and heads % heads_k == 0 and batch > 0 and cu_k.shape == cu_q.shape and cu_q.is_contiguous()
+          and cu_k.is_contiguous() and workspace.is_contiguous() and dev >= 0 and dev == _raw_device() and k.get_device() == dev
+          and v.get_device() == dev and out.get_device() == dev and cu_q.get_device() == dev and cu_k.get_device() == dev
+          and workspace.get_device() == dev)
+    if lse is not None and ok:
+        ok = lse.dtype == torch.float32 and lse.shape == (tokens, heads) and lse.is_contiguous() and lse.get_device() == dev
+        sums = lse.data_ptr()
+    if not ok:
+        where = "resq_attend_prompts"
+        for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+            _explain_heads(where, name, t)
+        _need(out.shape == shape and v.shape == k.shape and k.shape[2] == d and heads_k > 0 and heads % heads_k == 0, where,
+              f"q {tuple(shape)}, k {tuple(k.shape)}, v {tuple(v.shape)} and out {tuple(out.shape)} do not match")
+        _need(lse is None or (lse.dtype == torch.float32 and lse.shape == (tokens, heads) and lse.is_contiguous()), where,
+              f"lse must be a contiguous fp32 [{tokens}, {heads}] tensor")
+        _need(workspace.dtype == _U8 and workspace.is_contiguous(), where, "workspace must be a contiguous uint8 tensor")
+        _explain_ints(where, "cu_q", cu_q)
+        _explain_ints(where, "cu_k", cu_k, batch + 1)
+        _need(batch > 0, where, "cu_q must have two entries at least")
+        _explain_devices(where, q, k, v, cu_q, cu_k, out, lse, workspace)
+        raise ValueError(f"{where}: invalid arguments")
+    st = lib().resq_attend_prompts(
+        q.data_ptr(), ldq, ldqh, tokens, k.data_ptr(), ldk, ldkh, v.data_ptr(), ldv, ldvh, keys, cu_q.data_ptr(), cu_k.data_ptr(), batch, heads,
+        heads_k, d, d ** -0.5 if scale is None else scale, softcap, window, out.data_ptr(), ldo, ldoh, sums, workspace.data_ptr(),
+        workspace.numel(), _stream(stream))
+    if st:
+        _check(st, "resq_attend_prompts")
     return out
 
 

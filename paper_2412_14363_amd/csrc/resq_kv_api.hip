@@ -18,12 +18,6 @@ namespace {
 constexpr int64_t kInt32Max = 0x7FFFFFFF;
 constexpr int64_t kMaxAttendLen = 1 << 30;
 
-// rows of `width` elements, ld from one to the next of n and ldh from one to the next of heads, that do not overlap
-inline bool rows_apart(int64_t n, int64_t ld, int64_t heads, int64_t ldh, int64_t width) {
-    if ((n > 1 && ld < width) || (heads > 1 && ldh < width)) return false;
-    return n <= 1 || heads <= 1 || ld >= (heads - 1) * ldh + width || ldh >= (n - 1) * ld + width;
-}
-
 // a head's row in pages: as everywhere, or with an 8-bit group of an odd multiple of four channels, at even addresses then
 inline bool page_head_ok(int64_t d_head, int64_t r) {
     return kv_head_ok(d_head, r) || (kv_head_ok(d_head, r - 4) && r < d_head && d_head <= 256);

@@ -27,6 +27,12 @@ inline void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t lds, 
 // a launch counts the threads along an axis in 32 bits
 inline bool launch_fits(int64_t blocks, int64_t threads) { return blocks <= 0xFFFFFFFFll / threads; }
 
+// rows of `width` elements, ld from one to the next of n and ldh from one to the next of heads, that do not overlap
+inline bool rows_apart(int64_t n, int64_t ld, int64_t heads, int64_t ldh, int64_t width) {
+    if ((n > 1 && ld < width) || (heads > 1 && ldh < width)) return false;
+    return n <= 1 || heads <= 1 || ld >= (heads - 1) * ldh + width || ldh >= (n - 1) * ld + width;
+}
+
 // a head's row of the compact K/V cache: d_head and the width r of its 8-bit group
 inline bool kv_head_ok(int64_t d_head, int64_t r) {
     return d_head >= 8 && d_head <= 512 && d_head % 8 == 0 && r >= 0 && r <= d_head && r % 8 == 0;

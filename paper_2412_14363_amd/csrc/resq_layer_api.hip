@@ -1,0 +1,128 @@
+// C ABI of what stands around a layer's products beside the generation step: attention over whole prompts.
+// Argument checks on the host, then launches on the caller's stream.  See include/resq.h for the contract of every entry.
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "resq.h"
+#include "resq_launch.h"
+#include "resq_prompts.hip.h"
+
+using namespace resq;
+
+namespace {
+
+constexpr int64_t kInt32Max = 0x7FFFFFFF;
+constexpr int64_t kMaxTokens = 1 << 30;   // so that a place minus a window stays in 32 bits
+constexpr int kMaxHead = 256;
+
+// sizes that both entries of the prompts' attention check, and what they have in common
+struct PromptPlan {
+    int64_t tiles;       // of 128 rows, at most
+    int keys, parts, least;
+    size_t acc, bytes;   // workspace: maxima and sums, weighted sums behind them
+};
+bool prompt_plan(PromptPlan& p, int64_t tokens_q, int64_t tokens_k, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d) {
+    if (tokens_q < 0 || tokens_q > kMaxTokens || tokens_k < 0 || tokens_k > kMaxTokens || B < 1 || B > 65535 || heads_q < 1 || heads_q > 65535 ||
+        heads_k < 1 || heads_q % heads_k || d < 8 || d > kMaxHead || d % 8)
+        return false;
+    const int64_t share = heads_q / heads_k;
+    if (tokens_q * heads_q > kInt32Max - 65536) return false;   // rows are counted in 32 bits
+    p.tiles = (tokens_q * share + B * (kPromptRows - 1)) / kPromptRows;
+    p.keys = d <= 128 ? 64 : 32;
+    p.least = 512 / p.keys;
+    const int64_t units = p.tiles * heads_k;
+    int64_t parts = units >= 512 || units == 0 ? 1 : (1024 + units - 1) / units;
+    const int64_t most = (tokens_k / p.keys + p.least) / p.least;
+    if (parts > most) parts = most;
+    p.parts = (int)(parts > 64 ? 64 : parts);
+    if (!launch_fits(units * p.parts, kPromptThreads) || units * p.parts > kInt32Max) return false;
+    const size_t slots = p.parts > 1 ? (size_t)units * p.parts : 0;
+    p.acc = slots * kPromptRows * 2 * sizeof(float);
+    p.bytes = p.acc + slots * kPromptRows * d * sizeof(float);
+    if (p.bytes == 0) p.bytes = 256;
+    return true;
+}
+
+template <int W, int KEYS, int OCC>
+int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
+    const int lds = 4 * KEYS * FlashTile<W>::kPitch;
+    const auto kernel = attend_prompts_kernel<W, KEYS, OCC>;
+    if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               lds) != hipSuccess)
+        return RESQ_ERR_HIP;
+    launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(kPromptThreads), (size_t)lds, st, a);
+    if (p.parts > 1)
+        launch(attend_prompts_join_kernel<KEYS>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(kPromptThreads), 0, st, a);
+    return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t resq_attend_prompts_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head) {
+    PromptPlan p;
+    return prompt_plan(p, tokens_q, tokens_k, B, heads_q, heads_k, d_head) ? p.bytes : 0;
+}
+
+int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens_q, const void* k, int64_t ldk, int64_t ldkh, const void* v,
+                        int64_t ldv, int64_t ldvh, int64_t tokens_k, const int32_t* cu_q, const int32_t* cu_k, int64_t B, int64_t heads_q,
+                        int64_t heads_k, int64_t d_head, float scale, float softcap, int64_t window, void* out, int64_t ldo, int64_t ldoh,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    PromptPlan p;
+    if (!prompt_plan(p, tokens_q, tokens_k, B, heads_q, heads_k, d_head) || ldq < 0 || ldqh < 0 || ldk < 0 || ldkh < 0 || ldv < 0 ||
+        ldvh < 0 || !(scale > 0.0f) || !isfinite(scale) || !(softcap == 0.0f || softcap >= FLT_MIN) || !isfinite(softcap) || window < 0 ||
+        !rows_apart(tokens_q, ldo, heads_q, ldoh, d_head))
+        return RESQ_ERR_SHAPE;
+    if (tokens_q == 0) return RESQ_OK;
+    if (!q || (tokens_k > 0 && (!k || !v)) || !cu_q || !cu_k || !out || !workspace) return RESQ_ERR_NULL;
+    if (tokens_q == 1) ldq = ldo = 0;
+    if (tokens_k == 1) ldk = ldv = 0;
+    if (heads_q == 1) ldqh = ldoh = 0;
+    if (heads_k == 1) ldkh = ldvh = 0;
+    if (out == q && (ldq != ldo || ldqh != ldoh)) return RESQ_ERR_SHAPE;
+    if (!aligned(q, 2) || !aligned(out, 2) || !aligned(k, 16) || !aligned(v, 16) || ldk % 8 || ldkh % 8 || ldv % 8 || ldvh % 8 ||
+        !aligned(cu_q, 4) || !aligned(cu_k, 4) || !aligned(lse, 4) || !aligned(workspace, 256))
+        return RESQ_ERR_ALIGN;
+    if (workspace_bytes < p.bytes) return RESQ_ERR_BUFFER;
+    PromptArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.ldq = ldq;
+    a.ldqh = ldqh;
+    a.ldk = ldk;
+    a.ldkh = ldkh;
+    a.ldv = ldv;
+    a.ldvh = ldvh;
+    a.cu_q = cu_q;
+    a.cu_k = cu_k;
+    a.B = (int)B;
+    a.tokens_q = (int)tokens_q;
+    a.tokens_k = (int)tokens_k;
+    a.heads_k = (int)heads_k;
+    a.d = (int)d_head;
+    a.share = FastDiv((uint32_t)(heads_q / heads_k));
+    a.heads = FastDiv((uint32_t)heads_k);
+    a.parts = FastDiv((uint32_t)p.parts);
+    a.scale = scale;
+    a.softcap = softcap;
+    a.window = window > 0 && window < kMaxTokens ? (int)window : (int)kMaxTokens;
+    a.least = p.least;
+    a.out = static_cast<uint16_t*>(out);
+    a.ldo = ldo;
+    a.ldoh = ldoh;
+    a.lse = lse;
+    a.part_ml = static_cast<float*>(workspace);
+    a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + p.acc);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (d_head <= 64) return launch_prompts<64, 64, 2>(a, p, st);
+    if (d_head <= 96) return launch_prompts<96, 64, 2>(a, p, st);
+    if (d_head <= 128) return launch_prompts<128, 64, 2>(a, p, st);
+    if (d_head <= 192) return launch_prompts<192, 32, 1>(a, p, st);
+    return launch_prompts<256, 32, 1>(a, p, st);
+}
+
+}  // extern "C"

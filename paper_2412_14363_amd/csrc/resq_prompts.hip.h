@@ -1,0 +1,374 @@
+// Attention over whole prompts: causal, sequences packed one after the other, grouped heads, on top of cached tokens or not.
+//   x_ij = scale * q_i . k_j, capped to cap * tanh(x / cap) where there is a cap
+//   out_i = sum_j e^(x_ij - lse_i) v_j, lse_i = ln sum_j e^(x_ij)
+// over the keys j of the sequence with own(i) - window < j <= own(i), own(i) = i + nk - nq a query's own place among its sequence's keys.
+//
+// A workgroup has 128 rows, 32 to a wavefront (resq_flash.hip.h); a row is a query and one of the heads that share a K/V head, so that
+// a tile of keys and values in LDS serves all of them, and tiles on the diagonal are few (with four heads to a K/V head 128 rows are
+// 32 queries).  Keys and values come to LDS in tiles of 64 by way of registers, a tile ahead.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "resq_flash.hip.h"
+
+namespace resq {
+
+constexpr int kPromptThreads = 256;
+constexpr int kPromptWaves = kPromptThreads / 64;
+constexpr int kPromptRows = kFlashRows * kPromptWaves;   // of a workgroup
+
+struct PromptArgs {
+    const uint16_t *q, *k, *v;
+    int64_t ldq, ldqh, ldk, ldkh, ldv, ldvh;
+    const int32_t *cu_q, *cu_k;
+    int B, tokens_q, tokens_k, heads_k, d;
+    FastDiv share;       // query heads to a K/V head
+    FastDiv heads, parts;
+    float scale, softcap;
+    int window;          // 2^30: none
+    int least;           // tiles of keys of a part at least
+    uint16_t* out;
+    int64_t ldo, ldoh;
+    float* lse;
+    float* part_ml;      // [tile, head, part][128][2]: maximum (times log2 e) and sum (workspace)
+    float* part_acc;     // [tile, head, part][128][d]: weighted sums (workspace)
+};
+
+// A workgroup's rows: tile `tile` of a sequence's.
+struct PromptTile {
+    int q0, nq, k0, nk;  // the sequence's first query and key, and how many there are
+    int row0, rows;      // the first row of the tile among the sequence's (queries x share), and the sequence's rows
+};
+
+// The tile with the number `at` among all sequences' tiles, counted from the last one (later rows see more keys: the longest work
+// comes first).  False where there are not so many.
+__device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int at, PromptTile& tile) {
+    __shared__ int part[kPromptWaves], found[5];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    auto first = [&](const int32_t* cu, int b, int most) { return min(max(cu[b], 0), most); };
+    auto tiles = [&](int b) {
+        const int q0 = first(a.cu_q, b, a.tokens_q), q1 = first(a.cu_q, b + 1, a.tokens_q);
+        return (int)(((int64_t)max(q1 - q0, 0) * a.share.d + kPromptRows - 1) / kPromptRows);
+    };
+    const int per = (a.B + kPromptThreads - 1) / kPromptThreads;
+    const int b0 = min(t * per, a.B), b1 = min(b0 + per, a.B);
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) mine += tiles(b);
+    const int upto = wave_scan(mine);
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    int total = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < kPromptWaves; ++w) {
+        if (w == wave) before = total;
+        total += part[w];
+    }
+    if (at >= total) return false;
+    at = total - 1 - at;
+    int start = before + upto - mine;
+    if (start <= at && at < start + mine) {
+        for (int b = b0; b < b1; ++b) {
+            const int n = tiles(b);
+            if (at < start + n) {
+                found[0] = first(a.cu_q, b, a.tokens_q);
+                found[1] = first(a.cu_q, b + 1, a.tokens_q);
+                found[2] = first(a.cu_k, b, a.tokens_k);
+                found[3] = first(a.cu_k, b + 1, a.tokens_k);
+                found[4] = at - start;
+                break;
+            }
+            start += n;
+        }
+    }
+    __syncthreads();
+    tile.q0 = __builtin_amdgcn_readfirstlane(found[0]);
+    tile.nq = __builtin_amdgcn_readfirstlane(found[1]) - tile.q0;
+    tile.k0 = __builtin_amdgcn_readfirstlane(found[2]);
+    tile.nk = max(__builtin_amdgcn_readfirstlane(found[3]) - tile.k0, 0);
+    tile.row0 = __builtin_amdgcn_readfirstlane(found[4]) * kPromptRows;
+    tile.rows = tile.nq * (int)a.share.d;
+    return true;
+}
+
+// Keys that a tile's rows see, [begin, end) with begin a multiple of a tile of keys, cut into parts of so many tiles.
+struct PromptKeys {
+    int begin, end, per, parts;
+};
+template <int KEYS>
+__device__ __forceinline__ PromptKeys prompt_keys(const PromptArgs& a, const PromptTile& t) {
+    PromptKeys k;
+    const int last = min(t.row0 + kPromptRows, t.rows) - 1, shift = t.nk - t.nq;
+    const int own0 = (int)a.share(t.row0) + shift, own1 = (int)a.share(last) + shift;
+    k.end = max(own1 + 1, 0);   // at most nk
+    k.begin = min(max(own0 - (a.window - 1), 0), k.end) / KEYS * KEYS;
+    const int tiles = (k.end - k.begin + KEYS - 1) / KEYS;
+    const int parts = min((int)a.parts.d, max(tiles / a.least, 1));
+    k.per = (tiles + parts - 1) / parts;
+    k.parts = k.per ? (tiles + k.per - 1) / k.per : 1;
+    return k;
+}
+
+template <int W, int KEYS, int OCC>
+__global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(const PromptArgs a) {
+    using Tile = FlashTile<W>;
+    constexpr int kTileBytes = KEYS * Tile::kPitch;
+    constexpr int kMoves = kTileBytes / 16 / kPromptThreads;   // pieces of a tile's keys (values) that a thread moves
+    constexpr int kRowsAMove = kPromptThreads / Tile::kPieces;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values
+
+    const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    // heads are neighbours in the grid: with 8 of them (or a multiple) each die has a head's keys and values in its own L2
+    const int unit = (int)a.heads(blockIdx.x), hk = (int)blockIdx.x - unit * (int)a.heads.d;
+    const int order = (int)a.parts(unit), piece = unit - order * (int)a.parts.d;
+    PromptTile tile;
+    if (!prompt_tile(a, order, tile)) return;
+    const PromptKeys keys = prompt_keys<KEYS>(a, tile);
+    if (piece >= keys.parts) return;
+    const int begin = keys.begin + piece * keys.per * KEYS, end = min(keys.end, begin + keys.per * KEYS);
+
+    // ---- the own row ----
+    const int row = tile.row0 + wave * kFlashRows + (lane & 31);
+    const bool live = row < tile.rows;
+    const int token = (int)a.share(live ? row : 0), head = hk * (int)a.share.d + (live ? row : 0) - token * (int)a.share.d;
+    const int own = live ? token + tile.nk - tile.nq : -1;   // a row that is not there sees nothing
+    FlashRow<W, false> r;
+    {
+        const uint16_t* src = a.q + (tile.q0 + token) * a.ldq + head * a.ldqh;
+#pragma unroll
+        for (int s = 0; s < Tile::kSteps; ++s) {
+            const int ch = 16 * s + 8 * half;
+            Piece16 p{0u, 0u, 0u, 0u};
+            if (live && ch < a.d) p = *reinterpret_cast<const Piece16*>(src + ch);
+            r.q[s] = (v4u_flash){p.x, p.y, p.z, p.w};
+        }
+    }
+    r.clear();
+    // what the wavefront's rows see: all of them [all0, all1), some of them [some0, some1)
+    const int row0 = tile.row0 + wave * kFlashRows, row1 = min(row0 + kFlashRows, tile.rows) - 1;
+    const int shift = tile.nk - tile.nq;
+    const int own0 = (int)a.share(min(row0, tile.rows - 1)) + shift, own1 = (int)a.share(max(row1, 0)) + shift;
+    const bool any = row0 < tile.rows;
+    const int all0 = max(own1 - (a.window - 1), 0), all1 = own0 + 1;
+    const int some0 = max(own0 - (a.window - 1), 0), some1 = any ? own1 + 1 : 0;
+
+    // ---- tiles of keys and values, by way of registers ----
+    const int my_row = t / Tile::kPieces, my_piece = min(t % Tile::kPieces, (a.d >> 3) - 1);   // (channels behind the head's: any)
+    const uint16_t* k_src = a.k + tile.k0 * a.ldk + hk * a.ldkh + 8 * my_piece;
+    const uint16_t* v_src = a.v + tile.k0 * a.ldv + hk * a.ldvh + 8 * my_piece;
+    uint4 kreg[kMoves], vreg[kMoves];
+    auto load = [&](int key0) {
+#pragma unroll
+        for (int i = 0; i < kMoves; ++i) {
+            const int64_t j = min(key0 + my_row + i * kRowsAMove, end - 1);   // (keys behind the last: any that is there)
+            kreg[i] = *reinterpret_cast<const uint4*>(k_src + j * a.ldk);
+            vreg[i] = *reinterpret_cast<const uint4*>(v_src + j * a.ldv);
+        }
+    };
+    auto store = [&](int buffer) {
+        uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < kMoves; ++i) {
+            const int to = my_row + i * kRowsAMove;
+            *reinterpret_cast<uint4*>(kt + Tile::key_at(to, t % Tile::kPieces)) = kreg[i];
+            *reinterpret_cast<uint4*>(vt + Tile::value_at(to, t % Tile::kPieces)) = vreg[i];
+        }
+    };
+    const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
+    const float kLog2e = 1.44269504088896340736f;
+    const float sc2 = a.softcap > 0.0f ? kLog2e : a.scale * kLog2e;
+    const float inf = __builtin_huge_valf();
+
+    if (begin < end) {
+        load(begin);
+        store(0);
+        if (begin + KEYS < end) load(begin + KEYS);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int key0 = begin; key0 < end; key0 += KEYS, buffer ^= 1) {
+        if (key0 + KEYS < end) {
+            store(buffer ^ 1);
+            if (key0 + 2 * KEYS < end) load(key0 + 2 * KEYS);
+        }
+        if (key0 < some1 && key0 + KEYS > some0) {
+            const uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
+            const bool partly = key0 < all0 || key0 + KEYS > all1;
+            v16f_flash x[KEYS / 32];
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb) x[kb] = r.scores(kt, kb);
+            if (a.softcap > 0.0f) {
+#pragma unroll
+                for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[kb][i] = soft_cap(x[kb][i] * a.scale, a.softcap, inv_cap);
+            }
+            const int behind = own - key0 - 4 * half;   // keys from the lane's first one to the row's own
+            auto sees = [&](int kb, int i) {
+                return (unsigned)(behind - (32 * kb + 8 * (i >> 2) + (i & 3))) < (unsigned)a.window && behind >= 32 * kb + 8 * (i >> 2) + (i & 3);
+            };
+            if (partly) {
+#pragma unroll
+                for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[kb][i] = sees(kb, i) ? x[kb][i] : -inf;
+            }
+            // ---- the running maximum ----
+            float top = x[0][0];
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+            const float m_new = fmaxf(r.m, halves_max(top) * sc2);
+            const float back = __builtin_amdgcn_exp2f(r.m - m_new);
+            r.m = m_new;
+            r.l *= back;
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) r.acc[c] *= back;
+            // ---- weights, rounded once to bf16 as the product's operand (off by 2^-8 of each at most; their sum is taken unrounded) ----
+            v4u_flash p[KEYS / 16];
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(x[kb][i], sc2, -m_new)), p1 = __builtin_amdgcn_exp2f(fmaf(x[kb][i + 1], sc2, -m_new));
+                    r.l += p0 + p1;
+                    p[2 * kb + (i >> 3)][(i & 7) >> 1] = flash_pack<false>(p0, p1);
+                }
+            // ---- weighted sums of values ----
+            // A key that some row of the wavefront does not see has weight 0 there, which an infinity or NaN among its values would
+            // not care about: such values are left out of the product, and what they make of a row that sees them is added apart.
+            bool odd = false;
+            if (partly) {
+                uint32_t found = 0;
+#pragma unroll
+                for (int s = 0; s < KEYS / 16; ++s)
+#pragma unroll
+                    for (int c = 0; c < Tile::kBlocks; ++c) {
+                        const v4u_flash o = r.values(vt, s, c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) found |= ((o[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+                    }
+                odd = __builtin_amdgcn_ballot_w64(found != 0) != 0;
+            }
+            if (!odd) {
+#pragma unroll
+                for (int s = 0; s < KEYS / 16; ++s)
+#pragma unroll
+                    for (int c = 0; c < Tile::kBlocks; ++c) r.acc[c] = flash_mfma<false>(r.values(vt, s, c), p[s], r.acc[c]);
+            } else {
+                v4u_flash one[KEYS / 16];   // 1 where the row sees the key
+#pragma unroll
+                for (int s = 0; s < KEYS / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = 8 * (s & 1) + 2 * e;
+                        one[s][e] = (sees(s >> 1, i) ? 0x3F80u : 0u) | (sees(s >> 1, i + 1) ? 0x3F800000u : 0u);
+                    }
+                // kind 0: finite values, with their weights; 1, 2, 3: infinities, negative ones, NaN, counted
+#pragma unroll 1
+                for (int kind = 0; kind < 4; ++kind) {
+#pragma unroll
+                    for (int c = 0; c < Tile::kBlocks; ++c) {
+                        v16f_flash sum;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[i] = kind == 0 ? r.acc[c][i] : 0.0f;
+#pragma unroll
+                        for (int s = 0; s < KEYS / 16; ++s) {
+                            v4u_flash o = r.values(vt, s, c), w;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                uint32_t two = 0;
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const uint32_t u = o[e] >> (16 * k) & 0xFFFFu, mag = u & 0x7FFFu;
+                                    const int is = mag < 0x7F80u ? 0 : mag > 0x7F80u ? 3 : u >> 15 ? 2 : 1;
+                                    two |= (is != kind ? 0u : kind == 0 ? u : 0x3F80u) << (16 * k);
+                                }
+                                o[e] = two;
+                                w[e] = kind == 0 ? p[s][e] : one[s][e];
+                            }
+                            sum = flash_mfma<false>(o, w, sum);
+                        }
+                        const float what = kind == 1 ? inf : kind == 2 ? -inf : __builtin_nanf("");
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) r.acc[c][i] = kind == 0 ? sum[i] : sum[i] > 0.0f ? r.acc[c][i] + what : r.acc[c][i];
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    // ---- the result, or this part of it ----
+    const float sum = halves_sum(r.l);
+    if (!live) return;
+    if (keys.parts == 1) {
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        uint16_t* dst = a.out + (tile.q0 + token) * a.ldo + head * a.ldoh;
+#pragma unroll
+        for (int c = 0; c < Tile::kBlocks; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int ch = 32 * c + 8 * (i >> 2) + 4 * half;
+                if (ch < a.d)
+                    *reinterpret_cast<Piece8*>(dst + ch) = Piece8{pack_bf16_pair(r.acc[c][i] * f, r.acc[c][i + 1] * f),
+                                                                  pack_bf16_pair(r.acc[c][i + 2] * f, r.acc[c][i + 3] * f)};
+            }
+        if (a.lse && half == 0)
+            a.lse[(int64_t)(tile.q0 + token) * (a.heads.d * a.share.d) + head] = sum == 0.0f ? -inf : r.m * 0.69314718055994530942f + logf(sum);
+        return;
+    }
+    const int64_t slot = ((int64_t)order * a.heads.d + hk) * a.parts.d + piece;
+    const int at = wave * kFlashRows + (lane & 31);
+    float* dst = a.part_acc + (slot * kPromptRows + at) * a.d;
+#pragma unroll
+    for (int c = 0; c < Tile::kBlocks; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int ch = 32 * c + 8 * (i >> 2) + 4 * half;
+            if (ch < a.d) *reinterpret_cast<float4*>(dst + ch) = make_float4(r.acc[c][i], r.acc[c][i + 1], r.acc[c][i + 2], r.acc[c][i + 3]);
+        }
+    if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * kPromptRows + at) * 2) = make_float2(r.m, sum);
+}
+
+// Joins the parts of tiles that have several: m = max m_i, f_i = 2^(m_i - m), out = sum f_i acc_i / sum f_i l_i, lse = m ln 2 + ln sum f_i l_i
+template <int KEYS>
+__global__ __launch_bounds__(kPromptThreads) void attend_prompts_join_kernel(const PromptArgs a) {
+    const int order = (int)a.heads(blockIdx.x), hk = (int)blockIdx.x - order * (int)a.heads.d;
+    PromptTile tile;
+    if (!prompt_tile(a, order, tile)) return;
+    const PromptKeys keys = prompt_keys<KEYS>(a, tile);
+    if (keys.parts == 1) return;
+    const int fours = a.d >> 2, rows = min(kPromptRows, tile.rows - tile.row0);
+    const int64_t slot = ((int64_t)order * a.heads.d + hk) * a.parts.d;
+    for (int e = threadIdx.x + blockIdx.y * kPromptThreads; e < rows * fours; e += kPromptThreads * gridDim.y) {
+        const int row = e / fours, ch = 4 * (e - row * fours);
+        const float* ml = a.part_ml + (slot * kPromptRows + row) * 2;
+        const float* acc = a.part_acc + (slot * kPromptRows + row) * a.d + ch;
+        float top = kFlashNone, sum = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = 0; i < keys.parts; ++i) top = fmaxf(top, ml[(int64_t)i * kPromptRows * 2]);
+        for (int i = 0; i < keys.parts; ++i) {
+            const float2 part = *reinterpret_cast<const float2*>(ml + (int64_t)i * kPromptRows * 2);
+            const float4 v = *reinterpret_cast<const float4*>(acc + (int64_t)i * kPromptRows * a.d);
+            const float f = __builtin_amdgcn_exp2f(part.x - top);
+            if (f == 0.0f && part.y == part.y) continue;   // a part whose keys the row does not see, or that weigh nothing
+            sum = fmaf(f, part.y, sum);
+            o.x = fmaf(f, v.x, o.x);
+            o.y = fmaf(f, v.y, o.y);
+            o.z = fmaf(f, v.z, o.z);
+            o.w = fmaf(f, v.w, o.w);
+        }
+        const int r = tile.row0 + row, token = (int)a.share(r), head = hk * (int)a.share.d + r - token * (int)a.share.d;
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<Piece8*>(a.out + (tile.q0 + token) * a.ldo + head * a.ldoh + ch) =
+            Piece8{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
+        if (ch == 0 && a.lse)
+            a.lse[(int64_t)(tile.q0 + token) * (a.heads.d * a.share.d) + head] =
+                sum == 0.0f ? -__builtin_huge_valf() : top * 0.69314718055994530942f + logf(sum);
+    }
+}
+
+}  // namespace resq

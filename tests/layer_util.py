@@ -1,0 +1,65 @@
+"""Plain 64-bit implementations of the operators around a layer's products, for their tests: from the definitions in include/resq.h, in torch
+on the CPU, sharing nothing with the library."""
+import math
+
+import torch
+
+
+def rows(q, k, v, first, last, scale, cap, weight_step):
+    """One head: queries [n, d] over keys first[i] <= j < last[i] -> (out [n, d], lse [n], bound of the kernel's error before its last
+    rounding, bound of lse's), all in 64 bits.
+
+    The bounds.  A score is a sum of d products, each exact in fp32, of at most d roundings of 2^-24 of its terms' magnitudes; its
+    product with the scale, its difference from the maximum and the exponential's argument are three more, of the score and the
+    maximum; tanh moves it by 2^-22 of the cap.  A weight is off by twice what its score is (its own and the sum's), by its rounding
+    as an operand (weight_step, half a step of that type) and by 2^-21 for the exponential and the quotient.  The weighted sum has at
+    most as many roundings of 2^-24 as there are keys."""
+    x = scale * (q @ k.T)
+    size = scale * (q.abs() @ k.abs().T)
+    t = torch.arange(len(k))
+    seen = (t >= first[:, None]) & (t < last[:, None])
+    some = seen.any(1)
+    off = torch.where(seen, q.shape[1] * 2.0 ** -24 * size + 2.0 ** -22 * x.abs(), 0.0)
+    if cap:
+        x = cap * torch.tanh(x / cap)
+        off = off + 2.0 ** -22 * cap
+    x = torch.where(seen, x, -math.inf)
+    off = (off.nan_to_num().amax(1) if len(k) else torch.zeros(len(q), dtype=torch.float64)) + 2.0 ** -22 * torch.where(
+        some, x.amax(1) if len(k) else 0.0, 0.0).abs()
+    lse = torch.logsumexp(x, 1) if len(k) else torch.full((len(q),), -math.inf, dtype=torch.float64)
+    p = torch.where(some[:, None], torch.exp(x - lse[:, None]), 0.0)
+    v = torch.where(seen.any(0)[:, None], v, 0.0)
+    out, mag = p @ v, p @ v.abs()
+    step = 2 * off + weight_step + 2.0 ** -21 + 2.0 ** -24 * len(k)
+    return out, lse, step[:, None] * mag, off + 2.0 ** -21 * (1 + lse.abs()) + 2.0 ** -24 * len(k)
+
+
+def prompts(q, k, v, cu_q, cu_k, scale, cap=0.0, window=0):
+    """resq_attend_prompts: (out, lse, bounds of both) like rows(); NaN for rows outside of the sequences."""
+    q, k, v = (t.detach().cpu().double() for t in (q, k, v))
+    share = q.shape[1] // k.shape[1]
+    out, tol = torch.full_like(q, math.nan), torch.full_like(q, math.nan)
+    lse, tol_lse = torch.full(q.shape[:2], math.nan, dtype=torch.float64), torch.full(q.shape[:2], math.nan, dtype=torch.float64)
+    for q0, q1, k0, k1 in zip(cu_q, cu_q[1:], cu_k, cu_k[1:]):
+        last = torch.arange(q1 - q0) + (k1 - k0) - (q1 - q0) + 1
+        first = last - window if window else 0 * last
+        for h in range(q.shape[1] if q1 > q0 else 0):
+            got = rows(q[q0:q1, h], k[k0:k1, h // share], v[k0:k1, h // share], first, last, scale, cap, 2.0 ** -8)
+            out[q0:q1, h], lse[q0:q1, h], tol[q0:q1, h], tol_lse[q0:q1, h] = got
+    return out, lse, tol, tol_lse
+
+
+def check(got, got_lse, want, where=None):
+    """bf16 results and fp32 sums against rows()' bounds; `where`: the rows to look at (all where None)."""
+    out, lse, tol, tol_lse = want
+    got, got_lse = got.detach().cpu().double(), None if got_lse is None else got_lse.cpu().double()
+    if where is not None:
+        got, out, tol, lse, tol_lse = got[where], out[where], tol[where], lse[where], tol_lse[where]
+        got_lse = None if got_lse is None else got_lse[where]
+    over = (got - out).abs() - (tol + 2.0 ** -8 * (out.abs() + tol) + 2.0 ** -133)
+    assert bool((over <= 0).all()), (float(over.max()), torch.nonzero(~(over <= 0))[:5].tolist())
+    if got_lse is not None:
+        empty = lse == -math.inf
+        assert bool((got_lse[empty] == -math.inf).all())
+        over = ((got_lse - lse).abs() - tol_lse)[~empty]
+        assert bool((over <= 0).all()), float(over.max())

@@ -1,0 +1,57 @@
+"""What the entry points around a layer's products refuse, and their host functions, without a GPU."""
+import pytest
+import torch
+
+from paper_2412_14363_amd import binding
+
+P = 0x10000   # a plausible, aligned, never dereferenced address
+OK, NULL, SHAPE, ALIGN, BUFFER = 0, 1, 2, 3, 4
+
+
+def call(name, good, **change):
+    """The entry point with the arguments of `good` (in order), some changed."""
+    assert set(change) <= set(good)
+    return getattr(binding.lib(), name)(*{**good, **change}.values())
+
+
+PROMPTS = dict(q=P, ldq=1024, ldqh=128, tokens_q=40, k=P, ldk=256, ldkh=128, v=P, ldv=256, ldvh=128, tokens_k=50, cu_q=P, cu_k=P, B=3, heads_q=8,
+               heads_k=2, d=128, scale=0.1, softcap=0.0, window=0, out=P, ldo=1024, ldoh=128, lse=None, workspace=P, nbytes=1 << 40, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(tokens_q=-1), SHAPE), (dict(tokens_k=-1), SHAPE), (dict(tokens_q=(1 << 30) + 1, heads_q=1, heads_k=1), SHAPE), (dict(tokens_k=(1 << 30) + 1), SHAPE),
+    (dict(tokens_q=1 << 30), SHAPE), (dict(B=0), SHAPE), (dict(B=65536), SHAPE), (dict(heads_q=7), SHAPE), (dict(heads_k=0), SHAPE),
+    (dict(heads_q=0), SHAPE), (dict(heads_q=70000, heads_k=70000), SHAPE), (dict(d=4), SHAPE), (dict(d=100), SHAPE), (dict(d=264), SHAPE),
+    (dict(ldq=-1), SHAPE), (dict(ldkh=-8), SHAPE), (dict(ldv=-8), SHAPE), (dict(ldoh=100), SHAPE), (dict(ldo=1023), SHAPE), (dict(scale=0.0), SHAPE),
+    (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE), (dict(softcap=-1.0), SHAPE),
+    (dict(softcap=float("nan")), SHAPE), (dict(softcap=1e-39), SHAPE), (dict(window=-1), SHAPE), (dict(ldq=2048), SHAPE),
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(cu_q=None), NULL), (dict(cu_k=None), NULL), (dict(out=None), NULL),
+    (dict(workspace=None), NULL), (dict(q=P + 1), ALIGN), (dict(out=2 * P + 1), ALIGN), (dict(k=P + 8), ALIGN), (dict(v=P + 2), ALIGN),
+    (dict(ldk=260), ALIGN), (dict(ldvh=132), ALIGN), (dict(cu_q=P + 2), ALIGN), (dict(cu_k=P + 1), ALIGN), (dict(lse=P + 2), ALIGN),
+    (dict(workspace=P + 16), ALIGN), (dict(nbytes=8), BUFFER), (dict(tokens_q=0, q=None, out=None, workspace=None), OK)])
+def test_prompts_refuses(change, status):
+    assert call("resq_attend_prompts", PROMPTS, **change) == status
+
+
+def test_prompts_workspace_sizes():
+    f = binding.resq_attend_prompts_workspace_bytes
+    assert f(1, 1, 1, 32, 8, 128) > 0 and f(300, 100000, 1, 32, 8, 128) > f(300, 300, 1, 32, 8, 128) and f(0, 0, 65535, 8, 8, 256) > 0
+    for bad in ((-1, 1, 1, 8, 8, 64), (1, -1, 1, 8, 8, 64), (1, 1, 0, 8, 8, 64), (1, 1, 65536, 8, 8, 64), (1, 1, 1, 8, 3, 64), (1, 1, 1, 8, 0, 64),
+                (1, 1, 1, 8, 8, 60), (1, 1, 1, 8, 8, 264), (1 << 30, 1, 1, 8, 8, 64)):
+        assert f(*bad) == 0, bad
+    with pytest.raises(ValueError):
+        binding.resq_attend_prompts_workspace(1, 1, 1, 8, 3, 64)
+
+
+def test_prompts_binding_refuses():
+    bf16, i32 = torch.bfloat16, torch.int32
+    q, k, cu = torch.zeros(4, 8, 64, dtype=bf16), torch.zeros(5, 2, 64, dtype=bf16), torch.zeros(3, dtype=i32)
+    space = torch.zeros(256, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="device memory"):   # everything fits but where it lives
+        binding.resq_attend_prompts(q, k, k, cu, workspace=space)
+    for args, kw in (((q.float(), k, k, cu), {}), ((q.transpose(1, 2), k, k, cu), {}), ((q, k, k[:4], cu), {}), ((q, k[:, :, :32], k[:, :, :32], cu), {}),
+                     ((q, k.repeat(1, 2, 1)[:, :3], k.repeat(1, 2, 1)[:, :3], cu), {}), ((q, k, k, cu.long()), {}), ((q, k, k, cu, cu[:2]), {}),
+                     ((q, k, k, cu[:1]), {}), ((q, k, k, cu), dict(out=q[:3])), ((q, k, k, cu), dict(lse=torch.zeros(4, 2))),
+                     ((q, k[0], k[0], cu), {})):
+        with pytest.raises(ValueError):
+            binding.resq_attend_prompts(*args, workspace=space, **kw)
