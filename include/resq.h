@@ -608,6 +608,25 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
                         float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * What stands between two blocks of a layer, in one pass: the norm behind the block, its gate, the residual scale and sum, and the
+ * norm in front of the next block (whose output resq_quantize_act takes):
+ *   a  = y * rsqrt(mean(y^2) + eps) * (w_offset + w_post)   (w_post null: a = y;  y null: a = 0, what a first block needs)
+ *   h' = h + alpha * gate * a                               (gate null: 1)
+ *   x  = h' * rsqrt(mean(h'^2) + eps) * (w_offset + w_pre)
+ * in fp32 with one rounding of each output; x comes from h' as it was before its rounding.
+ *   y, gate, x  bf16 [tokens, width] with strides ldy, ldg, ldx (ldg 0: one gate for all tokens)   (read / read / written)
+ *   h, h_out  bf16, or fp32 (h_is_fp32), [tokens, width] with strides ldh, ldho          (read / written)
+ *            h_out may be h and x may be y, with the same strides; else outputs lie on no other tensor of the call, and rows of
+ *            an output do not overlap.  h_out or x may be null (not both): not written, w_pre is not read without x
+ *   w_pre, w_post  bf16 [width]; w_offset 0, or 1 for weights that are stored as their distance from 1             (read)
+ *   width    1 .. 32768; tokens = 0 does nothing; eps >= 0; w_offset, alpha finite; gate and w_post need y
+ * Alignment: that of the elements; rows of whole 16-byte pieces are the fastest.
+ */
+int resq_norm_residual(const void* y, int64_t ldy, const void* gate, int64_t ldg, const void* h, int64_t ldh, int h_is_fp32, int64_t tokens,
+                       int64_t width, const void* w_pre, const void* w_post, float w_offset, float eps, float alpha, void* h_out,
+                       int64_t ldho, void* x, int64_t ldx, void* stream);
+
+/*
  * Online Hadamard projection of the down_proj input (Section 4.3, U_D):
  *   y[m, c0 + g*b + j] = (1/sqrt(b)) * sum_i x[m, c0 + g*b + i] * H_b[i, j]
  * for each block g of b columns in [col_begin, col_end), H_b the Sylvester

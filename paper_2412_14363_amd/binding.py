@@ -62,6 +62,8 @@ SYMBOLS = {
     "resq_attend_prompts_workspace_bytes": (_sz, [_i64] * 6),
     "resq_attend_prompts": (C.c_int, [_p, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _i64, _i64, _i64, C.c_float,
                                       C.c_float, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
+    "resq_norm_residual": (C.c_int, [_p, _i64, _p, _i64, _p, _i64, C.c_int, _i64, _i64, _p, _p, C.c_float, C.c_float, C.c_float, _p, _i64, _p,
+                                     _i64, _p]),
     "resq_pack_weights": (C.c_int, [_p, _i64, _i64, _i64, _i64, _p, _sz, _p]),
     "resq_unpack_weights": (C.c_int, [_p, _i64, _i64, _i64, _p, _p, _p, _p, _p]),
     "resq_gemm_mixed": (C.c_int, [_p, _p, _p, _p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _p, _p, _p]),
@@ -887,7 +889,7 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     return out
 
 
-# ---- what stands around a layer's products: attention over whole prompts ---------------------------------------
+# ---- what stands around a layer's products: attention over whole prompts, the norms between blocks ---------------------------------------
 
 @functools.lru_cache(maxsize=1024, typed=True)
 def resq_attend_prompts_workspace_bytes(tokens_q: int, tokens_k: int, batch: int, heads_q: int, heads_k: int, d_head: int) -> int:
@@ -956,6 +958,57 @@ def resq_attend_prompts(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q:
     if st:
         _check(st, "resq_attend_prompts")
     return out
+
+
+_H_TYPES = (_BF16, torch.float32)
+
+
+def resq_norm_residual(y: Optional[torch.Tensor], h: torch.Tensor, w_pre: Optional[torch.Tensor], w_post: Optional[torch.Tensor] = None,
+                       gate: Optional[torch.Tensor] = None, alpha: float = 1.0, eps: float = 1e-6, w_offset: float = 0.0,
+                       h_out: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None, stream=None):
+    """(h + alpha * gate * norm(y; w_post), that normed with w_pre): h bf16 or fp32 [tokens, width], y (None: no block before) bf16
+    [tokens, width], gate bf16 [tokens, width] or [width], weights bf16 [width]; without w_post y is not normed, without w_pre there is
+    no second output (None).  h_out may be h, x may be y.  Without y and h_out the first output is h itself."""
+    tokens, width = shape = h.shape
+    if h_out is None and (y is not None or w_pre is None):
+        h_out = _empty(shape, h.dtype, h.device, stream)
+    if x is None and w_pre is not None:
+        x = _empty(shape, _BF16, h.device, stream)
+    dev = h.get_device()
+    ptr = {}
+    ok = h.dtype in _H_TYPES and h.stride(1) == 1 and dev >= 0 and dev == _raw_device() and (y is not None or (gate is None and w_post is None)) \
+        and (w_pre is not None or x is None)
+    for name, t, dtype in (("y", y, _BF16), ("h_out", h_out, h.dtype), ("x", x, _BF16)):
+        if t is not None:
+            ok = ok and t.dtype == dtype and t.shape == shape and t.stride(1) == 1 and t.get_device() == dev
+            ptr[name] = (t.data_ptr(), t.stride(0))
+    if gate is not None:
+        ok = ok and gate.dtype == _BF16 and (gate.shape == shape or gate.shape == shape[1:]) and gate.stride(-1) == 1 and gate.get_device() == dev
+        ptr["gate"] = (gate.data_ptr(), gate.stride(0) if gate.dim() == 2 else 0)
+    for w in (w_pre, w_post):
+        ok = ok and (w is None or (w.dtype == _BF16 and w.shape == shape[1:] and w.is_contiguous() and w.get_device() == dev))
+    if not ok:
+        where = "resq_norm_residual"
+        _need(h.dtype in _H_TYPES and h.stride(1) == 1, where, "h must be a row-major bf16 or fp32 [tokens, width] tensor")
+        for name, t, dtype in (("y", y, _BF16), ("h_out", h_out, h.dtype), ("x", x, _BF16)):
+            _need(t is None or (t.dtype == dtype and t.shape == shape and t.stride(1) == 1), where,
+                  f"{name} must be a row-major {dtype} [{tokens}, {width}] tensor")
+        _need(gate is None or (gate.dtype == _BF16 and gate.shape in (shape, shape[1:]) and gate.stride(-1) == 1), where,
+              f"gate must be a bf16 [{tokens}, {width}] or [{width}] tensor")
+        for name, w in (("w_pre", w_pre), ("w_post", w_post)):
+            _need(w is None or (w.dtype == _BF16 and w.shape == shape[1:] and w.is_contiguous()), where, f"{name} must be a contiguous bf16 [{width}] tensor")
+        _need(y is not None or (gate is None and w_post is None), where, "gate and w_post belong to y")
+        _need(w_pre is not None or x is None, where, "x needs w_pre")
+        _explain_devices(where, h, y, gate, w_pre, w_post, h_out, x)
+        raise ValueError(f"{where}: invalid arguments")
+    none = (None, 0)
+    to = ptr.get("h_out", none)
+    st = lib().resq_norm_residual(*ptr.get("y", none), *ptr.get("gate", none), h.data_ptr(), h.stride(0), int(h.dtype == torch.float32), tokens,
+                                  width, None if w_pre is None else w_pre.data_ptr(), None if w_post is None else w_post.data_ptr(), w_offset,
+                                  eps, alpha, *to, *ptr.get("x", none), _stream(stream))
+    if st:
+        _check(st, "resq_norm_residual")
+    return h if h_out is None else h_out, x
 
 
 def resq_online_hadamard(x: torch.Tensor, col_begin: int, col_end: int, block: int = 0,

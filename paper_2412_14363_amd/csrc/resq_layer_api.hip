@@ -1,4 +1,4 @@
-// C ABI of what stands around a layer's products beside the generation step: attention over whole prompts.
+// C ABI of what stands around a layer's products beside the generation step: attention over whole prompts, the norms between blocks.
 // Argument checks on the host, then launches on the caller's stream.  See include/resq.h for the contract of every entry.
 #include <float.h>
 #include <hip/hip_runtime.h>
@@ -7,6 +7,7 @@
 
 #include "resq.h"
 #include "resq_launch.h"
+#include "resq_norm.hip.h"
 #include "resq_prompts.hip.h"
 
 using namespace resq;
@@ -55,6 +56,15 @@ int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
     launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(kPromptThreads), (size_t)lds, st, a);
     if (p.parts > 1)
         launch(attend_prompts_join_kernel<KEYS>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(kPromptThreads), 0, st, a);
+    return launch_status();
+}
+
+template <int T, int P>
+int launch_norm(const NormArgs& a, bool wide, hipStream_t st) {
+    constexpr int threads = T < 256 ? 256 : T;
+    const int64_t blocks = (a.tokens + threads / T - 1) / (threads / T);
+    if (!launch_fits(blocks, threads)) return RESQ_ERR_SHAPE;
+    launch(wide ? norm_residual_kernel<T, P, float> : norm_residual_kernel<T, P, uint16_t>, dim3((unsigned)blocks), dim3(threads), 0, st, a);
     return launch_status();
 }
 
@@ -123,6 +133,34 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
     if (d_head <= 128) return launch_prompts<128, 64, 2>(a, p, st);
     if (d_head <= 192) return launch_prompts<192, 32, 1>(a, p, st);
     return launch_prompts<256, 32, 1>(a, p, st);
+}
+
+int resq_norm_residual(const void* y, int64_t ldy, const void* gate, int64_t ldg, const void* h, int64_t ldh, int h_is_fp32, int64_t tokens,
+                       int64_t width, const void* w_pre, const void* w_post, float w_offset, float eps, float alpha, void* h_out,
+                       int64_t ldho, void* x, int64_t ldx, void* stream) {
+    if (tokens < 0 || width < 1 || width > kNormMaxWidth || ldy < 0 || ldg < 0 || ldh < 0 || !(eps >= 0.0f) || !isfinite(eps) ||
+        !isfinite(w_offset) || !isfinite(alpha) || (tokens > 1 && ((h_out && ldho < width) || (x && ldx < width))))
+        return RESQ_ERR_SHAPE;
+    if (tokens == 0) return RESQ_OK;
+    if (!h || (!h_out && !x) || (x && !w_pre) || ((gate || w_post) && !y)) return RESQ_ERR_NULL;
+    if (tokens == 1) ldy = ldg = ldh = ldho = ldx = 0;
+    if ((h_out == h && ldho != ldh) || (x && x == y && ldx != ldy)) return RESQ_ERR_SHAPE;
+    const uintptr_t of_h = h_is_fp32 ? 4 : 2;
+    if (!aligned(y, 2) || !aligned(gate, 2) || !aligned(h, of_h) || !aligned(h_out, of_h) || !aligned(x, 2) || !aligned(w_pre, 2) ||
+        !aligned(w_post, 2))
+        return RESQ_ERR_ALIGN;
+    const NormArgs a{static_cast<const uint16_t*>(y), ldy, static_cast<const uint16_t*>(gate), ldg, h, ldh,
+                     static_cast<const uint16_t*>(w_post), static_cast<const uint16_t*>(w_pre), w_offset, eps, alpha, h_out, ldho,
+                     static_cast<uint16_t*>(x), ldx, tokens, (int)width};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool wide = h_is_fp32 != 0;
+    if (width <= 512) return launch_norm<64, 1>(a, wide, st);
+    if (width <= 1024) return launch_norm<128, 1>(a, wide, st);
+    if (width <= 2048) return launch_norm<256, 1>(a, wide, st);
+    if (width <= 4096) return launch_norm<512, 1>(a, wide, st);
+    if (width <= 8192) return launch_norm<1024, 1>(a, wide, st);
+    if (width <= 16384) return launch_norm<1024, 2>(a, wide, st);
+    return launch_norm<1024, 4>(a, wide, st);
 }
 
 }  // extern "C"

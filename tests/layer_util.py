@@ -63,3 +63,37 @@ def check(got, got_lse, want, where=None):
         assert bool((got_lse[empty] == -math.inf).all())
         over = ((got_lse - lse).abs() - tol_lse)[~empty]
         assert bool((over <= 0).all()), float(over.max())
+
+
+def norm_residual(y, h, w_pre, w_post, gate, alpha, eps, offset):
+    """resq_norm_residual: (h', x, bounds of the kernel's errors before its last roundings), in 64 bits.
+
+    The bounds.  A mean square is a sum of squares, all of one sign: each term is rounded at most 64 times (32 in a thread, the rest
+    between them, the quotient), its root halves that, and the root itself is off by 2^-23: 2^-18 + 2^-23 of the value, below 2^-17.
+    The products behind it are a few roundings of 2^-24 more."""
+    h = h.detach().cpu().double()
+    out, off = h, torch.zeros_like(h)
+    if y is not None:
+        a = y.detach().cpu().double()
+        if w_post is not None:
+            a = a / torch.sqrt((a * a).mean(1, keepdim=True) + eps) * (offset + w_post.cpu().double())
+        if gate is not None:
+            a = a * gate.cpu().double()
+        out = h + alpha * a
+        off = 2.0 ** -17 * (alpha * a).abs() + 2.0 ** -23 * (h.abs() + (alpha * a).abs())
+    if w_pre is None:
+        return out, None, off, None
+    f = (offset + w_pre.cpu().double()) / torch.sqrt((out * out).mean(1, keepdim=True) + eps)
+    # what h' is off by moves the root by no more than it moves the largest row norm
+    root = (off.square().mean(1, keepdim=True) / ((out * out).mean(1, keepdim=True) + eps)).sqrt()
+    return out, out * f, off, (out * f).abs() * (root + 2.0 ** -17 + 2.0 ** -22) + off * f.abs()
+
+
+def check_norm(h, x, want, wide):
+    out, y, off, off_x = want
+    if h is not None:
+        over = (h.cpu().double() - out).abs() - (off + (2.0 ** -24 if wide else 2.0 ** -8) * (out.abs() + off) + 2.0 ** -133)
+        assert bool((over <= 0).all()), float(over.max())
+    if x is not None:
+        over = (x.cpu().double() - y).abs() - (off_x + 2.0 ** -8 * (y.abs() + off_x) + 2.0 ** -133)
+        assert bool((over <= 0).all()), float(over.max())

@@ -55,3 +55,31 @@ def test_prompts_binding_refuses():
                      ((q, k[0], k[0], cu), {})):
         with pytest.raises(ValueError):
             binding.resq_attend_prompts(*args, workspace=space, **kw)
+
+
+NORM = dict(y=P, ldy=512, gate=P, ldg=0, h=2 * P, ldh=512, h_is_fp32=0, tokens=4, width=512, w_pre=P, w_post=P, w_offset=0.0, eps=1e-6, alpha=1.0,
+            h_out=3 * P, ldho=512, x=4 * P, ldx=512, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(tokens=-1), SHAPE), (dict(width=0), SHAPE), (dict(width=32769, ldho=40000, ldx=40000), SHAPE), (dict(ldy=-1), SHAPE), (dict(ldg=-1), SHAPE),
+    (dict(ldh=-1), SHAPE), (dict(ldho=511), SHAPE), (dict(ldx=100), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=float("nan")), SHAPE),
+    (dict(eps=float("inf")), SHAPE), (dict(alpha=float("nan")), SHAPE), (dict(w_offset=float("inf")), SHAPE), (dict(h_out=2 * P, ldho=520), SHAPE),
+    (dict(x=P, ldx=520), SHAPE), (dict(tokens=1 << 32), SHAPE), (dict(h=None), NULL), (dict(h_out=None, x=None), NULL), (dict(w_pre=None), NULL),
+    (dict(y=None), NULL), (dict(y=None, gate=None), NULL), (dict(y=P + 1), ALIGN), (dict(gate=P + 1), ALIGN), (dict(h=2 * P + 1), ALIGN),
+    (dict(h=2 * P + 2, h_is_fp32=1), ALIGN), (dict(h_out=3 * P + 2, h_is_fp32=1), ALIGN), (dict(x=4 * P + 1), ALIGN), (dict(w_pre=P + 1), ALIGN),
+    (dict(w_post=P + 1), ALIGN), (dict(tokens=0, h=None), OK)])
+def test_norm_refuses(change, status):
+    assert call("resq_norm_residual", NORM, **change) == status
+
+
+def test_norm_binding_refuses():
+    bf16 = torch.bfloat16
+    y, w = torch.zeros(4, 64, dtype=bf16), torch.zeros(64, dtype=bf16)
+    with pytest.raises(ValueError, match="device memory"):
+        binding.resq_norm_residual(y, y, w)
+    for args, kw in (((y, y.half(), w), {}), ((y.float(), y, w), {}), ((y[:3], y, w), {}), ((y, y, w[:32]), {}), ((y, y, w.float()), {}),
+                     ((y, y, w), dict(w_post=w[:32])), ((y, y, w), dict(gate=y[:2])), ((None, y, w), dict(gate=w)), ((None, y, w), dict(w_post=w)),
+                     ((y, y, None), dict(x=y)), ((y, y, w), dict(h_out=y.float())), ((y, y, w), dict(x=y[:2])), ((y, y.t().contiguous().t(), w), {})):
+        with pytest.raises(ValueError):
+            binding.resq_norm_residual(*args, **kw)

@@ -165,3 +165,72 @@ def test_prompts_without_tokens(rq):
     lse = torch.zeros(3, 4, device=DEV)
     out = rq.resq_attend_prompts(q, k[:0], k[:0], ints([0, 3]), ints([0, 0]), lse=lse)
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+# ---- the norms between blocks --------------------------------------------------------------------------
+
+def norm_inputs(seed, tokens, width, wide, gate, post, pad=0, shift=0):
+    """Tensors of rows `pad` apart from each other, `shift` elements behind an aligned address."""
+    g = gen(seed)
+
+    def make(x, dtype):
+        room = torch.zeros(tokens * (width + pad) + shift, dtype=dtype, device=DEV)
+        v = room[shift:].view(tokens, width + pad)[:, :width]
+        v.copy_(x)
+        return v
+    y, h = torch.randn(tokens, width, generator=g), 4 * torch.randn(tokens, width, generator=g) + 0.5
+    h[:, width // 3] *= 30
+    weight = lambda: (1 + 0.3 * torch.randn(width, generator=g)).to(torch.bfloat16).to(DEV)
+    gates = {"none": None, "channel": weight(), "token": make(torch.randn(tokens, width, generator=g), torch.bfloat16)}
+    return dict(y=make(y, torch.bfloat16), h=make(h, torch.float32 if wide else torch.bfloat16), w_pre=weight(), w_post=weight() if post else None,
+                gate=gates[gate])
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("tokens,width", [(1, 1), (1, 7), (3, 8), (5, 64), (9, 511), (4, 512), (7, 513), (3, 1000), (130, 1024), (6, 1030), (5, 2047),
+                                          (2, 2048), (3, 2056), (40, 4096), (2, 4104), (1, 5120), (3, 8192), (2, 8195), (2, 16384), (1, 20001), (2, 32768)])
+def test_norm_widths(rq, tokens, width, wide):
+    for gate, post, alpha, offset, pad, shift in (("none", False, 1.0, 0.0, 0, 0), ("token", True, 0.22, 1.0, 0, 0), ("channel", True, -1.5, 0.0, 3, 1),
+                                                  ("channel", False, 1.0, 1.0, 8, 0)):
+        i = norm_inputs(width + tokens, tokens, width, wide, gate, post, pad, shift)
+        h, x = rq.resq_norm_residual(**i, alpha=alpha, w_offset=offset, eps=1e-5)
+        plain.check_norm(h, x, plain.norm_residual(**i, alpha=alpha, eps=1e-5, offset=offset), wide)
+
+
+def test_norm_parts(rq):
+    """Without a block, without the second norm, into given tensors and in place; nothing else is written."""
+    for wide in (False, True):
+        i = norm_inputs(3, 37, 1000, wide, "none", True, pad=24)
+        want = plain.norm_residual(**i, alpha=1.0, eps=1e-6, offset=0.0)
+        first = plain.norm_residual(None, i["h"], i["w_pre"], None, None, 1.0, 1e-6, 0.0)
+        h, x = rq.resq_norm_residual(None, i["h"], i["w_pre"])
+        assert h is i["h"]
+        plain.check_norm(None, x, first, wide)
+        h, x = rq.resq_norm_residual(i["y"], i["h"], None, w_post=i["w_post"])
+        assert x is None
+        plain.check_norm(h, None, want, wide)
+        h, x = rq.resq_norm_residual(None, i["h"], None)
+        assert torch.equal(h, i["h"]) and x is None
+        room = torch.full((37, 1010), 9.0, dtype=torch.bfloat16, device=DEV)
+        h_room = torch.full((37, 1010), 9.0, dtype=i["h"].dtype, device=DEV)
+        rq.resq_norm_residual(**i, h_out=h_room[:, 3:1003], x=room[:, 5:1005])
+        plain.check_norm(h_room[:, 3:1003], room[:, 5:1005], want, wide)
+        assert bool((room[:, :5] == 9).all() and (room[:, 1005:] == 9).all() and (h_room[:, :3] == 9).all() and (h_room[:, 1003:] == 9).all())
+        h, x = rq.resq_norm_residual(**i, h_out=i["h"], x=i["y"])
+        assert h is i["h"] and x is i["y"]
+        plain.check_norm(h, x, want, wide)
+
+
+def test_norm_of_zeros_and_large_and_no_tokens(rq):
+    w = torch.ones(4096, dtype=torch.bfloat16, device=DEV)
+    zero = torch.zeros(2, 4096, dtype=torch.bfloat16, device=DEV)
+    h, x = rq.resq_norm_residual(zero, zero, w, w_post=w)
+    assert not bool(h.any()) and not bool(x.any())
+    big = torch.full((2, 4096), 1e15, device=DEV)
+    h, x = rq.resq_norm_residual(zero, big, w)
+    assert bool((h == big).all()) and bool((x == 1).all())
+    h, x = rq.resq_norm_residual(zero[:0], big[:0], w)
+    assert h.shape == x.shape == (0, 4096)
+    many = torch.ones(70000, 8, dtype=torch.bfloat16, device=DEV)
+    h, x = rq.resq_norm_residual(many, many, torch.ones(8, dtype=torch.bfloat16, device=DEV))
+    assert bool((h == 2).all()) and bool((x == 1).all())
