@@ -608,6 +608,30 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
                         float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention of one new token of each sequence, as resq_attend_kv_cache, behind a PREFIX that all sequences of the batch share (the
+ * instructions in front of every request, the question that many answers are tried for): the tokens of sequence b are the
+ * prefix's, then lens[b] of its own (its new token the last of them).  The prefix is read and made into numbers once for 128 queries
+ * of a K/V head instead of once for each sequence; results are those of resq_attend_kv_cache on tables that name both in a row.
+ *   prefix_len    int32 [1]: tokens of the prefix; what is above prefix_width * page_size (or 2^30) is read as that, below 0 as 0  (read)
+ *   prefix_table  int32 [prefix_width]: its pages                                        (read)
+ *   lens          int32 [B]: own tokens; 0: the prefix alone; below 0: the sequence is not there, its out is 0 and its lse -inf  (read)
+ *   block_table   the own tokens' pages; own tokens begin with a page of their own        (read)
+ *   window        counts own tokens first
+ *   workspace     resq_attend_kv_prefix_workspace_bytes bytes
+ * Everything else as resq_attend_kv_cache.  Rows of the prefix go into the products as fp16 numbers: k and v are off by 2^-11 of
+ * themselves at most, or by 2^-38 of the largest number among the keys of 16 tokens, among all values so far; weights by 2^-11
+ * of themselves or 2^-35 of the row's largest one.
+ * How the prefix is cut into parts depends on the sizes and its length alone, for the own tokens see above: equal calls give equal bits.
+ */
+size_t resq_attend_kv_prefix_workspace_bytes(int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head);
+int resq_attend_kv_prefix(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head, int64_t r,
+                          const int32_t* prefix_len, const int32_t* prefix_table, int64_t prefix_width, const int32_t* lens,
+                          const int32_t* block_table, int64_t ld_table, int64_t width, const void* k_pages, const void* v_pages,
+                          int64_t num_pages, int64_t page_size, int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale,
+                          float softcap, int64_t window, void* out, int64_t ldo, int64_t ldoh, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
  * What stands between two blocks of a layer, in one pass: the norm behind the block, its gate, the residual scale and sum, and the
  * norm in front of the next block (whose output resq_quantize_act takes):
  *   a  = y * rsqrt(mean(y^2) + eps) * (w_offset + w_post)   (w_post null: a = y;  y null: a = 0, what a first block needs)

@@ -62,6 +62,9 @@ SYMBOLS = {
     "resq_attend_prompts_workspace_bytes": (_sz, [_i64] * 6),
     "resq_attend_prompts": (C.c_int, [_p, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _i64, _i64, _i64, C.c_float,
                                       C.c_float, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
+    "resq_attend_kv_prefix_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "resq_attend_kv_prefix": (C.c_int, [_p, _i64, _i64, _i64, _i64, _i64, _i64, _i64, _p, _p, _i64, _p, _p, _i64, _i64, _p, _p, _i64, _i64, _i64,
+                                        _i64, _i64, C.c_float, C.c_float, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
     "resq_norm_residual": (C.c_int, [_p, _i64, _p, _i64, _p, _i64, C.c_int, _i64, _i64, _p, _p, C.c_float, C.c_float, C.c_float, _p, _i64, _p,
                                      _i64, _p]),
     "resq_pack_weights": (C.c_int, [_p, _i64, _i64, _i64, _i64, _p, _sz, _p]),
@@ -889,7 +892,7 @@ def resq_attend_kv_cache(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     return out
 
 
-# ---- what stands around a layer's products: attention over whole prompts, the norms between blocks ---------------------------------------
+# ---- what stands around a layer's products: attention over whole prompts and behind a shared prefix, the norms between blocks ---------------------------------------
 
 @functools.lru_cache(maxsize=1024, typed=True)
 def resq_attend_prompts_workspace_bytes(tokens_q: int, tokens_k: int, batch: int, heads_q: int, heads_k: int, d_head: int) -> int:
@@ -957,6 +960,79 @@ def resq_attend_prompts(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q:
         workspace.numel(), _stream(stream))
     if st:
         _check(st, "resq_attend_prompts")
+    return out
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def resq_attend_kv_prefix_workspace_bytes(batch: int, heads_q: int, heads_k: int, d_head: int) -> int:
+    return int(lib().resq_attend_kv_prefix_workspace_bytes(batch, heads_q, heads_k, d_head))
+
+
+def resq_attend_kv_prefix_workspace(batch: int, heads_q: int, heads_k: int, d_head: int, device="cuda") -> torch.Tensor:
+    """A workspace for resq_attend_kv_prefix calls of these sizes; calls on different streams need one each."""
+    nbytes = resq_attend_kv_prefix_workspace_bytes(batch, heads_q, heads_k, d_head)
+    if nbytes == 0:
+        raise ValueError(f"invalid (batch, heads_q, heads_k, d_head) = ({batch}, {heads_q}, {heads_k}, {d_head})")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def resq_attend_kv_prefix(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, prefix_len: torch.Tensor, prefix_table: torch.Tensor,
+                          lens: torch.Tensor, block_table: torch.Tensor, r: int, scale: Optional[float] = None, softcap: float = 0.0,
+                          window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """resq_attend_kv_cache behind a prefix of prefix_len (int32 [1]) tokens in the pages of prefix_table (int32 [pages]) that all
+    sequences share; lens (below 0: the sequence is not there) and block_table are their own tokens behind it."""
+    batch, heads, d = shape = q.shape
+    if out is None:
+        out = _empty(shape, _BF16, q.device, stream)
+    if batch == 0:
+        return out
+    n, heads_k, size, width = k_pages.shape if k_pages.dim() == 4 else (0, 0, 0, 0)
+    if workspace is None:
+        nbytes = resq_attend_kv_prefix_workspace_bytes(batch, heads, heads_k, d)
+        workspace = _made(lambda: torch.empty(max(nbytes, 1), dtype=_U8, device=q.device), stream, q.device, handed_out=False)
+    dev = q.get_device()
+    ldq, ldqh, one = q.stride()
+    ldo, ldoh, one_o = out.stride() if out.dim() == 3 else (0, 0, 0)
+    need = _page_row_bytes(d, r)
+    strides = k_pages.stride()
+    ld_table, one_t = block_table.stride() if block_table.dim() == 2 else (0, 0)
+    sums = None
+    ok = (q.dtype == _BF16 and out.dtype == _BF16 and lens.dtype == _I32 and block_table.dtype == _I32 and prefix_len.dtype == _I32
+          and prefix_table.dtype == _I32 and k_pages.dtype == _U8 and v_pages.dtype == _U8 and workspace.dtype == _U8 and one == 1
+          and one_o == 1 and one_t == 1 and out.shape == shape and heads_k > 0 and heads % heads_k == 0 and 0 < need <= width
+          and strides[3] == 1 and v_pages.shape == k_pages.shape and v_pages.stride() == strides and lens.shape == (batch,)
+          and lens.is_contiguous() and block_table.shape[0] == batch and block_table.shape[1] > 0 and prefix_len.shape == (1,)
+          and prefix_table.dim() == 1 and prefix_table.shape[0] > 0 and prefix_table.is_contiguous() and workspace.is_contiguous() and dev >= 0
+          and dev == _raw_device() and out.get_device() == dev and lens.get_device() == dev and block_table.get_device() == dev
+          and prefix_len.get_device() == dev and prefix_table.get_device() == dev and k_pages.get_device() == dev
+          and v_pages.get_device() == dev and workspace.get_device() == dev)
+    if lse is not None and ok:
+        ok = lse.dtype == torch.float32 and lse.shape == (batch, heads) and lse.is_contiguous() and lse.get_device() == dev
+        sums = lse.data_ptr()
+    if not ok:
+        where = "resq_attend_kv_prefix"
+        _explain_heads(where, "q", q)
+        _explain_heads(where, "out", out)
+        _need(out.shape == shape and heads_k > 0 and heads % heads_k == 0, where,
+              f"q {tuple(shape)}, out {tuple(out.shape)} or {heads_k} K/V heads do not match")
+        _need(lse is None or (lse.dtype == torch.float32 and lse.shape == (batch, heads) and lse.is_contiguous()), where,
+              f"lse must be a contiguous fp32 [{batch}, {heads}] tensor")
+        _need(workspace.dtype == _U8 and workspace.is_contiguous(), where, "workspace must be a contiguous uint8 tensor")
+        _explain_devices(where, q, k_pages, v_pages, prefix_len, prefix_table, lens, block_table, out, lse, workspace)
+        _explain_pages(where, k_pages, v_pages, heads_k, d, r)
+        _explain_table(where, block_table, batch)
+        _explain_ints(where, "lens", lens, batch)
+        _explain_ints(where, "prefix_len", prefix_len, 1)
+        _explain_ints(where, "prefix_table", prefix_table)
+        raise ValueError(f"{where}: invalid arguments")
+    st = lib().resq_attend_kv_prefix(
+        q.data_ptr(), ldq, ldqh, batch, heads, heads_k, d, r, prefix_len.data_ptr(), prefix_table.data_ptr(), prefix_table.shape[0],
+        lens.data_ptr(), block_table.data_ptr(), ld_table, block_table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), n, size, strides[0],
+        strides[1], strides[2], d ** -0.5 if scale is None else scale, softcap, window, out.data_ptr(), ldo, ldoh, sums,
+        workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st:
+        _check(st, "resq_attend_kv_prefix")
     return out
 
 

@@ -84,6 +84,7 @@ struct AttendArgs {
     uint16_t* out;
     int64_t ldo, ldoh;
     float* lse;
+    float* out32;      // not null: [B][heads][d] results in fp32, in place of out
     int32_t* joins;    // [B][heads][2]: a head's first partial result, and the workgroup that has its last one (workspace)
     float* part_ml;    // [2 grid][16][2]: maximum (times log2 e) and sum of a partial result's queries (workspace)
     float* part_acc;   // [2 grid][rows][d]: and its weighted sums (workspace)
@@ -744,8 +745,12 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             const int qhead = hk * a.share + qt * kAttendRows + row;
             if (whole) {
                 const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                uint16_t* dst = a.out + b * a.ldo + qhead * a.ldoh + ch;
-                *reinterpret_cast<Piece8*>(dst) = Piece8{pack_bf16_pair(o[0] * inv, o[1] * inv), pack_bf16_pair(o[2] * inv, o[3] * inv)};
+                if (a.out32) {
+                    *reinterpret_cast<v4f_att*>(a.out32 + ((int64_t)b * a.heads_k * a.share + qhead) * a.d + ch) = o * inv;
+                } else {
+                    uint16_t* dst = a.out + b * a.ldo + qhead * a.ldoh + ch;
+                    *reinterpret_cast<Piece8*>(dst) = Piece8{pack_bf16_pair(o[0] * inv, o[1] * inv), pack_bf16_pair(o[2] * inv, o[3] * inv)};
+                }
                 if (ch == 0 && a.lse)
                     a.lse[(int64_t)b * a.heads_k * a.share + qhead] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
             } else {
@@ -783,7 +788,10 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     const int fours = a.d >> 2;
     auto write = [&](int row, int ch, const float4& o, float top, float sum) {
         const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-        *reinterpret_cast<Piece8*>(out + row * a.ldoh + ch) = Piece8{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
+        if (a.out32)
+            *reinterpret_cast<float4*>(a.out32 + ((int64_t)b * a.heads_k * a.share + q0 + row) * a.d + ch) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        else
+            *reinterpret_cast<Piece8*>(out + row * a.ldoh + ch) = Piece8{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
         if (ch == 0 && lse) lse[row] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
     };
     const bool empty = attend_len(a, b) == 0;

@@ -21,6 +21,8 @@ namespace resq {
 
 constexpr int kFlashRows = 32;          // of a wavefront
 constexpr float kFlashNone = -3.0e38f;  // the maximum of no scores: finite, so that differences stay numbers
+// weights in fp16 are 2^10 times what they are: those down to 2^-24 of the largest one keep all their bits, and 2^-35 is the smallest
+constexpr float kFlashHalfBias = 10.0f;
 
 typedef float v16f_flash __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u_flash __attribute__((ext_vector_type(4)));
@@ -102,6 +104,128 @@ struct FlashRow {
         const uint8_t* p = vals + 16 * t * Tile::kPitch + Tile::value_at(row, piece) + 8 * (lane & 1);
         const v2u_flash a = flash_read_tr(p), b = flash_read_tr(p + 8 * Tile::kPitch);
         return (v4u_flash){a[0], a[1], b[0], b[1]};
+    }
+
+    // A tile of KEYS keys.  f[g]: what makes a score of keys 16 g .. 16 g + 15 one of base 2, or (softcap) what it is multiplied with in
+    // front of the cap; scaled: up[g] is what those keys' weights are multiplied with for the product with the values.
+    // partly: rows do not see some keys; sees(kb, i): whether the lane's row sees its key i of the block kb.
+    template <int KEYS, typename Sees>
+    __device__ __forceinline__ void step(const uint8_t* kt, const uint8_t* vt, const float (&f)[KEYS / 16], const float (&up)[KEYS / 16], bool scaled,
+                                         float softcap, float inv_cap, bool partly, Sees sees) {
+        constexpr float kBias = F16 ? kFlashHalfBias : 0.0f;
+        const float inf = __builtin_huge_valf();
+        v16f_flash x[KEYS / 32];
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb) x[kb] = scores(kt, kb);
+        if (softcap > 0.0f) {
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] = soft_cap(x[kb][i] * f[2 * kb + (i >> 3)], softcap, inv_cap) * 1.44269504088896340736f;
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] *= f[2 * kb + (i >> 3)];
+        }
+        if (partly) {
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] = sees(kb, i) ? x[kb][i] : -inf;
+        }
+        // ---- the running maximum ----
+        float top = x[0][0];
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+        const float m_new = fmaxf(m, halves_max(top));
+        const float back = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= back;
+#pragma unroll
+        for (int c = 0; c < Tile::kBlocks; ++c) acc[c] *= back;
+        // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
+        v4u_flash p[KEYS / 16];
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const float base = kBias - m_new;
+#pragma unroll
+                for (int i = 8 * g; i < 8 * g + 8; i += 2) {
+                    float p0 = __builtin_amdgcn_exp2f(x[kb][i] + base), p1 = __builtin_amdgcn_exp2f(x[kb][i + 1] + base);
+                    l += p0 + p1;
+                    if (scaled) {
+                        p0 *= up[2 * kb + g];
+                        p1 *= up[2 * kb + g];
+                    }
+                    p[2 * kb + g][(i & 7) >> 1] = flash_pack<F16>(p0, p1);
+                }
+            }
+        // ---- weighted sums of values ----
+        // A key that some row of the wavefront does not see has weight 0 there, which an infinity or NaN among its values would
+        // not care about: such values are left out of the product, and what they make of a row that sees them is added apart.
+        constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u, kOne = F16 ? 0x3C00u : 0x3F80u;
+        bool odd = false;
+        if (partly) {
+            uint32_t found = 0;
+#pragma unroll
+            for (int s = 0; s < KEYS / 16; ++s)
+#pragma unroll
+                for (int c = 0; c < Tile::kBlocks; ++c) {
+                    const v4u_flash o = values(vt, s, c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) found |= (o[e] & (kExp << 16 | kExp)) + ((0x8000u - kExp) << 16 | (0x8000u - kExp));
+                }
+            odd = __builtin_amdgcn_ballot_w64((found & 0x80008000u) != 0) != 0;
+        }
+        if (!odd) {
+#pragma unroll
+            for (int s = 0; s < KEYS / 16; ++s)
+#pragma unroll
+                for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(values(vt, s, c), p[s], acc[c]);
+            return;
+        }
+        v4u_flash one[KEYS / 16];   // 1 where the row sees the key
+#pragma unroll
+        for (int s = 0; s < KEYS / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 8 * (s & 1) + 2 * e;
+                one[s][e] = (sees(s >> 1, i) ? kOne : 0u) | (sees(s >> 1, i + 1) ? kOne << 16 : 0u);
+            }
+        // kind 0: finite values, with their weights; 1, 2, 3: infinities, negative ones, NaN, counted
+#pragma unroll 1
+        for (int kind = 0; kind < 4; ++kind) {
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) {
+                v16f_flash sum;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] = kind == 0 ? acc[c][i] : 0.0f;
+#pragma unroll
+                for (int s = 0; s < KEYS / 16; ++s) {
+                    v4u_flash o = values(vt, s, c), w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t two = 0;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const uint32_t u = o[e] >> (16 * k) & 0xFFFFu, mag = u & 0x7FFFu;
+                            const int is = mag < kExp ? 0 : mag > kExp ? 3 : u >> 15 ? 2 : 1;
+                            two |= (is != kind ? 0u : kind == 0 ? u : kOne) << (16 * k);
+                        }
+                        o[e] = two;
+                        w[e] = kind == 0 ? p[s][e] : one[s][e];
+                    }
+                    sum = flash_mfma<F16>(o, w, sum);
+                }
+                const float what = kind == 1 ? inf : kind == 2 ? -inf : __builtin_nanf("");
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c][i] = kind == 0 ? sum[i] : sum[i] > 0.0f ? acc[c][i] + what : acc[c][i];
+            }
+        }
     }
 };
 

@@ -128,6 +128,88 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
 
 }  // namespace
 
+namespace resq {
+
+int attend_kv_cache_call(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head,
+                         int64_t r, const int32_t* lens, const int32_t* block_table, int64_t ld_table, int64_t width,
+                         const void* k_pages, const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride,
+                         int64_t head_stride, int64_t row_stride, float scale, float softcap, int64_t window, void* out,
+                         int64_t ldo, int64_t ldoh, float* lse, float* out32, void* workspace, size_t workspace_bytes, void* stream) {
+    const size_t need = resq_attend_kv_cache_workspace_bytes(B, heads_q, heads_k, d_head);
+    if (need == 0 || ldq < 0 || ldqh < 0 || width < 1 || width > kInt32Max || (B > 1 && ld_table < width) || !(scale > 0.0f) ||
+        !isfinite(scale) || !(softcap == 0.0f || softcap >= FLT_MIN) || !isfinite(softcap) || window < 0 ||
+        (!out32 && !rows_apart(B, ldo, heads_q, ldoh, d_head)))
+        return RESQ_ERR_SHAPE;
+    PagesGeometry g{num_pages, page_size, heads_k, page_stride, head_stride, row_stride};
+    const int rc = check_pages(g, k_pages, v_pages, d_head, r);
+    if (rc != RESQ_OK && rc != RESQ_ERR_NULL && rc != RESQ_ERR_ALIGN) return rc;
+    if (!q || !lens || !block_table || (!out && !out32) || !workspace) return RESQ_ERR_NULL;
+    if (rc != RESQ_OK) return rc;
+    if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lens, 4) || !aligned(block_table, 4) || !aligned(lse, 4) ||
+        !aligned(workspace, 256))
+        return RESQ_ERR_ALIGN;
+    if (workspace_bytes < need) return RESQ_ERR_BUFFER;
+    const int64_t longest = width > kMaxAttendLen / page_size ? kMaxAttendLen : width * page_size;
+    // units of the longest sequences that the table can name: counted in 32 bits
+    const int64_t qtiles = (heads_q / heads_k + kAttendRows - 1) / kAttendRows;
+    const int64_t units = B * heads_k * qtiles * ((longest + kAttendUnit - 1) / kAttendUnit + kAttendHeadCost);
+    if (units > kInt32Max || !launch_fits(B * heads_q, kAttendThreads)) return RESQ_ERR_SHAPE;
+    AttendArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.ldq = ldq;
+    a.ldqh = ldqh;
+    a.B = (int)B;
+    a.heads_k = (int)heads_k;
+    a.share = (int)(heads_q / heads_k);
+    a.d = (int)d_head;
+    a.r = (int)r;
+    a.lens = lens;
+    a.table = block_table;
+    a.ld_table = ld_table;
+    a.pages[0] = static_cast<const uint8_t*>(k_pages);
+    a.pages[1] = static_cast<const uint8_t*>(v_pages);
+    a.num_pages = (int)num_pages;
+    a.page_size = FastDiv((uint32_t)page_size);
+    a.page_stride = g.page_stride;
+    a.head_stride = g.head_stride;
+    a.row_stride = g.row_stride;
+    a.row_bytes = (int)(r + (d_head - r) / 2 + 16);
+    a.qtiles = (int)qtiles;
+    const AttendWorkspace w = attend_workspace(B, heads_k, a.share, d_head);
+    a.joins = static_cast<int32_t*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.ml);
+    a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.acc);
+    a.rows = w.rows;
+    a.blocks16 = page_size % 16 == 0 && g.row_stride < (1 << 26);
+    a.fours_magic = 65536 / (a.d / 4) + 1;
+    a.lds_red = 0;
+    a.max_len = (int)longest;
+    a.window = window < kMaxAttendLen ? (int)window : 0;
+    a.scale = scale;
+    a.softcap = softcap;
+    a.out = static_cast<uint16_t*>(out);
+    a.ldo = ldo;
+    a.ldoh = ldoh;
+    a.lse = lse;
+    a.out32 = out32;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t low = d_head - r;
+    // The smallest kernel that holds the head's two groups of channels, in as many workgroups to a compute unit as its registers allow
+    // without spilling vector registers in the loop over tiles (<0, 16> in pages that are no multiple of 16 rows has one to four there; some
+    // others have up to 28 around it, once a head).  32 x 4096, in us: the next larger kernel for 128 (r = 16) 48.3 instead of 46.9, 64 (8)
+    // 43.7 instead of 36.3, 256 (32) 103.5 instead of 82.5; a workgroup less 54.7 for 46.9, 37.7 for 36.3 (128, r = 32: 62.4 for 51.1); one more,
+    // with spills, 310 for 82.5 (256, r = 32), 781 for 132.5 (r = 256), 57.2 for 57.3 (128, r = 64).
+    if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
+                                                                                   : launch_attend<0, 16, 1>(a, units, st);
+    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
+                                                                                   : launch_attend<4, 16, 1>(a, units, st);
+    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
+                           : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 1>(a, units, st);
+    return r <= 32 ? launch_attend<16, 2, 1>(a, units, st) : launch_attend<16, 8, 1>(a, units, st);
+}
+
+}  // namespace resq
+
 extern "C" {
 
 int resq_kv_slots(const int32_t* lens, const int32_t* new_tokens, int64_t B, int64_t page_size, int64_t num_pages,
@@ -295,75 +377,9 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
                          const void* k_pages, const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride,
                          int64_t head_stride, int64_t row_stride, float scale, float softcap, int64_t window, void* out,
                          int64_t ldo, int64_t ldoh, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    const size_t need = resq_attend_kv_cache_workspace_bytes(B, heads_q, heads_k, d_head);
-    if (need == 0 || ldq < 0 || ldqh < 0 || width < 1 || width > kInt32Max || (B > 1 && ld_table < width) || !(scale > 0.0f) ||
-        !isfinite(scale) || !(softcap == 0.0f || softcap >= FLT_MIN) || !isfinite(softcap) || window < 0 || !rows_apart(B, ldo, heads_q, ldoh, d_head))
-        return RESQ_ERR_SHAPE;
-    PagesGeometry g{num_pages, page_size, heads_k, page_stride, head_stride, row_stride};
-    const int rc = check_pages(g, k_pages, v_pages, d_head, r);
-    if (rc != RESQ_OK && rc != RESQ_ERR_NULL && rc != RESQ_ERR_ALIGN) return rc;
-    if (!q || !lens || !block_table || !out || !workspace) return RESQ_ERR_NULL;
-    if (rc != RESQ_OK) return rc;
-    if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lens, 4) || !aligned(block_table, 4) || !aligned(lse, 4) ||
-        !aligned(workspace, 256))
-        return RESQ_ERR_ALIGN;
-    if (workspace_bytes < need) return RESQ_ERR_BUFFER;
-    const int64_t longest = width > kMaxAttendLen / page_size ? kMaxAttendLen : width * page_size;
-    // units of the longest sequences that the table can name: counted in 32 bits
-    const int64_t qtiles = (heads_q / heads_k + kAttendRows - 1) / kAttendRows;
-    const int64_t units = B * heads_k * qtiles * ((longest + kAttendUnit - 1) / kAttendUnit + kAttendHeadCost);
-    if (units > kInt32Max || !launch_fits(B * heads_q, kAttendThreads)) return RESQ_ERR_SHAPE;
-    AttendArgs a;
-    a.q = static_cast<const uint16_t*>(q);
-    a.ldq = ldq;
-    a.ldqh = ldqh;
-    a.B = (int)B;
-    a.heads_k = (int)heads_k;
-    a.share = (int)(heads_q / heads_k);
-    a.d = (int)d_head;
-    a.r = (int)r;
-    a.lens = lens;
-    a.table = block_table;
-    a.ld_table = ld_table;
-    a.pages[0] = static_cast<const uint8_t*>(k_pages);
-    a.pages[1] = static_cast<const uint8_t*>(v_pages);
-    a.num_pages = (int)num_pages;
-    a.page_size = FastDiv((uint32_t)page_size);
-    a.page_stride = g.page_stride;
-    a.head_stride = g.head_stride;
-    a.row_stride = g.row_stride;
-    a.row_bytes = (int)(r + (d_head - r) / 2 + 16);
-    a.qtiles = (int)qtiles;
-    const AttendWorkspace w = attend_workspace(B, heads_k, a.share, d_head);
-    a.joins = static_cast<int32_t*>(workspace);
-    a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.ml);
-    a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.acc);
-    a.rows = w.rows;
-    a.blocks16 = page_size % 16 == 0 && g.row_stride < (1 << 26);
-    a.fours_magic = 65536 / (a.d / 4) + 1;
-    a.lds_red = 0;
-    a.max_len = (int)longest;
-    a.window = window < kMaxAttendLen ? (int)window : 0;
-    a.scale = scale;
-    a.softcap = softcap;
-    a.out = static_cast<uint16_t*>(out);
-    a.ldo = ldo;
-    a.ldoh = ldoh;
-    a.lse = lse;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t low = d_head - r;
-    // The smallest kernel that holds the head's two groups of channels, in as many workgroups to a compute unit as its registers allow
-    // without spilling vector registers in the loop over tiles (<0, 16> in pages that are no multiple of 16 rows has one to four there; some
-    // others have up to 28 around it, once a head).  32 x 4096, in us: the next larger kernel for 128 (r = 16) 48.3 instead of 46.9, 64 (8)
-    // 43.7 instead of 36.3, 256 (32) 103.5 instead of 82.5; a workgroup less 54.7 for 46.9, 37.7 for 36.3 (128, r = 32: 62.4 for 51.1); one more,
-    // with spills, 310 for 82.5 (256, r = 32), 781 for 132.5 (r = 256), 57.2 for 57.3 (128, r = 64).
-    if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
-                                                                                   : launch_attend<0, 16, 1>(a, units, st);
-    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
-                                                                                   : launch_attend<4, 16, 1>(a, units, st);
-    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
-                           : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 1>(a, units, st);
-    return r <= 32 ? launch_attend<16, 2, 1>(a, units, st) : launch_attend<16, 8, 1>(a, units, st);
+    return attend_kv_cache_call(q, ldq, ldqh, B, heads_q, heads_k, d_head, r, lens, block_table, ld_table, width, k_pages, v_pages, num_pages,
+                                page_size, page_stride, head_stride, row_stride, scale, softcap, window, out, ldo, ldoh, lse, nullptr,
+                                workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

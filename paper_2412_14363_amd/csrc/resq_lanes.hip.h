@@ -91,6 +91,12 @@ __device__ __forceinline__ float rows_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// and maximum over the wavefront of what is a row's alone
+__device__ __forceinline__ float rows_max(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return halves_max(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+}
+
 // cap * tanh(x / cap): by the exponential, or near 0, where that would cancel, by the series (its sixth term is below 2^-24)
 __device__ __forceinline__ float soft_cap(float x, float cap, float inv_cap) {
     const float y = x * inv_cap, y2 = y * y;

@@ -38,4 +38,11 @@ inline bool kv_head_ok(int64_t d_head, int64_t r) {
     return d_head >= 8 && d_head <= 512 && d_head % 8 == 0 && r >= 0 && r <= d_head && r % 8 == 0;
 }
 
+// resq_attend_kv_cache, with out32 not null its results in fp32 to [B][heads_q][d_head] of it in place of out (resq_kv_api.hip)
+int attend_kv_cache_call(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head, int64_t r,
+                         const int32_t* lens, const int32_t* block_table, int64_t ld_table, int64_t width, const void* k_pages,
+                         const void* v_pages, int64_t num_pages, int64_t page_size, int64_t page_stride, int64_t head_stride,
+                         int64_t row_stride, float scale, float softcap, int64_t window, void* out, int64_t ldo, int64_t ldoh, float* lse,
+                         float* out32, void* workspace, size_t workspace_bytes, void* stream);
+
 }  // namespace resq

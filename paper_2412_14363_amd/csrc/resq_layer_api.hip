@@ -1,4 +1,5 @@
-// C ABI of what stands around a layer's products beside the generation step: attention over whole prompts, the norms between blocks.
+// C ABI of what stands around a layer's products beside the generation step: attention over whole prompts,
+// attention of a batch behind a shared prefix, the norms between blocks.
 // Argument checks on the host, then launches on the caller's stream.  See include/resq.h for the contract of every entry.
 #include <float.h>
 #include <hip/hip_runtime.h>
@@ -8,6 +9,7 @@
 #include "resq.h"
 #include "resq_launch.h"
 #include "resq_norm.hip.h"
+#include "resq_prefix.hip.h"
 #include "resq_prompts.hip.h"
 
 using namespace resq;
@@ -56,6 +58,40 @@ int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
     launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(kPromptThreads), (size_t)lds, st, a);
     if (p.parts > 1)
         launch(attend_prompts_join_kernel<KEYS>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(kPromptThreads), 0, st, a);
+    return launch_status();
+}
+
+// workspace of the attention behind a shared prefix: that of the own tokens' attention, its results, then the prefix's parts
+struct PrefixPlan {
+    int64_t tiles;   // of 128 rows
+    int parts;
+    size_t own, out, lse, ml, acc, bytes;
+};
+constexpr size_t whole(size_t n) { return (n + 255) / 256 * 256; }
+bool prefix_plan(PrefixPlan& p, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d) {
+    p.own = resq_attend_kv_cache_workspace_bytes(B, heads_q, heads_k, d);   // 0 for sizes that it refuses
+    if (p.own == 0 || B * heads_q >= 1 << 24) return false;
+    p.tiles = (B * (heads_q / heads_k) + kPrefixRows - 1) / kPrefixRows;
+    const int64_t units = p.tiles * heads_k, at_once = d <= 128 ? 512 : 256;
+    p.parts = units >= at_once ? 1 : (int)(at_once / units);
+    p.out = whole(p.own);
+    p.lse = p.out + whole((size_t)B * heads_q * d * sizeof(float));
+    p.ml = p.lse + whole((size_t)B * heads_q * sizeof(float));
+    p.acc = p.ml + (size_t)units * p.parts * kPrefixRows * 2 * sizeof(float);
+    p.bytes = p.acc + (size_t)units * p.parts * kPrefixRows * d * sizeof(float);
+    return true;
+}
+
+template <int W, int OCC>
+int launch_prefix(const PrefixArgs& a, const PrefixPlan& p, hipStream_t st) {
+    const int lds = 4 * kPrefixKeys * FlashTile<W>::kPitch;
+    const auto kernel = attend_prefix_kernel<W, OCC>;
+    if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               lds) != hipSuccess)
+        return RESQ_ERR_HIP;
+    launch(kernel, dim3((unsigned)(p.tiles * a.heads_k * p.parts)), dim3(kPrefixThreads), (size_t)lds, st, a);
+    const int64_t threads = (int64_t)a.B * a.heads_k * a.share.d * (a.d / 4);
+    launch(attend_prefix_join_kernel, dim3((unsigned)((threads + kPrefixThreads - 1) / kPrefixThreads)), dim3(kPrefixThreads), 0, st, a);
     return launch_status();
 }
 
@@ -133,6 +169,75 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
     if (d_head <= 128) return launch_prompts<128, 64, 2>(a, p, st);
     if (d_head <= 192) return launch_prompts<192, 32, 1>(a, p, st);
     return launch_prompts<256, 32, 1>(a, p, st);
+}
+
+size_t resq_attend_kv_prefix_workspace_bytes(int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head) {
+    PrefixPlan p;
+    return prefix_plan(p, B, heads_q, heads_k, d_head) ? p.bytes : 0;
+}
+
+int resq_attend_kv_prefix(const void* q, int64_t ldq, int64_t ldqh, int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head, int64_t r,
+                          const int32_t* prefix_len, const int32_t* prefix_table, int64_t prefix_width, const int32_t* lens,
+                          const int32_t* block_table, int64_t ld_table, int64_t width, const void* k_pages, const void* v_pages,
+                          int64_t num_pages, int64_t page_size, int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale,
+                          float softcap, int64_t window, void* out, int64_t ldo, int64_t ldoh, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    PrefixPlan p;
+    if (!prefix_plan(p, B, heads_q, heads_k, d_head) || prefix_width < 1 || prefix_width > kInt32Max || !rows_apart(B, ldo, heads_q, ldoh, d_head))
+        return RESQ_ERR_SHAPE;
+    if (!prefix_len || !prefix_table || !out || !workspace) return RESQ_ERR_NULL;
+    if (B == 1) ldq = ldo = 0;
+    if (heads_q == 1) ldqh = ldoh = 0;
+    if (out == q && (ldq != ldo || ldqh != ldoh)) return RESQ_ERR_SHAPE;
+    if (!aligned(prefix_len, 4) || !aligned(prefix_table, 4) || !aligned(out, 2) || !aligned(lse, 4)) return RESQ_ERR_ALIGN;
+    if (workspace_bytes < p.bytes) return aligned(workspace, 256) ? RESQ_ERR_BUFFER : RESQ_ERR_ALIGN;
+    uint8_t* space = static_cast<uint8_t*>(workspace);
+    float *own_out = reinterpret_cast<float*>(space + p.out), *own_lse = reinterpret_cast<float*>(space + p.lse);
+    // checks everything else, and launches nothing where it refuses
+    const int rc = attend_kv_cache_call(q, ldq, ldqh, B, heads_q, heads_k, d_head, r, lens, block_table, ld_table, width, k_pages, v_pages, num_pages,
+                                        page_size, page_stride, head_stride, row_stride, scale, softcap, window, nullptr, 0, 0, own_lse, own_out,
+                                        workspace, p.own, stream);
+    if (rc != RESQ_OK) return rc;
+    PrefixArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.ldq = ldq;
+    a.ldqh = ldqh;
+    a.B = (int)B;
+    a.heads_k = (int)heads_k;
+    a.d = (int)d_head;
+    a.r = (int)r;
+    a.row_bytes = (int)(r + (d_head - r) / 2 + 16);
+    a.share = FastDiv((uint32_t)(heads_q / heads_k));
+    a.parts = FastDiv((uint32_t)p.parts);
+    a.heads = FastDiv((uint32_t)heads_k);
+    a.prefix_len = prefix_len;
+    a.prefix_table = prefix_table;
+    a.max_prefix = (int)(prefix_width > kMaxTokens / page_size ? kMaxTokens : prefix_width * page_size);
+    a.lens = lens;
+    a.pages[0] = static_cast<const uint8_t*>(k_pages);
+    a.pages[1] = static_cast<const uint8_t*>(v_pages);
+    a.num_pages = (int)num_pages;
+    a.page_size = FastDiv((uint32_t)page_size);
+    a.page_stride = page_stride;
+    a.head_stride = head_stride;
+    a.row_stride = row_stride;
+    a.scale = scale;
+    a.softcap = softcap;
+    a.window = window > 0 && window < kMaxTokens ? (int)window : (int)kMaxTokens;
+    a.own_out = own_out;
+    a.own_lse = own_lse;
+    a.out = static_cast<uint16_t*>(out);
+    a.ldo = ldo;
+    a.ldoh = ldoh;
+    a.lse = lse;
+    a.part_ml = reinterpret_cast<float*>(space + p.ml);
+    a.part_acc = reinterpret_cast<float*>(space + p.acc);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (d_head <= 64) return launch_prefix<64, 2>(a, p, st);
+    if (d_head <= 96) return launch_prefix<96, 2>(a, p, st);
+    if (d_head <= 128) return launch_prefix<128, 2>(a, p, st);
+    if (d_head <= 192) return launch_prefix<192, 1>(a, p, st);
+    return launch_prefix<256, 1>(a, p, st);
 }
 
 int resq_norm_residual(const void* y, int64_t ldy, const void* gate, int64_t ldg, const void* h, int64_t ldh, int h_is_fp32, int64_t tokens,

@@ -176,9 +176,10 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
         }
     };
     const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
-    const float kLog2e = 1.44269504088896340736f;
-    const float sc2 = a.softcap > 0.0f ? kLog2e : a.scale * kLog2e;
     const float inf = __builtin_huge_valf();
+    float f[KEYS / 16];
+#pragma unroll
+    for (int g = 0; g < KEYS / 16; ++g) f[g] = a.softcap > 0.0f ? a.scale : a.scale * 1.44269504088896340736f;
 
     if (begin < end) {
         load(begin);
@@ -195,108 +196,11 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
         if (key0 < some1 && key0 + KEYS > some0) {
             const uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
             const bool partly = key0 < all0 || key0 + KEYS > all1;
-            v16f_flash x[KEYS / 32];
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb) x[kb] = r.scores(kt, kb);
-            if (a.softcap > 0.0f) {
-#pragma unroll
-                for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[kb][i] = soft_cap(x[kb][i] * a.scale, a.softcap, inv_cap);
-            }
             const int behind = own - key0 - 4 * half;   // keys from the lane's first one to the row's own
-            auto sees = [&](int kb, int i) {
-                return (unsigned)(behind - (32 * kb + 8 * (i >> 2) + (i & 3))) < (unsigned)a.window && behind >= 32 * kb + 8 * (i >> 2) + (i & 3);
-            };
-            if (partly) {
-#pragma unroll
-                for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[kb][i] = sees(kb, i) ? x[kb][i] : -inf;
-            }
-            // ---- the running maximum ----
-            float top = x[0][0];
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
-            const float m_new = fmaxf(r.m, halves_max(top) * sc2);
-            const float back = __builtin_amdgcn_exp2f(r.m - m_new);
-            r.m = m_new;
-            r.l *= back;
-#pragma unroll
-            for (int c = 0; c < Tile::kBlocks; ++c) r.acc[c] *= back;
-            // ---- weights, rounded once to bf16 as the product's operand (off by 2^-8 of each at most; their sum is taken unrounded) ----
-            v4u_flash p[KEYS / 16];
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(x[kb][i], sc2, -m_new)), p1 = __builtin_amdgcn_exp2f(fmaf(x[kb][i + 1], sc2, -m_new));
-                    r.l += p0 + p1;
-                    p[2 * kb + (i >> 3)][(i & 7) >> 1] = flash_pack<false>(p0, p1);
-                }
-            // ---- weighted sums of values ----
-            // A key that some row of the wavefront does not see has weight 0 there, which an infinity or NaN among its values would
-            // not care about: such values are left out of the product, and what they make of a row that sees them is added apart.
-            bool odd = false;
-            if (partly) {
-                uint32_t found = 0;
-#pragma unroll
-                for (int s = 0; s < KEYS / 16; ++s)
-#pragma unroll
-                    for (int c = 0; c < Tile::kBlocks; ++c) {
-                        const v4u_flash o = r.values(vt, s, c);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) found |= ((o[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-                    }
-                odd = __builtin_amdgcn_ballot_w64(found != 0) != 0;
-            }
-            if (!odd) {
-#pragma unroll
-                for (int s = 0; s < KEYS / 16; ++s)
-#pragma unroll
-                    for (int c = 0; c < Tile::kBlocks; ++c) r.acc[c] = flash_mfma<false>(r.values(vt, s, c), p[s], r.acc[c]);
-            } else {
-                v4u_flash one[KEYS / 16];   // 1 where the row sees the key
-#pragma unroll
-                for (int s = 0; s < KEYS / 16; ++s)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 8 * (s & 1) + 2 * e;
-                        one[s][e] = (sees(s >> 1, i) ? 0x3F80u : 0u) | (sees(s >> 1, i + 1) ? 0x3F800000u : 0u);
-                    }
-                // kind 0: finite values, with their weights; 1, 2, 3: infinities, negative ones, NaN, counted
-#pragma unroll 1
-                for (int kind = 0; kind < 4; ++kind) {
-#pragma unroll
-                    for (int c = 0; c < Tile::kBlocks; ++c) {
-                        v16f_flash sum;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) sum[i] = kind == 0 ? r.acc[c][i] : 0.0f;
-#pragma unroll
-                        for (int s = 0; s < KEYS / 16; ++s) {
-                            v4u_flash o = r.values(vt, s, c), w;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                uint32_t two = 0;
-#pragma unroll
-                                for (int k = 0; k < 2; ++k) {
-                                    const uint32_t u = o[e] >> (16 * k) & 0xFFFFu, mag = u & 0x7FFFu;
-                                    const int is = mag < 0x7F80u ? 0 : mag > 0x7F80u ? 3 : u >> 15 ? 2 : 1;
-                                    two |= (is != kind ? 0u : kind == 0 ? u : 0x3F80u) << (16 * k);
-                                }
-                                o[e] = two;
-                                w[e] = kind == 0 ? p[s][e] : one[s][e];
-                            }
-                            sum = flash_mfma<false>(o, w, sum);
-                        }
-                        const float what = kind == 1 ? inf : kind == 2 ? -inf : __builtin_nanf("");
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) r.acc[c][i] = kind == 0 ? sum[i] : sum[i] > 0.0f ? r.acc[c][i] + what : r.acc[c][i];
-                    }
-                }
-            }
+            r.template step<KEYS>(kt, vt, f, f, false, a.softcap, inv_cap, partly, [&](int kb, int i) {
+                const int c = 32 * kb + 8 * (i >> 2) + (i & 3);
+                return behind >= c && behind - c < a.window;
+            });
         }
         __syncthreads();
     }

@@ -97,3 +97,57 @@ def check_norm(h, x, want, wide):
     if x is not None:
         over = (x.cpu().double() - y).abs() - (off_x + 2.0 ** -8 * (y.abs() + off_x) + 2.0 ** -133)
         assert bool((over <= 0).all()), float(over.max())
+
+
+def prefix(q, k_pages, v_pages, prefix_len, prefix_table, lens, table, r, scale, cap=0.0, window=0):
+    """resq_attend_kv_prefix: (out, lse, bounds of both).  The prefix's keys and values are off by 2^-11 of themselves (half a step of fp16)
+    and 2^-38 of the largest one; the own tokens' code products may carry offsets of up to 143 steps, 255 of the 8-bit group, and
+    their weights are two bf16 numbers: both are below what this takes for all tokens."""
+    from generation_util import decode_rows
+    q = q.cpu().double()
+    d, page, pages = q.shape[-1], k_pages.shape[2], k_pages.shape[0]
+    share = q.shape[1] // k_pages.shape[1]
+    out, lse = torch.zeros_like(q), torch.full(q.shape[:2], -math.inf, dtype=torch.float64)
+    tol, tol_lse = torch.zeros_like(q), torch.zeros(q.shape[:2], dtype=torch.float64)
+    n = min(max(int(prefix_len), 0), len(prefix_table) * page)
+
+    def there(ids, count):
+        t = torch.arange(count)
+        ids = ids.cpu().long()[t // page]
+        ok = (ids >= 0) & (ids < pages)
+        return ids[ok] * page + (t % page)[ok], t[ok]
+    front, front_t = there(prefix_table, n)
+    flat = [p.cpu().permute(0, 2, 1, 3).reshape(pages * page, *p.shape[1:2], p.shape[3]) for p in (k_pages, v_pages)]
+    for b, own in enumerate(int(x) for x in lens):
+        if own < 0:
+            continue
+        own = min(own, table.shape[1] * page)
+        back, back_t = there(table[b], own)
+        at, t = torch.cat((front, back)), torch.cat((front_t, back_t + n))
+        if window:
+            at = at[t >= n + own - window]
+        if not len(at):
+            continue
+        for h in range(k_pages.shape[1]):
+            rows_k, rows_v = (f[at, h] for f in flat)
+            k, v = decode_rows(rows_k, d, r), decode_rows(rows_v, d, r)
+            low = r + (d - r) // 2
+            big = []
+            for x, rows_x in ((k, rows_k), (v, rows_v)):
+                s = rows_x[:, low:low + 16].clone(memory_format=torch.contiguous_format).view(torch.float32).double().abs()
+                big.append(x.abs() + torch.cat((255 * s[:, 0:1].expand(-1, r), 143 * s[:, 2:3].expand(-1, d - r)), 1))
+            for i in range(h * share, (h + 1) * share):
+                x = scale * (k @ q[b, i])
+                size = scale * ((k.abs() @ q[b, i].abs()) * 2.0 ** -11 + (big[0] @ q[b, i].abs()) * 2.0 ** -18 +
+                                2.0 ** -38 * k.abs().max() * q[b, i].abs().sum())
+                off = (size + 2.0 ** -22 * x.abs()).max() + 2.0 ** -22 * x.max().abs()
+                if cap:
+                    x = cap * torch.tanh(x / cap)
+                    off = off + 2.0 ** -22 * cap
+                lse[b, i] = torch.logsumexp(x, 0)
+                p = torch.exp(x - lse[b, i])
+                out[b, i] = p @ v
+                step = 2 * off + 2.0 ** -15 + 2.0 ** -24 * len(at)
+                tol[b, i] = step * (p @ big[1]) + 2.0 ** -10 * (p @ v.abs()) + 2.0 ** -35 * v.abs().sum(0) + 2.0 ** -38 * v.abs().max()
+                tol_lse[b, i] = off + 2.0 ** -21 * (1 + lse[b, i].abs()) + 2.0 ** -24 * len(at)
+    return out, lse, tol, tol_lse

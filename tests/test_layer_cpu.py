@@ -83,3 +83,49 @@ def test_norm_binding_refuses():
                      ((y, y, None), dict(x=y)), ((y, y, w), dict(h_out=y.float())), ((y, y, w), dict(x=y[:2])), ((y, y.t().contiguous().t(), w), {})):
         with pytest.raises(ValueError):
             binding.resq_norm_residual(*args, **kw)
+
+
+PREFIX = dict(q=P, ldq=4096, ldqh=128, B=4, heads_q=32, heads_k=8, d=128, r=16, prefix_len=P, prefix_table=P, prefix_width=7, lens=P, table=P,
+              ld_table=10, width=10, k_pages=P, v_pages=P, num_pages=10, page_size=16, page_stride=8 * 16 * 88, head_stride=16 * 88, row_stride=88,
+              scale=0.1, softcap=0.0, window=0, out=P, ldo=4096, ldoh=128, lse=None, workspace=P, nbytes=1 << 40, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(d=124), SHAPE), (dict(d=264), SHAPE), (dict(d=4), SHAPE), (dict(r=136), SHAPE), (dict(r=10), SHAPE), (dict(r=-8), SHAPE), (dict(r=-4), SHAPE),
+    (dict(r=12, row_stride=84), BUFFER), (dict(r=12, k_pages=P + 1), ALIGN), (dict(num_pages=0), SHAPE), (dict(page_size=0), SHAPE),
+    (dict(num_pages=1 << 27), SHAPE), (dict(row_stride=84), BUFFER), (dict(head_stride=80), BUFFER), (dict(page_stride=0), BUFFER),
+    (dict(k_pages=None), NULL), (dict(v_pages=None), NULL), (dict(k_pages=P + 2), ALIGN), (dict(row_stride=90), ALIGN), (dict(B=0), SHAPE),
+    (dict(B=70000), SHAPE), (dict(heads_q=31), SHAPE), (dict(heads_k=0), SHAPE), (dict(ldq=-1), SHAPE), (dict(ldoh=64), SHAPE), (dict(ldo=4095), SHAPE),
+    (dict(prefix_width=0), SHAPE), (dict(prefix_width=1 << 31), SHAPE), (dict(width=0), SHAPE), (dict(width=11), SHAPE), (dict(scale=0.0), SHAPE),
+    (dict(scale=float("nan")), SHAPE), (dict(softcap=-1.0), SHAPE), (dict(softcap=1e-39), SHAPE), (dict(window=-1), SHAPE), (dict(ldq=8192), SHAPE),
+    (dict(q=None), NULL), (dict(prefix_len=None), NULL), (dict(prefix_table=None), NULL), (dict(lens=None), NULL), (dict(table=None), NULL),
+    (dict(out=None), NULL), (dict(workspace=None), NULL), (dict(q=P + 1), ALIGN), (dict(out=2 * P + 1), ALIGN), (dict(prefix_len=P + 2), ALIGN),
+    (dict(prefix_table=P + 1), ALIGN), (dict(lens=P + 2), ALIGN), (dict(table=P + 2), ALIGN), (dict(lse=P + 2), ALIGN), (dict(workspace=P + 16), ALIGN),
+    (dict(nbytes=64), BUFFER), (dict(B=65535, heads_q=512, heads_k=512, ldo=65536, ldq=65536), SHAPE)])
+def test_prefix_refuses(change, status):
+    assert call("resq_attend_kv_prefix", PREFIX, **change) == status
+
+
+def test_prefix_workspace_sizes():
+    f, own = binding.resq_attend_kv_prefix_workspace_bytes, binding.resq_attend_kv_cache_workspace_bytes
+    assert f(1, 32, 8, 128) > own(1, 32, 8, 128) and f(64, 32, 8, 128) > own(64, 32, 8, 128)
+    assert f(0, 32, 8, 128) == f(1, 31, 8, 128) == f(1, 32, 8, 264) == f(1, 32, 8, 100) == f(65536, 8, 8, 64) == f(1, 8, 0, 64) == 0
+    with pytest.raises(ValueError):
+        binding.resq_attend_kv_prefix_workspace(1, 31, 8, 128)
+
+
+def test_prefix_binding_refuses():
+    i32, bf16 = torch.int32, torch.bfloat16
+    q, n, pages, table = torch.zeros(4, 2, 64, dtype=bf16), torch.zeros(4, dtype=i32), torch.zeros(3, 2, 16, 52, dtype=torch.uint8), torch.zeros(4, 3, dtype=i32)
+    space = torch.zeros(256, dtype=torch.uint8)
+    f = binding.resq_attend_kv_prefix
+    with pytest.raises(ValueError, match="device memory"):
+        f(q, pages, pages, n[:1], n, n, table, 8, workspace=space)
+    for args, kw in (((q.float(), pages, pages, n[:1], n, n, table, 8), {}), ((q[:, :1], pages, pages, n[:1], n, n, table, 8), {}),
+                     ((q, pages, pages[:2], n[:1], n, n, table, 8), {}), ((q, pages, pages, n[:2], n, n, table, 8), {}),
+                     ((q, pages, pages, n[:1], table, n, table, 8), {}), ((q, pages, pages, n[:1], n.long(), n, table, 8), {}),
+                     ((q, pages, pages, n[:1], n, n[:3], table, 8), {}), ((q, pages, pages, n[:1], n, n, table[:3], 8), {}),
+                     ((q, pages, pages, n[:1], n, n, table, 64), {}), ((q, pages, pages, n[:1], n[:0], n, table, 8), {}),
+                     ((q, pages, pages, n[:1], n, n, table, 8), dict(lse=torch.zeros(4, 3))), ((q, pages, pages, n[:1], n, n, table, 8), dict(out=q[:2]))):
+        with pytest.raises(ValueError):
+            f(*args, workspace=space, **kw)

@@ -234,3 +234,121 @@ def test_norm_of_zeros_and_large_and_no_tokens(rq):
     many = torch.ones(70000, 8, dtype=torch.bfloat16, device=DEV)
     h, x = rq.resq_norm_residual(many, many, torch.ones(8, dtype=torch.bfloat16, device=DEV))
     assert bool((h == 2).all()) and bool((x == 1).all())
+
+
+# ---- a shared prefix -------------------------------------------------------------------------------
+
+def prefix_inputs(n, lens, hq, hk, d, r, page, order="head", pad=0, seed=1, extra=2):
+    from generation_util import make_pages
+    g = gen(seed)
+    first, held = -(-n // page), [-(-max(x, 0) // page) for x in lens]
+    total = first + sum(held) + extra
+    ids = torch.randperm(total, generator=g)
+    width = max(held) + 1
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    at = first
+    for b, h in enumerate(held):
+        table[b, :h] = ids[at:at + h].to(torch.int32)
+        at += h
+    k, v = make_pages(g, total, hk, page, d, r, order, pad), make_pages(g, total, hk, page, d, r, order, pad)
+    prefix_table = torch.cat((ids[:first].to(torch.int32), torch.tensor([-1], dtype=torch.int32)))
+    return dict(q=heads(g, len(lens), hq, d), k_pages=k, v_pages=v, prefix_len=ints([n]), prefix_table=prefix_table.to(DEV), lens=ints(lens),
+                block_table=table.to(DEV), r=r)
+
+
+def check_prefix(rq, i, **kw):
+    lse = torch.full(i["q"].shape[:2], 7.0, device=DEV)
+    out = rq.resq_attend_kv_prefix(**i, lse=lse, **kw)
+    torch.cuda.synchronize()
+    want = plain.prefix(i["q"], i["k_pages"], i["v_pages"], i["prefix_len"], i["prefix_table"], i["lens"], i["block_table"], i["r"],
+                        kw.get("scale") or i["q"].shape[-1] ** -0.5, kw.get("softcap", 0.0), kw.get("window", 0))
+    plain.check(out, lse, want)
+
+
+@pytest.mark.parametrize("n", [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 500, 2000])
+def test_prefix_lengths(rq, n):
+    check_prefix(rq, prefix_inputs(n, [0, 1, 5, 40, -1, 130, 0], 8, 2, 128, 16, 16, seed=n))
+
+
+@pytest.mark.parametrize("d,r", [(8, 0), (8, 8), (16, 8), (40, 16), (64, 8), (64, 0), (64, 64), (72, 8), (96, 12), (96, 4), (104, 96), (128, 16), (128, 128),
+                                 (128, 0), (136, 8), (192, 24), (192, 100), (248, 4), (256, 32), (256, 252), (256, 256), (256, 0)])
+def test_prefix_widths(rq, d, r):
+    check_prefix(rq, prefix_inputs(150, [0, 7, 33], 6, 2, d, r, 16, seed=d + r, pad=0 if r % 8 else 4))
+
+
+@pytest.mark.parametrize("hq,hk,batch", [(1, 1, 1), (1, 1, 40), (8, 1, 30), (12, 12, 5), (7, 1, 37), (32, 8, 33), (130, 1, 2), (64, 2, 9)])
+def test_prefix_heads(rq, hq, hk, batch):
+    check_prefix(rq, prefix_inputs(200, [(3 * b) % 7 for b in range(batch)], hq, hk, 64, 8, 16, seed=hq))
+
+
+@pytest.mark.parametrize("page,order", [(1, "head"), (7, "token"), (16, "token"), (24, "head"), (64, "head"), (100, "token"), (1024, "head")])
+def test_prefix_pages(rq, page, order):
+    check_prefix(rq, prefix_inputs(330, [0, 50, 1], 4, 2, 128, 16, page, order, pad=12, seed=page))
+
+
+@pytest.mark.parametrize("softcap", [0.0, 0.5, 30.0])
+@pytest.mark.parametrize("window", [1, 5, 64, 100, 300, 5000])
+def test_prefix_window_and_cap(rq, window, softcap):
+    check_prefix(rq, prefix_inputs(400, [0, 1, 4, 5, 6, 70, 99, 150, -3], 4, 2, 64, 8, 24, seed=window), window=window, softcap=softcap)
+
+
+@pytest.mark.parametrize("n,batch,hq,hk", [(9000, 2, 4, 1), (5000, 70, 8, 2), (1500, 300, 4, 2)])
+def test_prefix_long_and_many(rq, n, batch, hq, hk):
+    check_prefix(rq, prefix_inputs(n, [b % 3 for b in range(batch)], hq, hk, 64, 8, 32, seed=batch))
+
+
+def test_prefix_lengths_outside_and_pages_that_do_not_exist(rq):
+    i = prefix_inputs(300, [3, 0, 20], 4, 2, 64, 8, 16)
+    for n in (-5, 10000):   # the table's last entry names no page
+        i["prefix_len"] = ints([n])
+        check_prefix(rq, i)
+    i["prefix_len"] = ints([300])
+    i["prefix_table"][2], i["prefix_table"][7], i["prefix_table"][18] = -1, 1 << 20, -(1 << 31)
+    check_prefix(rq, i)
+    check_prefix(rq, i, window=250)
+    i["prefix_table"].fill_(-1)
+    check_prefix(rq, i)
+    i["lens"] = ints([-1, -2, 0])
+    lse = torch.zeros(3, 4, device=DEV)
+    assert not bool(rq.resq_attend_kv_prefix(**i, lse=lse).any()) and bool((lse == -math.inf).all())
+
+
+def test_prefix_is_what_one_table_of_both_gives(rq):
+    i = prefix_inputs(320, [16, 1, 40, 33], 8, 2, 128, 16, 16)
+    got = rq.resq_attend_kv_prefix(**i)
+    both = torch.cat((i["prefix_table"][:-1].expand(4, -1), i["block_table"]), 1).contiguous()
+    want = rq.resq_attend_kv_cache(i["q"], i["k_pages"], i["v_pages"], i["lens"] + 320, both, 16)
+    assert float((got.float() - want.float()).norm() / want.float().norm()) < 2.0 ** -8
+
+
+@pytest.mark.parametrize("key,value", [(1e-20, 1e-20), (1e20, 1.0), (1.0, 1e25), (1e-30, 1e30), (3e4, 7e4)])
+def test_prefix_of_very_small_and_very_large_numbers(rq, key, value):
+    """Scales that fp16 alone could not hold, some tokens a thousand times the others."""
+    i = prefix_inputs(300, [0, 20], 4, 2, 64, 8, 16)
+    for pages, f in ((i["k_pages"], key), (i["v_pages"], value)):
+        low = 8 + (64 - 8) // 2
+        par = pages[..., low:low + 16].contiguous().view(torch.float32) * f
+        par[3] *= 1000
+        par[7, :, 5] /= 1000
+        pages[..., low:low + 16] = par.view(torch.uint8)
+    check_prefix(rq, i, scale=0.01 / key)
+
+
+def test_prefix_values_that_are_not_finite_where_they_are_not_seen(rq):
+    """Behind a window and in pages that are not named an infinity or NaN does nothing; where a row sees it it does what it does."""
+    i = prefix_inputs(200, [0, 10, 60], 4, 2, 64, 8, 16)
+    low, page = 8 + (64 - 8) // 2, 16
+    t = i["prefix_table"].cpu()
+    for window in (100, 30):
+        j = {n: v.clone() if isinstance(v, torch.Tensor) else v for n, v in i.items()}
+        clean = plain.prefix(j["q"], j["k_pages"], j["v_pages"], 200, j["prefix_table"], j["lens"], j["block_table"], 8, 0.125, 0.0, window)
+        for tok, value in ((90, math.nan), (105, math.inf), (150, math.nan)):   # row 0 sees 100.., row 1 110.., row 2 160.. (window 100)
+            spot = j["v_pages"][int(t[tok // page]), 0, tok % page]
+            spot[low:low + 4] = torch.tensor([value]).view(torch.uint8).to(DEV)   # the 8-bit group's scale
+        got = rq.resq_attend_kv_prefix(**j, window=window).cpu().double()
+        gone = torch.zeros_like(got, dtype=torch.bool)
+        for b, own in enumerate((0, 10, 60)):
+            if any(tok >= 200 + own - window for tok in (90, 105, 150)):
+                gone[b, :2, :8] = True
+        over = (got - clean[0]).abs() - (clean[2] + 2.0 ** -8 * (clean[0].abs() + clean[2]))
+        assert bool((over[~gone] <= 0).all()) and not bool(torch.isfinite(got[gone]).any())
