@@ -23,6 +23,8 @@ constexpr int kFlashRows = 32;          // of a wavefront
 constexpr float kFlashNone = -3.0e38f;  // the maximum of no scores: finite, so that differences stay numbers
 // weights in fp16 are 2^10 times what they are: those down to 2^-24 of the largest one keep all their bits, and 2^-35 is the smallest
 constexpr float kFlashHalfBias = 10.0f;
+// by how many powers of two a score may be over the running maximum before that rises (in fp16 weights stay below 2^15)
+constexpr float kFlashSlack = 8.0f, kFlashHalfSlack = 5.0f;
 
 typedef float v16f_flash __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u_flash __attribute__((ext_vector_type(4)));
@@ -50,6 +52,13 @@ __device__ __forceinline__ v2u_flash flash_read_tr(const uint8_t* p) {
     return __builtin_bit_cast(v2u_flash, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                              (__attribute__((address_space(3))) v4s_flash*)(__attribute__((address_space(3))) uint8_t*)p));
 }
+
+// 16 bytes of each lane from base + off to lds + 16 lane in LDS, on their way past the compiler: it would have every later read of LDS wait
+// for them.  flash_landed() is the wait, and the workgroup's meeting behind it.
+__device__ __forceinline__ void flash_fetch(uint32_t lds, const uint8_t* base, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void flash_landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Layout of a tile: W channels (a multiple of 32) in rows of a power of two of pieces.
 template <int W>
@@ -106,70 +115,74 @@ struct FlashRow {
         return (v4u_flash){a[0], a[1], b[0], b[1]};
     }
 
-    // A tile of KEYS keys.  f[g]: what makes a score of keys 16 g .. 16 g + 15 one of base 2, or (softcap) what it is multiplied with in
-    // front of the cap; scaled: up[g] is what those keys' weights are multiplied with for the product with the values.
-    // partly: rows do not see some keys; sees(kb, i): whether the lane's row sees its key i of the block kb.
-    template <int KEYS, typename Sees>
-    __device__ __forceinline__ void step(const uint8_t* kt, const uint8_t* vt, const float (&f)[KEYS / 16], const float (&up)[KEYS / 16], bool scaled,
-                                         float softcap, float inv_cap, bool partly, Sees sees) {
-        constexpr float kBias = F16 ? kFlashHalfBias : 0.0f;
+    // A tile of KEYS keys.  f[g]: what makes a score of keys 16 g .. 16 g + 15 one of base 2, or (CAP) what it is multiplied with in
+    // front of the cap; ONE: all of them are f[0].  up (null: 1): what those keys' weights are multiplied with for the product with the values.
+    // PARTLY: rows do not see some keys; sees(kb, i): whether the lane's row sees its key i of the block kb.
+    template <int KEYS, bool CAP, bool ONE, bool PARTLY, typename Sees>
+    __device__ __forceinline__ void step(const uint8_t* kt, const uint8_t* vt, const float (&f)[KEYS / 16], const float* up, float softcap,
+                                         float inv_cap, Sees sees) {
+        constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
         const float inf = __builtin_huge_valf();
         v16f_flash x[KEYS / 32];
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb) x[kb] = scores(kt, kb);
-        if (softcap > 0.0f) {
+        if constexpr (CAP) {
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] = soft_cap(x[kb][i] * f[2 * kb + (i >> 3)], softcap, inv_cap) * 1.44269504088896340736f;
-        } else {
+                for (int i = 0; i < 16; ++i) x[kb][i] = soft_cap(x[kb][i] * f[ONE ? 0 : 2 * kb + (i >> 3)], softcap, inv_cap);
+        } else if constexpr (!ONE) {
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[kb][i] *= f[2 * kb + (i >> 3)];
         }
-        if (partly) {
+        const float unit = CAP ? 1.44269504088896340736f : ONE ? f[0] : 1.0f;   // of the scores now
+        if constexpr (PARTLY) {
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[kb][i] = sees(kb, i) ? x[kb][i] : -inf;
         }
-        // ---- the running maximum ----
-        float top = x[0][0];
+        // ---- the running maximum, where a score is 2^kSlack times what it allows ----
+        float tops[2] = {x[0][0], x[0][1]};
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
-        const float m_new = fmaxf(m, halves_max(top));
-        const float back = __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= back;
+            for (int i = 0; i < 16; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[kb][i]);
+        const float top = fmaxf(tops[0], tops[1]) * unit;
+        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+            const float m_new = fmaxf(m, halves_max(top));
+            const float back = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= back;
 #pragma unroll
-        for (int c = 0; c < Tile::kBlocks; ++c) acc[c] *= back;
+            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] *= back;
+        }
         // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
         v4u_flash p[KEYS / 16];
+        const float base = kBias - m;
+        float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const float base = kBias - m_new;
-#pragma unroll
-                for (int i = 8 * g; i < 8 * g + 8; i += 2) {
-                    float p0 = __builtin_amdgcn_exp2f(x[kb][i] + base), p1 = __builtin_amdgcn_exp2f(x[kb][i + 1] + base);
-                    l += p0 + p1;
-                    if (scaled) {
-                        p0 *= up[2 * kb + g];
-                        p1 *= up[2 * kb + g];
-                    }
-                    p[2 * kb + g][(i & 7) >> 1] = flash_pack<F16>(p0, p1);
+            for (int i = 0; i < 16; i += 2) {
+                float p0 = __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x[kb][i + 1], unit, base));
+                sums[0] += p0;
+                sums[1] += p1;
+                if (up) {
+                    p0 *= up[2 * kb + (i >> 3)];
+                    p1 *= up[2 * kb + (i >> 3)];
                 }
+                p[2 * kb + (i >> 3)][(i & 7) >> 1] = flash_pack<F16>(p0, p1);
             }
+        l += sums[0] + sums[1];
         // ---- weighted sums of values ----
         // A key that some row of the wavefront does not see has weight 0 there, which an infinity or NaN among its values would
         // not care about: such values are left out of the product, and what they make of a row that sees them is added apart.
         constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u, kOne = F16 ? 0x3C00u : 0x3F80u;
         bool odd = false;
-        if (partly) {
+        if constexpr (PARTLY) {
             uint32_t found = 0;
 #pragma unroll
             for (int s = 0; s < KEYS / 16; ++s)
@@ -188,6 +201,7 @@ struct FlashRow {
                 for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(values(vt, s, c), p[s], acc[c]);
             return;
         }
+        if constexpr (!PARTLY) return;
         v4u_flash one[KEYS / 16];   // 1 where the row sees the key
 #pragma unroll
         for (int s = 0; s < KEYS / 16; ++s)

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int64_t kInt32Max = 0x7FFFFFFF;
 constexpr int64_t kMaxTokens = 1 << 30;   // so that a place minus a window stays in 32 bits
+constexpr int64_t kMaxStride = 1 << 24;   // of keys and values from token to token: a tile's offsets stay in 32 bits
 constexpr int kMaxHead = 256;
 
 // sizes that both entries of the prompts' attention check, and what they have in common
@@ -51,7 +52,7 @@ bool prompt_plan(PromptPlan& p, int64_t tokens_q, int64_t tokens_k, int64_t B, i
 template <int W, int KEYS, int OCC>
 int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
     const int lds = 4 * KEYS * FlashTile<W>::kPitch;
-    const auto kernel = attend_prompts_kernel<W, KEYS, OCC>;
+    const auto kernel = a.softcap > 0.0f ? attend_prompts_kernel<W, KEYS, OCC, true> : attend_prompts_kernel<W, KEYS, OCC, false>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
@@ -85,7 +86,7 @@ bool prefix_plan(PrefixPlan& p, int64_t B, int64_t heads_q, int64_t heads_k, int
 template <int W, int OCC>
 int launch_prefix(const PrefixArgs& a, const PrefixPlan& p, hipStream_t st) {
     const int lds = 4 * kPrefixKeys * FlashTile<W>::kPitch;
-    const auto kernel = attend_prefix_kernel<W, OCC>;
+    const auto kernel = a.softcap > 0.0f ? attend_prefix_kernel<W, OCC, true> : attend_prefix_kernel<W, OCC, false>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
@@ -120,7 +121,7 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
     PromptPlan p;
     if (!prompt_plan(p, tokens_q, tokens_k, B, heads_q, heads_k, d_head) || ldq < 0 || ldqh < 0 || ldk < 0 || ldkh < 0 || ldv < 0 ||
         ldvh < 0 || !(scale > 0.0f) || !isfinite(scale) || !(softcap == 0.0f || softcap >= FLT_MIN) || !isfinite(softcap) || window < 0 ||
-        !rows_apart(tokens_q, ldo, heads_q, ldoh, d_head))
+        ldk >= kMaxStride || ldv >= kMaxStride || !rows_apart(tokens_q, ldo, heads_q, ldoh, d_head))
         return RESQ_ERR_SHAPE;
     if (tokens_q == 0) return RESQ_OK;
     if (!q || (tokens_k > 0 && (!k || !v)) || !cu_q || !cu_k || !out || !workspace) return RESQ_ERR_NULL;

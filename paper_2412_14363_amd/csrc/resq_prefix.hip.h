@@ -65,7 +65,7 @@ __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_
 __device__ __forceinline__ int exponent_of(float x) { return max((int)(__float_as_uint(x) >> 23), 27); }   // x >= 0; bits, 127 is 2^0
 __device__ __forceinline__ float to_half_range(int e) { return two_to(267 - e); }
 
-template <int W, int OCC>
+template <int W, int OCC, bool CAP>
 __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(const PrefixArgs a) {
     using Tile = FlashTile<W>;
     constexpr int KEYS = kPrefixKeys, kTileBytes = KEYS * Tile::kPitch;
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
             for (int i = 0; i < 4; ++i)
                 r.q[s][i] = flash_pack<true>(__uint_as_float(r.q[s][i] << 16) * f, __uint_as_float(r.q[s][i] & 0xFFFF0000u) * f);
         qf = a.scale * two_to(e - 13);
-        if (!(a.softcap > 0.0f)) qf *= 1.44269504088896340736f;
+        if (!CAP) qf *= 1.44269504088896340736f;
     }
     const bool looks = __builtin_amdgcn_ballot_w64(low < end) != 0;   // some row of the wavefront sees something
     const int low_there = low == 0x7FFFFFFF ? 0 : low;                // of a row that is there
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
         }
     };
     static_assert(KEYS == 16 * kPrefixWaves);
-    const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
+    const float inv_cap = CAP ? 1.0f / a.softcap : 0.0f;
 
     int value_e = 27;   // (the exponent of the tile that is attended to, and of all before)
     load_page(begin);
@@ -260,10 +260,13 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
             const bool partly = mask != ~0ull || __builtin_amdgcn_ballot_w64(low_there > key0) != 0;
             const uint64_t mine = mask >> (4 * half);
             const int from = low - key0 - 4 * half;
-            r.template step<KEYS>(kt, vt, f, up, scaled, a.softcap, inv_cap, partly, [&](int kb, int i) {
+            auto sees = [&](int kb, int i) {
                 const int c = 32 * kb + 8 * (i >> 2) + (i & 3);
                 return (mine >> c & 1) != 0 && c >= from;
-            });
+            };
+            const float* by = scaled ? up : nullptr;
+            if (partly) r.template step<KEYS, CAP, false, true>(kt, vt, f, by, a.softcap, inv_cap, sees);
+            else r.template step<KEYS, CAP, false, false>(kt, vt, f, by, a.softcap, inv_cap, sees);
         }
         __syncthreads();
     }

@@ -5,7 +5,7 @@
 //
 // A workgroup has 128 rows, 32 to a wavefront (resq_flash.hip.h); a row is a query and one of the heads that share a K/V head, so that
 // a tile of keys and values in LDS serves all of them, and tiles on the diagonal are few (with four heads to a K/V head 128 rows are
-// 32 queries).  Keys and values come to LDS in tiles of 64 by way of registers, a tile ahead.
+// 32 queries).  Keys and values come to LDS in tiles of 64, a tile ahead.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -109,12 +109,12 @@ __device__ __forceinline__ PromptKeys prompt_keys(const PromptArgs& a, const Pro
     return k;
 }
 
-template <int W, int KEYS, int OCC>
+template <int W, int KEYS, int OCC, bool CAP>
 __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(const PromptArgs a) {
     using Tile = FlashTile<W>;
     constexpr int kTileBytes = KEYS * Tile::kPitch;
-    constexpr int kMoves = kTileBytes / 16 / kPromptThreads;   // pieces of a tile's keys (values) that a thread moves
-    constexpr int kRowsAMove = kPromptThreads / Tile::kPieces;
+    constexpr int kMoves = kTileBytes / 1024 / kPromptWaves;   // of 1024 bytes of a tile's keys (values) that a wavefront fetches
+    constexpr int kRowsAMove = 64 / Tile::kPieces;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values
 
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
@@ -128,11 +128,45 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
     if (piece >= keys.parts) return;
     const int begin = keys.begin + piece * keys.per * KEYS, end = min(keys.end, begin + keys.per * KEYS);
 
+    // ---- tiles of keys and values, straight to LDS: a wavefront's move is some whole rows, a lane's place in it is given, so what is
+    // fetched there is the piece that belongs there ----
+    const uint8_t* k_src = reinterpret_cast<const uint8_t*>(a.k + tile.k0 * a.ldk + hk * a.ldkh);
+    const uint8_t* v_src = reinterpret_cast<const uint8_t*>(a.v + tile.k0 * a.ldv + hk * a.ldvh);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const int my_row = wave * (kMoves * kRowsAMove) + lane / Tile::kPieces;   // of the first move
+    auto fetch = [&](int key0, int buffer) {
+        const uint8_t *k = k_src + key0 * (2 * a.ldk), *v = v_src + key0 * (2 * a.ldv);
+#pragma unroll
+        for (int i = 0; i < kMoves; ++i) {
+            const int row = my_row + i * kRowsAMove;
+            const int pk = min((Tile::key_at(row, lane % Tile::kPieces) - row * Tile::kPitch) >> 4, (a.d >> 3) - 1);   // (channels behind
+            const int pv = min((Tile::value_at(row, lane % Tile::kPieces) - row * Tile::kPitch) >> 4, (a.d >> 3) - 1);   // the head's: any)
+            const uint32_t from = (uint32_t)min(row, end - 1 - key0);   // (keys behind the last: any that is there)
+            const uint32_t to = lds0 + buffer * kTileBytes + (wave * kMoves + i) * 1024;
+            flash_fetch(to, k, from * (uint32_t)(2 * a.ldk) + 16 * pk);
+            flash_fetch(to + 2 * kTileBytes, v, from * (uint32_t)(2 * a.ldv) + 16 * pv);
+        }
+    };
+
+    // ---- which tiles all rows see whole: those come first, then the ones in front of them and behind ----
+    const int last_row = min(tile.row0 + kPromptRows, tile.rows) - 1, shift = tile.nk - tile.nq;
+    const int own0 = (int)a.share(tile.row0) + shift, own1 = (int)a.share(last_row) + shift;
+    const int end_floor = end / KEYS * KEYS;   // (begin is a multiple of KEYS)
+    const int whole0 = min(max((max(own1 - (a.window - 1), 0) + KEYS - 1) / KEYS * KEYS, begin), end_floor);
+    const int whole1 = max(min((own0 + 1) / KEYS * KEYS, end_floor), whole0);
+    const int n_whole = (whole1 - whole0) / KEYS, n_front = (whole0 - begin) / KEYS;
+    const int n_all = (end - begin + KEYS - 1) / KEYS;
+    auto key_of = [&](int n) {
+        const int m = n - n_whole;
+        return m < 0 ? whole0 + n * KEYS : m < n_front ? begin + m * KEYS : whole1 + (m - n_front) * KEYS;
+    };
+    if (n_all > 0) fetch(key_of(0), 0);
+
     // ---- the own row ----
     const int row = tile.row0 + wave * kFlashRows + (lane & 31);
     const bool live = row < tile.rows;
     const int token = (int)a.share(live ? row : 0), head = hk * (int)a.share.d + (live ? row : 0) - token * (int)a.share.d;
-    const int own = live ? token + tile.nk - tile.nq : -1;   // a row that is not there sees nothing
+    const int own = live ? token + shift : -1;   // a row that is not there sees nothing
     FlashRow<W, false> r;
     {
         const uint16_t* src = a.q + (tile.q0 + token) * a.ldq + head * a.ldqh;
@@ -145,64 +179,31 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
         }
     }
     r.clear();
-    // what the wavefront's rows see: all of them [all0, all1), some of them [some0, some1)
-    const int row0 = tile.row0 + wave * kFlashRows, row1 = min(row0 + kFlashRows, tile.rows) - 1;
-    const int shift = tile.nk - tile.nq;
-    const int own0 = (int)a.share(min(row0, tile.rows - 1)) + shift, own1 = (int)a.share(max(row1, 0)) + shift;
-    const bool any = row0 < tile.rows;
-    const int all0 = max(own1 - (a.window - 1), 0), all1 = own0 + 1;
-    const int some0 = max(own0 - (a.window - 1), 0), some1 = any ? own1 + 1 : 0;
-
-    // ---- tiles of keys and values, by way of registers ----
-    const int my_row = t / Tile::kPieces, my_piece = min(t % Tile::kPieces, (a.d >> 3) - 1);   // (channels behind the head's: any)
-    const uint16_t* k_src = a.k + tile.k0 * a.ldk + hk * a.ldkh + 8 * my_piece;
-    const uint16_t* v_src = a.v + tile.k0 * a.ldv + hk * a.ldvh + 8 * my_piece;
-    uint4 kreg[kMoves], vreg[kMoves];
-    auto load = [&](int key0) {
-#pragma unroll
-        for (int i = 0; i < kMoves; ++i) {
-            const int64_t j = min(key0 + my_row + i * kRowsAMove, end - 1);   // (keys behind the last: any that is there)
-            kreg[i] = *reinterpret_cast<const uint4*>(k_src + j * a.ldk);
-            vreg[i] = *reinterpret_cast<const uint4*>(v_src + j * a.ldv);
-        }
-    };
-    auto store = [&](int buffer) {
-        uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
-#pragma unroll
-        for (int i = 0; i < kMoves; ++i) {
-            const int to = my_row + i * kRowsAMove;
-            *reinterpret_cast<uint4*>(kt + Tile::key_at(to, t % Tile::kPieces)) = kreg[i];
-            *reinterpret_cast<uint4*>(vt + Tile::value_at(to, t % Tile::kPieces)) = vreg[i];
-        }
-    };
-    const float inv_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
+    const float inv_cap = CAP ? 1.0f / a.softcap : 0.0f;
     const float inf = __builtin_huge_valf();
     float f[KEYS / 16];
-#pragma unroll
-    for (int g = 0; g < KEYS / 16; ++g) f[g] = a.softcap > 0.0f ? a.scale : a.scale * 1.44269504088896340736f;
+    f[0] = CAP ? a.scale : a.scale * 1.44269504088896340736f;
 
-    if (begin < end) {
-        load(begin);
-        store(0);
-        if (begin + KEYS < end) load(begin + KEYS);
+    flash_landed();
+    int n = 0, buffer = 0;
+    for (; n < n_whole; ++n, buffer ^= 1) {
+        if (n + 1 < n_all) fetch(key_of(n + 1), buffer ^ 1);
+        r.template step<KEYS, CAP, true, false>(lds + buffer * kTileBytes, lds + (2 + buffer) * kTileBytes, f, nullptr, a.softcap, inv_cap,
+                                                [](int, int) { return true; });
+        flash_landed();
     }
-    __syncthreads();
-    int buffer = 0;
-    for (int key0 = begin; key0 < end; key0 += KEYS, buffer ^= 1) {
-        if (key0 + KEYS < end) {
-            store(buffer ^ 1);
-            if (key0 + 2 * KEYS < end) load(key0 + 2 * KEYS);
-        }
-        if (key0 < some1 && key0 + KEYS > some0) {
-            const uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
-            const bool partly = key0 < all0 || key0 + KEYS > all1;
-            const int behind = own - key0 - 4 * half;   // keys from the lane's first one to the row's own
-            r.template step<KEYS>(kt, vt, f, f, false, a.softcap, inv_cap, partly, [&](int kb, int i) {
-                const int c = 32 * kb + 8 * (i >> 2) + (i & 3);
-                return behind >= c && behind - c < a.window;
-            });
-        }
-        __syncthreads();
+    for (; n < n_all; ++n, buffer ^= 1) {
+        const int key0 = key_of(n);
+        if (n + 1 < n_all) fetch(key_of(n + 1), buffer ^ 1);
+        const int behind = own - key0 - 4 * half;   // keys from the lane's first one to the row's own
+        // (a wavefront whose rows see nothing of the tile goes on to the next)
+        if (__builtin_amdgcn_ballot_w64(own >= key0 && own - key0 < a.window + KEYS - 1) != 0)
+            r.template step<KEYS, CAP, true, true>(lds + buffer * kTileBytes, lds + (2 + buffer) * kTileBytes, f, nullptr, a.softcap, inv_cap,
+                                                   [&](int kb, int i) {
+                                                       const int c = 32 * kb + 8 * (i >> 2) + (i & 3);
+                                                       return behind >= c && behind - c < a.window;
+                                                   });
+        flash_landed();
     }
 
     // ---- the result, or this part of it ----

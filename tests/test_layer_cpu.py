@@ -22,7 +22,7 @@ PROMPTS = dict(q=P, ldq=1024, ldqh=128, tokens_q=40, k=P, ldk=256, ldkh=128, v=P
     (dict(tokens_q=-1), SHAPE), (dict(tokens_k=-1), SHAPE), (dict(tokens_q=(1 << 30) + 1, heads_q=1, heads_k=1), SHAPE), (dict(tokens_k=(1 << 30) + 1), SHAPE),
     (dict(tokens_q=1 << 30), SHAPE), (dict(B=0), SHAPE), (dict(B=65536), SHAPE), (dict(heads_q=7), SHAPE), (dict(heads_k=0), SHAPE),
     (dict(heads_q=0), SHAPE), (dict(heads_q=70000, heads_k=70000), SHAPE), (dict(d=4), SHAPE), (dict(d=100), SHAPE), (dict(d=264), SHAPE),
-    (dict(ldq=-1), SHAPE), (dict(ldkh=-8), SHAPE), (dict(ldv=-8), SHAPE), (dict(ldoh=100), SHAPE), (dict(ldo=1023), SHAPE), (dict(scale=0.0), SHAPE),
+    (dict(ldq=-1), SHAPE), (dict(ldkh=-8), SHAPE), (dict(ldv=-8), SHAPE), (dict(ldk=1 << 24), SHAPE), (dict(ldv=1 << 40), SHAPE), (dict(ldoh=100), SHAPE), (dict(ldo=1023), SHAPE), (dict(scale=0.0), SHAPE),
     (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE), (dict(softcap=-1.0), SHAPE),
     (dict(softcap=float("nan")), SHAPE), (dict(softcap=1e-39), SHAPE), (dict(window=-1), SHAPE), (dict(ldq=2048), SHAPE),
     (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(cu_q=None), NULL), (dict(cu_k=None), NULL), (dict(out=None), NULL),
