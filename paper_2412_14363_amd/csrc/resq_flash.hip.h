@@ -126,31 +126,30 @@ struct FlashRow {
         v16f_flash x[KEYS / 32];
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb) x[kb] = scores(kt, kb);
-        if constexpr (CAP) {
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] = soft_cap(x[kb][i] * f[ONE ? 0 : 2 * kb + (i >> 3)], softcap, inv_cap);
-        } else if constexpr (!ONE) {
+        if constexpr (!ONE) {
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[kb][i] *= f[2 * kb + (i >> 3)];
         }
-        const float unit = CAP ? 1.44269504088896340736f : ONE ? f[0] : 1.0f;   // of the scores now
         if constexpr (PARTLY) {
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[kb][i] = sees(kb, i) ? x[kb][i] : -inf;
         }
+        // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
+        // few 2^-24 of the cap, is one of the score's, also where the score is small.
+        const float unit = ONE ? f[0] : 1.0f, bound = softcap * 1.44269504088896340736f, steep = unit * 2.88539008177792681472f * inv_cap;
+        auto tail = [&](float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * steep)); };
         // ---- the running maximum, where a score is 2^kSlack times what it allows ----
         float tops[2] = {x[0][0], x[0][1]};
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[kb][i]);
-        const float top = fmaxf(tops[0], tops[1]) * unit;
+        float top = fmaxf(tops[0], tops[1]);
+        top = CAP ? fmaf(-2.0f * bound, tail(top), bound) : top * unit;
         if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
             const float m_new = fmaxf(m, halves_max(top));
             const float back = __builtin_amdgcn_exp2f(m - m_new);
@@ -161,13 +160,18 @@ struct FlashRow {
         }
         // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
         v4u_flash p[KEYS / 16];
-        const float base = kBias - m;
+        const float base = CAP ? kBias + bound - m : kBias - m;
+        auto weight = [&](int kb, int i) {
+            if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base));
+            const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i]), base));   // (the cap of what is not seen is a number)
+            return PARTLY && x[kb][i] == -inf ? 0.0f : w;
+        };
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                float p0 = __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x[kb][i + 1], unit, base));
+                float p0 = weight(kb, i), p1 = weight(kb, i + 1);
                 sums[0] += p0;
                 sums[1] += p1;
                 if (up) {

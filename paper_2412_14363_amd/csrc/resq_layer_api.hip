@@ -56,7 +56,11 @@ int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
-    launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(kPromptThreads), (size_t)lds, st, a);
+    PromptArgs args = a;
+    args.units = (int)(p.tiles * p.parts);
+    args.fold = args.units * (int64_t)a.heads.d <= 256 * OCC && OCC > 1 ? 256 / (int)a.heads.d : args.units;
+    if (args.fold > args.units) args.fold = args.units;
+    launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(kPromptThreads), (size_t)lds, st, args);
     if (p.parts > 1)
         launch(attend_prompts_join_kernel<KEYS>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(kPromptThreads), 0, st, a);
     return launch_status();

@@ -28,6 +28,7 @@ struct PromptArgs {
     float scale, softcap;
     int window;          // 2^30: none
     int least;           // tiles of keys of a part at least
+    int fold, units;     // from unit `fold` on the order is turned round, see the launch
     uint16_t* out;
     int64_t ldo, ldoh;
     float* lse;
@@ -120,7 +121,9 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     // heads are neighbours in the grid: with 8 of them (or a multiple) each die has a head's keys and values in its own L2
-    const int unit = (int)a.heads(blockIdx.x), hk = (int)blockIdx.x - unit * (int)a.heads.d;
+    int unit = (int)a.heads(blockIdx.x);
+    const int hk = (int)blockIdx.x - unit * (int)a.heads.d;
+    if (unit >= a.fold) unit = a.fold + a.units - 1 - unit;
     const int order = (int)a.parts(unit), piece = unit - order * (int)a.parts.d;
     PromptTile tile;
     if (!prompt_tile(a, order, tile)) return;

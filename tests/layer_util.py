@@ -11,7 +11,8 @@ def rows(q, k, v, first, last, scale, cap, weight_step):
 
     The bounds.  A score is a sum of d products, each exact in fp32, of at most d roundings of 2^-24 of its terms' magnitudes; its
     product with the scale, its difference from the maximum and the exponential's argument are three more, of the score and the
-    maximum; tanh moves it by 2^-22 of the cap.  A weight is off by twice what its score is (its own and the sum's), by its rounding
+    maximum; cap tanh(x / cap) as cap (1 - 2 / (1 + e^(2 x / cap))) is off by 2^-21 of the cap: 2^-22 for the reciprocal's last place, 2^-23 for
+    the sum's and the exponential's, which the slope of 1 / (1 + e), at most 1 / 4 of e's relative error, makes smaller, 2^-23 for the rest.  A weight is off by twice what its score is (its own and the sum's), by its rounding
     as an operand (weight_step, half a step of that type) and by 2^-21 for the exponential and the quotient.  The weighted sum has at
     most as many roundings of 2^-24 as there are keys."""
     x = scale * (q @ k.T)
@@ -22,7 +23,7 @@ def rows(q, k, v, first, last, scale, cap, weight_step):
     off = torch.where(seen, q.shape[1] * 2.0 ** -24 * size + 2.0 ** -22 * x.abs(), 0.0)
     if cap:
         x = cap * torch.tanh(x / cap)
-        off = off + 2.0 ** -22 * cap
+        off = off + 2.0 ** -21 * cap
     x = torch.where(seen, x, -math.inf)
     off = (off.nan_to_num().amax(1) if len(k) else torch.zeros(len(q), dtype=torch.float64)) + 2.0 ** -22 * torch.where(
         some, x.amax(1) if len(k) else 0.0, 0.0).abs()
@@ -143,7 +144,7 @@ def prefix(q, k_pages, v_pages, prefix_len, prefix_table, lens, table, r, scale,
                 off = (size + 2.0 ** -22 * x.abs()).max() + 2.0 ** -22 * x.max().abs()
                 if cap:
                     x = cap * torch.tanh(x / cap)
-                    off = off + 2.0 ** -22 * cap
+                    off = off + 2.0 ** -21 * cap
                 lse[b, i] = torch.logsumexp(x, 0)
                 p = torch.exp(x - lse[b, i])
                 out[b, i] = p @ v
