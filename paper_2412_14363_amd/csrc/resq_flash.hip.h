@@ -48,17 +48,37 @@ __device__ __forceinline__ uint32_t flash_pack(float lo, float hi) {   // rounde
     if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f_flash){lo, hi}, v2h_flash));
     else return pack_bf16_pair(lo, hi);
 }
-__device__ __forceinline__ v2u_flash flash_read_tr(const uint8_t* p) {
-    return __builtin_bit_cast(v2u_flash, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                             (__attribute__((address_space(3))) v4s_flash*)(__attribute__((address_space(3))) uint8_t*)p));
+#define FlashLds __attribute__((address_space(3)))
+__device__ __forceinline__ uint32_t flash_lds(const uint8_t* p) { return (uint32_t)(uintptr_t)(const FlashLds uint8_t*)p; }
+__device__ __forceinline__ v2u_flash flash_read_tr(FlashLds uint8_t* p) {
+    return __builtin_bit_cast(v2u_flash, __builtin_amdgcn_ds_read_tr16_b64_v4i16((FlashLds v4s_flash*)p));
 }
 
 // 16 bytes of each lane from base + off to lds + 16 lane in LDS, on their way past the compiler: it would have every later read of LDS wait
 // for them.  flash_landed() is the wait, and the workgroup's meeting behind it.
 __device__ __forceinline__ void flash_fetch(uint32_t lds, const uint8_t* base, uint32_t off) {
+    // (both are the wavefront's, which the compiler loses sight of where many registers are taken)
+    lds = __builtin_amdgcn_readfirstlane(lds);
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    base = reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readfirstlane((int)at));
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void flash_landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Ends of a wavefront's turn at the matrix cores (it has read all that it needed of the keys, and of the values before), and of its turn
+// at the vector ALU (what it has fetched but the last LATER moves is there).
+__device__ __forceinline__ void flash_after_products() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_setprio 0\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <int LATER>
+__device__ __forceinline__ void flash_after_softmax() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_setprio 3\n\ts_barrier" ::"n"(LATER) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // Layout of a tile: W channels (a multiple of 32) in rows of a power of two of pieces.
 template <int W>
@@ -74,6 +94,16 @@ struct FlashTile {
     __device__ static __forceinline__ int value_at(int row, int piece) {
         return row * kPitch + 16 * (piece ^ (kPieces == 8 ? 4 * ((row >> 1) & 1) : 4 * (row & 3)));
     }
+};
+
+// What goes from one turn of a wavefront to the next: scores and weights of the tile at hand, and its values, which are asked for in front of
+// the softmax where registers allow it.
+template <int W, int KEYS>
+struct FlashTurn {
+    static constexpr int kAhead = W <= 64 || W > 128 ? 0 : KEYS / 16;   // sixteens of keys whose values are asked for in front of the softmax
+    v16f_flash x[KEYS / 32];
+    v4u_flash p[KEYS / 16];
+    v4u_flash v[kAhead ? kAhead : 1][FlashTile<W>::kBlocks];
 };
 
 // A lane's row: its query as the first product's operand, its running maximum (times log2 e) and sum (over the lane's own keys), and
@@ -93,33 +123,183 @@ struct FlashRow {
         m = kFlashNone;
         l = 0.0f;
     }
-    // scores of keys [32 kb, 32 kb + 32) of a tile
-    __device__ __forceinline__ v16f_flash scores(const uint8_t* keys, int kb) const {
+    // keys [32 kb, 32 kb + 32) of a tile, channels 16 t .. 16 t + 15, as the first product's operand.  (A piece's number is in the lower bits of
+    // its place, so that what t does to the address is one exclusive or.)
+    __device__ __forceinline__ v4u_flash keys(const uint8_t* kt, int kb, int t) const {
         const int lane = threadIdx.x & 63;
+        const uint32_t at = ((uint32_t)Tile::key_at(lane & 31, lane >> 5) ^ (32u * t)) + flash_lds(kt);
+        return *reinterpret_cast<const FlashLds v4u_flash*>(reinterpret_cast<const FlashLds uint8_t*>((uintptr_t)at) + 32 * kb * Tile::kPitch);
+    }
+    // scores of keys [32 kb, 32 kb + 32) of a tile
+    __device__ __forceinline__ v16f_flash scores(const uint8_t* kt, int kb) const {
         v16f_flash s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
         for (int t = 0; t < Tile::kSteps; ++t) {
-            const v4u_flash k = *reinterpret_cast<const v4u_flash*>(keys + 32 * kb * Tile::kPitch + Tile::key_at(lane & 31, 2 * t + (lane >> 5)));
-            s = flash_mfma<F16>(k, q[t], s);
+            s = flash_mfma<F16>(keys(kt, kb, t), q[t], s);
         }
         return s;
     }
     // values of keys 16 t .. 16 t + 15 and channels [32 c, 32 c + 32), as the second product's operand
     __device__ __forceinline__ v4u_flash values(const uint8_t* vals, int t, int c) const {
         const int lane = threadIdx.x & 63;
-        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), piece = 4 * c + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-        const uint8_t* p = vals + 16 * t * Tile::kPitch + Tile::value_at(row, piece) + 8 * (lane & 1);
+        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), piece = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        const uint32_t at = ((uint32_t)(Tile::value_at(row, piece) + 8 * (lane & 1)) ^ (64u * c)) + flash_lds(vals);
+        FlashLds uint8_t* p = reinterpret_cast<FlashLds uint8_t*>((uintptr_t)at) + 16 * t * Tile::kPitch;
         const v2u_flash a = flash_read_tr(p), b = flash_read_tr(p + 8 * Tile::kPitch);
         return (v4u_flash){a[0], a[1], b[0], b[1]};
     }
 
+    // ---- the same in two turns, one at the matrix cores and one at the vector ALU ----
+    // weighted sums of the tile before (PV), whose weights and first values are at hand, and scores of this one; what a product needs of
+    // LDS is asked for eight products ahead
+    template <int KEYS, bool PV>
+    __device__ __forceinline__ void products(FlashTurn<W, KEYS>& s, const uint8_t* kt, const uint8_t* vals_before) {
+        constexpr int kAhead = PV ? FlashTurn<W, KEYS>::kAhead : 0, kRest = PV && kAhead ? KEYS / 16 - kAhead : 0;
+        constexpr int kFirst = W <= 128 ? Tile::kSteps : 4;   // (all that registers allow)
+        v4u_flash k[KEYS / 32][Tile::kSteps], v[kRest ? kRest : 1][Tile::kBlocks];
+#pragma unroll
+        for (int t = 0; t < kFirst; ++t) k[0][t] = keys(kt, 0, t);
+#pragma unroll
+        for (int g = 0; g < kRest; ++g)
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) v[g][c] = values(vals_before, kAhead + g, c);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (PV) {
+            if constexpr (kAhead == 0) weigh<KEYS>(s.p, vals_before);
+#pragma unroll
+            for (int g = 0; g < kAhead; ++g)
+#pragma unroll
+                for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(s.v[g][c], s.p[g], acc[c]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int kb = 1; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int t = 0; t < Tile::kSteps; ++t) k[kb][t] = keys(kt, kb, t);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < kRest; ++g)
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(v[g][c], s.p[kAhead + g], acc[c]);
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s.x[kb][i] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < Tile::kSteps; ++t)
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+                s.x[kb] = flash_mfma<F16>(kb == 0 && t >= kFirst ? keys(kt, kb, t) : k[kb][t], q[t], s.x[kb]);
+    }
+    template <int KEYS>
+    __device__ __forceinline__ void weigh_ahead(const FlashTurn<W, KEYS>& s) {
+#pragma unroll
+        for (int g = 0; g < KEYS / 16; ++g)
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(s.v[g][c], s.p[g], acc[c]);
+    }
+    template <int KEYS>
+    __device__ __forceinline__ void weigh(const v4u_flash (&p)[KEYS / 16], const uint8_t* vt) {
+#pragma unroll
+        for (int g = 0; g < KEYS / 16; ++g)
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(values(vt, g, c), p[g], acc[c]);
+    }
+    // The same where some row of the wavefront does not see some key.  Its weight 0 is no part of the row's sum, but would make a NaN of an
+    // infinity or NaN among the key's values: those are left out here.  True: there are some, which belong to the rows that see them.
+    template <int KEYS>
+    __device__ __forceinline__ bool weigh_finite(const v4u_flash (&p)[KEYS / 16], const uint8_t* vt) {
+        typedef short v2s __attribute__((ext_vector_type(2)));
+        constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u, kUp = 0x8000u - kExp;
+        uint32_t found = 0;
+#pragma unroll
+        for (int g = 0; g < KEYS / 16; ++g)
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) {
+                v4u_flash o = values(vt, g, c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t odd = (o[e] & (kExp << 16 | kExp)) + (kUp << 16 | kUp);   // the sign bit of a half that is not finite
+                    found |= odd;
+                    o[e] &= ~__builtin_bit_cast(uint32_t, __builtin_bit_cast(v2s, odd) >> 15);
+                }
+                acc[c] = flash_mfma<F16>(o, p[g], acc[c]);
+            }
+        return __builtin_amdgcn_ballot_w64((found & 0x80008000u) != 0) != 0;
+    }
+    // a value that weigh_finite left out, or 0
+    __device__ static __forceinline__ float odd_value(uint32_t u) {
+        const uint32_t mag = u & 0x7FFFu;
+        if constexpr (F16) return mag < 0x7C00u ? 0.0f : __uint_as_float((u & 0x8000u) << 16 | 0x7F800000u | (mag & 0x3FFu) << 13);
+        return mag < 0x7F80u ? 0.0f : __uint_as_float(u << 16);
+    }
+    // weights of the tile at hand; PARTLY: its weighted sums too, as weigh_finite
+    template <int KEYS, bool CAP, bool PARTLY, typename Sees>
+    __device__ __forceinline__ bool softmax(FlashTurn<W, KEYS>& s, const uint8_t* vt, float unit, float bound, float steep, Sees sees) {
+        constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
+        const float inf = __builtin_huge_valf();
+        if constexpr (!PARTLY) {
+#pragma unroll
+            for (int g = 0; g < FlashTurn<W, KEYS>::kAhead; ++g)
+#pragma unroll
+                for (int c = 0; c < Tile::kBlocks; ++c) s.v[g][c] = values(vt, g, c);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        auto& x = s.x;
+        if constexpr (PARTLY) {
+            const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+            for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3) + 4 * half) ? x[kb][i] : -inf;
+        }
+        // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
+        // few 2^-24 of the cap, is one of the score's, also where the score is small.
+        auto tail = [&](float w) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * steep)); };
+        // ---- the running maximum, where a score is 2^kSlack times what it allows ----
+        float tops[2] = {x[0][0], x[0][1]};
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[kb][i]);
+        float top = fmaxf(tops[0], tops[1]);
+        top = CAP ? fmaf(-2.0f * bound, tail(top), bound) : top * unit;
+        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+            const float m_new = fmaxf(m, halves_max(top));
+            const float back = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= back;
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] *= back;
+        }
+        // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
+        const float base = CAP ? kBias + bound - m : kBias - m;
+        auto weight = [&](int kb, int i) {
+            if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base));
+            const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i]), base));   // (the cap of what is not seen is a number)
+            return PARTLY && x[kb][i] == -inf ? 0.0f : w;
+        };
+        float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float p0 = weight(kb, i), p1 = weight(kb, i + 1);
+                sums[0] += p0;
+                sums[1] += p1;
+                s.p[2 * kb + (i >> 3)][(i & 7) >> 1] = flash_pack<F16>(p0, p1);
+            }
+        l += sums[0] + sums[1];
+        if constexpr (PARTLY) return weigh_finite<KEYS>(s.p, vt);
+        return false;
+    }
     // A tile of KEYS keys.  f[g]: what makes a score of keys 16 g .. 16 g + 15 one of base 2, or (CAP) what it is multiplied with in
     // front of the cap; ONE: all of them are f[0].  up (null: 1): what those keys' weights are multiplied with for the product with the values.
-    // PARTLY: rows do not see some keys; sees(kb, i): whether the lane's row sees its key i of the block kb.
+    // PARTLY: rows do not see some keys; sees(key): whether the lane's row sees that key of the tile.
     template <int KEYS, bool CAP, bool ONE, bool PARTLY, typename Sees>
-    __device__ __forceinline__ void step(const uint8_t* kt, const uint8_t* vt, const float (&f)[KEYS / 16], const float* up, float softcap,
+    __device__ __forceinline__ bool step(const uint8_t* kt, const uint8_t* vt, const float (&f)[KEYS / 16], const float* up, float softcap,
                                          float inv_cap, Sees sees) {
         constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
         const float inf = __builtin_huge_valf();
@@ -133,10 +313,11 @@ struct FlashRow {
                 for (int i = 0; i < 16; ++i) x[kb][i] *= f[2 * kb + (i >> 3)];
         }
         if constexpr (PARTLY) {
+            const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] = sees(kb, i) ? x[kb][i] : -inf;
+                for (int i = 0; i < 16; ++i) x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3) + 4 * half) ? x[kb][i] : -inf;
         }
         // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
         // few 2^-24 of the cap, is one of the score's, also where the score is small.
@@ -182,68 +363,9 @@ struct FlashRow {
             }
         l += sums[0] + sums[1];
         // ---- weighted sums of values ----
-        // A key that some row of the wavefront does not see has weight 0 there, which an infinity or NaN among its values would
-        // not care about: such values are left out of the product, and what they make of a row that sees them is added apart.
-        constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u, kOne = F16 ? 0x3C00u : 0x3F80u;
-        bool odd = false;
-        if constexpr (PARTLY) {
-            uint32_t found = 0;
-#pragma unroll
-            for (int s = 0; s < KEYS / 16; ++s)
-#pragma unroll
-                for (int c = 0; c < Tile::kBlocks; ++c) {
-                    const v4u_flash o = values(vt, s, c);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) found |= (o[e] & (kExp << 16 | kExp)) + ((0x8000u - kExp) << 16 | (0x8000u - kExp));
-                }
-            odd = __builtin_amdgcn_ballot_w64((found & 0x80008000u) != 0) != 0;
-        }
-        if (!odd) {
-#pragma unroll
-            for (int s = 0; s < KEYS / 16; ++s)
-#pragma unroll
-                for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(values(vt, s, c), p[s], acc[c]);
-            return;
-        }
-        if constexpr (!PARTLY) return;
-        v4u_flash one[KEYS / 16];   // 1 where the row sees the key
-#pragma unroll
-        for (int s = 0; s < KEYS / 16; ++s)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 8 * (s & 1) + 2 * e;
-                one[s][e] = (sees(s >> 1, i) ? kOne : 0u) | (sees(s >> 1, i + 1) ? kOne << 16 : 0u);
-            }
-        // kind 0: finite values, with their weights; 1, 2, 3: infinities, negative ones, NaN, counted
-#pragma unroll 1
-        for (int kind = 0; kind < 4; ++kind) {
-#pragma unroll
-            for (int c = 0; c < Tile::kBlocks; ++c) {
-                v16f_flash sum;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i] = kind == 0 ? acc[c][i] : 0.0f;
-#pragma unroll
-                for (int s = 0; s < KEYS / 16; ++s) {
-                    v4u_flash o = values(vt, s, c), w;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t two = 0;
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t u = o[e] >> (16 * k) & 0xFFFFu, mag = u & 0x7FFFu;
-                            const int is = mag < kExp ? 0 : mag > kExp ? 3 : u >> 15 ? 2 : 1;
-                            two |= (is != kind ? 0u : kind == 0 ? u : kOne) << (16 * k);
-                        }
-                        o[e] = two;
-                        w[e] = kind == 0 ? p[s][e] : one[s][e];
-                    }
-                    sum = flash_mfma<F16>(o, w, sum);
-                }
-                const float what = kind == 1 ? inf : kind == 2 ? -inf : __builtin_nanf("");
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[c][i] = kind == 0 ? sum[i] : sum[i] > 0.0f ? acc[c][i] + what : acc[c][i];
-            }
-        }
+        if constexpr (PARTLY) return weigh_finite<KEYS>(p, vt);
+        weigh<KEYS>(p, vt);
+        return false;
     }
 };
 

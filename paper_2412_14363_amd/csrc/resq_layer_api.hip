@@ -23,7 +23,8 @@ constexpr int kMaxHead = 256;
 
 // sizes that both entries of the prompts' attention check, and what they have in common
 struct PromptPlan {
-    int64_t tiles;       // of 128 rows, at most
+    int waves;           // of a workgroup
+    int64_t tiles;       // of its rows, at most
     int keys, parts, least;
     size_t acc, bytes;   // workspace: maxima and sums, weighted sums behind them
 };
@@ -33,36 +34,34 @@ bool prompt_plan(PromptPlan& p, int64_t tokens_q, int64_t tokens_k, int64_t B, i
         return false;
     const int64_t share = heads_q / heads_k;
     if (tokens_q * heads_q > kInt32Max - 65536) return false;   // rows are counted in 32 bits
-    p.tiles = (tokens_q * share + B * (kPromptRows - 1)) / kPromptRows;
+    p.waves = d <= 64 ? 4 : 8;
+    const int rows = prompt_rows(p.waves);
+    p.tiles = (tokens_q * share + B * (rows - 1)) / rows;
     p.keys = d <= 128 ? 64 : 32;
     p.least = 512 / p.keys;
     const int64_t units = p.tiles * heads_k;
-    int64_t parts = units >= 512 || units == 0 ? 1 : (1024 + units - 1) / units;
+    int64_t parts = units >= 256 || units == 0 ? 1 : (512 + units - 1) / units;
     const int64_t most = (tokens_k / p.keys + p.least) / p.least;
     if (parts > most) parts = most;
     p.parts = (int)(parts > 64 ? 64 : parts);
-    if (!launch_fits(units * p.parts, kPromptThreads) || units * p.parts > kInt32Max) return false;
+    if (!launch_fits(units * p.parts, 64 * p.waves) || units * p.parts > kInt32Max) return false;
     const size_t slots = p.parts > 1 ? (size_t)units * p.parts : 0;
-    p.acc = slots * kPromptRows * 2 * sizeof(float);
-    p.bytes = p.acc + slots * kPromptRows * d * sizeof(float);
+    p.acc = slots * rows * 2 * sizeof(float);
+    p.bytes = p.acc + slots * rows * d * sizeof(float);
     if (p.bytes == 0) p.bytes = 256;
     return true;
 }
 
-template <int W, int KEYS, int OCC>
+template <int W, int KEYS, int WAVES, int OCC>
 int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
-    const int lds = 4 * KEYS * FlashTile<W>::kPitch;
-    const auto kernel = a.softcap > 0.0f ? attend_prompts_kernel<W, KEYS, OCC, true> : attend_prompts_kernel<W, KEYS, OCC, false>;
+    const int lds = 6 * KEYS * FlashTile<W>::kPitch;
+    const auto kernel = a.softcap > 0.0f ? attend_prompts_kernel<W, KEYS, WAVES, OCC, true> : attend_prompts_kernel<W, KEYS, WAVES, OCC, false>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
-    PromptArgs args = a;
-    args.units = (int)(p.tiles * p.parts);
-    args.fold = args.units * (int64_t)a.heads.d <= 256 * OCC && OCC > 1 ? 256 / (int)a.heads.d : args.units;
-    if (args.fold > args.units) args.fold = args.units;
-    launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(kPromptThreads), (size_t)lds, st, args);
+    launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(64 * WAVES), (size_t)lds, st, a);
     if (p.parts > 1)
-        launch(attend_prompts_join_kernel<KEYS>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(kPromptThreads), 0, st, a);
+        launch(attend_prompts_join_kernel<KEYS, WAVES>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(64 * WAVES), 0, st, a);
     return launch_status();
 }
 
@@ -169,11 +168,11 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
     a.part_ml = static_cast<float*>(workspace);
     a.part_acc = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + p.acc);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (d_head <= 64) return launch_prompts<64, 64, 2>(a, p, st);
-    if (d_head <= 96) return launch_prompts<96, 64, 2>(a, p, st);
-    if (d_head <= 128) return launch_prompts<128, 64, 2>(a, p, st);
-    if (d_head <= 192) return launch_prompts<192, 32, 1>(a, p, st);
-    return launch_prompts<256, 32, 1>(a, p, st);
+    if (d_head <= 64) return launch_prompts<64, 64, 4, 3>(a, p, st);
+    if (d_head <= 96) return launch_prompts<96, 64, 8, 2>(a, p, st);
+    if (d_head <= 128) return launch_prompts<128, 64, 8, 2>(a, p, st);
+    if (d_head <= 192) return launch_prompts<192, 32, 8, 2>(a, p, st);
+    return launch_prompts<256, 32, 8, 2>(a, p, st);
 }
 
 size_t resq_attend_kv_prefix_workspace_bytes(int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head) {

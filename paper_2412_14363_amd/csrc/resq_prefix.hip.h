@@ -258,12 +258,8 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
         if (looks) {
             const uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
             const bool partly = mask != ~0ull || __builtin_amdgcn_ballot_w64(low_there > key0) != 0;
-            const uint64_t mine = mask >> (4 * half);
-            const int from = low - key0 - 4 * half;
-            auto sees = [&](int kb, int i) {
-                const int c = 32 * kb + 8 * (i >> 2) + (i & 3);
-                return (mine >> c & 1) != 0 && c >= from;
-            };
+            const int from = low - key0;
+            auto sees = [&](int key) { return (mask >> key & 1) != 0 && key >= from; };
             const float* by = scaled ? up : nullptr;
             if (partly) r.template step<KEYS, CAP, false, true>(kt, vt, f, by, a.softcap, inv_cap, sees);
             else r.template step<KEYS, CAP, false, false>(kt, vt, f, by, a.softcap, inv_cap, sees);

@@ -14,9 +14,8 @@
 
 namespace resq {
 
-constexpr int kPromptThreads = 256;
-constexpr int kPromptWaves = kPromptThreads / 64;
-constexpr int kPromptRows = kFlashRows * kPromptWaves;   // of a workgroup
+constexpr int kPromptWaves = 8;   // of a workgroup at most
+constexpr __host__ __device__ int prompt_rows(int waves) { return kFlashRows * waves; }   // of a workgroup
 
 struct PromptArgs {
     const uint16_t *q, *k, *v;
@@ -28,7 +27,6 @@ struct PromptArgs {
     float scale, softcap;
     int window;          // 2^30: none
     int least;           // tiles of keys of a part at least
-    int fold, units;     // from unit `fold` on the order is turned round, see the launch
     uint16_t* out;
     int64_t ldo, ldoh;
     float* lse;
@@ -44,7 +42,9 @@ struct PromptTile {
 
 // The tile with the number `at` among all sequences' tiles, counted from the last one (later rows see more keys: the longest work
 // comes first).  False where there are not so many.
+template <int WAVES>
 __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int at, PromptTile& tile) {
+    constexpr int kPromptThreads = 64 * WAVES, kPromptRows = prompt_rows(WAVES);
     __shared__ int part[kPromptWaves], found[5];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     auto first = [&](const int32_t* cu, int b, int most) { return min(max(cu[b], 0), most); };
@@ -61,7 +61,7 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int at, PromptT
     __syncthreads();
     int total = 0, before = 0;
 #pragma unroll
-    for (int w = 0; w < kPromptWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w == wave) before = total;
         total += part[w];
     }
@@ -96,10 +96,10 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int at, PromptT
 struct PromptKeys {
     int begin, end, per, parts;
 };
-template <int KEYS>
+template <int WAVES, int KEYS>
 __device__ __forceinline__ PromptKeys prompt_keys(const PromptArgs& a, const PromptTile& t) {
     PromptKeys k;
-    const int last = min(t.row0 + kPromptRows, t.rows) - 1, shift = t.nk - t.nq;
+    const int last = min(t.row0 + prompt_rows(WAVES), t.rows) - 1, shift = t.nk - t.nq;
     const int own0 = (int)a.share(t.row0) + shift, own1 = (int)a.share(last) + shift;
     k.end = max(own1 + 1, 0);   // at most nk
     k.begin = min(max(own0 - (a.window - 1), 0), k.end) / KEYS * KEYS;
@@ -110,60 +110,67 @@ __device__ __forceinline__ PromptKeys prompt_keys(const PromptArgs& a, const Pro
     return k;
 }
 
-template <int W, int KEYS, int OCC, bool CAP>
-__global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(const PromptArgs a) {
+// WAVES: 8, in two groups half a tile apart, or 4; OCC: wavefronts to a SIMD
+template <int W, int KEYS, int WAVES, int OCC, bool CAP>
+__global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const PromptArgs a) {
     using Tile = FlashTile<W>;
-    constexpr int kTileBytes = KEYS * Tile::kPitch;
-    constexpr int kMoves = kTileBytes / 1024 / kPromptWaves;   // of 1024 bytes of a tile's keys (values) that a wavefront fetches
+    constexpr bool kPair = WAVES == 8;
+    constexpr int kTileBytes = KEYS * Tile::kPitch, kPromptRows = prompt_rows(WAVES);
+    constexpr int kMoves = kTileBytes / 1024 / 4;   // of 1024 bytes of a tile that a wavefront fetches
     constexpr int kRowsAMove = 64 / Tile::kPieces;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // three tiles of keys, three of values
 
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), group = kPair ? wave >> 2 : 0;
     // heads are neighbours in the grid: with 8 of them (or a multiple) each die has a head's keys and values in its own L2
-    int unit = (int)a.heads(blockIdx.x);
-    const int hk = (int)blockIdx.x - unit * (int)a.heads.d;
-    if (unit >= a.fold) unit = a.fold + a.units - 1 - unit;
+    const int unit = (int)a.heads(blockIdx.x), hk = (int)blockIdx.x - unit * (int)a.heads.d;
     const int order = (int)a.parts(unit), piece = unit - order * (int)a.parts.d;
     PromptTile tile;
-    if (!prompt_tile(a, order, tile)) return;
-    const PromptKeys keys = prompt_keys<KEYS>(a, tile);
+    if (!prompt_tile<WAVES>(a, order, tile)) return;
+    const PromptKeys keys = prompt_keys<WAVES, KEYS>(a, tile);
     if (piece >= keys.parts) return;
     const int begin = keys.begin + piece * keys.per * KEYS, end = min(keys.end, begin + keys.per * KEYS);
+    const int n_all = (end - begin + KEYS - 1) / KEYS;
 
-    // ---- tiles of keys and values, straight to LDS: a wavefront's move is some whole rows, a lane's place in it is given, so what is
-    // fetched there is the piece that belongs there ----
+    // ---- tiles straight to LDS, keys by the first group and values by the second: a wavefront's move is some whole rows, a lane's place
+    // in it is given, so what is fetched there is the piece that belongs there ----
     const uint8_t* k_src = reinterpret_cast<const uint8_t*>(a.k + tile.k0 * a.ldk + hk * a.ldkh);
     const uint8_t* v_src = reinterpret_cast<const uint8_t*>(a.v + tile.k0 * a.ldv + hk * a.ldvh);
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    const int my_row = wave * (kMoves * kRowsAMove) + lane / Tile::kPieces;   // of the first move
-    auto fetch = [&](int key0, int buffer) {
-        const uint8_t *k = k_src + key0 * (2 * a.ldk), *v = v_src + key0 * (2 * a.ldv);
-#pragma unroll
-        for (int i = 0; i < kMoves; ++i) {
-            const int row = my_row + i * kRowsAMove;
-            const int pk = min((Tile::key_at(row, lane % Tile::kPieces) - row * Tile::kPitch) >> 4, (a.d >> 3) - 1);   // (channels behind
-            const int pv = min((Tile::value_at(row, lane % Tile::kPieces) - row * Tile::kPitch) >> 4, (a.d >> 3) - 1);   // the head's: any)
-            const uint32_t from = (uint32_t)min(row, end - 1 - key0);   // (keys behind the last: any that is there)
-            const uint32_t to = lds0 + buffer * kTileBytes + (wave * kMoves + i) * 1024;
-            flash_fetch(to, k, from * (uint32_t)(2 * a.ldk) + 16 * pk);
-            flash_fetch(to + 2 * kTileBytes, v, from * (uint32_t)(2 * a.ldv) + 16 * pv);
-        }
-    };
-
-    // ---- which tiles all rows see whole: those come first, then the ones in front of them and behind ----
-    const int last_row = min(tile.row0 + kPromptRows, tile.rows) - 1, shift = tile.nk - tile.nq;
-    const int own0 = (int)a.share(tile.row0) + shift, own1 = (int)a.share(last_row) + shift;
+    const int my_row = (wave & 3) * (kMoves * kRowsAMove) + lane / Tile::kPieces;   // of the first move
+    // tiles that all rows see whole come first, then the ones in front of them and behind
+    const int shift = tile.nk - tile.nq;
+    const int own0 = (int)a.share(tile.row0) + shift, own1 = (int)a.share(min(tile.row0 + kPromptRows, tile.rows) - 1) + shift;
     const int end_floor = end / KEYS * KEYS;   // (begin is a multiple of KEYS)
     const int whole0 = min(max((max(own1 - (a.window - 1), 0) + KEYS - 1) / KEYS * KEYS, begin), end_floor);
     const int whole1 = max(min((own0 + 1) / KEYS * KEYS, end_floor), whole0);
     const int n_whole = (whole1 - whole0) / KEYS, n_front = (whole0 - begin) / KEYS;
-    const int n_all = (end - begin + KEYS - 1) / KEYS;
     auto key_of = [&](int n) {
         const int m = n - n_whole;
         return m < 0 ? whole0 + n * KEYS : m < n_front ? begin + m * KEYS : whole1 + (m - n_front) * KEYS;
     };
-    if (n_all > 0) fetch(key_of(0), 0);
+    auto fetch_one = [&](int n, bool vals) __attribute__((always_inline)) {
+        const int key0 = key_of(n), last = end - 1 - key0;
+        const int64_t ld2 = 2 * (vals ? a.ldv : a.ldk);
+        const uint8_t* from = (vals ? v_src : k_src) + key0 * ld2;
+        const uint32_t to = flash_lds(lds) + (3 * vals + n % 3) * kTileBytes + (wave & 3) * kMoves * 1024;
+#pragma unroll
+        for (int i = 0; i < kMoves; ++i) {
+            const int row = my_row + i * kRowsAMove, place = vals ? Tile::value_at(row, lane % Tile::kPieces) : Tile::key_at(row, lane % Tile::kPieces);
+            const int piece = min((place % Tile::kPitch) >> 4, (a.d >> 3) - 1);   // (channels behind the head's: any)
+            flash_fetch(to + i * 1024, from, (uint32_t)min(row, last) * (uint32_t)ld2 + 16 * piece);   // (keys behind the last: any that is there)
+        }
+    };
+    auto fetch = [&](int n) __attribute__((always_inline)) {
+        if constexpr (kPair) {
+            fetch_one(n, group != 0);
+        } else {
+            fetch_one(n, false);
+            fetch_one(n, true);
+        }
+    };
+    constexpr int kFetch = kPair ? kMoves : 2 * kMoves;   // of a wavefront for a tile
+    if (n_all > 0) fetch(0);
+    if (n_all > 1) fetch(1);
 
     // ---- the own row ----
     const int row = tile.row0 + wave * kFlashRows + (lane & 31);
@@ -182,31 +189,81 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
         }
     }
     r.clear();
-    const float inv_cap = CAP ? 1.0f / a.softcap : 0.0f;
     const float inf = __builtin_huge_valf();
-    float f[KEYS / 16];
-    f[0] = CAP ? a.scale : a.scale * 1.44269504088896340736f;
+    const float factor = CAP ? a.scale : a.scale * 1.44269504088896340736f, bound = CAP ? a.softcap * 1.44269504088896340736f : 0.0f;
+    const float steep = CAP ? a.scale * 2.88539008177792681472f / a.softcap : 0.0f;
 
+    // ---- Two groups of wavefronts, one of each to a SIMD, half a tile apart: while one is at the matrix cores the other is at the vector ALU. ----
+    FlashTurn<W, KEYS> s;
+    auto keys_in = [&](int n) { return lds + n % 3 * kTileBytes; };
+    auto values_in = [&](int n) { return lds + (3 + n % 3) * kTileBytes; };
     flash_landed();
-    int n = 0, buffer = 0;
-    for (; n < n_whole; ++n, buffer ^= 1) {
-        if (n + 1 < n_all) fetch(key_of(n + 1), buffer ^ 1);
-        r.template step<KEYS, CAP, true, false>(lds + buffer * kTileBytes, lds + (2 + buffer) * kTileBytes, f, nullptr, a.softcap, inv_cap,
-                                                [](int, int) { return true; });
-        flash_landed();
+    if (kPair && group) flash_after_products();
+    uint64_t odd = 0;   // tiles with values that are not finite, of those behind the whole ones (at most 512 / KEYS + 4)
+    int n = 0;
+    if (n_whole > 0) {
+        auto softmax = [&]() __attribute__((always_inline)) {
+            flash_after_products();
+            if (n + 2 < n_all) fetch(n + 2);
+            r.template softmax<KEYS, CAP, false>(s, values_in(n), factor, bound, steep, [](int) { return true; });
+            if (n + 2 < n_all) flash_after_softmax<kFetch>();
+            else flash_after_softmax<0>();
+            ++n;
+        };
+        r.template products<KEYS, false>(s, keys_in(0), nullptr);
+        softmax();
+        while (n < n_whole) {
+            r.template products<KEYS, true>(s, keys_in(n), values_in(n + 2));
+            softmax();
+        }
+        if constexpr (FlashTurn<W, KEYS>::kAhead == KEYS / 16) r.template weigh_ahead<KEYS>(s);
+        else r.template weigh<KEYS>(s.p, values_in(n + 2));
     }
-    for (; n < n_all; ++n, buffer ^= 1) {
-        const int key0 = key_of(n);
-        if (n + 1 < n_all) fetch(key_of(n + 1), buffer ^ 1);
-        const int behind = own - key0 - 4 * half;   // keys from the lane's first one to the row's own
-        // (a wavefront whose rows see nothing of the tile goes on to the next)
-        if (__builtin_amdgcn_ballot_w64(own >= key0 && own - key0 < a.window + KEYS - 1) != 0)
-            r.template step<KEYS, CAP, true, true>(lds + buffer * kTileBytes, lds + (2 + buffer) * kTileBytes, f, nullptr, a.softcap, inv_cap,
-                                                   [&](int kb, int i) {
-                                                       const int c = 32 * kb + 8 * (i >> 2) + (i & 3);
-                                                       return behind >= c && behind - c < a.window;
-                                                   });
-        flash_landed();
+    for (; n < n_all; ++n) {
+        r.template products<KEYS, false>(s, keys_in(n), nullptr);
+        flash_after_products();
+        if (n + 2 < n_all) fetch(n + 2);
+        const int behind = own - key_of(n);   // keys from the tile's first one to the row's own
+        odd |= (uint64_t)r.template softmax<KEYS, CAP, true>(s, values_in(n), factor, bound, steep,
+                                                             [&](int key) { return (unsigned)(behind - key) < (unsigned)a.window; })
+               << (n - n_whole);
+        if (n + 2 < n_all) flash_after_softmax<kFetch>();
+        else flash_after_softmax<0>();
+    }
+    if (!kPair && group) flash_after_products();
+
+    // ---- what infinities and NaN among the values make of the rows that see them, one after the other ----
+    for (; odd != 0; odd &= odd - 1) {
+        const int key0 = key_of(n_whole + __builtin_ctzll(odd));
+#pragma unroll 1
+        for (int key = key0; key < min(key0 + KEYS, end); ++key) {
+            const uint16_t *k = a.k + (tile.k0 + key) * a.ldk + hk * a.ldkh, *v = a.v + (tile.k0 + key) * a.ldv + hk * a.ldvh;
+            float x = 0.0f;
+            int d = a.d;   // (compared where it is needed, not in front of everything)
+            asm volatile("" : "+s"(d));
+#pragma unroll
+            for (int s = 0; s < Tile::kSteps; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int ch = 16 * s + 8 * half + e;
+                    const float of_q = bf16_bits_to_f32(r.q[s][e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
+                    if (ch < d) x = fmaf(of_q, bf16_bits_to_f32(k[ch]), x);
+                }
+            x = halves_sum(x);
+            x = CAP ? fmaf(-2.0f * bound, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * steep)), bound) : x * factor;
+            if ((unsigned)(own - key) >= (unsigned)a.window) continue;
+            const float w = __builtin_amdgcn_exp2f(x - r.m);
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int ch = 32 * c + 8 * (i >> 2) + 4 * half + (i & 3);
+                    if (ch < d) {
+                        const float o = r.odd_value(v[ch]);
+                        r.acc[c][i] = o == 0.0f ? r.acc[c][i] : fmaf(w, o, r.acc[c][i]);
+                    }
+                }
+        }
     }
 
     // ---- the result, or this part of it ----
@@ -242,12 +299,13 @@ __global__ __launch_bounds__(kPromptThreads, OCC) void attend_prompts_kernel(con
 }
 
 // Joins the parts of tiles that have several: m = max m_i, f_i = 2^(m_i - m), out = sum f_i acc_i / sum f_i l_i, lse = m ln 2 + ln sum f_i l_i
-template <int KEYS>
-__global__ __launch_bounds__(kPromptThreads) void attend_prompts_join_kernel(const PromptArgs a) {
+template <int KEYS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attend_prompts_join_kernel(const PromptArgs a) {
+    constexpr int kPromptThreads = 64 * WAVES, kPromptRows = prompt_rows(WAVES);
     const int order = (int)a.heads(blockIdx.x), hk = (int)blockIdx.x - order * (int)a.heads.d;
     PromptTile tile;
-    if (!prompt_tile(a, order, tile)) return;
-    const PromptKeys keys = prompt_keys<KEYS>(a, tile);
+    if (!prompt_tile<WAVES>(a, order, tile)) return;
+    const PromptKeys keys = prompt_keys<WAVES, KEYS>(a, tile);
     if (keys.parts == 1) return;
     const int fours = a.d >> 2, rows = min(kPromptRows, tile.rows - tile.row0);
     const int64_t slot = ((int64_t)order * a.heads.d + hk) * a.parts.d;
