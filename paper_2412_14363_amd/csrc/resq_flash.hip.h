@@ -73,6 +73,11 @@ __device__ __forceinline__ void flash_after_products() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_setprio 0\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
+__device__ __forceinline__ void flash_after_making() {   // ... where it writes to LDS itself
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_setprio 3\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 template <int LATER>
 __device__ __forceinline__ void flash_after_softmax() {
     __builtin_amdgcn_sched_barrier(0);
@@ -98,9 +103,9 @@ struct FlashTile {
 
 // What goes from one turn of a wavefront to the next: scores and weights of the tile at hand, and its values, which are asked for in front of
 // the softmax where registers allow it.
-template <int W, int KEYS>
+template <int W, int KEYS, int AHEAD>   // AHEAD: sixteens of keys whose values are asked for in front of the softmax
 struct FlashTurn {
-    static constexpr int kAhead = W <= 64 || W > 128 ? 0 : KEYS / 16;   // sixteens of keys whose values are asked for in front of the softmax
+    static constexpr int kAhead = AHEAD;
     v16f_flash x[KEYS / 32];
     v4u_flash p[KEYS / 16];
     v4u_flash v[kAhead ? kAhead : 1][FlashTile<W>::kBlocks];
@@ -130,17 +135,6 @@ struct FlashRow {
         const uint32_t at = ((uint32_t)Tile::key_at(lane & 31, lane >> 5) ^ (32u * t)) + flash_lds(kt);
         return *reinterpret_cast<const FlashLds v4u_flash*>(reinterpret_cast<const FlashLds uint8_t*>((uintptr_t)at) + 32 * kb * Tile::kPitch);
     }
-    // scores of keys [32 kb, 32 kb + 32) of a tile
-    __device__ __forceinline__ v16f_flash scores(const uint8_t* kt, int kb) const {
-        v16f_flash s;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-        for (int t = 0; t < Tile::kSteps; ++t) {
-            s = flash_mfma<F16>(keys(kt, kb, t), q[t], s);
-        }
-        return s;
-    }
     // values of keys 16 t .. 16 t + 15 and channels [32 c, 32 c + 32), as the second product's operand
     __device__ __forceinline__ v4u_flash values(const uint8_t* vals, int t, int c) const {
         const int lane = threadIdx.x & 63;
@@ -151,12 +145,12 @@ struct FlashRow {
         return (v4u_flash){a[0], a[1], b[0], b[1]};
     }
 
-    // ---- the same in two turns, one at the matrix cores and one at the vector ALU ----
+    // ---- a tile in two turns, one at the matrix cores and one at the vector ALU ----
     // weighted sums of the tile before (PV), whose weights and first values are at hand, and scores of this one; what a product needs of
     // LDS is asked for eight products ahead
-    template <int KEYS, bool PV>
-    __device__ __forceinline__ void products(FlashTurn<W, KEYS>& s, const uint8_t* kt, const uint8_t* vals_before) {
-        constexpr int kAhead = PV ? FlashTurn<W, KEYS>::kAhead : 0, kRest = PV && kAhead ? KEYS / 16 - kAhead : 0;
+    template <int KEYS, bool PV, int AHEAD>
+    __device__ __forceinline__ void products(FlashTurn<W, KEYS, AHEAD>& s, const uint8_t* kt, const uint8_t* vals_before) {
+        constexpr int kAhead = PV ? AHEAD : 0, kRest = PV && kAhead ? KEYS / 16 - kAhead : 0;
         constexpr int kFirst = W <= 128 ? Tile::kSteps : 4;   // (all that registers allow)
         v4u_flash k[KEYS / 32][Tile::kSteps], v[kRest ? kRest : 1][Tile::kBlocks];
 #pragma unroll
@@ -193,12 +187,12 @@ struct FlashRow {
             for (int kb = 0; kb < KEYS / 32; ++kb)
                 s.x[kb] = flash_mfma<F16>(kb == 0 && t >= kFirst ? keys(kt, kb, t) : k[kb][t], q[t], s.x[kb]);
     }
-    template <int KEYS>
-    __device__ __forceinline__ void weigh_ahead(const FlashTurn<W, KEYS>& s) {
+    template <int KEYS, int AHEAD>
+    __device__ __forceinline__ void weigh_rest(const FlashTurn<W, KEYS, AHEAD>& s, const uint8_t* vt) {
 #pragma unroll
         for (int g = 0; g < KEYS / 16; ++g)
 #pragma unroll
-            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(s.v[g][c], s.p[g], acc[c]);
+            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] = flash_mfma<F16>(g < AHEAD ? s.v[g < AHEAD ? g : 0][c] : values(vt, g, c), s.p[g], acc[c]);
     }
     template <int KEYS>
     __device__ __forceinline__ void weigh(const v4u_flash (&p)[KEYS / 16], const uint8_t* vt) {
@@ -235,26 +229,27 @@ struct FlashRow {
         if constexpr (F16) return mag < 0x7C00u ? 0.0f : __uint_as_float((u & 0x8000u) << 16 | 0x7F800000u | (mag & 0x3FFu) << 13);
         return mag < 0x7F80u ? 0.0f : __uint_as_float(u << 16);
     }
-    // weights of the tile at hand; PARTLY: its weighted sums too, as weigh_finite
-    template <int KEYS, bool CAP, bool PARTLY, typename Sees>
-    __device__ __forceinline__ bool softmax(FlashTurn<W, KEYS>& s, const uint8_t* vt, float unit, float bound, float steep, Sees sees) {
+    template <int KEYS, int AHEAD>
+    __device__ __forceinline__ void ask_ahead(FlashTurn<W, KEYS, AHEAD>& s, const uint8_t* vt) {
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g)
+#pragma unroll
+            for (int c = 0; c < Tile::kBlocks; ++c) s.v[g][c] = values(vt, g, c);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // scores of keys that the row does not see become -inf; sees(c): whether it sees key c + 4 half of the tile
+    template <int KEYS, int AHEAD, typename Sees>
+    __device__ __forceinline__ void mask(FlashTurn<W, KEYS, AHEAD>& s, Sees sees) {
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s.x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3)) ? s.x[kb][i] : -__builtin_huge_valf();
+    }
+    // Weights of the tile at hand; MASKED: there may be scores of -inf.
+    template <int KEYS, bool CAP, bool MASKED, int AHEAD>
+    __device__ __forceinline__ void softmax(FlashTurn<W, KEYS, AHEAD>& s, float unit, float bound, float steep) {
         constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
-        const float inf = __builtin_huge_valf();
-        if constexpr (!PARTLY) {
-#pragma unroll
-            for (int g = 0; g < FlashTurn<W, KEYS>::kAhead; ++g)
-#pragma unroll
-                for (int c = 0; c < Tile::kBlocks; ++c) s.v[g][c] = values(vt, g, c);
-            __builtin_amdgcn_sched_barrier(0);
-        }
         auto& x = s.x;
-        if constexpr (PARTLY) {
-            const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3) + 4 * half) ? x[kb][i] : -inf;
-        }
         // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
         // few 2^-24 of the cap, is one of the score's, also where the score is small.
         auto tail = [&](float w) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * steep)); };
@@ -279,7 +274,7 @@ struct FlashRow {
         auto weight = [&](int kb, int i) {
             if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base));
             const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i]), base));   // (the cap of what is not seen is a number)
-            return PARTLY && x[kb][i] == -inf ? 0.0f : w;
+            return MASKED && x[kb][i] == -__builtin_huge_valf() ? 0.0f : w;
         };
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -292,80 +287,6 @@ struct FlashRow {
                 s.p[2 * kb + (i >> 3)][(i & 7) >> 1] = flash_pack<F16>(p0, p1);
             }
         l += sums[0] + sums[1];
-        if constexpr (PARTLY) return weigh_finite<KEYS>(s.p, vt);
-        return false;
-    }
-    // A tile of KEYS keys.  f[g]: what makes a score of keys 16 g .. 16 g + 15 one of base 2, or (CAP) what it is multiplied with in
-    // front of the cap; ONE: all of them are f[0].  up (null: 1): what those keys' weights are multiplied with for the product with the values.
-    // PARTLY: rows do not see some keys; sees(key): whether the lane's row sees that key of the tile.
-    template <int KEYS, bool CAP, bool ONE, bool PARTLY, typename Sees>
-    __device__ __forceinline__ bool step(const uint8_t* kt, const uint8_t* vt, const float (&f)[KEYS / 16], const float* up, float softcap,
-                                         float inv_cap, Sees sees) {
-        constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
-        const float inf = __builtin_huge_valf();
-        v16f_flash x[KEYS / 32];
-#pragma unroll
-        for (int kb = 0; kb < KEYS / 32; ++kb) x[kb] = scores(kt, kb);
-        if constexpr (!ONE) {
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] *= f[2 * kb + (i >> 3)];
-        }
-        if constexpr (PARTLY) {
-            const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-            for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3) + 4 * half) ? x[kb][i] : -inf;
-        }
-        // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
-        // few 2^-24 of the cap, is one of the score's, also where the score is small.
-        const float unit = ONE ? f[0] : 1.0f, bound = softcap * 1.44269504088896340736f, steep = unit * 2.88539008177792681472f * inv_cap;
-        auto tail = [&](float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * steep)); };
-        // ---- the running maximum, where a score is 2^kSlack times what it allows ----
-        float tops[2] = {x[0][0], x[0][1]};
-#pragma unroll
-        for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[kb][i]);
-        float top = fmaxf(tops[0], tops[1]);
-        top = CAP ? fmaf(-2.0f * bound, tail(top), bound) : top * unit;
-        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
-            const float m_new = fmaxf(m, halves_max(top));
-            const float back = __builtin_amdgcn_exp2f(m - m_new);
-            m = m_new;
-            l *= back;
-#pragma unroll
-            for (int c = 0; c < Tile::kBlocks; ++c) acc[c] *= back;
-        }
-        // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
-        v4u_flash p[KEYS / 16];
-        const float base = CAP ? kBias + bound - m : kBias - m;
-        auto weight = [&](int kb, int i) {
-            if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base));
-            const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i]), base));   // (the cap of what is not seen is a number)
-            return PARTLY && x[kb][i] == -inf ? 0.0f : w;
-        };
-        float sums[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int kb = 0; kb < KEYS / 32; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float p0 = weight(kb, i), p1 = weight(kb, i + 1);
-                sums[0] += p0;
-                sums[1] += p1;
-                if (up) {
-                    p0 *= up[2 * kb + (i >> 3)];
-                    p1 *= up[2 * kb + (i >> 3)];
-                }
-                p[2 * kb + (i >> 3)][(i & 7) >> 1] = flash_pack<F16>(p0, p1);
-            }
-        l += sums[0] + sums[1];
-        // ---- weighted sums of values ----
-        if constexpr (PARTLY) return weigh_finite<KEYS>(p, vt);
-        weigh<KEYS>(p, vt);
-        return false;
     }
 };
 

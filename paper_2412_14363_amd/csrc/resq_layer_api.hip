@@ -76,8 +76,8 @@ bool prefix_plan(PrefixPlan& p, int64_t B, int64_t heads_q, int64_t heads_k, int
     p.own = resq_attend_kv_cache_workspace_bytes(B, heads_q, heads_k, d);   // 0 for sizes that it refuses
     if (p.own == 0 || B * heads_q >= 1 << 24) return false;
     p.tiles = (B * (heads_q / heads_k) + kPrefixRows - 1) / kPrefixRows;
-    const int64_t units = p.tiles * heads_k, at_once = d <= 128 ? 512 : 256;
-    p.parts = units >= at_once ? 1 : (int)(at_once / units);
+    const int64_t units = p.tiles * heads_k;
+    p.parts = units >= 256 ? 1 : (int)(256 / units);   // a workgroup to a compute unit
     p.out = whole(p.own);
     p.lse = p.out + whole((size_t)B * heads_q * d * sizeof(float));
     p.ml = p.lse + whole((size_t)B * heads_q * sizeof(float));
@@ -86,16 +86,16 @@ bool prefix_plan(PrefixPlan& p, int64_t B, int64_t heads_q, int64_t heads_k, int
     return true;
 }
 
-template <int W, int OCC>
+template <int W>
 int launch_prefix(const PrefixArgs& a, const PrefixPlan& p, hipStream_t st) {
     const int lds = 4 * kPrefixKeys * FlashTile<W>::kPitch;
-    const auto kernel = a.softcap > 0.0f ? attend_prefix_kernel<W, OCC, true> : attend_prefix_kernel<W, OCC, false>;
+    const auto kernel = a.softcap > 0.0f ? attend_prefix_kernel<W, true> : attend_prefix_kernel<W, false>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
     launch(kernel, dim3((unsigned)(p.tiles * a.heads_k * p.parts)), dim3(kPrefixThreads), (size_t)lds, st, a);
     const int64_t threads = (int64_t)a.B * a.heads_k * a.share.d * (a.d / 4);
-    launch(attend_prefix_join_kernel, dim3((unsigned)((threads + kPrefixThreads - 1) / kPrefixThreads)), dim3(kPrefixThreads), 0, st, a);
+    launch(attend_prefix_join_kernel, dim3((unsigned)((threads + kPrefixJoinThreads - 1) / kPrefixJoinThreads)), dim3(kPrefixJoinThreads), 0, st, a);
     return launch_status();
 }
 
@@ -237,11 +237,11 @@ int resq_attend_kv_prefix(const void* q, int64_t ldq, int64_t ldqh, int64_t B, i
     a.part_ml = reinterpret_cast<float*>(space + p.ml);
     a.part_acc = reinterpret_cast<float*>(space + p.acc);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (d_head <= 64) return launch_prefix<64, 2>(a, p, st);
-    if (d_head <= 96) return launch_prefix<96, 2>(a, p, st);
-    if (d_head <= 128) return launch_prefix<128, 2>(a, p, st);
-    if (d_head <= 192) return launch_prefix<192, 1>(a, p, st);
-    return launch_prefix<256, 1>(a, p, st);
+    if (d_head <= 64) return launch_prefix<64>(a, p, st);
+    if (d_head <= 96) return launch_prefix<96>(a, p, st);
+    if (d_head <= 128) return launch_prefix<128>(a, p, st);
+    if (d_head <= 192) return launch_prefix<192>(a, p, st);
+    return launch_prefix<256>(a, p, st);
 }
 
 int resq_norm_residual(const void* y, int64_t ldy, const void* gate, int64_t ldg, const void* h, int64_t ldh, int h_is_fp32, int64_t tokens,

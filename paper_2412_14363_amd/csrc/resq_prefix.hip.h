@@ -3,7 +3,9 @@
 // numbers once for 128 of them and not once for each sequence.  The sequences' own tokens are resq_attend.hip.h's; a last kernel joins both.
 //   k_t = code * s + z of each group, x = scale * q . k_t, capped or not; out = sum e^(x - lse) v, as there
 //
-// A workgroup makes a tile of 64 rows into fp16 numbers in LDS and has 128 queries attend to it (resq_flash.hip.h).  fp16 holds
+// A workgroup makes a tile of 64 rows into fp16 numbers in LDS and has 256 queries attend to it (resq_flash.hip.h), in two groups of
+// wavefronts half a tile apart as the prompts' kernel has them; the first makes the keys of the tile behind, the second the values, each
+// in its turn at the vector ALU.  fp16 holds
 // code * s + z to 2^-12 of itself, an eighth of what bf16 loses, which would add as much again to the error of a bf16 result; its range is
 // made up for by powers of two: of a query (its largest channel becomes 2^13), of the keys of 16 tokens, and of the values of all tokens so
 // far.  What is below 2^-27 of the largest number of its 16 tokens loses bits, down to 2^-38 of it.
@@ -15,11 +17,12 @@
 
 namespace resq {
 
-constexpr int kPrefixThreads = 256;
+constexpr int kPrefixThreads = 512;
 constexpr int kPrefixWaves = kPrefixThreads / 64;
+constexpr int kPrefixJoinThreads = 256;
 constexpr int kPrefixRows = kFlashRows * kPrefixWaves;   // of a workgroup
 constexpr int kPrefixKeys = 64;
-constexpr int kPrefixLeast = 512 / kPrefixKeys;          // tiles of a part at least
+constexpr int kPrefixLeast = 2;                          // tiles of a part at least
 
 struct PrefixArgs {
     const uint16_t* q;
@@ -65,31 +68,135 @@ __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_
 __device__ __forceinline__ int exponent_of(float x) { return max((int)(__float_as_uint(x) >> 23), 27); }   // x >= 0; bits, 127 is 2^0
 __device__ __forceinline__ float to_half_range(int e) { return two_to(267 - e); }
 
-template <int W, int OCC, bool CAP>
-__global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(const PrefixArgs a) {
+template <int W, bool CAP>
+__global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const PrefixArgs a) {
     using Tile = FlashTile<W>;
     constexpr int KEYS = kPrefixKeys, kTileBytes = KEYS * Tile::kPitch;
-    constexpr int kLanes = kPrefixThreads / KEYS;       // threads of a token
+    constexpr int kLanes = kPrefixThreads / 2 / KEYS;   // threads of a token's keys (values)
     constexpr int kUnits = Tile::kPieces / kLanes;      // pieces of 8 channels of a thread
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values
-    struct Group { int key, value, there, pad; };       // of 16 tokens: exponents of keys and values, and which of them there are
-    __shared__ __attribute__((aligned(16))) Group groups[2][KEYS / 16];
+    // of 16 tokens: the exponent of keys (values), which tokens there are, and which of them have an 8-bit (4-bit) group of values that is
+    // not finite
+    struct Group { int e, there, odd_high, odd_low; };
+    __shared__ __attribute__((aligned(16))) Group groups[2][2][KEYS / 16];   // [keys or values][buffer]
 
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), group = wave >> 2;   // what it makes: 0 keys, 1 values
     const int unit = (int)a.heads(blockIdx.x), hk = (int)blockIdx.x - unit * a.heads_k;
     const int tile = (int)a.parts(unit), piece = unit - tile * (int)a.parts.d;
     const PrefixKeys keys = prefix_keys(a);
     if (piece >= keys.parts) return;
     const int begin = keys.begin + piece * keys.per * KEYS, end = min(keys.end, begin + keys.per * KEYS);
+    const int n_all = (end - begin + KEYS - 1) / KEYS;
+    const float inf = __builtin_huge_valf();
+
+    // ---- rows of a tile: read two tiles ahead, made into numbers one ahead ----
+    const int my_token = (t & 255) / kLanes, my_unit = t % kLanes;
+    const uint8_t* pages = a.pages[group] + hk * a.head_stride;
+    int page_next = -1;
+    bool there = false;
+    uint2 code[kUnits];
+    float par[4];
+    auto load_page = [&](int n) {
+        const int tok = begin + n * KEYS + my_token;
+        page_next = -1;
+        if (tok < end) page_next = a.prefix_table[a.page_size((uint32_t)tok)];
+    };
+    auto load = [&](int n) {
+        const int tok = begin + n * KEYS + my_token;
+        there = (unsigned)page_next < (unsigned)a.num_pages;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) par[i] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) code[u] = make_uint2(0u, 0u);
+        if (there) {
+            const uint8_t* src = pages + page_next * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride;
+            const Piece16 p = *reinterpret_cast<const Piece16*>(src + a.row_bytes - 16);
+            par[0] = __uint_as_float(p.x);
+            par[1] = __uint_as_float(p.y);
+            par[2] = __uint_as_float(p.z);
+            par[3] = __uint_as_float(p.w);
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int ch = 8 * (my_unit + u * kLanes);   // of the 8-bit group, of the 4-bit one, or half and half
+                if (ch + 8 <= a.r) {
+                    const Piece8 c = *reinterpret_cast<const Piece8*>(src + ch);
+                    code[u] = make_uint2(c.x, c.y);
+                } else if (ch >= a.r) {
+                    if (ch < a.d) code[u].x = reinterpret_cast<const Piece4*>(src + a.r + ((ch - a.r) >> 1))->x;
+                } else {
+                    code[u].x = reinterpret_cast<const Piece4*>(src + ch)->x;
+                    code[u].y = *reinterpret_cast<const uint16_t*>(src + a.r);
+                }
+            }
+        }
+    };
+    // least: the exponent that values are counted in so far
+    auto store = [&](int n, int least) {
+        uint8_t* dst = lds + (2 * group + (n & 1)) * kTileBytes;
+        float high = 0.0f, low = 0.0f;   // the groups' largest magnitudes
+        if (a.r > 0) high = fmaxf(fabsf(par[1]), fabsf(fmaf(255.0f, par[0], par[1])));
+        if (a.r < a.d) low = fmaxf(fabsf(par[3]), fabsf(fmaf(15.0f, par[2], par[3])));
+        // (of numbers that are not finite keys keep what they have, values are left out: `odd` below)
+        const bool odd_high = !(fabsf(par[0]) + fabsf(par[1]) < inf), odd_low = !(fabsf(par[2]) + fabsf(par[3]) < inf);
+        const float top = fmaxf(odd_high || !(high < inf) ? 0.0f : high, odd_low || !(low < inf) ? 0.0f : low);
+        int e = exponent_of(rows_max(row_max16(top)));   // a wavefront has 16 tokens
+        if (group) e = max(e, least);
+        const float f = to_half_range(e);
+        const float fh = group && odd_high ? 0.0f : f, fl = group && odd_low ? 0.0f : f;
+        const float sh = fh == 0.0f ? 0.0f : par[0] * fh, zh = fh == 0.0f ? 0.0f : par[1] * fh;
+        const float sl = fl == 0.0f ? 0.0f : par[2] * fl, zl = fl == 0.0f ? 0.0f : par[3] * fl;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int piece = my_unit + u * kLanes, ch = 8 * piece;
+            const uint2 c = code[u];
+            float v[8];
+            if (ch >= a.r) {
+                const uint32_t even = c.x & 0x0F0F0F0Fu, odd = c.x >> 4 & 0x0F0F0F0Fu;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[2 * i] = fmaf((float)(even >> (8 * i) & 255u), sl, zl);
+                    v[2 * i + 1] = fmaf((float)(odd >> (8 * i) & 255u), sl, zl);
+                }
+            } else {
+                const bool mixed = ch + 8 > a.r;
+                const uint32_t second = mixed ? (c.y & 0xFu) | (c.y & 0xF0u) << 4 | (c.y & 0xF00u) << 8 | (c.y & 0xF000u) << 12 : c.y;
+                const float s2 = mixed ? sl : sh, z2 = mixed ? zl : zh;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = fmaf((float)(c.x >> (8 * i) & 255u), sh, zh);
+                    v[4 + i] = fmaf((float)(second >> (8 * i) & 255u), s2, z2);
+                }
+            }
+            const v4u_flash o = {flash_pack<true>(v[0], v[1]), flash_pack<true>(v[2], v[3]), flash_pack<true>(v[4], v[5]), flash_pack<true>(v[6], v[7])};
+            *reinterpret_cast<v4u_flash*>(dst + (group ? Tile::value_at(my_token, piece) : Tile::key_at(my_token, piece))) = o;
+        }
+        // a token's first lane speaks for it
+        auto tokens = [&](bool x) {
+            const uint64_t all = __builtin_amdgcn_ballot_w64(x);
+            int bits = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bits |= (int)(all >> (kLanes * i) & 1) << i;
+            return bits;
+        };
+        const int some = tokens(there), high_bits = tokens(odd_high), low_bits = tokens(odd_low);
+        if (lane == 0) groups[group][n & 1][wave & 3] = Group{e, some, high_bits, low_bits};
+    };
+    static_assert(KEYS == 64 && kPrefixWaves == 8);
+    load_page(0);
+    load(0);
+    load_page(1);
+    store(0, 27);
+    load(1);
+    load_page(2);
 
     // ---- the own row ----
     const int rows = a.B * (int)a.share.d, row = tile * kPrefixRows + wave * kFlashRows + (lane & 31);
     const bool live = row < rows;
     const int b = (int)a.share(live ? row : 0), head = hk * (int)a.share.d + (live ? row : 0) - b * (int)a.share.d;
     const int own = a.lens[b];
-    // the first token that the row sees: own tokens count for the window too
-    const int low = live && own >= 0 ? (int)max((int64_t)keys.end + own - a.window, (int64_t)0) : 0x7FFFFFFF;
+    // the first token that the row sees, own tokens count for the window too (a row that is not there sees all: nothing comes of it)
+    const int from = live && own >= 0 ? (int)max((int64_t)keys.end + own - a.window, (int64_t)0) : 0;
     FlashRow<W, true> r;
     r.clear();
     float qf;   // what a score's product is multiplied with for the query's part
@@ -106,7 +213,8 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
             for (int e = 0; e < 4; ++e)
                 top = fmaxf(top, fmaxf(__uint_as_float(r.q[s][e] << 16 & 0x7FFF0000u), __uint_as_float(r.q[s][e] & 0x7FFF0000u)));
         }
-        const int e = exponent_of(halves_max(top));
+        top = halves_max(top);
+        const int e = exponent_of(top < inf ? top : 0.0f);
         const float f = to_half_range(e);
 #pragma unroll
         for (int s = 0; s < Tile::kSteps; ++s)
@@ -116,125 +224,32 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
         qf = a.scale * two_to(e - 13);
         if (!CAP) qf *= 1.44269504088896340736f;
     }
-    const bool looks = __builtin_amdgcn_ballot_w64(low < end) != 0;   // some row of the wavefront sees something
-    const int low_there = low == 0x7FFFFFFF ? 0 : low;                // of a row that is there
+    const float bound = CAP ? a.softcap * 1.44269504088896340736f : 0.0f, steep = CAP ? 2.88539008177792681472f / a.softcap : 0.0f;
 
-    // ---- rows of a tile: read two tiles ahead, made into numbers one ahead ----
-    const int my_token = t / kLanes, my_unit = t % kLanes;
-    const int64_t head_off = hk * a.head_stride;
-    int page_next = -1;
-    bool there = false;
-    uint2 code[2][kUnits];
-    float par[2][4];
-    auto load_page = [&](int key0) {
-        const int tok = key0 + my_token;
-        page_next = -1;
-        if (tok < end) page_next = a.prefix_table[a.page_size((uint32_t)tok)];
-    };
-    auto load = [&](int key0) {
-        const int tok = key0 + my_token;
-        there = (unsigned)page_next < (unsigned)a.num_pages;
-        if (there) {
-            const int64_t off = page_next * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride + head_off;
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                const uint8_t* src = a.pages[kv] + off;
-                const Piece16 p = *reinterpret_cast<const Piece16*>(src + a.row_bytes - 16);
-                par[kv][0] = __uint_as_float(p.x);
-                par[kv][1] = __uint_as_float(p.y);
-                par[kv][2] = __uint_as_float(p.z);
-                par[kv][3] = __uint_as_float(p.w);
-#pragma unroll
-                for (int u = 0; u < kUnits; ++u) {
-                    const int ch = 8 * (my_unit + u * kLanes);   // of the 8-bit group, of the 4-bit one, or half and half
-                    code[kv][u] = make_uint2(0u, 0u);
-                    if (ch + 8 <= a.r) {
-                        const Piece8 c = *reinterpret_cast<const Piece8*>(src + ch);
-                        code[kv][u] = make_uint2(c.x, c.y);
-                    } else if (ch >= a.r) {
-                        if (ch < a.d) code[kv][u].x = reinterpret_cast<const Piece4*>(src + a.r + ((ch - a.r) >> 1))->x;
-                    } else {
-                        code[kv][u].x = reinterpret_cast<const Piece4*>(src + ch)->x;
-                        code[kv][u].y = *reinterpret_cast<const uint16_t*>(src + a.r);
-                    }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) par[kv][i] = 0.0f;
-#pragma unroll
-                for (int u = 0; u < kUnits; ++u) code[kv][u] = make_uint2(0u, 0u);
-            }
-        }
-    };
-    const float inf = __builtin_huge_valf();
-    // value_e: the exponent that values are counted in so far
-    auto store = [&](int buffer, int value_e) {
-        uint8_t* dst[2] = {lds + buffer * kTileBytes, lds + (2 + buffer) * kTileBytes};
-        int e[2];
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            float top = 0.0f;
-            if (a.r > 0) top = fmaxf(fabsf(par[kv][1]), fabsf(fmaf(255.0f, par[kv][0], par[kv][1])));
-            if (a.r < a.d) top = fmaxf(top, fmaxf(fabsf(par[kv][3]), fabsf(fmaf(15.0f, par[kv][2], par[kv][3]))));
-            e[kv] = exponent_of(rows_max(row_max16(top < inf ? top : 0.0f)));   // a wavefront has 16 tokens
-            if (kv == 1) e[1] = max(e[1], value_e);
-            const float f = to_half_range(e[kv]);
-            const float sh = par[kv][0] * f, zh = par[kv][1] * f, sl = par[kv][2] * f, zl = par[kv][3] * f;
-#pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-                const int piece = my_unit + u * kLanes, ch = 8 * piece;
-                const uint2 c = code[kv][u];
-                float v[8];
-                if (ch >= a.r) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = fmaf((float)(c.x >> (4 * i) & 15u), sl, zl);
-                } else {
-                    const bool mixed = ch + 8 > a.r;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[i] = fmaf((float)(c.x >> (8 * i) & 255u), sh, zh);
-                        v[4 + i] = mixed ? fmaf((float)(c.y >> (4 * i) & 15u), sl, zl) : fmaf((float)(c.y >> (8 * i) & 255u), sh, zh);
-                    }
-                }
-                const v4u_flash o = {flash_pack<true>(v[0], v[1]), flash_pack<true>(v[2], v[3]), flash_pack<true>(v[4], v[5]), flash_pack<true>(v[6], v[7])};
-                *reinterpret_cast<v4u_flash*>(dst[kv] + (kv ? Tile::value_at(my_token, piece) : Tile::key_at(my_token, piece))) = o;
-            }
-        }
-        const uint64_t some = __builtin_amdgcn_ballot_w64(there);
-        if (lane == 0) {
-            int mask = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mask |= (int)(some >> (kLanes * i) & 1) << i;
-            groups[buffer][wave] = Group{e[0], e[1], mask, 0};
-        }
-    };
-    static_assert(KEYS == 16 * kPrefixWaves);
-    const float inv_cap = CAP ? 1.0f / a.softcap : 0.0f;
-
-    int value_e = 27;   // (the exponent of the tile that is attended to, and of all before)
-    load_page(begin);
-    load(begin);
-    load_page(begin + KEYS);
-    store(0, value_e);
-    load(begin + KEYS);
-    load_page(begin + 2 * KEYS);
-    __syncthreads();
-    int buffer = 0;
-    for (int key0 = begin; key0 < end; key0 += KEYS, buffer ^= 1) {
+    constexpr int kAhead = W <= 128 ? 2 : 0;
+    FlashTurn<W, KEYS, kAhead> s;
+    int value_e = 27;        // the exponent of the values that are weighed, and of all before
+    uint32_t odd = 0;        // bit 0 (1): a value of the 8-bit (4-bit) group that the row sees is not finite
+    auto keys_in = [&](int n) { return lds + (n & 1) * kTileBytes; };
+    auto values_in = [&](int n) { return lds + (2 + (n & 1)) * kTileBytes; };
+    auto turn = [&](int n) __attribute__((always_inline)) {
+        flash_after_products();
+        r.ask_ahead(s, values_in(n));
         // ---- what this tile is counted in ----
-        float f[KEYS / 16], up[KEYS / 16];
+        float up[KEYS / 16];
+        uint32_t seen[2] = {0, 0}, high[2] = {0, 0}, low[2] = {0, 0};
         int ve[KEYS / 16], e_new = value_e;
-        uint64_t mask = 0;
 #pragma unroll
         for (int g = 0; g < KEYS / 16; ++g) {
-            const Group gr = groups[buffer][g];
-            f[g] = qf * two_to(__builtin_amdgcn_readfirstlane(gr.key) - 13);
-            ve[g] = __builtin_amdgcn_readfirstlane(gr.value);
+            const Group of_k = groups[0][n & 1][g], of_v = groups[1][n & 1][g];
+            const float f = qf * two_to(__builtin_amdgcn_readfirstlane(of_k.e) - 13);
+#pragma unroll
+            for (int i = 8 * (g & 1); i < 8 * (g & 1) + 8; ++i) s.x[g >> 1][i] *= f;
+            ve[g] = __builtin_amdgcn_readfirstlane(of_v.e);
             e_new = max(e_new, ve[g]);
-            mask |= (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(gr.there) << (16 * g);
+            seen[g >> 1] |= (uint32_t)__builtin_amdgcn_readfirstlane(of_k.there) << (16 * (g & 1));
+            high[g >> 1] |= (uint32_t)__builtin_amdgcn_readfirstlane(of_v.odd_high) << (16 * (g & 1));
+            low[g >> 1] |= (uint32_t)__builtin_amdgcn_readfirstlane(of_v.odd_low) << (16 * (g & 1));
         }
         bool scaled = false;
 #pragma unroll
@@ -248,24 +263,54 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
             for (int c = 0; c < Tile::kBlocks; ++c) r.acc[c] *= back;
             value_e = e_new;
         }
-        if (key0 + KEYS < end) {
-            store(buffer ^ 1, value_e);
-            if (key0 + 2 * KEYS < end) {
-                load(key0 + 2 * KEYS);
-                load_page(key0 + 3 * KEYS);
+        // ---- keys that are not there, or behind the row's window ----
+        const int key0 = begin + n * KEYS, behind = from - key0;
+        if ((seen[0] & seen[1]) != 0xFFFFFFFFu || __builtin_amdgcn_ballot_w64(behind > 0) != 0) {
+            uint32_t sees[2];   // the row's keys of both halves
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const int gone = min(max(behind - 32 * kb, 0), 32);
+                sees[kb] = seen[kb] & (gone == 32 ? 0u : 0xFFFFFFFFu << gone);
+                odd |= ((sees[kb] & high[kb]) != 0 ? 1u : 0u) | ((sees[kb] & low[kb]) != 0 ? 2u : 0u);
+                sees[kb] >>= 4 * half;
+            }
+            r.mask(s, [&](int c) { return (sees[c >> 5] >> (c & 31) & 1) != 0; });
+        } else {
+            odd |= ((high[0] | high[1]) != 0 ? 1u : 0u) | ((low[0] | low[1]) != 0 ? 2u : 0u);
+        }
+        r.template softmax<KEYS, CAP, true>(s, 1.0f, bound, steep);
+        if (scaled) {
+#pragma unroll
+            for (int g = 0; g < KEYS / 16; ++g) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t bits = s.p[g][e];
+                    const v2h_flash two = __builtin_bit_cast(v2h_flash, bits);
+                    s.p[g][e] = flash_pack<true>((float)two[0] * up[g], (float)two[1] * up[g]);
+                }
             }
         }
-        if (looks) {
-            const uint8_t *kt = lds + buffer * kTileBytes, *vt = lds + (2 + buffer) * kTileBytes;
-            const bool partly = mask != ~0ull || __builtin_amdgcn_ballot_w64(low_there > key0) != 0;
-            const int from = low - key0;
-            auto sees = [&](int key) { return (mask >> key & 1) != 0 && key >= from; };
-            const float* by = scaled ? up : nullptr;
-            if (partly) r.template step<KEYS, CAP, false, true>(kt, vt, f, by, a.softcap, inv_cap, sees);
-            else r.template step<KEYS, CAP, false, false>(kt, vt, f, by, a.softcap, inv_cap, sees);
+        // ---- the tile behind ----
+        if (n + 1 < n_all) {
+            store(n + 1, value_e);
+            if (n + 2 < n_all) {
+                load(n + 2);
+                load_page(n + 3);
+            }
         }
-        __syncthreads();
+        flash_after_making();
+    };
+
+    flash_landed();
+    if (group) flash_after_products();
+    r.template products<KEYS, false>(s, keys_in(0), nullptr);
+    turn(0);
+    for (int n = 1; n < n_all; ++n) {
+        r.template products<KEYS, true>(s, keys_in(n), values_in(n - 1));
+        turn(n);
     }
+    r.weigh_rest(s, values_in(n_all - 1));
+    if (!group) flash_after_products();
 
     // ---- this part of the result ----
     const float sum = halves_sum(r.l) * two_to(127 - (int)kFlashHalfBias);
@@ -278,17 +323,19 @@ __global__ __launch_bounds__(kPrefixThreads, OCC) void attend_prefix_kernel(cons
     for (int c = 0; c < Tile::kBlocks; ++c)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const int ch = 32 * c + 8 * (i >> 2) + 4 * half;
+            const int ch = 32 * c + 8 * (i >> 2) + 4 * half;   // four channels of one group
+            const bool nan = (odd & (ch < a.r ? 1u : 2u)) != 0;
+            const float w = nan ? __builtin_nanf("") : f;
             if (ch < a.d)
-                *reinterpret_cast<float4*>(dst + ch) = make_float4(r.acc[c][i] * f, r.acc[c][i + 1] * f, r.acc[c][i + 2] * f, r.acc[c][i + 3] * f);
+                *reinterpret_cast<float4*>(dst + ch) = make_float4(r.acc[c][i] * w, r.acc[c][i + 1] * w, r.acc[c][i + 2] * w, r.acc[c][i + 3] * w);
         }
     if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * kPrefixRows + at) * 2) = make_float2(r.m, sum);
 }
 
 // Joins the parts of the prefix and the own tokens' result, whose maximum is its log-sum-exp and whose sum is 1; four channels to a thread.
-__global__ __launch_bounds__(kPrefixThreads) void attend_prefix_join_kernel(const PrefixArgs a) {
+__global__ __launch_bounds__(kPrefixJoinThreads) void attend_prefix_join_kernel(const PrefixArgs a) {
     const int fours = a.d >> 2, heads_q = a.heads_k * (int)a.share.d;
-    const int64_t e = (int64_t)blockIdx.x * kPrefixThreads + threadIdx.x, line = e / fours;
+    const int64_t e = (int64_t)blockIdx.x * kPrefixJoinThreads + threadIdx.x, line = e / fours;
     if (line >= (int64_t)a.B * heads_q) return;
     const int ch = 4 * (int)(e - line * fours), b = (int)(line / heads_q), head = (int)(line - (int64_t)b * heads_q);
     const int hk = (int)a.share(head), row = b * (int)a.share.d + head - hk * (int)a.share.d;

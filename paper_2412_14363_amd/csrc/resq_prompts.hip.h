@@ -194,7 +194,8 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
     const float steep = CAP ? a.scale * 2.88539008177792681472f / a.softcap : 0.0f;
 
     // ---- Two groups of wavefronts, one of each to a SIMD, half a tile apart: while one is at the matrix cores the other is at the vector ALU. ----
-    FlashTurn<W, KEYS> s;
+    constexpr int kAhead = W <= 64 || W > 128 ? 0 : KEYS / 16;
+    FlashTurn<W, KEYS, kAhead> s;
     auto keys_in = [&](int n) { return lds + n % 3 * kTileBytes; };
     auto values_in = [&](int n) { return lds + (3 + n % 3) * kTileBytes; };
     flash_landed();
@@ -205,7 +206,8 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
         auto softmax = [&]() __attribute__((always_inline)) {
             flash_after_products();
             if (n + 2 < n_all) fetch(n + 2);
-            r.template softmax<KEYS, CAP, false>(s, values_in(n), factor, bound, steep, [](int) { return true; });
+            r.ask_ahead(s, values_in(n));
+            r.template softmax<KEYS, CAP, false>(s, factor, bound, steep);
             if (n + 2 < n_all) flash_after_softmax<kFetch>();
             else flash_after_softmax<0>();
             ++n;
@@ -216,17 +218,16 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
             r.template products<KEYS, true>(s, keys_in(n), values_in(n + 2));
             softmax();
         }
-        if constexpr (FlashTurn<W, KEYS>::kAhead == KEYS / 16) r.template weigh_ahead<KEYS>(s);
-        else r.template weigh<KEYS>(s.p, values_in(n + 2));
+        r.weigh_rest(s, values_in(n + 2));
     }
     for (; n < n_all; ++n) {
         r.template products<KEYS, false>(s, keys_in(n), nullptr);
         flash_after_products();
         if (n + 2 < n_all) fetch(n + 2);
-        const int behind = own - key_of(n);   // keys from the tile's first one to the row's own
-        odd |= (uint64_t)r.template softmax<KEYS, CAP, true>(s, values_in(n), factor, bound, steep,
-                                                             [&](int key) { return (unsigned)(behind - key) < (unsigned)a.window; })
-               << (n - n_whole);
+        const int behind = own - key_of(n) - 4 * half;   // keys from the lane's first one to the row's own
+        r.mask(s, [&](int key) { return (unsigned)(behind - key) < (unsigned)a.window; });
+        r.template softmax<KEYS, CAP, true>(s, factor, bound, steep);
+        odd |= (uint64_t)r.template weigh_finite<KEYS>(s.p, values_in(n)) << (n - n_whole);
         if (n + 2 < n_all) flash_after_softmax<kFetch>();
         else flash_after_softmax<0>();
     }
