@@ -94,8 +94,7 @@ int launch_prefix(const PrefixArgs& a, const PrefixPlan& p, hipStream_t st) {
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
     launch(kernel, dim3((unsigned)(p.tiles * a.heads_k * p.parts)), dim3(kPrefixThreads), (size_t)lds, st, a);
-    const int64_t threads = (int64_t)a.B * a.heads_k * a.share.d * (a.d / 4);
-    launch(attend_prefix_join_kernel, dim3((unsigned)((threads + kPrefixJoinThreads - 1) / kPrefixJoinThreads)), dim3(kPrefixJoinThreads), 0, st, a);
+    launch(attend_prefix_join_kernel, dim3((unsigned)a.B * a.heads_k * a.share.d), dim3(kPrefixJoinThreads), 0, st, a);
     return launch_status();
 }
 

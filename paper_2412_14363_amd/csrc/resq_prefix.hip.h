@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     const float inf = __builtin_huge_valf();
 
     // ---- rows of a tile: read two tiles ahead, made into numbers one ahead ----
-    const int my_token = (t & 255) / kLanes, my_unit = t % kLanes;
+    const int my_token = 16 * (wave & 3) + (lane & 15), my_unit = lane >> 4;
     const uint8_t* pages = a.pages[group] + hk * a.head_stride;
     int page_next = -1;
     bool there = false;
@@ -102,38 +102,31 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         page_next = -1;
         if (tok < end) page_next = a.prefix_table[a.page_size((uint32_t)tok)];
     };
+    // (a token that is not there: the first row of the first page in its place, of which nothing is used.  No branches: a load behind
+    // one would wait for the loads in front of it.)
     auto load = [&](int n) {
         const int tok = begin + n * KEYS + my_token;
         there = (unsigned)page_next < (unsigned)a.num_pages;
+        const int64_t off = page_next * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride;
+        const uint8_t* src = pages + (there ? off : 0);
+        const Piece16 p = *reinterpret_cast<const Piece16*>(src + a.row_bytes - 16);
+        par[0] = __uint_as_float(p.x);
+        par[1] = __uint_as_float(p.y);
+        par[2] = __uint_as_float(p.z);
+        par[3] = __uint_as_float(p.w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) par[i] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) code[u] = make_uint2(0u, 0u);
-        if (there) {
-            const uint8_t* src = pages + page_next * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride;
-            const Piece16 p = *reinterpret_cast<const Piece16*>(src + a.row_bytes - 16);
-            par[0] = __uint_as_float(p.x);
-            par[1] = __uint_as_float(p.y);
-            par[2] = __uint_as_float(p.z);
-            par[3] = __uint_as_float(p.w);
-#pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-                const int ch = 8 * (my_unit + u * kLanes);   // of the 8-bit group, of the 4-bit one, or half and half
-                if (ch + 8 <= a.r) {
-                    const Piece8 c = *reinterpret_cast<const Piece8*>(src + ch);
-                    code[u] = make_uint2(c.x, c.y);
-                } else if (ch >= a.r) {
-                    if (ch < a.d) code[u].x = reinterpret_cast<const Piece4*>(src + a.r + ((ch - a.r) >> 1))->x;
-                } else {
-                    code[u].x = reinterpret_cast<const Piece4*>(src + ch)->x;
-                    code[u].y = *reinterpret_cast<const uint16_t*>(src + a.r);
-                }
-            }
+        for (int u = 0; u < kUnits; ++u) {
+            // a piece of the 8-bit group, eight bytes, of the 4-bit one, four, or of both, four and two (behind the head: any)
+            const int ch = 8 * (my_unit + u * kLanes);
+            const int first = min(ch >= a.r ? (ch + a.r) >> 1 : ch, a.row_bytes - 8), second = ch >= a.r ? first : ch + 8 <= a.r ? ch + 4 : a.r;
+            code[u] = make_uint2(reinterpret_cast<const Piece4*>(src + first)->x, reinterpret_cast<const Piece4*>(src + second)->x);
         }
     };
     // least: the exponent that values are counted in so far
     auto store = [&](int n, int least) {
         uint8_t* dst = lds + (2 * group + (n & 1)) * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) par[i] = there ? par[i] : 0.0f;
         float high = 0.0f, low = 0.0f;   // the groups' largest magnitudes
         if (a.r > 0) high = fmaxf(fabsf(par[1]), fabsf(fmaf(255.0f, par[0], par[1])));
         if (a.r < a.d) low = fmaxf(fabsf(par[3]), fabsf(fmaf(15.0f, par[2], par[3])));
@@ -171,18 +164,12 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
             const v4u_flash o = {flash_pack<true>(v[0], v[1]), flash_pack<true>(v[2], v[3]), flash_pack<true>(v[4], v[5]), flash_pack<true>(v[6], v[7])};
             *reinterpret_cast<v4u_flash*>(dst + (group ? Tile::value_at(my_token, piece) : Tile::key_at(my_token, piece))) = o;
         }
-        // a token's first lane speaks for it
-        auto tokens = [&](bool x) {
-            const uint64_t all = __builtin_amdgcn_ballot_w64(x);
-            int bits = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) bits |= (int)(all >> (kLanes * i) & 1) << i;
-            return bits;
-        };
-        const int some = tokens(there), high_bits = tokens(odd_high), low_bits = tokens(odd_low);
+        // lanes 0 to 15 speak for the tokens
+        const int some = (int)(__builtin_amdgcn_ballot_w64(there) & 0xFFFF), high_bits = (int)(__builtin_amdgcn_ballot_w64(odd_high) & 0xFFFF);
+        const int low_bits = (int)(__builtin_amdgcn_ballot_w64(odd_low) & 0xFFFF);
         if (lane == 0) groups[group][n & 1][wave & 3] = Group{e, some, high_bits, low_bits};
     };
-    static_assert(KEYS == 64 && kPrefixWaves == 8);
+    static_assert(KEYS == 64 && kPrefixWaves == 8 && kLanes == 4);
     load_page(0);
     load(0);
     load_page(1);
@@ -332,51 +319,82 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * kPrefixRows + at) * 2) = make_float2(r.m, sum);
 }
 
-// Joins the parts of the prefix and the own tokens' result, whose maximum is its log-sum-exp and whose sum is 1; four channels to a thread.
+// Joins the parts of the prefix and the own tokens' result, whose maximum is its log-sum-exp and whose sum is 1: a workgroup to a query,
+// four channels to a thread, what threads are left over the parts.
 __global__ __launch_bounds__(kPrefixJoinThreads) void attend_prefix_join_kernel(const PrefixArgs a) {
-    const int fours = a.d >> 2, heads_q = a.heads_k * (int)a.share.d;
-    const int64_t e = (int64_t)blockIdx.x * kPrefixJoinThreads + threadIdx.x, line = e / fours;
-    if (line >= (int64_t)a.B * heads_q) return;
-    const int ch = 4 * (int)(e - line * fours), b = (int)(line / heads_q), head = (int)(line - (int64_t)b * heads_q);
+    __shared__ float weight[kPrefixJoinThreads + 1], sums[kPrefixJoinThreads + 1], top_of[kPrefixJoinThreads / 64];
+    __shared__ float4 red[kPrefixJoinThreads];
+    const int t = threadIdx.x, fours = a.d >> 2, heads_q = a.heads_k * (int)a.share.d;
+    const int b = (int)(blockIdx.x / (uint32_t)heads_q), head = (int)(blockIdx.x - (uint32_t)b * heads_q);
     const int hk = (int)a.share(head), row = b * (int)a.share.d + head - hk * (int)a.share.d;
-    const int parts = prefix_keys(a).parts;
-    const bool live = a.lens[b] >= 0;
+    const int parts = prefix_keys(a).parts;   // at most 256
     const float inf = __builtin_huge_valf();
+    uint16_t* out = a.out + b * a.ldo + head * a.ldoh;
+    if (a.lens[b] < 0) {
+        if (t < fours) *reinterpret_cast<Piece8*>(out + 4 * t) = Piece8{0u, 0u};
+        if (t == 0 && a.lse) a.lse[blockIdx.x] = -inf;
+        return;
+    }
     const int64_t slot = ((int64_t)(row / kPrefixRows) * a.heads_k + hk) * a.parts.d;
     const float* ml = a.part_ml + (slot * kPrefixRows + row % kPrefixRows) * 2;
-    const float* acc = a.part_acc + (slot * kPrefixRows + row % kPrefixRows) * a.d + ch;
-    const float own = live ? a.own_lse[line] * 1.44269504088896340736f : -inf;
-    float top = own == -inf ? kFlashNone : own, sum = own == -inf ? 0.0f : 1.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (sum != 0.0f) o = *reinterpret_cast<const float4*>(a.own_out + line * a.d + ch);
-    const float own_top = top;
-    if (live) {
-        for (int i = 0; i < parts; ++i) top = fmaxf(top, ml[(int64_t)i * kPrefixRows * 2]);
-        const float f0 = __builtin_amdgcn_exp2f(own_top - top);
-        if (!(f0 == 0.0f)) {
-            sum *= f0;
-            o.x *= f0;
-            o.y *= f0;
-            o.z *= f0;
-            o.w *= f0;
-        } else {
-            sum = o.x = o.y = o.z = o.w = 0.0f;
-        }
-        for (int i = 0; i < parts; ++i) {
-            const float2 part = *reinterpret_cast<const float2*>(ml + (int64_t)i * kPrefixRows * 2);
-            const float4 v = *reinterpret_cast<const float4*>(acc + (int64_t)i * kPrefixRows * a.d);
-            const float f = __builtin_amdgcn_exp2f(part.x - top);
-            if (f == 0.0f && part.y == part.y) continue;   // a part whose keys the row does not see, or that weigh nothing
-            sum = fmaf(f, part.y, sum);
-            o.x = fmaf(f, v.x, o.x);
-            o.y = fmaf(f, v.y, o.y);
-            o.z = fmaf(f, v.z, o.z);
-            o.w = fmaf(f, v.w, o.w);
-        }
+    const float* acc = a.part_acc + (slot * kPrefixRows + row % kPrefixRows) * a.d;
+    // weight i < parts: a part's; weight `parts`: the own tokens'
+    float2 mine = make_float2(kFlashNone, 0.0f);
+    if (t < parts) mine = *reinterpret_cast<const float2*>(ml + (int64_t)t * kPrefixRows * 2);
+    float own = a.own_lse[blockIdx.x] * 1.44269504088896340736f;
+    const float own_sum = own == -inf ? 0.0f : 1.0f;
+    if (own == -inf) own = kFlashNone;
+    float top = rows_max(row_max16(mine.x));
+    if ((t & 63) == 0) top_of[t >> 6] = top;
+    __syncthreads();
+    top = own;
+#pragma unroll
+    for (int w = 0; w < kPrefixJoinThreads / 64; ++w) top = fmaxf(top, top_of[w]);
+    const float f = __builtin_amdgcn_exp2f(mine.x - top), f_own = __builtin_amdgcn_exp2f(own - top);
+    if (t < parts) {
+        weight[t] = f;
+        sums[t] = f == 0.0f && mine.y == mine.y ? 0.0f : f * mine.y;   // (of a part whose keys the row does not see, or that weigh nothing)
     }
-    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *reinterpret_cast<Piece8*>(a.out + b * a.ldo + head * a.ldoh + ch) = Piece8{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
-    if (ch == 0 && a.lse) a.lse[line] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
+    if (t == 0) {
+        weight[parts] = own_sum == 0.0f ? 0.0f : f_own;
+        sums[parts] = own_sum == 0.0f ? 0.0f : f_own;
+    }
+    __syncthreads();
+    const int groups = kPrefixJoinThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](float w, float s, const float4& v) {
+        if (w == 0.0f && s == 0.0f) return;   // nothing, whatever v holds
+        o.x = fmaf(w, v.x, o.x);
+        o.y = fmaf(w, v.y, o.y);
+        o.z = fmaf(w, v.z, o.z);
+        o.w = fmaf(w, v.w, o.w);
+    };
+    if (group < groups) {
+        for (int i = group; i < parts; i += 4 * groups) {
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(acc + (int64_t)min(i + k * groups, parts - 1) * kPrefixRows * a.d + ch);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k * groups < parts) add(weight[i + k * groups], sums[i + k * groups], v[k]);
+        }
+        if (group == 0) add(weight[parts], sums[parts], *reinterpret_cast<const float4*>(a.own_out + (int64_t)blockIdx.x * a.d + ch));
+    }
+    red[t] = o;
+    __syncthreads();
+    if (t >= fours) return;
+    for (int k = 1; k < groups; ++k) {
+        const float4 v = red[k * fours + t];
+        o.x += v.x;
+        o.y += v.y;
+        o.z += v.z;
+        o.w += v.w;
+    }
+    float sum = 0.0f;
+    for (int i = 0; i <= parts; ++i) sum += sums[i];
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    *reinterpret_cast<Piece8*>(out + 4 * t) = Piece8{pack_bf16_pair(o.x * inv, o.y * inv), pack_bf16_pair(o.z * inv, o.w * inv)};
+    if (t == 0 && a.lse) a.lse[blockIdx.x] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);
 }
 
 }  // namespace resq
