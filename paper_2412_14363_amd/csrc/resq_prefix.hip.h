@@ -114,17 +114,22 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         par[1] = __uint_as_float(p.y);
         par[2] = __uint_as_float(p.z);
         par[3] = __uint_as_float(p.w);
+        int unit0 = my_unit;
+        asm volatile("" : "+v"(unit0));   // made anew here: kept over the products, the offsets would go to scratch memory
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             // a piece of the 8-bit group, eight bytes, of the 4-bit one, four, or of both, four and two (behind the head: any)
-            const int ch = 8 * (my_unit + u * kLanes);
+            const int ch = 8 * (unit0 + u * kLanes);
             const int first = min(ch >= a.r ? (ch + a.r) >> 1 : ch, a.row_bytes - 8), second = ch >= a.r ? first : ch + 8 <= a.r ? ch + 4 : a.r;
             code[u] = make_uint2(reinterpret_cast<const Piece4*>(src + first)->x, reinterpret_cast<const Piece4*>(src + second)->x);
         }
     };
     // least: the exponent that values are counted in so far
     auto store = [&](int n, int least) {
-        uint8_t* dst = lds + (2 * group + (n & 1)) * kTileBytes;
+        // (the pieces' order in a row is by exclusive or: piece my_unit + 4 u stands where piece my_unit stands, but for u)
+        uint32_t at = (2 * group + (n & 1)) * kTileBytes + (group ? Tile::value_at(my_token, my_unit) : Tile::key_at(my_token, my_unit));
+        int unit0 = my_unit;
+        asm volatile("" : "+v"(at), "+v"(unit0));
 #pragma unroll
         for (int i = 0; i < 4; ++i) par[i] = there ? par[i] : 0.0f;
         float high = 0.0f, low = 0.0f;   // the groups' largest magnitudes
@@ -141,7 +146,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         const float sl = fl == 0.0f ? 0.0f : par[2] * fl, zl = fl == 0.0f ? 0.0f : par[3] * fl;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const int piece = my_unit + u * kLanes, ch = 8 * piece;
+            const int ch = 8 * (unit0 + u * kLanes);
             const uint2 c = code[u];
             float v[8];
             if (ch >= a.r) {
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
                 }
             }
             const v4u_flash o = {flash_pack<true>(v[0], v[1]), flash_pack<true>(v[2], v[3]), flash_pack<true>(v[4], v[5]), flash_pack<true>(v[6], v[7])};
-            *reinterpret_cast<v4u_flash*>(dst + (group ? Tile::value_at(my_token, piece) : Tile::key_at(my_token, piece))) = o;
+            *reinterpret_cast<v4u_flash*>(lds + (at ^ 16 * kLanes * u)) = o;
         }
         // lanes 0 to 15 speak for the tokens
         const int some = (int)(__builtin_amdgcn_ballot_w64(there) & 0xFFFF), high_bits = (int)(__builtin_amdgcn_ballot_w64(odd_high) & 0xFFFF);
