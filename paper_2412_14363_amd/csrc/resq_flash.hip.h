@@ -245,22 +245,27 @@ struct FlashRow {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s.x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3)) ? s.x[kb][i] : -__builtin_huge_valf();
     }
-    // Weights of the tile at hand; MASKED: there may be scores of -inf.
-    template <int KEYS, bool CAP, bool MASKED, int AHEAD>
-    __device__ __forceinline__ void softmax(FlashTurn<W, KEYS, AHEAD>& s, float unit, float bound, float steep) {
+    // Weights of the tile at hand; MASKED: there may be scores of -inf.  unit, not negative: what makes a product a score, one for all or one
+    // for each 16 keys.
+    template <int KEYS, bool CAP, bool MASKED, int AHEAD, int UNITS>
+    __device__ __forceinline__ void softmax(FlashTurn<W, KEYS, AHEAD>& s, const float (&unit)[UNITS], float bound, float steep) {
         constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
         auto& x = s.x;
         // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
         // few 2^-24 of the cap, is one of the score's, also where the score is small.
-        auto tail = [&](float w) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * steep)); };
+        auto tail = [&](float w, float by) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * by)); };
         // ---- the running maximum, where a score is 2^kSlack times what it allows ----
-        float tops[2] = {x[0][0], x[0][1]};
+        float top;
 #pragma unroll
-        for (int kb = 0; kb < KEYS / 32; ++kb)
+        for (int u = 0; u < UNITS; ++u) {
+            constexpr int kOf = KEYS / 2 / UNITS;   // numbers of a lane that share a unit
+            float tops[2] = {x[kOf * u >> 4][kOf * u & 15], x[kOf * u >> 4][(kOf * u & 15) + 1]};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[kb][i]);
-        float top = fmaxf(tops[0], tops[1]);
-        top = CAP ? fmaf(-2.0f * bound, tail(top), bound) : top * unit;
+            for (int i = kOf * u + 2; i < kOf * u + kOf; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[i >> 4][i & 15]);
+            const float most = fmaxf(tops[0], tops[1]) * (CAP && UNITS == 1 ? 1.0f : unit[u]);
+            top = u == 0 ? most : fmaxf(top, most);
+        }
+        if (CAP) top = fmaf(-2.0f * bound, tail(top, steep), bound);
         if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
             const float m_new = fmaxf(m, halves_max(top));
             const float back = __builtin_amdgcn_exp2f(m - m_new);
@@ -272,9 +277,10 @@ struct FlashRow {
         // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
         const float base = CAP ? kBias + bound - m : kBias - m;
         auto weight = [&](int kb, int i) {
-            if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], unit, base));
-            const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i]), base));   // (the cap of what is not seen is a number)
-            return MASKED && x[kb][i] == -__builtin_huge_valf() ? 0.0f : w;
+            const float factor = unit[UNITS == 1 ? 0 : 2 * kb + (i >> 3)];
+            if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], factor, base));
+            const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i], UNITS == 1 ? steep : steep * factor), base));
+            return MASKED && x[kb][i] == -__builtin_huge_valf() ? 0.0f : w;   // (the cap of what is not seen is a number)
         };
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll

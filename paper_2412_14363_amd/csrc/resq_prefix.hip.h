@@ -75,10 +75,16 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     constexpr int kLanes = kPrefixThreads / 2 / KEYS;   // threads of a token's keys (values)
     constexpr int kUnits = Tile::kPieces / kLanes;      // pieces of 8 channels of a thread
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values
-    // of 16 tokens: the exponent of keys (values), which tokens there are, and which of them have an 8-bit (4-bit) group of values that is
-    // not finite
-    struct Group { int e, there, odd_high, odd_low; };
-    __shared__ __attribute__((aligned(16))) Group groups[2][2][KEYS / 16];   // [keys or values][buffer]
+    // of each 16 tokens of a tile: the exponent of keys (values), which tokens there are, and which of them have an 8-bit (4-bit) group of
+    // values that is not finite
+    struct About {
+        uint8_t e[KEYS / 16];
+        uint16_t there[KEYS / 16], odd_high[KEYS / 16], odd_low[KEYS / 16];
+        uint32_t unused;
+    };
+    constexpr int kAbout = sizeof(About) / 4;
+    static_assert(kAbout == 8);
+    __shared__ __attribute__((aligned(16))) About about[2][2];   // [buffer][keys or values]
 
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6), group = wave >> 2;   // what it makes: 0 keys, 1 values
@@ -118,10 +124,11 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         asm volatile("" : "+v"(unit0));   // made anew here: kept over the products, the offsets would go to scratch memory
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            // a piece of the 8-bit group, eight bytes, of the 4-bit one, four, or of both, four and two (behind the head: any)
+            // a piece of the 8-bit group, eight bytes, of the 4-bit one, four, or of both, four and two, which follow each other (behind the
+            // head: any); ch >= r where (ch + r) / 2 <= ch
             const int ch = 8 * (unit0 + u * kLanes);
-            const int first = min(ch >= a.r ? (ch + a.r) >> 1 : ch, a.row_bytes - 8), second = ch >= a.r ? first : ch + 8 <= a.r ? ch + 4 : a.r;
-            code[u] = make_uint2(reinterpret_cast<const Piece4*>(src + first)->x, reinterpret_cast<const Piece4*>(src + second)->x);
+            const Piece8 c = *reinterpret_cast<const Piece8*>(src + min(min(ch, (ch + a.r) >> 1), a.row_bytes - 8));
+            code[u] = make_uint2(c.x, c.y);
         }
     };
     // least: the exponent that values are counted in so far
@@ -144,35 +151,46 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         const float fh = group && odd_high ? 0.0f : f, fl = group && odd_low ? 0.0f : f;
         const float sh = fh == 0.0f ? 0.0f : par[0] * fh, zh = fh == 0.0f ? 0.0f : par[1] * fh;
         const float sl = fl == 0.0f ? 0.0f : par[2] * fl, zl = fl == 0.0f ? 0.0f : par[3] * fl;
+        auto number = [](uint32_t codes, int i) __attribute__((always_inline)) { return (float)(codes >> (8 * i) & 255u); };
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const int ch = 8 * (unit0 + u * kLanes);
             const uint2 c = code[u];
-            float v[8];
-            if (ch >= a.r) {
+            const int ch0 = 8 * kLanes * u;
+            v4u_flash o;
+            auto low = [&]() __attribute__((always_inline)) {
                 const uint32_t even = c.x & 0x0F0F0F0Fu, odd = c.x >> 4 & 0x0F0F0F0Fu;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[2 * i] = fmaf((float)(even >> (8 * i) & 255u), sl, zl);
-                    v[2 * i + 1] = fmaf((float)(odd >> (8 * i) & 255u), sl, zl);
-                }
+                for (int i = 0; i < 4; ++i) o[i] = flash_pack<true>(fmaf(number(even, i), sl, zl), fmaf(number(odd, i), sl, zl));
+            };
+            if (ch0 >= a.r) {   // (the same for all)
+                low();
             } else {
-                const bool mixed = ch + 8 > a.r;
-                const uint32_t second = mixed ? (c.y & 0xFu) | (c.y & 0xF0u) << 4 | (c.y & 0xF00u) << 8 | (c.y & 0xF000u) << 12 : c.y;
-                const float s2 = mixed ? sl : sh, z2 = mixed ? zl : zh;
+                const int ch = 8 * unit0 + ch0;
+                if (ch >= a.r) {
+                    low();
+                } else {
+                    const bool mixed = ch + 8 > a.r;
+                    const uint32_t second = mixed ? (c.y & 0xFu) | (c.y & 0xF0u) << 4 | (c.y & 0xF00u) << 8 | (c.y & 0xF000u) << 12 : c.y;
+                    const float s2 = mixed ? sl : sh, z2 = mixed ? zl : zh;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] = fmaf((float)(c.x >> (8 * i) & 255u), sh, zh);
-                    v[4 + i] = fmaf((float)(second >> (8 * i) & 255u), s2, z2);
+                    for (int i = 0; i < 2; ++i) {
+                        o[i] = flash_pack<true>(fmaf(number(c.x, 2 * i), sh, zh), fmaf(number(c.x, 2 * i + 1), sh, zh));
+                        o[2 + i] = flash_pack<true>(fmaf(number(second, 2 * i), s2, z2), fmaf(number(second, 2 * i + 1), s2, z2));
+                    }
                 }
             }
-            const v4u_flash o = {flash_pack<true>(v[0], v[1]), flash_pack<true>(v[2], v[3]), flash_pack<true>(v[4], v[5]), flash_pack<true>(v[6], v[7])};
             *reinterpret_cast<v4u_flash*>(lds + (at ^ 16 * kLanes * u)) = o;
         }
         // lanes 0 to 15 speak for the tokens
         const int some = (int)(__builtin_amdgcn_ballot_w64(there) & 0xFFFF), high_bits = (int)(__builtin_amdgcn_ballot_w64(odd_high) & 0xFFFF);
         const int low_bits = (int)(__builtin_amdgcn_ballot_w64(odd_low) & 0xFFFF);
-        if (lane == 0) groups[group][n & 1][wave & 3] = Group{e, some, high_bits, low_bits};
+        if (lane == 0) {
+            About& of = about[n & 1][group];
+            of.e[wave & 3] = (uint8_t)e;
+            of.there[wave & 3] = (uint16_t)some;
+            of.odd_high[wave & 3] = (uint16_t)high_bits;
+            of.odd_low[wave & 3] = (uint16_t)low_bits;
+        }
     };
     static_assert(KEYS == 64 && kPrefixWaves == 8 && kLanes == 4);
     load_page(0);
@@ -226,22 +244,19 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     auto values_in = [&](int n) { return lds + (2 + (n & 1)) * kTileBytes; };
     auto turn = [&](int n) __attribute__((always_inline)) {
         flash_after_products();
+        const uint32_t word = reinterpret_cast<const uint32_t*>(about[n & 1])[lane & (2 * kAbout - 1)];   // all of both
         r.ask_ahead(s, values_in(n));
         // ---- what this tile is counted in ----
-        float up[KEYS / 16];
-        uint32_t seen[2] = {0, 0}, high[2] = {0, 0}, low[2] = {0, 0};
+        auto read = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)word, i); };
+        const uint32_t ke = read(0), ve_all = read(kAbout), seen[2] = {read(1), read(2)};
+        const uint32_t high[2] = {read(kAbout + 3), read(kAbout + 4)}, low[2] = {read(kAbout + 5), read(kAbout + 6)};
+        float unit[KEYS / 16], up[KEYS / 16];
         int ve[KEYS / 16], e_new = value_e;
 #pragma unroll
         for (int g = 0; g < KEYS / 16; ++g) {
-            const Group of_k = groups[0][n & 1][g], of_v = groups[1][n & 1][g];
-            const float f = qf * two_to(__builtin_amdgcn_readfirstlane(of_k.e) - 13);
-#pragma unroll
-            for (int i = 8 * (g & 1); i < 8 * (g & 1) + 8; ++i) s.x[g >> 1][i] *= f;
-            ve[g] = __builtin_amdgcn_readfirstlane(of_v.e);
+            unit[g] = fmaxf(qf * two_to((int)(ke >> (8 * g) & 255u) - 13), 1.17549435e-38f);   // (not 0, which would make a NaN of -inf)
+            ve[g] = (int)(ve_all >> (8 * g) & 255u);
             e_new = max(e_new, ve[g]);
-            seen[g >> 1] |= (uint32_t)__builtin_amdgcn_readfirstlane(of_k.there) << (16 * (g & 1));
-            high[g >> 1] |= (uint32_t)__builtin_amdgcn_readfirstlane(of_v.odd_high) << (16 * (g & 1));
-            low[g >> 1] |= (uint32_t)__builtin_amdgcn_readfirstlane(of_v.odd_low) << (16 * (g & 1));
         }
         bool scaled = false;
 #pragma unroll
@@ -270,7 +285,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         } else {
             odd |= ((high[0] | high[1]) != 0 ? 1u : 0u) | ((low[0] | low[1]) != 0 ? 2u : 0u);
         }
-        r.template softmax<KEYS, CAP, true>(s, 1.0f, bound, steep);
+        r.template softmax<KEYS, CAP, true>(s, unit, bound, steep);
         if (scaled) {
 #pragma unroll
             for (int g = 0; g < KEYS / 16; ++g) {

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
             flash_after_products();
             if (n + 2 < n_all) fetch(n + 2);
             r.ask_ahead(s, values_in(n));
-            r.template softmax<KEYS, CAP, false>(s, factor, bound, steep);
+            r.template softmax<KEYS, CAP, false>(s, {factor}, bound, steep);
             if (n + 2 < n_all) flash_after_softmax<kFetch>();
             else flash_after_softmax<0>();
             ++n;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
         if (n + 2 < n_all) fetch(n + 2);
         const int behind = own - key_of(n) - 4 * half;   // keys from the lane's first one to the row's own
         r.mask(s, [&](int key) { return (unsigned)(behind - key) < (unsigned)a.window; });
-        r.template softmax<KEYS, CAP, true>(s, factor, bound, steep);
+        r.template softmax<KEYS, CAP, true>(s, {factor}, bound, steep);
         odd |= (uint64_t)r.template weigh_finite<KEYS>(s.p, values_in(n)) << (n - n_whole);
         if (n + 2 < n_all) flash_after_softmax<kFetch>();
         else flash_after_softmax<0>();
