@@ -610,7 +610,7 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
 /*
  * Attention of one new token of each sequence, as resq_attend_kv_cache, behind a PREFIX that all sequences of the batch share (the
  * instructions in front of every request, the question that many answers are tried for): the tokens of sequence b are the
- * prefix's, then lens[b] of its own (its new token the last of them).  The prefix is read and made into numbers once for 128 queries
+ * prefix's, then lens[b] of its own (its new token the last of them).  The prefix is read and made into numbers once for 256 queries
  * of a K/V head instead of once for each sequence; results are those of resq_attend_kv_cache on tables that name both in a row.
  *   prefix_len    int32 [1]: tokens of the prefix; what is above prefix_width * page_size (or 2^30) is read as that, below 0 as 0  (read)
  *   prefix_table  int32 [prefix_width]: its pages                                        (read)
@@ -618,9 +618,10 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
  *   block_table   the own tokens' pages; own tokens begin with a page of their own        (read)
  *   window        counts own tokens first
  *   workspace     resq_attend_kv_prefix_workspace_bytes bytes
- * Everything else as resq_attend_kv_cache.  Rows of the prefix go into the products as fp16 numbers: k and v are off by 2^-11 of
- * themselves at most, or by 2^-38 of the largest number among the keys of 16 tokens, among all values so far; weights by 2^-11
- * of themselves or 2^-35 of the row's largest one.
+ * Everything else as resq_attend_kv_cache.  Rows of the prefix go into the products as fp16 numbers, k as two of them: k is off by 2^-22 of
+ * itself at most, v by 2^-11, both or by 2^-38 of the largest number among those of a tile of 64 tokens (v: among all so far); weights by
+ * 2^-11 of themselves or 2^-35 of the row's largest one.  A value of the prefix that is not finite makes the channels of its group (of r
+ * or of the others) NaN in every row that sees it, and does nothing in others.
  * How the prefix is cut into parts depends on the sizes and its length alone, for the own tokens see above: equal calls give equal bits.
  */
 size_t resq_attend_kv_prefix_workspace_bytes(int64_t B, int64_t heads_q, int64_t heads_k, int64_t d_head);

@@ -147,9 +147,9 @@ struct FlashRow {
 
     // ---- a tile in two turns, one at the matrix cores and one at the vector ALU ----
     // weighted sums of the tile before (PV), whose weights and first values are at hand, and scores of this one; what a product needs of
-    // LDS is asked for eight products ahead
-    template <int KEYS, bool PV, int AHEAD>
-    __device__ __forceinline__ void products(FlashTurn<W, KEYS, AHEAD>& s, const uint8_t* kt, const uint8_t* vals_before) {
+    // LDS is asked for eight products ahead.  LOW: `low` bytes behind the keys' tile is one of what their rounding to 16 bits left out.
+    template <int KEYS, bool PV, bool LOW, int AHEAD>
+    __device__ __forceinline__ void products(FlashTurn<W, KEYS, AHEAD>& s, const uint8_t* kt, const uint8_t* vals_before, int low = 0) {
         constexpr int kAhead = PV ? AHEAD : 0, kRest = PV && kAhead ? KEYS / 16 - kAhead : 0;
         constexpr int kFirst = W <= 128 ? Tile::kSteps : 4;   // (all that registers allow)
         v4u_flash k[KEYS / 32][Tile::kSteps], v[kRest ? kRest : 1][Tile::kBlocks];
@@ -182,10 +182,23 @@ struct FlashRow {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s.x[kb][i] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < Tile::kSteps; ++t)
+        for (int t = 0; t < Tile::kSteps; ++t) {
 #pragma unroll
             for (int kb = 0; kb < KEYS / 32; ++kb)
                 s.x[kb] = flash_mfma<F16>(kb == 0 && t >= kFirst ? keys(kt, kb, t) : k[kb][t], q[t], s.x[kb]);
+            if constexpr (LOW) {   // (into the registers that the products behind leave)
+#pragma unroll
+                for (int kb = 0; kb < KEYS / 32; ++kb)
+                    if (t < kFirst) k[kb][t] = keys(kt + low, kb, t);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (LOW) {
+#pragma unroll
+            for (int t = 0; t < Tile::kSteps; ++t)
+#pragma unroll
+                for (int kb = 0; kb < KEYS / 32; ++kb) s.x[kb] = flash_mfma<F16>(t >= kFirst ? keys(kt + low, kb, t) : k[kb][t], q[t], s.x[kb]);
+        }
     }
     template <int KEYS, int AHEAD>
     __device__ __forceinline__ void weigh_rest(const FlashTurn<W, KEYS, AHEAD>& s, const uint8_t* vt) {
@@ -245,11 +258,12 @@ struct FlashRow {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s.x[kb][i] = sees(32 * kb + 8 * (i >> 2) + (i & 3)) ? s.x[kb][i] : -__builtin_huge_valf();
     }
-    // Weights of the tile at hand; MASKED: there may be scores of -inf.  unit, not negative: what makes a product a score, one for all or one
-    // for each 16 keys.
+    // Weights of the tile at hand; MASKED: there may be scores of -inf.  unit, not negative: what makes a product a score, one for all or
+    // UNITS for as many parts of the tile.
     template <int KEYS, bool CAP, bool MASKED, int AHEAD, int UNITS>
     __device__ __forceinline__ void softmax(FlashTurn<W, KEYS, AHEAD>& s, const float (&unit)[UNITS], float bound, float steep) {
         constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
+        constexpr int kOf = KEYS / 2 / UNITS;   // numbers of a lane that share a unit
         auto& x = s.x;
         // What makes x a score of base 2: a factor, or cap log2(e) tanh(x / cap) = c (1 - 2 / (1 + e^(2 x / cap))), whose error in fp32, a
         // few 2^-24 of the cap, is one of the score's, also where the score is small.
@@ -258,7 +272,6 @@ struct FlashRow {
         float top;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            constexpr int kOf = KEYS / 2 / UNITS;   // numbers of a lane that share a unit
             float tops[2] = {x[kOf * u >> 4][kOf * u & 15], x[kOf * u >> 4][(kOf * u & 15) + 1]};
 #pragma unroll
             for (int i = kOf * u + 2; i < kOf * u + kOf; ++i) tops[i & 1] = fmaxf(tops[i & 1], x[i >> 4][i & 15]);
@@ -277,7 +290,7 @@ struct FlashRow {
         // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
         const float base = CAP ? kBias + bound - m : kBias - m;
         auto weight = [&](int kb, int i) {
-            const float factor = unit[UNITS == 1 ? 0 : 2 * kb + (i >> 3)];
+            const float factor = unit[(16 * kb + i) / kOf];
             if constexpr (!CAP) return __builtin_amdgcn_exp2f(fmaf(x[kb][i], factor, base));
             const float w = __builtin_amdgcn_exp2f(fmaf(-2.0f * bound, tail(x[kb][i], UNITS == 1 ? steep : steep * factor), base));
             return MASKED && x[kb][i] == -__builtin_huge_valf() ? 0.0f : w;   // (the cap of what is not seen is a number)

@@ -67,7 +67,7 @@ int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
 
 // workspace of the attention behind a shared prefix: that of the own tokens' attention, its results, then the prefix's parts
 struct PrefixPlan {
-    int64_t tiles;   // of 128 rows
+    int64_t tiles;   // of 256 rows
     int parts;
     size_t own, out, lse, ml, acc, bytes;
 };
@@ -88,7 +88,7 @@ bool prefix_plan(PrefixPlan& p, int64_t B, int64_t heads_q, int64_t heads_k, int
 
 template <int W>
 int launch_prefix(const PrefixArgs& a, const PrefixPlan& p, hipStream_t st) {
-    const int lds = 4 * kPrefixKeys * FlashTile<W>::kPitch;
+    const int lds = 6 * prefix_keys_of(W) * FlashTile<W>::kPitch;
     const auto kernel = a.softcap > 0.0f ? attend_prefix_kernel<W, true> : attend_prefix_kernel<W, false>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)

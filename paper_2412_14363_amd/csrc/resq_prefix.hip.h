@@ -1,17 +1,27 @@
 // Attention of one new token of each sequence over a prefix that all sequences of the batch share, in pages of compact K/V rows
 // (resq_kv_row.hip.h): for each K/V head the queries of all sequences are rows of one product, so that the prefix is read and made into
-// numbers once for 128 of them and not once for each sequence.  The sequences' own tokens are resq_attend.hip.h's; a last kernel joins both.
+// numbers once for 256 of them and not once for each sequence.  The sequences' own tokens are resq_attend.hip.h's; a last kernel joins both.
 //   k_t = code * s + z of each group, x = scale * q . k_t, capped or not; out = sum e^(x - lse) v, as there
 //
-// A workgroup makes a tile of 64 rows into fp16 numbers in LDS and has 256 queries attend to it (resq_flash.hip.h), in two groups of
-// wavefronts half a tile apart as the prompts' kernel has them; the first makes the keys of the tile behind, the second the values, each
-// in its turn at the vector ALU.  fp16 holds
-// code * s + z to 2^-12 of itself, an eighth of what bf16 loses, which would add as much again to the error of a bf16 result; its range is
-// made up for by powers of two: of a query (its largest channel becomes 2^13), of the keys of 16 tokens, and of the values of all tokens so
-// far.  What is below 2^-27 of the largest number of its 16 tokens loses bits, down to 2^-38 of it.
+// A workgroup makes a tile of 64 rows (of 32 for heads above 128: what LDS and registers hold) into fp16 numbers in LDS and has 256 queries
+// attend to it (resq_flash.hip.h), in two groups of wavefronts half a tile apart as the prompts' kernel has them; the first makes the keys
+// of the tile behind, the second the values, each in its turn at the vector ALU.  A value is rounded to fp16, half a step 2^-11 of itself,
+// an eighth of what bf16 loses, which would add as much again to the error of a bf16 result.  A key is two such numbers, itself and
+// what its rounding left out, 2^-22 of it: with one the log-sum-exp, an fp32 result, was off by up to 10^-3 of itself.  (The products that
+// this takes more, a third of all, are made while the vector ALU is at work; what making them costs there is 464 -> 525 us of the largest
+// case below.)  fp16's range is made up for by powers of two: of a query (its largest channel becomes 2^13), of a wavefront's keys of a
+// tile, and of the values of all tokens so far.  What is below 2^-27 of the largest number there loses bits, down to 2^-38 of it.
+//
+// What bounds it is the vector ALU: of a tile's two turns the one of codes and weights takes about 4500 cycles of a wavefront, 700 instructions
+// of it, half of them from codes to numbers; the matrix cores' turn takes 2050, 1536 of them products.  Measured on MI355X (kernel alone,
+// the own tokens' attention and the joining of parts beside it): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 490 us of
+// 525, 420 TFLOP/s; 64 of 32 heads over 8192: 37 of 62.  Loads were in branches at first, each of which waited for all before it: 765
+// us; the places of a piece kept in registers went to scratch memory: 650 -> 500; factors of 16 keys in a pass of their own: 500 -> 390.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "resq_flash.hip.h"
 
@@ -21,7 +31,7 @@ constexpr int kPrefixThreads = 512;
 constexpr int kPrefixWaves = kPrefixThreads / 64;
 constexpr int kPrefixJoinThreads = 256;
 constexpr int kPrefixRows = kFlashRows * kPrefixWaves;   // of a workgroup
-constexpr int kPrefixKeys = 64;
+__host__ __device__ constexpr int prefix_keys_of(int d) { return d <= 128 ? 64 : 32; }   // of a tile: what registers and LDS hold
 constexpr int kPrefixLeast = 2;                          // tiles of a part at least
 
 struct PrefixArgs {
@@ -44,8 +54,8 @@ struct PrefixArgs {
     uint16_t* out;
     int64_t ldo, ldoh;
     float* lse;
-    float* part_ml;        // [tile, head, part][128][2]: maximum (times log2 e) and sum (workspace)
-    float* part_acc;       // [tile, head, part][128][d]: weighted sums (workspace)
+    float* part_ml;        // [tile, head, part][256][2]: maximum (times log2 e) and sum (workspace)
+    float* part_acc;       // [tile, head, part][256][d]: weighted sums (workspace)
 };
 
 // The tokens of the prefix that some row may see, [begin, end) with begin a multiple of a tile, and the parts they are cut into.
@@ -54,9 +64,10 @@ struct PrefixKeys {
 };
 __device__ __forceinline__ PrefixKeys prefix_keys(const PrefixArgs& a) {
     PrefixKeys k;
+    const int tile = prefix_keys_of(a.d);
     k.end = min(max(a.prefix_len[0], 0), a.max_prefix);
-    k.begin = max(k.end - a.window, 0) / kPrefixKeys * kPrefixKeys;   // (own tokens leave fewer)
-    const int tiles = (k.end - k.begin + kPrefixKeys - 1) / kPrefixKeys;
+    k.begin = max(k.end - a.window, 0) & -tile;   // (own tokens leave fewer)
+    const int tiles = (k.end - k.begin + tile - 1) / tile;
     const int parts = min((int)a.parts.d, max(tiles / kPrefixLeast, 1));
     k.per = (tiles + parts - 1) / parts;
     k.parts = k.per ? (tiles + k.per - 1) / k.per : 0;
@@ -71,20 +82,21 @@ __device__ __forceinline__ float to_half_range(int e) { return two_to(267 - e); 
 template <int W, bool CAP>
 __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const PrefixArgs a) {
     using Tile = FlashTile<W>;
-    constexpr int KEYS = kPrefixKeys, kTileBytes = KEYS * Tile::kPitch;
+    constexpr int KEYS = prefix_keys_of(W), kTileBytes = KEYS * Tile::kPitch;
+    constexpr int kGroups = kPrefixWaves / 2, kGroup = KEYS / kGroups;   // tokens of a wavefront
     constexpr int kLanes = kPrefixThreads / 2 / KEYS;   // threads of a token's keys (values)
     constexpr int kUnits = Tile::kPieces / kLanes;      // pieces of 8 channels of a thread
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values
-    // of each 16 tokens of a tile: the exponent of keys (values), which tokens there are, and which of them have an 8-bit (4-bit) group of
-    // values that is not finite
-    struct About {
-        uint8_t e[KEYS / 16];
-        uint16_t there[KEYS / 16], odd_high[KEYS / 16], odd_low[KEYS / 16];
-        uint32_t unused;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // two tiles of keys, two of values, two of what the keys' rounding left out
+    // of each wavefront's tokens of a tile: the exponent of keys (values), which tokens there are, and which of them have an 8-bit (4-bit)
+    // group of values that is not finite
+    typedef typename std::conditional<kGroup == 16, uint16_t, uint8_t>::type Bits;
+    struct alignas(16) About {
+        uint8_t e[kGroups];
+        Bits there[kGroups], odd_high[kGroups], odd_low[kGroups];
     };
-    constexpr int kAbout = sizeof(About) / 4;
-    static_assert(kAbout == 8);
-    __shared__ __attribute__((aligned(16))) About about[2][2];   // [buffer][keys or values]
+    constexpr int kAbout = sizeof(About) / 4, kWords = KEYS / 32;
+    static_assert(kGroups == 4 && kGroup * kGroups == KEYS && (kAbout == 4 || kAbout == 8));
+    __shared__ About about[2][2];   // [buffer][keys or values]
 
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6), group = wave >> 2;   // what it makes: 0 keys, 1 values
@@ -97,20 +109,20 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     const float inf = __builtin_huge_valf();
 
     // ---- rows of a tile: read two tiles ahead, made into numbers one ahead ----
-    const int my_token = 16 * (wave & 3) + (lane & 15), my_unit = lane >> 4;
+    const int my_token = kGroup * (wave & 3) + lane % kGroup, my_unit = lane / kGroup;
     const uint8_t* pages = a.pages[group] + hk * a.head_stride;
     int page_next = -1;
     bool there = false;
     uint2 code[kUnits];
     float par[4];
-    auto load_page = [&](int n) {
+    auto load_page = [&](int n) __attribute__((always_inline)) {
         const int tok = begin + n * KEYS + my_token;
         page_next = -1;
         if (tok < end) page_next = a.prefix_table[a.page_size((uint32_t)tok)];
     };
     // (a token that is not there: the first row of the first page in its place, of which nothing is used.  No branches: a load behind
     // one would wait for the loads in front of it.)
-    auto load = [&](int n) {
+    auto load = [&](int n) __attribute__((always_inline)) {
         const int tok = begin + n * KEYS + my_token;
         there = (unsigned)page_next < (unsigned)a.num_pages;
         const int64_t off = page_next * a.page_stride + (tok - (int)a.page_size((uint32_t)tok) * (int)a.page_size.d) * a.row_stride;
@@ -132,8 +144,9 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         }
     };
     // least: the exponent that values are counted in so far
-    auto store = [&](int n, int least) {
-        // (the pieces' order in a row is by exclusive or: piece my_unit + 4 u stands where piece my_unit stands, but for u)
+    auto store_of = [&](auto values, int n, int least) __attribute__((always_inline)) {
+        constexpr int group = decltype(values)::value;
+        // (the pieces' order in a row is by exclusive or: piece my_unit + kLanes u stands where piece my_unit stands, but for u)
         uint32_t at = (2 * group + (n & 1)) * kTileBytes + (group ? Tile::value_at(my_token, my_unit) : Tile::key_at(my_token, my_unit));
         int unit0 = my_unit;
         asm volatile("" : "+v"(at), "+v"(unit0));
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         // (of numbers that are not finite keys keep what they have, values are left out: `odd` below)
         const bool odd_high = !(fabsf(par[0]) + fabsf(par[1]) < inf), odd_low = !(fabsf(par[2]) + fabsf(par[3]) < inf);
         const float top = fmaxf(odd_high || !(high < inf) ? 0.0f : high, odd_low || !(low < inf) ? 0.0f : low);
-        int e = exponent_of(rows_max(row_max16(top)));   // a wavefront has 16 tokens
+        int e = exponent_of(rows_max(row_max16(top)));
         if (group) e = max(e, least);
         const float f = to_half_range(e);
         const float fh = group && odd_high ? 0.0f : f, fl = group && odd_low ? 0.0f : f;
@@ -156,11 +169,21 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         for (int u = 0; u < kUnits; ++u) {
             const uint2 c = code[u];
             const int ch0 = 8 * kLanes * u;
-            v4u_flash o;
+            v4u_flash o, rest;   // numbers, and what their rounding leaves out
+            auto two = [&](float v0, float v1) __attribute__((always_inline)) {
+                const uint32_t bits = flash_pack<true>(v0, v1);
+                if constexpr (group != 0) return make_uint2(bits, 0u);
+                const v2h_flash h = __builtin_bit_cast(v2h_flash, bits);
+                return make_uint2(bits, flash_pack<true>(fmaf((float)h[0], -1.0f, v0), fmaf((float)h[1], -1.0f, v1)));
+            };
+            auto put = [&](uint2 a0, uint2 a1, uint2 a2, uint2 a3) __attribute__((always_inline)) {
+                o = (v4u_flash){a0.x, a1.x, a2.x, a3.x};
+                rest = (v4u_flash){a0.y, a1.y, a2.y, a3.y};
+            };
             auto low = [&]() __attribute__((always_inline)) {
                 const uint32_t even = c.x & 0x0F0F0F0Fu, odd = c.x >> 4 & 0x0F0F0F0Fu;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = flash_pack<true>(fmaf(number(even, i), sl, zl), fmaf(number(odd, i), sl, zl));
+                auto pair = [&](int i) __attribute__((always_inline)) { return two(fmaf(number(even, i), sl, zl), fmaf(number(odd, i), sl, zl)); };
+                put(pair(0), pair(1), pair(2), pair(3));
             };
             if (ch0 >= a.r) {   // (the same for all)
                 low();
@@ -172,27 +195,35 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
                     const bool mixed = ch + 8 > a.r;
                     const uint32_t second = mixed ? (c.y & 0xFu) | (c.y & 0xF0u) << 4 | (c.y & 0xF00u) << 8 | (c.y & 0xF000u) << 12 : c.y;
                     const float s2 = mixed ? sl : sh, z2 = mixed ? zl : zh;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        o[i] = flash_pack<true>(fmaf(number(c.x, 2 * i), sh, zh), fmaf(number(c.x, 2 * i + 1), sh, zh));
-                        o[2 + i] = flash_pack<true>(fmaf(number(second, 2 * i), s2, z2), fmaf(number(second, 2 * i + 1), s2, z2));
-                    }
+                    auto pair = [&](uint32_t codes, int i, float s, float z) __attribute__((always_inline)) {
+                        return two(fmaf(number(codes, i), s, z), fmaf(number(codes, i + 1), s, z));
+                    };
+                    put(pair(c.x, 0, sh, zh), pair(c.x, 2, sh, zh), pair(second, 0, s2, z2), pair(second, 2, s2, z2));
                 }
             }
             *reinterpret_cast<v4u_flash*>(lds + (at ^ 16 * kLanes * u)) = o;
+            if constexpr (group == 0) {
+                const bool nothing = odd_high || odd_low;   // (an infinity less itself)
+                rest = (v4u_flash){nothing ? 0u : rest[0], nothing ? 0u : rest[1], nothing ? 0u : rest[2], nothing ? 0u : rest[3]};
+                *reinterpret_cast<v4u_flash*>(lds + 4 * kTileBytes + (at ^ 16 * kLanes * u)) = rest;
+            }
         }
-        // lanes 0 to 15 speak for the tokens
-        const int some = (int)(__builtin_amdgcn_ballot_w64(there) & 0xFFFF), high_bits = (int)(__builtin_amdgcn_ballot_w64(odd_high) & 0xFFFF);
-        const int low_bits = (int)(__builtin_amdgcn_ballot_w64(odd_low) & 0xFFFF);
+        // the first lanes speak for the tokens
+        const int some = (int)(__builtin_amdgcn_ballot_w64(there) & ((1 << kGroup) - 1)), high_bits = (int)(__builtin_amdgcn_ballot_w64(odd_high) & ((1 << kGroup) - 1));
+        const int low_bits = (int)(__builtin_amdgcn_ballot_w64(odd_low) & ((1 << kGroup) - 1));
         if (lane == 0) {
             About& of = about[n & 1][group];
             of.e[wave & 3] = (uint8_t)e;
-            of.there[wave & 3] = (uint16_t)some;
-            of.odd_high[wave & 3] = (uint16_t)high_bits;
-            of.odd_low[wave & 3] = (uint16_t)low_bits;
+            of.there[wave & 3] = (Bits)some;
+            of.odd_high[wave & 3] = (Bits)high_bits;
+            of.odd_low[wave & 3] = (Bits)low_bits;
         }
     };
-    static_assert(KEYS == 64 && kPrefixWaves == 8 && kLanes == 4);
+    auto store = [&](int n, int least) __attribute__((always_inline)) {   // (one branch, the same for a wavefront)
+        if (group) store_of(std::integral_constant<int, 1>(), n, least);
+        else store_of(std::integral_constant<int, 0>(), n, least);
+    };
+    static_assert(kLanes * kGroup == 64 && (kLanes & (kLanes - 1)) == 0);
     load_page(0);
     load(0);
     load_page(1);
@@ -248,19 +279,27 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         r.ask_ahead(s, values_in(n));
         // ---- what this tile is counted in ----
         auto read = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)word, i); };
-        const uint32_t ke = read(0), ve_all = read(kAbout), seen[2] = {read(1), read(2)};
-        const uint32_t high[2] = {read(kAbout + 3), read(kAbout + 4)}, low[2] = {read(kAbout + 5), read(kAbout + 6)};
-        float unit[KEYS / 16], up[KEYS / 16];
-        int ve[KEYS / 16], e_new = value_e;
+        const uint32_t ke = read(0), ve_all = read(kAbout);
+        uint32_t seen[kWords], high[kWords], low[kWords], missing = 0, odd_here = 0;
 #pragma unroll
-        for (int g = 0; g < KEYS / 16; ++g) {
+        for (int i = 0; i < kWords; ++i) {
+            seen[i] = read(1 + i);
+            high[i] = read(kAbout + 1 + kWords + i);
+            low[i] = read(kAbout + 1 + 2 * kWords + i);
+            missing |= ~seen[i];
+            odd_here |= high[i] | low[i];
+        }
+        float unit[kGroups], up[kGroups];
+        int ve[kGroups], e_new = value_e;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
             unit[g] = fmaxf(qf * two_to((int)(ke >> (8 * g) & 255u) - 13), 1.17549435e-38f);   // (not 0, which would make a NaN of -inf)
             ve[g] = (int)(ve_all >> (8 * g) & 255u);
             e_new = max(e_new, ve[g]);
         }
         bool scaled = false;
 #pragma unroll
-        for (int g = 0; g < KEYS / 16; ++g) {
+        for (int g = 0; g < kGroups; ++g) {
             up[g] = two_to(max(127 + ve[g] - e_new, 0));
             scaled |= ve[g] != e_new;
         }
@@ -272,18 +311,19 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         }
         // ---- keys that are not there, or behind the row's window ----
         const int key0 = begin + n * KEYS, behind = from - key0;
-        if ((seen[0] & seen[1]) != 0xFFFFFFFFu || __builtin_amdgcn_ballot_w64(behind > 0) != 0) {
-            uint32_t sees[2];   // the row's keys of both halves
+        if (missing != 0 || __builtin_amdgcn_ballot_w64(behind > 0) != 0) {
+            uint32_t sees[kWords];   // the row's keys of both halves
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
+            for (int kb = 0; kb < kWords; ++kb) {
                 const int gone = min(max(behind - 32 * kb, 0), 32);
                 sees[kb] = seen[kb] & (gone == 32 ? 0u : 0xFFFFFFFFu << gone);
                 odd |= ((sees[kb] & high[kb]) != 0 ? 1u : 0u) | ((sees[kb] & low[kb]) != 0 ? 2u : 0u);
                 sees[kb] >>= 4 * half;
             }
             r.mask(s, [&](int c) { return (sees[c >> 5] >> (c & 31) & 1) != 0; });
-        } else {
-            odd |= ((high[0] | high[1]) != 0 ? 1u : 0u) | ((low[0] | low[1]) != 0 ? 2u : 0u);
+        } else if (odd_here != 0) {
+#pragma unroll
+            for (int kb = 0; kb < kWords; ++kb) odd |= (high[kb] != 0 ? 1u : 0u) | (low[kb] != 0 ? 2u : 0u);
         }
         r.template softmax<KEYS, CAP, true>(s, unit, bound, steep);
         if (scaled) {
@@ -293,7 +333,8 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t bits = s.p[g][e];
                     const v2h_flash two = __builtin_bit_cast(v2h_flash, bits);
-                    s.p[g][e] = flash_pack<true>((float)two[0] * up[g], (float)two[1] * up[g]);
+                    const float f = up[(8 * g + 2 * e) / (KEYS / 2 / kGroups)];
+                    s.p[g][e] = flash_pack<true>((float)two[0] * f, (float)two[1] * f);
                 }
             }
         }
@@ -310,10 +351,10 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
 
     flash_landed();
     if (group) flash_after_products();
-    r.template products<KEYS, false>(s, keys_in(0), nullptr);
+    r.template products<KEYS, false, true>(s, keys_in(0), nullptr, 4 * kTileBytes);
     turn(0);
     for (int n = 1; n < n_all; ++n) {
-        r.template products<KEYS, true>(s, keys_in(n), values_in(n - 1));
+        r.template products<KEYS, true, true>(s, keys_in(n), values_in(n - 1), 4 * kTileBytes);
         turn(n);
     }
     r.weigh_rest(s, values_in(n_all - 1));

@@ -212,16 +212,16 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
             else flash_after_softmax<0>();
             ++n;
         };
-        r.template products<KEYS, false>(s, keys_in(0), nullptr);
+        r.template products<KEYS, false, false>(s, keys_in(0), nullptr);
         softmax();
         while (n < n_whole) {
-            r.template products<KEYS, true>(s, keys_in(n), values_in(n + 2));
+            r.template products<KEYS, true, false>(s, keys_in(n), values_in(n + 2));
             softmax();
         }
         r.weigh_rest(s, values_in(n + 2));
     }
     for (; n < n_all; ++n) {
-        r.template products<KEYS, false>(s, keys_in(n), nullptr);
+        r.template products<KEYS, false, false>(s, keys_in(n), nullptr);
         flash_after_products();
         if (n + 2 < n_all) fetch(n + 2);
         const int behind = own - key_of(n) - 4 * half;   // keys from the lane's first one to the row's own

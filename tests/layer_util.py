@@ -101,8 +101,8 @@ def check_norm(h, x, want, wide):
 
 
 def prefix(q, k_pages, v_pages, prefix_len, prefix_table, lens, table, r, scale, cap=0.0, window=0):
-    """resq_attend_kv_prefix: (out, lse, bounds of both).  The prefix's keys and values are off by 2^-11 of themselves (half a step of fp16)
-    and 2^-38 of the largest one; the own tokens' code products may carry offsets of up to 143 steps, 255 of the 8-bit group, and
+    """resq_attend_kv_prefix: (out, lse, bounds of both).  The prefix's values are off by 2^-11 of themselves (half a step of fp16), its
+    keys, two such numbers each, by 2^-22, both by 2^-38 of the largest one; the own tokens' code products may carry offsets of up to 143 steps, 255 of the 8-bit group, and
     their weights are two bf16 numbers: both are below what this takes for all tokens."""
     from generation_util import decode_rows
     q = q.cpu().double()
@@ -139,7 +139,7 @@ def prefix(q, k_pages, v_pages, prefix_len, prefix_table, lens, table, r, scale,
                 big.append(x.abs() + torch.cat((255 * s[:, 0:1].expand(-1, r), 143 * s[:, 2:3].expand(-1, d - r)), 1))
             for i in range(h * share, (h + 1) * share):
                 x = scale * (k @ q[b, i])
-                size = scale * ((k.abs() @ q[b, i].abs()) * 2.0 ** -11 + (big[0] @ q[b, i].abs()) * 2.0 ** -18 +
+                size = scale * ((k.abs() @ q[b, i].abs()) * 2.0 ** -22 + (big[0] @ q[b, i].abs()) * 2.0 ** -18 +
                                 2.0 ** -38 * k.abs().max() * q[b, i].abs().sum())
                 off = (size + 2.0 ** -22 * x.abs()).max() + 2.0 ** -22 * x.max().abs()
                 if cap:
