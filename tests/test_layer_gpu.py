@@ -352,3 +352,195 @@ def test_prefix_values_that_are_not_finite_where_they_are_not_seen(rq):
                 gone[b, :2, :8] = True
         over = (got - clean[0]).abs() - (clean[2] + 2.0 ** -8 * (clean[0].abs() + clean[2]))
         assert bool((over[~gone] <= 0).all()) and not bool(torch.isfinite(got[gone]).any())
+
+
+# ---- as a program calls them ---------------------------------------------------------------------------
+
+def three_calls(rq):
+    """A call of each operator on fixed inputs: functions of (stream, outputs or None) that return the outputs, and sizes of what
+    they make for themselves."""
+    g = gen(77)
+    cu, cuk = ints(sums([70, 0, 5, 300])), ints(sums([500, 2, 5, 300]))
+    q, k, v = heads(g, 375, 8, 128), heads(g, 807, 2, 128), heads(g, 807, 2, 128)
+    i = prefix_inputs(1200, [0, 1, 40, -1, 130], 8, 2, 128, 16, 16)
+    n = norm_inputs(5, 40, 1000, False, "channel", True)
+    calls = [lambda s, o=None: (rq.resq_attend_prompts(q, k, v, cu, cuk, out=o and o[0], stream=s),),
+             lambda s, o=None: (rq.resq_attend_kv_prefix(**i, out=o and o[0], stream=s),),
+             lambda s, o=None: rq.resq_norm_residual(**n, h_out=o and o[0], x=o and o[1], stream=s)]
+    return calls, [rq.resq_attend_prompts_workspace_bytes(375, 807, 4, 8, 2, 128), rq.resq_attend_kv_prefix_workspace_bytes(5, 8, 2, 128)]
+
+
+def test_buffers_that_calls_make_on_another_stream(rq):
+    calls, sizes = three_calls(rq)
+    want = [f(None) for f in calls]
+    sizes += [t.nbytes for ts in want for t in ts]
+    side, own = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream, current in ((side, own), (side.cuda_stream, own), (0, own), (side, torch.cuda.default_stream())):
+        with torch.cuda.stream(current):
+            for f, expected in zip(calls, want):
+                busy = torch.randn(2048, 2048, device=DEV)
+                for _ in range(40):
+                    busy = busy @ busy * 1e-2
+                junk = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(3)]
+                for j in junk:
+                    j.fill_(255)   # behind what is running
+                del junk, j
+                got = f(stream)
+                torch.cuda.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, expected))
+
+
+def test_calls_on_two_streams_at_once(rq):
+    calls, _ = three_calls(rq)
+    want = [f(None) for f in calls]
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [(f, calls[f](side[(n + f) % 2], tuple(torch.empty_like(t) for t in want[f]))) for n in range(10) for f in range(3)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for f, outs in got for a, b in zip(outs, want[f]))
+
+
+def test_equal_calls_give_equal_bits(rq):
+    calls, _ = three_calls(rq)
+    for f in calls:
+        want = f(None)
+        assert all(torch.equal(a, b) for _ in range(50) for a, b in zip(f(None), want))
+
+
+def test_graphs_that_share_a_workspace(rq):
+    """Captured calls of several sizes with one workspace, replayed in turn with eager calls on it between them; lengths change between
+    replays, and the captured calls go by them."""
+    g = gen(50)
+    q, k, v = heads(g, 90, 4, 128), heads(g, 4000, 2, 128), heads(g, 4000, 2, 128)
+    cu_q, cu_k = ints([0, 40, 90]), ints([0, 1500, 4000])
+    wide = [heads(g, 200, 2, 256) for _ in range(3)]
+    i = [prefix_inputs(700, [3, 0, 20], 4, 2, 64, 8, 16), prefix_inputs(2500, [b % 50 for b in range(70)], 8, 2, 128, 16, 32)]
+    size = max([rq.resq_attend_prompts_workspace_bytes(90, 4000, 2, 4, 2, 128), rq.resq_attend_prompts_workspace_bytes(200, 200, 2, 2, 2, 256)] +
+               [rq.resq_attend_kv_prefix_workspace_bytes(len(x["lens"]), x["q"].shape[1], 2, x["q"].shape[2]) for x in i])
+    work = torch.full((size,), 255, dtype=torch.uint8, device=DEV)   # NaN wherever something is read that was not written
+    outs = [torch.empty_like(q), torch.empty_like(wide[0]), torch.empty_like(i[0]["q"]), torch.empty_like(i[1]["q"])]
+    run = [lambda o, w: rq.resq_attend_prompts(q, k, v, cu_q, cu_k, out=o, workspace=w),
+           lambda o, w: rq.resq_attend_prompts(*wide, ints_wide, out=o, workspace=w),
+           lambda o, w: rq.resq_attend_kv_prefix(**i[0], out=o, workspace=w),
+           lambda o, w: rq.resq_attend_kv_prefix(**i[1], out=o, workspace=w)]
+    ints_wide = ints([0, 130, 200])
+    for f, o in zip(run, outs):
+        f(o, work)
+    torch.cuda.synchronize()
+    graphs = []
+    for f, o in zip(run, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            f(o, work)
+    lengths = [(cu_q, [[0, 40, 90], [0, 0, 90], [0, 1, 77]]), (ints_wide, [[0, 130, 200], [0, 200, 200], [5, 6, 7]]),
+               (i[0]["prefix_len"], [[700], [0], [333]]), (i[1]["prefix_len"], [[2500], [1], [64]])]
+    for n in range(3):
+        for t, values in lengths:
+            t.copy_(ints(values[n]))
+        want = []
+        for f, o in zip(run, outs):
+            fresh = torch.full_like(o, 7)
+            f(fresh, None)
+            want.append(fresh)
+        for which in (0, 1, 2, 3, 3, 1, 2, 0):
+            outs[which].fill_(7)
+            graphs[which].replay()
+            run[(which + 1 + n) % 4](torch.empty_like(outs[(which + 1 + n) % 4]), work)
+            torch.cuda.synchronize()
+            assert torch.equal(outs[which], want[which])
+
+
+def test_prefix_in_place_and_strides(rq):
+    i = prefix_inputs(300, [0, 1, 5, 40, -1], 8, 2, 96, 12, 16, pad=8)
+    want = plain.prefix(i["q"], i["k_pages"], i["v_pages"], 300, i["prefix_table"], i["lens"], i["block_table"], 12, 96 ** -0.5)
+    room = torch.full((5 * (8 * 99 + 7) + 1,), 5.0, dtype=torch.bfloat16, device=DEV)
+    odd = room[1:].view(5, 8 * 99 + 7)[:, :8 * 99].view(5, 8, 99)[..., :96]   # rows at odd addresses
+    odd.copy_(i["q"])
+    plain.check(rq.resq_attend_kv_prefix(**(i | {"q": odd})), None, want)
+    rq.resq_attend_kv_prefix(**(i | {"q": odd}), out=odd)
+    plain.check(odd, None, want)
+    kept = room[1:].view(5, 8 * 99 + 7)
+    assert bool((room[0] == 5).all()) and bool((kept[:, 8 * 99:] == 5).all()) and bool((kept[:, :8 * 99].view(5, 8, 99)[..., 96:] == 5).all())
+
+
+def test_offsets_that_pass_32_bits(rq):
+    g, d, n = gen(4), 64, 300
+    far = (1 << 24) - 8   # elements between tokens: the last ones are 10 GB behind the first
+    room = torch.empty(n * far, dtype=torch.bfloat16, device=DEV)
+    k, v = (room[at:].as_strided((n, 1, d), (far, d, 1)) for at in (0, 8 * d))
+    k.copy_(heads(g, n, 1, d))
+    v.copy_(heads(g, n, 1, d))
+    q = heads(g, n, 2, d)
+    plain.check(rq.resq_attend_prompts(q, k, v, ints([0, n])), None, plain.prompts(q, k, v, [0, n], [0, n], d ** -0.5))
+    i = prefix_inputs(100, [0, 20], 4, 2, 64, 8, 16)
+    raw = room.view(torch.uint8)
+    apart, (pages, hk, size, width) = raw.numel() // 12 // 16 * 16, i["k_pages"].shape
+    assert pages <= 11 and apart * (pages - 1) > 1 << 32
+    for at, name in ((0, "k_pages"), (1 << 20, "v_pages")):
+        x = raw[at:].as_strided((pages, hk, size, width), (apart, size * width, width, 1))
+        x.copy_(i[name])
+        i[name] = x
+    check_prefix(rq, i)
+
+
+def test_a_layer_from_prompts_to_tokens(rq):
+    """Ragged prompts with a shared first part through norm, rotation, writer and attention; then a token each behind the prefix, captured and
+    replayed, with the norm behind it.  Each result against the 64-bit one on what the step before it wrote."""
+    batch, hq, hk, d, r, page, total, width = 5, 8, 2, 128, 16, 16, 60, 10
+    model, every, g = hq * d, hq + 2 * hk, gen(31)
+    free, freq = torch.randperm(total, generator=g).to(torch.int32).to(DEV), rq.resq_rope_frequencies(d)[0]
+    pages = [torch.full((total, hk, page, rq.resq_kv_cache_row_bytes(d, r)), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    w_in, w_pre, w_post = ((torch.randn(*s, generator=g) * f + o).to(torch.bfloat16).to(DEV) for s, f, o in
+                           (((every * d, model), 0.03, 0), ((model,), 0.2, 1), ((model,), 0.2, 1)))
+
+    def layer(h, plan, at=None):
+        x = rq.resq_norm_residual(None, h, w_pre)[1]
+        qkv = (x.float() @ w_in.float().T).to(torch.bfloat16).view(len(h), every, d)
+        y = rq.resq_rope_heads(qkv[:, :hq + hk], plan.positions if at is None else at, freq, heads_q=hq)
+        rq.resq_append_kv_cache(y[:, hq:], qkv[:, hq + hk:], plan.slots, *pages, r)
+        return y, qkv[:, hq + hk:]
+
+    # the prefix: one prompt of 85 tokens, in a batch padded to 100
+    table = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    first = rq.KvSlots(1, 100)
+    rq.resq_kv_slots(first.lens, ints([85]), free, None, table, page, total, out=first)
+    h = torch.randn(100, model, generator=g).to(torch.bfloat16).to(DEV)
+    y, v = layer(h, first)
+    out = torch.full((100, hq, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    rq.resq_attend_prompts(y[:, :hq], y[:, hq:], v, first.cu_tokens, out=out)
+    plain.check(out, None, plain.prompts(y[:, :hq], y[:, hq:], v, [0, 85], [0, 85], d ** -0.5), slice(0, 85))
+    assert bool((out[85:] == 7).all())
+    o = out.view(100, model)[:85].clone()
+    args = dict(y=o, h=h[:85], w_pre=w_pre, w_post=w_post, gate=None)
+    plain.check_norm(*rq.resq_norm_residual(**args), plain.norm_residual(**args, alpha=1.0, eps=1e-6, offset=0.0), False)
+
+    # each request's own tokens behind it, one at a time
+    own_table, plan = torch.full((batch, width), -1, dtype=torch.int32, device=DEV), rq.KvSlots(batch, batch)
+    plan.state.copy_(first.state)
+    ones, prefix_len, h = ints([1] * batch), ints([85]), torch.empty(batch, model, dtype=torch.bfloat16, device=DEV)
+    out, lse = torch.empty(batch, hq, d, dtype=torch.bfloat16, device=DEV), torch.empty(batch, hq, device=DEV)
+    work = rq.resq_attend_kv_prefix_workspace(batch, hq, hk, d)
+
+    def token():
+        rq.resq_kv_slots(plan.lens, ones, free, None, own_table, page, total, out=plan)
+        y, _ = layer(h, plan, plan.positions + 85)
+        rq.resq_attend_kv_prefix(y[:, :hq], *pages, prefix_len, table[0], plan.lens, own_table, r, out=out, lse=lse, workspace=work)
+        return y, rq.resq_norm_residual(out.view(batch, model), h, w_pre, w_post)
+    kept = [t.clone() for t in (plan.lens, plan.state, own_table)]
+    h.zero_()
+    token()   # once eagerly, and back
+    for t, k in zip((plan.lens, plan.state, own_table), kept):
+        t.copy_(k)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, normed = token()
+    for n in range(18):
+        h.copy_(torch.randn(h.shape, generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert plan.lens.tolist() == [n + 1] * batch and plan.state.tolist()[1] == 0
+        plain.check(out, lse, plain.prefix(y[:, :hq], *pages, 85, table[0], plan.lens, own_table, r, d ** -0.5))
+        args = dict(y=out.view(batch, model), h=h, w_pre=w_pre, w_post=w_post, gate=None)
+        plain.check_norm(*normed, plain.norm_residual(**args, alpha=1.0, eps=1e-6, offset=0.0), False)
