@@ -61,7 +61,7 @@ int launch_prompts(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
         return RESQ_ERR_HIP;
     launch(kernel, dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(64 * WAVES), (size_t)lds, st, a);
     if (p.parts > 1)
-        launch(attend_prompts_join_kernel<KEYS, WAVES>, dim3((unsigned)(p.tiles * a.heads.d), 4), dim3(64 * WAVES), 0, st, a);
+        launch(attend_prompts_join_kernel<KEYS, WAVES>, dim3((unsigned)(p.tiles * a.heads.d), 16), dim3(64 * WAVES), 0, st, a);
     return launch_status();
 }
 

@@ -316,17 +316,31 @@ __global__ __launch_bounds__(64 * WAVES) void attend_prompts_join_kernel(const P
         const float* acc = a.part_acc + (slot * kPromptRows + row) * a.d + ch;
         float top = kFlashNone, sum = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int i = 0; i < keys.parts; ++i) top = fmaxf(top, ml[(int64_t)i * kPromptRows * 2]);
-        for (int i = 0; i < keys.parts; ++i) {
-            const float2 part = *reinterpret_cast<const float2*>(ml + (int64_t)i * kPromptRows * 2);
-            const float4 v = *reinterpret_cast<const float4*>(acc + (int64_t)i * kPromptRows * a.d);
-            const float f = __builtin_amdgcn_exp2f(part.x - top);
-            if (f == 0.0f && part.y == part.y) continue;   // a part whose keys the row does not see, or that weigh nothing
-            sum = fmaf(f, part.y, sum);
-            o.x = fmaf(f, v.x, o.x);
-            o.y = fmaf(f, v.y, o.y);
-            o.z = fmaf(f, v.z, o.z);
-            o.w = fmaf(f, v.w, o.w);
+        // four parts' loads at a time, none behind a branch
+        auto part_of = [&](int i) { return (int64_t)min(i, keys.parts - 1) * kPromptRows; };
+        for (int i = 0; i < keys.parts; i += 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, ml[part_of(i + k) * 2]);
+        }
+        for (int i = 0; i < keys.parts; i += 4) {
+            float2 part[4];
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                part[k] = *reinterpret_cast<const float2*>(ml + part_of(i + k) * 2);
+                v[k] = *reinterpret_cast<const float4*>(acc + part_of(i + k) * a.d);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = __builtin_amdgcn_exp2f(part[k].x - top);
+                // no part, or one whose keys the row does not see, or that weigh nothing
+                const bool none = i + k >= keys.parts || (f == 0.0f && part[k].y == part[k].y);
+                sum = none ? sum : fmaf(f, part[k].y, sum);
+                o.x = none ? o.x : fmaf(f, v[k].x, o.x);
+                o.y = none ? o.y : fmaf(f, v[k].y, o.y);
+                o.z = none ? o.z : fmaf(f, v[k].z, o.z);
+                o.w = none ? o.w : fmaf(f, v[k].w, o.w);
+            }
         }
         const int r = tile.row0 + row, token = (int)a.share(r), head = hk * (int)a.share.d + r - token * (int)a.share.d;
         const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
