@@ -81,10 +81,9 @@ struct AttendArgs {
     int max_len;      // tokens that a table row can name
     int window;       // 0: none
     float scale, softcap;
-    uint16_t* out;
+    uint16_t* out;     // WIDE: float [B][heads][d], of which ldo and ldoh say nothing
     int64_t ldo, ldoh;
     float* lse;
-    float* out32;      // not null: [B][heads][d] results in fp32, in place of out
     int32_t* joins;    // [B][heads][2]: a head's first partial result, and the workgroup that has its last one (workspace)
     float* part_ml;    // [2 grid][16][2]: maximum (times log2 e) and sum of a partial result's queries (workspace)
     float* part_acc;   // [2 grid][rows][d]: and its weighted sums (workspace)
@@ -146,8 +145,9 @@ __device__ __forceinline__ int64_t lane_of64(int64_t x, int lane) {
 // NL: 4-bit channels of a lane in the second product (16 NL channels in all), HT: 16-channel tiles of the 8-bit group,
 // Q: queries that fit, 8 or 16, BLOCKS: pages of a multiple of 16 rows, so that 16 tokens in a row from a multiple of 16 on are one
 // page's and two scalar offsets serve a tile instead of one per row (32 x 4096 without an 8-bit group 44.9
-// us against 46.9, 256 channels in 8 bits 132 against 175, 256 x 512 56.5 against 58.9), OCC: workgroups to a compute unit
-template <int NL, int HT, int Q, bool BLOCKS, int OCC>
+// us against 46.9, 256 channels in 8 bits 132 against 175, 256 x 512 56.5 against 58.9), OCC: workgroups to a compute unit,
+// WIDE: results in fp32
+template <int NL, int HT, int Q, bool BLOCKS, int OCC, bool WIDE>
 __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(const AttendArgs a) {
     constexpr int LS = NL / 2, HS = (HT + 1) / 2;   // steps of 32 channels of the first product
     constexpr int P = attend_pitch(NL, HT);
@@ -745,8 +745,8 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
             const int qhead = hk * a.share + qt * kAttendRows + row;
             if (whole) {
                 const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                if (a.out32) {
-                    *reinterpret_cast<v4f_att*>(a.out32 + ((int64_t)b * a.heads_k * a.share + qhead) * a.d + ch) = o * inv;
+                if constexpr (WIDE) {
+                    *reinterpret_cast<v4f_att*>(reinterpret_cast<float*>(a.out) + ((int64_t)b * a.heads_k * a.share + qhead) * a.d + ch) = o * inv;
                 } else {
                     uint16_t* dst = a.out + b * a.ldo + qhead * a.ldoh + ch;
                     *reinterpret_cast<Piece8*>(dst) = Piece8{pack_bf16_pair(o[0] * inv, o[1] * inv), pack_bf16_pair(o[2] * inv, o[3] * inv)};
@@ -770,6 +770,7 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kv_cache_kernel(co
 // Bound by the launch and two dependent reads: by a trace 3.8 us for 8 heads of 4 queries in 7 parts, 5.6 for 8 of 8 in 64.  A workgroup
 // to every query always: 256 x 512 59.5 us with the main kernel instead of 56.5; to every head always: 1 x 8192 22.1 instead of 15.1,
 // 1 x 131072 with 64 queries 68.5 instead of 49.0.  512 threads instead of 256: 256 x 512 an eighth more.
+template <bool WIDE>
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a) {
     __shared__ float weight[kAttendMaxGrid], weight_sum[kAttendMaxGrid], part[2 * kAttendWaves];
     __shared__ float4 red[kAttendThreads];
@@ -788,8 +789,8 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     const int fours = a.d >> 2;
     auto write = [&](int row, int ch, const float4& o, float top, float sum) {
         const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-        if (a.out32)
-            *reinterpret_cast<float4*>(a.out32 + ((int64_t)b * a.heads_k * a.share + q0 + row) * a.d + ch) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        if constexpr (WIDE)
+            *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + ((int64_t)b * a.heads_k * a.share + q0 + row) * a.d + ch) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
         else
             *reinterpret_cast<Piece8*>(out + row * a.ldoh + ch) = Piece8{pack_bf16_pair(o.x * f, o.y * f), pack_bf16_pair(o.z * f, o.w * f)};
         if (ch == 0 && lse) lse[row] = sum == 0.0f ? -inf : top * 0.69314718055994530942f + logf(sum);

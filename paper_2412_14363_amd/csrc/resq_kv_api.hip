@@ -102,8 +102,8 @@ AttendWorkspace attend_workspace(int64_t B, int64_t heads_k, int64_t share, int6
     return w;
 }
 
-template <int NL, int HT, int OCC>
-int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
+template <int NL, int HT, int OCC, bool WIDE>
+int launch_attend_as(const AttendArgs& a, int64_t units, hipStream_t st) {
     const int Q = a.share <= 8 ? 8 : 16;
     int lds = attend_tiles_bytes(NL, HT) + kAttendWaves * attend_weights_bytes(Q);
     const int red = kAttendWaves * a.rows * a.d * (int)sizeof(float);
@@ -112,8 +112,8 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
     args.lds_red = lds;
     lds += kAttendWaves * kAttendRows * (int)sizeof(float4);
     void (*kernel)(const AttendArgs);
-    if (Q == 8) kernel = a.blocks16 ? attend_kv_cache_kernel<NL, HT, 8, true, OCC> : attend_kv_cache_kernel<NL, HT, 8, false, OCC>;
-    else kernel = a.blocks16 ? attend_kv_cache_kernel<NL, HT, 16, true, OCC> : attend_kv_cache_kernel<NL, HT, 16, false, OCC>;
+    if (Q == 8) kernel = a.blocks16 ? attend_kv_cache_kernel<NL, HT, 8, true, OCC, WIDE> : attend_kv_cache_kernel<NL, HT, 8, false, OCC, WIDE>;
+    else kernel = a.blocks16 ? attend_kv_cache_kernel<NL, HT, 16, true, OCC, WIDE> : attend_kv_cache_kernel<NL, HT, 16, false, OCC, WIDE>;
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                lds) != hipSuccess)
         return RESQ_ERR_HIP;
@@ -122,8 +122,13 @@ int launch_attend(const AttendArgs& a, int64_t units, hipStream_t st) {
     const int64_t grid = units < 256 * OCC ? (units + 7) / 8 * 8 : 256 * OCC;   // a multiple of the dies
     launch(kernel, dim3((unsigned)grid), dim3(kAttendThreads), (size_t)lds, st, args);
     const int64_t heads = (int64_t)a.B * a.heads_k * a.qtiles;
-    launch(attend_join_kernel, dim3((unsigned)heads, heads < kAttendJoinSplit ? (unsigned)a.rows : 1), dim3(kAttendThreads), 0, st, args);
+    launch(attend_join_kernel<WIDE>, dim3((unsigned)heads, heads < kAttendJoinSplit ? (unsigned)a.rows : 1), dim3(kAttendThreads), 0, st, args);
     return launch_status();
+}
+// (fp32 results by kernels of their own: a branch for them cost the other calls 0.4 us)
+template <int NL, int HT, int OCC>
+int launch_attend(const AttendArgs& a, bool wide, int64_t units, hipStream_t st) {
+    return wide ? launch_attend_as<NL, HT, OCC, true>(a, units, st) : launch_attend_as<NL, HT, OCC, false>(a, units, st);
 }
 
 }  // namespace
@@ -187,11 +192,11 @@ int attend_kv_cache_call(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     a.window = window < kMaxAttendLen ? (int)window : 0;
     a.scale = scale;
     a.softcap = softcap;
-    a.out = static_cast<uint16_t*>(out);
+    a.out = static_cast<uint16_t*>(out32 ? static_cast<void*>(out32) : out);
     a.ldo = ldo;
     a.ldoh = ldoh;
     a.lse = lse;
-    a.out32 = out32;
+    const bool wide = out32 != nullptr;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t low = d_head - r;
     // The smallest kernel that holds the head's two groups of channels, in as many workgroups to a compute unit as its registers allow
@@ -199,13 +204,13 @@ int attend_kv_cache_call(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
     // others have up to 28 around it, once a head).  32 x 4096, in us: the next larger kernel for 128 (r = 16) 48.3 instead of 46.9, 64 (8)
     // 43.7 instead of 36.3, 256 (32) 103.5 instead of 82.5; a workgroup less 54.7 for 46.9, 37.7 for 36.3 (128, r = 32: 62.4 for 51.1); one more,
     // with spills, 310 for 82.5 (256, r = 32), 781 for 132.5 (r = 256), 57.2 for 57.3 (128, r = 64).
-    if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, units, st)
-                                                                                   : launch_attend<0, 16, 1>(a, units, st);
-    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, units, st)
-                                                                                   : launch_attend<4, 16, 1>(a, units, st);
-    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, units, st)
-                           : r <= 64 ? launch_attend<8, 4, 2>(a, units, st) : launch_attend<8, 16, 1>(a, units, st);
-    return r <= 32 ? launch_attend<16, 2, 1>(a, units, st) : launch_attend<16, 8, 1>(a, units, st);
+    if (low == 0) return r <= 64 ? launch_attend<0, 4, 3>(a, wide, units, st) : r <= 128 ? launch_attend<0, 8, 2>(a, wide, units, st)
+                                                                                   : launch_attend<0, 16, 1>(a, wide, units, st);
+    if (low <= 64) return r <= 16 ? launch_attend<4, 1, 3>(a, wide, units, st) : r <= 64 ? launch_attend<4, 4, 2>(a, wide, units, st)
+                                                                                   : launch_attend<4, 16, 1>(a, wide, units, st);
+    if (low <= 128) return r <= 16 ? launch_attend<8, 1, 2>(a, wide, units, st) : r <= 32 ? launch_attend<8, 2, 2>(a, wide, units, st)
+                           : r <= 64 ? launch_attend<8, 4, 2>(a, wide, units, st) : launch_attend<8, 16, 1>(a, wide, units, st);
+    return r <= 32 ? launch_attend<16, 2, 1>(a, wide, units, st) : launch_attend<16, 8, 1>(a, wide, units, st);
 }
 
 }  // namespace resq
