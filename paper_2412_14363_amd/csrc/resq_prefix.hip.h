@@ -12,11 +12,13 @@
 // case below.)  fp16's range is made up for by powers of two: of a query (its largest channel becomes 2^13), of a wavefront's keys of a
 // tile, and of the values of all tokens so far.  What is below 2^-27 of the largest number there loses bits, down to 2^-38 of it.
 //
-// What bounds it is the vector ALU: of a tile's two turns the one of codes and weights takes about 4500 cycles of a wavefront, 700 instructions
-// of it, half of them from codes to numbers; the matrix cores' turn takes 2050, 1536 of them products.  Measured on MI355X (kernel alone,
-// the own tokens' attention and the joining of parts beside it): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 490 us of
-// 525, 420 TFLOP/s; 64 of 32 heads over 8192: 37 of 62.  Loads were in branches at first, each of which waited for all before it: 765
-// us; the places of a piece kept in registers went to scratch memory: 650 -> 500; factors of 16 keys in a pass of their own: 500 -> 390.
+// What bounds it is the vector ALU: 600 instructions of a wavefront to a tile, more than half of them from codes to numbers, of which a turn
+// is made of some 4200 cycles; the matrix cores' turn takes 2050, 1536 of them products.  Measured on MI355X (all four kernels of a
+// call, the own tokens' attention and the joins beside this one): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 521 us,
+// 380 TFLOP/s; 64 of 32 heads over 8192 62 us, 31 of them here; 4 over 1000 27 us, 13 here, the latency of page, row and result.  On the way, at
+// 200 queries: loads in branches, each of which waited for all before it, 842 us; without 732; places of a piece made anew in place of kept in
+// scratch memory 577; factors of the keys in the softmax's own multiplications 464; keys in two numbers 525.  Loads made in the other
+// turn, at the matrix cores, where there is time: 468 for 464, they come too late then.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
