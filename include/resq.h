@@ -585,7 +585,8 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
  *   x_j = scale * q . k_j;  softcap > 0: softcap * tanh(x_j / softcap);  window > 0: only the last `window` keys, j > own - window
  *   out = sum_j e^(x_j - lse) v_j (rounded to bf16 once),  lse = ln sum_j e^(x_j)
  * Weights go into the products rounded to bf16 (off by 2^-8 of each at most), sums are fp32.  Where a query sees no key (more queries than keys) out is 0
- * and lse -inf.  What a query does not see has no part in its result, infinities and NaN neither.
+ * and lse -inf.  What a query does not see has no part in its result, infinities and NaN neither.  (Infinities in a query or in
+ * keys that it sees may make NaN of its result.)
  *   q, out   bf16 [tokens_q, heads_q, d_head] with strides (ldq, ldqh), (ldo, ldoh); rows of out do not overlap; rows outside of the
  *            sequences are left as they were                                             (read / written)
  *   k, v     bf16 [tokens_k, heads_k, d_head] with strides (ldk, ldkh), (ldv, ldvh): views of a projection's output, or what

@@ -220,6 +220,7 @@ int resq_attend_kv_prefix(const void* q, int64_t ldq, int64_t ldqh, int64_t B, i
     a.prefix_table = prefix_table;
     a.max_prefix = (int)(prefix_width > kMaxTokens / page_size ? kMaxTokens : prefix_width * page_size);
     a.lens = lens;
+    a.max_own = (int)(width > kMaxTokens / page_size ? kMaxTokens : width * page_size);
     a.pages[0] = static_cast<const uint8_t*>(k_pages);
     a.pages[1] = static_cast<const uint8_t*>(v_pages);
     a.num_pages = (int)num_pages;

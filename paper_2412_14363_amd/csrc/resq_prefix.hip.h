@@ -45,6 +45,7 @@ struct PrefixArgs {
     const int32_t* prefix_table;
     int max_prefix;        // tokens that the prefix's table can name
     const int32_t* lens;   // own tokens of each sequence, below 0: the sequence is not there
+    int max_own;           // that a sequence's table can name
     const uint8_t* pages[2];
     int num_pages;
     FastDiv page_size;
@@ -152,8 +153,9 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
         uint32_t at = (2 * group + (n & 1)) * kTileBytes + (group ? Tile::value_at(my_token, my_unit) : Tile::key_at(my_token, my_unit));
         int unit0 = my_unit;
         asm volatile("" : "+v"(at), "+v"(unit0));
+        // (what a row holds as the numbers of a group without channels is nothing)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) par[i] = there ? par[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) par[i] = there && (i < 2 ? a.r > 0 : a.r < a.d) ? par[i] : 0.0f;
         float high = 0.0f, low = 0.0f;   // the groups' largest magnitudes
         if (a.r > 0) high = fmaxf(fabsf(par[1]), fabsf(fmaf(255.0f, par[0], par[1])));
         if (a.r < a.d) low = fmaxf(fabsf(par[3]), fabsf(fmaf(15.0f, par[2], par[3])));
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     const int rows = a.B * (int)a.share.d, row = tile * kPrefixRows + wave * kFlashRows + (lane & 31);
     const bool live = row < rows;
     const int b = (int)a.share(live ? row : 0), head = hk * (int)a.share.d + (live ? row : 0) - b * (int)a.share.d;
-    const int own = a.lens[b];
+    const int own = min(a.lens[b], a.max_own);
     // the first token that the row sees, own tokens count for the window too (a row that is not there sees all: nothing comes of it)
     const int from = live && own >= 0 ? (int)max((int64_t)keys.end + own - a.window, (int64_t)0) : 0;
     FlashRow<W, true> r;

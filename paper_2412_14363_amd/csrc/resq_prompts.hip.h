@@ -247,7 +247,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
         if (n + 2 < n_all) flash_after_softmax<kFetch>();
         else flash_after_softmax<0>();
     }
-    if (!kPair && group) flash_after_products();
+    if (kPair && !group) flash_after_products();   // as many barriers as the other group
 
     // ---- what infinities and NaN among the values make of the rows that see them, one after the other ----
     for (; odd != 0; odd &= odd - 1) {

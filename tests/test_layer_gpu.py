@@ -354,6 +354,23 @@ def test_prefix_values_that_are_not_finite_where_they_are_not_seen(rq):
         assert bool((over[~gone] <= 0).all()) and not bool(torch.isfinite(got[gone]).any())
 
 
+def test_prefix_own_lengths_beyond_their_tables(rq):
+    i = prefix_inputs(300, [3, 16, 20], 4, 2, 64, 8, 16)   # tables of three pages
+    i["lens"] = ints([3, 1000, 2 ** 31 - 1])
+    for window in (0, 1, 50, 200):   # counts the 48 tokens that there can be
+        check_prefix(rq, i, window=window)
+
+
+@pytest.mark.parametrize("d,r", [(8, 8), (40, 40), (72, 72), (136, 136), (200, 200), (40, 0), (72, 0), (128, 128), (128, 0)])
+def test_prefix_numbers_of_a_group_without_channels(rq, d, r):
+    i = prefix_inputs(150, [0, 0, 0], 6, 2, d, r, 16, seed=d)
+    got = rq.resq_attend_kv_prefix(**i)
+    low = r + (d - r) // 2 + (8 if r == d else 0)
+    for pages in (i["k_pages"], i["v_pages"]):
+        pages[..., low:low + 8] = 255   # NaN
+    assert torch.equal(rq.resq_attend_kv_prefix(**i), got) and bool(torch.isfinite(got).all())
+
+
 # ---- as a program calls them ---------------------------------------------------------------------------
 
 def three_calls(rq):
