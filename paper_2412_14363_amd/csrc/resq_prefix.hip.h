@@ -14,10 +14,10 @@
 //
 // What bounds it is the vector ALU: 600 instructions of a wavefront to a tile, more than half of them from codes to numbers, of which a turn
 // is made of some 4200 cycles; the matrix cores' turn takes 2050, 1536 of them products.  Measured on MI355X (all four kernels of a
-// call, the own tokens' attention and the joins beside this one): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 521 us,
-// 380 TFLOP/s; 64 of 32 heads over 8192 62 us, 31 of them here; 4 over 1000 27 us, 13 here, the latency of page, row and result.  On the way, at
+// call, the own tokens' attention and the joins beside this one): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 507 us,
+// 390 TFLOP/s; 64 of 32 heads over 8192 62 us, 31 of them here; 4 over 1000 27 us, 13 here, the latency of page, row and result.  On the way, at
 // 200 queries: loads in branches, each of which waited for all before it, 842 us; without 732; places of a piece made anew in place of kept in
-// scratch memory 577; factors of the keys in the softmax's own multiplications 464; keys in two numbers 525.  Loads made in the other
+// scratch memory 577; factors of the keys in the softmax's own multiplications 464; keys in two numbers 525, the join by a wavefront to a query 507.  Loads made in the other
 // turn, at the matrix cores, where there is time: 468 for 464, they come too late then.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -31,7 +31,7 @@ namespace resq {
 
 constexpr int kPrefixThreads = 512;
 constexpr int kPrefixWaves = kPrefixThreads / 64;
-constexpr int kPrefixJoinThreads = 256;
+constexpr int kPrefixJoinSmall = 64, kPrefixJoinLarge = 256;
 constexpr int kPrefixRows = kFlashRows * kPrefixWaves;   // of a workgroup
 __host__ __device__ constexpr int prefix_keys_of(int d) { return d <= 128 ? 64 : 32; }   // of a tile: what registers and LDS hold
 constexpr int kPrefixLeast = 2;                          // tiles of a part at least
@@ -386,13 +386,14 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
 
 // Joins the parts of the prefix and the own tokens' result, whose maximum is its log-sum-exp and whose sum is 1: a workgroup to a query,
 // four channels to a thread, what threads are left over the parts.
-__global__ __launch_bounds__(kPrefixJoinThreads) void attend_prefix_join_kernel(const PrefixArgs a) {
-    __shared__ float weight[kPrefixJoinThreads + 1], sums[kPrefixJoinThreads + 1], top_of[kPrefixJoinThreads / 64];
-    __shared__ float4 red[kPrefixJoinThreads];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void attend_prefix_join_kernel(const PrefixArgs a) {
+    __shared__ float weight[THREADS + 1], sums[THREADS + 1], top_of[THREADS / 64];
+    __shared__ float4 red[THREADS];
     const int t = threadIdx.x, fours = a.d >> 2, heads_q = a.heads_k * (int)a.share.d;
     const int b = (int)(blockIdx.x / (uint32_t)heads_q), head = (int)(blockIdx.x - (uint32_t)b * heads_q);
     const int hk = (int)a.share(head), row = b * (int)a.share.d + head - hk * (int)a.share.d;
-    const int parts = prefix_keys(a).parts;   // at most 256
+    const int parts = prefix_keys(a).parts;   // at most THREADS
     const float inf = __builtin_huge_valf();
     uint16_t* out = a.out + b * a.ldo + head * a.ldoh;
     if (a.lens[b] < 0) {
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(kPrefixJoinThreads) void attend_prefix_join_kernel(
     __syncthreads();
     top = own;
 #pragma unroll
-    for (int w = 0; w < kPrefixJoinThreads / 64; ++w) top = fmaxf(top, top_of[w]);
+    for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, top_of[w]);
     const float f = __builtin_amdgcn_exp2f(mine.x - top), f_own = __builtin_amdgcn_exp2f(own - top);
     if (t < parts) {
         weight[t] = f;
@@ -425,7 +426,7 @@ __global__ __launch_bounds__(kPrefixJoinThreads) void attend_prefix_join_kernel(
         sums[parts] = own_sum == 0.0f ? 0.0f : f_own;
     }
     __syncthreads();
-    const int groups = kPrefixJoinThreads / fours, group = t / fours, ch = 4 * (t - group * fours);
+    const int groups = THREADS / fours, group = t / fours, ch = 4 * (t - group * fours);
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     auto add = [&](float w, float s, const float4& v) {
         if (w == 0.0f && s == 0.0f) return;   // nothing, whatever v holds
