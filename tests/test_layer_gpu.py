@@ -297,6 +297,12 @@ def test_prefix_long_and_many(rq, n, batch, hq, hk):
     check_prefix(rq, prefix_inputs(n, [b % 3 for b in range(batch)], hq, hk, 64, 8, 32, seed=batch))
 
 
+@pytest.mark.parametrize("heads_k,share,batch,d,r,n", [(48, 1, 3, 64, 8, 900), (40, 2, 2, 256, 32, 700), (33, 1, 4, 128, 16, 1300), (260, 1, 2, 8, 8, 200),
+                                                       (32, 3, 90, 40, 8, 500), (64, 1, 1, 192, 24, 1)])
+def test_prefix_of_many_heads(rq, heads_k, share, batch, d, r, n):
+    check_prefix(rq, prefix_inputs(n, [(5 * b) % 19 - 1 for b in range(batch)], heads_k * share, heads_k, d, r, 16, seed=heads_k))
+
+
 def test_prefix_lengths_outside_and_pages_that_do_not_exist(rq):
     i = prefix_inputs(300, [3, 0, 20], 4, 2, 64, 8, 16)
     for n in (-5, 10000):   # the table's last entry names no page
