@@ -595,7 +595,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
  *            (tokens_k) is read as that; results of arrays that decrease are unspecified (no access leaves the tensors)  (read)
  *   lse      fp32 [tokens_q, heads_q] or null                                            (written)
  *   d_head   multiple of 8, 8 .. 256; heads_q a multiple of heads_k; 1 <= B <= 65535; tokens_q = 0 does nothing
- *   scale, softcap, window   as resq_attend_kv_cache
+ *   scale, softcap, window   as resq_attend_kv_cache; a capped score is off by 2^-21 of the cap at most, a small one too
  *   tokens_q, tokens_k <= 2^30, tokens_q * heads_q < 2^31 - 65536; ldk, ldv < 2^24
  *   workspace  device memory, 256-byte aligned, resq_attend_prompts_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents
  *            meaningless before and after; calls that overlap (different streams) need one each
@@ -619,7 +619,7 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
  *   block_table   the own tokens' pages; own tokens begin with a page of their own        (read)
  *   window        counts own tokens first
  *   workspace     resq_attend_kv_prefix_workspace_bytes bytes
- * Everything else as resq_attend_kv_cache.  Rows of the prefix go into the products as fp16 numbers, k as two of them: k is off by 2^-22 of
+ * Everything else as resq_attend_kv_cache, capped scores of the prefix as in resq_attend_prompts.  Rows of the prefix go into the products as fp16 numbers, k as two of them: k is off by 2^-22 of
  * itself at most, v by 2^-11, both or by 2^-38 of the largest number among those of a tile of 64 tokens (v: among all so far); weights by
  * 2^-11 of themselves or 2^-35 of the row's largest one.  A value of the prefix that is not finite makes the channels of its group (of r
  * or of the others) NaN in every row that sees it, and does nothing in others.
