@@ -31,6 +31,7 @@
 namespace resq {
 
 constexpr int kPromptWaves = 8;   // of a workgroup at most
+constexpr int kPromptMost = (1 << 25) - 1;   // tiles that a thread counts, of which a call has 2^24 + 65535 at most
 constexpr __host__ __device__ int prompt_rows(int waves) { return kFlashRows * waves; }   // of a workgroup
 
 struct PromptArgs {
@@ -61,7 +62,8 @@ struct PromptTile {
 template <int WAVES>
 __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int at, PromptTile& tile) {
     constexpr int kPromptThreads = 64 * WAVES, kPromptRows = prompt_rows(WAVES);
-    __shared__ int part[kPromptWaves], found[5];
+    __shared__ uint32_t part[kPromptWaves];
+    __shared__ int found[5];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     auto first = [&](const int32_t* cu, int b, int most) { return min(max(cu[b], 0), most); };
     auto tiles = [&](int b) {
@@ -70,29 +72,30 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int at, PromptT
     };
     const int per = (a.B + kPromptThreads - 1) / kPromptThreads;
     const int b0 = min(t * per, a.B), b1 = min(b0 + per, a.B);
+    // (lengths that decrease name rows again and again: their counts stop at what 32 bits hold, so that one thread still finds each tile)
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles(b);
-    const int upto = wave_scan(mine);
+    for (int b = b0; b < b1; ++b) mine = min(mine + tiles(b), kPromptMost);
+    const uint32_t upto = (uint32_t)wave_scan(mine);
     if (lane == 63) part[wave] = upto;
     __syncthreads();
-    int total = 0, before = 0;
+    uint32_t total = 0, before = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
         if (w == wave) before = total;
-        total += part[w];
+        total = min(total + part[w], 64u * kPromptMost);
     }
-    if (at >= total) return false;
-    at = total - 1 - at;
-    int start = before + upto - mine;
-    if (start <= at && at < start + mine) {
+    if ((uint32_t)at >= total) return false;
+    const uint32_t mirror = total - 1 - (uint32_t)at;
+    uint32_t start = before + upto - (uint32_t)mine;
+    if (start <= mirror && mirror < start + (uint32_t)mine) {
         for (int b = b0; b < b1; ++b) {
-            const int n = tiles(b);
-            if (at < start + n) {
+            const uint32_t n = (uint32_t)tiles(b);
+            if (mirror < start + n) {
                 found[0] = first(a.cu_q, b, a.tokens_q);
                 found[1] = first(a.cu_q, b + 1, a.tokens_q);
                 found[2] = first(a.cu_k, b, a.tokens_k);
                 found[3] = first(a.cu_k, b + 1, a.tokens_k);
-                found[4] = at - start;
+                found[4] = (int)(mirror - start);
                 break;
             }
             start += n;
