@@ -266,10 +266,9 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 r.q[s][i] = flash_pack<true>(__uint_as_float(r.q[s][i] << 16) * f, __uint_as_float(r.q[s][i] & 0xFFFF0000u) * f);
-        qf = a.scale * two_to(e - 13);
-        if (!CAP) qf *= 1.44269504088896340736f;
+        qf = a.scale * two_to(e - 13) * 1.44269504088896340736f;
     }
-    const float bound = CAP ? a.softcap * 1.44269504088896340736f : 0.0f, steep = CAP ? 2.88539008177792681472f / a.softcap : 0.0f;
+    const FlashCap cap(CAP ? a.softcap : 1.0f);
 
     constexpr int kAhead = W <= 128 ? 2 : 0;
     FlashTurn<W, KEYS, kAhead> s;
@@ -329,7 +328,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
 #pragma unroll
             for (int kb = 0; kb < kWords; ++kb) odd |= (high[kb] != 0 ? 1u : 0u) | (low[kb] != 0 ? 2u : 0u);
         }
-        r.template softmax<KEYS, CAP, true>(s, unit, bound, steep);
+        r.template softmax<KEYS, CAP, true>(s, unit, cap);
         if (scaled) {
 #pragma unroll
             for (int g = 0; g < KEYS / 16; ++g) {

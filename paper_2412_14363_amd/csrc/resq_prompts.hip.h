@@ -20,7 +20,7 @@
 // 46 % of all cycles, LDS banks never in conflict.  2048 tokens 66 us: the last workgroup has all 32 tiles of keys, at 2 us each, when half of
 // the compute units are idle; cut in two 91, for a workgroup's way to its first product is 7 us and results of parts take another pass.
 // On the way, at 8192 tokens: tiles through registers and masks everywhere 1649 us; tiles straight to LDS, whole ones in a loop without
-// masks, maxima that rise only when they must 585; the two groups 526-548.  24 ragged prompts of heads of 64 with window and cap 178-184 us,
+// masks, maxima that rise only when they must 585; the two groups 526-548.  24 ragged prompts of heads of 64 with window and cap 194 us,
 // three chunks of up to 300 tokens behind up to 30000 316, of which the join is 16 (28 with one part's loads at a time).
 #pragma once
 #include <hip/hip_runtime.h>
@@ -209,8 +209,8 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
     }
     r.clear();
     const float inf = __builtin_huge_valf();
-    const float factor = CAP ? a.scale : a.scale * 1.44269504088896340736f, bound = CAP ? a.softcap * 1.44269504088896340736f : 0.0f;
-    const float steep = CAP ? a.scale * 2.88539008177792681472f / a.softcap : 0.0f;
+    const float factor = a.scale * 1.44269504088896340736f;
+    const FlashCap cap(CAP ? a.softcap : 1.0f);
 
     // ---- Two groups of wavefronts, one of each to a SIMD, half a tile apart: while one is at the matrix cores the other is at the vector ALU. ----
     constexpr int kAhead = W <= 64 || W > 128 ? 0 : KEYS / 16;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
             flash_after_products();
             if (n + 2 < n_all) fetch(n + 2);
             r.ask_ahead(s, values_in(n));
-            r.template softmax<KEYS, CAP, false>(s, {factor}, bound, steep);
+            r.template softmax<KEYS, CAP, false>(s, {factor}, cap);
             if (n + 2 < n_all) flash_after_softmax<kFetch>();
             else flash_after_softmax<0>();
             ++n;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
         if (n + 2 < n_all) fetch(n + 2);
         const int behind = own - key_of(n) - 4 * half;   // keys from the lane's first one to the row's own
         r.mask(s, [&](int key) { return (unsigned)(behind - key) < (unsigned)a.window; });
-        r.template softmax<KEYS, CAP, true>(s, {factor}, bound, steep);
+        r.template softmax<KEYS, CAP, true>(s, {factor}, cap);
         odd |= (uint64_t)r.template weigh_finite<KEYS>(s.p, values_in(n)) << (n - n_whole);
         if (n + 2 < n_all) flash_after_softmax<kFetch>();
         else flash_after_softmax<0>();
@@ -270,7 +270,8 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
                     if (ch < d) x = fmaf(of_q, bf16_bits_to_f32(k[ch]), x);
                 }
             x = halves_sum(x);
-            x = CAP ? fmaf(-2.0f * bound, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * steep)), bound) : x * factor;
+            x *= factor;
+            if (CAP) x = cap(x);
             if ((unsigned)(own - key) >= (unsigned)a.window) continue;
             const float w = __builtin_amdgcn_exp2f(x - r.m);
 #pragma unroll

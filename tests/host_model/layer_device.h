@@ -82,3 +82,4 @@ inline V read_tr(V* p) {
 #define __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, x, y, z) model::mfma32<true>(a, b, c)
 #define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) model::read_tr(p)
 #define __builtin_amdgcn_rsqf(x) (1.0f / sqrtf(x))
+#define __builtin_amdgcn_fmed3f(x, lo, hi) fminf(fmaxf(x, lo), hi)   // (of NaN too: the lower bound)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import layer_util as plain
-from test_layer_gpu import DEV, gen, heads, ints, rq, sums   # noqa: F401
+from test_layer_gpu import DEV, gen, heads, ints, prefix_inputs, rq   # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,75 @@ def test_prompts_lengths_that_decrease_beyond_32_bits(rq):   # noqa: F811
         rq.resq_attend_prompts(q, k, k, cu_q, cu_k, out=out, lse=lse)
         torch.cuda.synchronize()
         assert out_kept() and lse_kept()
+
+
+# ---- capped scores ------------------------------------------------------------------------------------
+# Off by 2^-20 of themselves at most: two polynomials of four steps with terms of one sign, a roundings' 2^-24 for each (8), the reciprocal's last
+# place (2) and the quotient's rounding (1), the argument's square, seven roundings of which at most half reach the quotient (3.5), and
+# the fit (0.3): 14.8 roundings.  A weight is off by twice that.
+
+def capped(want, exact, most):
+    """(results with the cap, bounds): those without it, in whose place the cap puts its own error and no other; scores below `most`."""
+    out, lse, tol, tol_lse = want
+    off = 2.0 ** -20 * most
+    return out, lse, tol + 2 * off * exact, tol_lse + off
+
+
+@pytest.mark.parametrize("cap", [1e4, 1e6, 1e8, 1.5e38, 3.4e38])
+@pytest.mark.parametrize("d,window", [(64, 0), (128, 50), (200, 0)])
+def test_prompts_caps_far_above_the_scores(rq, d, window, cap):   # noqa: F811
+    g, cu_q, cu_k = gen(d), [0, 70, 75, 200], [0, 90, 95, 320]
+    q, k, v = heads(g, 200, 4, d), heads(g, 320, 2, d), heads(g, 320, 2, d)
+    out, lse = torch.empty_like(q), torch.empty(200, 4, device=DEV)
+    rq.resq_attend_prompts(q, k, v, ints(cu_q), ints(cu_k), softcap=cap, window=window, out=out, lse=lse)
+    without = plain.prompts(q, k, v, cu_q, cu_k, d ** -0.5, 0.0, window)   # its bounds know nothing of a cap
+    want = plain.prompts(q, k, v, cu_q, cu_k, d ** -0.5, cap, window)
+    most = 20.0
+    assert float((q.float().norm(dim=2).max() * k.float().norm(dim=2).max()) * d ** -0.5) < 2 * most
+    plain.check(out, lse, capped((want[0], want[1], without[2] * 1.01, without[3] * 1.01), v.double().abs().amax().cpu(), 2 * most))
+
+
+@pytest.mark.parametrize("cap", [1e4, 1e6, 1e8, 1.5e38, 3.4e38])
+@pytest.mark.parametrize("d,r,window", [(64, 8, 0), (128, 16, 150), (256, 32, 0)])
+def test_prefix_caps_far_above_the_scores(rq, d, r, window, cap):   # noqa: F811
+    i = prefix_inputs(300, [0, 1, 40, -1], 4, 2, d, r, 16, seed=d)
+    args = i["q"], i["k_pages"], i["v_pages"], 300, i["prefix_table"], i["lens"], i["block_table"], r, d ** -0.5
+    without, want = plain.prefix(*args, 0.0, window), plain.prefix(*args, cap, window)
+    lse = torch.empty(4, 4, device=DEV)
+    out = rq.resq_attend_kv_prefix(**i, softcap=cap, window=window, lse=lse)
+    live = want[1][torch.isfinite(want[1])]
+    most = float(live.abs().max()) + 8   # a log of a few hundred exponentials is no more than that below the largest score
+    plain.check(out, lse, capped((want[0], want[1], without[2] * 1.01, without[3] * 1.01), want[0].abs().max() + 8, most))
+
+
+@pytest.mark.parametrize("cap", [1e-30, 0.5, 5.0, 50.0, 1e3, 1e5])
+@pytest.mark.parametrize("d", [64, 128])
+def test_log_sum_exps_of_one_capped_score(rq, d, cap):   # noqa: F811
+    """A query that sees one key has its score as log-sum-exp: small scores, scores about the cap, far above it, and of either sign."""
+    g, n = gen(7), 400
+    q, k = heads(g, n, 2, d), heads(g, n, 2, d)
+    k *= torch.exp(torch.linspace(-12, 12, n, device=DEV))[:, None, None].to(torch.bfloat16)
+    lse = torch.empty(n, 2, device=DEV)
+    rq.resq_attend_prompts(q, k, k, ints([0, n]), softcap=cap, window=1, lse=lse)
+    x, size = ((a * b).sum(-1) * d ** -0.5 for a, b in ((q.cpu().double(), k.cpu().double()), (q.cpu().double().abs(), k.cpu().double().abs())))
+    want = cap * torch.tanh(x / cap)
+    # what the score itself may be off by, as far as the cap lets it through; the cap's error and three roundings of constants.  Then m ln 2 + ln w of
+    # w = 2^(x - m), where m may be up to 8 below x: that difference (2^-22), the exponential (2^-23), a logarithm below 5.6 (2^-21) and two
+    # roundings of m ln 2, 5.6 of which x does not account for (2^-20.5): 2^-19.3
+    off = d * 2.0 ** -24 * size + 2.0 ** -22 * x.abs()
+    through = torch.maximum(cap * torch.tanh((x + off) / cap) - want, want - cap * torch.tanh((x - off) / cap))
+    tol = through + (2.0 ** -20 + 2.0 ** -22) * want.abs() + 2.0 ** -19.3
+    over = (lse.cpu().double() - want).abs() - tol
+    assert bool((over <= 0).all()), (float(over.max()), float(cap))
+
+
+def test_caps_of_scores_that_are_not_numbers(rq):   # noqa: F811
+    """A NaN among the keys that a row sees is one in its result, capped or not, and nothing to the others."""
+    g, n = gen(5), 200
+    q, k, v = (heads(g, n, 1, 64) for _ in range(3))
+    k[100, 0, 3] = math.nan
+    for cap in (0.0, 1.0, 30.0, 1e4):
+        lse = torch.empty(n, 1, device=DEV)
+        out = rq.resq_attend_prompts(q, k, v, ints([0, n]), softcap=cap, lse=lse)
+        assert bool(torch.isfinite(out[:100]).all()) and bool(torch.isfinite(lse[:100]).all())
+        assert bool(torch.isnan(out[100:]).all()) and bool(torch.isnan(lse[100:]).all())
