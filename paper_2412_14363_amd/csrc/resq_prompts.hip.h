@@ -352,9 +352,9 @@ __global__ __launch_bounds__(64 * WAVES) void attend_prompts_join_kernel(const P
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+                // (a part whose keys the row does not see has sums of 0; one whose keys weigh nothing may have NaN, which stays)
                 const float f = __builtin_amdgcn_exp2f(part[k].x - top);
-                // no part, or one whose keys the row does not see, or that weigh nothing
-                const bool none = i + k >= keys.parts || (f == 0.0f && part[k].y == part[k].y);
+                const bool none = i + k >= keys.parts;
                 sum = none ? sum : fmaf(f, part[k].y, sum);
                 o.x = none ? o.x : fmaf(f, v[k].x, o.x);
                 o.y = none ? o.y : fmaf(f, v[k].y, o.y);

@@ -111,3 +111,19 @@ def test_caps_of_scores_that_are_not_numbers(rq):   # noqa: F811
         out = rq.resq_attend_prompts(q, k, v, ints([0, n]), softcap=cap, lse=lse)
         assert bool(torch.isfinite(out[:100]).all()) and bool(torch.isfinite(lse[:100]).all())
         assert bool(torch.isnan(out[100:]).all()) and bool(torch.isnan(lse[100:]).all())
+
+
+# ---- values that are not finite and weigh next to nothing -------------------------------------------------
+
+@pytest.mark.parametrize("hk", [1, 300])   # keys in parts, and in one
+def test_prompts_values_that_are_seen_and_weigh_nothing(rq, hk):   # noqa: F811
+    """NaN times a weight is NaN however small the weight is, and however the keys are cut."""
+    g, n = gen(1), 1500
+    q = torch.ones(2, hk, 8, dtype=torch.bfloat16, device=DEV)
+    k, v = torch.full((n, hk, 8), -30.0, dtype=torch.bfloat16, device=DEV), heads(g, n, hk, 8)
+    k[1000:] = 30   # e^-480 of these is what the first ones weigh
+    v[10, :, 3], v[1200, :, 5] = math.nan, math.nan
+    for window in (0, 600):
+        out = rq.resq_attend_prompts(q, k, v, ints([0, 2]), ints([0, n]), scale=1.0, window=window)
+        bad = torch.isnan(out)
+        assert bool(bad[..., 5].all()) and bool((bad[..., 3] == (window == 0)).all()) and not bool(bad[..., [0, 1, 2, 4, 6, 7]].any())
