@@ -427,8 +427,7 @@ __global__ __launch_bounds__(THREADS) void attend_prefix_join_kernel(const Prefi
     __syncthreads();
     const int groups = THREADS / fours, group = t / fours, ch = 4 * (t - group * fours);
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto add = [&](float w, float s, const float4& v) {
-        if (w == 0.0f && s == 0.0f) return;   // nothing, whatever v holds
+    auto add = [&](float w, const float4& v) {   // (of weight 0 too: a part whose tokens weigh nothing may have NaN, which stays)
         o.x = fmaf(w, v.x, o.x);
         o.y = fmaf(w, v.y, o.y);
         o.z = fmaf(w, v.z, o.z);
@@ -441,9 +440,9 @@ __global__ __launch_bounds__(THREADS) void attend_prefix_join_kernel(const Prefi
             for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(acc + (int64_t)min(i + k * groups, parts - 1) * kPrefixRows * a.d + ch);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (i + k * groups < parts) add(weight[i + k * groups], sums[i + k * groups], v[k]);
+                if (i + k * groups < parts) add(weight[i + k * groups], v[k]);
         }
-        if (group == 0) add(weight[parts], sums[parts], *reinterpret_cast<const float4*>(a.own_out + (int64_t)blockIdx.x * a.d + ch));
+        if (group == 0) add(weight[parts], *reinterpret_cast<const float4*>(a.own_out + (int64_t)blockIdx.x * a.d + ch));
     }
     red[t] = o;
     __syncthreads();

@@ -127,3 +127,20 @@ def test_prompts_values_that_are_seen_and_weigh_nothing(rq, hk):   # noqa: F811
         out = rq.resq_attend_prompts(q, k, v, ints([0, 2]), ints([0, n]), scale=1.0, window=window)
         bad = torch.isnan(out)
         assert bool(bad[..., 5].all()) and bool((bad[..., 3] == (window == 0)).all()) and not bool(bad[..., [0, 1, 2, 4, 6, 7]].any())
+
+
+@pytest.mark.parametrize("n,batch,hk", [(500, 3, 1), (500, 3, 300), (100, 3, 1)])   # the prefix in parts, in one
+def test_prefix_values_that_are_seen_and_weigh_nothing(rq, n, batch, hk):   # noqa: F811
+    i = prefix_inputs(n, [0, 5, 60], hk, hk, 16, 8, 16)
+    low, t = 8 + 4, i["prefix_table"].cpu()
+    i["q"].fill_(1)
+    for tok in range(n):
+        par = i["k_pages"][int(t[tok // 16]), :, tok % 16, low:low + 16]
+        z = -20.0 if tok < n // 2 else 20.0
+        par.copy_(torch.tensor([0.0, z, 0.0, z]).view(torch.uint8).to(DEV))
+    spot = i["v_pages"][int(t[10 // 16]), :, 10 % 16]
+    spot[:, low:low + 4] = torch.tensor([math.nan]).view(torch.uint8).to(DEV)   # the 8-bit group's scale
+    for window in (0, n // 2):
+        out = rq.resq_attend_kv_prefix(**i, scale=1.0, window=window)
+        bad = torch.isnan(out)
+        assert bool((bad[..., :8] == (window == 0)).all()) and not bool(bad[..., 8:].any())
