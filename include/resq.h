@@ -639,7 +639,8 @@ int resq_attend_kv_prefix(const void* q, int64_t ldq, int64_t ldqh, int64_t B, i
  *   a  = y * rsqrt(mean(y^2) + eps) * (w_offset + w_post)   (w_post null: a = y;  y null: a = 0, what a first block needs)
  *   h' = h + alpha * gate * a                               (gate null: 1)
  *   x  = h' * rsqrt(mean(h'^2) + eps) * (w_offset + w_pre)
- * in fp32 with one rounding of each output; x comes from h' as it was before its rounding.
+ * in fp32 with one rounding of each output; x comes from h' as it was before its rounding.  (Squares are fp32 numbers too: what is above 1.8e19
+ * in a row has none.)
  *   y, gate, x  bf16 [tokens, width] with strides ldy, ldg, ldx (ldg 0: one gate for all tokens)   (read / read / written)
  *   h, h_out  bf16, or fp32 (h_is_fp32), [tokens, width] with strides ldh, ldho          (read / written)
  *            h_out may be h and x may be y, with the same strides; else outputs lie on no other tensor of the call, and rows of

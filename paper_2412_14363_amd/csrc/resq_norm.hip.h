@@ -114,7 +114,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_residual_kernel(const 
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) s += part[which][first + w];
         }
-        return __builtin_amdgcn_rsqf(s / (float)a.width + a.eps);
+        // (the instruction takes what is below the normal numbers for 0)
+        s = s / (float)a.width + a.eps;
+        const bool tiny = s < 1.17549435e-38f;
+        return __builtin_amdgcn_rsqf(tiny ? s * 4294967296.0f : s) * (tiny ? 65536.0f : 1.0f);
     };
 
     float y[P][8], h[P][8];

@@ -144,3 +144,18 @@ def test_prefix_values_that_are_seen_and_weigh_nothing(rq, n, batch, hk):   # no
         out = rq.resq_attend_kv_prefix(**i, scale=1.0, window=window)
         bad = torch.isnan(out)
         assert bool((bad[..., :8] == (window == 0)).all()) and not bool(bad[..., 8:].any())
+
+
+# ---- norms of numbers far from 1 -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("size", [1e-18, 1e-19, 3e-20, 1e-21, 1e-22])
+@pytest.mark.parametrize("width", [64, 4096])
+def test_norm_of_small_rows_without_eps(rq, width, size):   # noqa: F811
+    """Mean squares below the smallest normal number of fp32, 1.2e-38, hold 2^-149 steps: of 1e-44 some two digits are left."""
+    i = dict(y=None, h=(torch.rand(3, width, generator=gen(width)) + 0.5).to(DEV) * size, w_pre=torch.ones(width, dtype=torch.bfloat16, device=DEV))
+    x = rq.resq_norm_residual(**i, eps=0.0)[1]
+    want = plain.norm_residual(**i, w_post=None, gate=None, alpha=1.0, eps=0.0, offset=0.0)[1]
+    step = 2.0 ** -149 / (size * size)   # of a mean square; a sum's terms are rounded to it, each by half a step of the 1.08 they are
+    off = 2.0 ** -17 + min(64 * step, 1.0)
+    over = (x.cpu().double() - want).abs() - want * (off + 2.0 ** -8)
+    assert bool((over <= 0).all()), float(over.max())
