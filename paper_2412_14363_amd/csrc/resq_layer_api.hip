@@ -127,6 +127,7 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
                         int64_t ldv, int64_t ldvh, int64_t tokens_k, const int32_t* cu_q, const int32_t* cu_k, int64_t B, int64_t heads_q,
                         int64_t heads_k, int64_t d_head, float scale, float softcap, int64_t window, void* out, int64_t ldo, int64_t ldoh,
                         float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (tokens_k == 1 && ldk >= 0 && ldv >= 0) ldk = ldv = 0;
     PromptPlan p;
     if (!prompt_plan(p, tokens_q, tokens_k, B, heads_q, heads_k, d_head) || ldq < 0 || ldqh < 0 || ldk < 0 || ldkh < 0 || ldv < 0 ||
         ldvh < 0 || !(scale > 0.0f) || !isfinite(scale) || !(softcap == 0.0f || softcap >= FLT_MIN) || !isfinite(softcap) || window < 0 ||
@@ -135,7 +136,6 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
     if (tokens_q == 0) return RESQ_OK;
     if (!q || (tokens_k > 0 && (!k || !v)) || !cu_q || !cu_k || !out || !workspace) return RESQ_ERR_NULL;
     if (tokens_q == 1) ldq = ldo = 0;
-    if (tokens_k == 1) ldk = ldv = 0;
     if (heads_q == 1) ldqh = ldoh = 0;
     if (heads_k == 1) ldkh = ldvh = 0;
     if (out == q && (ldq != ldo || ldqh != ldoh)) return RESQ_ERR_SHAPE;
