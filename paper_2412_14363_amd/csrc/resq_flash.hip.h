@@ -89,27 +89,36 @@ __device__ __forceinline__ void flash_after_softmax() {
 // large the cap is, where 1 - 2 / (1 + e^(2 y / B)) would be off by 2^-21 of the cap.  f is P / Q, fitted for the least relative error up to
 // |y| = 8.7 B, from where on y f is B to fp32 (2^-25.9; all terms are positive, so that nothing cancels), or where a wavefront's scores of
 // a tile are all within 0.33 B, as scores below a cap mostly are, a polynomial (2^-25.2).  Measured on MI355X, 24 ragged prompts of heads of 64:
-// 194 us, 259 by P / Q everywhere, 182 by the exponential and its reciprocal.
+// 194 us, 259 by P / Q everywhere, 182 by the exponential and its reciprocal; 8192 tokens, heads of 128, 688 with all scores within 0.33 B, 928 with
+// larger ones in every tile, 669 by the exponential.
 struct FlashCap {
-    float most, small, inv;   // 8.7 B, 0.33 B, and 1 / B
+    float most, small, inv;   // 8.7 B, 0.33 B, and 1 / B, in scalar registers
     __device__ __forceinline__ explicit FlashCap(float cap)
-        : most(fminf(12.5514472f * cap, 3.4028235e38f)), small(0.47608936f * cap), inv(0.69314718055994530942f / cap) {}
-    __device__ __forceinline__ float small_factor(float y) const {
+        : most(scalar(fminf(12.5514472f * cap, 3.4028235e38f))), small(scalar(0.47608936f * cap)), inv(scalar(0.69314718055994530942f / cap)) {}
+    __device__ static __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+    // A constant in a vector register from here on: kept over a loop it would take another's place, which goes to scratch memory, and reads of
+    // that wait for tiles on their way to LDS (8192 tokens, heads of 128, 1016 us for 688; 200 queries over 30001 tokens 723 for 658).
+    __device__ static __forceinline__ float here(float x) {
+        asm volatile("" : "+v"(x));
+        return x;
+    }
+    __device__ __forceinline__ float small_factor(float y, float c2) const {   // c2: here(kSmall2)
         const float u = y * inv, t = u * u;
-        return fmaf(fmaf(fmaf(-0.04965299f, t, 0.133066013f), t, -0.333328575f), t, 1.0f);
+        return fmaf(fmaf(fmaf(-0.04965299f, t, c2), t, -0.333328575f), t, 1.0f);
     }
     // y within +-most (which makes a number of NaN)
     __device__ __forceinline__ float within(float y) const { return __builtin_amdgcn_fmed3f(y, -most, most); }
-    __device__ __forceinline__ float factor(float y) const {
+    __device__ __forceinline__ float factor(float y, float p3, float q3) const {   // here(kP3), here(kQ3)
         const float u = y * inv, t = u * u;
-        const float p = fmaf(fmaf(fmaf(fmaf(1.39620733e-8f, t, 2.10437538e-5f), t, 3.52193834e-3f), t, 0.134032145f), t, 1.0f);
-        const float q = fmaf(fmaf(fmaf(fmaf(8.02389081e-7f, t, 3.32875614e-4f), t, 2.59772241e-2f), t, 0.467365384f), t, 1.0f);
+        const float p = fmaf(fmaf(fmaf(fmaf(1.39620733e-8f, t, p3), t, 3.52193834e-3f), t, 0.134032145f), t, 1.0f);
+        const float q = fmaf(fmaf(fmaf(fmaf(8.02389081e-7f, t, q3), t, 2.59772241e-2f), t, 0.467365384f), t, 1.0f);
         return p * __builtin_amdgcn_rcpf(q);
     }
     __device__ __forceinline__ float operator()(float y) const {
         const float x = within(y);
-        return x * factor(x);
+        return x * factor(x, kP3, kQ3);
     }
+    static constexpr float kSmall2 = 0.133066013f, kP3 = 2.10437538e-5f, kQ3 = 3.32875614e-4f;
 };
 
 // Layout of a tile: W channels (a multiple of 32) in rows of a power of two of pieces.
@@ -339,13 +348,15 @@ struct FlashRow {
         if constexpr (!CAP) {
             weigh_all([&](float v, float of) { return __builtin_amdgcn_exp2f(fmaf(v, of, base)); });
         } else if (__builtin_amdgcn_ballot_w64(!(size <= cap.small)) == 0) {
+            const float c2 = cap.here(cap.kSmall2);
             weigh_all([&](float v, float of) {
-                const float y = v * of, w = __builtin_amdgcn_exp2f(fmaf(y, cap.small_factor(y), base));
+                const float y = v * of, w = __builtin_amdgcn_exp2f(fmaf(y, cap.small_factor(y, c2), base));
                 return MASKED && v == -__builtin_huge_valf() ? 0.0f : w;   // (the cap of what is not seen is no score)
             });
         } else {
+            const float p3 = cap.here(cap.kP3), q3 = cap.here(cap.kQ3);
             weigh_all([&](float v, float of) {
-                const float y = cap.within(v * of), w = __builtin_amdgcn_exp2f(fmaf(y, cap.factor(y), base));
+                const float y = cap.within(v * of), w = __builtin_amdgcn_exp2f(fmaf(y, cap.factor(y, p3, q3), base));
                 return MASKED && v == -__builtin_huge_valf() ? 0.0f : w;
             });
         }

@@ -270,7 +270,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
     }
     const FlashCap cap(CAP ? a.softcap : 1.0f);
 
-    constexpr int kAhead = W <= 128 ? 2 : 0;
+    constexpr int kAhead = W <= 128 && !CAP ? 2 : 0;   // (capped scores need the registers)
     FlashTurn<W, KEYS, kAhead> s;
     int value_e = 27;        // the exponent of the values that are weighed, and of all before
     uint32_t odd = 0;        // bit 0 (1): a value of the 8-bit (4-bit) group that the row sees is not finite

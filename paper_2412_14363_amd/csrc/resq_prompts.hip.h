@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
     const FlashCap cap(CAP ? a.softcap : 1.0f);
 
     // ---- Two groups of wavefronts, one of each to a SIMD, half a tile apart: while one is at the matrix cores the other is at the vector ALU. ----
-    constexpr int kAhead = W <= 64 || W > 128 ? 0 : KEYS / 16;
+    constexpr int kAhead = W <= 64 || W > 128 ? 0 : CAP ? 2 : KEYS / 16;   // (capped scores need the registers)
     FlashTurn<W, KEYS, kAhead> s;
     auto keys_in = [&](int n) { return lds + n % 3 * kTileBytes; };
     auto values_in = [&](int n) { return lds + (3 + n % 3) * kTileBytes; };

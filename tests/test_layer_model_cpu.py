@@ -37,6 +37,7 @@ def source(name):
             (r'asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");', wait(0)),
             (r'asm volatile("s_waitcnt lgkmcnt(0)\n\ts_setprio 0\n\ts_barrier" ::: "memory");', "model::barrier();"),
             (r'asm volatile("s_waitcnt lgkmcnt(0)\n\ts_setprio 3\n\ts_barrier" ::: "memory");', "model::barrier();"),
+            ('asm volatile("" : "+v"(x));', ""),
             (r'asm volatile("s_waitcnt vmcnt(%0)\n\ts_setprio 3\n\ts_barrier" ::"n"(LATER) : "memory");', wait("LATER"))])
         assert "asm volatile" not in text
     return text

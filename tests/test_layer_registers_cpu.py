@@ -1,0 +1,89 @@
+"""What the kernels around a layer's products keep in scratch memory, from their machine code: reads of it wait for the tiles that are on their way
+to LDS, so that a loop over tiles must have none."""
+import re
+import subprocess
+
+import pytest
+
+from test_kernel_code_cpu import OBJDUMP
+from test_layer_code_cpu import code_objects, numbers   # noqa: F401
+
+
+def loops_of(code):
+    """(matrix instructions, accesses of scratch memory) of each loop with matrix instructions in [(address, instruction)]: of instructions that
+    lead to each other"""
+    at, behind = {a: n for n, (a, _) in enumerate(code)}, [[] for _ in code]
+    for n, (a, op) in enumerate(code):
+        m = re.match(r"s_(c?)branch\S*\s+(\d+)$", op)
+        if m:   # in words from the next instruction
+            behind[n].append(at[a + 4 + 4 * (int(m[2]) - (65536 if int(m[2]) > 32767 else 0))])
+        if n + 1 < len(code) and not (m and not m[1]) and op.split()[0] not in ("s_endpgm", "s_setpc_b64"):
+            behind[n].append(n + 1)
+    before = [[] for _ in code]
+    for n, to in enumerate(behind):
+        for k in to:
+            before[k].append(n)
+    done, order = set(), []
+    for start in range(len(code)):   # by the time that all behind an instruction have been seen
+        todo = [] if start in done else [(start, iter(behind[start]))]
+        done.add(start)
+        while todo:
+            n, rest = todo[-1]
+            k = next((k for k in rest if k not in done), None)
+            if k is None:
+                order.append(todo.pop()[0])
+            else:
+                done.add(k)
+                todo.append((k, iter(behind[k])))
+    got, done = [], set()
+    for start in reversed(order):
+        body, todo = [], [] if start in done else [start]
+        done.add(start)
+        while todo:
+            body.append(todo.pop())
+            more = [k for k in before[body[-1]] if k not in done]
+            done.update(more)
+            todo += more
+        if len(body) > 1 and (products := sum("v_mfma" in code[n][1] for n in body)):
+            got.append((products, sum(code[n][1].startswith("scratch_") for n in body)))
+    return got
+
+
+@pytest.fixture(scope="module")
+def tile_loops(code_objects, tmp_path_factory):   # noqa: F811
+    """kernel -> loops_of() it"""
+    found = {}
+    for path in code_objects:
+        symbols = subprocess.run([OBJDUMP, "-t", str(path)], capture_output=True, text=True, check=True).stdout
+        names = sorted(set(re.findall(r"\s(_Z\w*attend_(?:prompts|prefix)_kernel\w*)$", symbols, re.M)))
+        if not names:
+            continue
+        text = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", "--disassemble-symbols=" + ",".join(names), str(path)],
+                              capture_output=True, text=True, check=True).stdout
+        for part in re.split(r"(?m)^[0-9a-f]+ <(?=_Z)", text)[1:]:
+            code = [(int(m[2], 16), m[1]) for m in re.finditer(r"^\t(.*?)\s*// ([0-9A-F]{12}):", part, re.M)]
+            found[part[:part.index(">")]] = loops_of(code)
+    assert len(found) == 20 and all(found.values())
+    return found
+
+
+def test_no_scratch_memory_in_loops_over_tiles(tile_loops):
+    for name, loops in tile_loops.items():
+        if int(re.search(r"kernelILi(\d+)E", name)[1]) < 256:
+            assert all(scratch == 0 for _, scratch in loops), (name, loops)
+
+
+def test_scratch_memory_of_each_kernel(code_objects):   # noqa: F811
+    """Bytes of a lane at most: heads up to 128 a few in front of their loops, heads up to 192 none; heads of 256 and norms of more than 16384
+    channels have more than their registers hold."""
+    most = {("prompts", 128): 48, ("prompts", 256): 448, ("prefix", 128): 8, ("prefix", 256): 448}
+    found = numbers(code_objects, r"attend_(prompts|prefix)_kernelILi(\d+)E", "private_segment_fixed_size")
+    assert len(found) == 20
+    for name, (m, (scratch,)) in found.items():
+        assert scratch <= most.get((m[1], int(m[2])), 0), (name, scratch)
+    found = numbers(code_objects, r"norm_residual_kernelILi(\d+)ELi(\d+)E", "private_segment_fixed_size")
+    assert len(found) == 14
+    for name, (m, (scratch,)) in found.items():
+        assert scratch <= (104 if m[2] == "4" else 0), (name, scratch)
+    for name, (_, (scratch,)) in numbers(code_objects, r"attend_(prompts|prefix)_join_kernel", "private_segment_fixed_size").items():
+        assert scratch == 0, (name, scratch)
