@@ -612,7 +612,8 @@ int resq_attend_prompts(const void* q, int64_t ldq, int64_t ldqh, int64_t tokens
  * Attention of one new token of each sequence, as resq_attend_kv_cache, behind a PREFIX that all sequences of the batch share (the
  * instructions in front of every request, the question that many answers are tried for): the tokens of sequence b are the
  * prefix's, then lens[b] of its own (its new token the last of them).  The prefix is read and made into numbers once for 256 queries
- * of a K/V head instead of once for each sequence; results are those of resq_attend_kv_cache on tables that name both in a row.
+ * of a K/V head instead of once for each sequence; results are those of resq_attend_kv_cache on tables that name both in a row, but for the
+ * roundings below (there codes are multiplied as they are).
  *   prefix_len    int32 [1]: tokens of the prefix; what is above prefix_width * page_size (or 2^30) is read as that, below 0 as 0  (read)
  *   prefix_table  int32 [prefix_width]: its pages                                        (read)
  *   lens          int32 [B]: own tokens; 0: the prefix alone; below 0: the sequence is not there, its out is 0 and its lse -inf  (read)
