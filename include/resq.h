@@ -595,7 +595,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
  *            (tokens_k) is read as that; results of arrays that decrease are unspecified (no access leaves the tensors)  (read)
  *   lse      fp32 [tokens_q, heads_q] or null                                            (written)
  *   d_head   multiple of 8, 8 .. 256; heads_q a multiple of heads_k; 1 <= B <= 65535; tokens_q = 0 does nothing
- *   scale, softcap, window   as resq_attend_kv_cache; a capped score is off by 2^-20 of itself at most beside what it was before
+ *   scale, softcap, window   as resq_attend_kv_cache; a capped score is off by 2^-19.9 of itself at most beside what it was before
  *   tokens_q, tokens_k <= 2^30, tokens_q * heads_q < 2^31 - 65536; ldk, ldv < 2^24 (of one key: any)
  *   workspace  device memory, 256-byte aligned, resq_attend_prompts_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents
  *            meaningless before and after; calls that overlap (different streams) need one each

@@ -85,38 +85,42 @@ __device__ __forceinline__ void flash_after_softmax() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// A capped score in base 2: B tanh(y / B) = y f(t), t = (y / B)^2, B = cap log2 e, off by a few roundings of itself (2^-20 at most) however
+// A capped score in base 2: B tanh(y / B) = y f(t), t = (y / B)^2, B = cap log2 e, off by a few roundings of itself (2^-19.9 at most) however
 // large the cap is, where 1 - 2 / (1 + e^(2 y / B)) would be off by 2^-21 of the cap.  f is P / Q, fitted for the least relative error up to
 // |y| = 8.7 B, from where on y f is B to fp32 (2^-25.9; all terms are positive, so that nothing cancels), or where a wavefront's scores of
-// a tile are all within 0.33 B, as scores below a cap mostly are, a polynomial (2^-25.2).  Measured on MI355X, 24 ragged prompts of heads of 64:
-// 194 us, 259 by P / Q everywhere, 182 by the exponential and its reciprocal; 8192 tokens, heads of 128, 688 with all scores within 0.33 B, 928 with
-// larger ones in every tile, 669 by the exponential.
+// a tile are all within 0.33 B, as scores below a cap mostly are, a polynomial (2^-25.2).  Measured on MI355X: 24 ragged prompts of heads of 64
+// 179 us, 259 by P / Q everywhere, 175 by the exponential and its reciprocal; 8192 tokens, heads of 128, 647 with all scores within 0.33 B, 855 with
+// larger ones in every tile, 660 by the exponential.
+// UNIT: of products that make y = unit x, one unit for all, which is then in the numerators; else of y itself.
+template <bool UNIT>
 struct FlashCap {
-    float most, small, inv;   // 8.7 B, 0.33 B, and 1 / B, in scalar registers
-    __device__ __forceinline__ explicit FlashCap(float cap)
-        : most(scalar(fminf(12.5514472f * cap, 3.4028235e38f))), small(scalar(0.47608936f * cap)), inv(scalar(0.69314718055994530942f / cap)) {}
+    float unit, most, small, inv;   // 8.7 B, 0.33 B and 1 / B, for UNIT of x, in scalar registers
+    __device__ __forceinline__ FlashCap(float cap, float unit_)
+        : unit(scalar(unit_)), most(scalar(fminf(12.5514472f * cap / unit, 3.4028235e38f))), small(scalar(0.47608936f * cap / unit)),
+          inv(scalar(fminf(0.69314718055994530942f / cap * unit, 3.4028235e38f))) {}
     __device__ static __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
     // A constant in a vector register from here on: kept over a loop it would take another's place, which goes to scratch memory, and reads of
-    // that wait for tiles on their way to LDS (8192 tokens, heads of 128, 1016 us for 688; 200 queries over 30001 tokens 723 for 658).
+    // that wait for tiles on their way to LDS (a few of them there: 8192 tokens, heads of 128, 1016 us for 688; 200 queries over 30001 tokens 723 for 658).
     __device__ static __forceinline__ float here(float x) {
         asm volatile("" : "+v"(x));
         return x;
     }
-    __device__ __forceinline__ float small_factor(float y, float c2) const {   // c2: here(kSmall2)
+    __device__ __forceinline__ float of(float c) const { return UNIT ? scalar(unit * c) : c; }
+    __device__ __forceinline__ float small_factor(float y, float c2) const {   // c2: here(of(kSmall2))
         const float u = y * inv, t = u * u;
-        return fmaf(fmaf(fmaf(-0.04965299f, t, c2), t, -0.333328575f), t, 1.0f);
+        return fmaf(fmaf(fmaf(of(-0.04965299f), t, c2), t, of(-0.333328575f)), t, of(1.0f));
     }
     // y within +-most (which makes a number of NaN)
     __device__ __forceinline__ float within(float y) const { return __builtin_amdgcn_fmed3f(y, -most, most); }
-    __device__ __forceinline__ float factor(float y, float p3, float q3) const {   // here(kP3), here(kQ3)
+    __device__ __forceinline__ float factor(float y, float p3, float q3) const {   // here(of(kP3)), here(kQ3)
         const float u = y * inv, t = u * u;
-        const float p = fmaf(fmaf(fmaf(fmaf(1.39620733e-8f, t, p3), t, 3.52193834e-3f), t, 0.134032145f), t, 1.0f);
+        const float p = fmaf(fmaf(fmaf(fmaf(of(1.39620733e-8f), t, p3), t, of(3.52193834e-3f)), t, of(0.134032145f)), t, of(1.0f));
         const float q = fmaf(fmaf(fmaf(fmaf(8.02389081e-7f, t, q3), t, 2.59772241e-2f), t, 0.467365384f), t, 1.0f);
         return p * __builtin_amdgcn_rcpf(q);
     }
     __device__ __forceinline__ float operator()(float y) const {
         const float x = within(y);
-        return x * factor(x, kP3, kQ3);
+        return x * factor(x, of(kP3), kQ3);
     }
     static constexpr float kSmall2 = 0.133066013f, kP3 = 2.10437538e-5f, kQ3 = 3.32875614e-4f;
 };
@@ -297,38 +301,46 @@ struct FlashRow {
     // Weights of the tile at hand; MASKED: there may be scores of -inf.  unit, not negative: what makes a product a score of base 2, one for all
     // or UNITS for as many parts of the tile.
     template <int KEYS, bool CAP, bool MASKED, int AHEAD, int UNITS>
-    __device__ __forceinline__ void softmax(FlashTurn<W, KEYS, AHEAD>& s, const float (&unit)[UNITS], const FlashCap& cap) {
+    __device__ __forceinline__ void softmax(FlashTurn<W, KEYS, AHEAD>& s, const float (&unit)[UNITS], const FlashCap<UNITS == 1>& cap) {
         constexpr float kBias = F16 ? kFlashHalfBias : 0.0f, kSlack = F16 ? kFlashHalfSlack : kFlashSlack;
         constexpr int kOf = KEYS / 2 / UNITS;   // numbers of a lane that share a unit
+        constexpr bool kOwnUnit = CAP && UNITS == 1;   // the cap has it
         auto& x = s.x;
-        // the largest magnitude of what is seen, or NaN, which capping would lose and the sum keeps
-        auto larger = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
-        auto size_of = [](float v) { return MASKED && v == -__builtin_huge_valf() ? 0.0f : fabsf(v); };
-        // ---- the running maximum, where a score is 2^kSlack times what it allows ----
-        float top, size = 0.0f;
+        // the largest of what each unit's numbers are, that all make a score of
+        auto most_of = [&](auto number, auto larger) __attribute__((always_inline)) {
+            float most;
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            float tops[2] = {x[kOf * u >> 4][kOf * u & 15], x[kOf * u >> 4][(kOf * u & 15) + 1]}, sizes[2] = {size_of(tops[0]), size_of(tops[1])};
+            for (int u = 0; u < UNITS; ++u) {
+                float tops[2] = {number(x[kOf * u >> 4][kOf * u & 15]), number(x[kOf * u >> 4][(kOf * u & 15) + 1])};
 #pragma unroll
-            for (int i = kOf * u + 2; i < kOf * u + kOf; ++i) {
-                tops[i & 1] = fmaxf(tops[i & 1], x[i >> 4][i & 15]);
-                if (CAP) sizes[i & 1] = larger(sizes[i & 1], size_of(x[i >> 4][i & 15]));
+                for (int i = kOf * u + 2; i < kOf * u + kOf; ++i) tops[i & 1] = larger(tops[i & 1], number(x[i >> 4][i & 15]));
+                const float top = larger(tops[0], tops[1]) * (kOwnUnit ? 1.0f : unit[u]);
+                most = u == 0 ? top : larger(most, top);
             }
-            const float most = fmaxf(tops[0], tops[1]) * unit[u];
-            top = u == 0 ? most : fmaxf(top, most);
-            if (CAP) size = larger(size, larger(sizes[0], sizes[1]) * unit[u]);
-        }
-        if constexpr (CAP) {
-            l = size == size ? l : size;
-            top = cap(top);
-        }
-        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+            return most;
+        };
+        auto top_of = [&]() __attribute__((always_inline)) { return most_of([](float v) { return v; }, [](float a, float b) { return fmaxf(a, b); }); };
+        auto raise = [&](float top) __attribute__((always_inline)) {
             const float m_new = fmaxf(m, halves_max(top));
             const float back = __builtin_amdgcn_exp2f(m - m_new);
             m = m_new;
             l *= back;
 #pragma unroll
             for (int c = 0; c < Tile::kBlocks; ++c) acc[c] *= back;
+        };
+        // ---- the running maximum, where a score is 2^kSlack times what it allows ----
+        float size = 0.0f;   // the largest magnitude of what is seen, or NaN, which capping would lose and the sum keeps
+        if constexpr (CAP) {
+            size = most_of([](float v) { return MASKED && v == -__builtin_huge_valf() ? 0.0f : fabsf(v); },
+                           [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
+            l = size == size ? l : size;
+            if (__builtin_amdgcn_ballot_w64(!(size * (kOwnUnit ? cap.unit : 1.0f) <= m + kSlack)) != 0) {
+                const float top = cap(top_of());
+                if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) raise(top);
+            }
+        } else {
+            const float top = top_of();
+            if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) raise(top);
         }
         // ---- weights, rounded once as the product's operand (their sum is taken unrounded) ----
         const float base = kBias - m;
@@ -348,15 +360,15 @@ struct FlashRow {
         if constexpr (!CAP) {
             weigh_all([&](float v, float of) { return __builtin_amdgcn_exp2f(fmaf(v, of, base)); });
         } else if (__builtin_amdgcn_ballot_w64(!(size <= cap.small)) == 0) {
-            const float c2 = cap.here(cap.kSmall2);
+            const float c2 = cap.here(cap.of(cap.kSmall2));
             weigh_all([&](float v, float of) {
-                const float y = v * of, w = __builtin_amdgcn_exp2f(fmaf(y, cap.small_factor(y, c2), base));
+                const float y = kOwnUnit ? v : v * of, w = __builtin_amdgcn_exp2f(fmaf(y, cap.small_factor(y, c2), base));
                 return MASKED && v == -__builtin_huge_valf() ? 0.0f : w;   // (the cap of what is not seen is no score)
             });
         } else {
-            const float p3 = cap.here(cap.kP3), q3 = cap.here(cap.kQ3);
+            const float p3 = cap.here(cap.of(cap.kP3)), q3 = cap.here(cap.kQ3);
             weigh_all([&](float v, float of) {
-                const float y = cap.within(v * of), w = __builtin_amdgcn_exp2f(fmaf(y, cap.factor(y, p3, q3), base));
+                const float y = cap.within(kOwnUnit ? v : v * of), w = __builtin_amdgcn_exp2f(fmaf(y, cap.factor(y, p3, q3), base));
                 return MASKED && v == -__builtin_huge_valf() ? 0.0f : w;
             });
         }

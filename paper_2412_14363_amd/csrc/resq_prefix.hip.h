@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void attend_prefix_kernel(const 
                 r.q[s][i] = flash_pack<true>(__uint_as_float(r.q[s][i] << 16) * f, __uint_as_float(r.q[s][i] & 0xFFFF0000u) * f);
         qf = a.scale * two_to(e - 13) * 1.44269504088896340736f;
     }
-    const FlashCap cap(CAP ? a.softcap : 1.0f);
+    const FlashCap<false> cap(CAP ? a.softcap : 1.0f, 1.0f);
 
     constexpr int kAhead = W <= 128 && !CAP ? 2 : 0;   // (capped scores need the registers)
     FlashTurn<W, KEYS, kAhead> s;

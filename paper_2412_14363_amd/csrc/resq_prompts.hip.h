@@ -24,7 +24,7 @@
 // 46 % of all cycles, LDS banks never in conflict.  2048 tokens 66 us: the last workgroup has all 32 tiles of keys, at 2 us each, when half of
 // the compute units are idle; cut in two 91, for a workgroup's way to its first product is 7 us and results of parts take another pass.
 // On the way, at 8192 tokens: tiles through registers and masks everywhere 1649 us; tiles straight to LDS, whole ones in a loop without
-// masks, maxima that rise only when they must 585; the two groups 526-548.  24 ragged prompts of heads of 64 with window and cap 194 us,
+// masks, maxima that rise only when they must 585; the two groups 526-548.  24 ragged prompts of heads of 64 with window and cap 179 us,
 // three chunks of up to 300 tokens behind up to 30000 316, of which the join is 16 (28 with one part's loads at a time).
 #pragma once
 #include <hip/hip_runtime.h>
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
     r.clear();
     const float inf = __builtin_huge_valf();
     const float factor = a.scale * 1.44269504088896340736f;
-    const FlashCap cap(CAP ? a.softcap : 1.0f);
+    const FlashCap<true> cap(CAP ? a.softcap : 1.0f, factor);
 
     // ---- Two groups of wavefronts, one of each to a SIMD, half a tile apart: while one is at the matrix cores the other is at the vector ALU. ----
     constexpr int kAhead = W <= 64 || W > 128 ? 0 : CAP ? 2 : KEYS / 16;   // (capped scores need the registers)
@@ -277,8 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void attend_prompts_kernel(const P
                     if (ch < d) x = fmaf(of_q, bf16_bits_to_f32(k[ch]), x);
                 }
             x = halves_sum(x);
-            x *= factor;
-            if (CAP) x = cap(x);
+            x = CAP ? cap(x) : x * factor;
             if ((unsigned)(own - key) >= (unsigned)a.window) continue;
             const float w = __builtin_amdgcn_exp2f(x - r.m);
 #pragma unroll

@@ -42,14 +42,14 @@ def test_prompts_lengths_that_decrease_beyond_32_bits(rq):   # noqa: F811
 
 
 # ---- capped scores ------------------------------------------------------------------------------------
-# Off by 2^-20 of themselves at most: two polynomials of four steps with terms of one sign, a roundings' 2^-24 for each (8), the reciprocal's last
-# place (2) and the quotient's rounding (1), the argument's square, seven roundings of which at most half reach the quotient (3.5), and
-# the fit (0.3): 14.8 roundings.  A weight is off by twice that.
+# Off by 2^-19.9 of themselves at most: two polynomials of four steps with terms of one sign, a rounding of 2^-24 for each (8), one of the
+# numerator's constants, the reciprocal's last place (2) and the quotient's rounding (1), the argument's square, nine roundings of which at most
+# half reach the quotient (4.5), and the fit (0.3): 16.8 roundings.  A weight is off by twice that.
 
 def capped(want, exact, most):
     """(results with the cap, bounds): those without it, in whose place the cap puts its own error and no other; scores below `most`."""
     out, lse, tol, tol_lse = want
-    off = 2.0 ** -20 * most
+    off = 2.0 ** -19.9 * most
     return out, lse, tol + 2 * off * exact, tol_lse + off
 
 
@@ -96,7 +96,7 @@ def test_log_sum_exps_of_one_capped_score(rq, d, cap):   # noqa: F811
     # roundings of m ln 2, 5.6 of which x does not account for (2^-20.5): 2^-19.3
     off = d * 2.0 ** -24 * size + 2.0 ** -22 * x.abs()
     through = torch.maximum(cap * torch.tanh((x + off) / cap) - want, want - cap * torch.tanh((x - off) / cap))
-    tol = through + (2.0 ** -20 + 2.0 ** -22) * want.abs() + 2.0 ** -19.3
+    tol = through + (2.0 ** -19.9 + 2.0 ** -22) * want.abs() + 2.0 ** -19.3
     over = (lse.cpu().double() - want).abs() - tol
     assert bool((over <= 0).all()), (float(over.max()), float(cap))
 
