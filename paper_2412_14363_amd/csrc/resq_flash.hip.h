@@ -95,9 +95,19 @@ __device__ __forceinline__ void flash_after_softmax() {
 template <bool UNIT>
 struct FlashCap {
     float unit, most, small, inv;   // 8.7 B, 0.33 B and 1 / B, for UNIT of x, in scalar registers
-    __device__ __forceinline__ FlashCap(float cap, float unit_)
-        : unit(scalar(unit_)), most(scalar(fminf(12.5514472f * cap / unit, 3.4028235e38f))), small(scalar(0.47608936f * cap / unit)),
-          inv(scalar(fminf(0.69314718055994530942f / cap * unit, 3.4028235e38f))) {}
+    __device__ __forceinline__ FlashCap(float cap, float unit_) : unit(scalar(unit_)) {
+        most = 12.5514472f * cap;
+        small = 0.47608936f * cap;
+        inv = 0.69314718055994530942f / cap;
+        if constexpr (UNIT) {
+            most /= unit;
+            small /= unit;
+            inv = fminf(inv * unit, 3.4028235e38f);
+        }
+        most = scalar(fminf(most, 3.4028235e38f));
+        small = scalar(small);
+        inv = scalar(inv);
+    }
     __device__ static __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
     // A constant in a vector register from here on: kept over a loop it would take another's place, which goes to scratch memory, and reads of
     // that wait for tiles on their way to LDS (a few of them there: 8192 tokens, heads of 128, 1016 us for 688; 200 queries over 30001 tokens 723 for 658).
