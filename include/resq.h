@@ -587,8 +587,8 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
  * Weights go into the products rounded to bf16 (off by 2^-8 of each at most), sums are fp32.  Where a query sees no key (more queries than keys) out is 0
  * and lse -inf.  What a query does not see has no part in its result, infinities and NaN neither.  (Infinities in a query or in
  * keys that it sees may make NaN of its result.)
- *   q, out   bf16 [tokens_q, heads_q, d_head] with strides (ldq, ldqh), (ldo, ldoh); rows of out do not overlap; rows outside of the
- *            sequences are left as they were                                             (read / written)
+ *   q, out   bf16 [tokens_q, heads_q, d_head] with strides (ldq, ldqh), (ldo, ldoh); rows of out do not overlap, out may be q with the
+ *            same strides, else it lies on no other tensor of the call; rows outside of the sequences are left as they were  (read / written)
  *   k, v     bf16 [tokens_k, heads_k, d_head] with strides (ldk, ldkh), (ldv, ldvh): views of a projection's output, or what
  *            resq_gather_kv_cache wrote                                                  (read)
  *   cu_q, cu_k  int32 [B + 1], not decreasing, from resq_kv_slots' cu_tokens; may be one array.  What is below 0 or above tokens_q
@@ -596,7 +596,7 @@ int resq_attend_kv_cache(const void* q, int64_t ldq, int64_t ldqh, int64_t B, in
  *   lse      fp32 [tokens_q, heads_q] or null                                            (written)
  *   d_head   multiple of 8, 8 .. 256; heads_q a multiple of heads_k; 1 <= B <= 65535; tokens_q = 0 does nothing
  *   scale, softcap, window   as resq_attend_kv_cache; a capped score is off by 2^-19.9 of itself at most beside what it was before
- *   tokens_q, tokens_k <= 2^30, tokens_q * heads_q < 2^31 - 65536; ldk, ldv < 2^24 (of one key: any)
+ *   tokens_q, tokens_k <= 2^30, tokens_q * heads_q + 255 B heads_k < 2^31, the first of both < 2^31 - 65536; ldk, ldv < 2^24 (of one key: any)
  *   workspace  device memory, 256-byte aligned, resq_attend_prompts_workspace_bytes bytes (else RESQ_ERR_BUFFER); contents
  *            meaningless before and after; calls that overlap (different streams) need one each
  * Alignment: k and v 16 bytes, their strides multiples of 8 (else RESQ_ERR_ALIGN); the others their elements'.
@@ -647,7 +647,7 @@ int resq_attend_kv_prefix(const void* q, int64_t ldq, int64_t ldqh, int64_t B, i
  *            h_out may be h and x may be y, with the same strides; else outputs lie on no other tensor of the call, and rows of
  *            an output do not overlap.  h_out or x may be null (not both): not written, w_pre is not read without x
  *   w_pre, w_post  bf16 [width]; w_offset 0, or 1 for weights that are stored as their distance from 1             (read)
- *   width    1 .. 32768; tokens = 0 does nothing; eps >= 0; w_offset, alpha finite; gate and w_post need y
+ *   width    1 .. 32768; tokens < 2^22 (more of narrow rows), 0 does nothing; eps >= 0; w_offset, alpha finite; gate and w_post need y
  * Alignment: that of the elements; rows of whole 16-byte pieces are the fastest.
  */
 int resq_norm_residual(const void* y, int64_t ldy, const void* gate, int64_t ldg, const void* h, int64_t ldh, int h_is_fp32, int64_t tokens,
