@@ -89,8 +89,8 @@ __device__ __forceinline__ void flash_after_softmax() {
 // large the cap is, where 1 - 2 / (1 + e^(2 y / B)) would be off by 2^-21 of the cap.  f is P / Q, fitted for the least relative error up to
 // |y| = 8.7 B, from where on y f is B to fp32 (2^-25.9; all terms are positive, so that nothing cancels), or where a wavefront's scores of
 // a tile are all within 0.33 B, as scores below a cap mostly are, a polynomial (2^-25.2).  Measured on MI355X: 24 ragged prompts of heads of 64
-// 179 us, 259 by P / Q everywhere, 175 by the exponential and its reciprocal; 8192 tokens, heads of 128, 647 with all scores within 0.33 B, 855 with
-// larger ones in every tile, 660 by the exponential.
+// 185 us, 259 by P / Q everywhere, 177 by the exponential and its reciprocal; 8192 tokens, heads of 128, 662 with all scores within 0.33 B, 885 with
+// larger ones in every tile, 666 by the exponential.
 // UNIT: of products that make y = unit x, one unit for all, which is then in the numerators; else of y itself.
 template <bool UNIT>
 struct FlashCap {

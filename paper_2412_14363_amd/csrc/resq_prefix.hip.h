@@ -13,9 +13,10 @@
 // tile, and of the values of all tokens so far.  What is below 2^-27 of the largest number there loses bits, down to 2^-38 of it.
 //
 // What bounds it is the vector ALU: 600 instructions of a wavefront to a tile, more than half of them from codes to numbers, of which a turn
-// is made of some 4200 cycles; the matrix cores' turn takes 2050, 1536 of them products.  Measured on MI355X (all four kernels of a
-// call, the own tokens' attention and the joins beside this one): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 507 us,
-// 390 TFLOP/s; 64 of 32 heads over 8192 62 us, 31 of them here; 4 over 1000 27 us, 13 here, the latency of page, row and result.  On the way, at
+// is made of some 4200 cycles (of values) to 4800 (of keys); the matrix cores' turn takes 2100, 1536 of them products.  Measured on MI355X (all four kernels of a
+// call, the own tokens' attention and the joins beside this one): 200 queries of 64 heads over 30001 tokens, 8 K/V heads of 128: 508 us,
+// 390 TFLOP/s (capped 637); 64 of 32 heads over 8192 62 us, 31 of them here; 4 over 1000 27 us, 13 here, the latency of page, row and result; 64 of 16 heads on 8 over
+// 8192, heads of 192 70 us, of 256, for which registers do not suffice, 171.  On the way, at
 // 200 queries: loads in branches, each of which waited for all before it, 842 us; without 732; places of a piece made anew in place of kept in
 // scratch memory 577; factors of the keys in the softmax's own multiplications 464; keys in two numbers 525, the join by a wavefront to a query 507.  Loads made in the other
 // turn, at the matrix cores, where there is time: 468 for 464, they come too late then.

@@ -7,7 +7,7 @@
 // that a tile of keys and values in LDS serves all of them, and tiles on the diagonal are few (with four heads to a K/V head 256 rows are
 // 64 queries).  Keys and values come straight to LDS in tiles of 64 (32 for heads above 128), two tiles ahead, three of each in LDS.  The
 // wavefronts are two groups half a tile apart: while one has the matrix cores, which a tile's products keep busy for 1024 cycles of a
-// wavefront, the other makes weights of its scores (1200 cycles) and asks for tiles (430).  Heads of 64 and less take four wavefronts and
+// wavefront, the other makes weights of its scores and asks for tiles (1000 cycles).  Heads of 64 and less take four wavefronts and
 // three workgroups to a compute unit, which find each other's gaps by themselves.
 //
 // Weights are rounded to bf16 for the second product, which takes the values as they are: a result, rounded to bf16 itself, is then off by 1.7 10^-3 of
@@ -18,14 +18,15 @@
 // that are infinite or NaN are left out of the masked tiles' products (0 times them is NaN) and given to the rows that see them, one by one,
 // at the end.  Where there are fewer workgroups than compute units the keys are cut into parts, and a second kernel joins them.
 //
-// What bounds it: the matrix turn, 1750 to 2150 cycles where its products are 1024, that is LDS, 48 reads of a wavefront in each turn; and on
+// What bounds it: the matrix turn, 2020 cycles where its products are 1024, that is LDS, 48 reads of a wavefront in each turn; and on
 // large calls the power limit (products of random numbers alone run at 1.6 GHz).  Measured on MI355X: 8192 tokens, 32 heads on 8 of 128
-// 526-548 us, 1.0 PFLOP/s of the pairs that are seen, where a plain product of 8192 x 8192 x 8192 reaches 1.3; the matrix cores are busy
+// 528-550 us, 1.0 PFLOP/s of the pairs that are seen, where a plain product of 8192 x 8192 x 8192 reaches 1.3; the matrix cores are busy
 // 46 % of all cycles, LDS banks never in conflict.  2048 tokens 66 us: the last workgroup has all 32 tiles of keys, at 2 us each, when half of
 // the compute units are idle; cut in two 91, for a workgroup's way to its first product is 7 us and results of parts take another pass.
 // On the way, at 8192 tokens: tiles through registers and masks everywhere 1649 us; tiles straight to LDS, whole ones in a loop without
-// masks, maxima that rise only when they must 585; the two groups 526-548.  24 ragged prompts of heads of 64 with window and cap 179 us,
-// three chunks of up to 300 tokens behind up to 30000 316, of which the join is 16 (28 with one part's loads at a time).
+// masks, maxima that rise only when they must 585; the two groups 528-550.  24 ragged prompts of heads of 64 with window and cap 189-192
+// us, three chunks of up to 300 tokens behind up to 30000 316, of which the join is 11 (28 with one part's loads at a time).  Heads of 192 238 for 4096
+// tokens of 16 heads on 8, 430 TFLOP/s; of 256, for which registers do not suffice, 689, 200.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
