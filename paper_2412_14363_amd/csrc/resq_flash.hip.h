@@ -96,16 +96,13 @@ template <bool UNIT>
 struct FlashCap {
     float unit, most, small, inv;   // 8.7 B, 0.33 B and 1 / B, for UNIT of x, in scalar registers
     __device__ __forceinline__ FlashCap(float cap, float unit_) : unit(scalar(unit_)) {
-        most = 12.5514472f * cap;
-        small = 0.47608936f * cap;
         inv = 0.69314718055994530942f / cap;
         if constexpr (UNIT) {
-            most /= unit;
-            small /= unit;
             inv = fminf(inv * unit, 3.4028235e38f);
+            cap /= unit;
         }
-        most = scalar(fminf(most, 3.4028235e38f));
-        small = scalar(small);
+        most = scalar(fminf(12.5514472f * cap, 3.4028235e38f));
+        small = scalar(0.47608936f * cap);
         inv = scalar(inv);
     }
     __device__ static __forceinline__ float scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }

@@ -178,3 +178,4 @@ def test_caps_of_any_size(layer):
     check(layer, [prompt([(70, 40)], 2, 1, 64, window=w, cap=cap, scale=1.0) for cap in caps for w in (0, 50)], PROMPTS, SUMS)   # scores of up to 100
     check(layer, [prefix(130, [0, 30], 2, 1, 64, 8, 16, cap=cap) for cap in caps], PREFIX, SUMS)
     check(layer, [prompt([(70, 40)], 2, 1, 64, cap=1.2e-38, scale=scale) for scale in (1e-6, 50.0)], PROMPTS, SUMS)
+    check(layer, [prompt([(70, 40)], 2, 1, 64, cap=3.4e38, scale=scale) for scale in (1e-6, 2.0)], PROMPTS, SUMS)
